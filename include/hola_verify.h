@@ -107,6 +107,7 @@ typedef struct hola_wmix {
 #define HOLA_FLAG_BAD_UNIFORM 2u /* a uniform outside [0,1): clamped into [0, 1 - 2^-24]                     */
 #define HOLA_FLAG_TIMEOUT 4u     /* an on-chip wait ran out of iterations; outputs of this call are invalid  */
 #define HOLA_FLAG_R_ZERO 8u      /* residual mass was zero (p <= q everywhere): token drawn from p instead   */
+#define HOLA_FLAG_BAD_LOGIT 32u  /* hola_token_logprobs: a row of logits holds NaN or +inf                     */
 
 /* Bits of hola_verify_args::flags. */
 #define HOLA_ARG_CLEAR_STATUS 1 /* the call stores 0 to status_word before it OR-s anything in, so the caller need not  */
@@ -282,6 +283,48 @@ hola_status hola_accept_sample(hola_ctx* ctx, const hola_verify_args* args, void
  * are safe, but two calls that overlap on the GPU (issued on different streams, say) race on it and give
  * wrong entropy / logZ.  Serialise them. */
 hola_status hola_lm_head_entropy_static(const hola_verify_args* args, void* cuda_stream);
+
+/* Log probabilities of given tokens under rows of logits in memory, with their ranks, each row's entropy and its most probable
+ * entries.  The paper has no counterpart; it is what a server hands to its clients beside the tokens that a verify call
+ * emitted (logits_out, logZ of that call), and how a text is scored.  Per row r and token x:
+ *   logprob = l[r][x] - logZ[r],  logZ = ln sum_v e^l[r][v],  entropy = -sum p ln p in nats,
+ *   rank    = entries that come before x in the order (logit descending, id ascending): 0 for the arg-max, and top_ids[rank] = x,
+ *   top     = the first n_top entries in that order.
+ * Everything is held in fp32 (16-bit logits are exact in it).  A token of -1 is none: logprob 0, rank -1.  Any other token outside
+ * [0, V): logprob NaN, rank -1, HOLA_FLAG_BAD_TOKEN.  Entries of -inf have probability 0.  Where nothing else is in a row: logZ and
+ * every logprob -inf, entropy 0.  A row that holds NaN or +inf has no distribution: its outputs are NaN, ids and ranks -1, and
+ * HOLA_FLAG_BAD_LOGIT is set (where the row is read, that is, and except the log probabilities under a given logZ).
+ * Emitted form (accept_len given; tokens must be null then, T = 1 and logZ_in is required): rows are the k + 1 positions of
+ * rows / (k + 1) sequences behind a verify call.  Position j holds draft_tok[b][j] for j < accept_len[b] and next_tok[b] for
+ * j = accept_len[b].  Rows behind that are not read: logprob 0, rank and ids -1, top_logprobs 0.
+ * With logZ_in the row's sums are not made (entropy and logZ must be null); with neither rank nor n_top the tokens' entries are
+ * all that is read.  Ranks of more than four tokens per row take a pass over the logits for every four.
+ * Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing, needs no context,
+ * and launched like hola_verify (programmatic stream serialization, waits before it reads). */
+typedef enum { HOLA_L_F32 = 0, HOLA_L_BF16 = 1, HOLA_L_F16 = 2 } hola_l_dtype;
+typedef struct hola_logprobs_args {
+  int32_t rows;             /* >= 0                                                                       */
+  int32_t V;                /* entries per row, >= 1                                                      */
+  int32_t T;                /* tokens per row, >= 0                                                       */
+  int32_t n_top;            /* entries listed per row, 0 .. min(V, 32)                                    */
+  const void* logits;       /* row r starts at entry r * row_stride; any alignment of the element type    */
+  int64_t row_stride;       /* entries, >= 0                                                              */
+  int32_t l_dtype;          /* hola_l_dtype                                                               */
+  int32_t k;                /* emitted form: draft tokens per sequence                                    */
+  const int32_t* tokens;    /* [rows][T]                                                                  */
+  const int32_t* draft_tok; /* emitted form: [B][k]                                                       */
+  const int32_t* accept_len;/* emitted form: [B], 0 .. k                                                  */
+  const int32_t* next_tok;  /* emitted form: [B]                                                          */
+  const float* logZ_in;     /* [rows], optional                                                           */
+  float* logprob;           /* out [rows][T] (T > 0)                                                      */
+  int32_t* rank;            /* out [rows][T], optional                                                    */
+  float* entropy;           /* out [rows], optional                                                       */
+  float* logZ;              /* out [rows], optional                                                       */
+  int32_t* top_ids;         /* out [rows][n_top] (n_top > 0)                                              */
+  float* top_logprobs;      /* out [rows][n_top] (n_top > 0)                                              */
+  uint32_t* status_word;    /* in/out [1], optional: HOLA_FLAG_* bits are OR-ed in                        */
+} hola_logprobs_args;
+hola_status hola_token_logprobs(const hola_logprobs_args* args, void* cuda_stream);
 
 /* Quantises a bf16 W_lm [V][H] (device) to the HOLA_W_INT8 form, on the current device, asynchronously on the
  * stream: scale[v] = max_h |W[v][h]| / 127 (1 for an all-zero row), q = clip(rint(W / scale), -127, 127), evaluated in

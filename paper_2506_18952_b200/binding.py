@@ -25,12 +25,14 @@ HOLA_W_BF16, HOLA_W_INT8, HOLA_W8A8, HOLA_W8A16, HOLA_W_MIXED = 0, 1, 2, 3, 4
 HOLA_HIDDEN_IN_PLACE, HOLA_HIDDEN_ON_LINES, HOLA_HIDDEN_8BIT = 0, 1, 2
 HOLA_ARG_CLEAR_STATUS = 1
 GROUP_ROWS, SUB_BLOCK, HOLA_PACE_WORDS = 256, 128, 256
-FLAG_BAD_TOKEN, FLAG_BAD_UNIFORM, FLAG_TIMEOUT, FLAG_R_ZERO = 1, 2, 4, 8
+FLAG_BAD_TOKEN, FLAG_BAD_UNIFORM, FLAG_TIMEOUT, FLAG_R_ZERO, FLAG_BAD_LOGIT = 1, 2, 4, 8, 32
+HOLA_L_F32, HOLA_L_BF16, HOLA_L_F16 = 0, 1, 2
+HOLA_MAX_TOP = 32
 HOLA_OPT_RING_SLOTS, HOLA_OPT_ROTATING_UNITS, HOLA_OPT_HOST_OVERLAP, HOLA_OPT_HOST_ROWS_ON_DEMAND, HOLA_OPT_PASSES, HOLA_OPT_PAIR_MMA, HOLA_OPT_HOST_IN_PLACE, HOLA_OPT_CONVERTER_GROUP, HOLA_OPT_FUSED_PASSES = 1, 2, 3, 4, 5, 6, 7, 8, 9
 
 EXPORTS = ["hola_create", "hola_destroy", "hola_workspace_bytes", "hola_verify", "hola_verify_host",
            "hola_lm_head_entropy", "hola_accept_sample", "hola_host_traffic", "hola_shard_record_bytes", "hola_shard_lm_head",
-           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
+           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_token_logprobs", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
            "hola_version"]
 
 
@@ -59,6 +61,15 @@ class hola_shard_args(ctypes.Structure):
     _fields_ = [("world", ctypes.c_int32), ("rank", ctypes.c_int32), ("v_offset", ctypes.c_int32),
                 ("V_global", ctypes.c_int32), ("q_tok", ctypes.c_void_p), ("record_out", ctypes.c_void_p),
                 ("records", ctypes.c_void_p), ("mass_out", ctypes.c_void_p), ("masses", ctypes.c_void_p)]
+
+
+class hola_logprobs_args(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("V", ctypes.c_int32), ("T", ctypes.c_int32), ("n_top", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("l_dtype", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("tokens", ctypes.c_void_p), ("draft_tok", ctypes.c_void_p), ("accept_len", ctypes.c_void_p),
+                ("next_tok", ctypes.c_void_p), ("logZ_in", ctypes.c_void_p), ("logprob", ctypes.c_void_p),
+                ("rank", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("logZ", ctypes.c_void_p),
+                ("top_ids", ctypes.c_void_p), ("top_logprobs", ctypes.c_void_p), ("status_word", ctypes.c_void_p)]
 
 
 class hola_plan_info(ctypes.Structure):
@@ -107,6 +118,8 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         fn.argtypes = [ctypes.c_void_p, ctypes.POINTER(hola_verify_args), ctypes.c_void_p]
     lib.hola_lm_head_entropy_static.restype = ctypes.c_int
     lib.hola_lm_head_entropy_static.argtypes = [ctypes.POINTER(hola_verify_args), ctypes.c_void_p]
+    lib.hola_token_logprobs.restype = ctypes.c_int
+    lib.hola_token_logprobs.argtypes = [ctypes.POINTER(hola_logprobs_args), ctypes.c_void_p]
     lib.hola_quantize_w8.restype = ctypes.c_int
     lib.hola_quantize_w8.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                      ctypes.c_void_p]
@@ -295,6 +308,106 @@ def hola_lm_head_entropy_static(hidden, W_lm, logits, entropy, logZ, stream=None
     a.status_word = _dptr(status)
     _check(lib, None, lib.hola_lm_head_entropy_static(ctypes.byref(a), _stream_ptr(stream)),
            "hola_lm_head_entropy_static")
+
+
+@dataclass
+class TokenLogprobs:
+    """What hola_token_logprobs fills; the fields that were not asked for are None.  `...` is the shape of the rows."""
+    logprob: torch.Tensor | None        # fp32 [..., T], or [...] where the tokens came without that axis
+    rank: torch.Tensor | None           # int32, like logprob
+    entropy: torch.Tensor | None        # fp32 [...]
+    logZ: torch.Tensor | None           # fp32 [...]
+    top_ids: torch.Tensor | None        # int32 [..., n_top]
+    top_logprobs: torch.Tensor | None   # fp32 [..., n_top]
+
+
+_L_DTYPES = {torch.float32: HOLA_L_F32, torch.bfloat16: HOLA_L_BF16, torch.float16: HOLA_L_F16}
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Entries from one row (last axis) of `t` to the next; the rows have to lie at one distance from each other."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise HolaError("hola_token_logprobs: the entries of a row must lie side by side")
+    stride, rows = None, 1
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if stride is None:
+            stride = s
+        elif s != stride * rows:
+            raise HolaError("hola_token_logprobs: the rows must lie at one distance from each other")
+        rows *= n
+    return t.shape[-1] if stride is None else stride
+
+
+def hola_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_top: int = 0, logZ: torch.Tensor | None = None,
+                        emitted=None, want_rank: bool = True, out: TokenLogprobs | None = None, status: torch.Tensor | None = None,
+                        stream=None) -> TokenLogprobs:
+    """Log probabilities and ranks of given tokens, entropy, logZ and the `n_top` most probable entries of every row of `logits`
+    (fp32, bf16 or fp16 [..., V]; the rows at any one distance from each other).
+
+    tokens: int32 [..., T], or [...] for one per row; -1 is no token (logprob 0, rank -1).  emitted: (draft_tok [B, k], accept_len
+    [B], next_tok [B]) of a verify call instead, for logits [B, k + 1, V]: position j holds draft_tok[b, j] up to accept_len[b],
+    then next_tok[b], nothing behind.  logZ: fp32 [...] where it is known (a verify call's): entropy and logZ are not made then;
+    the emitted form needs it.  Without ranks and alternatives nothing but the tokens' entries is read in that case.
+    status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  out: an earlier call's result of the same form, filled again."""
+    lib = load_library()
+    if logits.dtype not in _L_DTYPES or not logits.is_cuda or logits.dim() < 1:
+        raise HolaError("hola_token_logprobs takes fp32, bf16 or fp16 logits on a device")
+    shape, dev = logits.shape[:-1], logits.device
+    a = hola_logprobs_args()
+    a.rows, a.V, a.n_top = shape.numel(), logits.shape[-1], n_top
+    a.logits, a.row_stride, a.l_dtype = logits.data_ptr(), _row_stride(logits), _L_DTYPES[logits.dtype]
+
+    def check(t, dtype, size, name):
+        if t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(size) or not t.is_contiguous():
+            raise HolaError(f"hola_token_logprobs: {name} must be a contiguous {dtype} tensor of shape {tuple(size)} on {dev}")
+        return t.data_ptr()
+
+    per_row = None                                               # shape of the tokens
+    if emitted is not None:
+        if tokens is not None or logits.dim() != 3 or logZ is None:
+            raise HolaError("hola_token_logprobs: the emitted form takes logits [B, k + 1, V] and logZ, and no tokens")
+        draft_tok, accept_len, next_tok = emitted
+        B, k1 = shape
+        a.k, a.T, per_row = k1 - 1, 1, shape
+        if k1 > 1:
+            a.draft_tok = check(draft_tok, torch.int32, (B, k1 - 1), "draft_tok")
+        a.accept_len = check(accept_len, torch.int32, (B,), "accept_len")
+        a.next_tok = check(next_tok, torch.int32, (B,), "next_tok")
+    elif tokens is not None:
+        per_row = tokens.shape
+        if per_row[:len(shape)] != shape or len(per_row) > len(shape) + 1:
+            raise HolaError("hola_token_logprobs: tokens must have the shape of the rows, and one more axis at most")
+        a.T = per_row[-1] if len(per_row) > len(shape) else 1
+        if a.T:
+            a.tokens = check(tokens, torch.int32, per_row, "tokens")
+    if logZ is not None:
+        a.logZ_in = check(logZ, torch.float32, shape, "logZ")
+    if n_top and not 0 < n_top <= min(a.V, HOLA_MAX_TOP):
+        raise HolaError(f"hola_token_logprobs: n_top must be 0 .. min(V, {HOLA_MAX_TOP})")
+    sums, some = logZ is None, per_row is not None and a.T > 0
+
+    def field(name, dtype, size, wanted):
+        if not wanted:
+            return None
+        t = torch.empty(size, dtype=dtype, device=dev) if out is None else getattr(out, name)
+        if t is None:
+            raise HolaError(f"hola_token_logprobs: out has no {name}")
+        setattr(a, name, t.data_ptr() if out is None else check(t, dtype, size, name))
+        return t
+
+    got = TokenLogprobs(field("logprob", torch.float32, per_row, some), field("rank", torch.int32, per_row, some and want_rank),
+                        field("entropy", torch.float32, shape, sums), field("logZ", torch.float32, shape, sums),
+                        field("top_ids", torch.int32, (*shape, n_top), n_top > 0),
+                        field("top_logprobs", torch.float32, (*shape, n_top), n_top > 0))
+    if status is not None:
+        a.status_word = check(status, torch.int32, (1,), "status")
+    if a.rows == 0 or not (sums or some or n_top):
+        return got
+    with torch.cuda.device(dev):
+        _check(lib, None, lib.hola_token_logprobs(ctypes.byref(a), _stream_ptr(stream)), "hola_token_logprobs")
+    return got
 
 
 @dataclass

@@ -23,6 +23,8 @@
 //       shared exponent per sub-block of 128 channels) or in groups of mixed width, one launch for the whole head.
 //   quantize_hidden_kernel      the hidden rows of a call as one or two 8-bit planes.
 //   align_hidden_kernel         the hidden rows of a call once more, on 128-byte lines.
+//   token_logprobs_kernel       (token_logprobs.cuh) log probabilities and ranks of given tokens, entropy and top alternatives, from
+//       logits in memory; gather_logprobs_kernel, the tokens' entries alone.
 //   bounded_wait_selftest_kernel, staged_wait_selftest_kernel  waits that are made to run out, to exercise the give-up paths
 //       without breaking anything; quotient_selftest_kernel, the division behind every entropy.
 //   draft_entropy_kernel        H(q_j) of the draft rows, for the gate on the draft distribution.
@@ -39,6 +41,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
@@ -1821,6 +1824,8 @@ __global__ void __launch_bounds__(256) finalize_kernel(const float4* partials, i
   Stats st = warp_merge_row(partials, nparts, row_stride, row, lane, false);
   if (lane == 0) stats_to_outputs(st, &logZ[row], &entropy[row]);
 }
+
+#include "token_logprobs.cuh"
 
 // Vocabulary-parallel form, first exchange record of a rank: per verify row the statistics of this shard's logits
 // (m, s, t, arg-max as a GLOBAL vocabulary index), then per draft position the logit of the draft token if this shard
@@ -4463,6 +4468,42 @@ hola_status hola_host_traffic(const hola_ctx* ctx, unsigned long long* h2d_bytes
   if (!ctx || !h2d_bytes || !d2h_bytes) return HOLA_ERR_INVALID_ARG;
   *h2d_bytes = ctx->last_h2d; *d2h_bytes = ctx->last_d2h;
   return HOLA_OK;
+}
+
+hola_status hola_token_logprobs(const hola_logprobs_args* a, void* cuda_stream) {
+  if (!a || a->rows < 0 || a->V <= 0 || a->T < 0 || a->n_top < 0 || a->row_stride < 0) return HOLA_ERR_INVALID_ARG;
+  const bool emitted = a->accept_len || a->next_tok || a->draft_tok;
+  if (a->l_dtype < HOLA_L_F32 || a->l_dtype > HOLA_L_F16) return HOLA_ERR_INVALID_ARG;
+  if (a->n_top > kLpMaxTop || a->n_top > a->V) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (emitted) {
+    if (a->tokens || a->T != 1 || a->k < 0 || a->k == INT32_MAX || a->rows % (a->k + 1) != 0) return HOLA_ERR_INVALID_ARG;
+    if (!a->accept_len || !a->next_tok || (a->k > 0 && !a->draft_tok) || !a->logZ_in) return HOLA_ERR_INVALID_ARG;
+  } else if (a->T > 0 && !a->tokens) {
+    return HOLA_ERR_INVALID_ARG;
+  }
+  if ((a->T > 0) != (a->logprob != nullptr) || (a->rank && a->T == 0)) return HOLA_ERR_INVALID_ARG;
+  if ((a->n_top > 0) != (a->top_ids != nullptr) || (a->n_top > 0) != (a->top_logprobs != nullptr)) return HOLA_ERR_INVALID_ARG;
+  if (a->logZ_in && (a->entropy || a->logZ)) return HOLA_ERR_INVALID_ARG;
+  if (!a->logprob && !a->top_ids && !a->entropy && !a->logZ) return HOLA_ERR_INVALID_ARG;
+  if (a->rows == 0) return HOLA_OK;
+  const unsigned elem = a->l_dtype == HOLA_L_F32 ? 4 : 2;
+  if (!a->logits || reinterpret_cast<uintptr_t>(a->logits) % elem) return HOLA_ERR_INVALID_ARG;
+  if (static_cast<long long>(a->rows) * kLpMaxCluster > INT32_MAX || a->V > INT32_MAX - 64 ||
+      static_cast<long long>(a->rows) * a->T / 128 >= INT32_MAX)
+    return HOLA_ERR_UNSUPPORTED_SHAPE;
+  int dev = 0, sms = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10)
+    return HOLA_ERR_NO_DEVICE;
+  LpParams p = {};
+  p.logits = a->logits; p.row_stride = a->row_stride; p.rows = a->rows; p.V = a->V; p.T = a->T; p.n_top = a->n_top;
+  p.tokens = a->tokens; p.draft_tok = a->draft_tok; p.accept_len = a->accept_len; p.next_tok = a->next_tok; p.k = a->k;
+  p.logZ_in = a->logZ_in; p.logprob = a->logprob; p.rank = a->rank; p.entropy = a->entropy; p.logZ = a->logZ;
+  p.top_ids = a->top_ids; p.top_logprobs = a->top_logprobs; p.status = a->status_word;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = a->l_dtype == HOLA_L_F32 ? run_logprobs<float>(p, sms, stream)
+                        : a->l_dtype == HOLA_L_BF16 ? run_logprobs<__nv_bfloat16>(p, sms, stream) : run_logprobs<__half>(p, sms, stream);
+  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }
 
 static hola_status launch_quantiser(const void* W, int V, int H, const QuantOut& o, void* cuda_stream,

@@ -107,6 +107,7 @@ typedef struct hola_wmix {
 #define HOLA_FLAG_BAD_UNIFORM 2u /* a uniform outside [0,1): clamped into [0, 1 - 2^-24]                     */
 #define HOLA_FLAG_TIMEOUT 4u     /* an on-chip wait ran out of iterations; outputs of this call are invalid  */
 #define HOLA_FLAG_R_ZERO 8u      /* residual mass was zero (p <= q everywhere): token drawn from p instead   */
+#define HOLA_FLAG_BAD_ADAPTER 16u /* an adapter index outside [-1,slots): that sequence gets the bare head         */
 #define HOLA_FLAG_BAD_LOGIT 32u  /* hola_token_logprobs: a row of logits holds NaN or +inf                     */
 
 /* Bits of hola_verify_args::flags. */
@@ -283,6 +284,26 @@ hola_status hola_accept_sample(hola_ctx* ctx, const hola_verify_args* args, void
  * are safe, but two calls that overlap on the GPU (issued on different streams, say) race on it and give
  * wrong entropy / logZ.  Serialise them. */
 hola_status hola_lm_head_entropy_static(const hola_verify_args* args, void* cuda_stream);
+
+/* Low-rank adapters beside the LM head, one per sequence (the Lo-Bi section's W' = W + AB, kept apart from W so that a batch may hold
+ * the requests of many fine-tunes):  for a sequence that uses adapter a, position by position,
+ *   l[r][v] = sum_h W[v][h] x[r][h] + sum_i B[v][a][i] u[r][i],   u[r][i] = scale[a] * sum_h A[a][i][h] x[r][h],   i < rank,
+ * and entropy, logZ and everything behind are those of these logits.  W_lm in any of its storage forms; A, B and x are bf16, u and the
+ * logits fp32.  An adapter of a lower rank is filled up with zeros.
+ * hola_lm_head_adapters is hola_lm_head_entropy, hola_verify_adapters is hola_verify, with the same arguments, checks, streams and
+ * outputs; the arrays of `adapters` (a host struct, not looked at after the call) are resident on the device. */
+typedef struct hola_adapters {
+  const void* A;            /* bf16 [slots][rank][H], 16-byte aligned                                          */
+  const void* B;            /* bf16 [V][b_pitch], 16-byte aligned: slot s at columns s * rank ..               */
+  const float* scale;       /* fp32 [slots], or NULL: 1                                                        */
+  const int32_t* ids;       /* int32 [args->B]: the slot that each sequence uses, -1 = none (the bare head)     */
+  int32_t slots;            /* >= 1                                                                            */
+  int32_t rank;             /* multiple of 8, 8 .. 128                                                         */
+  int32_t b_pitch;          /* columns from one row of B to the next, >= slots * rank, multiple of 8           */
+  int32_t reserved_;
+} hola_adapters;
+hola_status hola_lm_head_adapters(hola_ctx* ctx, const hola_verify_args* args, const hola_adapters* adapters, void* cuda_stream);
+hola_status hola_verify_adapters(hola_ctx* ctx, const hola_verify_args* args, const hola_adapters* adapters, void* cuda_stream);
 
 /* Log probabilities of given tokens under rows of logits in memory, with their ranks, each row's entropy and its most probable
  * entries.  The paper has no counterpart; it is what a server hands to its clients beside the tokens that a verify call

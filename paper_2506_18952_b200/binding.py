@@ -25,14 +25,14 @@ HOLA_W_BF16, HOLA_W_INT8, HOLA_W8A8, HOLA_W8A16, HOLA_W_MIXED = 0, 1, 2, 3, 4
 HOLA_HIDDEN_IN_PLACE, HOLA_HIDDEN_ON_LINES, HOLA_HIDDEN_8BIT = 0, 1, 2
 HOLA_ARG_CLEAR_STATUS = 1
 GROUP_ROWS, SUB_BLOCK, HOLA_PACE_WORDS = 256, 128, 256
-FLAG_BAD_TOKEN, FLAG_BAD_UNIFORM, FLAG_TIMEOUT, FLAG_R_ZERO, FLAG_BAD_LOGIT = 1, 2, 4, 8, 32
+FLAG_BAD_TOKEN, FLAG_BAD_UNIFORM, FLAG_TIMEOUT, FLAG_R_ZERO, FLAG_BAD_ADAPTER, FLAG_BAD_LOGIT = 1, 2, 4, 8, 16, 32
 HOLA_L_F32, HOLA_L_BF16, HOLA_L_F16 = 0, 1, 2
-HOLA_MAX_TOP = 32
+HOLA_MAX_TOP, HOLA_MAX_RANK = 32, 128
 HOLA_OPT_RING_SLOTS, HOLA_OPT_ROTATING_UNITS, HOLA_OPT_HOST_OVERLAP, HOLA_OPT_HOST_ROWS_ON_DEMAND, HOLA_OPT_PASSES, HOLA_OPT_PAIR_MMA, HOLA_OPT_HOST_IN_PLACE, HOLA_OPT_CONVERTER_GROUP, HOLA_OPT_FUSED_PASSES = 1, 2, 3, 4, 5, 6, 7, 8, 9
 
 EXPORTS = ["hola_create", "hola_destroy", "hola_workspace_bytes", "hola_verify", "hola_verify_host",
            "hola_lm_head_entropy", "hola_accept_sample", "hola_host_traffic", "hola_shard_record_bytes", "hola_shard_lm_head",
-           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_token_logprobs", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
+           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_lm_head_adapters", "hola_verify_adapters", "hola_token_logprobs", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
            "hola_version"]
 
 
@@ -61,6 +61,11 @@ class hola_shard_args(ctypes.Structure):
     _fields_ = [("world", ctypes.c_int32), ("rank", ctypes.c_int32), ("v_offset", ctypes.c_int32),
                 ("V_global", ctypes.c_int32), ("q_tok", ctypes.c_void_p), ("record_out", ctypes.c_void_p),
                 ("records", ctypes.c_void_p), ("mass_out", ctypes.c_void_p), ("masses", ctypes.c_void_p)]
+
+
+class hola_adapters(ctypes.Structure):
+    _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ids", ctypes.c_void_p),
+                ("slots", ctypes.c_int32), ("rank", ctypes.c_int32), ("b_pitch", ctypes.c_int32), ("reserved_", ctypes.c_int32)]
 
 
 class hola_logprobs_args(ctypes.Structure):
@@ -118,6 +123,10 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         fn.argtypes = [ctypes.c_void_p, ctypes.POINTER(hola_verify_args), ctypes.c_void_p]
     lib.hola_lm_head_entropy_static.restype = ctypes.c_int
     lib.hola_lm_head_entropy_static.argtypes = [ctypes.POINTER(hola_verify_args), ctypes.c_void_p]
+    for name in ("hola_lm_head_adapters", "hola_verify_adapters"):
+        fn = getattr(lib, name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = [ctypes.c_void_p, ctypes.POINTER(hola_verify_args), ctypes.POINTER(hola_adapters), ctypes.c_void_p]
     lib.hola_token_logprobs.restype = ctypes.c_int
     lib.hola_token_logprobs.argtypes = [ctypes.POINTER(hola_logprobs_args), ctypes.c_void_p]
     lib.hola_quantize_w8.restype = ctypes.c_int
@@ -308,6 +317,56 @@ def hola_lm_head_entropy_static(hidden, W_lm, logits, entropy, logZ, stream=None
     a.status_word = _dptr(status)
     _check(lib, None, lib.hola_lm_head_entropy_static(ctypes.byref(a), _stream_ptr(stream)),
            "hola_lm_head_entropy_static")
+
+
+class AdapterBank:
+    """Low-rank adapters resident on the device for hola_lm_head_adapters and hola_verify_adapters: slot s adds scale[s] * B[s] A[s] to
+    the LM head of the sequences that name it.  Laid out once: A as [slots, rank, H], B as rows of all slots side by side
+    [V, pitch], the rank filled up with zeros to a multiple of 8."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None):
+        """A: bf16 [slots, rank, H], B: bf16 [slots, V, rank], scale: fp32 [slots] (None: 1 for all)."""
+        if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+            raise HolaError("AdapterBank takes A [slots, rank, H] and B [slots, V, rank]")
+        if scale is not None and tuple(scale.shape) != (A.shape[0],):
+            raise HolaError("AdapterBank: scale must have one value per slot")
+        self._make(*A.shape, B.shape[1], A.device)
+        for s in range(self.slots):
+            self.set(s, A[s], B[s], None if scale is None else scale[s])
+
+    @classmethod
+    def empty(cls, slots: int, rank: int, H: int, V: int, device=None) -> "AdapterBank":
+        """Slots of zeros, to be filled by set() with adapters of up to this rank."""
+        bank = cls.__new__(cls)
+        bank._make(slots, rank, H, V, torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device))
+        return bank
+
+    def _make(self, slots, rank, H, V, device):
+        if slots < 1 or not 1 <= rank <= HOLA_MAX_RANK:
+            raise HolaError(f"AdapterBank: at least one slot, ranks 1 .. {HOLA_MAX_RANK}")
+        self.slots, self.rank, self.H, self.V, self.device = slots, -(-rank // 8) * 8, H, V, device
+        self.A = torch.zeros((slots, self.rank, H), dtype=torch.bfloat16, device=device)
+        # (rows of whole 128-byte lines)
+        self.B = torch.zeros((V, -(-slots * self.rank // 64) * 64), dtype=torch.bfloat16, device=device)
+        self.scale = torch.ones((slots,), dtype=torch.float32, device=device)
+        self.struct = st = hola_adapters()
+        st.A, st.B, st.scale = self.A.data_ptr(), self.B.data_ptr(), self.scale.data_ptr()
+        st.slots, st.rank, st.b_pitch = slots, self.rank, self.B.shape[1]
+
+    def set(self, slot: int, A: torch.Tensor, B: torch.Tensor, scale=None) -> None:
+        """Puts an adapter into a slot, in order with the current stream's work: A bf16 [r, H], B bf16 [V, r], r at most the bank's
+        rank; scale: a number or a tensor of one (None: 1)."""
+        r = A.shape[0] if A.dim() == 2 else -1
+        if not 0 <= slot < self.slots or not 1 <= r <= self.rank or tuple(A.shape) != (r, self.H) or tuple(B.shape) != (self.V, r):
+            raise HolaError(f"AdapterBank.set: slot 0 .. {self.slots - 1}, A [r, {self.H}], B [{self.V}, r], r at most {self.rank}")
+        if A.dtype != torch.bfloat16 or B.dtype != torch.bfloat16:
+            raise HolaError("AdapterBank.set takes bfloat16 factors")
+        at = slot * self.rank
+        self.A[slot, :r] = A
+        self.A[slot, r:] = 0
+        self.B[:, at:at + r] = B
+        self.B[:, at + r:at + self.rank] = 0
+        self.scale[slot] = 1.0 if scale is None else scale
 
 
 @dataclass
@@ -705,6 +764,50 @@ class HolaVerify:
             st = self.lib.hola_lm_head_entropy(self._ctx, ctypes.byref(a), _stream_ptr(stream))
         if st:
             _check(self.lib, self._ctx, st, "hola_lm_head_entropy")
+        return out
+
+    def _with_adapters(self, bank: AdapterBank, ids: torch.Tensor, hidden) -> hola_adapters:
+        if bank.H != self.H or bank.V != self.V or bank.device != self._dev:
+            raise HolaError("the adapter bank must be made for the context's H and V, on its device")
+        if ids.dtype != torch.int32 or ids.device != self._dev or tuple(ids.shape) != (hidden.shape[0],) or not ids.is_contiguous():
+            raise HolaError("adapter_ids must be a contiguous int32 tensor on the context's device, one per sequence")
+        st = hola_adapters.from_buffer_copy(bank.struct)
+        st.ids = ids.data_ptr()
+        return st
+
+    def hola_lm_head_adapters(self, hidden, W_lm, adapters: AdapterBank, adapter_ids, out: VerifyOutputs | None = None,
+                              want_logits: bool = True, stream=None, w_scale=None, a8: bool = False) -> VerifyOutputs:
+        """hola_lm_head_entropy with low-rank adapters beside the head: adapter_ids int32 [B] names each sequence's slot of the
+        bank, -1 the bare head."""
+        B, k1 = hidden.shape[:2]
+        ad = self._with_adapters(adapters, adapter_ids, hidden)
+        fresh = not out
+        if fresh:
+            out = _fresh_outputs(self, B, k1, want_logits, False, False)
+        a = self._args(hidden, W_lm, None, None, None, 0.0, out, B, k1 - 1, w_scale=w_scale, a8=a8, draws=False)
+        if fresh:
+            a.flags = HOLA_ARG_CLEAR_STATUS
+        st = self.lib.hola_lm_head_adapters(self._ctx, ctypes.byref(a), ctypes.byref(ad), _stream_ptr(stream))
+        if st:
+            _check(self.lib, self._ctx, st, "hola_lm_head_adapters")
+        return out
+
+    def hola_verify_adapters(self, hidden, W_lm, draft_tok, draft_q, uniforms, tau, adapters: AdapterBank, adapter_ids,
+                             out: VerifyOutputs | None = None, want_logits: bool = False, stream=None,
+                             gate_source: int = HOLA_GATE_TARGET_ENTROPY, fallback: int = HOLA_FALLBACK_SAMPLE, w_scale=None,
+                             a8: bool = False) -> VerifyOutputs:
+        """hola_verify with low-rank adapters beside the head (see hola_lm_head_adapters)."""
+        B, k1 = hidden.shape[:2]
+        ad = self._with_adapters(adapters, adapter_ids, hidden)
+        fresh = not out
+        if fresh:
+            out = _fresh_outputs(self, B, k1, want_logits, True, gate_source == HOLA_GATE_DRAFT_ENTROPY)
+        a = self._args(hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, B, k1 - 1, gate_source, fallback, w_scale, a8)
+        if fresh:
+            a.flags = HOLA_ARG_CLEAR_STATUS
+        st = self.lib.hola_verify_adapters(self._ctx, ctypes.byref(a), ctypes.byref(ad), _stream_ptr(stream))
+        if st:
+            _check(self.lib, self._ctx, st, "hola_verify_adapters")
         return out
 
     def hola_accept_sample(self, logits, entropy, logZ, draft_tok, draft_q, uniforms, tau, stream=None) -> VerifyOutputs:

@@ -12,7 +12,7 @@ import sysconfig
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(_PKG, "csrc", "hola_verify.cu")
-PARTS = [os.path.join(_PKG, "csrc", name) for name in ("token_logprobs.cuh",)]      # what it includes
+PARTS = [os.path.join(_PKG, "csrc", name) for name in ("adapters.cuh", "token_logprobs.cuh")]      # what it includes
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "hola_verify.h")
 LIB = os.path.join(_PKG, "libhola_verify.so")
 HOST_SRC = os.path.join(_PKG, "csrc", "host_call.cpp")

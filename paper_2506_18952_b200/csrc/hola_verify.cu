@@ -23,6 +23,7 @@
 //       shared exponent per sub-block of 128 channels) or in groups of mixed width, one launch for the whole head.
 //   quantize_hidden_kernel      the hidden rows of a call as one or two 8-bit planes.
 //   align_hidden_kernel         the hidden rows of a call once more, on 128-byte lines.
+//   adapter_down_kernel, adapter_up_kernel  (adapters.cuh) low-rank adapters of many requests beside the LM head.
 //   token_logprobs_kernel       (token_logprobs.cuh) log probabilities and ranks of given tokens, entropy and top alternatives, from
 //       logits in memory; gather_logprobs_kernel, the tokens' entries alone.
 //   bounded_wait_selftest_kernel, staged_wait_selftest_kernel  waits that are made to run out, to exercise the give-up paths
@@ -1825,6 +1826,7 @@ __global__ void __launch_bounds__(256) finalize_kernel(const float4* partials, i
   if (lane == 0) stats_to_outputs(st, &logZ[row], &entropy[row]);
 }
 
+#include "adapters.cuh"
 #include "token_logprobs.cuh"
 
 // Vocabulary-parallel form, first exchange record of a rank: per verify row the statistics of this shard's logits
@@ -2890,6 +2892,7 @@ struct hola_ctx {
   double* hq;               // [max_rows][kHqSlices] slice sums of q ln q over the draft rows
   signed char* hid8;        // [rows][hidden_pitch8] int8 hidden rows (8-bit activation modes), or bf16 rows (aligns_hidden)
   float* hid_scale;         // [max_rows]
+  float* ad_u;              // [max_rows][kAdMaxRank] hidden rows behind their adapters' first factors
   // staging for hola_verify_host
   void* st_hidden; int* st_tok; void* st_q; float* st_u;
   unsigned char* st_out;      // device block of one call's outputs (status, accept_len, next_tok, entropy, logZ, ...)
@@ -2947,7 +2950,7 @@ OutBlock out_block(int B, int k) {
 }
 
 struct WsLayout {
-  size_t logits, partials, status, pace, hq, hid8, hid_scale, st_hidden, st_tok, st_q, st_u, st_out, st_qtok, st_small_end, total;
+  size_t logits, partials, status, pace, hq, hid8, hid_scale, ad_u, st_hidden, st_tok, st_q, st_u, st_out, st_qtok, st_small_end, total;
 };
 
 // Bytes from one 8-bit hidden row to the next: rows start on 128-byte lines, so that a K block of a row is one line instead of
@@ -2971,6 +2974,7 @@ WsLayout ws_layout(int maxB, int maxK, int H, int V, int num_sms) {
   w.hid8 = take(2 * align_up(rows, 32) * hidden_pitch8(H));           // one or two 8-bit planes of the hidden rows, or those
                                                                       // rows as they are, on whole lines
   w.hid_scale = take(2 * rows * 4);                                   // their scales (second plane after the first)
+  w.ad_u = take(rows * kAdMaxRank * 4);
   w.st_hidden = take(rows * H * 2);
   // the three small per-step inputs side by side: hola_verify_host sends them as one copy
   w.st_tok = take(static_cast<size_t>(maxB) * maxK * 4);
@@ -3550,6 +3554,38 @@ hola_status run_lm_head(hola_ctx* ctx, const hola_verify_args* a, float* logits,
 // Partials per row that a GEMM launch (or one per pass) leaves: one per CTA that works on the row's pass.
 int row_partials(const Plan& pl) { return pl.fused ? pl.grid / pl.passes : pl.grid; }
 
+// Steps 1-2 with adapters beside the head (`ad` null: without): their first product ahead of the GEMM, the second behind it.
+// `logits` may not be null then.
+hola_status run_adapted_lm_head(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, float* logits, int ldl, const Plan& pl,
+                                cudaStream_t stream, bool few_before, bool next_reads_inputs = false, bool draft_pass = false) {
+  if (!ad) return run_lm_head(ctx, a, logits, ldl, pl, stream, few_before, next_reads_inputs, draft_pass);
+  AdapterParams p = {};
+  p.A = static_cast<const uint16_t*>(ad->A); p.Bm = static_cast<const uint16_t*>(ad->B); p.scale = ad->scale; p.ids = ad->ids;
+  p.slots = ad->slots; p.rank = ad->rank; p.pitch = ad->b_pitch;
+  p.B = a->B; p.rows_per_seq = a->k + 1; p.H = a->H; p.V = a->V;
+  p.hidden = static_cast<const uint16_t*>(a->hidden); p.u = ctx->ad_u;
+  p.logits = logits; p.ldl = ldl; p.partials = ctx->partials; p.part_stride = ctx->part_stride; p.nparts = row_partials(pl);
+  p.want_arg = a->fallback == HOLA_FALLBACK_GREEDY;
+  p.status = a->status_word; p.clear_status = (a->flags & HOLA_ARG_CLEAR_STATUS) != 0;
+  cudaError_t e = launch_adapter_down(p, stream);
+  if (e != cudaSuccess) { set_error(ctx, "launch adapter_down_kernel", e); return HOLA_ERR_CUDA; }
+  hola_verify_args rest = *a;
+  rest.flags &= ~HOLA_ARG_CLEAR_STATUS;                  // (cleared by now)
+  const hola_status s = run_lm_head(ctx, &rest, logits, ldl, pl, stream, few_before, next_reads_inputs, draft_pass);
+  if (s != HOLA_OK) return s;
+  e = launch_adapter_up(p, ctx->num_sms, stream);
+  if (e != cudaSuccess) { set_error(ctx, "launch adapter_up_kernel", e); return HOLA_ERR_CUDA; }
+  return HOLA_OK;
+}
+
+hola_status check_adapters(const hola_adapters* ad) {
+  if (!ad || !ad->A || !ad->B || !ad->ids || ad->slots <= 0 || ad->rank <= 0) return HOLA_ERR_INVALID_ARG;
+  if (!aligned16(ad->A) || !aligned16(ad->B)) return HOLA_ERR_INVALID_ARG;
+  if (ad->rank % 8 != 0 || ad->rank > kAdMaxRank) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (ad->b_pitch % 8 != 0 || static_cast<long long>(ad->slots) * ad->rank > ad->b_pitch) return HOLA_ERR_INVALID_ARG;
+  return HOLA_OK;
+}
+
 cudaError_t launch_finalize(const hola_ctx* ctx, const hola_verify_args* a, int M, int nparts, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((M + 7) / 8)); cfg.blockDim = dim3(256); cfg.stream = stream;
@@ -3786,6 +3822,7 @@ hola_status hola_create(hola_ctx** out, int device, int maxB, int maxK, int H, i
   ctx->hq = reinterpret_cast<double*>(ctx->ws + w.hq);
   ctx->hid8 = reinterpret_cast<signed char*>(ctx->ws + w.hid8);
   ctx->hid_scale = reinterpret_cast<float*>(ctx->ws + w.hid_scale);
+  ctx->ad_u = reinterpret_cast<float*>(ctx->ws + w.ad_u);
   ctx->st_hidden = ctx->ws + w.st_hidden; ctx->st_tok = reinterpret_cast<int*>(ctx->ws + w.st_tok);
   ctx->st_q = ctx->ws + w.st_q; ctx->st_u = reinterpret_cast<float*>(ctx->ws + w.st_u);
   ctx->st_out = reinterpret_cast<unsigned char*>(ctx->ws + w.st_out);
@@ -3995,7 +4032,7 @@ hola_status hola_selftest_quotient(hola_ctx* ctx, const float* t, const float* s
   return HOLA_OK;
 }
 
-hola_status hola_lm_head_entropy(hola_ctx* ctx, const hola_verify_args* a, void* cuda_stream) {
+static hola_status lm_head_entropy(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, void* cuda_stream) {
   hola_status s = check_common(ctx, a);
   if (s != HOLA_OK) return s;
   if (a->B == 0) return empty_batch(ctx, a, cuda_stream);
@@ -4007,10 +4044,19 @@ hola_status hola_lm_head_entropy(hola_ctx* ctx, const hola_verify_args* a, void*
   const Plan& pl = plan_for(ctx, M, a->w_dtype);
   float* logits = a->logits_out ? a->logits_out : ctx->logits;
   const int ldl = a->logits_out ? a->V : ctx->ldl;
-  if ((s = run_lm_head(ctx, a, logits, ldl, pl, stream, M <= 256)) != HOLA_OK) return s;
+  if ((s = run_adapted_lm_head(ctx, a, ad, logits, ldl, pl, stream, M <= 256)) != HOLA_OK) return s;
   const cudaError_t e = launch_finalize(ctx, a, M, row_partials(pl), stream);
   if (e != cudaSuccess) { set_error(ctx, "launch finalize_kernel", e); return HOLA_ERR_CUDA; }
   return HOLA_OK;
+}
+
+hola_status hola_lm_head_entropy(hola_ctx* ctx, const hola_verify_args* a, void* cuda_stream) {
+  return lm_head_entropy(ctx, a, nullptr, cuda_stream);
+}
+
+hola_status hola_lm_head_adapters(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, void* cuda_stream) {
+  const hola_status s = check_adapters(ad);
+  return s == HOLA_OK ? lm_head_entropy(ctx, a, ad, cuda_stream) : s;
 }
 
 hola_status hola_accept_sample(hola_ctx* ctx, const hola_verify_args* a, void* cuda_stream) {
@@ -4030,9 +4076,10 @@ namespace {
 
 // The whole step on device buffers.  `before_sample`, when given, is an event the accept/sample part waits for
 // (the draft tensor still being copied in by hola_verify_host).
-hola_status verify_device(hola_ctx* ctx, const hola_verify_args* a, cudaStream_t stream, cudaEvent_t before_sample) {
+hola_status verify_device(hola_ctx* ctx, const hola_verify_args* a, cudaStream_t stream, cudaEvent_t before_sample,
+                          const hola_adapters* ad = nullptr) {
   const Plan& pl = plan_for(ctx, a->B * (a->k + 1), a->w_dtype);
-  float* logits = a->logits_out ? a->logits_out : logits_buffer(ctx, a);
+  float* logits = a->logits_out ? a->logits_out : ad ? ctx->logits : logits_buffer(ctx, a);
   const int ldl = a->logits_out ? a->V : ctx->ldl;
   const bool prof = ctx->prof_on && ctx->prof_n < ctx->prof_cap;
   cudaEvent_t* ev = prof ? ctx->prof_ev + 3 * ctx->prof_n : nullptr;
@@ -4058,7 +4105,7 @@ hola_status verify_device(hola_ctx* ctx, const hola_verify_args* a, cudaStream_t
   // 8 59.9 / 61.4: no line there that holds for all.)
   const SampleForm f = sample_form(ctx->num_sms, a->B, a->k, a->V, a->q_dtype, a->fallback, rows_of_pieces(a, logits, ldl));
   const bool few_before = a->B * f.S * (f.solo ? 2 : 4) <= ctx->num_sms;
-  hola_status s = run_lm_head(ctx, a, logits, ldl, pl, stream, few_before, !before_sample, inside);
+  hola_status s = run_adapted_lm_head(ctx, a, ad, logits, ldl, pl, stream, few_before, !before_sample, inside);
   if (s != HOLA_OK) return s;
   if (prof) cudaEventRecord(ev[1], stream);
   if (side) {
@@ -4252,14 +4299,21 @@ hola_status verify_host_lazy(hola_ctx* ctx, const hola_verify_args* a, cudaStrea
 
 extern "C" {
 
-hola_status hola_verify(hola_ctx* ctx, const hola_verify_args* a, void* cuda_stream) {
+static hola_status verify(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, void* cuda_stream) {
   hola_status s = check_common(ctx, a);
   if (s != HOLA_OK) return s;
   if (a->B == 0) return empty_batch(ctx, a, cuda_stream);
   if ((s = check_lm_head_args(ctx, a)) != HOLA_OK) return s;
   if ((s = check_sample_args(a)) != HOLA_OK) return s;
   DeviceGuard guard(ctx->device);
-  return verify_device(ctx, a, static_cast<cudaStream_t>(cuda_stream), nullptr);
+  return verify_device(ctx, a, static_cast<cudaStream_t>(cuda_stream), nullptr, ad);
+}
+
+hola_status hola_verify(hola_ctx* ctx, const hola_verify_args* a, void* cuda_stream) { return verify(ctx, a, nullptr, cuda_stream); }
+
+hola_status hola_verify_adapters(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, void* cuda_stream) {
+  const hola_status s = check_adapters(ad);
+  return s == HOLA_OK ? verify(ctx, a, ad, cuda_stream) : s;
 }
 
 hola_status hola_profile_begin(hola_ctx* ctx, int max_calls) {

@@ -1,0 +1,345 @@
+"""Low-rank adapters beside the LM head: logits, statistics and the whole step against the definition in 64 bits."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import compare, ref
+from paper_2506_18952_b200 import binding, workloads
+
+gpu = pytest.mark.gpu
+U = 2.0 ** -24                          # half a unit in the last place of fp32, relative
+
+
+# ------------------------------------------------------------------------------------------------ inputs and reference
+def make(B, k, H, V, slots, rank, seed=0, weights="bf16"):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")                     # noqa: E731
+    hidden = rnd(B, k + 1, H).to(torch.bfloat16)
+    W = (rnd(V, H) * 1.28 / H ** 0.5).to(torch.bfloat16)
+    A = (rnd(slots, rank, H) / H ** 0.5).to(torch.bfloat16)
+    Bup = (rnd(slots, V, rank) * 0.5 / rank ** 0.5).to(torch.bfloat16)
+    scale = torch.rand((slots,), generator=g, device="cuda") * 1.5 + 0.25
+    ids = torch.randint(-1, slots, (B,), generator=g, device="cuda", dtype=torch.int32)
+    w_scale, a8 = None, False
+    if weights == "mixed":
+        widths = [(4, 8, 16)[i % 3] for i in range(-(-V // 256))]
+        W = binding.hola_quantize_mixed(W, widths)
+    elif weights != "bf16":
+        W, w_scale = binding.hola_quantize_w8(W)
+        a8 = {"int8": False, "w8a8": True, "w8a16": "a16"}[weights]
+    return dict(hidden=hidden, W=W, A=A, Bup=Bup, scale=scale, ids=ids, w_scale=w_scale, a8=a8)
+
+
+def delta64(d):
+    """The adapters' part of the logits in 64 bits, and what bounds its fp32 evaluation.  A tensor-core step of 16 products adds no
+    more than 2^-22 of its operands' absolute sum (products are exact, terms are cut off at the largest one's last place); u passes
+    through H / 16 such steps and 16 additions, the second product through 3 rank / 16; u itself enters it as two bf16 planes at
+    least, which leave 2^-18 of it; the scale is one more rounding."""
+    H, rank = d["hidden"].shape[-1], d["A"].shape[1]
+    x, ids = d["hidden"].double(), d["ids"].long()
+    B, k1, _ = x.shape
+    out = torch.zeros((B, k1, d["Bup"].shape[1]), dtype=torch.float64, device="cuda")
+    bound = torch.zeros_like(out)
+    for b in range(B):
+        a = int(ids[b])
+        if 0 <= a < d["A"].shape[0]:
+            A, Bu, s = d["A"][a].double(), d["Bup"][a].double(), d["scale"][a].double()
+            u, u_abs = s * (x[b] @ A.T), s * (x[b].abs() @ A.abs().T)
+            out[b] = u @ Bu.T
+            e_u = u_abs * ((-(-H // 16)) * 2.0 ** -22 + 17 * U) + u.abs() * (2.0 ** -18 + U)
+            bound[b] = e_u @ Bu.abs().T + (u.abs() @ Bu.abs().T) * (3 * -(-rank // 16) + 3) * 2.0 ** -22
+    return out, bound
+
+
+def check_stats(out, V, logits=None):
+    """entropy and logZ are those of the logits that came with them: fp32 sums of V terms in pieces (V / 1000 + 40 roundings deep
+    at most, 2^-22 per exponential), H = ln s - t / s with |t / s| <= ln V."""
+    l = (out.logits if logits is None else logits).double()
+    logZ = torch.logsumexp(l, dim=-1)
+    lp = l - logZ[..., None]
+    H = -(lp.exp() * lp).sum(-1)
+    E = (V / 1000 + 40) * U + 2.0 ** -22 + 4 * U * float(l.abs().max())
+    assert (out.logZ.double() - logZ).abs().max() <= E + 2 * U * float(l.abs().max())
+    assert (out.entropy.double() - H).abs().max() <= E * (1 + 3 * np.log(V + 1)) + 4 * U * np.log(V + 1)
+
+
+def check_logits(got, base, d):
+    """Against the bare head's own logits, plus the adapters' part.  Where both products are accumulated together the running sum
+    is rounded once per step: 2^-22 of it for each of 2 x slots x rank / 16 steps."""
+    want, bound = delta64(d)
+    want = want + base.double()
+    steps = 2 * -(-d["A"].shape[0] * (-(-d["A"].shape[1] // 8) * 8) // 64) * 4 + 4
+    tol = bound + steps * 2.0 ** -22 * (base.double().abs() + want.abs() + want.abs().amax(dim=-1, keepdim=True) * 0.25)
+    assert ((got.double() - want).abs() <= tol).all(), float(((got.double() - want).abs() - tol).max())
+
+
+SHAPES = [  # B, k, H, V, slots, rank
+    (1, 4, 64, 1000, 1, 8), (1, 0, 64, 33, 2, 8), (2, 3, 128, 8, 3, 16), (5, 1, 72, 1001, 4, 24), (3, 4, 256, 5003, 2, 16),
+    (1, 4, 4096, 32000, 4, 16), (7, 20, 512, 3001, 5, 8), (2, 40, 264, 2000, 2, 40), (23, 3, 1032, 50003, 8, 24), (64, 5, 512, 32000, 16, 16),
+    (9, 5, 1024, 4099, 3, 128), (40, 7, 256, 6000, 64, 8), (100, 5, 256, 2000, 7, 16), (32, 0, 1024, 128256, 16, 32), (300, 8, 64, 700, 9, 16),
+    (17, 2, 640, 9001, 64, 16)]
+
+
+@gpu
+@pytest.mark.parametrize("B,k,H,V,slots,rank", SHAPES)
+def test_logits_and_statistics(B, k, H, V, slots, rank):
+    d = make(B, k, H, V, slots, rank, seed=B + V)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        base = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True)
+        out = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"])
+        assert out.status.item() == 0
+        check_logits(out.logits, base.logits, d)
+        check_stats(out, V)
+        kept = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"], want_logits=False)     # logits in the context's scratch
+        check_stats(kept, V, out.logits)
+        # a sequence without an adapter gets what the bare head gives it
+        d["ids"].fill_(-1)
+        none = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"])
+        assert torch.equal(none.logits, base.logits)
+        check_stats(none, V)
+
+
+@gpu
+@pytest.mark.parametrize("weights", ["int8", "w8a8", "w8a16", "mixed"])
+@pytest.mark.parametrize("B,k,H,V,slots,rank", [(1, 4, 256, 3001, 3, 16), (16, 5, 1024, 8000, 4, 8), (64, 5, 512, 9000, 8, 24),
+                                                (90, 5, 256, 5000, 64, 16)])
+def test_every_storage_form_of_the_head(weights, B, k, H, V, slots, rank):
+    d = make(B, k, H, V, slots, rank, seed=3, weights=weights)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    kw = dict(w_scale=d["w_scale"], a8=d["a8"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        base = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True, **kw)
+        out = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"], **kw)
+        check_logits(out.logits, base.logits, d)
+        check_stats(out, V)
+        bare = (d["ids"] < 0).nonzero()[:, 0]
+        assert torch.equal(out.logits[bare], base.logits[bare])
+
+
+@gpu
+def test_against_the_whole_definition():
+    """W x + s B A x in 64 bits throughout."""
+    B, k, H, V = 6, 3, 1024, 7001
+    d = make(B, k, H, V, 4, 16, seed=8)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        out = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"])
+    want, bound = delta64(d)
+    x, W = d["hidden"].double(), d["W"].double()
+    want += x @ W.T
+    bound += (x.abs() @ W.abs().T) * (H // 16 + 8) * 2.0 ** -22 + 8 * 2.0 ** -22 * want.abs()
+    assert ((out.logits.double() - want).abs() <= bound).all()
+
+
+def _verify_inputs(B, k, H, V, slots, rank, seed, q_dtype=torch.bfloat16):
+    w = workloads.gaussian_head("adapters", B, k, H, V, seed=seed, device="cuda", w_std=2.0 / H ** 0.5, sigma=0.5, tau=2.0,
+                                sigma_far=1.5, q_dtype=q_dtype)
+    d = make(B, k, H, V, slots, rank, seed)
+    d["hidden"], d["W"] = w.hidden, w.W_lm
+    return w, d
+
+
+@gpu
+@pytest.mark.parametrize("gate,fallback", [(0, 0), (1, 0), (0, 1), (1, 1)])
+@pytest.mark.parametrize("B,k,H,V", [(1, 4, 512, 6000), (24, 5, 256, 5000), (70, 4, 256, 3001), (5, 0, 64, 1000)])
+def test_whole_step(B, k, H, V, gate, fallback):
+    if k == 0 and gate == 1:
+        pytest.skip("no draft rows")
+    w, d = _verify_inputs(B, k, H, V, 5, 16, seed=21 + B)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        out = ctx.hola_verify_adapters(w.hidden, w.W_lm, w.draft_tok, w.draft_q, w.uniforms, w.tau, bank, d["ids"], want_logits=True,
+                                       gate_source=gate, fallback=fallback)
+        again = ctx.hola_verify_adapters(w.hidden, w.W_lm, w.draft_tok, w.draft_q, w.uniforms, w.tau, bank, d["ids"],
+                                         gate_source=gate, fallback=fallback)            # logits in the context's scratch
+        torch.cuda.synchronize()
+    want, _ = delta64(d)
+    want += w.hidden.double() @ w.W_lm.double().T
+    n = compare.torch_to_numpy
+    orc = ref.verify_from_logits(want.cpu().numpy(), n(w.draft_tok), n(w.draft_q), n(w.uniforms), w.tau, gate, fallback)
+    rep = compare.compare(orc, n(w.draft_q), n(w.uniforms), n(out.accept_len), n(out.next_tok), n(out.entropy), n(out.logZ),
+                          n(out.logits))
+    assert rep.ok, rep.summary()
+    assert out.status.item() == 0
+    for f in ("accept_len", "next_tok", "entropy", "logZ"):
+        assert torch.equal(getattr(out, f), getattr(again, f))
+
+
+@gpu
+def test_adapters_then_scores_of_what_was_emitted():
+    """The run of them as a server makes it: adapted verify step, then the log probabilities of the tokens that it emitted."""
+    B, k, H, V = 12, 4, 256, 5003
+    w, d = _verify_inputs(B, k, H, V, 3, 16, seed=5)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        out = ctx.hola_verify_adapters(w.hidden, w.W_lm, w.draft_tok, w.draft_q, w.uniforms, w.tau, bank, d["ids"], want_logits=True)
+        lp = binding.hola_token_logprobs(out.logits, n_top=5, logZ=out.logZ, emitted=(w.draft_tok, out.accept_len, out.next_tok))
+    l = delta64(d)[0] + w.hidden.double() @ w.W_lm.double().T
+    want = torch.log_softmax(l, dim=-1)
+    for b in range(B):
+        n = int(out.accept_len[b])
+        for j in range(k + 1):
+            if j > n:
+                assert lp.logprob[b, j] == 0 and lp.rank[b, j] == -1 and (lp.top_ids[b, j] == -1).all()
+                continue
+            x = int(w.draft_tok[b, j] if j < n else out.next_tok[b])
+            assert abs(float(lp.logprob[b, j] - want[b, j, x])) <= compare.ENTROPY_ATOL
+            row = out.logits[b, j]
+            before = int(((row > row[x]) | ((row == row[x]) & (torch.arange(V, device="cuda") < x))).sum())
+            assert int(lp.rank[b, j]) == before
+            assert int(lp.top_ids[b, j, 0]) == int((row == row.max()).nonzero()[0])
+
+
+@gpu
+def test_indices_that_no_slot_has():
+    B, k, H, V = 6, 2, 128, 999
+    d = make(B, k, H, V, 2, 8, seed=4)
+    d["ids"].copy_(torch.tensor([0, 1, -1, 2, -2, 2 ** 31 - 1]))
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        base = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True)
+        out = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"])
+        assert out.status.item() == binding.FLAG_BAD_ADAPTER
+        assert torch.equal(out.logits[2:], base.logits[2:])
+        check_logits(out.logits, base.logits, d)
+        check_stats(out, V)
+        out.status.fill_(binding.FLAG_R_ZERO)                 # the caller's word: bits are added
+        ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"], out=out)
+        assert out.status.item() == binding.FLAG_BAD_ADAPTER | binding.FLAG_R_ZERO
+
+
+@gpu
+def test_ranks_are_filled_up_and_slots_are_replaced():
+    B, k, H, V = 8, 3, 256, 3000
+    d = make(B, k, H, V, 4, 13, seed=9)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    assert bank.rank == 16 and bank.B.shape[1] == 64
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        base = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True)
+        check_logits(ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"]).logits, base.logits, d)
+        e = make(B, k, H, V, 4, 4, seed=10)                   # rank 4 takes a slot's place
+        other = binding.AdapterBank.empty(4, 13, H, V)
+        for s in (3, 0, 2, 1):
+            other.set(s, d["A"][s], d["Bup"][s], float(d["scale"][s]))
+        other.set(2, e["A"][2], e["Bup"][2], e["scale"][2])
+        d["A"][2], d["Bup"][2] = 0, 0
+        d["A"][2, :4], d["Bup"][2, :, :4], d["scale"][2] = e["A"][2], e["Bup"][2], e["scale"][2]
+        check_logits(ctx.hola_lm_head_adapters(d["hidden"], d["W"], other, d["ids"]).logits, base.logits, d)
+        ones = binding.AdapterBank(d["A"], d["Bup"])
+        d["scale"].fill_(1.0)
+        check_logits(ctx.hola_lm_head_adapters(d["hidden"], d["W"], ones, d["ids"]).logits, base.logits, d)
+
+
+@gpu
+def test_graphs_streams_and_changing_batches():
+    """A captured call follows its inputs: the hidden rows and the adapters of the batch change between replays."""
+    B, k, H, V = 20, 4, 512, 8000
+    d = make(B, k, H, V, 6, 16, seed=12)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        src, ids = d["hidden"].clone(), d["ids"].clone()
+        out = ctx.hola_lm_head_adapters(src, d["W"], bank, ids)
+        ctx.hola_lm_head_adapters(src, d["W"], bank, ids, out=out)
+        torch.cuda.synchronize()
+        hid = torch.empty_like(src)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            torch.mul(src, 1, out=hid)                        # written right in front of the call
+            ctx.hola_lm_head_adapters(hid, d["W"], bank, ids, out=out)
+        for r in range(3):
+            src.copy_(d["hidden"].roll(r, 0))
+            ids.copy_(d["ids"].roll(2 * r, 0))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in (out.logits, out.logZ, out.entropy)]
+            want = ctx.hola_lm_head_adapters(src, d["W"], bank, ids)
+            assert all(torch.equal(x, y) for x, y in zip(got, (want.logits, want.logZ, want.entropy)))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        aside = ctx.hola_lm_head_adapters(src, d["W"], bank, ids, stream=side)
+        side.synchronize()
+        assert torch.equal(aside.logits, want.logits)
+
+
+@gpu
+def test_rows_behind_the_batch_and_calls_in_between_keep_their_results():
+    """A context made for more: nothing beyond the batch's rows is written, and bare calls before and after give the same bits."""
+    B, k, H, V = 3, 2, 128, 1003
+    d = make(B, k, H, V, 2, 8, seed=14)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(10, 6, H, V) as ctx:
+        before = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True)
+        room = torch.full((B * (k + 1) * V + 2 * V,), 7.5, device="cuda")
+        stats = torch.full((2, B * (k + 1) + 32), 7.5, device="cuda")
+        out = ctx.alloc_outputs(B, k)
+        out.logits = room[V:-V].view(B, k + 1, V)
+        out.entropy, out.logZ = (stats[i, 16:-16].view(B, k + 1) for i in range(2))
+        ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"], out=out)
+        check_logits(out.logits, before.logits, d)
+        assert (room[:V] == 7.5).all() and (room[-V:] == 7.5).all()
+        assert (stats[:, :16] == 7.5).all() and (stats[:, -16:] == 7.5).all()
+        after = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True)
+        for f in ("logits", "entropy", "logZ"):
+            assert torch.equal(getattr(before, f), getattr(after, f))
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+def _adapters(**kw):
+    a = binding.hola_adapters()
+    for n, v in dict(dict(A=4096, B=4096, scale=4096, ids=4096, slots=3, rank=8, b_pitch=24), **kw).items():
+        setattr(a, n, v)
+    return a
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(A=None), 1), (dict(B=None), 1), (dict(ids=None), 1), (dict(slots=0), 1), (dict(slots=-1), 1), (dict(rank=0), 1), (dict(rank=-8), 1),
+    (dict(A=4104), 1), (dict(B=4104), 1), (dict(rank=4), 2), (dict(rank=136, b_pitch=408), 2), (dict(b_pitch=16), 1), (dict(b_pitch=28), 1),
+    (dict(slots=2 ** 31 - 1, b_pitch=2 ** 31 - 8), 1), ({}, 1)])
+def test_refused_by_the_library(change, status):
+    """(The last one: adapters that are in order, and no context.)"""
+    lib = binding.load_library()
+    ad, a = _adapters(**change), binding.hola_verify_args()
+    for fn in (lib.hola_lm_head_adapters, lib.hola_verify_adapters):
+        assert fn(None, ctypes.byref(a), ctypes.byref(ad), None) == status
+        assert fn(None, ctypes.byref(a), None, None) == 1
+
+
+def test_struct_layout():
+    assert ctypes.sizeof(binding.hola_adapters) == 4 * 8 + 4 * 4
+
+
+def test_bank_layout_and_refusals_need_no_device():
+    A, Bup = torch.randn(3, 5, 16).bfloat16(), torch.randn(3, 40, 5).bfloat16()
+    bank = binding.AdapterBank(A, Bup, torch.tensor([1.0, 2.0, 3.0]))
+    assert (bank.slots, bank.rank, bank.H, bank.V) == (3, 8, 16, 40) and bank.struct.b_pitch == 64
+    for s in range(3):
+        assert torch.equal(bank.A[s, :5], A[s]) and (bank.A[s, 5:] == 0).all()
+        assert torch.equal(bank.B[:, 8 * s:8 * s + 5], Bup[s]) and (bank.B[:, 8 * s + 5:8 * s + 8] == 0).all()
+    assert (bank.B[:, 24:] == 0).all() and bank.scale.tolist() == [1.0, 2.0, 3.0]
+    bank.set(1, A[0, :2], Bup[0][:, :2], 0.5)
+    assert (bank.A[1, 2:] == 0).all() and (bank.B[:, 10:16] == 0).all() and bank.scale[1] == 0.5
+    for bad in (lambda: binding.AdapterBank(A, Bup[:2]), lambda: binding.AdapterBank(A, Bup.transpose(1, 2)), lambda: binding.AdapterBank(A[0], Bup),
+                lambda: binding.AdapterBank(A, Bup, torch.ones(2)), lambda: binding.AdapterBank(A.float(), Bup),
+                lambda: binding.AdapterBank.empty(0, 8, 16, 40, "cpu"), lambda: binding.AdapterBank.empty(1, 129, 16, 40, "cpu"),
+                lambda: bank.set(3, A[0], Bup[0]), lambda: bank.set(-1, A[0], Bup[0]), lambda: bank.set(0, A[0][:, :8], Bup[0]),
+                lambda: bank.set(0, A[0], Bup[0][:, :4]), lambda: bank.set(0, A[0].float(), Bup[0])):
+        with pytest.raises(binding.HolaError):
+            bad()
+
+
+@gpu
+def test_refused_by_the_binding():
+    d = make(2, 1, 64, 500, 2, 8)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(2, 1, 64, 500) as ctx:
+        for ids in (d["ids"].long(), d["ids"].cpu(), d["ids"][:1], d["ids"].repeat(2)[::2]):
+            with pytest.raises(binding.HolaError):
+                ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, ids)
+        for other in (binding.AdapterBank.empty(2, 8, 128, 500), binding.AdapterBank.empty(2, 8, 64, 501), binding.AdapterBank.empty(2, 8, 64, 500, "cpu")):
+            with pytest.raises(binding.HolaError):
+                ctx.hola_lm_head_adapters(d["hidden"], d["W"], other, d["ids"])
+        with pytest.raises(binding.HolaError):
+            ctx.hola_verify_adapters(d["hidden"], d["W"], None, None, None, 1.0, bank, d["ids"])

@@ -98,7 +98,8 @@ def _load_host(lib: ctypes.CDLL):
     except (ImportError, OSError, subprocess.CalledProcessError) as e:
         warnings.warn(f"host-side helper not available, calls cost a few microseconds more: {e}")
         return
-    for name in ("hola_verify", "hola_verify_host", "hola_lm_head_entropy", "hola_quantize_mixed_widths"):
+    for name in ("hola_verify", "hola_verify_host", "hola_lm_head_entropy", "hola_quantize_mixed_widths", "hola_lm_head_adapters",
+                 "hola_verify_adapters", "hola_token_logprobs"):
         _entry[name] = ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
     _host = helper
 
@@ -352,6 +353,7 @@ class AdapterBank:
         self.struct = st = hola_adapters()
         st.A, st.B, st.scale = self.A.data_ptr(), self.B.data_ptr(), self.scale.data_ptr()
         st.slots, st.rank, st.b_pitch = slots, self.rank, self.B.shape[1]
+        self.address = ctypes.addressof(st)
 
     def set(self, slot: int, A: torch.Tensor, B: torch.Tensor, scale=None) -> None:
         """Puts an adapter into a slot, in order with the current stream's work: A bf16 [r, H], B bf16 [V, r], r at most the bank's
@@ -411,6 +413,14 @@ def hola_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None
     the emitted form needs it.  Without ranks and alternatives nothing but the tokens' entries is read in that case.
     status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  out: an earlier call's result of the same form, filled again."""
     lib = load_library()
+    if _host is not None and stream is None and out is None:
+        draft_tok, accept_len, next_tok = emitted if emitted is not None else (None, None, None)
+        got = _host.score(_entry["hola_token_logprobs"], logits, tokens, n_top, logZ, draft_tok, accept_len, next_tok, emitted is not None,
+                          want_rank, status, torch._C._cuda_getDevice(), _stream_ptr(None))
+        if got is not None:
+            if got[0]:
+                _check(lib, None, got[0], "hola_token_logprobs")
+            return TokenLogprobs(*got[1:])
     if logits.dtype not in _L_DTYPES or not logits.is_cuda or logits.dim() < 1:
         raise HolaError("hola_token_logprobs takes fp32, bf16 or fp16 logits on a device")
     shape, dev = logits.shape[:-1], logits.device
@@ -702,7 +712,7 @@ class HolaVerify:
         return a
 
     def _native(self, entry, hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, draws, flags, gate_source, fallback, w_scale,
-                a8, stream):
+                a8, stream, bank=None, ids=None):
         """The call through the native helper: its status, or None where the arguments have to be made from Python."""
         if _host is None or self.lib is not _lib:
             return None
@@ -712,6 +722,11 @@ class HolaVerify:
                 return None
             wmix, w_scale = ctypes.addressof(W_lm.struct), W_lm.w_scale
             W_lm = W_lm.W8 if W_lm.W8 is not None else (W_lm.W4 if W_lm.W4 is not None else W_lm.W16)
+        if bank is not None:
+            if type(bank) is not AdapterBank or bank.H != self.H or bank.V != self.V or bank.device != self._dev:
+                return None
+            return _host.call(_entry[entry], self._ctx.value, self.H, self.V, hidden, W_lm, draft_tok, draft_q, uniforms, tau, out,
+                              draws, flags, gate_source, fallback, w_scale, a8, wmix, _stream_ptr(stream), bank.address, ids, self.device)
         return _host.call(_entry[entry], self._ctx.value, self.H, self.V, hidden, W_lm, draft_tok, draft_q, uniforms, tau, out,
                           draws, flags, gate_source, fallback, w_scale, a8, wmix, _stream_ptr(stream))
 
@@ -779,15 +794,19 @@ class HolaVerify:
                               want_logits: bool = True, stream=None, w_scale=None, a8: bool = False) -> VerifyOutputs:
         """hola_lm_head_entropy with low-rank adapters beside the head: adapter_ids int32 [B] names each sequence's slot of the
         bank, -1 the bare head."""
-        B, k1 = hidden.shape[:2]
-        ad = self._with_adapters(adapters, adapter_ids, hidden)
         fresh = not out
         if fresh:
+            B, k1 = hidden.shape[:2]
             out = _fresh_outputs(self, B, k1, want_logits, False, False)
-        a = self._args(hidden, W_lm, None, None, None, 0.0, out, B, k1 - 1, w_scale=w_scale, a8=a8, draws=False)
-        if fresh:
-            a.flags = HOLA_ARG_CLEAR_STATUS
-        st = self.lib.hola_lm_head_adapters(self._ctx, ctypes.byref(a), ctypes.byref(ad), _stream_ptr(stream))
+        st = self._native("hola_lm_head_adapters", hidden, W_lm, None, None, None, 0.0, out, 0, HOLA_ARG_CLEAR_STATUS if fresh else 0, 0,
+                          0, w_scale, a8, stream, adapters, adapter_ids)
+        if st is None:
+            B, k1 = hidden.shape[:2]
+            ad = self._with_adapters(adapters, adapter_ids, hidden)
+            a = self._args(hidden, W_lm, None, None, None, 0.0, out, B, k1 - 1, w_scale=w_scale, a8=a8, draws=False)
+            if fresh:
+                a.flags = HOLA_ARG_CLEAR_STATUS
+            st = self.lib.hola_lm_head_adapters(self._ctx, ctypes.byref(a), ctypes.byref(ad), _stream_ptr(stream))
         if st:
             _check(self.lib, self._ctx, st, "hola_lm_head_adapters")
         return out
@@ -797,15 +816,19 @@ class HolaVerify:
                              gate_source: int = HOLA_GATE_TARGET_ENTROPY, fallback: int = HOLA_FALLBACK_SAMPLE, w_scale=None,
                              a8: bool = False) -> VerifyOutputs:
         """hola_verify with low-rank adapters beside the head (see hola_lm_head_adapters)."""
-        B, k1 = hidden.shape[:2]
-        ad = self._with_adapters(adapters, adapter_ids, hidden)
         fresh = not out
         if fresh:
+            B, k1 = hidden.shape[:2]
             out = _fresh_outputs(self, B, k1, want_logits, True, gate_source == HOLA_GATE_DRAFT_ENTROPY)
-        a = self._args(hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, B, k1 - 1, gate_source, fallback, w_scale, a8)
-        if fresh:
-            a.flags = HOLA_ARG_CLEAR_STATUS
-        st = self.lib.hola_verify_adapters(self._ctx, ctypes.byref(a), ctypes.byref(ad), _stream_ptr(stream))
+        st = self._native("hola_verify_adapters", hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, 1,
+                          HOLA_ARG_CLEAR_STATUS if fresh else 0, gate_source, fallback, w_scale, a8, stream, adapters, adapter_ids)
+        if st is None:
+            B, k1 = hidden.shape[:2]
+            ad = self._with_adapters(adapters, adapter_ids, hidden)
+            a = self._args(hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, B, k1 - 1, gate_source, fallback, w_scale, a8)
+            if fresh:
+                a.flags = HOLA_ARG_CLEAR_STATUS
+            st = self.lib.hola_verify_adapters(self._ctx, ctypes.byref(a), ctypes.byref(ad), _stream_ptr(stream))
         if st:
             _check(self.lib, self._ctx, st, "hola_verify_adapters")
         return out

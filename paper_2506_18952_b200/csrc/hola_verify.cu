@@ -53,6 +53,7 @@
 #include <cooperative_groups.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "../../include/hola_verify.h"
 

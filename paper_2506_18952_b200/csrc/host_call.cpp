@@ -1,5 +1,5 @@
 // The host side of a call on torch tensors, in native code: reads the tensors, fills hola_verify_args and calls the C ABI;
-// makes the output tensors of a call that is given none.  What a call costs the host bounds small problems.  us, Python -> native:
+// makes the output tensors of a call that is given none (scores: all of it in one).  What a call costs the host bounds small problems.  us, Python -> native:
 // arguments filled and a call that is refused 3.5 -> 0.8, five output tensors 8.2 -> 5.1, seven 11.7 -> 7.0, beside 5 for the two
 // launches; whole calls: one sequence, V = 1000 10.45 -> 9.75; three, V = 5000, fresh outputs 19.75 -> 13.2; host entry, two sequences,
 // V = 10000 42.1 -> 37.4; mixed-width quantiser, 1000 x 128 50 -> 13.8.
@@ -20,6 +20,8 @@
 namespace {
 
 typedef hola_status (*EntryFn)(hola_ctx*, const hola_verify_args*, void*);
+typedef hola_status (*AdapterFn)(hola_ctx*, const hola_verify_args*, const hola_adapters*, void*);
+typedef hola_status (*ScoreFn)(const hola_logprobs_args*, void*);
 
 // A tensor whose memory can be handed over as it is: null for anything else.
 const at::Tensor* plain(PyObject* o) {
@@ -77,11 +79,12 @@ bool address(PyObject* o, void** p) {
 PyObject *n_accept, *n_next, *n_entropy, *n_logZ, *n_logits, *n_status, *n_dent;
 
 // call(function, ctx, H, V, hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, draws, flags, gate_source, fallback, w_scale,
-//      a8, wmix, stream) -> status, or None where the caller has to go the long way.  wmix: address of the hola_wmix of a head of
-// mixed widths, whose first buffer is W_lm then, or 0.
+//      a8, wmix, stream[, adapters, ids, device]) -> status, or None where the caller has to go the long way.  wmix: address of the
+// hola_wmix of a head of mixed widths, whose first buffer is W_lm then, or 0.  adapters: address of the hola_adapters of a bank that
+// fits the context, whose function takes it; ids: the sequences' slots, on the context's device.
 PyObject* call(PyObject*, PyObject* const* v, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 19) { PyErr_SetString(PyExc_TypeError, "call() takes 19 arguments"); return nullptr; }
+  if (n != 19 && n != 22) { PyErr_SetString(PyExc_TypeError, "call() takes 19 or 22 arguments"); return nullptr; }
   void *fn = nullptr, *ctx = nullptr, *stream = nullptr, *wmix = nullptr, *p = nullptr;
   hola_verify_args a = {};
   int32_t H = 0, V = 0, draws = 0;
@@ -147,9 +150,21 @@ PyObject* call(PyObject*, PyObject* const* v, Py_ssize_t n) {
     p = nullptr; if (!output(out, n_dent, &p)) Py_RETURN_NONE;
     a.draft_entropy = static_cast<float*>(p);
   }
+  hola_adapters ad = {};
+  if (n == 22) {
+    void* bank = nullptr;
+    int32_t device = 0;
+    const at::Tensor* ids = plain(v[20]);
+    if (!address(v[19], &bank) || !bank || !int32(v[21], &device) || !ids || ids->scalar_type() != at::kInt || !ids->is_cuda() ||
+        ids->get_device() != device || ids->dim() != 1 || ids->size(0) != a.B || !ids->is_contiguous())
+      Py_RETURN_NONE;
+    ad = *static_cast<const hola_adapters*>(bank);
+    ad.ids = static_cast<const int32_t*>(ids->data_ptr());
+  }
   hola_status s;
   Py_BEGIN_ALLOW_THREADS
-  s = reinterpret_cast<EntryFn>(fn)(static_cast<hola_ctx*>(ctx), &a, stream);
+  s = n == 22 ? reinterpret_cast<AdapterFn>(fn)(static_cast<hola_ctx*>(ctx), &a, &ad, stream)
+              : reinterpret_cast<EntryFn>(fn)(static_cast<hola_ctx*>(ctx), &a, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(s);
   END_HANDLE_TH_ERRORS
@@ -192,6 +207,99 @@ PyObject* outputs(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (x[5] && (!put(n_accept, accept) || !put(n_next, next))) return nullptr;
   if (x[6] && !put(n_dent, dent)) return nullptr;
   Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// score(function, logits, tokens, n_top, logZ, draft_tok, accept_len, next_tok, emitted, want_rank, status, current device, stream)
+// -> (status, logprob, rank, entropy, logZ, top_ids, top_logprobs), or None where the caller has to go the long way: logits that are
+// not on the current device, rows that are not evenly spaced, anything that will be refused, nothing to do.
+PyObject* score(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 13) { PyErr_SetString(PyExc_TypeError, "score() takes 13 arguments"); return nullptr; }
+  void *fn = nullptr, *stream = nullptr;
+  int32_t device = 0;
+  hola_logprobs_args a = {};
+  if (!address(v[0], &fn) || !fn || !int32(v[3], &a.n_top) || !int32(v[11], &device) || !address(v[12], &stream)) Py_RETURN_NONE;
+  const at::Tensor* l = plain(v[1]);
+  if (!l || !l->is_cuda() || l->get_device() != device || l->dim() < 1 || l->numel() == 0 || l->numel() / l->size(-1) > INT32_MAX ||
+      l->size(-1) > INT32_MAX)
+    Py_RETURN_NONE;
+  const at::ScalarType type = l->scalar_type();
+  if (type != at::kFloat && type != at::kBFloat16 && type != at::kHalf) Py_RETURN_NONE;
+  a.l_dtype = type == at::kFloat ? HOLA_L_F32 : type == at::kBFloat16 ? HOLA_L_BF16 : HOLA_L_F16;
+  const int64_t axes = l->dim() - 1, V = l->size(axes);
+  int64_t rows = 1, stride = -1;
+  if (V > 1 && l->stride(axes) != 1) Py_RETURN_NONE;
+  for (int64_t i = axes - 1; i >= 0; --i) {
+    if (l->size(i) == 1) continue;
+    if (stride < 0) stride = l->stride(i);
+    else if (l->stride(i) != stride * rows) Py_RETURN_NONE;
+    rows *= l->size(i);
+  }
+  a.rows = static_cast<int32_t>(rows); a.V = static_cast<int32_t>(V);
+  a.logits = l->data_ptr(); a.row_stride = stride < 0 ? V : stride;
+  // (contiguous, on the logits' device, of that type and shape)
+  auto operand = [&](PyObject* o, at::ScalarType t, at::IntArrayRef size) -> void* {
+    const at::Tensor* x = plain(o);
+    return x && x->is_cuda() && x->get_device() == device && x->scalar_type() == t && x->is_contiguous() && x->sizes() == size ? x->data_ptr()
+                                                                                                                              : nullptr;
+  };
+  const at::IntArrayRef shape = l->sizes().slice(0, axes);
+  if (v[4] != Py_None) {
+    a.logZ_in = static_cast<const float*>(operand(v[4], at::kFloat, shape));
+    if (!a.logZ_in) Py_RETURN_NONE;
+  }
+  at::DimVector per_row(shape.begin(), shape.end());
+  bool some = false;
+  if (v[8] == Py_True) {
+    if (v[2] != Py_None || axes != 2 || !a.logZ_in) Py_RETURN_NONE;
+    const int64_t B = shape[0], k = shape[1] - 1;
+    a.k = static_cast<int32_t>(k); a.T = 1;
+    if (k > 0 && !(a.draft_tok = static_cast<const int32_t*>(operand(v[5], at::kInt, {B, k})))) Py_RETURN_NONE;
+    a.accept_len = static_cast<const int32_t*>(operand(v[6], at::kInt, {B}));
+    a.next_tok = static_cast<const int32_t*>(operand(v[7], at::kInt, {B}));
+    if (!a.accept_len || !a.next_tok) Py_RETURN_NONE;
+    some = true;
+  } else if (v[2] != Py_None) {
+    const at::Tensor* t = plain(v[2]);
+    if (!t || t->dim() < axes || t->dim() > axes + 1 || t->numel() == 0 || t->numel() / rows > INT32_MAX) Py_RETURN_NONE;
+    a.T = t->dim() > axes ? static_cast<int32_t>(t->size(axes)) : 1;
+    if (t->dim() > axes) per_row.push_back(a.T);
+    a.tokens = static_cast<const int32_t*>(operand(v[2], at::kInt, per_row));
+    if (!a.tokens) Py_RETURN_NONE;
+    some = true;
+  }
+  const int want_rank = PyObject_IsTrue(v[9]);
+  if (want_rank < 0) return nullptr;
+  if (a.n_top < 0 || a.n_top > 32 || a.n_top > a.V || (!some && a.n_top == 0 && a.logZ_in)) Py_RETURN_NONE;
+  if (v[10] != Py_None && !(a.status_word = static_cast<uint32_t*>(operand(v[10], at::kInt, {1})))) Py_RETURN_NONE;
+  at::Tensor logprob, rank, entropy, logZ, top_ids, top_logprobs;
+  hola_status s = HOLA_OK;
+  Py_BEGIN_ALLOW_THREADS
+  try {
+    const auto f32 = at::TensorOptions().dtype(at::kFloat).device(l->device());
+    const auto i32 = f32.dtype(at::kInt);
+    if (some) { logprob = at::empty(per_row, f32); a.logprob = static_cast<float*>(logprob.data_ptr()); }
+    if (some && want_rank) { rank = at::empty(per_row, i32); a.rank = static_cast<int32_t*>(rank.data_ptr()); }
+    if (!a.logZ_in) {
+      entropy = at::empty(shape, f32); a.entropy = static_cast<float*>(entropy.data_ptr());
+      logZ = at::empty(shape, f32); a.logZ = static_cast<float*>(logZ.data_ptr());
+    }
+    if (a.n_top > 0) {
+      at::DimVector top(shape.begin(), shape.end());
+      top.push_back(a.n_top);
+      top_ids = at::empty(top, i32); a.top_ids = static_cast<int32_t*>(top_ids.data_ptr());
+      top_logprobs = at::empty(top, f32); a.top_logprobs = static_cast<float*>(top_logprobs.data_ptr());
+    }
+    s = reinterpret_cast<ScoreFn>(fn)(&a, stream);
+  } catch (...) {
+    Py_BLOCK_THREADS
+    throw;
+  }
+  Py_END_ALLOW_THREADS
+  auto wrap = [](const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); };
+  return Py_BuildValue("iNNNNNN", static_cast<int>(s), wrap(logprob), wrap(rank), wrap(entropy), wrap(logZ), wrap(top_ids),
+                       wrap(top_logprobs));
   END_HANDLE_TH_ERRORS
 }
 
@@ -271,6 +379,7 @@ PyObject* quantize(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL, nullptr},
     {"outputs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(outputs)), METH_FASTCALL, nullptr},
+    {"score", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(score)), METH_FASTCALL, nullptr},
     {"quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantize)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -4,17 +4,22 @@
 // One pass over a row of V logits:  m = max l,  s = sum e^(l-m),  t = sum e^(l-m)(l-m),  logZ = m + ln s,  H = ln s - t/s,
 // logprob(x) = (l[x] - m) - ln s,  rank(x) = #{v : l[v] > l[x], or l[v] = l[x] and v < x},  and the n entries that come first in the
 // order (logit descending, id ascending).  A row is one CTA's or is cut into parts for the CTAs of a cluster, which merge over
-// distributed shared memory; thread i of a part takes groups of eight neighbouring entries i, i + 256, ...
+// distributed shared memory; thread i of a part takes groups i, i + 256, ... of 32 bytes (one load each).
 //
-// The alternatives cost the pass next to nothing: every thread keeps the maximum of what it has seen (which the running sums
-// need anyway) and the group that it first met it in.  Let the n-th best of the threads' (maximum, group) pairs in the order
-// (value descending, group ascending) be (w, g): at least n entries lie at or before it (those maxima), so every one of the
+// The alternatives cost the pass next to nothing: every thread keeps the maximum of what it has seen and the group that it first
+// met it in.  Every eight threads put the best of their (maximum, group) pairs, in the order (value descending, group ascending),
+// on a board of 32; let the n-th best there be (w, g).  At least n entries lie at or before it (those maxima), so every one of the
 // part's n best has a value above w, or w itself in a group up to g.  Only threads whose own pair is at or before (w, g) can hold
-// such entries; a warp reads those threads' groups again, out of the L2, and keeps the best 32 it meets.
+// such entries.  A thread holds on to the group of its maximum; where its second-best group may qualify too, its groups are read
+// again, out of the L2.  What qualifies (n entries and some more) goes to the row's first CTA, which places each entry by counting
+// those before it.
 
 constexpr int kLpThreads = 256;
 constexpr int kLpWarps = kLpThreads / 32;
-constexpr int kLpGroup = 8;            // neighbouring entries that a thread takes at once
+constexpr int kLpGroupBytes = 32;      // neighbouring entries that a thread loads at once
+constexpr int kLpDepth = 2;            // groups that it has on the way
+constexpr int kLpSpots = 64;           // entries that a part may send unsorted; beyond that it sends its 32 best
+constexpr float kLpSlack = 4.f;        // how far a maximum may rise above the point that the sums are taken about
 constexpr int kLpMaxTop = 32;          // alternatives: a sorted list lies across a warp, one entry per lane
 constexpr int kLpTok = 4;              // tokens ranked in one pass (counters in registers)
 constexpr int kLpMaxCluster = 8;
@@ -45,6 +50,7 @@ struct LpPart {
   float m, s, t;
   unsigned bad;
   int count[kLpTok];
+  int spots;                   // entries it sends
 };
 
 // Floats in the order of their values as unsigned whole numbers (one zero; NaN does not occur).
@@ -84,6 +90,15 @@ __device__ __forceinline__ uint64_t lp_merge(uint64_t a, uint64_t reversed, int 
   for (int stride = 16; stride > 0; stride >>= 1) a = lp_exchange(a, stride, (lane & stride) == 0);
   return a;
 }
+// The first `n` of 32 waiting keys into a sorted list.  (Out of line: rarely called, and code that is not fetched costs nothing.)
+__device__ __noinline__ uint64_t lp_take_in(uint64_t best, const uint64_t* waiting, int n) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  const uint64_t a = lp_sort(lane < n ? waiting[lane] : 0, lane);
+  best = lp_merge(best, __shfl_sync(0xffffffffu, a, 31 - lane), lane);
+  __syncwarp();
+  return best;
+}
 // The lists of all warps of the CTA into warp 0's.  `lists`: [kLpWarps][32] in shared memory.
 __device__ __forceinline__ uint64_t lp_merge_warps(uint64_t a, uint64_t* lists, int warp, int lane) {
   lists[warp * 32 + lane] = a;
@@ -98,11 +113,6 @@ __device__ __forceinline__ uint64_t lp_merge_warps(uint64_t a, uint64_t* lists, 
   return a;
 }
 
-__device__ __forceinline__ float min3(float a, float b, float c) {
-  float d;
-  asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {     // NaN where one of them is
   float d;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -113,163 +123,328 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// 16 bytes that this kernel never sees change, past the L1.
-__device__ __forceinline__ uint4 load_once(const void* p) {
-  uint4 x;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
-  return x;
-}
-
-// Eight neighbouring logits as loaded and as fp32.
-template <typename T>
-struct LpRaw {
-  static constexpr int kPieces = kLpGroup * sizeof(T) / 16;
-  uint4 x[kPieces];
-};
 __device__ __forceinline__ float lp_float(float x) { return x; }
 __device__ __forceinline__ float lp_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float lp_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ void lp_expand(const LpRaw<float>& r, float* f) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    f[4 * i] = __uint_as_float(r.x[i].x); f[4 * i + 1] = __uint_as_float(r.x[i].y);
-    f[4 * i + 2] = __uint_as_float(r.x[i].z); f[4 * i + 3] = __uint_as_float(r.x[i].w);
-  }
-}
-__device__ __forceinline__ void lp_expand(const LpRaw<__nv_bfloat16>& r, float* f) {
-  const uint32_t w[4] = {r.x[0].x, r.x[0].y, r.x[0].z, r.x[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void lp_expand(const LpRaw<__half>& r, float* f) {
-  const uint32_t w[4] = {r.x[0].x, r.x[0].y, r.x[0].z, r.x[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-    f[2 * i] = y.x;
-    f[2 * i + 1] = y.y;
-  }
-}
 
-// A row as groups that start on 16-byte boundaries: group j holds entries 8 j - off ... 8 j - off + 7, the first and the last
-// one perhaps fewer (what they lack reads as -inf).
+// A group of neighbouring logits as loaded.
+template <typename T>
+struct LpGroup {
+  static constexpr int kEntries = kLpGroupBytes / sizeof(T);
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const T* p) {     // 32 bytes that this kernel never sees change, past the L1
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+  }
+  // Entries 2 i and 2 i + 1.
+  __device__ __forceinline__ void pair(int i, float& lo, float& hi) const {
+    if (sizeof(T) == 4) {
+      lo = __uint_as_float(w[(2 * i) & 7]); hi = __uint_as_float(w[(2 * i + 1) & 7]);
+    } else if (std::is_same<T, __nv_bfloat16>::value) {
+      lo = __uint_as_float(w[i & 7] << 16); hi = __uint_as_float(w[i & 7] & 0xffff0000u);
+    } else {
+      const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[i & 7]));
+      lo = y.x; hi = y.y;
+    }
+  }
+  __device__ __forceinline__ float entry(int i) const {
+    float lo, hi;
+    pair(i >> 1, lo, hi);
+    return i & 1 ? hi : lo;
+  }
+  __device__ __forceinline__ float largest() const {     // NaN where there is one
+    if (sizeof(T) == 4) {
+      const float* f = reinterpret_cast<const float*>(w);
+      return max3_nan(max3_nan(f[0], f[1], f[2]), max3_nan(f[3], f[4], f[5]), max3_nan(f[6], f[7], f[7]));
+    }
+    uint32_t m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = w[i];
+#pragma unroll
+    for (int n = 4; n > 0; n >>= 1)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        if (std::is_same<T, __nv_bfloat16>::value) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m[i]) : "r"(m[i + n]));
+        else asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(m[i]) : "r"(m[i + n]));
+      }
+    LpGroup<T> g;
+    g.w[0] = m[0];
+    float lo, hi;
+    g.pair(0, lo, hi);
+    return max3_nan(lo, hi, hi);
+  }
+};
+
+// A row as groups that start on 32-byte boundaries: with E entries in one, group j holds entries E j - off ... E j - off + E - 1, the
+// first and the last one perhaps fewer (what they lack reads as -inf).
 template <typename T>
 struct LpRow {
-  const T* base;               // entry -off, on a 16-byte boundary (not read before entry 0)
+  static constexpr int E = LpGroup<T>::kEntries;
+  const T* base;               // entry -off, on a 32-byte boundary (not read before entry 0)
   int off, V, groups;          // groups whole_begin .. whole_end - 1 are whole
   int whole_begin, whole_end;
   __device__ __forceinline__ LpRow(const T* row, int V_) : V(V_) {
-    off = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
+    off = static_cast<int>((reinterpret_cast<uintptr_t>(row) & (kLpGroupBytes - 1u)) / sizeof(T));
     base = row - off;
-    groups = static_cast<int>((static_cast<long long>(V_) + off + kLpGroup - 1) / kLpGroup);
+    groups = static_cast<int>((static_cast<long long>(V_) + off + E - 1) / E);
     whole_begin = off ? 1 : 0;
-    whole_end = static_cast<int>((static_cast<long long>(V_) + off) / kLpGroup);
+    whole_end = static_cast<int>((static_cast<long long>(V_) + off) / E);
   }
   __device__ __forceinline__ bool whole(int j) const { return j >= whole_begin && j < whole_end; }
-  __device__ __forceinline__ LpRaw<T> fetch(int j) const {        // (whole groups)
-    LpRaw<T> r;
-    const char* p = reinterpret_cast<const char*>(base + static_cast<size_t>(j) * kLpGroup);
-#pragma unroll
-    for (int i = 0; i < LpRaw<T>::kPieces; ++i) r.x[i] = load_once(p + 16 * i);
-    return r;
+  __device__ __forceinline__ int first(int j) const { return j * E - off; }
+  __device__ __forceinline__ LpGroup<T> get(int j) const {
+    if (!whole(j)) return get_ragged(j);
+    LpGroup<T> g;
+    g.load(base + static_cast<size_t>(j) * E);
+    return g;
   }
-  __device__ __forceinline__ void get(int j, float* f) const {
-    if (whole(j)) {
-      lp_expand(fetch(j), f);
-    } else {
+  __device__ __noinline__ LpGroup<T> get_ragged(int j) const {
+    LpGroup<T> g;
+    {
+      const uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __nv_bfloat16>::value ? 0xff80u : 0xfc00u;
 #pragma unroll
-      for (int i = 0; i < kLpGroup; ++i) {
-        const long long v = static_cast<long long>(j) * kLpGroup - off + i;
-        f[i] = v >= 0 && v < V ? lp_float(base[v + off]) : -CUDART_INF_F;
+      for (int i = 0; i < 8; ++i) g.w[i] = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const long long v = static_cast<long long>(j) * E - off + i;
+        uint32_t bits = none;
+        if (v >= 0 && v < V) {
+          if (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t*>(base)[v + off];
+          else bits = reinterpret_cast<const uint16_t*>(base)[v + off];
+        }
+        if (sizeof(T) == 4) g.w[i & 7] = bits;
+        else g.w[(i >> 1) & 7] |= bits << (16 * (i & 1));
       }
     }
+    return g;
   }
-  __device__ __forceinline__ int first(int j) const { return j * kLpGroup - off; }
 };
 
-// One thread's view of its part of the row.
-template <bool kSums, bool kTop, bool kRank>
-struct LpThread {
-  float m, s, t;
-  int at;                      // group that the maximum was first met in
-  bool bad;
-  int count[kLpTok];
+// A token that is ranked.  An entry comes before it where its logit is larger, or as large and its id smaller: in groups before the
+// token's own where !(l <= below), `below` the type's next number under its logit (for -inf a NaN, and every entry counts), in groups
+// behind it where !(l <= l[x]).
+template <typename T>
+struct LpToken {
+  int x;
+  float l;
+  uint32_t limit[2];           // 0: behind it, 1: before it; the number's bits, 16-bit ones twice
+  __device__ __forceinline__ void set(int x_, bool have, const T* at) {
+    x = x_;
+    uint32_t b;
+    if (sizeof(T) == 4) {
+      b = have ? *reinterpret_cast<const uint32_t*>(at) : 0x7fffffffu;
+      l = __uint_as_float(b);
+      if (b == 0x80000000u) b = 0u;
+      limit[0] = b;
+      limit[1] = b == 0u ? 0x80000001u : b & 0x80000000u ? b + 1u : b - 1u;
+    } else {
+      b = have ? *reinterpret_cast<const uint16_t*>(at) : 0x7fffu;
+      LpGroup<T> g;
+      g.w[0] = b;
+      l = g.entry(0);
+      if (b == 0x8000u) b = 0u;
+      limit[0] = b * 0x10001u;
+      limit[1] = (b == 0u ? 0x8001u : b & 0x8000u ? b + 1u : b - 1u) * 0x10001u;
+    }
+  }
+};
 
-  __device__ __forceinline__ explicit LpThread(int first) : s(0.f), t(0.f), at(first), bad(false), count{0, 0, 0, 0} {
-    m = -CUDART_INF_F;
+// Entries of the group above a limit (or not comparable with it): 1.0 for each, added up two at a time.
+template <typename T>
+__device__ __forceinline__ int lp_count(const LpGroup<T>& g, uint32_t limit) {
+  if (sizeof(T) == 4) {
+    uint64_t n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      g.pair(i, a, b);
+      asm("set.gtu.f32.f32 %0, %0, %1;" : "+f"(a) : "f"(__uint_as_float(limit)));
+      asm("set.gtu.f32.f32 %0, %0, %1;" : "+f"(b) : "f"(__uint_as_float(limit)));
+      n = add2(n, pack2(a, b));
+    }
+    float a, b;
+    unpack2(n, a, b);
+    return static_cast<int>(a + b);
+  }
+  LpGroup<T> n;
+  n.w[0] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (std::is_same<T, __nv_bfloat16>::value) {
+      const __nv_bfloat162 one = __hgtu2(*reinterpret_cast<const __nv_bfloat162*>(&g.w[i]), *reinterpret_cast<const __nv_bfloat162*>(&limit));
+      const __nv_bfloat162 sum = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&n.w[0]), one);
+      n.w[0] = *reinterpret_cast<const uint32_t*>(&sum);
+    } else {
+      const __half2 one = __hgtu2(*reinterpret_cast<const __half2*>(&g.w[i]), *reinterpret_cast<const __half2*>(&limit));
+      const __half2 sum = __hadd2(*reinterpret_cast<const __half2*>(&n.w[0]), one);
+      n.w[0] = *reinterpret_cast<const uint32_t*>(&sum);
+    }
+  }
+  float a, b;
+  n.pair(0, a, b);
+  return static_cast<int>(a + b);
+}
+
+// One thread's view of its part of the row.  Its sums are taken about `ref`, which trails the maximum by kLpSlack at most: a rise of
+// the maximum then rarely makes a warp rescale.  In units of ln 2: x = l log2 e - ref log2 e, s = sum 2^x, t = sum 2^x x.
+template <typename T, bool kSums, bool kTop, int kRank>
+struct LpThread {
+  static constexpr int E = LpGroup<T>::kEntries;
+  float m, second;             // maximum, and that of the other groups
+  float ref, rise, shift;      // rise: where the next rescaling is due; shift = -ref log2 e
+  uint64_t s2, t2;             // two halves of either sum
+  int at;                      // group that the maximum was first met in
+  LpGroup<T> held;             // (alternatives) its entries
+  bool bad;
+  int count[kRank ? kRank : 1];
+
+  __device__ __forceinline__ explicit LpThread(int first) : shift(0.f), s2(0), t2(0), at(first), bad(false) {
+    m = second = ref = rise = -CUDART_INF_F;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) held.w[i] = 0;
+#pragma unroll
+    for (int q = 0; q < (kRank ? kRank : 1); ++q) count[q] = 0;
   }
 
-  __device__ __forceinline__ void take(const float* f, int j, int v0, const float* lx, const int* x, float lx_min, int n) {
-    const float hi = max3_nan(max3_nan(f[0], f[1], f[2]), max3_nan(f[3], f[4], f[5]), max3_nan(f[6], f[7], f[7]));
-    if (!(hi < CUDART_INF_F)) { bad = true; return; }
-    if (kRank && hi >= lx_min) {
+  // Group j, whose first entry is v0; `ragged`: it lacks some.
+  __device__ __forceinline__ void take(const LpGroup<T>& g, int j, int v0, const LpToken<T>* tok, float l_min, bool ragged) {
+    const float top = g.largest();
+    if (!kSums && !(top < CUDART_INF_F)) bad = true;
+    if (kRank && top >= l_min) {
 #pragma unroll
-      for (int q = 0; q < kLpTok; ++q) {
-        if (q < n && hi >= lx[q]) {
-#pragma unroll
-          for (int i = 0; i < kLpGroup; ++i)
-            count[q] += f[i] > lx[q] || (f[i] == lx[q] && v0 + i < x[q] && v0 + i >= 0) ? 1 : 0;
+      for (int q = 0; q < kRank; ++q) {
+        if (!(top >= tok[q].l)) continue;
+        if (ragged || (v0 <= tok[q].x && v0 + E > tok[q].x)) {
+          for (int i = 0; i < E; ++i) {
+            const float l = g.entry(i);
+            count[q] += v0 + i >= 0 && (l > tok[q].l || (l == tok[q].l && v0 + i < tok[q].x)) ? 1 : 0;
+          }
+        } else {
+          count[q] += lp_count(g, v0 < tok[q].x ? tok[q].limit[1] : tok[q].limit[0]);
         }
       }
     }
-    if (hi > m) {
-      if (kSums && m != -CUDART_INF_F) {
-        const float d = lp_below(m, hi), e = ex2_approx(d * kLog2e);
-        t = e * (t + d * s);
-        s *= e;
-      }
-      m = hi;
+    if (kTop) second = fmaxf(second, fminf(top, m));
+    if (top > m || (kTop && at == j)) {                  // (its first group is held whatever it is)
+      m = top;
       at = j;
+      if (kTop) held = g;
     }
-    if (!kSums || hi == -CUDART_INF_F) return;
-    const float lo = min3(min3(f[0], f[1], f[2]), min3(f[3], f[4], f[5]), fminf(f[6], f[7]));
-    if (lo > -1e37f) {
-      const uint64_t mm = pack2(-m, -m), l2e = pack2(kLog2e, kLog2e);
-      uint64_t s2 = pack2(0.f, 0.f), a2 = pack2(0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < kLpGroup / 2; ++i) {
-        const uint64_t d2 = add2(pack2(f[2 * i], f[2 * i + 1]), mm);
-        float x0, x1;
-        unpack2(mul2(d2, l2e), x0, x1);
-        const uint64_t e2 = pack2(ex2_approx(x0), ex2_approx(x1));
-        s2 = add2(s2, e2);
-        a2 = fma2(e2, d2, a2);
+    if (!kSums || top == -CUDART_INF_F) return;
+    if (top > rise) {
+      const float old = shift;
+      shift = fabsf(top) < 1e37f ? -top * kLog2e : CUDART_NAN_F;      // (NaN: every group goes the long way below)
+      if (ref != -CUDART_INF_F) {
+        float dx = shift - old;
+        if (!(dx == dx)) dx = (ref - top) * kLog2e;
+        dx = fmaxf(dx, -1e28f);
+        const float e = ex2_approx(dx);
+        const uint64_t e2 = pack2(e, e);
+        t2 = mul2(fma2(pack2(dx, dx), s2, t2), e2);
+        s2 = mul2(s2, e2);
       }
-      float a, b, c, d;
-      unpack2(s2, a, b);
-      unpack2(a2, c, d);
-      s += a + b;
-      t += c + d;
-    } else {
-      // masked entries (-inf, or as low as the type goes): differences are kept finite, their exponentials are zeros
-#pragma unroll
-      for (int i = 0; i < kLpGroup; ++i) {
-        const float d = lp_below(f[i], m), e = ex2_approx(d * kLog2e);
-        s += e;
-        t = fmaf(e, d, t);
-      }
+      ref = top;
+      rise = top + kLpSlack;
     }
+    const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
+    uint64_t ps[2] = {0, 0}, pt[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+      float a, b;
+      g.pair(i, a, b);
+      const uint64_t x = fma2(pack2(a, b), l2e, sh);
+      unpack2(x, a, b);
+      const uint64_t e = pack2(ex2_approx(a), ex2_approx(b));
+      ps[i & 1] = add2(ps[i & 1], e);
+      pt[i & 1] = fma2(e, x, pt[i & 1]);
+    }
+    const uint64_t both = add2(pt[0], pt[1]);
+    float a, b;
+    unpack2(both, a, b);
+    if (a + b == a + b) {
+      s2 = add2(s2, add2(ps[0], ps[1]));
+      t2 = add2(t2, both);
+      return;
+    }
+    // 0 * -inf: entries that are masked (-inf, or as low as the type goes), or too large for x; or there is no distribution
+    if (!(top < CUDART_INF_F)) { bad = true; return; }
+    float s = 0.f, t = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float x = lp_below(g.entry(i), ref) * kLog2e, e = ex2_approx(x);
+      s += e;
+      t = fmaf(e, x, t);
+    }
+    s2 = add2(s2, pack2(s, 0.f));
+    t2 = add2(t2, pack2(t, 0.f));
+  }
+
+  // The sums about the thread's own maximum: m, sum e^(l-m), sum e^(l-m)(l-m).
+  __device__ __forceinline__ void sums(float& s, float& t) const {
+    float a, b, c, d;
+    unpack2(s2, a, b);
+    unpack2(t2, c, d);
+    s = a + b;
+    t = c + d;
+    if (m == -CUDART_INF_F) return;
+    const float x = shift == shift ? fmaf(m, kLog2e, shift) : (m - ref) * kLog2e;     // (of the maximum, as it was summed)
+    const float e = ex2_approx(-x);
+    t = kLn2 * (e * fmaf(-x, s, t));
+    s *= e;
   }
 };
 
-// What bounds it: HBM for large batches; for a few rows the chain token -> its logit -> pass -> merges.
-template <typename T, bool kSums, bool kTop, bool kRank>
-__global__ void __launch_bounds__(kLpThreads, 4) token_logprobs_kernel(const LpParams p, int C) {
-  __shared__ uint64_t lists[kLpWarps * 32];
-  __shared__ uint64_t fresh[kLpWarps][32];               // candidates a warp has met and not sorted in yet
-  __shared__ uint64_t cluster_lists[kLpMaxCluster][kTop ? 32 : 1];
+// Entries of group j at or before (w, g_last) to the part's spots, as far as there is room.
+template <typename T>
+__device__ __forceinline__ void lp_send(const LpGroup<T>& g, const LpRow<T>& r, int j, uint64_t lim, float w, int g_last, uint64_t* spots,
+                                        int* n_spots) {
+  if (lim != 0) {
+    const float top = g.largest();
+    if (!(top > w || (top == w && j <= g_last))) return;
+  }
+  const int v0 = r.first(j);
+#pragma unroll
+  for (int e = 0; e < LpGroup<T>::kEntries; ++e) {
+    const float l = g.entry(e);
+    if ((lim == 0 || l > w || (l == w && j <= g_last)) && v0 + e >= 0 && v0 + e < r.V) {
+      const int spot = atomicAdd(n_spots, 1);
+      if (spot < kLpSpots) spots[spot] = lp_key(l, v0 + e);
+    }
+  }
+}
+
+// Writes what a row without a token gets (see the header), or one whose accept length cannot be.
+__device__ __forceinline__ void lp_no_token(const LpParams& p, int row, bool valid, bool rank) {
+  const float none = valid ? 0.f : CUDART_NAN_F;
+  if (threadIdx.x == 0) {
+    p.logprob[row] = none;
+    if (rank) p.rank[row] = -1;
+    if (!valid && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  }
+  if (threadIdx.x < p.n_top) {
+    p.top_ids[static_cast<size_t>(row) * p.n_top + threadIdx.x] = -1;
+    p.top_logprobs[static_cast<size_t>(row) * p.n_top + threadIdx.x] = none;
+  }
+}
+
+// What bounds it: HBM for large batches; for a few rows the chain token -> its logit -> pass -> board -> second look -> counting.
+template <typename T, bool kSums, bool kTop, int kRank>
+__global__ void __launch_bounds__(kLpThreads, kSums && sizeof(T) == 2 ? 3 : 4) token_logprobs_kernel(const LpParams p, int C) {
+  constexpr int E = LpGroup<T>::kEntries;
+  __shared__ uint64_t spots[kTop ? kLpMaxCluster : 1][kLpSpots];       // first CTA: what every part sends
+  __shared__ LpPart parts[kLpMaxCluster];
+  __shared__ uint64_t own_spots[kTop ? kLpSpots : 1];
+  __shared__ uint64_t lists[kTop ? kLpWarps * 32 : 1];   // board, or the warps' sorted lists
+  __shared__ uint64_t fresh[kTop ? kLpWarps : 1][32];
   __shared__ uint8_t looked_at[kLpWarps][32];
   __shared__ LpPart warp_parts[kLpWarps];
-  __shared__ LpPart cluster_parts[kLpMaxCluster];
-  __shared__ uint64_t limit;
+  __shared__ int n_spots;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x / C, part = blockIdx.x - row * C;
   // the other CTAs of the cluster have started (looked at before anything is sent to them)
   if (C > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+  if (tid == 0) n_spots = 0;
+  if (kTop && tid < kLpSpots) own_spots[tid] = 0;
   grid_dependency_wait();
   grid_dependency_release();
 
@@ -280,7 +455,6 @@ __global__ void __launch_bounds__(kLpThreads, 4) token_logprobs_kernel(const LpP
 
   // What the row is asked for.  (Emitted form: row j of a sequence holds a token up to its accept length.)
   int j_seq = 0, len = 0;
-  unsigned flags = 0;
   if (p.accept_len) {
     const int b = row / (p.k + 1);
     j_seq = row - b * (p.k + 1);
@@ -288,90 +462,55 @@ __global__ void __launch_bounds__(kLpThreads, 4) token_logprobs_kernel(const LpP
     const bool valid = len >= 0 && len <= p.k;
     if (!valid || j_seq > len) {                         // (the same in every CTA of the cluster)
       if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
-      if (part != 0) return;
-      // no token: nothing is read; an accept length that cannot be: NaN
-      const float none = valid ? 0.f : CUDART_NAN_F;
-      if (tid == 0) {
-        p.logprob[row] = none;
-        if (kRank) p.rank[row] = -1;
-        if (!valid && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
-      }
-      if (kTop && tid < p.n_top) {
-        p.top_ids[static_cast<size_t>(row) * p.n_top + tid] = -1;
-        p.top_logprobs[static_cast<size_t>(row) * p.n_top + tid] = none;
-      }
+      if (part == 0) lp_no_token(p, row, valid, kRank > 0);
       return;
     }
   }
 
   // The first groups are on their way while the tokens and their logits are looked up.
-  constexpr int kUnroll = 4 / LpRaw<T>::kPieces;
-  constexpr int kAhead = (kUnroll - 1) * kLpThreads;
-  LpRaw<T> raw[kUnroll];
-  const int whole_end = min(j_end, r.whole_end);
+  LpGroup<T> next[kLpDepth];
   int j = j_begin + tid;
-  const bool ragged_first = j < j_end && j < r.whole_begin;
-  if (ragged_first) j += kLpThreads;
-  bool more = j + kAhead < whole_end;
-  if (more) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u] = r.fetch(j + u * kLpThreads);
-  }
+  for (int u = 0; u < kLpDepth; ++u)
+    if (r.whole(j + u * kLpThreads) && j + u * kLpThreads < j_end) next[u].load(r.base + static_cast<size_t>(j + u * kLpThreads) * E);
 
-  int x[kLpTok];
-  float lx[kLpTok], lx_min = CUDART_INF_F;
+  LpToken<T> tok[kRank ? kRank : 1];
+  float l_min = CUDART_INF_F;
   const int n = p.tn;
 #pragma unroll
-  for (int q = 0; q < kLpTok; ++q) {
-    x[q] = -1;
-    if (kRank && q < n) {
-      x[q] = p.accept_len ? (j_seq < len ? p.draft_tok[static_cast<size_t>(row / (p.k + 1)) * p.k + j_seq] : p.next_tok[row / (p.k + 1)])
-                          : p.tokens[static_cast<size_t>(row) * p.T + p.t0 + q];
-    }
-    const bool have = x[q] >= 0 && x[q] < p.V;
-    lx[q] = have ? lp_float(r.base[static_cast<size_t>(x[q]) + r.off]) : CUDART_NAN_F;
-    if (have) lx_min = fminf(lx_min, lx[q]);
+  for (int q = 0; q < kRank; ++q) {
+    int x = -1;
+    if (q < n)
+      x = p.accept_len ? (j_seq < len ? p.draft_tok[static_cast<size_t>(row / (p.k + 1)) * p.k + j_seq] : p.next_tok[row / (p.k + 1)])
+                       : p.tokens[static_cast<size_t>(row) * p.T + p.t0 + q];
+    const bool have = x >= 0 && x < p.V;
+    tok[q].set(x, have, r.base + (have ? static_cast<size_t>(x) + r.off : 0));
+    if (have) l_min = fminf(l_min, tok[q].l);
   }
 
-  LpThread<kSums, kTop, kRank> th(j_begin + tid);
-  if (ragged_first) {
-    float f[kLpGroup];
-    r.get(0, f);
-    th.take(f, 0, r.first(0), lx, x, lx_min, n);
-  }
-  while (more) {
-    LpRaw<T> now[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) now[u] = raw[u];
-    const int next = j + kUnroll * kLpThreads;
-    more = next + kAhead < whole_end;
-    if (more) {
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) raw[u] = r.fetch(next + u * kLpThreads);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float f[kLpGroup];
-      lp_expand(now[u], f);
-      th.take(f, j + u * kLpThreads, r.first(j + u * kLpThreads), lx, x, lx_min, n);
-    }
-    j = next;
-  }
+  LpThread<T, kSums, kTop, kRank> th(j);
+#pragma unroll 1
   for (; j < j_end; j += kLpThreads) {
-    float f[kLpGroup];
-    r.get(j, f);
-    th.take(f, j, r.first(j), lx, x, lx_min, n);
+    LpGroup<T> g = next[0];
+#pragma unroll
+    for (int u = 0; u + 1 < kLpDepth; ++u) next[u] = next[u + 1];
+    const int ahead = j + kLpDepth * kLpThreads;
+    if (ahead < j_end && r.whole(ahead)) next[kLpDepth - 1].load(r.base + static_cast<size_t>(ahead) * E);
+    const bool ragged = !r.whole(j);
+    if (ragged) g = r.get_ragged(j);
+    th.take(g, j, r.first(j), tok, l_min, ragged);
   }
 
-  // The threads' sums and counts, over the warp and the CTA.
-  const float wm = warp_max_f32(th.m);
+  // The threads' sums and counts, over the warp.
   LpPart mine;
-  mine.m = wm;
+  mine.m = warp_max_f32(th.m);
   mine.s = mine.t = 0.f;
+  mine.spots = 0;
   if (kSums) {
-    const float d = th.m == -CUDART_INF_F ? 0.f : lp_below(th.m, wm), e = ex2_approx(d * kLog2e);
-    mine.s = e * th.s;
-    mine.t = e * fmaf(d, th.s, th.t);
+    th.sums(mine.s, mine.t);
+    const float d = th.m == -CUDART_INF_F ? 0.f : lp_below(th.m, mine.m), e = ex2_approx(d * kLog2e);
+    mine.t = e * fmaf(d, mine.s, mine.t);
+    mine.s *= e;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       mine.s += __shfl_xor_sync(0xffffffffu, mine.s, o);
@@ -380,165 +519,228 @@ __global__ void __launch_bounds__(kLpThreads, 4) token_logprobs_kernel(const LpP
   }
   mine.bad = __any_sync(0xffffffffu, th.bad) ? 1u : 0u;
 #pragma unroll
-  for (int q = 0; q < kLpTok; ++q) mine.count[q] = kRank ? __reduce_add_sync(0xffffffffu, th.count[q]) : 0;
+  for (int q = 0; q < kLpTok; ++q) mine.count[q] = q < kRank ? __reduce_add_sync(0xffffffffu, th.count[q < kRank ? q : 0]) : 0;
   if (lane == 0) warp_parts[warp] = mine;
 
-  uint64_t best = 0;                                     // kTop: warp 0's sorted list of the part's best entries
   if (kTop) {
     const uint64_t own = th.at < j_end ? lp_key(th.m, th.at) : 0;
-    const uint64_t all = lp_merge_warps(lp_sort(own, lane), lists, warp, lane);
-    if (warp == 0 && lane == p.n_top - 1) limit = all;
-    __syncthreads();
-    const uint64_t lim = limit;                          // (0: fewer threads than that hold anything)
-    const float w = lp_value(static_cast<uint32_t>(lim >> 32));
-    const int g = static_cast<int>(~static_cast<uint32_t>(lim));
-    const unsigned look = __ballot_sync(0xffffffffu, own != 0 && own >= lim);
-    int waiting = 0;
-    // The groups of those threads, dealt out to the lanes.
-    if (look >> lane & 1u) looked_at[warp][__popc(look & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
-    __syncwarp();
-    const int steps = (j_end - j_begin + kLpThreads - 1) / kLpThreads;         // groups per thread at most
-    const int total = __popc(look) * steps;
-    for (int i0 = 0; i0 < total; i0 += 32) {
-      const int i = i0 + lane;
-      float f[kLpGroup];
-      int jj = -1;
-      if (i < total) {
-        const int who = i / steps;
-        jj = j_begin + warp * 32 + looked_at[warp][who] + (i - who * steps) * kLpThreads;
-        if (jj >= j_end) jj = -1;
-      }
-      if (jj >= 0) r.get(jj, f);
-      const int v0 = r.first(jj);
+    uint64_t a = own;
 #pragma unroll
-      for (int e = 0; e < kLpGroup; ++e) {
-        const bool in = jj >= 0 && v0 + e >= 0 && v0 + e < p.V && (lim == 0 || f[e] > w || (f[e] == w && jj <= g));
-        const unsigned mask = __ballot_sync(0xffffffffu, in);
-        if (!mask) continue;
-        const int fit = __popc(mask);
-        if (waiting + fit > 32) {                        // full: sort what waits into the list
-          __syncwarp();
-          const uint64_t a = lp_sort(lane < waiting ? fresh[warp][lane] : 0, lane);
-          best = lp_merge(best, __shfl_sync(0xffffffffu, a, 31 - lane), lane);
-          waiting = 0;
-          __syncwarp();
-        }
-        if (in) fresh[warp][waiting + __popc(mask & ((1u << lane) - 1u))] = lp_key(f[e], v0 + e);
-        waiting += fit;
+    for (int o = 1; o < 8; o <<= 1) {
+      const uint64_t b = __shfl_xor_sync(0xffffffffu, a, o);
+      if (b > a) a = b;
+    }
+    if ((lane & 7) == 0) lists[warp * 4 + (lane >> 3)] = a;
+    __syncthreads();
+    // every warp for itself: the n-th best on the board (its keys differ, but for empty ones)
+    const uint64_t key = lists[lane];
+    int before = 0;
+#pragma unroll 4
+    for (int i = 0; i < 32; ++i) before += lists[i] > key ? 1 : 0;
+    const unsigned nth = __ballot_sync(0xffffffffu, key != 0 && before == p.n_top - 1);
+    uint64_t lim = nth ? __shfl_sync(0xffffffffu, key, __ffs(nth) - 1) : 0;     // (0: fewer hold anything)
+    float w = lp_value(static_cast<uint32_t>(lim >> 32));
+    int g_last = static_cast<int>(~static_cast<uint32_t>(lim));
+    const bool mine_too = own != 0 && own >= lim;
+    const bool again = mine_too && th.at + kLpThreads * (th.at == j_begin + tid) < j_end && (lim == 0 || th.second >= w);
+    if (mine_too && !again) lp_send(th.held, r, th.at, lim, w, g_last, own_spots, &n_spots);
+    const unsigned look = __ballot_sync(0xffffffffu, again);
+    if (look) {
+      // The groups of those threads, dealt out to the lanes.
+      if (again) looked_at[warp][__popc(look & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
+      __syncwarp();
+      const int steps = (j_end - j_begin + kLpThreads - 1) / kLpThreads;       // groups per thread at most
+      const int total = __popc(look) * steps;
+      for (int i = lane; i < total; i += 32) {
+        const int who = i / steps, jj = j_begin + warp * 32 + looked_at[warp][who] + (i - who * steps) * kLpThreads;
+        if (jj < j_end) lp_send(r.get(jj), r, jj, lim, w, g_last, own_spots, &n_spots);
       }
     }
-    __syncwarp();
-    if (waiting > 0) {
-      const uint64_t a = lp_sort(lane < waiting ? fresh[warp][lane] : 0, lane);
-      best = lp_merge(best, __shfl_sync(0xffffffffu, a, 31 - lane), lane);
+    __syncthreads();
+    if (n_spots > kLpSpots) {
+      // More than there is room for (the best entries crowd together, or many are equal): with the n-th best of ALL threads' pairs for
+      // a limit, the part's 32 best by sorted lists, from all groups of the threads that may hold some.
+      __syncthreads();                                   // (everyone has seen n_spots, and the board)
+      const uint64_t firsts = lp_merge_warps(lp_sort(own, lane), lists, warp, lane);
+      if (warp == 0 && lane == p.n_top - 1) own_spots[0] = firsts;
+      __syncthreads();
+      lim = own_spots[0];
+      w = lp_value(static_cast<uint32_t>(lim >> 32));
+      g_last = static_cast<int>(~static_cast<uint32_t>(lim));
+      const bool holds = own != 0 && own >= lim;
+      const unsigned all = __ballot_sync(0xffffffffu, holds);
+      if (holds) looked_at[warp][__popc(all & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
+      __syncwarp();
+      const int steps = (j_end - j_begin + kLpThreads - 1) / kLpThreads, total = __popc(all) * steps;
+      uint64_t best = 0;
+      int waiting = 0;
+#pragma unroll 1
+      for (int i0 = 0; i0 < total; i0 += 32) {
+        const int i = i0 + lane;
+        int jj = -1;
+        if (i < total) {
+          const int who = i / steps;
+          jj = j_begin + warp * 32 + looked_at[warp][who] + (i - who * steps) * kLpThreads;
+          if (jj >= j_end) jj = -1;
+        }
+        LpGroup<T> g = {};
+        if (jj >= 0) g = r.get(jj);
+        const int v0 = r.first(jj);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float l = g.entry(e);
+          const bool in = jj >= 0 && v0 + e >= 0 && v0 + e < p.V && (lim == 0 || l > w || (l == w && jj <= g_last));
+          const unsigned mask = __ballot_sync(0xffffffffu, in);
+          if (!mask) continue;
+          const int fit = __popc(mask);
+          if (waiting + fit > 32) {                      // full: what waits goes into the list
+            best = lp_take_in(best, fresh[warp], waiting);
+            waiting = 0;
+          }
+          if (in) fresh[warp][waiting + __popc(mask & ((1u << lane) - 1u))] = lp_key(l, v0 + e);
+          waiting += fit;
+        }
+      }
+      best = lp_take_in(best, fresh[warp], waiting);
+      __syncthreads();
+      best = lp_merge_warps(best, lists, warp, lane);
+      if (warp == 0) own_spots[lane] = best;
+      if (tid == 0) n_spots = 32;
+      __syncthreads();
     }
-    best = lp_merge_warps(best, lists, warp, lane);      // (the lists of before are read no more)
   } else {
     __syncthreads();
   }
 
-  // Warp 0: the CTA's part, to the first CTA of the cluster.
+  // The part, to the first CTA of the cluster.
+  if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
   if (warp == 0) {
-    LpPart w8 = {-CUDART_INF_F, 0.f, 0.f, 0u, {0, 0, 0, 0}};
-    if (lane < kLpWarps) w8 = warp_parts[lane];
-    const float m = warp_max_f32(w8.m);
+    LpPart all = {-CUDART_INF_F, 0.f, 0.f, 0u, {0, 0, 0, 0}, 0};
+    if (lane < kLpWarps) all = warp_parts[lane];
+    const float m = warp_max_f32(all.m);
     if (kSums) {
-      const float d = w8.m == -CUDART_INF_F ? 0.f : lp_below(w8.m, m), e = ex2_approx(d * kLog2e);
-      w8.t = e * fmaf(d, w8.s, w8.t);
-      w8.s *= e;
+      const float d = all.m == -CUDART_INF_F ? 0.f : lp_below(all.m, m), e = ex2_approx(d * kLog2e);
+      all.t = e * fmaf(d, all.s, all.t);
+      all.s *= e;
     }
-    w8.m = m;
+    all.m = m;
 #pragma unroll
     for (int o = kLpWarps / 2; o > 0; o >>= 1) {
-      w8.s += __shfl_xor_sync(0xffffffffu, w8.s, o);
-      w8.t += __shfl_xor_sync(0xffffffffu, w8.t, o);
-      w8.bad |= __shfl_xor_sync(0xffffffffu, w8.bad, o);
+      all.s += __shfl_xor_sync(0xffffffffu, all.s, o);
+      all.t += __shfl_xor_sync(0xffffffffu, all.t, o);
+      all.bad |= __shfl_xor_sync(0xffffffffu, all.bad, o);
 #pragma unroll
-      for (int q = 0; q < kLpTok; ++q) w8.count[q] += __shfl_xor_sync(0xffffffffu, w8.count[q], o);
+      for (int q = 0; q < kRank; ++q) all.count[q] += __shfl_xor_sync(0xffffffffu, all.count[q], o);
     }
-    if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
-    LpPart* to = C > 1 ? cg::this_cluster().map_shared_rank(&cluster_parts[part], 0) : &cluster_parts[part];
-    if (lane == 0) *to = w8;
-    if (kTop) {
-      uint64_t* to_list = C > 1 ? cg::this_cluster().map_shared_rank(&cluster_lists[part][0], 0) : &cluster_lists[part][0];
-      to_list[lane] = best;
-    }
-    __syncwarp();
-  } else if (C > 1) {
-    asm volatile("barrier.cluster.wait;" ::: "memory");
+    all.spots = kTop ? n_spots : 0;
+    LpPart* to = C > 1 ? cg::this_cluster().map_shared_rank(&parts[part], 0) : &parts[part];
+    if (lane == 0) *to = all;
+  } else if (kTop && warp <= 2) {
+    uint64_t* to = C > 1 ? cg::this_cluster().map_shared_rank(&spots[part][0], 0) : &spots[part][0];
+    const int i = (warp - 1) * 32 + lane;
+    if (i < ((n_spots + 7) & ~7)) to[i] = own_spots[i];  // (whole eights, for the counting)
   }
   if (C > 1) cluster_sync_all();
-  if (part != 0 || warp != 0) return;
+  else __syncthreads();
+  if (part != 0) return;
 
-  // The row.
-  LpPart all = cluster_parts[0];
-  if (kTop) best = cluster_lists[0][lane];
-  for (int c = 1; c < C; ++c) {
-    const LpPart o = cluster_parts[c];
-    if (kSums && o.m != -CUDART_INF_F) {
-      const float m = fmaxf(all.m, o.m);
-      const float da = all.m == -CUDART_INF_F ? 0.f : lp_below(all.m, m), db = lp_below(o.m, m);
-      const float ea = ex2_approx(da * kLog2e), eb = ex2_approx(db * kLog2e);
-      all.t = ea * fmaf(da, all.s, all.t) + eb * fmaf(db, o.s, o.t);
-      all.s = ea * all.s + eb * o.s;
-      all.m = m;
-    }
-    all.bad |= o.bad;
+  // The row: its sums, by every warp that needs them.
+  if (warp > 0 && !kTop) return;
+  LpPart all = {-CUDART_INF_F, 0.f, 0.f, 0u, {0, 0, 0, 0}, 0};
+  if (lane < C) all = parts[lane];
+  float m = warp_max_f32(all.m), ls, logZ, H = 0.f;
+  const bool bad = __any_sync(0xffffffffu, all.bad != 0);
+  if (kSums) {
+    const float d = all.m == -CUDART_INF_F ? 0.f : lp_below(all.m, m), e = ex2_approx(d * kLog2e);
+    float s = e * all.s, t = e * fmaf(d, all.s, all.t);
 #pragma unroll
-    for (int q = 0; q < kLpTok; ++q) all.count[q] += o.count[q];
-    if (kTop) best = lp_merge(best, cluster_lists[c][31 - lane], lane);
-  }
-  float m = 0.f, ls, logZ, H = 0.f;
-  if (!kSums) {
+    for (int o = kLpMaxCluster / 2; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      t += __shfl_xor_sync(0xffffffffu, t, o);
+    }
+    if (bad) {
+      m = ls = logZ = H = CUDART_NAN_F;
+    } else if (m == -CUDART_INF_F) {
+      ls = logZ = m;                                     // nothing is left of the row
+    } else {
+      ls = logf(s);
+      logZ = m + ls;
+      H = fmaxf(0.f, ls - quotient(t, s));
+    }
+    // (lanes beyond the parts hold other sums' halves)
+    m = __shfl_sync(0xffffffffu, m, 0); ls = __shfl_sync(0xffffffffu, ls, 0);
+  } else {
+    m = 0.f;
     ls = logZ = p.logZ_in[row];
-  } else if (all.bad) {
-    m = ls = logZ = H = CUDART_NAN_F;
-  } else if (all.m == -CUDART_INF_F) {
-    m = ls = logZ = -CUDART_INF_F;                       // nothing is left of the row
-  } else {
-    m = all.m;
-    ls = logf(all.s);
-    logZ = m + ls;
-    H = fmaxf(0.f, ls - quotient(all.t, all.s));
   }
-  if (all.bad) flags |= HOLA_FLAG_BAD_LOGIT;
-  if (lane == 0) {
-    if (kSums && p.entropy) p.entropy[row] = H;
-    if (kSums && p.logZ) p.logZ[row] = logZ;
-  }
-  // (no token: 0; one that the vocabulary does not have: NaN)
-  if (kRank) {
-    if (lane < n) {
-      int tok = x[0], before = all.count[0];
-      float l = lx[0];
+  if (warp == 0) {
+    if (lane == 0) {
+      if (kSums && p.entropy) p.entropy[row] = H;
+      if (kSums && p.logZ) p.logZ[row] = logZ;
+    }
+    unsigned flags = bad ? HOLA_FLAG_BAD_LOGIT : 0u;
+    // (no token: 0; one that the vocabulary does not have: NaN)
+    if (kRank) {
 #pragma unroll
-      for (int q = 1; q < kLpTok; ++q)
-        if (lane == q) { tok = x[q]; before = all.count[q]; l = lx[q]; }
-      const size_t at = static_cast<size_t>(row) * p.T + p.t0 + lane;
-      const bool have = tok >= 0 && tok < p.V, none = !p.accept_len && tok == -1;
-      if (!have && !none) flags |= HOLA_FLAG_BAD_TOKEN;
-      p.logprob[at] = have ? lp_logprob(l, m, ls) : none ? 0.f : CUDART_NAN_F;
-      p.rank[at] = have && !all.bad ? before : -1;
-    }
-  } else {
-    for (int q = lane; q < p.T; q += 32) {
-      const int tok = !p.accept_len ? p.tokens[static_cast<size_t>(row) * p.T + q]
+      for (int q = 0; q < kRank; ++q) all.count[q] = __reduce_add_sync(0xffffffffu, all.count[q]);
+      if (lane < n) {
+        int x = tok[0].x, before = all.count[0];
+        float l = tok[0].l;
+#pragma unroll
+        for (int q = 1; q < kRank; ++q)
+          if (lane == q) { x = tok[q].x; before = all.count[q]; l = tok[q].l; }
+        const size_t at = static_cast<size_t>(row) * p.T + p.t0 + lane;
+        const bool have = x >= 0 && x < p.V, none = !p.accept_len && x == -1;
+        if (!have && !none) flags |= HOLA_FLAG_BAD_TOKEN;
+        p.logprob[at] = have ? lp_logprob(l, m, ls) : none ? 0.f : CUDART_NAN_F;
+        p.rank[at] = have && !bad ? before : -1;
+      }
+    } else {
+      for (int q = lane; q < p.T; q += 32) {
+        const int x = !p.accept_len ? p.tokens[static_cast<size_t>(row) * p.T + q]
                       : j_seq < len ? p.draft_tok[static_cast<size_t>(row / (p.k + 1)) * p.k + j_seq] : p.next_tok[row / (p.k + 1)];
-      const bool have = tok >= 0 && tok < p.V, none = !p.accept_len && tok == -1;
-      if (!have && !none) flags |= HOLA_FLAG_BAD_TOKEN;
-      p.logprob[static_cast<size_t>(row) * p.T + q] =
-          have ? lp_logprob(lp_float(r.base[static_cast<size_t>(tok) + r.off]), m, ls) : none ? 0.f : CUDART_NAN_F;
+        const bool have = x >= 0 && x < p.V, none = !p.accept_len && x == -1;
+        if (!have && !none) flags |= HOLA_FLAG_BAD_TOKEN;
+        p.logprob[static_cast<size_t>(row) * p.T + q] =
+            have ? lp_logprob(lp_float(r.base[static_cast<size_t>(x) + r.off]), m, ls) : none ? 0.f : CUDART_NAN_F;
+      }
+    }
+    if (p.status) {
+      __syncwarp();
+      flags = __reduce_or_sync(0xffffffffu, flags);
+      if (lane == 0 && flags) atomicOr(p.status, flags);
     }
   }
-  if (kTop && lane < p.n_top) {
-    const size_t at = static_cast<size_t>(row) * p.n_top + lane;
-    p.top_ids[at] = all.bad ? -1 : static_cast<int>(~static_cast<uint32_t>(best));
-    p.top_logprobs[at] = all.bad ? CUDART_NAN_F : lp_logprob(lp_value(static_cast<uint32_t>(best >> 32)), m, ls);
-  }
-  if (p.status) {
-    __syncwarp();
-    flags = __reduce_or_sync(0xffffffffu, flags);
-    if (lane == 0 && flags) atomicOr(p.status, flags);
+  if (kTop) {
+    const size_t at = static_cast<size_t>(row) * p.n_top;
+    if (bad) {
+      if (tid < p.n_top) { p.top_ids[at + tid] = -1; p.top_logprobs[at + tid] = CUDART_NAN_F; }
+      return;
+    }
+    // Every entry that was sent finds its place by counting those before it: thread i takes entry i, i + 256, ...
+    for (int i0 = warp * 32; ; i0 += kLpThreads) {
+      int i = i0 + lane, from = -1, total = 0;
+      for (int c = 0; c < C; ++c) {
+        const int sent = __shfl_sync(0xffffffffu, all.spots, c);
+        if (from < 0 && i < sent) from = c;
+        if (from < 0) i -= sent;
+        total += sent;
+      }
+      if (i0 >= total) break;
+      const uint64_t key = from >= 0 ? spots[from][i] : 0;
+      int before = 0;
+      for (int c = 0; c < C; ++c) {
+        const int sent = __shfl_sync(0xffffffffu, all.spots, c);
+#pragma unroll 1
+        for (int k = 0; k < sent; k += 8)                // (whole eights were sent)
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) before += spots[c][k + kk] > key ? 1 : 0;
+      }
+      if (before < p.n_top && key != 0) {
+        p.top_ids[at + before] = static_cast<int>(~static_cast<uint32_t>(key));
+        p.top_logprobs[at + before] = lp_logprob(lp_value(static_cast<uint32_t>(key >> 32)), m, ls);
+      }
+    }
   }
 }
 
@@ -570,11 +772,11 @@ __global__ void __launch_bounds__(128) gather_logprobs_kernel(const LpParams p) 
 // CTAs per row: enough for four on every SM, as long as a thread keeps a group or two of its own.
 int lp_cluster(int num_sms, int rows, int V) {
   int C = 1;
-  while (C < kLpMaxCluster && static_cast<long long>(rows) * C < 4ll * num_sms && V / (2 * C) >= kLpThreads * kLpGroup) C <<= 1;
+  while (C < kLpMaxCluster && static_cast<long long>(rows) * C < 4ll * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;
   return C;
 }
 
-template <typename T, bool kSums, bool kTop, bool kRank>
+template <typename T, bool kSums, bool kTop, int kRank>
 cudaError_t launch_logprobs(const LpParams& p, int C, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.rows) * C); cfg.blockDim = dim3(kLpThreads); cfg.stream = stream;
@@ -585,6 +787,13 @@ cudaError_t launch_logprobs(const LpParams& p, int C, cudaStream_t stream) {
   attr[1].val.clusterDim.x = static_cast<unsigned>(C); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kSums, kTop, kRank>, p, C);
+}
+
+// One token per row is the rule: the pass then carries one comparison instead of kLpTok.
+template <typename T, bool kSums, bool kTop>
+cudaError_t launch_logprobs_of(const LpParams& p, bool rank, int C, cudaStream_t stream) {
+  return !rank ? launch_logprobs<T, kSums, kTop, 0>(p, C, stream)
+         : p.tn == 1 ? launch_logprobs<T, kSums, kTop, 1>(p, C, stream) : launch_logprobs<T, kSums, kTop, kLpTok>(p, C, stream);
 }
 
 template <typename T>
@@ -608,10 +817,8 @@ cudaError_t run_logprobs(LpParams p, int num_sms, cudaStream_t stream) {
     p.tn = p.T - p.t0 < kLpTok ? p.T - p.t0 : kLpTok;
     const bool first = p.t0 == 0;
     if (!first) { p.entropy = nullptr; p.logZ = nullptr; }
-    e = top && first ? (sums ? (rank ? launch_logprobs<T, true, true, true>(p, C, stream) : launch_logprobs<T, true, true, false>(p, C, stream))
-                             : (rank ? launch_logprobs<T, false, true, true>(p, C, stream) : launch_logprobs<T, false, true, false>(p, C, stream)))
-        : sums ? (rank ? launch_logprobs<T, true, false, true>(p, C, stream) : launch_logprobs<T, true, false, false>(p, C, stream))
-               : launch_logprobs<T, false, false, true>(p, C, stream);
+    e = top && first ? (sums ? launch_logprobs_of<T, true, true>(p, rank, C, stream) : launch_logprobs_of<T, false, true>(p, rank, C, stream))
+                     : (sums ? launch_logprobs_of<T, true, false>(p, rank, C, stream) : launch_logprobs_of<T, false, false>(p, rank, C, stream));
   }
   return e;
 }

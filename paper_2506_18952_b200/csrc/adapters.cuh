@@ -3,17 +3,28 @@
 // Sequence b uses adapter a = ids[b] (or none): its k + 1 verify rows x[r] get the logits of the head W + s_a B_a A_a,
 //   l[r,v] = sum_h W[v,h] x[r,h] + sum_i B_a[v,i] u[r,i],   u[r,i] = s_a sum_h A_a[i,h] x[r,h],   i < rank.
 //
-//   adapter_down_kernel  u, ahead of the GEMM: one CTA per sequence, 16 ranks and 16 rows, whose warps share the hidden channels.
+//   adapter_down_kernel  u, ahead of the GEMM: one CTA per sequence, 16 ranks and 16 rows, whose warps share the hidden channels; and
+//       one CTA that sorts the batch's rows by adapter into tiles of eight.
 //   adapter_up_kernel    behind the GEMM, whatever its weight mode: adds the second product to the stored logits and makes the
 //       rows' softmax statistics anew, in the form in which the GEMM's epilogue leaves them (partials of each row), so that
 //       everything behind reads them as before.  Rows without an adapter are left alone.
 // Both products run on bf16 operands with fp32 accumulation; u, which is fp32, enters the second one as three bf16 planes that
 // add up to it exactly (8 significant bits each), so that no rounding is added to what an fp32 product would have.
+//
+// (Why not inside the GEMM, as further K blocks [B_0 B_1 ...] against rows that are zero but for their own slot's columns: a number
+// that is not finite in one slot would reach the rows of every other request as 0 * inf, and each block costs all rows' MMAs.)
 
 constexpr int kAdMaxRank = 128;
 constexpr int kAdDownWarps = 16;
 constexpr int kAdUpWarps = 4;
-constexpr int kAdChunk = 32;           // vocabulary entries per warp step
+constexpr int kAdRows = 8;             // verify rows of a tile: the N of the MMA
+constexpr int kAdChunk = 64;           // vocabulary entries per warp step
+constexpr int kAdMaxSorted = 2048;     // sequences up to which rows of different sequences share tiles
+
+// Up to eight verify rows that use one adapter.
+struct AdapterTile {
+  int adapter, n, row[kAdRows];
+};
 
 struct AdapterParams {
   const uint16_t* A;           // bf16 [slots][rank][H]
@@ -24,6 +35,8 @@ struct AdapterParams {
   int B, rows_per_seq, H, V;
   const uint16_t* hidden;      // [B][rows_per_seq][H]
   float* u;                    // [rows][kAdMaxRank]
+  AdapterTile* tiles;          // [max_tiles], those that are not needed with n = 0
+  int max_tiles;
   float* logits;
   int ldl;
   float4* partials;
@@ -45,26 +58,86 @@ __device__ __forceinline__ int adapter_of(const AdapterParams& p, int b) {
   return a >= 0 && a < p.slots ? a : -1;
 }
 
+// The batch's rows by adapter, in tiles of eight, by one CTA.  Sequences with the same adapter keep their order; a sequence finds its
+// place by looking at all others (B^2 comparisons: 256 sequences take as long as the loads of the other CTAs).  Beyond kAdMaxSorted
+// sequences every one has tiles of its own.
+__device__ __forceinline__ void adapter_tiles(const AdapterParams& p) {
+  __shared__ int ids[kAdMaxSorted], users[kAdMaxSorted];
+  const int tid = threadIdx.x, nthr = blockDim.x, k1 = p.rows_per_seq, B = p.B;
+  const int per_seq = (k1 + kAdRows - 1) / kAdRows;
+  for (int t = tid; t < p.max_tiles; t += nthr) p.tiles[t].n = 0;
+  if (B > kAdMaxSorted) {
+    __syncthreads();
+    for (int i = tid; i < B * per_seq; i += nthr) {
+      const int b = i / per_seq, j0 = (i - b * per_seq) * kAdRows, a = adapter_of(p, b);
+      if (a < 0) continue;
+      AdapterTile& t = p.tiles[i];
+      t.adapter = a;
+      t.n = min(kAdRows, k1 - j0);
+      for (int j = 0; j < kAdRows; ++j) t.row[j] = b * k1 + j0 + j;
+    }
+    return;
+  }
+  for (int b = tid; b < B; b += nthr) ids[b] = adapter_of(p, b);
+  __syncthreads();
+  for (int b = tid; b < B; b += nthr) {                  // how many use the adapter, at its first user; 0 at the others
+    int n = 0, before = 0;
+    for (int c = 0; c < B; ++c) {
+      const bool same = ids[c] == ids[b];
+      n += same ? 1 : 0;
+      before += same && c < b ? 1 : 0;
+    }
+    users[b] = ids[b] < 0 || before > 0 ? 0 : n;
+  }
+  __syncthreads();
+  for (int b = tid; b < B; b += nthr) {
+    if (ids[b] < 0) continue;
+    int first = 0, before = 0, all = 0;
+    for (int c = 0; c < B; ++c) {
+      if (ids[c] < ids[b]) first += (users[c] * k1 + kAdRows - 1) / kAdRows;
+      if (ids[c] == ids[b]) {
+        all += users[c];
+        before += c < b ? 1 : 0;
+      }
+    }
+    for (int j = 0; j < k1; ++j) {
+      const int i = before * k1 + j;
+      AdapterTile& t = p.tiles[first + i / kAdRows];
+      t.row[i % kAdRows] = b * k1 + j;
+      if (i % kAdRows == 0) {
+        t.adapter = ids[b];
+        t.n = min(kAdRows, all * k1 - i);
+      }
+    }
+  }
+}
+
 // The order of the channels inside a sum is free, so lane (g, q) of a warp loads 16 bytes = 8 neighbouring channels of its row and
 // hands them to two MMAs: channels 8q .. 8q+3 in the places the first one gives lane q, 8q+4 .. 8q+7 in those of the second.
-__global__ void __launch_bounds__(kAdDownWarps * 32) adapter_down_kernel(const AdapterParams p) {
+__global__ void __launch_bounds__(kAdDownWarps * 32, 1) adapter_down_kernel(const AdapterParams p) {
   __shared__ float sums[kAdDownWarps][16][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int b = blockIdx.x, i0 = blockIdx.y * 16, j0 = blockIdx.z * 16;
   grid_dependency_wait();
   grid_dependency_release();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && warp == 0 && p.status) {
-    bool bad = false;
-    for (int i = lane; i < p.B; i += 32) bad = bad || p.ids[i] < -1 || p.ids[i] >= p.slots;
-    const unsigned flags = __any_sync(0xffffffffu, bad) ? HOLA_FLAG_BAD_ADAPTER : 0u;
-    if (lane == 0) {
-      if (p.clear_status) *p.status = flags;
-      else if (flags) atomicOr(p.status, flags);
+  if (b == p.B) {
+    if (blockIdx.y != 0 || blockIdx.z != 0) return;
+    if (warp == 0 && p.status) {
+      bool bad = false;
+      for (int i = lane; i < p.B; i += 32) bad = bad || p.ids[i] < -1 || p.ids[i] >= p.slots;
+      const unsigned flags = __any_sync(0xffffffffu, bad) ? HOLA_FLAG_BAD_ADAPTER : 0u;
+      if (lane == 0) {
+        if (p.clear_status) *p.status = flags;
+        else if (flags) atomicOr(p.status, flags);
+      }
     }
+    adapter_tiles(p);
+    return;
   }
   const int a = adapter_of(p, b);
   if (a < 0) return;
   const int rows = min(16, p.rows_per_seq - j0), ranks = min(16, p.rank - i0);
+  const float scale = p.scale ? p.scale[a] : 1.f;
   const uint16_t* x = p.hidden + (static_cast<size_t>(b) * p.rows_per_seq + j0) * p.H;
   const uint16_t* A = p.A + (static_cast<size_t>(a) * p.rank + i0) * p.H;
   float d[2][4] = {};
@@ -93,166 +166,239 @@ __global__ void __launch_bounds__(kAdDownWarps * 32) adapter_down_kernel(const A
     float s = 0.f;
 #pragma unroll
     for (int w = 0; w < kAdDownWarps; ++w) s += sums[w][j][i];
-    p.u[(static_cast<size_t>(b) * p.rows_per_seq + j0 + j) * kAdMaxRank + i0 + i] = p.scale ? s * p.scale[a] : s;
+    p.u[(static_cast<size_t>(b) * p.rows_per_seq + j0 + j) * kAdMaxRank + i0 + i] = s * scale;
   }
 }
 
-__device__ __forceinline__ void stats_fold8(const float* v, int vocab0, int want_arg, Stats& st) {
-  const float cmax = fmaxf(max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), v[6]), v[7]);
-  if (cmax > st.m) {
-    if (st.m != -CUDART_INF_F) {
-      const float d = st.m - cmax, sc = ex2_approx(d * kLog2e);
-      st.t = sc * (st.t + d * st.s);
-      st.s *= sc;
-    }
-    st.m = cmax;
-    if (want_arg) {
+// Running statistics of a row about a point `ref` that trails the maximum by 4 at most, so that a rise of the maximum rarely makes a
+// warp rescale.  In units of ln 2: x = l log2 e - ref log2 e, s = sum 2^x, t = sum 2^x x.
+struct RowStats {
+  float m, rise, shift;
+  uint64_t s2, t2;
+  int arg;
+  __device__ __forceinline__ void clear() {
+    m = rise = -CUDART_INF_F;
+    shift = 0.f;
+    s2 = t2 = 0;
+    arg = 0x7fffffff;
+  }
+  // Eight logits; entry i is vocabulary entry v(i), rising with i.  -inf: none (all of them none: nothing is called).
+  template <typename Entry>
+  __device__ __forceinline__ void fold(const float* l, int want_arg, Entry v) {
+    const float top = fmaxf(max3(max3(l[0], l[1], l[2]), max3(l[3], l[4], l[5]), l[6]), l[7]);
+    if (want_arg && top > m) {
       int first = 0;
 #pragma unroll
       for (int i = 7; i > 0; --i)
-        if (v[i] == cmax) first = i;
-      st.arg = vocab0 + (v[0] == cmax ? 0 : first);
+        if (l[i] == top) first = v(i);
+      arg = l[0] == top ? v(0) : first;
+    }
+    m = fmaxf(m, top);
+    if (top > rise) {
+      const float old = shift;
+      shift = -top * kLog2e;
+      if (rise != -CUDART_INF_F) {
+        const float dx = shift - old, e = ex2_approx(dx);
+        const uint64_t e2 = pack2(e, e);
+        uint64_t d;
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(fma2(pack2(dx, dx), s2, t2)), "l"(e2));
+        t2 = d;
+        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(s2), "l"(e2));
+        s2 = d;
+      }
+      rise = top + 4.f;
+    }
+    const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t x = fma2(pack2(l[2 * i], l[2 * i + 1]), l2e, sh);
+      float a, b;
+      unpack2(x, a, b);
+      // (none: 2^-126, of which nothing is left beside the sum, and a product that stays finite)
+      const uint64_t y = pack2(fmaxf(a, -126.f), fmaxf(b, -126.f)), e = pack2(ex2_approx(a), ex2_approx(b));
+      s2 = add2(s2, e);
+      t2 = fma2(e, y, t2);
     }
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (v[i] == -CUDART_INF_F) continue;                 // (entries past the vocabulary)
-    const float d = v[i] - st.m, e = ex2_approx(d * kLog2e);
-    st.s += e;
-    st.t = fmaf(e, d, st.t);
+  __device__ __forceinline__ Stats stats() const {
+    if (m == -CUDART_INF_F) return stats_empty();
+    float a, b, c, d;
+    unpack2(s2, a, b);
+    unpack2(t2, c, d);
+    const float x = fmaf(m, kLog2e, shift), e = ex2_approx(-x), s = a + b;    // (x of the maximum, as it was summed)
+    return Stats{m, s * e, kLn2 * (e * fmaf(-x, s, c + d)), arg};
   }
-}
+};
 
-// A warp step covers 32 vocabulary entries and 16 rows: column n of tile j of the four MMAs stands for entry 8 (n / 2) + 2 j + n % 2,
-// so that a lane ends up with eight neighbouring entries of rows g and g + 8.
+// A warp step covers 64 vocabulary entries, the M of four MMAs, and the tile's eight rows, their N.  Lane (g, q) ends up with rows
+// 2 q and 2 q + 1 and, of every 32 entries, the four that stand at m = g and g + 8 of two MMAs: side by side, 16 bytes of each row.
+// Rows that do not lie on 16-byte boundaries (kVec false) pass through shared memory, so that eight lanes share a sector; every lane
+// sums the same entries in the same order either way.
+__device__ __forceinline__ int adapter_entry(int e, int g) { return 32 * (e >> 2) + 4 * g + (e & 3); }     // e: 0 .. 7
 template <bool kVec>
-__global__ void __launch_bounds__(kAdUpWarps * 32) adapter_up_kernel(const AdapterParams p, int P) {
-  __shared__ uint2 planes[3][kAdMaxRank / 16][16][4];    // [plane][16 ranks][row][q]: ranks 4q .. 4q+3 of the sixteen
-  __shared__ float4 warp_stats[kAdUpWarps][16];
+__global__ void __launch_bounds__(kAdUpWarps * 32, 5) adapter_up_kernel(const AdapterParams p, int P) {
+  __shared__ uint2 planes[3][kAdMaxRank / 16][kAdRows][4];       // [plane][16 ranks][row][q]: ranks 4q .. 4q+3 of the sixteen
+  __shared__ float4 warp_stats[kAdUpWarps][kAdRows];
+  __shared__ __align__(16) float shift_buf[kVec ? 1 : kAdUpWarps][kVec ? 1 : kAdRows][kAdChunk + 4];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int b = blockIdx.x, part = blockIdx.y;
+  const int part = blockIdx.y;
   grid_dependency_wait();
-  const int a = adapter_of(p, b);
-  if (a < 0) return;
+  const AdapterTile& tile = p.tiles[blockIdx.x];
+  const int n = tile.n;
+  if (n == 0) return;
   const int chunks = (p.V + kAdChunk - 1) / kAdChunk, per = (chunks + P - 1) / P;
   const int c_end = min(chunks, (part + 1) * per);
   const int steps = (p.rank + 15) >> 4;
-  const uint16_t* Bm = p.Bm + static_cast<size_t>(a) * p.rank;
-  for (int j0 = 0; j0 < p.rows_per_seq; j0 += 16) {
-    const int rows = min(16, p.rows_per_seq - j0);
-    const size_t row0 = static_cast<size_t>(b) * p.rows_per_seq + j0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < steps * 64; i += kAdUpWarps * 32) {
-      const int k = i >> 6, r = (i >> 2) & 15, qq = i & 3;
-      uint32_t w[3][2] = {};
-      if (r < rows) {
-        const float4 u4 = *reinterpret_cast<const float4*>(p.u + (row0 + r) * kAdMaxRank + 16 * k + 4 * qq);
-        float u[4] = {u4.x, u4.y, u4.z, u4.w};
+  const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.rank;
+  for (int i = threadIdx.x; i < steps * kAdRows * 4; i += kAdUpWarps * 32) {
+    const int k = i >> 5, r = (i >> 2) & 7, qq = i & 3;
+    uint32_t w[3][2] = {};
+    if (r < n) {
+      const float4 u4 = *reinterpret_cast<const float4*>(p.u + static_cast<size_t>(tile.row[r]) * kAdMaxRank + 16 * k + 4 * qq);
+      float u[4] = {u4.x, u4.y, u4.z, u4.w};
 #pragma unroll
-        for (int pl = 0; pl < 3; ++pl)
+      for (int pl = 0; pl < 3; ++pl)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat16 h = __float2bfloat16_rn(u[e]);
-            u[e] -= __bfloat162float(h);                 // (exact)
-            w[pl][e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(h)) << (16 * (e & 1));
-          }
-      }
-#pragma unroll
-      for (int pl = 0; pl < 3; ++pl) planes[pl][k][r][qq] = make_uint2(w[pl][0], w[pl][1]);
+        for (int e = 0; e < 4; ++e) {
+          const __nv_bfloat16 h = __float2bfloat16_rn(u[e]);
+          u[e] -= __bfloat162float(h);                   // (exact)
+          w[pl][e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(h)) << (16 * (e & 1));
+        }
     }
-    __syncthreads();
-    Stats st[2] = {stats_empty(), stats_empty()};
-    for (int c = part * per + warp; c < c_end; c += kAdUpWarps) {
-      const int v0 = c * kAdChunk + 8 * q;               // this lane's entries
-      float l[2][8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = g + 8 * h;
-        const float* at = p.logits + (row0 + r) * p.ldl + v0;
+    for (int pl = 0; pl < 3; ++pl) planes[pl][k][r][qq] = make_uint2(w[pl][0], w[pl][1]);
+  }
+  const bool have[2] = {2 * q < n, 2 * q + 1 < n};
+  float* at[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) l[h][e] = -CUDART_INF_F;
-        if (r < rows) {
-          if (kVec && v0 + 8 <= p.V) {
-            const float4 x = *reinterpret_cast<const float4*>(at), y = *reinterpret_cast<const float4*>(at + 4);
-            l[h][0] = x.x; l[h][1] = x.y; l[h][2] = x.z; l[h][3] = x.w;
-            l[h][4] = y.x; l[h][5] = y.y; l[h][6] = y.z; l[h][7] = y.w;
-          } else {
+  for (int h = 0; h < 2; ++h) at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl;
+  __syncthreads();
+  RowStats st[2];
+  st[0].clear(); st[1].clear();
+  for (int c = part * per + warp; c < c_end; c += kAdUpWarps) {
+    const int v0 = c * kAdChunk;
+    const bool whole = v0 + kAdChunk <= p.V;
+    float l[2][8];
+    if (!kVec && whole) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (v0 + e < p.V) l[h][e] = at[e];
-          }
-        }
-      }
-      float d[4][4] = {};
-      for (int k = 0; k < steps; ++k) {
-        uint32_t f[3][4];
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int pl = 0; pl < 3; ++pl) {
-          const uint2 x = planes[pl][k][g][q], y = planes[pl][k][g + 8][q];
-          f[pl][0] = x.x; f[pl][1] = y.x; f[pl][2] = x.y; f[pl][3] = y.y;
-        }
-        const bool in = 16 * k + 4 * q < p.rank;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int v = c * kAdChunk + 8 * (g >> 1) + 2 * j + (g & 1);
-          uint2 w = make_uint2(0u, 0u);
-          if (in && v < p.V) w = *reinterpret_cast<const uint2*>(Bm + static_cast<size_t>(v) * p.pitch + 16 * k + 4 * q);
-#pragma unroll
-          for (int pl = 2; pl >= 0; --pl) mma_bf16(d[j], f[pl], w.x, w.y);
-        }
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = g + 8 * h;
-        if (r >= rows) continue;
-        float* at = p.logits + (row0 + r) * p.ldl + v0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) l[h][e] += d[e >> 1][2 * h + (e & 1)];       // (past the vocabulary: -inf + 0)
-        if (kVec && v0 + 8 <= p.V) {
-          *reinterpret_cast<float4*>(at) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
-          *reinterpret_cast<float4*>(at + 4) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (v0 + e < p.V) at[e] = l[h][e];
-        }
-        if (v0 < p.V) stats_fold8(l[h], v0, p.want_arg, st[h]);
-      }
+        for (int e = 0; e < 8; ++e) shift_buf[warp][2 * q + h][8 * e + g] = have[h] ? at[h][v0 + 8 * e + g] : 0.f;
+      __syncwarp();
     }
-    // a row's statistics over the four lanes that hold it, then over the warps
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      if (whole) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+        if (!kVec) {
+          x = *reinterpret_cast<const float4*>(&shift_buf[warp][2 * q + h][4 * g]);
+          y = *reinterpret_cast<const float4*>(&shift_buf[warp][2 * q + h][32 + 4 * g]);
+        } else if (have[h]) {
+          x = *reinterpret_cast<const float4*>(at[h] + v0 + 4 * g);
+          y = *reinterpret_cast<const float4*>(at[h] + v0 + 32 + 4 * g);
+        }
+        l[h][0] = x.x; l[h][1] = x.y; l[h][2] = x.z; l[h][3] = x.w;
+        l[h][4] = y.x; l[h][5] = y.y; l[h][6] = y.z; l[h][7] = y.w;
+      } else {
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        Stats x;
-        x.m = __shfl_xor_sync(0xffffffffu, st[h].m, o); x.s = __shfl_xor_sync(0xffffffffu, st[h].s, o);
-        x.t = __shfl_xor_sync(0xffffffffu, st[h].t, o); x.arg = __shfl_xor_sync(0xffffffffu, st[h].arg, o);
-        st[h] = stats_merge(st[h], x);
+        for (int e = 0; e < 8; ++e) {
+          const int v = v0 + adapter_entry(e, g);
+          l[h][e] = have[h] && v < p.V ? at[h][v] : -CUDART_INF_F;
+        }
       }
-      if (q == 0) warp_stats[warp][g + 8 * h] = make_float4(st[h].m, st[h].s, st[h].t, __int_as_float(st[h].arg));
     }
-    __syncthreads();
-    if (threadIdx.x < rows) {
-      Stats all = stats_empty();
+    float d[4][4] = {};
+    for (int k = 0; k < steps; ++k) {
+      const bool in = 16 * k + 4 * q < p.rank;
+      uint2 w[8];
 #pragma unroll
-      for (int w = 0; w < kAdUpWarps; ++w) {
-        const float4 x = warp_stats[w][threadIdx.x];
-        all = stats_merge(all, Stats{x.x, x.y, x.z, __float_as_int(x.w)});
+      for (int e = 0; e < 8; ++e) {
+        const int v = v0 + adapter_entry(e, g);
+        w[e] = make_uint2(0u, 0u);
+        if (in && v < p.V) w[e] = *reinterpret_cast<const uint2*>(Bm + static_cast<size_t>(v) * p.pitch + 16 * k + 4 * q);
       }
-      p.partials[(row0 + threadIdx.x) * p.part_stride + part] = make_float4(all.m, all.s, all.t, __int_as_float(all.arg));
+#pragma unroll
+      for (int pl = 2; pl >= 0; --pl) {
+        const uint2 u = planes[pl][k][g][q];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {                    // entries 2 t at m = g, 2 t + 1 at m = g + 8
+          const uint32_t f[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y};
+          mma_bf16(d[t], f, u.x, u.y);
+        }
+      }
     }
-    if (part == 0) {                                     // what the GEMM left beyond this kernel's parts counts no more
-      const int stale = p.nparts - P;
-      for (int i = threadIdx.x; i < rows * stale; i += kAdUpWarps * 32)
-        p.partials[(row0 + i / stale) * p.part_stride + P + i % stale] =
-            make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(0x7fffffff));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (!have[h]) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) l[h][e] += d[e >> 1][2 * (e & 1) + h];         // (past the vocabulary: -inf + 0)
+      if (!kVec && whole) {
+        *reinterpret_cast<float4*>(&shift_buf[warp][2 * q + h][4 * g]) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
+        *reinterpret_cast<float4*>(&shift_buf[warp][2 * q + h][32 + 4 * g]) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
+      } else if (whole) {
+        *reinterpret_cast<float4*>(at[h] + v0 + 4 * g) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
+        *reinterpret_cast<float4*>(at[h] + v0 + 32 + 4 * g) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int v = v0 + adapter_entry(e, g);
+          if (v < p.V) at[h][v] = l[h][e];
+        }
+      }
+      if (v0 + adapter_entry(0, g) < p.V)
+        st[h].fold(l[h], p.want_arg, [&](int e) { return v0 + adapter_entry(e, g); });
+    }
+    if (!kVec && whole) {
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (have[h]) at[h][v0 + 8 * e + g] = shift_buf[warp][2 * q + h][8 * e + g];
+      __syncwarp();
     }
   }
+  // a row's statistics over the eight lanes that hold it, then over the warps
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    Stats s = st[h].stats();
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      Stats x;
+      x.m = __shfl_xor_sync(0xffffffffu, s.m, o); x.s = __shfl_xor_sync(0xffffffffu, s.s, o);
+      x.t = __shfl_xor_sync(0xffffffffu, s.t, o); x.arg = __shfl_xor_sync(0xffffffffu, s.arg, o);
+      s = stats_merge(s, x);
+    }
+    if (g == 0) warp_stats[warp][2 * q + h] = make_float4(s.m, s.s, s.t, __int_as_float(s.arg));
+  }
+  __syncthreads();
+  if (threadIdx.x < n) {
+    Stats all = stats_empty();
+#pragma unroll
+    for (int w = 0; w < kAdUpWarps; ++w) {
+      const float4 x = warp_stats[w][threadIdx.x];
+      all = stats_merge(all, Stats{x.x, x.y, x.z, __float_as_int(x.w)});
+    }
+    p.partials[static_cast<size_t>(tile.row[threadIdx.x]) * p.part_stride + part] = make_float4(all.m, all.s, all.t, __int_as_float(all.arg));
+  }
+  if (part == 0) {                                       // what the GEMM left beyond this kernel's parts counts no more
+    const int stale = p.nparts - P;
+    for (int i = threadIdx.x; i < n * stale; i += kAdUpWarps * 32)
+      p.partials[static_cast<size_t>(tile.row[i / stale]) * p.part_stride + P + i % stale] =
+          make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(0x7fffffff));
+  }
+}
+
+// Tiles that a batch may need: whole ones, and one more for each adapter; or those of every sequence by itself.
+int adapter_max_tiles(int B, int k1, int slots) {
+  const long long own = static_cast<long long>(B) * ((k1 + kAdRows - 1) / kAdRows);
+  const long long shared = static_cast<long long>(B) * k1 / kAdRows + (B < slots ? B : slots);
+  return static_cast<int>(B <= kAdMaxSorted && shared < own ? shared : own);
 }
 
 cudaError_t launch_adapter_down(const AdapterParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(p.B), static_cast<unsigned>((p.rank + 15) / 16), static_cast<unsigned>((p.rows_per_seq + 15) / 16));
+  cfg.gridDim = dim3(static_cast<unsigned>(p.B + 1), static_cast<unsigned>((p.rank + 15) / 16), static_cast<unsigned>((p.rows_per_seq + 15) / 16));
   cfg.blockDim = dim3(kAdDownWarps * 32); cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -264,13 +410,13 @@ cudaError_t launch_adapter_down(const AdapterParams& p, cudaStream_t stream) {
 cudaError_t launch_adapter_up(const AdapterParams& p, int num_sms, cudaStream_t stream) {
   // Parts of the vocabulary: eight CTAs per SM, a chunk per warp at least, and no more partials than a row has room for.
   const int chunks = (p.V + kAdChunk - 1) / kAdChunk;
-  int P = (8 * num_sms + p.B - 1) / p.B;
+  int P = (8 * num_sms + p.max_tiles - 1) / p.max_tiles;
   if (P > (chunks + kAdUpWarps - 1) / kAdUpWarps) P = (chunks + kAdUpWarps - 1) / kAdUpWarps;
   if (P > p.nparts) P = p.nparts;
   if (P < 1) P = 1;
   const bool vec = p.ldl % 4 == 0 && (reinterpret_cast<uintptr_t>(p.logits) & 15u) == 0;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(p.B), static_cast<unsigned>(P));
+  cfg.gridDim = dim3(static_cast<unsigned>(p.max_tiles), static_cast<unsigned>(P));
   cfg.blockDim = dim3(kAdUpWarps * 32); cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

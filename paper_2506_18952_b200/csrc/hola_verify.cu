@@ -2894,6 +2894,7 @@ struct hola_ctx {
   signed char* hid8;        // [rows][hidden_pitch8] int8 hidden rows (8-bit activation modes), or bf16 rows (aligns_hidden)
   float* hid_scale;         // [max_rows]
   float* ad_u;              // [max_rows][kAdMaxRank] hidden rows behind their adapters' first factors
+  AdapterTile* ad_tiles;    // [max_rows] the batch's rows by adapter
   // staging for hola_verify_host
   void* st_hidden; int* st_tok; void* st_q; float* st_u;
   unsigned char* st_out;      // device block of one call's outputs (status, accept_len, next_tok, entropy, logZ, ...)
@@ -2951,7 +2952,7 @@ OutBlock out_block(int B, int k) {
 }
 
 struct WsLayout {
-  size_t logits, partials, status, pace, hq, hid8, hid_scale, ad_u, st_hidden, st_tok, st_q, st_u, st_out, st_qtok, st_small_end, total;
+  size_t logits, partials, status, pace, hq, hid8, hid_scale, ad_u, ad_tiles, st_hidden, st_tok, st_q, st_u, st_out, st_qtok, st_small_end, total;
 };
 
 // Bytes from one 8-bit hidden row to the next: rows start on 128-byte lines, so that a K block of a row is one line instead of
@@ -2976,6 +2977,7 @@ WsLayout ws_layout(int maxB, int maxK, int H, int V, int num_sms) {
                                                                       // rows as they are, on whole lines
   w.hid_scale = take(2 * rows * 4);                                   // their scales (second plane after the first)
   w.ad_u = take(rows * kAdMaxRank * 4);
+  w.ad_tiles = take(rows * sizeof(AdapterTile));
   w.st_hidden = take(rows * H * 2);
   // the three small per-step inputs side by side: hola_verify_host sends them as one copy
   w.st_tok = take(static_cast<size_t>(maxB) * maxK * 4);
@@ -3565,6 +3567,7 @@ hola_status run_adapted_lm_head(hola_ctx* ctx, const hola_verify_args* a, const 
   p.slots = ad->slots; p.rank = ad->rank; p.pitch = ad->b_pitch;
   p.B = a->B; p.rows_per_seq = a->k + 1; p.H = a->H; p.V = a->V;
   p.hidden = static_cast<const uint16_t*>(a->hidden); p.u = ctx->ad_u;
+  p.tiles = ctx->ad_tiles; p.max_tiles = adapter_max_tiles(a->B, a->k + 1, ad->slots);
   p.logits = logits; p.ldl = ldl; p.partials = ctx->partials; p.part_stride = ctx->part_stride; p.nparts = row_partials(pl);
   p.want_arg = a->fallback == HOLA_FALLBACK_GREEDY;
   p.status = a->status_word; p.clear_status = (a->flags & HOLA_ARG_CLEAR_STATUS) != 0;
@@ -3824,6 +3827,7 @@ hola_status hola_create(hola_ctx** out, int device, int maxB, int maxK, int H, i
   ctx->hid8 = reinterpret_cast<signed char*>(ctx->ws + w.hid8);
   ctx->hid_scale = reinterpret_cast<float*>(ctx->ws + w.hid_scale);
   ctx->ad_u = reinterpret_cast<float*>(ctx->ws + w.ad_u);
+  ctx->ad_tiles = reinterpret_cast<AdapterTile*>(ctx->ws + w.ad_tiles);
   ctx->st_hidden = ctx->ws + w.st_hidden; ctx->st_tok = reinterpret_cast<int*>(ctx->ws + w.st_tok);
   ctx->st_q = ctx->ws + w.st_q; ctx->st_u = reinterpret_cast<float*>(ctx->ws + w.st_u);
   ctx->st_out = reinterpret_cast<unsigned char*>(ctx->ws + w.st_out);

@@ -287,20 +287,18 @@ hola_status hola_lm_head_entropy_static(const hola_verify_args* args, void* cuda
 
 /* Low-rank adapters beside the LM head, one per sequence (the Lo-Bi section's W' = W + AB, kept apart from W so that a batch may hold
  * the requests of many fine-tunes):  for a sequence that uses adapter a, position by position,
- *   l[r][v] = sum_h W[v][h] x[r][h] + sum_i B[v][a][i] u[r][i],   u[r][i] = scale[a] * sum_h A[a][i][h] x[r][h],   i < rank,
+ *   l[r][v] = sum_h W[v][h] x[r][h] + sum_i B[a][v][i] u[r][i],   u[r][i] = scale[a] * sum_h A[a][i][h] x[r][h],   i < rank,
  * and entropy, logZ and everything behind are those of these logits.  W_lm in any of its storage forms; A, B and x are bf16, u and the
  * logits fp32.  An adapter of a lower rank is filled up with zeros.
  * hola_lm_head_adapters is hola_lm_head_entropy, hola_verify_adapters is hola_verify, with the same arguments, checks, streams and
  * outputs; the arrays of `adapters` (a host struct, not looked at after the call) are resident on the device. */
 typedef struct hola_adapters {
   const void* A;            /* bf16 [slots][rank][H], 16-byte aligned                                          */
-  const void* B;            /* bf16 [V][b_pitch], 16-byte aligned: slot s at columns s * rank ..               */
+  const void* B;            /* bf16 [slots][V][rank], 16-byte aligned                                          */
   const float* scale;       /* fp32 [slots], or NULL: 1                                                        */
   const int32_t* ids;       /* int32 [args->B]: the slot that each sequence uses, -1 = none (the bare head)     */
   int32_t slots;            /* >= 1                                                                            */
   int32_t rank;             /* multiple of 8, 8 .. 128                                                         */
-  int32_t b_pitch;          /* columns from one row of B to the next, >= slots * rank, multiple of 8           */
-  int32_t reserved_;
 } hola_adapters;
 hola_status hola_lm_head_adapters(hola_ctx* ctx, const hola_verify_args* args, const hola_adapters* adapters, void* cuda_stream);
 hola_status hola_verify_adapters(hola_ctx* ctx, const hola_verify_args* args, const hola_adapters* adapters, void* cuda_stream);

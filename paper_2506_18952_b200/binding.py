@@ -65,7 +65,7 @@ class hola_shard_args(ctypes.Structure):
 
 class hola_adapters(ctypes.Structure):
     _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ids", ctypes.c_void_p),
-                ("slots", ctypes.c_int32), ("rank", ctypes.c_int32), ("b_pitch", ctypes.c_int32), ("reserved_", ctypes.c_int32)]
+                ("slots", ctypes.c_int32), ("rank", ctypes.c_int32)]
 
 
 class hola_logprobs_args(ctypes.Structure):
@@ -322,8 +322,8 @@ def hola_lm_head_entropy_static(hidden, W_lm, logits, entropy, logZ, stream=None
 
 class AdapterBank:
     """Low-rank adapters resident on the device for hola_lm_head_adapters and hola_verify_adapters: slot s adds scale[s] * B[s] A[s] to
-    the LM head of the sequences that name it.  Laid out once: A as [slots, rank, H], B as rows of all slots side by side
-    [V, pitch], the rank filled up with zeros to a multiple of 8."""
+    the LM head of the sequences that name it.  Laid out once: A as [slots, rank, H], B as [slots, V, rank], the rank filled up with
+    zeros to a multiple of 8."""
 
     def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None):
         """A: bf16 [slots, rank, H], B: bf16 [slots, V, rank], scale: fp32 [slots] (None: 1 for all)."""
@@ -347,12 +347,11 @@ class AdapterBank:
             raise HolaError(f"AdapterBank: at least one slot, ranks 1 .. {HOLA_MAX_RANK}")
         self.slots, self.rank, self.H, self.V, self.device = slots, -(-rank // 8) * 8, H, V, device
         self.A = torch.zeros((slots, self.rank, H), dtype=torch.bfloat16, device=device)
-        # (rows of whole 128-byte lines)
-        self.B = torch.zeros((V, -(-slots * self.rank // 64) * 64), dtype=torch.bfloat16, device=device)
+        self.B = torch.zeros((slots, V, self.rank), dtype=torch.bfloat16, device=device)
         self.scale = torch.ones((slots,), dtype=torch.float32, device=device)
         self.struct = st = hola_adapters()
         st.A, st.B, st.scale = self.A.data_ptr(), self.B.data_ptr(), self.scale.data_ptr()
-        st.slots, st.rank, st.b_pitch = slots, self.rank, self.B.shape[1]
+        st.slots, st.rank = slots, self.rank
         self.address = ctypes.addressof(st)
 
     def set(self, slot: int, A: torch.Tensor, B: torch.Tensor, scale=None) -> None:
@@ -363,11 +362,10 @@ class AdapterBank:
             raise HolaError(f"AdapterBank.set: slot 0 .. {self.slots - 1}, A [r, {self.H}], B [{self.V}, r], r at most {self.rank}")
         if A.dtype != torch.bfloat16 or B.dtype != torch.bfloat16:
             raise HolaError("AdapterBank.set takes bfloat16 factors")
-        at = slot * self.rank
         self.A[slot, :r] = A
         self.A[slot, r:] = 0
-        self.B[:, at:at + r] = B
-        self.B[:, at + r:at + self.rank] = 0
+        self.B[slot, :, :r] = B
+        self.B[slot, :, r:] = 0
         self.scale[slot] = 1.0 if scale is None else scale
 
 

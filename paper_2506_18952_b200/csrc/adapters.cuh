@@ -28,10 +28,10 @@ struct AdapterTile {
 
 struct AdapterParams {
   const uint16_t* A;           // bf16 [slots][rank][H]
-  const uint16_t* Bm;          // bf16 [V][pitch]: slot s at columns s * rank
+  const uint16_t* Bm;          // bf16 [slots][V][rank]
   const float* scale;          // [slots], or null: 1
   const int* ids;              // [B]
-  int slots, rank, pitch;
+  int slots, rank;
   int B, rows_per_seq, H, V;
   const uint16_t* hidden;      // [B][rows_per_seq][H]
   float* u;                    // [rows][kAdMaxRank]
@@ -170,11 +170,11 @@ __global__ void __launch_bounds__(kAdDownWarps * 32, 1) adapter_down_kernel(cons
   }
 }
 
-// Running statistics of a row about a point `ref` that trails the maximum by 4 at most, so that a rise of the maximum rarely makes a
-// warp rescale.  In units of ln 2: x = l log2 e - ref log2 e, s = sum 2^x, t = sum 2^x x.
+// Running statistics of a row about a point that trails the maximum by 4 at most, so that a rise of the maximum rarely makes a
+// warp rescale.  In units of ln 2: x = l log2 e + shift, s = sum 2^x, t = sum 2^x x.
 struct RowStats {
   float m, rise, shift;
-  uint64_t s2, t2;
+  uint64_t s2, t2;             // two halves of either sum
   int arg;
   __device__ __forceinline__ void clear() {
     m = rise = -CUDART_INF_F;
@@ -182,8 +182,8 @@ struct RowStats {
     s2 = t2 = 0;
     arg = 0x7fffffff;
   }
-  // Eight logits; entry i is vocabulary entry v(i), rising with i.  -inf: none (all of them none: nothing is called).
-  template <typename Entry>
+  // Eight logits; entry i is vocabulary entry v(i), rising with i.  kSome: those that are -inf are none (the first one is a logit).
+  template <bool kSome, typename Entry>
   __device__ __forceinline__ void fold(const float* l, int want_arg, Entry v) {
     const float top = fmaxf(max3(max3(l[0], l[1], l[2]), max3(l[3], l[4], l[5]), l[6]), l[7]);
     if (want_arg && top > m) {
@@ -200,32 +200,31 @@ struct RowStats {
       if (rise != -CUDART_INF_F) {
         const float dx = shift - old, e = ex2_approx(dx);
         const uint64_t e2 = pack2(e, e);
-        uint64_t d;
-        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(fma2(pack2(dx, dx), s2, t2)), "l"(e2));
-        t2 = d;
-        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(s2), "l"(e2));
-        s2 = d;
+        t2 = mul2(fma2(pack2(dx, dx), s2, t2), e2);
+        s2 = mul2(s2, e2);
       }
       rise = top + 4.f;
     }
     const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint64_t x = fma2(pack2(l[2 * i], l[2 * i + 1]), l2e, sh);
+      uint64_t x = fma2(pack2(l[2 * i], l[2 * i + 1]), l2e, sh);
       float a, b;
       unpack2(x, a, b);
-      // (none: 2^-126, of which nothing is left beside the sum, and a product that stays finite)
-      const uint64_t y = pack2(fmaxf(a, -126.f), fmaxf(b, -126.f)), e = pack2(ex2_approx(a), ex2_approx(b));
+      const uint64_t e = pack2(ex2_approx(a), ex2_approx(b));
+      if (kSome) x = pack2(fmaxf(a, -1e30f), fmaxf(b, -1e30f));       // (0 * -inf)
       s2 = add2(s2, e);
-      t2 = fma2(e, y, t2);
+      t2 = fma2(e, x, t2);
     }
   }
   __device__ __forceinline__ Stats stats() const {
-    if (m == -CUDART_INF_F) return stats_empty();
     float a, b, c, d;
     unpack2(s2, a, b);
     unpack2(t2, c, d);
-    const float x = fmaf(m, kLog2e, shift), e = ex2_approx(-x), s = a + b;    // (x of the maximum, as it was summed)
+    const float s = a + b;
+    if (s == 0.f) return stats_empty();
+    if (!(s < CUDART_INF_F)) return Stats{CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F, arg};       // (no distribution)
+    const float x = fmaf(m, kLog2e, shift), e = ex2_approx(-x);               // (x of the maximum, as it was summed)
     return Stats{m, s * e, kLn2 * (e * fmaf(-x, s, c + d)), arg};
   }
 };
@@ -234,27 +233,36 @@ struct RowStats {
 // 2 q and 2 q + 1 and, of every 32 entries, the four that stand at m = g and g + 8 of two MMAs: side by side, 16 bytes of each row.
 // Rows that do not lie on 16-byte boundaries (kVec false) pass through shared memory, so that eight lanes share a sector; every lane
 // sums the same entries in the same order either way.
-__device__ __forceinline__ int adapter_entry(int e, int g) { return 32 * (e >> 2) + 4 * g + (e & 3); }     // e: 0 .. 7
-template <bool kVec>
-__global__ void __launch_bounds__(kAdUpWarps * 32, 5) adapter_up_kernel(const AdapterParams p, int P) {
-  __shared__ uint2 planes[3][kAdMaxRank / 16][kAdRows][4];       // [plane][16 ranks][row][q]: ranks 4q .. 4q+3 of the sixteen
+__device__ __forceinline__ constexpr int adapter_entry(int e) { return 32 * (e >> 2) + (e & 3); }     // e: 0 .. 7; + 4 g
+
+// As in the first product, the order of the ranks is free.  Sixteen at a time, lane q loads four (8 bytes) of a row of B; where whole
+// blocks of 32 ranks are known beforehand (kR: the rank, or 0), eight (16 bytes) for two MMA steps.
+template <int kR>
+__device__ __forceinline__ int adapter_rank(int k, int q) {      // first of the four ranks that lane q holds in step k
+  return kR % 32 == 0 && kR > 0 ? 32 * (k >> 1) + 8 * q + 4 * (k & 1) : 16 * k + 4 * q;
+}
+
+// What bounds it: for many rows HBM (the logits come and go once more), else the L2; a warp step takes some 130 issue slots.
+template <bool kVec, int kR>
+__global__ void __launch_bounds__(kAdUpWarps * 32, kR % 16 == 0 && kR != 16 ? 4 : 5) adapter_up_kernel(const AdapterParams p, int P) {
+  constexpr int kSteps = (kR + 15) / 16;                 // 0: not known beforehand
+  __shared__ uint2 planes[3][kR ? kSteps : kAdMaxRank / 16][kAdRows][4];         // [plane][16 ranks][row][q]
   __shared__ float4 warp_stats[kAdUpWarps][kAdRows];
   __shared__ __align__(16) float shift_buf[kVec ? 1 : kAdUpWarps][kVec ? 1 : kAdRows][kAdChunk + 4];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int part = blockIdx.y;
+  const int rank = kR ? kR : p.rank, steps = kR ? kSteps : (rank + 15) >> 4;
   grid_dependency_wait();
   const AdapterTile& tile = p.tiles[blockIdx.x];
   const int n = tile.n;
   if (n == 0) return;
   const int chunks = (p.V + kAdChunk - 1) / kAdChunk, per = (chunks + P - 1) / P;
   const int c_end = min(chunks, (part + 1) * per);
-  const int steps = (p.rank + 15) >> 4;
-  const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.rank;
   for (int i = threadIdx.x; i < steps * kAdRows * 4; i += kAdUpWarps * 32) {
     const int k = i >> 5, r = (i >> 2) & 7, qq = i & 3;
     uint32_t w[3][2] = {};
     if (r < n) {
-      const float4 u4 = *reinterpret_cast<const float4*>(p.u + static_cast<size_t>(tile.row[r]) * kAdMaxRank + 16 * k + 4 * qq);
+      const float4 u4 = *reinterpret_cast<const float4*>(p.u + static_cast<size_t>(tile.row[r]) * kAdMaxRank + adapter_rank<kR>(k, qq));
       float u[4] = {u4.x, u4.y, u4.z, u4.w};
 #pragma unroll
       for (int pl = 0; pl < 3; ++pl)
@@ -268,62 +276,92 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, 5) adapter_up_kernel(const Ad
 #pragma unroll
     for (int pl = 0; pl < 3; ++pl) planes[pl][k][r][qq] = make_uint2(w[pl][0], w[pl][1]);
   }
+  // This lane's rows of the logits, from entry 4 g (kVec) or g on, and its ranks of B, from entry 4 g on.
   const bool have[2] = {2 * q < n, 2 * q + 1 < n};
   float* at[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl;
+  for (int h = 0; h < 2; ++h)
+    at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl + (kVec ? 4 * g : g);
+  const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.V * rank;
   __syncthreads();
   RowStats st[2];
   st[0].clear(); st[1].clear();
   for (int c = part * per + warp; c < c_end; c += kAdUpWarps) {
-    const int v0 = c * kAdChunk;
+    const int v0 = c * kAdChunk, v4 = v0 + 4 * g;
     const bool whole = v0 + kAdChunk <= p.V;
     float l[2][8];
-    if (!kVec && whole) {
+    if (whole) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (kVec) {
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+          if (have[h]) {
+            x = *reinterpret_cast<const float4*>(at[h] + v0);
+            y = *reinterpret_cast<const float4*>(at[h] + v0 + 32);
+          }
+          l[h][0] = x.x; l[h][1] = x.y; l[h][2] = x.z; l[h][3] = x.w;
+          l[h][4] = y.x; l[h][5] = y.y; l[h][6] = y.z; l[h][7] = y.w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) shift_buf[warp][2 * q + h][8 * e + g] = have[h] ? at[h][v0 + 8 * e] : 0.f;
+        }
+      }
+      if (!kVec) {
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) l[h][e] = shift_buf[warp][2 * q + h][4 * g + adapter_entry(e)];
+      }
+    } else {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) shift_buf[warp][2 * q + h][8 * e + g] = have[h] ? at[h][v0 + 8 * e + g] : 0.f;
-      __syncwarp();
+        for (int e = 0; e < 8; ++e)
+          l[h][e] = have[h] && v4 + adapter_entry(e) < p.V ? at[h][v0 + adapter_entry(e) + (kVec ? 0 : 3 * g)] : -CUDART_INF_F;
     }
+    float d[4][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (whole) {
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-        if (!kVec) {
-          x = *reinterpret_cast<const float4*>(&shift_buf[warp][2 * q + h][4 * g]);
-          y = *reinterpret_cast<const float4*>(&shift_buf[warp][2 * q + h][32 + 4 * g]);
-        } else if (have[h]) {
-          x = *reinterpret_cast<const float4*>(at[h] + v0 + 4 * g);
-          y = *reinterpret_cast<const float4*>(at[h] + v0 + 32 + 4 * g);
+    for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
+    const uint16_t* rows = Bm + static_cast<size_t>(v4) * rank;
+    const int past = p.V - 1 - v4;                       // (a ragged step: entries past the vocabulary read its last row)
+    auto row = [&](int e) { return rows + static_cast<ptrdiff_t>(whole ? adapter_entry(e) : min(adapter_entry(e), past)) * rank; };
+    if (kR % 32 == 0 && kR > 0) {
+#pragma unroll 1
+      for (int k = 0; k < kSteps; k += 2) {
+        uint4 w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint4*>(row(e) + 16 * k + 8 * q);
+#pragma unroll
+        for (int pl = 2; pl >= 0; --pl) {
+          const uint2 u0 = planes[pl][k][g][q], u1 = planes[pl][k + 1][g][q];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {                  // entries 2 t at m = g, 2 t + 1 at m = g + 8
+            const uint32_t f0[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y},
+                           f1[4] = {w[2 * t].z, w[2 * t + 1].z, w[2 * t].w, w[2 * t + 1].w};
+            mma_bf16(d[t], f0, u0.x, u0.y);
+            mma_bf16(d[t], f1, u1.x, u1.y);
+          }
         }
-        l[h][0] = x.x; l[h][1] = x.y; l[h][2] = x.z; l[h][3] = x.w;
-        l[h][4] = y.x; l[h][5] = y.y; l[h][6] = y.z; l[h][7] = y.w;
-      } else {
+      }
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < steps; ++k) {
+        const bool in = kR % 16 == 0 && kR > 0 ? true : 16 * k + 4 * q < rank;
+        uint2 w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int v = v0 + adapter_entry(e, g);
-          l[h][e] = have[h] && v < p.V ? at[h][v] : -CUDART_INF_F;
+          w[e] = make_uint2(0u, 0u);
+          if (in) w[e] = *reinterpret_cast<const uint2*>(row(e) + 16 * k + 4 * q);
         }
-      }
-    }
-    float d[4][4] = {};
-    for (int k = 0; k < steps; ++k) {
-      const bool in = 16 * k + 4 * q < p.rank;
-      uint2 w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int v = v0 + adapter_entry(e, g);
-        w[e] = make_uint2(0u, 0u);
-        if (in && v < p.V) w[e] = *reinterpret_cast<const uint2*>(Bm + static_cast<size_t>(v) * p.pitch + 16 * k + 4 * q);
-      }
+        for (int pl = 2; pl >= 0; --pl) {
+          const uint2 u = planes[pl][k][g][q];
 #pragma unroll
-      for (int pl = 2; pl >= 0; --pl) {
-        const uint2 u = planes[pl][k][g][q];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {                    // entries 2 t at m = g, 2 t + 1 at m = g + 8
-          const uint32_t f[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y};
-          mma_bf16(d[t], f, u.x, u.y);
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t f[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y};
+            mma_bf16(d[t], f, u.x, u.y);
+          }
         }
       }
     }
@@ -331,22 +369,24 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, 5) adapter_up_kernel(const Ad
     for (int h = 0; h < 2; ++h) {
       if (!have[h]) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) l[h][e] += d[e >> 1][2 * (e & 1) + h];         // (past the vocabulary: -inf + 0)
-      if (!kVec && whole) {
-        *reinterpret_cast<float4*>(&shift_buf[warp][2 * q + h][4 * g]) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
-        *reinterpret_cast<float4*>(&shift_buf[warp][2 * q + h][32 + 4 * g]) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
-      } else if (whole) {
-        *reinterpret_cast<float4*>(at[h] + v0 + 4 * g) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
-        *reinterpret_cast<float4*>(at[h] + v0 + 32 + 4 * g) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
-      } else {
+      for (int e = 0; e < 8; ++e) l[h][e] += d[e >> 1][2 * (e & 1) + h];         // (past the vocabulary: -inf + something)
+      if (!whole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int v = v0 + adapter_entry(e, g);
-          if (v < p.V) at[h][v] = l[h][e];
+          if (v4 + adapter_entry(e) < p.V) at[h][v0 + adapter_entry(e) + (kVec ? 0 : 3 * g)] = l[h][e];
+          else l[h][e] = -CUDART_INF_F;
         }
+        if (v4 < p.V) st[h].template fold<true>(l[h], p.want_arg, [&](int e) { return v4 + adapter_entry(e); });
+        continue;
       }
-      if (v0 + adapter_entry(0, g) < p.V)
-        st[h].fold(l[h], p.want_arg, [&](int e) { return v0 + adapter_entry(e, g); });
+      if (kVec) {
+        *reinterpret_cast<float4*>(at[h] + v0) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
+        *reinterpret_cast<float4*>(at[h] + v0 + 32) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) shift_buf[warp][2 * q + h][4 * g + adapter_entry(e)] = l[h][e];
+      }
+      st[h].template fold<false>(l[h], p.want_arg, [&](int e) { return v4 + adapter_entry(e); });
     }
     if (!kVec && whole) {
       __syncwarp();
@@ -354,7 +394,7 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, 5) adapter_up_kernel(const Ad
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (have[h]) at[h][v0 + 8 * e + g] = shift_buf[warp][2 * q + h][8 * e + g];
+          if (have[h]) at[h][v0 + 8 * e] = shift_buf[warp][2 * q + h][8 * e + g];
       __syncwarp();
     }
   }
@@ -422,5 +462,13 @@ cudaError_t launch_adapter_up(const AdapterParams& p, int num_sms, cudaStream_t 
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return vec ? cudaLaunchKernelEx(&cfg, adapter_up_kernel<true>, p, P) : cudaLaunchKernelEx(&cfg, adapter_up_kernel<false>, p, P);
+  auto* kernel = adapter_up_kernel<true, 0>;
+  switch (p.rank) {
+    case 8: kernel = vec ? adapter_up_kernel<true, 8> : adapter_up_kernel<false, 8>; break;
+    case 16: kernel = vec ? adapter_up_kernel<true, 16> : adapter_up_kernel<false, 16>; break;
+    case 32: kernel = vec ? adapter_up_kernel<true, 32> : adapter_up_kernel<false, 32>; break;
+    case 64: kernel = vec ? adapter_up_kernel<true, 64> : adapter_up_kernel<false, 64>; break;
+    default: kernel = vec ? adapter_up_kernel<true, 0> : adapter_up_kernel<false, 0>;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, p, P);
 }

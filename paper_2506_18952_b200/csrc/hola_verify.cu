@@ -647,6 +647,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -3564,7 +3569,7 @@ hola_status run_adapted_lm_head(hola_ctx* ctx, const hola_verify_args* a, const 
   if (!ad) return run_lm_head(ctx, a, logits, ldl, pl, stream, few_before, next_reads_inputs, draft_pass);
   AdapterParams p = {};
   p.A = static_cast<const uint16_t*>(ad->A); p.Bm = static_cast<const uint16_t*>(ad->B); p.scale = ad->scale; p.ids = ad->ids;
-  p.slots = ad->slots; p.rank = ad->rank; p.pitch = ad->b_pitch;
+  p.slots = ad->slots; p.rank = ad->rank;
   p.B = a->B; p.rows_per_seq = a->k + 1; p.H = a->H; p.V = a->V;
   p.hidden = static_cast<const uint16_t*>(a->hidden); p.u = ctx->ad_u;
   p.tiles = ctx->ad_tiles; p.max_tiles = adapter_max_tiles(a->B, a->k + 1, ad->slots);
@@ -3586,7 +3591,6 @@ hola_status check_adapters(const hola_adapters* ad) {
   if (!ad || !ad->A || !ad->B || !ad->ids || ad->slots <= 0 || ad->rank <= 0) return HOLA_ERR_INVALID_ARG;
   if (!aligned16(ad->A) || !aligned16(ad->B)) return HOLA_ERR_INVALID_ARG;
   if (ad->rank % 8 != 0 || ad->rank > kAdMaxRank) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (ad->b_pitch % 8 != 0 || static_cast<long long>(ad->slots) * ad->rank > ad->b_pitch) return HOLA_ERR_INVALID_ARG;
   return HOLA_OK;
 }
 

@@ -118,11 +118,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {     // Na
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ float lp_float(float x) { return x; }
 __device__ __forceinline__ float lp_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float lp_float(__half x) { return __half2float(x); }

@@ -35,7 +35,8 @@ struct AdapterParams {
   int B, rows_per_seq, H, V;
   const uint16_t* hidden;      // [B][rows_per_seq][H]
   float* u;                    // [rows][kAdMaxRank]
-  AdapterTile* tiles;          // [max_tiles], those that are not needed with n = 0
+  AdapterTile* tiles;          // [max_tiles]
+  int* n_tiles;                // how many the batch needs
   int max_tiles;
   float* logits;
   int ldl;
@@ -65,19 +66,18 @@ __device__ __forceinline__ void adapter_tiles(const AdapterParams& p) {
   __shared__ int ids[kAdMaxSorted], users[kAdMaxSorted];
   const int tid = threadIdx.x, nthr = blockDim.x, k1 = p.rows_per_seq, B = p.B;
   const int per_seq = (k1 + kAdRows - 1) / kAdRows;
-  for (int t = tid; t < p.max_tiles; t += nthr) p.tiles[t].n = 0;
   if (B > kAdMaxSorted) {
-    __syncthreads();
     for (int i = tid; i < B * per_seq; i += nthr) {
       const int b = i / per_seq, j0 = (i - b * per_seq) * kAdRows, a = adapter_of(p, b);
-      if (a < 0) continue;
       AdapterTile& t = p.tiles[i];
       t.adapter = a;
-      t.n = min(kAdRows, k1 - j0);
+      t.n = a < 0 ? 0 : min(kAdRows, k1 - j0);
       for (int j = 0; j < kAdRows; ++j) t.row[j] = b * k1 + j0 + j;
     }
+    if (tid == 0) *p.n_tiles = B * per_seq;
     return;
   }
+  if (tid == 0) *p.n_tiles = 0;
   for (int b = tid; b < B; b += nthr) ids[b] = adapter_of(p, b);
   __syncthreads();
   for (int b = tid; b < B; b += nthr) {                  // how many use the adapter, at its first user; 0 at the others
@@ -107,6 +107,7 @@ __device__ __forceinline__ void adapter_tiles(const AdapterParams& p) {
       if (i % kAdRows == 0) {
         t.adapter = ids[b];
         t.n = min(kAdRows, all * k1 - i);
+        if (t.n == all * k1 - i) atomicMax(p.n_tiles, first + i / kAdRows + 1);        // (the adapter's last one)
       }
     }
   }
@@ -229,203 +230,258 @@ struct RowStats {
   }
 };
 
-// A warp step covers 64 vocabulary entries, the M of four MMAs, and the tile's eight rows, their N.  Lane (g, q) ends up with rows
-// 2 q and 2 q + 1 and, of every 32 entries, the four that stand at m = g and g + 8 of two MMAs: side by side, 16 bytes of each row.
-// Rows that do not lie on 16-byte boundaries (kVec false) pass through shared memory, so that eight lanes share a sector; every lane
-// sums the same entries in the same order either way.
-__device__ __forceinline__ constexpr int adapter_entry(int e) { return 32 * (e >> 2) + (e & 3); }     // e: 0 .. 7; + 4 g
-
+// A warp step covers 64 vocabulary entries, the M of four MMAs, and the tile's eight rows, their N.  Lane (g, q) holds entries g, 8 + g,
+// 16 + g ... of rows 2 q and 2 q + 1.  Rows of the logits that start on 16-byte boundaries (kVec) come and go by bulk copies through
+// three buffers of the warp's own, two steps ahead; others are loaded and stored by the lanes, eight of which share a sector.  Every
+// lane sums the same entries in the same order either way.
+//
 // As in the first product, the order of the ranks is free.  Sixteen at a time, lane q loads four (8 bytes) of a row of B; where whole
 // blocks of 32 ranks are known beforehand (kR: the rank, or 0), eight (16 bytes) for two MMA steps.
 template <int kR>
 __device__ __forceinline__ int adapter_rank(int k, int q) {      // first of the four ranks that lane q holds in step k
   return kR % 32 == 0 && kR > 0 ? 32 * (k >> 1) + 8 * q + 4 * (k & 1) : 16 * k + 4 * q;
 }
+constexpr int kAdStages = 3, kAdPitch = kAdChunk + 4;            // (floats from row to row: no two rows of a step on the same banks)
 
-// What bounds it: for many rows HBM (the logits come and go once more), else the L2; a warp step takes some 130 issue slots.
+// A warp's wait on its own copies.  Should it run out it says so, and the copies get as long again before the warp goes on.
+__device__ __forceinline__ bool adapter_wait(uint32_t bar, uint32_t parity, unsigned* status) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const long long t0 = clock64();
+  bool late = false;
+  while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+    const long long waited = clock64() - t0;
+    if (__any_sync(0xffffffffu, waited > kWaitLimitCycles) && !late) {
+      late = true;
+      if (status && (threadIdx.x & 31) == 0) atomicOr(status, HOLA_FLAG_TIMEOUT);
+    }
+    if (__any_sync(0xffffffffu, waited > 2 * kWaitLimitCycles)) return false;
+  }
+  return true;
+}
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+
+// What bounds it: for many rows HBM (the logits come and go once more), else the L2 and the chain of a step.
 template <bool kVec, int kR>
-__global__ void __launch_bounds__(kAdUpWarps * 32, kR % 16 == 0 && kR != 16 ? 4 : 5) adapter_up_kernel(const AdapterParams p, int P) {
+__global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) adapter_up_kernel(const AdapterParams p) {
   constexpr int kSteps = (kR + 15) / 16;                 // 0: not known beforehand
+  constexpr bool kAhead = kR == 8 || kR == 16;           // a step's ranks are asked for while the step before is worked on
   __shared__ uint2 planes[3][kR ? kSteps : kAdMaxRank / 16][kAdRows][4];         // [plane][16 ranks][row][q]
   __shared__ float4 warp_stats[kAdUpWarps][kAdRows];
-  __shared__ __align__(16) float shift_buf[kVec ? 1 : kAdUpWarps][kVec ? 1 : kAdRows][kAdChunk + 4];
+  __shared__ __align__(128) float buffers[kVec ? kAdUpWarps : 1][kVec ? kAdStages : 1][kVec ? kAdRows * kAdPitch : 4];
+  __shared__ __align__(8) uint64_t arrived[kAdUpWarps][kAdStages];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int part = blockIdx.y;
   const int rank = kR ? kR : p.rank, steps = kR ? kSteps : (rank + 15) >> 4;
+  if (kVec && lane < kAdStages) mbar_init(smem_u32(&arrived[warp][lane]), 1);
+  if (kVec) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   grid_dependency_wait();
-  const AdapterTile& tile = p.tiles[blockIdx.x];
-  const int n = tile.n;
-  if (n == 0) return;
-  const int chunks = (p.V + kAdChunk - 1) / kAdChunk, per = (chunks + P - 1) / P;
-  const int c_end = min(chunks, (part + 1) * per);
-  for (int i = threadIdx.x; i < steps * kAdRows * 4; i += kAdUpWarps * 32) {
-    const int k = i >> 5, r = (i >> 2) & 7, qq = i & 3;
-    uint32_t w[3][2] = {};
-    if (r < n) {
-      const float4 u4 = *reinterpret_cast<const float4*>(p.u + static_cast<size_t>(tile.row[r]) * kAdMaxRank + adapter_rank<kR>(k, qq));
-      float u[4] = {u4.x, u4.y, u4.z, u4.w};
-#pragma unroll
-      for (int pl = 0; pl < 3; ++pl)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const __nv_bfloat16 h = __float2bfloat16_rn(u[e]);
-          u[e] -= __bfloat162float(h);                   // (exact)
-          w[pl][e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(h)) << (16 * (e & 1));
-        }
+  // The CTAs are dealt out to the tiles that there are: P parts of the vocabulary each, in one go as far as there are enough CTAs.
+  const int n_tiles = *p.n_tiles, chunks = (p.V + kAdChunk - 1) / kAdChunk;
+  if (n_tiles == 0) return;
+  const int P = max(1, min(min(static_cast<int>(gridDim.x) / n_tiles, p.nparts), (chunks + kAdUpWarps - 1) / kAdUpWarps));
+  const int per = (chunks + P - 1) / P;
+  int stage = 0;
+  uint32_t parity = 0;
+  bool lost = false;                                     // (a wait of this warp ran out)
+  for (int item = blockIdx.x; item < n_tiles * P; item += gridDim.x) {
+    const int part = item / n_tiles;
+    const AdapterTile& tile = p.tiles[item - part * n_tiles];
+    const int n = tile.n;
+    if (n == 0) continue;
+    const int c_begin = part * per + warp, c_end = min(chunks, (part + 1) * per);
+
+    // Lane r < n moves row r of the tile: 256 bytes a step, the last one of the vocabulary perhaps fewer, in whole 16-byte pieces (a
+    // row's last one lies within its pitch; entries past the vocabulary go back as they came).
+    float* own_row = p.logits + static_cast<size_t>(tile.row[lane < n ? lane : 0]) * p.ldl;
+    auto bytes_of = [&](int c) { return static_cast<uint32_t>((min(kAdChunk, p.V - c * kAdChunk) + 3) & ~3) * 4u; };
+    auto fetch = [&](int c, int stage) {
+      const uint32_t bar = smem_u32(&arrived[warp][stage]), bytes = bytes_of(c);
+      if (lane == 0) mbar_expect_tx(bar, static_cast<uint32_t>(n) * bytes);
+      __syncwarp();
+      if (lane < n) bulk_load(smem_u32(&buffers[warp][stage][lane * kAdPitch]), own_row + c * kAdChunk, bytes, bar);
+    };
+    if (kVec) {
+      __syncwarp();
+      if (c_begin < c_end) fetch(c_begin, stage);
+      if (c_begin + kAdUpWarps < c_end) fetch(c_begin + kAdUpWarps, stage + 1 == kAdStages ? 0 : stage + 1);
     }
+
+    for (int i = threadIdx.x; i < steps * kAdRows * 4; i += kAdUpWarps * 32) {
+      const int k = i >> 5, r = (i >> 2) & 7, qq = i & 3;
+      uint32_t w[3][2] = {};
+      if (r < n) {
+        const float4 u4 = *reinterpret_cast<const float4*>(p.u + static_cast<size_t>(tile.row[r]) * kAdMaxRank + adapter_rank<kR>(k, qq));
+        float u[4] = {u4.x, u4.y, u4.z, u4.w};
 #pragma unroll
-    for (int pl = 0; pl < 3; ++pl) planes[pl][k][r][qq] = make_uint2(w[pl][0], w[pl][1]);
-  }
-  // This lane's rows of the logits, from entry 4 g (kVec) or g on, and its ranks of B, from entry 4 g on.
-  const bool have[2] = {2 * q < n, 2 * q + 1 < n};
-  float* at[2];
+        for (int pl = 0; pl < 3; ++pl)
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl + (kVec ? 4 * g : g);
-  const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.V * rank;
-  __syncthreads();
-  RowStats st[2];
-  st[0].clear(); st[1].clear();
-  for (int c = part * per + warp; c < c_end; c += kAdUpWarps) {
-    const int v0 = c * kAdChunk, v4 = v0 + 4 * g;
-    const bool whole = v0 + kAdChunk <= p.V;
-    float l[2][8];
-    if (whole) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (kVec) {
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-          if (have[h]) {
-            x = *reinterpret_cast<const float4*>(at[h] + v0);
-            y = *reinterpret_cast<const float4*>(at[h] + v0 + 32);
+          for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat16 h = __float2bfloat16_rn(u[e]);
+            u[e] -= __bfloat162float(h);                   // (exact)
+            w[pl][e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(h)) << (16 * (e & 1));
           }
-          l[h][0] = x.x; l[h][1] = x.y; l[h][2] = x.z; l[h][3] = x.w;
-          l[h][4] = y.x; l[h][5] = y.y; l[h][6] = y.z; l[h][7] = y.w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) shift_buf[warp][2 * q + h][8 * e + g] = have[h] ? at[h][v0 + 8 * e] : 0.f;
-        }
       }
+#pragma unroll
+      for (int pl = 0; pl < 3; ++pl) planes[pl][k][r][qq] = make_uint2(w[pl][0], w[pl][1]);
+    }
+    // This lane's rows of the logits, from entry g on, and B from entry g and its first rank on.
+    const bool have[2] = {2 * q < n, 2 * q + 1 < n};
+    float* at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl + g;
+    const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.V * rank;
+    __syncthreads();
+    RowStats st[2];
+    st[0].clear(); st[1].clear();
+    uint2 ahead[8];
+    auto row = [&](int c, int e) {                         // (a ragged step: entries past the vocabulary read its last row)
+      const int v = c * kAdChunk + 8 * e + g;
+      return Bm + static_cast<size_t>(c * kAdChunk + kAdChunk <= p.V ? v : min(v, p.V - 1)) * rank;
+    };
+    auto ask = [&](int c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ahead[e] = make_uint2(0u, 0u);
+        if (kR == 16 || 4 * q < kR) ahead[e] = *reinterpret_cast<const uint2*>(row(c, e) + 4 * q);
+      }
+    };
+    if (kAhead && c_begin < c_end) ask(c_begin);
+    for (int c = c_begin; c < c_end; c += kAdUpWarps) {
+      const int v0 = c * kAdChunk, vg = v0 + g;
+      const bool whole = v0 + kAdChunk <= p.V;
+      float* buf[2];
+      float l[2][8];
       if (!kVec) {
-        __syncwarp();
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) l[h][e] = shift_buf[warp][2 * q + h][4 * g + adapter_entry(e)];
+          for (int e = 0; e < 8; ++e) l[h][e] = have[h] && vg + 8 * e < p.V ? at[h][v0 + 8 * e] : -CUDART_INF_F;
       }
-    } else {
+      float d[4][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          l[h][e] = have[h] && v4 + adapter_entry(e) < p.V ? at[h][v0 + adapter_entry(e) + (kVec ? 0 : 3 * g)] : -CUDART_INF_F;
-    }
-    float d[4][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
-    const uint16_t* rows = Bm + static_cast<size_t>(v4) * rank;
-    const int past = p.V - 1 - v4;                       // (a ragged step: entries past the vocabulary read its last row)
-    auto row = [&](int e) { return rows + static_cast<ptrdiff_t>(whole ? adapter_entry(e) : min(adapter_entry(e), past)) * rank; };
-    if (kR % 32 == 0 && kR > 0) {
-#pragma unroll 1
-      for (int k = 0; k < kSteps; k += 2) {
-        uint4 w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint4*>(row(e) + 16 * k + 8 * q);
-#pragma unroll
-        for (int pl = 2; pl >= 0; --pl) {
-          const uint2 u0 = planes[pl][k][g][q], u1 = planes[pl][k + 1][g][q];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {                  // entries 2 t at m = g, 2 t + 1 at m = g + 8
-            const uint32_t f0[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y},
-                           f1[4] = {w[2 * t].z, w[2 * t + 1].z, w[2 * t].w, w[2 * t + 1].w};
-            mma_bf16(d[t], f0, u0.x, u0.y);
-            mma_bf16(d[t], f1, u1.x, u1.y);
-          }
-        }
-      }
-    } else {
-#pragma unroll 1
-      for (int k = 0; k < steps; ++k) {
-        const bool in = kR % 16 == 0 && kR > 0 ? true : 16 * k + 4 * q < rank;
+      for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
+      if (kAhead) {
         uint2 w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[e] = make_uint2(0u, 0u);
-          if (in) w[e] = *reinterpret_cast<const uint2*>(row(e) + 16 * k + 4 * q);
-        }
+        for (int e = 0; e < 8; ++e) w[e] = ahead[e];
+        if (c + kAdUpWarps < c_end) ask(c + kAdUpWarps);
 #pragma unroll
         for (int pl = 2; pl >= 0; --pl) {
-          const uint2 u = planes[pl][k][g][q];
+          const uint2 u = planes[pl][0][g][q];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
+          for (int t = 0; t < 4; ++t) {                    // entries 16 t + g at m = g, 16 t + 8 + g at m = g + 8
             const uint32_t f[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y};
             mma_bf16(d[t], f, u.x, u.y);
           }
         }
-      }
-    }
+      } else if (kR % 32 == 0 && kR > 0) {
+#pragma unroll 1
+        for (int k = 0; k < kSteps; k += 2) {
+          uint4 w[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (!have[h]) continue;
+          for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint4*>(row(c, e) + 16 * k + 8 * q);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) l[h][e] += d[e >> 1][2 * (e & 1) + h];         // (past the vocabulary: -inf + something)
-      if (!whole) {
+          for (int pl = 2; pl >= 0; --pl) {
+            const uint2 u0 = planes[pl][k][g][q], u1 = planes[pl][k + 1][g][q];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (v4 + adapter_entry(e) < p.V) at[h][v0 + adapter_entry(e) + (kVec ? 0 : 3 * g)] = l[h][e];
-          else l[h][e] = -CUDART_INF_F;
+            for (int t = 0; t < 4; ++t) {
+              const uint32_t f0[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y},
+                             f1[4] = {w[2 * t].z, w[2 * t + 1].z, w[2 * t].w, w[2 * t + 1].w};
+              mma_bf16(d[t], f0, u0.x, u0.y);
+              mma_bf16(d[t], f1, u1.x, u1.y);
+            }
+          }
         }
-        if (v4 < p.V) st[h].template fold<true>(l[h], p.want_arg, [&](int e) { return v4 + adapter_entry(e); });
-        continue;
+      } else {
+#pragma unroll 1
+        for (int k = 0; k < steps; ++k) {
+          const bool in = 16 * k + 4 * q < rank;
+          uint2 w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = make_uint2(0u, 0u);
+            if (in) w[e] = *reinterpret_cast<const uint2*>(row(c, e) + 16 * k + 4 * q);
+          }
+#pragma unroll
+          for (int pl = 2; pl >= 0; --pl) {
+            const uint2 u = planes[pl][k][g][q];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const uint32_t f[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y};
+              mma_bf16(d[t], f, u.x, u.y);
+            }
+          }
+        }
       }
       if (kVec) {
-        *reinterpret_cast<float4*>(at[h] + v0) = make_float4(l[h][0], l[h][1], l[h][2], l[h][3]);
-        *reinterpret_cast<float4*>(at[h] + v0 + 32) = make_float4(l[h][4], l[h][5], l[h][6], l[h][7]);
-      } else {
+        lost = !adapter_wait(smem_u32(&arrived[warp][stage]), parity, p.status);
+        if (lost) break;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) shift_buf[warp][2 * q + h][4 * g + adapter_entry(e)] = l[h][e];
+        for (int h = 0; h < 2; ++h) {
+          buf[h] = &buffers[warp][stage][(2 * q + h) * kAdPitch + g];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) l[h][e] = whole || (have[h] && vg + 8 * e < p.V) ? buf[h][8 * e] : -CUDART_INF_F;
+        }
       }
-      st[h].template fold<false>(l[h], p.want_arg, [&](int e) { return v4 + adapter_entry(e); });
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!have[h]) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          l[h][e] += d[e >> 1][2 * (e & 1) + h];
+          if (!whole && vg + 8 * e >= p.V) l[h][e] = -CUDART_INF_F;
+          else if (kVec) buf[h][8 * e] = l[h][e];
+          else at[h][v0 + 8 * e] = l[h][e];
+        }
+        if (whole) st[h].template fold<false>(l[h], p.want_arg, [&](int e) { return vg + 8 * e; });
+        else if (vg < p.V) st[h].template fold<true>(l[h], p.want_arg, [&](int e) { return vg + 8 * e; });
+      }
+      if (kVec) {
+        fence_async_shared();
+        __syncwarp();
+        if (lane < n) bulk_store(own_row + v0, smem_u32(&buffers[warp][stage][lane * kAdPitch]), bytes_of(c));
+        bulk_commit();
+        // the buffer of the step before is free for the step after next once its rows have been read out
+        const int next = c + 2 * kAdUpWarps;
+        if (next < c_end) {
+          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          fetch(next, stage == 0 ? kAdStages - 1 : stage - 1);
+        }
+        if (++stage == kAdStages) { stage = 0; parity ^= 1u; }
+      }
     }
-    if (!kVec && whole) {
-      __syncwarp();
+    if (kVec) bulk_wait_all();
+    // a row's statistics over the eight lanes that hold it, then over the warps
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      Stats s = st[h].stats();
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (have[h]) at[h][v0 + 8 * e] = shift_buf[warp][2 * q + h][8 * e + g];
-      __syncwarp();
+      for (int o = 4; o < 32; o <<= 1) {
+        Stats x;
+        x.m = __shfl_xor_sync(0xffffffffu, s.m, o); x.s = __shfl_xor_sync(0xffffffffu, s.s, o);
+        x.t = __shfl_xor_sync(0xffffffffu, s.t, o); x.arg = __shfl_xor_sync(0xffffffffu, s.arg, o);
+        s = stats_merge(s, x);
+      }
+      if (g == 0) warp_stats[warp][2 * q + h] = make_float4(s.m, s.s, s.t, __int_as_float(s.arg));
     }
-  }
-  // a row's statistics over the eight lanes that hold it, then over the warps
+    __syncthreads();
+    if (threadIdx.x < n) {
+      Stats all = stats_empty();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    Stats s = st[h].stats();
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      Stats x;
-      x.m = __shfl_xor_sync(0xffffffffu, s.m, o); x.s = __shfl_xor_sync(0xffffffffu, s.s, o);
-      x.t = __shfl_xor_sync(0xffffffffu, s.t, o); x.arg = __shfl_xor_sync(0xffffffffu, s.arg, o);
-      s = stats_merge(s, x);
+      for (int w = 0; w < kAdUpWarps; ++w) {
+        const float4 x = warp_stats[w][threadIdx.x];
+        all = stats_merge(all, Stats{x.x, x.y, x.z, __float_as_int(x.w)});
+      }
+      p.partials[static_cast<size_t>(tile.row[threadIdx.x]) * p.part_stride + part] = make_float4(all.m, all.s, all.t, __int_as_float(all.arg));
     }
-    if (g == 0) warp_stats[warp][2 * q + h] = make_float4(s.m, s.s, s.t, __int_as_float(s.arg));
-  }
-  __syncthreads();
-  if (threadIdx.x < n) {
-    Stats all = stats_empty();
-#pragma unroll
-    for (int w = 0; w < kAdUpWarps; ++w) {
-      const float4 x = warp_stats[w][threadIdx.x];
-      all = stats_merge(all, Stats{x.x, x.y, x.z, __float_as_int(x.w)});
+    if (part == 0) {                                       // what the GEMM left beyond this kernel's parts counts no more
+      const int stale = p.nparts - P;
+      for (int i = threadIdx.x; i < n * stale; i += kAdUpWarps * 32)
+        p.partials[static_cast<size_t>(tile.row[i / stale]) * p.part_stride + P + i % stale] =
+            make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(0x7fffffff));
     }
-    p.partials[static_cast<size_t>(tile.row[threadIdx.x]) * p.part_stride + part] = make_float4(all.m, all.s, all.t, __int_as_float(all.arg));
-  }
-  if (part == 0) {                                       // what the GEMM left beyond this kernel's parts counts no more
-    const int stale = p.nparts - P;
-    for (int i = threadIdx.x; i < n * stale; i += kAdUpWarps * 32)
-      p.partials[static_cast<size_t>(tile.row[i / stale]) * p.part_stride + P + i % stale] =
-          make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(0x7fffffff));
+    if (__syncthreads_or(lost)) return;                  // (the planes and the warps' statistics have been read)
   }
 }
 
@@ -448,15 +504,13 @@ cudaError_t launch_adapter_down(const AdapterParams& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_adapter_up(const AdapterParams& p, int num_sms, cudaStream_t stream) {
-  // Parts of the vocabulary: eight CTAs per SM, a chunk per warp at least, and no more partials than a row has room for.
-  const int chunks = (p.V + kAdChunk - 1) / kAdChunk;
-  int P = (8 * num_sms + p.max_tiles - 1) / p.max_tiles;
-  if (P > (chunks + kAdUpWarps - 1) / kAdUpWarps) P = (chunks + kAdUpWarps - 1) / kAdUpWarps;
-  if (P > p.nparts) P = p.nparts;
-  if (P < 1) P = 1;
+  // As many CTAs as fit (by registers), a chunk per warp at least.
+  const int chunks = (p.V + kAdChunk - 1) / kAdChunk, resident = p.rank == 8 || p.rank == 16 ? 5 : 4;
+  const long long most = static_cast<long long>(p.max_tiles) * ((chunks + kAdUpWarps - 1) / kAdUpWarps);
+  const unsigned grid = static_cast<unsigned>(most < resident * num_sms ? most : resident * num_sms);
   const bool vec = p.ldl % 4 == 0 && (reinterpret_cast<uintptr_t>(p.logits) & 15u) == 0;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(p.max_tiles), static_cast<unsigned>(P));
+  cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kAdUpWarps * 32); cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -470,5 +524,5 @@ cudaError_t launch_adapter_up(const AdapterParams& p, int num_sms, cudaStream_t 
     case 64: kernel = vec ? adapter_up_kernel<true, 64> : adapter_up_kernel<false, 64>; break;
     default: kernel = vec ? adapter_up_kernel<true, 0> : adapter_up_kernel<false, 0>;
   }
-  return cudaLaunchKernelEx(&cfg, kernel, p, P);
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }

@@ -1832,9 +1832,6 @@ __global__ void __launch_bounds__(256) finalize_kernel(const float4* partials, i
   if (lane == 0) stats_to_outputs(st, &logZ[row], &entropy[row]);
 }
 
-#include "adapters.cuh"
-#include "token_logprobs.cuh"
-
 // Vocabulary-parallel form, first exchange record of a rank: per verify row the statistics of this shard's logits
 // (m, s, t, arg-max as a GLOBAL vocabulary index), then per draft position the logit of the draft token if this shard
 // owns it (-inf otherwise).  Blocks 0 .. ceil(M/8)-1 merge the per-CTA partials, the others gather the logits.
@@ -2464,6 +2461,10 @@ __global__ void __launch_bounds__(kSoloWarps ? kSoloThreads : kK3Threads, kSoloW
   }
 }
 
+// ------------------------------------------------------------------------------------------------ adapters, token log probabilities
+#include "adapters.cuh"
+#include "token_logprobs.cuh"
+
 // ------------------------------------------------------------------------------------------------ 8-bit quantiser
 // The 8-bit case of the Lo-Bi quantiser on the LM head (Lo-Bi Optimization section; the quantiser itself is not
 // spelled out there): one vocabulary row per sub-block, symmetric integers in [-127, 127], one fp32 scale per row,
@@ -2900,6 +2901,7 @@ struct hola_ctx {
   float* hid_scale;         // [max_rows]
   float* ad_u;              // [max_rows][kAdMaxRank] hidden rows behind their adapters' first factors
   AdapterTile* ad_tiles;    // [max_rows] the batch's rows by adapter
+  int* ad_n_tiles;          // [1]
   // staging for hola_verify_host
   void* st_hidden; int* st_tok; void* st_q; float* st_u;
   unsigned char* st_out;      // device block of one call's outputs (status, accept_len, next_tok, entropy, logZ, ...)
@@ -2957,7 +2959,7 @@ OutBlock out_block(int B, int k) {
 }
 
 struct WsLayout {
-  size_t logits, partials, status, pace, hq, hid8, hid_scale, ad_u, ad_tiles, st_hidden, st_tok, st_q, st_u, st_out, st_qtok, st_small_end, total;
+  size_t logits, partials, status, pace, hq, hid8, hid_scale, ad_u, ad_tiles, ad_n_tiles, st_hidden, st_tok, st_q, st_u, st_out, st_qtok, st_small_end, total;
 };
 
 // Bytes from one 8-bit hidden row to the next: rows start on 128-byte lines, so that a K block of a row is one line instead of
@@ -2983,6 +2985,7 @@ WsLayout ws_layout(int maxB, int maxK, int H, int V, int num_sms) {
   w.hid_scale = take(2 * rows * 4);                                   // their scales (second plane after the first)
   w.ad_u = take(rows * kAdMaxRank * 4);
   w.ad_tiles = take(rows * sizeof(AdapterTile));
+  w.ad_n_tiles = take(4);
   w.st_hidden = take(rows * H * 2);
   // the three small per-step inputs side by side: hola_verify_host sends them as one copy
   w.st_tok = take(static_cast<size_t>(maxB) * maxK * 4);
@@ -3572,7 +3575,7 @@ hola_status run_adapted_lm_head(hola_ctx* ctx, const hola_verify_args* a, const 
   p.slots = ad->slots; p.rank = ad->rank;
   p.B = a->B; p.rows_per_seq = a->k + 1; p.H = a->H; p.V = a->V;
   p.hidden = static_cast<const uint16_t*>(a->hidden); p.u = ctx->ad_u;
-  p.tiles = ctx->ad_tiles; p.max_tiles = adapter_max_tiles(a->B, a->k + 1, ad->slots);
+  p.tiles = ctx->ad_tiles; p.n_tiles = ctx->ad_n_tiles; p.max_tiles = adapter_max_tiles(a->B, a->k + 1, ad->slots);
   p.logits = logits; p.ldl = ldl; p.partials = ctx->partials; p.part_stride = ctx->part_stride; p.nparts = row_partials(pl);
   p.want_arg = a->fallback == HOLA_FALLBACK_GREEDY;
   p.status = a->status_word; p.clear_status = (a->flags & HOLA_ARG_CLEAR_STATUS) != 0;
@@ -3832,6 +3835,7 @@ hola_status hola_create(hola_ctx** out, int device, int maxB, int maxK, int H, i
   ctx->hid_scale = reinterpret_cast<float*>(ctx->ws + w.hid_scale);
   ctx->ad_u = reinterpret_cast<float*>(ctx->ws + w.ad_u);
   ctx->ad_tiles = reinterpret_cast<AdapterTile*>(ctx->ws + w.ad_tiles);
+  ctx->ad_n_tiles = reinterpret_cast<int*>(ctx->ws + w.ad_n_tiles);
   ctx->st_hidden = ctx->ws + w.st_hidden; ctx->st_tok = reinterpret_cast<int*>(ctx->ws + w.st_tok);
   ctx->st_q = ctx->ws + w.st_q; ctx->st_u = reinterpret_cast<float*>(ctx->ws + w.st_u);
   ctx->st_out = reinterpret_cast<unsigned char*>(ctx->ws + w.st_out);

@@ -398,14 +398,20 @@ __device__ __forceinline__ void lp_send(const LpGroup<T>& g, const LpRow<T>& r, 
     if (!(top > w || (top == w && j <= g_last))) return;
   }
   const int v0 = r.first(j);
+  unsigned which = 0;
 #pragma unroll
   for (int e = 0; e < LpGroup<T>::kEntries; ++e) {
     const float l = g.entry(e);
-    if ((lim == 0 || l > w || (l == w && j <= g_last)) && v0 + e >= 0 && v0 + e < r.V) {
-      const int spot = atomicAdd(n_spots, 1);
-      if (spot < kLpSpots) spots[spot] = lp_key(l, v0 + e);
-    }
+    which |= (lim == 0 || l > w || (l == w && j <= g_last)) && v0 + e >= 0 && v0 + e < r.V ? 1u << e : 0u;
   }
+  if (!which) return;
+  int spot = atomicAdd(n_spots, __popc(which));
+#pragma unroll
+  for (int e = 0; e < LpGroup<T>::kEntries; ++e)
+    if (which >> e & 1u) {
+      if (spot < kLpSpots) spots[spot] = lp_key(g.entry(e), v0 + e);
+      ++spot;
+    }
 }
 
 // Writes what a row without a token gets (see the header), or one whose accept length cannot be.
@@ -422,13 +428,20 @@ __device__ __forceinline__ void lp_no_token(const LpParams& p, int row, bool val
   }
 }
 
+// CTAs per SM, by registers.
+template <typename T>
+constexpr int lp_per_sm(bool sums) { return sums && sizeof(T) == 2 ? 3 : 4; }
+
 // What bounds it: HBM for large batches; for a few rows the chain token -> its logit -> pass -> board -> second look -> counting.
 template <typename T, bool kSums, bool kTop, int kRank>
-__global__ void __launch_bounds__(kLpThreads, kSums && sizeof(T) == 2 ? 3 : 4) token_logprobs_kernel(const LpParams p, int C) {
+__global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprobs_kernel(const LpParams p, int C) {
   constexpr int E = LpGroup<T>::kEntries;
   __shared__ uint64_t spots[kTop ? kLpMaxCluster : 1][kLpSpots];       // first CTA: what every part sends
   __shared__ LpPart parts[kLpMaxCluster];
   __shared__ uint64_t own_spots[kTop ? kLpSpots : 1];
+  __shared__ uint64_t side[kTop ? kLpMaxCluster * kLpSpots : 1];       // first CTA: all of it, and each entry's place
+  __shared__ int before_it[kTop ? kLpMaxCluster * kLpSpots : 1];
+  __shared__ float row_m, row_ls;
   __shared__ uint64_t lists[kTop ? kLpWarps * 32 : 1];   // board, or the warps' sorted lists
   __shared__ uint64_t fresh[kTop ? kLpWarps : 1][32];
   __shared__ uint8_t looked_at[kLpWarps][32];
@@ -439,7 +452,6 @@ __global__ void __launch_bounds__(kLpThreads, kSums && sizeof(T) == 2 ? 3 : 4) t
   // the other CTAs of the cluster have started (looked at before anything is sent to them)
   if (C > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   if (tid == 0) n_spots = 0;
-  if (kTop && tid < kLpSpots) own_spots[tid] = 0;
   grid_dependency_wait();
   grid_dependency_release();
 
@@ -530,7 +542,7 @@ __global__ void __launch_bounds__(kLpThreads, kSums && sizeof(T) == 2 ? 3 : 4) t
     // every warp for itself: the n-th best on the board (its keys differ, but for empty ones)
     const uint64_t key = lists[lane];
     int before = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < 32; ++i) before += lists[i] > key ? 1 : 0;
     const unsigned nth = __ballot_sync(0xffffffffu, key != 0 && before == p.n_top - 1);
     uint64_t lim = nth ? __shfl_sync(0xffffffffu, key, __ffs(nth) - 1) : 0;     // (0: fewer hold anything)
@@ -633,45 +645,77 @@ __global__ void __launch_bounds__(kLpThreads, kSums && sizeof(T) == 2 ? 3 : 4) t
   } else if (kTop && warp <= 2) {
     uint64_t* to = C > 1 ? cg::this_cluster().map_shared_rank(&spots[part][0], 0) : &spots[part][0];
     const int i = (warp - 1) * 32 + lane;
-    if (i < ((n_spots + 7) & ~7)) to[i] = own_spots[i];  // (whole eights, for the counting)
+    if (i < n_spots) to[i] = own_spots[i];
   }
   if (C > 1) cluster_sync_all();
   else __syncthreads();
-  if (part != 0) return;
+  if (part != 0 || (!kTop && warp != 0)) return;
 
-  // The row: its sums, by every warp that needs them.
-  if (warp > 0 && !kTop) return;
-  LpPart all = {-CUDART_INF_F, 0.f, 0.f, 0u, {0, 0, 0, 0}, 0};
-  if (lane < C) all = parts[lane];
-  float m = warp_max_f32(all.m), ls, logZ, H = 0.f;
-  const bool bad = __any_sync(0xffffffffu, all.bad != 0);
-  if (kSums) {
-    const float d = all.m == -CUDART_INF_F ? 0.f : lp_below(all.m, m), e = ex2_approx(d * kLog2e);
-    float s = e * all.s, t = e * fmaf(d, all.s, all.t);
+  // What the parts sent, side by side: warp c copies part c's.
+  int total = 0;
+  if (kTop) {
+    const int sent = lane < C ? parts[lane].spots : 0;
+    int upto = sent;
 #pragma unroll
-    for (int o = kLpMaxCluster / 2; o > 0; o >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, o);
-      t += __shfl_xor_sync(0xffffffffu, t, o);
+    for (int o = 1; o < kLpMaxCluster; o <<= 1) {
+      const int below = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += below;
     }
-    if (bad) {
-      m = ls = logZ = H = CUDART_NAN_F;
-    } else if (m == -CUDART_INF_F) {
-      ls = logZ = m;                                     // nothing is left of the row
-    } else {
-      ls = logf(s);
-      logZ = m + ls;
-      H = fmaxf(0.f, ls - quotient(t, s));
+    total = __shfl_sync(0xffffffffu, upto, kLpMaxCluster - 1);
+    const int mine = __shfl_sync(0xffffffffu, sent, warp), first = __shfl_sync(0xffffffffu, upto, warp) - mine;
+#pragma unroll 1
+    for (int i = lane; i < mine; i += 32) {
+      side[first + i] = spots[warp][i];
+      before_it[first + i] = 0;
     }
-    // (lanes beyond the parts hold other sums' halves)
-    m = __shfl_sync(0xffffffffu, m, 0); ls = __shfl_sync(0xffffffffu, ls, 0);
-  } else {
-    m = 0.f;
-    ls = logZ = p.logZ_in[row];
+    __syncthreads();
+    // Every entry's place is the number of those before it: a warp compares all of them with an eighth of them.
+    const int slice = (total + kLpWarps - 1) / kLpWarps, from = warp * slice, to = min(total, from + slice);
+    if (from < to) {
+#pragma unroll 1
+      for (int i = lane; i < total; i += 32) {
+        const uint64_t key = side[i];
+        int n_before = 0;
+#pragma unroll 4
+        for (int k = from; k < to; ++k) n_before += side[k] > key ? 1 : 0;
+        atomicAdd(&before_it[i], n_before);
+      }
+    }
   }
+
+  // The row, by warp 0.
   if (warp == 0) {
+    LpPart all = {-CUDART_INF_F, 0.f, 0.f, 0u, {0, 0, 0, 0}, 0};
+    if (lane < C) all = parts[lane];
+    const bool bad = __any_sync(0xffffffffu, all.bad != 0);
+    float m = 0.f, ls, logZ, H = 0.f;
+    if (kSums) {
+      m = warp_max_f32(all.m);
+      const float d = all.m == -CUDART_INF_F ? 0.f : lp_below(all.m, m), e = ex2_approx(d * kLog2e);
+      float s = e * all.s, t = e * fmaf(d, all.s, all.t);
+#pragma unroll
+      for (int o = kLpMaxCluster / 2; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        t += __shfl_xor_sync(0xffffffffu, t, o);
+      }
+      if (bad) {
+        m = ls = logZ = H = CUDART_NAN_F;
+      } else if (m == -CUDART_INF_F) {
+        ls = logZ = m;                                   // nothing is left of the row
+      } else {
+        ls = logf(s);
+        logZ = m + ls;
+        H = fmaxf(0.f, ls - quotient(t, s));
+      }
+      ls = __shfl_sync(0xffffffffu, ls, 0);              // (lanes beyond the parts hold other sums)
+    } else {
+      ls = logZ = p.logZ_in[row];
+    }
     if (lane == 0) {
       if (kSums && p.entropy) p.entropy[row] = H;
       if (kSums && p.logZ) p.logZ[row] = logZ;
+      row_m = bad ? CUDART_NAN_F : m;
+      row_ls = ls;
     }
     unsigned flags = bad ? HOLA_FLAG_BAD_LOGIT : 0u;
     // (no token: 0; one that the vocabulary does not have: NaN)
@@ -707,33 +751,20 @@ __global__ void __launch_bounds__(kLpThreads, kSums && sizeof(T) == 2 ? 3 : 4) t
     }
   }
   if (kTop) {
+    __syncthreads();
     const size_t at = static_cast<size_t>(row) * p.n_top;
-    if (bad) {
+    const float m = row_m, ls = row_ls;
+    if (m != m) {
       if (tid < p.n_top) { p.top_ids[at + tid] = -1; p.top_logprobs[at + tid] = CUDART_NAN_F; }
       return;
     }
-    // Every entry that was sent finds its place by counting those before it: thread i takes entry i, i + 256, ...
-    for (int i0 = warp * 32; ; i0 += kLpThreads) {
-      int i = i0 + lane, from = -1, total = 0;
-      for (int c = 0; c < C; ++c) {
-        const int sent = __shfl_sync(0xffffffffu, all.spots, c);
-        if (from < 0 && i < sent) from = c;
-        if (from < 0) i -= sent;
-        total += sent;
-      }
-      if (i0 >= total) break;
-      const uint64_t key = from >= 0 ? spots[from][i] : 0;
-      int before = 0;
-      for (int c = 0; c < C; ++c) {
-        const int sent = __shfl_sync(0xffffffffu, all.spots, c);
 #pragma unroll 1
-        for (int k = 0; k < sent; k += 8)                // (whole eights were sent)
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk) before += spots[c][k + kk] > key ? 1 : 0;
-      }
-      if (before < p.n_top && key != 0) {
-        p.top_ids[at + before] = static_cast<int>(~static_cast<uint32_t>(key));
-        p.top_logprobs[at + before] = lp_logprob(lp_value(static_cast<uint32_t>(key >> 32)), m, ls);
+    for (int i = tid; i < total; i += kLpThreads) {
+      const int place = before_it[i];
+      const uint64_t key = side[i];
+      if (place < p.n_top) {
+        p.top_ids[at + place] = static_cast<int>(~static_cast<uint32_t>(key));
+        p.top_logprobs[at + place] = lp_logprob(lp_value(static_cast<uint32_t>(key >> 32)), m, ls);
       }
     }
   }
@@ -764,10 +795,11 @@ __global__ void __launch_bounds__(128) gather_logprobs_kernel(const LpParams p) 
   if (!have && !none && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
 }
 
-// CTAs per row: enough for four on every SM, as long as a thread keeps a group or two of its own.
-int lp_cluster(int num_sms, int rows, int V) {
+// CTAs per row: as many as fit on the chip at once, as long as a thread keeps a group or two of its own.  (A second wave for a few of
+// them costs as much as the first: start, merges and the second look are latency, which nothing hides in so short a kernel.)
+int lp_cluster(int num_sms, int rows, int V, int per_sm) {
   int C = 1;
-  while (C < kLpMaxCluster && static_cast<long long>(rows) * C < 4ll * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;
+  while (C < kLpMaxCluster && 2ll * rows * C <= static_cast<long long>(per_sm) * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;
   return C;
 }
 
@@ -805,7 +837,7 @@ cudaError_t run_logprobs(LpParams p, int num_sms, cudaStream_t stream) {
     cfg.attrs = attr; cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, gather_logprobs_kernel<T>, p);
   }
-  const int C = lp_cluster(num_sms, p.rows, p.V);
+  const int C = lp_cluster(num_sms, p.rows, p.V, lp_per_sm<T>(sums));
   // More tokens than a pass has counters for: their ranks take a pass each four.
   cudaError_t e = cudaSuccess;
   for (p.t0 = 0; e == cudaSuccess && (p.t0 == 0 || (rank && p.t0 < p.T)); p.t0 += kLpTok) {

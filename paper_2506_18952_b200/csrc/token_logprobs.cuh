@@ -10,14 +10,12 @@
 // met it in.  Every eight threads put the best of their (maximum, group) pairs, in the order (value descending, group ascending),
 // on a board of 32; let the n-th best there be (w, g).  At least n entries lie at or before it (those maxima), so every one of the
 // part's n best has a value above w, or w itself in a group up to g.  Only threads whose own pair is at or before (w, g) can hold
-// such entries.  A thread holds on to the group of its maximum; where its second-best group may qualify too, its groups are read
-// again, out of the L2.  What qualifies (n entries and some more) goes to the row's first CTA, which places each entry by counting
-// those before it.
+// such entries.  The group of their maximum is read again, out of the L2, and their other groups where the second-best may qualify
+// too.  What qualifies (n entries and some more) goes to the row's first CTA, which places each entry by counting those before it.
 
 constexpr int kLpThreads = 256;
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpGroupBytes = 32;      // neighbouring entries that a thread loads at once
-constexpr int kLpDepth = 2;            // groups that it has on the way
 constexpr int kLpSpots = 64;           // entries that a part may send unsorted; beyond that it sends its 32 best
 constexpr float kLpSlack = 4.f;        // how far a maximum may rise above the point that the sums are taken about
 constexpr int kLpMaxTop = 32;          // alternatives: a sorted list lies across a warp, one entry per lane
@@ -187,6 +185,15 @@ struct LpRow {
   }
   __device__ __forceinline__ bool whole(int j) const { return j >= whole_begin && j < whole_end; }
   __device__ __forceinline__ int first(int j) const { return j * E - off; }
+  static __device__ __forceinline__ uint32_t none_bits() {        // -inf
+    return sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __nv_bfloat16>::value ? 0xff80u : 0xfc00u;
+  }
+  static __device__ __forceinline__ LpGroup<T> none() {
+    LpGroup<T> g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g.w[i] = sizeof(T) == 4 ? none_bits() : none_bits() * 0x10001u;
+    return g;
+  }
   __device__ __forceinline__ LpGroup<T> get(int j) const {
     if (!whole(j)) return get_ragged(j);
     LpGroup<T> g;
@@ -196,7 +203,7 @@ struct LpRow {
   __device__ __noinline__ LpGroup<T> get_ragged(int j) const {
     LpGroup<T> g;
     {
-      const uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __nv_bfloat16>::value ? 0xff80u : 0xfc00u;
+      const uint32_t none = none_bits();
 #pragma unroll
       for (int i = 0; i < 8; ++i) g.w[i] = 0;
 #pragma unroll
@@ -288,59 +295,61 @@ struct LpThread {
   float m, second;             // maximum, and that of the other groups
   float ref, rise, shift;      // rise: where the next rescaling is due; shift = -ref log2 e
   uint64_t s2, t2;             // two halves of either sum
-  int at;                      // group that the maximum was first met in
-  LpGroup<T> held;             // (alternatives) its entries
+  int at;                      // group that holds the maximum, the first one that does
   bool bad;
   int count[kRank ? kRank : 1];
 
   __device__ __forceinline__ explicit LpThread(int first) : shift(0.f), s2(0), t2(0), at(first), bad(false) {
     m = second = ref = rise = -CUDART_INF_F;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) held.w[i] = 0;
-#pragma unroll
     for (int q = 0; q < (kRank ? kRank : 1); ++q) count[q] = 0;
   }
 
-  // Group j, whose first entry is v0; `ragged`: it lacks some.
+  // Group j, by all lanes of a warp together (a lane without one brings a group of -inf); v0: its first entry.  kPlain: it is whole
+  // and comes behind those before it.
+  template <bool kPlain>
   __device__ __forceinline__ void take(const LpGroup<T>& g, int j, int v0, const LpToken<T>* tok, float l_min, bool ragged) {
     const float top = g.largest();
-    if (!kSums && !(top < CUDART_INF_F)) bad = true;
-    if (kRank && top >= l_min) {
+    if (!kSums) bad = bad || !(top < CUDART_INF_F);
+    if (kTop) {
+      second = fmaxf(second, fminf(top, m));
+      if (top > m || (!kPlain && top == m && j < at)) at = j;
+    }
+    m = fmaxf(m, top);
+    // seldom: the maximum rises, or there are entries before a token
+    if (__any_sync(0xffffffffu, (kSums && top > rise) || (kRank && top >= l_min))) {
+      if (kRank && top >= l_min) {
 #pragma unroll
-      for (int q = 0; q < kRank; ++q) {
-        if (!(top >= tok[q].l)) continue;
-        if (ragged || (v0 <= tok[q].x && v0 + E > tok[q].x)) {
-          for (int i = 0; i < E; ++i) {
-            const float l = g.entry(i);
-            count[q] += v0 + i >= 0 && (l > tok[q].l || (l == tok[q].l && v0 + i < tok[q].x)) ? 1 : 0;
+        for (int q = 0; q < kRank; ++q) {
+          if (!(top >= tok[q].l)) continue;
+          if (ragged || (v0 <= tok[q].x && v0 + E > tok[q].x)) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+              const float l = g.entry(i);
+              count[q] += v0 + i >= 0 && (l > tok[q].l || (l == tok[q].l && v0 + i < tok[q].x)) ? 1 : 0;
+            }
+          } else {
+            count[q] += lp_count(g, v0 < tok[q].x ? tok[q].limit[1] : tok[q].limit[0]);
           }
-        } else {
-          count[q] += lp_count(g, v0 < tok[q].x ? tok[q].limit[1] : tok[q].limit[0]);
         }
       }
-    }
-    if (kTop) second = fmaxf(second, fminf(top, m));
-    if (top > m || (kTop && at == j)) {                  // (its first group is held whatever it is)
-      m = top;
-      at = j;
-      if (kTop) held = g;
-    }
-    if (!kSums || top == -CUDART_INF_F) return;
-    if (top > rise) {
-      const float old = shift;
-      shift = fabsf(top) < 1e37f ? -top * kLog2e : CUDART_NAN_F;      // (NaN: every group goes the long way below)
-      if (ref != -CUDART_INF_F) {
-        float dx = shift - old;
-        if (!(dx == dx)) dx = (ref - top) * kLog2e;
-        dx = fmaxf(dx, -1e28f);
-        const float e = ex2_approx(dx);
-        const uint64_t e2 = pack2(e, e);
-        t2 = mul2(fma2(pack2(dx, dx), s2, t2), e2);
-        s2 = mul2(s2, e2);
+      if (kSums && top > rise) {
+        const float old = shift;
+        shift = fabsf(top) < 1e37f ? -top * kLog2e : CUDART_NAN_F;    // (NaN: every group goes the long way below)
+        if (ref != -CUDART_INF_F) {
+          float dx = shift - old;
+          if (!(dx == dx)) dx = (ref - top) * kLog2e;
+          dx = fmaxf(dx, -1e28f);
+          const float e = ex2_approx(dx);
+          const uint64_t e2 = pack2(e, e);
+          t2 = mul2(fma2(pack2(dx, dx), s2, t2), e2);
+          s2 = mul2(s2, e2);
+        }
+        ref = top;
+        rise = top + kLpSlack;
       }
-      ref = top;
-      rise = top + kLpSlack;
     }
+    if (!kSums) return;
     const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
     uint64_t ps[2] = {0, 0}, pt[2] = {0, 0};
 #pragma unroll
@@ -350,28 +359,35 @@ struct LpThread {
       const uint64_t x = fma2(pack2(a, b), l2e, sh);
       unpack2(x, a, b);
       const uint64_t e = pack2(ex2_approx(a), ex2_approx(b));
-      ps[i & 1] = add2(ps[i & 1], e);
-      pt[i & 1] = fma2(e, x, pt[i & 1]);
+      ps[i & 1] = i < 2 ? e : add2(ps[i & 1], e);
+      pt[i & 1] = i < 2 ? mul2(e, x) : fma2(e, x, pt[i & 1]);
     }
     const uint64_t both = add2(pt[0], pt[1]);
     float a, b;
     unpack2(both, a, b);
-    if (a + b == a + b) {
+    const bool fine = a + b == a + b;
+    if (__all_sync(0xffffffffu, fine)) {
       s2 = add2(s2, add2(ps[0], ps[1]));
       t2 = add2(t2, both);
       return;
     }
-    // 0 * -inf: entries that are masked (-inf, or as low as the type goes), or too large for x; or there is no distribution
-    if (!(top < CUDART_INF_F)) { bad = true; return; }
-    float s = 0.f, t = 0.f;
+    if (fine) {
+      s2 = add2(s2, add2(ps[0], ps[1]));
+      t2 = add2(t2, both);
+    } else if (!(top < CUDART_INF_F)) {                  // there is no distribution
+      bad = true;
+    } else if (top != -CUDART_INF_F) {
+      // 0 * -inf: entries that are masked (-inf, or as low as the type goes), or too large for x
+      float s = 0.f, t = 0.f;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float x = lp_below(g.entry(i), ref) * kLog2e, e = ex2_approx(x);
-      s += e;
-      t = fmaf(e, x, t);
+      for (int i = 0; i < E; ++i) {
+        const float x = lp_below(g.entry(i), ref) * kLog2e, e = ex2_approx(x);
+        s += e;
+        t = fmaf(e, x, t);
+      }
+      s2 = add2(s2, pack2(s, 0.f));
+      t2 = add2(t2, pack2(t, 0.f));
     }
-    s2 = add2(s2, pack2(s, 0.f));
-    t2 = add2(t2, pack2(t, 0.f));
   }
 
   // The sums about the thread's own maximum: m, sum e^(l-m), sum e^(l-m)(l-m).
@@ -428,13 +444,14 @@ __device__ __forceinline__ void lp_no_token(const LpParams& p, int row, bool val
   }
 }
 
-// CTAs per SM, by registers.
+// CTAs per SM, by registers: what 16-bit logits are expanded to and the alternatives' bookkeeping do not fit 64 together (us at
+// 80 / at 64: 192 x 32000 bf16, 8 alternatives 22.3 / 24.6; 2304 x 128256 bf16, none 137.7 / 117.2).
 template <typename T>
-constexpr int lp_per_sm(bool sums) { return sums && sizeof(T) == 2 ? 3 : 4; }
+constexpr int lp_per_sm(bool sums, bool top) { return sums && top && sizeof(T) == 2 ? 3 : 4; }
 
 // What bounds it: HBM for large batches; for a few rows the chain token -> its logit -> pass -> board -> second look -> counting.
 template <typename T, bool kSums, bool kTop, int kRank>
-__global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprobs_kernel(const LpParams p, int C) {
+__global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_logprobs_kernel(const LpParams p, int C) {
   constexpr int E = LpGroup<T>::kEntries;
   __shared__ uint64_t spots[kTop ? kLpMaxCluster : 1][kLpSpots];       // first CTA: what every part sends
   __shared__ LpPart parts[kLpMaxCluster];
@@ -474,12 +491,12 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprob
     }
   }
 
-  // The first groups are on their way while the tokens and their logits are looked up.
-  LpGroup<T> next[kLpDepth];
-  int j = j_begin + tid;
-#pragma unroll
-  for (int u = 0; u < kLpDepth; ++u)
-    if (r.whole(j + u * kLpThreads) && j + u * kLpThreads < j_end) next[u].load(r.base + static_cast<size_t>(j + u * kLpThreads) * E);
+  // Rounds in which every thread has a whole group, and one for what is left; the row's first group, where it lacks entries, has one
+  // of its own.  The first group is on its way while the tokens and their logits are looked up.
+  const int j_first = max(j_begin, min(r.whole_begin, j_end)), rounds = max(0, min(j_end, r.whole_end) - j_first) / kLpThreads;
+  LpGroup<T> next;
+  const T* ptr = r.base + static_cast<size_t>(j_first + tid) * E;
+  if (rounds > 0) next.load(ptr);
 
   LpToken<T> tok[kRank ? kRank : 1];
   float l_min = CUDART_INF_F;
@@ -495,17 +512,25 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprob
     if (have) l_min = fminf(l_min, tok[q].l);
   }
 
+  int j = j_first + tid;
   LpThread<T, kSums, kTop, kRank> th(j);
 #pragma unroll 1
-  for (; j < j_end; j += kLpThreads) {
-    LpGroup<T> g = next[0];
-#pragma unroll
-    for (int u = 0; u + 1 < kLpDepth; ++u) next[u] = next[u + 1];
-    const int ahead = j + kLpDepth * kLpThreads;
-    if (ahead < j_end && r.whole(ahead)) next[kLpDepth - 1].load(r.base + static_cast<size_t>(ahead) * E);
-    const bool ragged = !r.whole(j);
-    if (ragged) g = r.get_ragged(j);
-    th.take(g, j, r.first(j), tok, l_min, ragged);
+  for (int i = 0; i < rounds; ++i, j += kLpThreads) {
+    const LpGroup<T> g = next;
+    ptr += kLpThreads * E;
+    if (i + 1 < rounds) next.load(ptr);
+    th.template take<true>(g, j, r.first(j), tok, l_min, false);
+  }
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {
+    if (i == 1) {
+      if (j_begin == j_first || warp != 0) break;
+      j = lane == 0 ? 0 : j_end;
+    }
+    const bool some = j < j_end, ragged = !some || !r.whole(j);
+    LpGroup<T> g = r.none();
+    if (some) g = r.get(j);
+    th.template take<false>(g, j, some ? r.first(j) : INT32_MAX - E, tok, l_min, ragged);
   }
 
   // The threads' sums and counts, over the warp.
@@ -530,7 +555,7 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprob
   if (lane == 0) warp_parts[warp] = mine;
 
   if (kTop) {
-    const uint64_t own = th.at < j_end ? lp_key(th.m, th.at) : 0;
+    const uint64_t own = th.at < j_end ? lp_key(th.m, th.at) : 0;       // (a thread without a group: nothing)
     uint64_t a = own;
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) {
@@ -549,17 +574,22 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprob
     float w = lp_value(static_cast<uint32_t>(lim >> 32));
     int g_last = static_cast<int>(~static_cast<uint32_t>(lim));
     const bool mine_too = own != 0 && own >= lim;
-    const bool again = mine_too && th.at + kLpThreads * (th.at == j_begin + tid) < j_end && (lim == 0 || th.second >= w);
-    if (mine_too && !again) lp_send(th.held, r, th.at, lim, w, g_last, own_spots, &n_spots);
+    const bool again = mine_too && (lim == 0 || th.second >= w);
+    if (mine_too && !again) lp_send(r.get(th.at), r, th.at, lim, w, g_last, own_spots, &n_spots);
+    // The groups of a thread, the row's first one last; dealt out to the lanes.
+    const int steps = (j_end - j_first + kLpThreads - 1) / kLpThreads + (j_begin < j_first ? 1 : 0);
+    auto group_of = [&](int i) {
+      const int who = i / steps, k = i - who * steps, t = warp * 32 + looked_at[warp][who];
+      const int jj = j_first + t + k * kLpThreads;
+      return k == steps - 1 && j_begin < j_first ? (t == 0 ? 0 : j_end) : jj;
+    };
     const unsigned look = __ballot_sync(0xffffffffu, again);
     if (look) {
-      // The groups of those threads, dealt out to the lanes.
       if (again) looked_at[warp][__popc(look & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
       __syncwarp();
-      const int steps = (j_end - j_begin + kLpThreads - 1) / kLpThreads;       // groups per thread at most
       const int total = __popc(look) * steps;
       for (int i = lane; i < total; i += 32) {
-        const int who = i / steps, jj = j_begin + warp * 32 + looked_at[warp][who] + (i - who * steps) * kLpThreads;
+        const int jj = group_of(i);
         if (jj < j_end) lp_send(r.get(jj), r, jj, lim, w, g_last, own_spots, &n_spots);
       }
     }
@@ -578,7 +608,7 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprob
       const unsigned all = __ballot_sync(0xffffffffu, holds);
       if (holds) looked_at[warp][__popc(all & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
       __syncwarp();
-      const int steps = (j_end - j_begin + kLpThreads - 1) / kLpThreads, total = __popc(all) * steps;
+      const int total = __popc(all) * steps;
       uint64_t best = 0;
       int waiting = 0;
 #pragma unroll 1
@@ -586,8 +616,7 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums)) token_logprob
         const int i = i0 + lane;
         int jj = -1;
         if (i < total) {
-          const int who = i / steps;
-          jj = j_begin + warp * 32 + looked_at[warp][who] + (i - who * steps) * kLpThreads;
+          jj = group_of(i);
           if (jj >= j_end) jj = -1;
         }
         LpGroup<T> g = {};
@@ -795,11 +824,13 @@ __global__ void __launch_bounds__(128) gather_logprobs_kernel(const LpParams p) 
   if (!have && !none && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
 }
 
-// CTAs per row: as many as fit on the chip at once, as long as a thread keeps a group or two of its own.  (A second wave for a few of
-// them costs as much as the first: start, merges and the second look are latency, which nothing hides in so short a kernel.)
-int lp_cluster(int num_sms, int rows, int V, int per_sm) {
+// CTAs per row: up to three on an SM, as long as a thread keeps a group or two of its own.  Start, merges and the second look are
+// latency, some 4 us a CTA, which more CTAs only add to, and a second wave for a few of them costs as much as the first.  us with 1 /
+// 2 / 4 / 8: 69 x 50003 fp16 19.2 / 15.6 / 15.4 / 22.9; 192 x 32000 bf16 30.5 / 22.3 / 30.9 / 48.4; 384 x 128256 fp32 52.0 / 58.7 /
+// 58.9 / 86.8; 5 x 32000 fp32 9.8 / 7.8 / 6.4 / 6.6.
+int lp_cluster(int num_sms, int rows, int V) {
   int C = 1;
-  while (C < kLpMaxCluster && 2ll * rows * C <= static_cast<long long>(per_sm) * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;
+  while (C < kLpMaxCluster && 2ll * rows * C <= 3ll * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;
   return C;
 }
 
@@ -837,7 +868,7 @@ cudaError_t run_logprobs(LpParams p, int num_sms, cudaStream_t stream) {
     cfg.attrs = attr; cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, gather_logprobs_kernel<T>, p);
   }
-  const int C = lp_cluster(num_sms, p.rows, p.V, lp_per_sm<T>(sums));
+  const int C = lp_cluster(num_sms, p.rows, p.V);
   // More tokens than a pass has counters for: their ranks take a pass each four.
   cudaError_t e = cudaSuccess;
   for (p.t0 = 0; e == cudaSuccess && (p.t0 == 0 || (rank && p.t0 < p.T)); p.t0 += kLpTok) {

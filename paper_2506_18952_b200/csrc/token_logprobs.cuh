@@ -573,8 +573,29 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
     uint64_t lim = nth ? __shfl_sync(0xffffffffu, key, __ffs(nth) - 1) : 0;     // (0: fewer hold anything)
     float w = lp_value(static_cast<uint32_t>(lim >> 32));
     int g_last = static_cast<int>(~static_cast<uint32_t>(lim));
-    const bool mine_too = own != 0 && own >= lim;
-    const bool again = mine_too && (lim == 0 || th.second >= w);
+    // Masked rows: fewer entries than alternatives are left, the others are -inf by rising id.  The part's first ones serve, where 64
+    // entries hold enough of them (otherwise: as where there is no room).
+    const bool masked = lim != 0 && w == -CUDART_INF_F;
+    if (masked) {
+      g_last = -1;                                       // (entries above w only)
+      if (warp == 0) {
+        const int v_begin = max(0, r.first(j_begin)), v_end = min(p.V, r.first(j_end));
+        const int v = v_begin + 2 * lane;
+        const bool a = v < v_end && lp_float(r.base[static_cast<size_t>(v) + r.off]) == w,
+                   b = v + 1 < v_end && lp_float(r.base[static_cast<size_t>(v) + 1 + r.off]) == w;
+        const unsigned as = __ballot_sync(0xffffffffu, a), bs = __ballot_sync(0xffffffffu, b), below = (1u << lane) - 1u;
+        const int found = __popc(as) + __popc(bs), place = __popc(as & below) + __popc(bs & below);
+        const bool enough = found >= p.n_top || v_end - v_begin <= 64;
+        int first = 0;
+        if (lane == 0) first = atomicAdd(&n_spots, enough ? min(found, p.n_top) : kLpSpots + 1);
+        first = __shfl_sync(0xffffffffu, first, 0);
+        if (enough && a && place < p.n_top && first + place < kLpSpots) own_spots[first + place] = lp_key(w, v);
+        if (enough && b && place + (a ? 1 : 0) < p.n_top && first + place + (a ? 1 : 0) < kLpSpots)
+          own_spots[first + place + (a ? 1 : 0)] = lp_key(w, v + 1);
+      }
+    }
+    const bool mine_too = masked ? th.m > w : own != 0 && own >= lim;
+    const bool again = mine_too && (lim == 0 || (masked ? th.second > w : th.second >= w));
     if (mine_too && !again) lp_send(r.get(th.at), r, th.at, lim, w, g_last, own_spots, &n_spots);
     // The groups of a thread, the row's first one last; dealt out to the lanes.
     const int steps = (j_end - j_first + kLpThreads - 1) / kLpThreads + (j_begin < j_first ? 1 : 0);

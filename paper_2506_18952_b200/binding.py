@@ -331,9 +331,14 @@ class AdapterBank:
             raise HolaError("AdapterBank takes A [slots, rank, H] and B [slots, V, rank]")
         if scale is not None and tuple(scale.shape) != (A.shape[0],):
             raise HolaError("AdapterBank: scale must have one value per slot")
+        if A.dtype != torch.bfloat16 or B.dtype != torch.bfloat16 or A.device != B.device:
+            raise HolaError("AdapterBank takes bfloat16 factors on one device")
+        rank = A.shape[1]
         self._make(*A.shape, B.shape[1], A.device)
-        for s in range(self.slots):
-            self.set(s, A[s], B[s], None if scale is None else scale[s])
+        self.A[:, :rank] = A
+        self.B[:, :, :rank] = B
+        if scale is not None:
+            self.scale.copy_(scale)
 
     @classmethod
     def empty(cls, slots: int, rank: int, H: int, V: int, device=None) -> "AdapterBank":

@@ -10,6 +10,10 @@ The two models are seeded synthetic stand-ins (the paper's trained draft / verif
 read the context through embedding tables and share the LM head; the verifier sees two tokens back, the draft only
 one, so q is close to p but not equal.  They are harness code in stock torch; every step of the verify path itself
 runs in the CUDA library.  Everything stays on the device: no host read-back inside the loop.
+
+Two options of the serving path: `score` has the emitted tokens' log probabilities under the verifier (hola_token_logprobs, on the
+logits and logZ that the verify call leaves), and a bank of low-rank adapters gives every sequence its own LM head
+(hola_verify_adapters).
 """
 from __future__ import annotations
 
@@ -51,6 +55,17 @@ class SyntheticPair:
         return torch.softmax(h @ self.W_lm.float().T, dim=-1)
 
 
+def seeded_adapters(models: SyntheticPair, slots: int, rank: int, seed: int, strength: float = 0.25) -> binding.AdapterBank:
+    """Low-rank adapters for the pair's LM head, each an update of `strength` times the head's own logits on average."""
+    g = torch.Generator(device=models.device)
+    g.manual_seed(seed)
+    std = float(models.W_lm[:256].float().std())
+    A = (torch.randn((slots, rank, models.H), generator=g, device=models.device) / models.H ** 0.5).to(torch.bfloat16)
+    Bm = (torch.randn((slots, models.V, rank), generator=g, device=models.device)
+          * (strength * std * (models.H / rank) ** 0.5)).to(torch.bfloat16)
+    return binding.AdapterBank(A, Bm)
+
+
 @dataclass
 class RoundRecord:
     """What one round handed to hola_verify and got back (device tensors)."""
@@ -69,12 +84,15 @@ class DecodeResult:
     verify_ms: float            # CUDA-event time of all hola_verify calls
     total_ms: float             # CUDA-event time of the whole loop (draft + trunk stand-ins included)
     accepted: torch.Tensor      # int64 [B]: draft tokens kept, summed over the rounds
+    logprob: torch.Tensor | None = None   # fp64 [B]: log probability of a sequence's emitted tokens under the verifier (score)
     records: list = field(default_factory=list)
 
 
 def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Tensor, k: int, tau: float, rounds: int,
-               seed: int, gate_source: int = 0, fallback: int = 0, keep_records: bool = False) -> DecodeResult:
-    """Runs `rounds` draft-and-verify rounds for a batch of sequences.  prompt: int64 [B, 2] (two context tokens)."""
+               seed: int, gate_source: int = 0, fallback: int = 0, keep_records: bool = False, score: bool = False,
+               adapters: binding.AdapterBank | None = None, adapter_ids: torch.Tensor | None = None) -> DecodeResult:
+    """Runs `rounds` draft-and-verify rounds for a batch of sequences.  prompt: int64 [B, 2] (two context tokens).  score: the
+    emitted tokens' log probabilities are summed up.  adapters, adapter_ids: the sequences' LM-head adapters."""
     dev = prompt.device
     B = prompt.shape[0]
     g = torch.Generator(device=dev)
@@ -86,7 +104,9 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
     accepted = torch.zeros((B,), dtype=torch.int64, device=dev)
     rows = torch.arange(B, device=dev)
     steps = torch.arange(k + 1, device=dev)
-    out = ctx.alloc_outputs(B, k, False)
+    out = ctx.alloc_outputs(B, k, score)
+    options = dict(out=out, gate_source=gate_source, fallback=fallback)
+    logprob = torch.zeros((B,), dtype=torch.float64, device=dev) if score else None
     records = []
     ev = [torch.cuda.Event(enable_timing=True) for _ in range(2 * rounds + 2)]
     ev[-2].record()
@@ -109,9 +129,14 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
         uniforms = torch.rand((B, k + 1), generator=g, device=dev, dtype=torch.float32)
         tok32 = draft_tok.to(torch.int32).contiguous()
         ev[2 * r].record()
-        ctx.hola_verify(hidden, models.W_lm, tok32, draft_q, uniforms, tau, out=out, gate_source=gate_source,
-                        fallback=fallback)
+        if adapters is None:
+            ctx.hola_verify(hidden, models.W_lm, tok32, draft_q, uniforms, tau, **options)
+        else:
+            ctx.hola_verify_adapters(hidden, models.W_lm, tok32, draft_q, uniforms, tau, adapters, adapter_ids, **options)
         ev[2 * r + 1].record()
+        if score:
+            scored = binding.hola_token_logprobs(out.logits, logZ=out.logZ, emitted=(tok32, out.accept_len, out.next_tok), want_rank=False)
+            logprob += scored.logprob.double().sum(dim=1)
         # the context grows by the accepted drafts and the verifier's token (no host read-back)
         n = out.accept_len.to(torch.int64)
         new = torch.cat([draft_tok, torch.zeros((B, 1), dtype=torch.int64, device=dev)], dim=1)
@@ -128,7 +153,7 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
     ev[-1].record()
     torch.cuda.synchronize()
     verify_ms = sum(ev[2 * r].elapsed_time(ev[2 * r + 1]) for r in range(rounds))
-    return DecodeResult(tokens, lengths, rounds, verify_ms, ev[-2].elapsed_time(ev[-1]), accepted, records)
+    return DecodeResult(tokens, lengths, rounds, verify_ms, ev[-2].elapsed_time(ev[-1]), accepted, logprob, records)
 
 
 def main():
@@ -142,6 +167,9 @@ def main():
     ap.add_argument("--gate", default="target", choices=["target", "draft"])
     ap.add_argument("--fallback", default="sample", choices=["sample", "greedy"])
     ap.add_argument("--seed", type=int, default=2506189520)
+    ap.add_argument("--score", action="store_true", help="report the emitted tokens' mean log probability under the verifier")
+    ap.add_argument("--adapters", type=int, default=0, help="seeded low-rank adapters beside the LM head, dealt out to the sequences")
+    ap.add_argument("--rank", type=int, default=4, help="rank of the adapters")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         raise SystemExit("driver: no CUDA device; the verify path has no CPU fallback")
@@ -149,10 +177,17 @@ def main():
     models = SyntheticPair(args.V, args.H, args.seed, dev)
     prompt = torch.randint(0, args.V, (args.B, 2), device=dev, generator=torch.Generator(device=dev).manual_seed(args.seed + 1))
     gs, fb = int(args.gate == "draft"), int(args.fallback == "greedy")
+    more = {"score": args.score}
+    if args.adapters > 0:
+        more["adapters"] = seeded_adapters(models, args.adapters, args.rank, args.seed + 2)
+        more["adapter_ids"] = torch.arange(args.B, device=dev, dtype=torch.int32) % args.adapters
     with binding.HolaVerify(args.B, args.k, args.H, args.V) as ctx:
-        hsd_decode(ctx, models, prompt, args.k, args.tau, 3, args.seed, gs, fb)          # warm-up
-        res = hsd_decode(ctx, models, prompt, args.k, args.tau, args.rounds, args.seed, gs, fb)
+        hsd_decode(ctx, models, prompt, args.k, args.tau, 3, args.seed, gs, fb, **more)          # warm-up
+        res = hsd_decode(ctx, models, prompt, args.k, args.tau, args.rounds, args.seed, gs, fb, **more)
     emitted = int((res.lengths - 2).sum().item())
+    extra = {"mean_logprob": float(res.logprob.sum().item()) / emitted} if args.score else {}
+    if args.adapters > 0:
+        extra.update(adapters=args.adapters, rank=args.rank)
     print(json.dumps({
         "workload": f"multi-round HSD decode: B={args.B} k={args.k} H={args.H} V={args.V}, synthetic draft/verifier pair",
         "tau": args.tau, "gate": args.gate, "fallback": args.fallback, "rounds": res.rounds,
@@ -163,7 +198,7 @@ def main():
         "tokens_per_s_verify_only": emitted / (res.verify_ms * 1e-3),
         "loop_ms_per_round": res.total_ms / res.rounds,
         "tokens_per_s_whole_loop": emitted / (res.total_ms * 1e-3),
-        "data": "synthetic"}))
+        "data": "synthetic", **extra}))
 
 
 if __name__ == "__main__":

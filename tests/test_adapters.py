@@ -373,3 +373,30 @@ def test_refused_by_the_binding():
                 ctx.hola_lm_head_adapters(d["hidden"], d["W"], other, d["ids"])
         with pytest.raises(binding.HolaError):
             ctx.hola_verify_adapters(d["hidden"], d["W"], None, None, None, 1.0, bank, d["ids"])
+
+
+@gpu
+def test_decode_loop_with_adapters_and_scores():
+    """The driver's loop on adapted heads: log probabilities as the records' logits have them, tokens as a bare loop's without adapters."""
+    from paper_2506_18952_b200 import driver
+    B, k, H, V, rounds = 6, 3, 256, 2000, 4
+    dev = torch.device("cuda", torch.cuda.current_device())
+    models = driver.SyntheticPair(V, H, 5, dev)
+    prompt = torch.randint(0, V, (B, 2), device=dev, generator=torch.Generator(device=dev).manual_seed(1))
+    bank = driver.seeded_adapters(models, 3, 4, 9)
+    ids = torch.tensor([0, 1, 2, -1, 0, 2], dtype=torch.int32, device=dev)
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        run = lambda **kw: driver.hsd_decode(ctx, models, prompt, k, 1.5, rounds, 3, keep_records=True, **kw)     # noqa: E731
+        bare, none = run(), run(adapters=bank, adapter_ids=torch.full_like(ids, -1), score=True)
+        assert torch.equal(bare.tokens, none.tokens) and bare.logprob is None
+        res = run(adapters=bank, adapter_ids=ids, score=True)
+    want = torch.zeros(B, dtype=torch.float64)
+    for rec in res.records:
+        d = dict(hidden=rec.hidden, ids=ids, A=bank.A, Bup=bank.B, scale=bank.scale)
+        lp = torch.log_softmax(delta64(d)[0] + rec.hidden.double() @ models.W_lm.double().T, dim=-1)
+        for b in range(B):
+            n = int(rec.out.accept_len[b])
+            for j in range(n + 1):
+                want[b] += float(lp[b, j, rec.draft_tok[b, j] if j < n else rec.out.next_tok[b]])
+    assert (res.logprob.cpu() - want).abs().max() <= rounds * (k + 1) * 1e-4
+    assert not torch.equal(res.tokens, bare.tokens)

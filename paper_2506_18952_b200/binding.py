@@ -344,7 +344,10 @@ class AdapterBank:
     def empty(cls, slots: int, rank: int, H: int, V: int, device=None) -> "AdapterBank":
         """Slots of zeros, to be filled by set() with adapters of up to this rank."""
         bank = cls.__new__(cls)
-        bank._make(slots, rank, H, V, torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device))
+        device = torch.device("cuda" if device is None else device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        bank._make(slots, rank, H, V, device)
         return bank
 
     def _make(self, slots, rank, H, V, device):

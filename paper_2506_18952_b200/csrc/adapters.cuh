@@ -183,10 +183,10 @@ struct RowStats {
     s2 = t2 = 0;
     arg = 0x7fffffff;
   }
-  // Eight logits; entry i is vocabulary entry v(i), rising with i.  kSome: those that are -inf are none (the first one is a logit).
-  template <bool kSome, typename Entry>
-  __device__ __forceinline__ void fold(const float* l, int want_arg, Entry v) {
-    const float top = fmaxf(max3(max3(l[0], l[1], l[2]), max3(l[3], l[4], l[5]), l[6]), l[7]);
+  // Eight logits and their largest; entry i is vocabulary entry v(i), rising with i.  First what is seldom (the maximum rises by
+  // more than 4, the arg-max is wanted), then the sums.  kSome: logits that are -inf are none.
+  template <typename Entry>
+  __device__ __forceinline__ void rises(const float* l, float top, int want_arg, Entry v) {
     if (want_arg && top > m) {
       int first = 0;
 #pragma unroll
@@ -194,7 +194,6 @@ struct RowStats {
         if (l[i] == top) first = v(i);
       arg = l[0] == top ? v(0) : first;
     }
-    m = fmaxf(m, top);
     if (top > rise) {
       const float old = shift;
       shift = -top * kLog2e;
@@ -206,6 +205,10 @@ struct RowStats {
       }
       rise = top + 4.f;
     }
+  }
+  template <bool kSome>
+  __device__ __forceinline__ void add(const float* l, float top) {
+    m = fmaxf(m, top);
     const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -231,9 +234,10 @@ struct RowStats {
 };
 
 // A warp step covers 64 vocabulary entries, the M of four MMAs, and the tile's eight rows, their N.  Lane (g, q) holds entries g, 8 + g,
-// 16 + g ... of rows 2 q and 2 q + 1.  Rows of the logits that start on 16-byte boundaries (kVec) come and go by bulk copies through
-// three buffers of the warp's own, two steps ahead; others are loaded and stored by the lanes, eight of which share a sector.  Every
-// lane sums the same entries in the same order either way.
+// 16 + g ... of rows 2 q and 2 q + 1.  Rows of the logits that start on 16-byte boundaries (kVec) are loaded and stored 16 bytes a lane,
+// a step ahead, and change hands in shared memory; others lane by lane, eight of which share a sector.  Every lane sums the same
+// entries in the same order either way.  (Bulk copies in place of the loads and stores, three buffers of 256-byte rows a warp, took
+// as long: a copy keeps its lane some 100 cycles, and memory bounds both.)
 //
 // As in the first product, the order of the ranks is free.  Sixteen at a time, lane q loads four (8 bytes) of a row of B; where whole
 // blocks of 32 ranks are known beforehand (kR: the rank, or 0), eight (16 bytes) for two MMA steps.
@@ -241,49 +245,28 @@ template <int kR>
 __device__ __forceinline__ int adapter_rank(int k, int q) {      // first of the four ranks that lane q holds in step k
   return kR % 32 == 0 && kR > 0 ? 32 * (k >> 1) + 8 * q + 4 * (k & 1) : 16 * k + 4 * q;
 }
-constexpr int kAdStages = 3, kAdPitch = kAdChunk + 4;            // (floats from row to row: no two rows of a step on the same banks)
+constexpr int kAdPitch = kAdChunk + 4;                           // (floats from row to row: no two rows of a step on the same banks)
 
-// A warp's wait on its own copies.  Should it run out it says so, and the copies get as long again before the warp goes on.
-__device__ __forceinline__ bool adapter_wait(uint32_t bar, uint32_t parity, unsigned* status) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  const long long t0 = clock64();
-  bool late = false;
-  while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
-    const long long waited = clock64() - t0;
-    if (__any_sync(0xffffffffu, waited > kWaitLimitCycles) && !late) {
-      late = true;
-      if (status && (threadIdx.x & 31) == 0) atomicOr(status, HOLA_FLAG_TIMEOUT);
-    }
-    if (__any_sync(0xffffffffu, waited > 2 * kWaitLimitCycles)) return false;
-  }
-  return true;
-}
-__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
-}
-
-// What bounds it: for many rows HBM (the logits come and go once more), else the L2 and the chain of a step.
+// What bounds it: memory.  64 adapters of rank 16, 384 rows, V = 128256: 262 MB of B and the logits in and out, 197 MB each, 132 us from
+// the first CTA's start to the last one's end, 5.0 TB/s; 48 tiles of 16 adapters, V = 32000 26 us (18 of them the steps, 87 MB at
+// 4.9 TB/s out of the L2, the rest start and end); 16 adapters of rank 32 for 28 rows, V = 128256 35 us, 4.6 TB/s.  Without the stores
+// 5 us less of 26, without the sums 1, without two of the three planes 1.
+constexpr int kAdUpCtas = 4;                                     // per SM, by registers
 template <bool kVec, int kR>
-__global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) adapter_up_kernel(const AdapterParams p) {
+__global__ void __launch_bounds__(kAdUpWarps * 32, kAdUpCtas) adapter_up_kernel(const AdapterParams p) {
   constexpr int kSteps = (kR + 15) / 16;                 // 0: not known beforehand
   constexpr bool kAhead = kR == 8 || kR == 16;           // a step's ranks are asked for while the step before is worked on
   __shared__ uint2 planes[3][kR ? kSteps : kAdMaxRank / 16][kAdRows][4];         // [plane][16 ranks][row][q]
   __shared__ float4 warp_stats[kAdUpWarps][kAdRows];
-  __shared__ __align__(128) float buffers[kVec ? kAdUpWarps : 1][kVec ? kAdStages : 1][kVec ? kAdRows * kAdPitch : 4];
-  __shared__ __align__(8) uint64_t arrived[kAdUpWarps][kAdStages];
+  __shared__ __align__(16) float buffer[kVec ? kAdUpWarps : 1][kVec ? kAdRows : 1][kAdPitch];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int rank = kR ? kR : p.rank, steps = kR ? kSteps : (rank + 15) >> 4;
-  if (kVec && lane < kAdStages) mbar_init(smem_u32(&arrived[warp][lane]), 1);
-  if (kVec) asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   grid_dependency_wait();
   // The CTAs are dealt out to the tiles that there are: P parts of the vocabulary each, in one go as far as there are enough CTAs.
   const int n_tiles = *p.n_tiles, chunks = (p.V + kAdChunk - 1) / kAdChunk;
   if (n_tiles == 0) return;
   const int P = max(1, min(min(static_cast<int>(gridDim.x) / n_tiles, p.nparts), (chunks + kAdUpWarps - 1) / kAdUpWarps));
   const int per = (chunks + P - 1) / P;
-  int stage = 0;
-  uint32_t parity = 0;
-  bool lost = false;                                     // (a wait of this warp ran out)
   for (int item = blockIdx.x; item < n_tiles * P; item += gridDim.x) {
     const int part = item / n_tiles;
     const AdapterTile& tile = p.tiles[item - part * n_tiles];
@@ -291,21 +274,36 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) 
     if (n == 0) continue;
     const int c_begin = part * per + warp, c_end = min(chunks, (part + 1) * per);
 
-    // Lane r < n moves row r of the tile: 256 bytes a step, the last one of the vocabulary perhaps fewer, in whole 16-byte pieces (a
-    // row's last one lies within its pitch; entries past the vocabulary go back as they came).
-    float* own_row = p.logits + static_cast<size_t>(tile.row[lane < n ? lane : 0]) * p.ldl;
-    auto bytes_of = [&](int c) { return static_cast<uint32_t>((min(kAdChunk, p.V - c * kAdChunk) + 3) & ~3) * 4u; };
-    auto fetch = [&](int c, int stage) {
-      const uint32_t bar = smem_u32(&arrived[warp][stage]), bytes = bytes_of(c);
-      if (lane == 0) mbar_expect_tx(bar, static_cast<uint32_t>(n) * bytes);
-      __syncwarp();
-      if (lane < n) bulk_load(smem_u32(&buffers[warp][stage][lane * kAdPitch]), own_row + c * kAdChunk, bytes, bar);
+    // This lane's two rows of the logits (one that the tile lacks: its first one, read and not written), from entry 4 g or g on, and B from
+    // entry g and its first rank on.
+    const bool have[2] = {2 * q < n, 2 * q + 1 < n};
+    float* at[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl + (kVec ? 4 * g : g);
+    const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.V * rank;
+    float4 near[2][2];                                   // (kVec) logits of the next step
+    auto fetch = [&](int c) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        near[h][0] = *reinterpret_cast<const float4*>(at[h] + c * kAdChunk);
+        near[h][1] = *reinterpret_cast<const float4*>(at[h] + c * kAdChunk + 32);
+      }
     };
-    if (kVec) {
-      __syncwarp();
-      if (c_begin < c_end) fetch(c_begin, stage);
-      if (c_begin + kAdUpWarps < c_end) fetch(c_begin + kAdUpWarps, stage + 1 == kAdStages ? 0 : stage + 1);
-    }
+    const int c_whole = min(c_end, p.V / kAdChunk);      // steps before it are whole
+    if (kVec && c_begin < c_whole) fetch(c_begin);
+    auto row = [&](int c, int e) {                       // (a ragged step: entries past the vocabulary read its last row)
+      const int v = c * kAdChunk + 8 * e + g;
+      return Bm + static_cast<size_t>(c < c_whole ? v : min(v, p.V - 1)) * rank;
+    };
+    uint2 ahead[8];
+    auto ask = [&](int c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ahead[e] = make_uint2(0u, 0u);
+        if (kR == 16 || 4 * q < kR) ahead[e] = *reinterpret_cast<const uint2*>(row(c, e) + 4 * q);
+      }
+    };
+    if (kAhead && c_begin < c_end) ask(c_begin);
 
     for (int i = threadIdx.x; i < steps * kAdRows * 4; i += kAdUpWarps * 32) {
       const int k = i >> 5, r = (i >> 2) & 7, qq = i & 3;
@@ -318,45 +316,38 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) 
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const __nv_bfloat16 h = __float2bfloat16_rn(u[e]);
-            u[e] -= __bfloat162float(h);                   // (exact)
+            u[e] -= __bfloat162float(h);                 // (exact)
             w[pl][e >> 1] |= static_cast<uint32_t>(__bfloat16_as_ushort(h)) << (16 * (e & 1));
           }
       }
 #pragma unroll
       for (int pl = 0; pl < 3; ++pl) planes[pl][k][r][qq] = make_uint2(w[pl][0], w[pl][1]);
     }
-    // This lane's rows of the logits, from entry g on, and B from entry g and its first rank on.
-    const bool have[2] = {2 * q < n, 2 * q + 1 < n};
-    float* at[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) at[h] = p.logits + static_cast<size_t>(tile.row[have[h] ? 2 * q + h : 0]) * p.ldl + g;
-    const uint16_t* Bm = p.Bm + static_cast<size_t>(tile.adapter) * p.V * rank;
     __syncthreads();
     RowStats st[2];
     st[0].clear(); st[1].clear();
-    uint2 ahead[8];
-    auto row = [&](int c, int e) {                         // (a ragged step: entries past the vocabulary read its last row)
-      const int v = c * kAdChunk + 8 * e + g;
-      return Bm + static_cast<size_t>(c * kAdChunk + kAdChunk <= p.V ? v : min(v, p.V - 1)) * rank;
-    };
-    auto ask = [&](int c) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        ahead[e] = make_uint2(0u, 0u);
-        if (kR == 16 || 4 * q < kR) ahead[e] = *reinterpret_cast<const uint2*>(row(c, e) + 4 * q);
-      }
-    };
-    if (kAhead && c_begin < c_end) ask(c_begin);
     for (int c = c_begin; c < c_end; c += kAdUpWarps) {
       const int v0 = c * kAdChunk, vg = v0 + g;
-      const bool whole = v0 + kAdChunk <= p.V;
-      float* buf[2];
+      const bool whole = c < c_whole;
       float l[2][8];
-      if (!kVec) {
+      if (kVec && whole) {
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          *reinterpret_cast<float4*>(&buffer[warp][2 * q + h][4 * g]) = near[h][0];
+          *reinterpret_cast<float4*>(&buffer[warp][2 * q + h][32 + 4 * g]) = near[h][1];
+        }
+        __syncwarp();
+        if (c + kAdUpWarps < c_whole) fetch(c + kAdUpWarps);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) l[h][e] = have[h] && vg + 8 * e < p.V ? at[h][v0 + 8 * e] : -CUDART_INF_F;
+          for (int e = 0; e < 8; ++e) l[h][e] = buffer[warp][2 * q + h][8 * e + g];
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) l[h][e] = whole || vg + 8 * e < p.V ? at[h][v0 + 8 * e - (kVec ? 3 * g : 0)] : -CUDART_INF_F;
       }
       float d[4][4];
 #pragma unroll
@@ -370,7 +361,7 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) 
         for (int pl = 2; pl >= 0; --pl) {
           const uint2 u = planes[pl][0][g][q];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {                    // entries 16 t + g at m = g, 16 t + 8 + g at m = g + 8
+          for (int t = 0; t < 4; ++t) {                  // entries 16 t + g at m = g, 16 t + 8 + g at m = g + 8
             const uint32_t f[4] = {w[2 * t].x, w[2 * t + 1].x, w[2 * t].y, w[2 * t + 1].y};
             mma_bf16(d[t], f, u.x, u.y);
           }
@@ -414,44 +405,51 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) 
           }
         }
       }
-      if (kVec) {
-        lost = !adapter_wait(smem_u32(&arrived[warp][stage]), parity, p.status);
-        if (lost) break;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          buf[h] = &buffers[warp][stage][(2 * q + h) * kAdPitch + g];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) l[h][e] = whole || (have[h] && vg + 8 * e < p.V) ? buf[h][8 * e] : -CUDART_INF_F;
-        }
-      }
+      // (Both rows in one stretch of code: a lane without them carries numbers that nobody reads.)
+      float top[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (!have[h]) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          l[h][e] += d[e >> 1][2 * (e & 1) + h];
-          if (!whole && vg + 8 * e >= p.V) l[h][e] = -CUDART_INF_F;
-          else if (kVec) buf[h][8 * e] = l[h][e];
-          else at[h][v0 + 8 * e] = l[h][e];
+        for (int e = 0; e < 8; ++e) l[h][e] += d[e >> 1][2 * (e & 1) + h];         // (past the vocabulary: -inf + something)
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (vg + 8 * e >= p.V) l[h][e] = -CUDART_INF_F;
         }
-        if (whole) st[h].template fold<false>(l[h], p.want_arg, [&](int e) { return vg + 8 * e; });
-        else if (vg < p.V) st[h].template fold<true>(l[h], p.want_arg, [&](int e) { return vg + 8 * e; });
+        top[h] = fmaxf(max3(max3(l[h][0], l[h][1], l[h][2]), max3(l[h][3], l[h][4], l[h][5]), l[h][6]), l[h][7]);
       }
-      if (kVec) {
-        fence_async_shared();
+      if (__any_sync(0xffffffffu, p.want_arg || top[0] > st[0].rise || top[1] > st[1].rise)) {
+        st[0].rises(l[0], top[0], p.want_arg, [&](int e) { return vg + 8 * e; });
+        st[1].rises(l[1], top[1], p.want_arg, [&](int e) { return vg + 8 * e; });
+      }
+      if (whole) {
+        st[0].template add<false>(l[0], top[0]);
+        st[1].template add<false>(l[1], top[1]);
+      } else if (vg < p.V) {
+        st[0].template add<true>(l[0], top[0]);
+        st[1].template add<true>(l[1], top[1]);
+      }
+      if (kVec && whole) {
         __syncwarp();
-        if (lane < n) bulk_store(own_row + v0, smem_u32(&buffers[warp][stage][lane * kAdPitch]), bytes_of(c));
-        bulk_commit();
-        // the buffer of the step before is free for the step after next once its rows have been read out
-        const int next = c + 2 * kAdUpWarps;
-        if (next < c_end) {
-          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          fetch(next, stage == 0 ? kAdStages - 1 : stage - 1);
-        }
-        if (++stage == kAdStages) { stage = 0; parity ^= 1u; }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) buffer[warp][2 * q + h][8 * e + g] = l[h][e];
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (have[h]) {
+            *reinterpret_cast<float4*>(at[h] + v0) = *reinterpret_cast<const float4*>(&buffer[warp][2 * q + h][4 * g]);
+            *reinterpret_cast<float4*>(at[h] + v0 + 32) = *reinterpret_cast<const float4*>(&buffer[warp][2 * q + h][32 + 4 * g]);
+          }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (have[h] && (whole || vg + 8 * e < p.V)) at[h][v0 + 8 * e - (kVec ? 3 * g : 0)] = l[h][e];
       }
     }
-    if (kVec) bulk_wait_all();
     // a row's statistics over the eight lanes that hold it, then over the warps
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -481,7 +479,7 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kR == 8 || kR == 16 ? 5 : 4) 
         p.partials[static_cast<size_t>(tile.row[i / stale]) * p.part_stride + P + i % stale] =
             make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(0x7fffffff));
     }
-    if (__syncthreads_or(lost)) return;                  // (the planes and the warps' statistics have been read)
+    __syncthreads();                                     // (the planes and the warps' statistics have been read)
   }
 }
 
@@ -505,7 +503,7 @@ cudaError_t launch_adapter_down(const AdapterParams& p, cudaStream_t stream) {
 
 cudaError_t launch_adapter_up(const AdapterParams& p, int num_sms, cudaStream_t stream) {
   // As many CTAs as fit (by registers), a chunk per warp at least.
-  const int chunks = (p.V + kAdChunk - 1) / kAdChunk, resident = p.rank == 8 || p.rank == 16 ? 5 : 4;
+  const int chunks = (p.V + kAdChunk - 1) / kAdChunk, resident = kAdUpCtas;
   const long long most = static_cast<long long>(p.max_tiles) * ((chunks + kAdUpWarps - 1) / kAdUpWarps);
   const unsigned grid = static_cast<unsigned>(most < resident * num_sms ? most : resident * num_sms);
   const bool vec = p.ldl % 4 == 0 && (reinterpret_cast<uintptr_t>(p.logits) & 15u) == 0;

@@ -3590,8 +3590,8 @@ hola_status run_adapted_lm_head(hola_ctx* ctx, const hola_verify_args* a, const 
   return HOLA_OK;
 }
 
-hola_status check_adapters(const hola_adapters* ad) {
-  if (!ad || !ad->A || !ad->B || !ad->ids || ad->slots <= 0 || ad->rank <= 0) return HOLA_ERR_INVALID_ARG;
+hola_status check_adapters(const hola_adapters* ad, const hola_verify_args* a) {
+  if (!ad || !a || !ad->A || !ad->B || (!ad->ids && a->B != 0) || ad->slots <= 0 || ad->rank <= 0) return HOLA_ERR_INVALID_ARG;
   if (!aligned16(ad->A) || !aligned16(ad->B)) return HOLA_ERR_INVALID_ARG;
   if (ad->rank % 8 != 0 || ad->rank > kAdMaxRank) return HOLA_ERR_UNSUPPORTED_SHAPE;
   return HOLA_OK;
@@ -4068,7 +4068,7 @@ hola_status hola_lm_head_entropy(hola_ctx* ctx, const hola_verify_args* a, void*
 }
 
 hola_status hola_lm_head_adapters(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, void* cuda_stream) {
-  const hola_status s = check_adapters(ad);
+  const hola_status s = check_adapters(ad, a);
   return s == HOLA_OK ? lm_head_entropy(ctx, a, ad, cuda_stream) : s;
 }
 
@@ -4325,7 +4325,7 @@ static hola_status verify(hola_ctx* ctx, const hola_verify_args* a, const hola_a
 hola_status hola_verify(hola_ctx* ctx, const hola_verify_args* a, void* cuda_stream) { return verify(ctx, a, nullptr, cuda_stream); }
 
 hola_status hola_verify_adapters(hola_ctx* ctx, const hola_verify_args* a, const hola_adapters* ad, void* cuda_stream) {
-  const hola_status s = check_adapters(ad);
+  const hola_status s = check_adapters(ad, a);
   return s == HOLA_OK ? verify(ctx, a, ad, cuda_stream) : s;
 }
 

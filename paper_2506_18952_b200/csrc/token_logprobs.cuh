@@ -125,8 +125,8 @@ template <typename T>
 struct LpGroup {
   static constexpr int kEntries = kLpGroupBytes / sizeof(T);
   uint32_t w[8];
-  __device__ __forceinline__ void load(const T* p) {     // 32 bytes that this kernel never sees change, past the L1
-    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+  __device__ __forceinline__ void load(const T* p) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
   }
   // Entries 2 i and 2 i + 1.

@@ -225,6 +225,15 @@ def test_what_is_not_finite_stays_in_its_requests():
 
 
 @gpu
+def test_an_empty_batch():
+    bank = binding.AdapterBank.empty(2, 8, 64, 500, "cuda")
+    with binding.HolaVerify(2, 1, 64, 500) as ctx:
+        hidden, W = torch.zeros((0, 2, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((500, 64), dtype=torch.bfloat16, device="cuda")
+        out = ctx.hola_lm_head_adapters(hidden, W, bank, torch.zeros((0,), dtype=torch.int32, device="cuda"))
+        assert out.logits.shape == (0, 2, 500) and out.status.item() == 0
+
+
+@gpu
 def test_indices_that_no_slot_has():
     B, k, H, V = 6, 2, 128, 999
     d = make(B, k, H, V, 2, 8, seed=4)
@@ -327,14 +336,34 @@ def _adapters(**kw):
 
 @pytest.mark.parametrize("change,status", [
     (dict(A=None), 1), (dict(B=None), 1), (dict(ids=None), 1), (dict(slots=0), 1), (dict(slots=-1), 1), (dict(rank=0), 1), (dict(rank=-8), 1),
-    (dict(A=4104), 1), (dict(B=4104), 1), (dict(rank=4), 2), (dict(rank=136), 2), (dict(rank=12), 2), ({}, 1)])
+    (dict(A=4104), 1), (dict(B=4104), 1), (dict(rank=4), 2), (dict(rank=136), 2), (dict(rank=12), 2), ({}, 1), (dict(B=None, ids=None), 1)])
 def test_refused_by_the_library(change, status):
     """(The last one: adapters that are in order, and no context.)"""
     lib = binding.load_library()
     ad, a = _adapters(**change), binding.hola_verify_args()
+    a.B = 1
     for fn in (lib.hola_lm_head_adapters, lib.hola_verify_adapters):
         assert fn(None, ctypes.byref(a), ctypes.byref(ad), None) == status
         assert fn(None, ctypes.byref(a), None, None) == 1
+
+
+@gpu
+def test_two_contexts_on_two_streams_at_once():
+    B, k, H, V = 16, 3, 256, 20000
+    d = make(B, k, H, V, 4, 16, seed=31)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as one, binding.HolaVerify(B, k, H, V) as two:
+        want = one.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"])
+        other = d["ids"].roll(1)
+        want2 = two.hola_lm_head_adapters(d["hidden"], d["W"], bank, other)
+        torch.cuda.synchronize()
+        s, t = torch.cuda.Stream(), torch.cuda.Stream()
+        for _ in range(5):
+            a = one.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"], stream=s)
+            b = two.hola_lm_head_adapters(d["hidden"], d["W"], bank, other, stream=t)
+            torch.cuda.synchronize()
+            for f in ("logits", "logZ", "entropy"):
+                assert torch.equal(getattr(a, f), getattr(want, f)) and torch.equal(getattr(b, f), getattr(want2, f))
 
 
 def test_struct_layout():

@@ -305,63 +305,74 @@ struct LpThread {
     for (int q = 0; q < (kRank ? kRank : 1); ++q) count[q] = 0;
   }
 
-  // Group j, by all lanes of a warp together (a lane without one brings a group of -inf); v0: its first entry.  kPlain: it is whole
-  // and comes behind those before it.
-  template <bool kPlain>
-  __device__ __forceinline__ void take(const LpGroup<T>& g, int j, int v0, const LpToken<T>* tok, float l_min, bool ragged) {
-    const float top = g.largest();
-    if (!kSums) bad = bad || !(top < CUDART_INF_F);
-    if (kTop) {
-      second = fmaxf(second, fminf(top, m));
-      if (top > m || (!kPlain && top == m && j < at)) at = j;
+  // Groups j, j + kLpThreads ... (N of them), by all lanes of a warp together (a lane without one brings a group of -inf); v0: the first
+  // one's first entry.  kPlain: they are whole and come behind those before them.
+  template <bool kPlain, int N>
+  __device__ __forceinline__ void take(const LpGroup<T>* g, int j, int v0, const LpToken<T>* tok, float l_min, bool ragged) {
+    float top[N], most;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      top[u] = g[u].largest();
+      if (!kSums) bad = bad || !(top[u] < CUDART_INF_F);
+      if (kTop) {
+        second = fmaxf(second, fminf(top[u], m));
+        if (top[u] > m || (!kPlain && top[u] == m && j < at)) at = j + u * kLpThreads;
+      }
+      m = fmaxf(m, top[u]);
+      most = u ? fmaxf(most, top[u]) : top[u];
     }
-    m = fmaxf(m, top);
     // seldom: the maximum rises, or there are entries before a token
-    if (__any_sync(0xffffffffu, (kSums && top > rise) || (kRank && top >= l_min))) {
-      if (kRank && top >= l_min) {
+    if (__any_sync(0xffffffffu, (kSums && most > rise) || (kRank && most >= l_min))) {
+      if (kRank && most >= l_min) {
 #pragma unroll
-        for (int q = 0; q < kRank; ++q) {
-          if (!(top >= tok[q].l)) continue;
-          if (ragged || (v0 <= tok[q].x && v0 + E > tok[q].x)) {
+        for (int u = 0; u < N; ++u) {
+          const int v = v0 + u * kLpThreads * E;
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-              const float l = g.entry(i);
-              count[q] += v0 + i >= 0 && (l > tok[q].l || (l == tok[q].l && v0 + i < tok[q].x)) ? 1 : 0;
+          for (int q = 0; q < kRank; ++q) {
+            if (!(top[u] >= tok[q].l)) continue;
+            if (ragged || (v <= tok[q].x && v + E > tok[q].x)) {
+#pragma unroll
+              for (int i = 0; i < E; ++i) {
+                const float l = g[u].entry(i);
+                count[q] += v + i >= 0 && (l > tok[q].l || (l == tok[q].l && v + i < tok[q].x)) ? 1 : 0;
+              }
+            } else {
+              count[q] += lp_count(g[u], v < tok[q].x ? tok[q].limit[1] : tok[q].limit[0]);
             }
-          } else {
-            count[q] += lp_count(g, v0 < tok[q].x ? tok[q].limit[1] : tok[q].limit[0]);
           }
         }
       }
-      if (kSums && top > rise) {
+      if (kSums && most > rise) {
         const float old = shift;
-        shift = fabsf(top) < 1e37f ? -top * kLog2e : CUDART_NAN_F;    // (NaN: every group goes the long way below)
+        shift = fabsf(most) < 1e37f ? -most * kLog2e : CUDART_NAN_F;  // (NaN: every group goes the long way below)
         if (ref != -CUDART_INF_F) {
           float dx = shift - old;
-          if (!(dx == dx)) dx = (ref - top) * kLog2e;
+          if (!(dx == dx)) dx = (ref - most) * kLog2e;
           dx = fmaxf(dx, -1e28f);
           const float e = ex2_approx(dx);
           const uint64_t e2 = pack2(e, e);
           t2 = mul2(fma2(pack2(dx, dx), s2, t2), e2);
           s2 = mul2(s2, e2);
         }
-        ref = top;
-        rise = top + kLpSlack;
+        ref = most;
+        rise = most + kLpSlack;
       }
     }
     if (!kSums) return;
     const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
     uint64_t ps[2] = {0, 0}, pt[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      float a, b;
-      g.pair(i, a, b);
-      const uint64_t x = fma2(pack2(a, b), l2e, sh);
-      unpack2(x, a, b);
-      const uint64_t e = pack2(ex2_approx(a), ex2_approx(b));
-      ps[i & 1] = i < 2 ? e : add2(ps[i & 1], e);
-      pt[i & 1] = i < 2 ? mul2(e, x) : fma2(e, x, pt[i & 1]);
-    }
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) {
+        float a, b;
+        g[u].pair(i, a, b);
+        const uint64_t x = fma2(pack2(a, b), l2e, sh);
+        unpack2(x, a, b);
+        const uint64_t e = pack2(ex2_approx(a), ex2_approx(b));
+        ps[i & 1] = u == 0 && i < 2 ? e : add2(ps[i & 1], e);
+        pt[i & 1] = u == 0 && i < 2 ? mul2(e, x) : fma2(e, x, pt[i & 1]);
+      }
     const uint64_t both = add2(pt[0], pt[1]);
     float a, b;
     unpack2(both, a, b);
@@ -374,19 +385,24 @@ struct LpThread {
     if (fine) {
       s2 = add2(s2, add2(ps[0], ps[1]));
       t2 = add2(t2, both);
-    } else if (!(top < CUDART_INF_F)) {                  // there is no distribution
-      bad = true;
-    } else if (top != -CUDART_INF_F) {
-      // 0 * -inf: entries that are masked (-inf, or as low as the type goes), or too large for x
-      float s = 0.f, t = 0.f;
+      return;
+    }
+    // 0 * -inf: entries that are masked (-inf, or as low as the type goes), or too large for x; or there is no distribution
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float x = lp_below(g.entry(i), ref) * kLog2e, e = ex2_approx(x);
-        s += e;
-        t = fmaf(e, x, t);
+    for (int u = 0; u < N; ++u) {
+      if (!(top[u] < CUDART_INF_F)) {
+        bad = true;
+      } else if (top[u] != -CUDART_INF_F) {
+        float s = 0.f, t = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float x = lp_below(g[u].entry(i), ref) * kLog2e, e = ex2_approx(x);
+          s += e;
+          t = fmaf(e, x, t);
+        }
+        s2 = add2(s2, pack2(s, 0.f));
+        t2 = add2(t2, pack2(t, 0.f));
       }
-      s2 = add2(s2, pack2(s, 0.f));
-      t2 = add2(t2, pack2(t, 0.f));
     }
   }
 
@@ -447,7 +463,10 @@ __device__ __forceinline__ void lp_no_token(const LpParams& p, int row, bool val
 // CTAs per SM, by registers: what 16-bit logits are expanded to and the alternatives' bookkeeping do not fit 64 together (us at
 // 80 / at 64: 192 x 32000 bf16, 8 alternatives 22.3 / 24.6; 2304 x 128256 bf16, none 137.7 / 117.2).
 template <typename T>
-constexpr int lp_per_sm(bool sums, bool top) { return sums && top && sizeof(T) == 2 ? 3 : 4; }
+constexpr int lp_per_sm(bool sums, bool top) { return (sums && top && sizeof(T) == 2) || sizeof(T) == 4 ? 3 : 4; }
+// Groups that a thread takes together: sixteen entries.
+template <typename T>
+constexpr int kLpTogether = sizeof(T) == 4 ? 2 : 1;
 
 // What bounds it: HBM for large batches; for a few rows the chain token -> its logit -> pass -> board -> second look -> counting.
 template <typename T, bool kSums, bool kTop, int kRank>
@@ -491,12 +510,16 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
     }
   }
 
-  // Rounds in which every thread has a whole group, and one for what is left; the row's first group, where it lacks entries, has one
-  // of its own.  The first group is on its way while the tokens and their logits are looked up.
-  const int j_first = max(j_begin, min(r.whole_begin, j_end)), rounds = max(0, min(j_end, r.whole_end) - j_first) / kLpThreads;
-  LpGroup<T> next;
+  // Rounds in which every thread has N whole groups, and some for what is left; the row's first group, where it lacks entries, has one
+  // of its own.  The first groups are on their way while the tokens and their logits are looked up.
+  constexpr int N = kLpTogether<T>;
+  const int j_first = max(j_begin, min(r.whole_begin, j_end)), rounds = max(0, min(j_end, r.whole_end) - j_first) / (N * kLpThreads);
+  LpGroup<T> next[N];
   const T* ptr = r.base + static_cast<size_t>(j_first + tid) * E;
-  if (rounds > 0) next.load(ptr);
+  if (rounds > 0) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) next[u].load(ptr + u * kLpThreads * E);
+  }
 
   LpToken<T> tok[kRank ? kRank : 1];
   float l_min = CUDART_INF_F;
@@ -515,22 +538,29 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
   int j = j_first + tid;
   LpThread<T, kSums, kTop, kRank> th(j);
 #pragma unroll 1
-  for (int i = 0; i < rounds; ++i, j += kLpThreads) {
-    const LpGroup<T> g = next;
-    ptr += kLpThreads * E;
-    if (i + 1 < rounds) next.load(ptr);
-    th.template take<true>(g, j, r.first(j), tok, l_min, false);
+  for (int i = 0; i < rounds; ++i, j += N * kLpThreads) {
+    LpGroup<T> g[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) g[u] = next[u];
+    ptr += N * kLpThreads * E;
+    if (i + 1 < rounds) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) next[u].load(ptr + u * kLpThreads * E);
+    }
+    th.template take<true, N>(g, j, r.first(j), tok, l_min, false);
   }
 #pragma unroll 1
-  for (int i = 0; i < 2; ++i) {
-    if (i == 1) {
+  for (int i = 0; i <= N; ++i, j += kLpThreads) {        // (less than N groups a thread and a ragged one; the first)
+    if (i == N) {
       if (j_begin == j_first || warp != 0) break;
       j = lane == 0 ? 0 : j_end;
+    } else if (j - tid >= j_end) {
+      continue;
     }
     const bool some = j < j_end, ragged = !some || !r.whole(j);
     LpGroup<T> g = r.none();
     if (some) g = r.get(j);
-    th.template take<false>(g, j, some ? r.first(j) : INT32_MAX - E, tok, l_min, ragged);
+    th.template take<false, 1>(&g, j, some ? r.first(j) : INT32_MAX - E, tok, l_min, ragged);
   }
 
   // The threads' sums and counts, over the warp.

@@ -8,7 +8,7 @@
 //
 // The alternatives cost the pass next to nothing: every thread keeps the maximum of what it has seen and the group that it first
 // met it in.  Every eight threads put the best of their (maximum, group) pairs, in the order (value descending, group ascending),
-// on a board of 32; let the n-th best there be (w, g).  At least n entries lie at or before it (those maxima), so every one of the
+// on a board of 32 (every four on one of 64, for more than twenty alternatives); let the n-th best there be (w, g).  At least n entries lie at or before it (those maxima), so every one of the
 // part's n best has a value above w, or w itself in a group up to g.  Only threads whose own pair is at or before (w, g) can hold
 // such entries.  The group of their maximum is read again, out of the L2, and their other groups where the second-best may qualify
 // too.  What qualifies (n entries and some more) goes to the row's first CTA, which places each entry by counting those before it.
@@ -16,7 +16,7 @@
 constexpr int kLpThreads = 256;
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpGroupBytes = 32;      // neighbouring entries that a thread loads at once
-constexpr int kLpSpots = 64;           // entries that a part may send unsorted; beyond that it sends its 32 best
+constexpr int kLpSpots = 128;          // entries that a part may send unsorted; beyond that it sends its 32 best
 constexpr float kLpSlack = 4.f;        // how far a maximum may rise above the point that the sums are taken about
 constexpr int kLpMaxTop = 32;          // alternatives: a sorted list lies across a warp, one entry per lane
 constexpr int kLpTok = 4;              // tokens ranked in one pass (counters in registers)
@@ -586,21 +586,27 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
 
   if (kTop) {
     const uint64_t own = th.at < j_end ? lp_key(th.m, th.at) : 0;       // (a thread without a group: nothing)
+    // (fewer threads to a place of the board where not all of them have groups)
+    const int held = j_end - j_begin, board = p.n_top > 20 ? 64 : 32;
+    int share = kLpThreads / board;
+    while (share > 1 && held <= share / 2 * board) share >>= 1;
     uint64_t a = own;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
+    for (int o = 1; o < share; o <<= 1) {
       const uint64_t b = __shfl_xor_sync(0xffffffffu, a, o);
       if (b > a) a = b;
     }
-    if ((lane & 7) == 0) lists[warp * 4 + (lane >> 3)] = a;
+    if ((lane & (share - 1)) == 0 && tid < board * share) lists[tid / share] = a;
     __syncthreads();
     // every warp for itself: the n-th best on the board (its keys differ, but for empty ones)
-    const uint64_t key = lists[lane];
-    int before = 0;
+    uint64_t lim = 0;                                    // (0: fewer hold anything)
+    for (int at = 0; at < board; at += 32) {
+      const uint64_t key = lists[at + lane];
+      int before = 0;
 #pragma unroll 8
-    for (int i = 0; i < 32; ++i) before += lists[i] > key ? 1 : 0;
-    const unsigned nth = __ballot_sync(0xffffffffu, key != 0 && before == p.n_top - 1);
-    uint64_t lim = nth ? __shfl_sync(0xffffffffu, key, __ffs(nth) - 1) : 0;     // (0: fewer hold anything)
+      for (int i = 0; i < board; ++i) before += lists[i] > key ? 1 : 0;
+      const unsigned nth = __ballot_sync(0xffffffffu, key != 0 && before == p.n_top - 1);
+      if (nth) lim = __shfl_sync(0xffffffffu, key, __ffs(nth) - 1);
+    }
     float w = lp_value(static_cast<uint32_t>(lim >> 32));
     int g_last = static_cast<int>(~static_cast<uint32_t>(lim));
     // Masked rows: fewer entries than alternatives are left, the others are -inf by rising id.  The part's first ones serve, where 64
@@ -722,7 +728,7 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
     all.spots = kTop ? n_spots : 0;
     LpPart* to = C > 1 ? cg::this_cluster().map_shared_rank(&parts[part], 0) : &parts[part];
     if (lane == 0) *to = all;
-  } else if (kTop && warp <= 2) {
+  } else if (kTop && warp <= kLpSpots / 32) {
     uint64_t* to = C > 1 ? cg::this_cluster().map_shared_rank(&spots[part][0], 0) : &spots[part][0];
     const int i = (warp - 1) * 32 + lane;
     if (i < n_spots) to[i] = own_spots[i];

@@ -305,6 +305,41 @@ def test_graphs_streams_and_changing_batches():
 
 
 @gpu
+def test_the_whole_run_in_two_graphs_of_one_context():
+    """Adapted verify step and scores of what it emitted, captured twice on one context (they share its workspace) and replayed in
+    turn; every input is written by kernels right in front of the call."""
+    B, k, H, V = 12, 4, 256, 6000
+    w, d = _verify_inputs(B, k, H, V, 3, 16, seed=41)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    src = [w.hidden, w.draft_tok, w.draft_q, w.uniforms, d["ids"]]
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        def run(x, out=None):
+            out = ctx.hola_verify_adapters(x[0], w.W_lm, x[1], x[2], x[3], w.tau, bank, x[4], want_logits=True, out=out)
+            lp = binding.hola_token_logprobs(out.logits, n_top=7, logZ=out.logZ, emitted=(x[1], out.accept_len, out.next_tok))
+            return [out.accept_len, out.next_tok, out.entropy, out.logZ, out.logits, lp.logprob, lp.rank, lp.top_ids, lp.top_logprobs]
+        graphs = []
+        for _ in range(2):
+            host = [t.clone() for t in src]
+            run(host)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                x = [t.roll(0, 0) if t.dtype != torch.bfloat16 else t * 1 for t in host]
+                got = run(x)
+            graphs.append((graph, host, x, got))
+        for r in range(4):
+            graph, host, x, got = graphs[r % 2]
+            for h, t in zip(host, src):
+                h.copy_(t.roll(r, 0))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in got]
+            want = run([t.roll(r, 0) for t in src])
+            for a, b in zip(got, want):
+                assert torch.equal(a, b)
+
+
+@gpu
 def test_rows_behind_the_batch_and_calls_in_between_keep_their_results():
     """A context made for more: nothing beyond the batch's rows is written, and bare calls before and after give the same bits."""
     B, k, H, V = 3, 2, 128, 1003

@@ -460,16 +460,15 @@ __device__ __forceinline__ void lp_no_token(const LpParams& p, int row, bool val
   }
 }
 
-// CTAs per SM, by registers: what 16-bit logits are expanded to and the alternatives' bookkeeping do not fit 64 together (us at
-// 80 / at 64: 192 x 32000 bf16, 8 alternatives 22.3 / 24.6; 2304 x 128256 bf16, none 137.7 / 117.2).
+// CTAs per SM, by registers: what 16-bit logits are expanded to and the alternatives' bookkeeping do not fit 64 together, nor do two
+// groups of fp32 on the way (us at 80 / at 64 registers: 192 x 32000 bf16, 8 alternatives 12.7 / 15.0; 384 x 128256 fp32, 20
+// alternatives 42.5 / 46.5; but 2304 x 128256 bf16, none 134.3 / 116.2).
 template <typename T>
 constexpr int lp_per_sm(bool sums, bool top) { return (sums && top && sizeof(T) == 2) || sizeof(T) == 4 ? 3 : 4; }
-// Groups that a thread takes together: sixteen entries.
-template <typename T>
-constexpr int kLpTogether = sizeof(T) == 4 ? 2 : 1;
 
 // What bounds it: HBM for large batches; for a few rows the chain token -> its logit -> pass -> board -> second look -> counting.
-template <typename T, bool kSums, bool kTop, int kRank>
+// N: groups that a thread takes together.
+template <typename T, bool kSums, bool kTop, int kRank, int N>
 __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_logprobs_kernel(const LpParams p, int C) {
   constexpr int E = LpGroup<T>::kEntries;
   __shared__ uint64_t spots[kTop ? kLpMaxCluster : 1][kLpSpots];       // first CTA: what every part sends
@@ -512,7 +511,6 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
 
   // Rounds in which every thread has N whole groups, and some for what is left; the row's first group, where it lacks entries, has one
   // of its own.  The first groups are on their way while the tokens and their logits are looked up.
-  constexpr int N = kLpTogether<T>;
   const int j_first = max(j_begin, min(r.whole_begin, j_end)), rounds = max(0, min(j_end, r.whole_end) - j_first) / (N * kLpThreads);
   LpGroup<T> next[N];
   const T* ptr = r.base + static_cast<size_t>(j_first + tid) * E;
@@ -883,15 +881,15 @@ __global__ void __launch_bounds__(128) gather_logprobs_kernel(const LpParams p) 
 
 // CTAs per row: up to three on an SM, as long as a thread keeps a group or two of its own.  Start, merges and the second look are
 // latency, some 4 us a CTA, which more CTAs only add to, and a second wave for a few of them costs as much as the first.  us with 1 /
-// 2 / 4 / 8: 69 x 50003 fp16 19.2 / 15.6 / 15.4 / 22.9; 192 x 32000 bf16 30.5 / 22.3 / 30.9 / 48.4; 384 x 128256 fp32 52.0 / 58.7 /
-// 58.9 / 86.8; 5 x 32000 fp32 9.8 / 7.8 / 6.4 / 6.6.
+// 2 / 4 / 8: 69 x 50003 fp16 18.3 / 14.8 / 15.4 / 23.0; 192 x 32000 bf16 13.7 / 12.7 / 18.4 / 30.3; 384 x 128256 fp32 42.5 / 49.5 /
+// 63.2 / 99.9; 5 x 32000 fp32 9.5 / 7.8 / 6.7 / 7.0.
 int lp_cluster(int num_sms, int rows, int V) {
   int C = 1;
   while (C < kLpMaxCluster && 2ll * rows * C <= 3ll * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;
   return C;
 }
 
-template <typename T, bool kSums, bool kTop, int kRank>
+template <typename T, bool kSums, bool kTop, int kRank, int N>
 cudaError_t launch_logprobs(const LpParams& p, int C, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.rows) * C); cfg.blockDim = dim3(kLpThreads); cfg.stream = stream;
@@ -901,14 +899,22 @@ cudaError_t launch_logprobs(const LpParams& p, int C, cudaStream_t stream) {
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = static_cast<unsigned>(C); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kSums, kTop, kRank>, p, C);
+  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kSums, kTop, kRank, N>, p, C);
 }
 
-// One token per row is the rule: the pass then carries one comparison instead of kLpTok.
+// One token per row is the rule: the pass then carries one comparison instead of kLpTok.  Long rows of fp32 are taken two groups at a
+// time, which halves what each costs beside its sums and doubles what is on the way (us, one / two: 384 x 128256, one CTA a row,
+// 63 groups a thread 49.7 / 42.5; 32000 entries, 16 groups a thread 10.3 / 11.3; 16-bit logits 116 / 142).
+template <typename T, bool kSums, bool kTop, int N>
+cudaError_t launch_logprobs_of(const LpParams& p, bool rank, int C, cudaStream_t stream) {
+  return !rank ? launch_logprobs<T, kSums, kTop, 0, N>(p, C, stream)
+         : p.tn == 1 ? launch_logprobs<T, kSums, kTop, 1, N>(p, C, stream) : launch_logprobs<T, kSums, kTop, kLpTok, N>(p, C, stream);
+}
 template <typename T, bool kSums, bool kTop>
 cudaError_t launch_logprobs_of(const LpParams& p, bool rank, int C, cudaStream_t stream) {
-  return !rank ? launch_logprobs<T, kSums, kTop, 0>(p, C, stream)
-         : p.tn == 1 ? launch_logprobs<T, kSums, kTop, 1>(p, C, stream) : launch_logprobs<T, kSums, kTop, kLpTok>(p, C, stream);
+  const bool two = sizeof(T) == 4 && p.V / C >= 32 * kLpThreads * (kLpGroupBytes / 4);
+  return two ? launch_logprobs_of<T, kSums, kTop, sizeof(T) == 4 ? 2 : 1>(p, rank, C, stream)
+             : launch_logprobs_of<T, kSums, kTop, 1>(p, rank, C, stream);
 }
 
 template <typename T>

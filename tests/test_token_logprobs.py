@@ -111,7 +111,7 @@ def some_tokens(logits, T, seed):
 @gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows,V", [(1, 1), (3, 2), (5, 7), (2, 8), (7, 9), (4, 33), (9, 255), (6, 2048), (3, 2049), (5, 4097),
-                                    (2, 16384), (130, 1000), (700, 513), (5, 32000), (33, 50003), (2, 128256)])
+                                    (2, 16384), (130, 1000), (700, 513), (5, 32000), (33, 50003), (2, 128256), (3, 600001)])
 def test_rows_of_all_sizes(rows, V, dtype):
     n = min(V, 32)
     for pad, lead, n_top, T in ((0, 0, n, 1), (3, 1, min(5, n), 3), (1, 5, 0, 2), (8, 0, 1, 0)):
@@ -154,11 +154,12 @@ def test_ties_go_to_the_lowest_id(dtype, n_top):
 
 
 @gpu
+@pytest.mark.parametrize("rows", [6, 230])          # a cluster per row; one CTA, long rows of which are taken two groups at a time
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_best_entries_gathered_in_few_threads(dtype):
+def test_best_entries_gathered_in_few_threads(dtype, rows):
     """The best entries all lie in one thread's groups, in one warp's, in one CTA's part: lists fill up and are merged."""
-    V, n_top = 70000, 32
-    l = make(6, V, dtype, 3, spread=0.5)
+    V, n_top = (70000, 32) if rows == 6 else (66000, 20)
+    l = make(rows, V, dtype, 3, spread=0.5)
     at = torch.arange(V, device="cuda")
     l[0, (at // 8) % 256 == 37] += 20
     l[1, ((at // 8) % 256) // 32 == 6] += 20
@@ -168,7 +169,12 @@ def test_best_entries_gathered_in_few_threads(dtype):
     l[5, 12345] += 30
     t = some_tokens(l, 2, 9)
     out = binding.hola_token_logprobs(l, t, n_top=n_top)
-    check(out, reference(l, t, n_top), l, V, t, n_top)
+    some = slice(0, 8)                                        # (the others: as the first ones' kind, less to compare)
+    assert all(torch.equal(a, b) for a, b in zip((out.top_ids[some], out.rank[some]),
+                                                 (lambda o: (o.top_ids, o.rank))(binding.hola_token_logprobs(l[some], t[some], n_top=n_top))))
+    ref = reference(l[some], t[some], n_top)
+    part = binding.TokenLogprobs(**{f: getattr(out, f)[some] for f in ("logprob", "rank", "entropy", "logZ", "top_ids", "top_logprobs")})
+    check(part, ref, l[some], V, t[some], n_top)
 
 
 @gpu

@@ -344,7 +344,9 @@ struct LpThread {
       }
       if (kSums && most > rise) {
         const float old = shift;
-        shift = fabsf(most) < 1e37f ? -most * kLog2e : CUDART_NAN_F;  // (NaN: every group goes the long way below)
+        // (Rounded, the shift is off by up to 2^-24 of itself, in every exponent alike: 0.05 at most here.  Beyond, where it would be
+        // the exponents that count, NaN: every group goes the long way below, from differences.)
+        shift = fabsf(most) < 5e5f ? -most * kLog2e : CUDART_NAN_F;
         if (ref != -CUDART_INF_F) {
           float dx = shift - old;
           if (!(dx == dx)) dx = (ref - most) * kLog2e;

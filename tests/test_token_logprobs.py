@@ -154,6 +154,28 @@ def test_ties_go_to_the_lowest_id(dtype, n_top):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [40, 3000, 70001])
+def test_masks_of_any_depth_and_logits_of_any_size(dtype, V):
+    """Masks of -1e4 .. -1e38 in single entries, in whole groups and throughout, and logits far from zero: sums are of differences."""
+    sizes = [1e4, 4e5, 6e5, 1e7, 1e9, 1e12, 1e20, 1e30, 9e36, 2e37, 2e38]
+    l = make(5 * len(sizes), V, dtype, V)
+    for i, big in enumerate(sizes):
+        l[5 * i, 1::2] = -big
+        l[5 * i + 1, V // 3:] = -big
+        l[5 * i + 2] = -big                                   # all of it
+        l[5 * i + 3] = l[5 * i + 3] + big                     # (where the type has it: a handful of steps)
+        l[5 * i + 4] = -big
+        l[5 * i + 4, V // 2] = big
+    t = some_tokens(l, 2, 3)
+    out = binding.hola_token_logprobs(l, t, n_top=9)
+    ref = reference(l, t, 9)
+    for name in ("logprob", "top_logprobs"):    # -4e38 (2e38 below a maximum of 2e38) has no fp32 of its own: it rounds to -inf
+        ref[name] = torch.where(ref[name] < -torch.finfo(torch.float32).max, -torch.inf, ref[name])
+    check(out, ref, l, V, t, 9)
+
+
+@gpu
 @pytest.mark.parametrize("rows", [6, 230])          # a cluster per row; one CTA, long rows of which are taken two groups at a time
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_best_entries_gathered_in_few_threads(dtype, rows):

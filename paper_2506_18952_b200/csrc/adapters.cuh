@@ -172,17 +172,19 @@ __global__ void __launch_bounds__(kAdDownWarps * 32, 1) adapter_down_kernel(cons
 }
 
 // Running statistics of a row about a point that trails the maximum by 4 at most, so that a rise of the maximum rarely makes a
-// warp rescale.  In units of ln 2: x = l log2 e + shift, s = sum 2^x, t = sum 2^x x.
+// warp rescale.  In units of ln 2: x = (l - ref) log2 e, s = sum 2^x, t = sum 2^x x.  (Differences first: one addition more a pair
+// than l log2 e + shift, whose shift would be off by 2^-24 of itself, which large logits turn into sums of zero or infinity.)
 struct RowStats {
-  float m, rise, shift;
+  float m, ref;                // (a row's first step: -inf and 0)
   uint64_t s2, t2;             // two halves of either sum
   int arg;
   __device__ __forceinline__ void clear() {
-    m = rise = -CUDART_INF_F;
-    shift = 0.f;
+    m = -CUDART_INF_F;
+    ref = 0.f;
     s2 = t2 = 0;
     arg = 0x7fffffff;
   }
+  __device__ __forceinline__ float rise() const { return m == -CUDART_INF_F ? m : ref + 4.f; }
   // Eight logits and their largest; entry i is vocabulary entry v(i), rising with i.  First what is seldom (the maximum rises by
   // more than 4, the arg-max is wanted), then the sums.  kSome: logits that are -inf are none.
   template <typename Entry>
@@ -194,25 +196,23 @@ struct RowStats {
         if (l[i] == top) first = v(i);
       arg = l[0] == top ? v(0) : first;
     }
-    if (top > rise) {
-      const float old = shift;
-      shift = -top * kLog2e;
-      if (rise != -CUDART_INF_F) {
-        const float dx = shift - old, e = ex2_approx(dx);
+    if (top > rise()) {
+      if (m != -CUDART_INF_F) {
+        const float dx = fmaxf((ref - top) * kLog2e, -1e30f), e = ex2_approx(dx);            // (finite: e is 0 there)
         const uint64_t e2 = pack2(e, e);
         t2 = mul2(fma2(pack2(dx, dx), s2, t2), e2);
         s2 = mul2(s2, e2);
       }
-      rise = top + 4.f;
+      ref = top;
     }
   }
   template <bool kSome>
   __device__ __forceinline__ void add(const float* l, float top) {
     m = fmaxf(m, top);
-    const uint64_t l2e = pack2(kLog2e, kLog2e), sh = pack2(shift, shift);
+    const uint64_t l2e = pack2(kLog2e, kLog2e), from = pack2(-ref, -ref);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint64_t x = fma2(pack2(l[2 * i], l[2 * i + 1]), l2e, sh);
+      uint64_t x = mul2(add2(pack2(l[2 * i], l[2 * i + 1]), from), l2e);
       float a, b;
       unpack2(x, a, b);
       const uint64_t e = pack2(ex2_approx(a), ex2_approx(b));
@@ -228,7 +228,7 @@ struct RowStats {
     const float s = a + b;
     if (s == 0.f) return stats_empty();
     if (!(s < CUDART_INF_F)) return Stats{CUDART_NAN_F, CUDART_NAN_F, CUDART_NAN_F, arg};       // (no distribution)
-    const float x = fmaf(m, kLog2e, shift), e = ex2_approx(-x);               // (x of the maximum, as it was summed)
+    const float x = (m - ref) * kLog2e, e = ex2_approx(-x);                   // (x of the maximum, as it was summed)
     return Stats{m, s * e, kLn2 * (e * fmaf(-x, s, c + d)), arg};
   }
 };
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kAdUpCtas) adapter_up_kernel(
         }
         top[h] = fmaxf(max3(max3(l[h][0], l[h][1], l[h][2]), max3(l[h][3], l[h][4], l[h][5]), l[h][6]), l[h][7]);
       }
-      if (__any_sync(0xffffffffu, p.want_arg || top[0] > st[0].rise || top[1] > st[1].rise)) {
+      if (__any_sync(0xffffffffu, p.want_arg || top[0] > st[0].rise() || top[1] > st[1].rise())) {
         st[0].rises(l[0], top[0], p.want_arg, [&](int e) { return vg + 8 * e; });
         st[1].rises(l[1], top[1], p.want_arg, [&](int e) { return vg + 8 * e; });
       }

@@ -103,6 +103,28 @@ def test_logits_and_statistics(B, k, H, V, slots, rank):
 
 
 @gpu
+@pytest.mark.parametrize("V", [1000, 9003])
+def test_statistics_of_logits_far_from_zero(V):
+    """A logit's distance to the maximum counts, not where the maximum is.  Sums of differences, which are rounded once: relative to
+    e^d |d| <= 0.37 per unit, like each merge's."""
+    sizes = [1e3, 1e5, 1e7, 1e9, 1e10, 3e12, 1e20, 1e30]
+    d = make(2 * len(sizes), 3, 256, V, len(sizes), 8, seed=V)
+    for i, big in enumerate(sizes):
+        d["Bup"][i, :, 0] = big                              # all of a row's logits by the same
+    d["ids"] = torch.arange(2 * len(sizes), device="cuda", dtype=torch.int32) // 2
+    with binding.HolaVerify(2 * len(sizes), 3, 256, V) as ctx:
+        out = ctx.hola_lm_head_adapters(d["hidden"], d["W"], binding.AdapterBank(d["A"], d["Bup"], d["scale"]), d["ids"])
+    l = out.logits.double()
+    m = l.amax(dim=-1)
+    logZ = torch.logsumexp(l - m[..., None], dim=-1)
+    lp = l - m[..., None] - logZ[..., None]
+    H = -(lp.exp() * lp).sum(-1)
+    E = (V / 1000 + 80) * U + 2.0 ** -22
+    assert ((out.logZ.double() - m - logZ).abs() <= E + 2 * U * m.abs()).all()
+    assert ((out.entropy.double() - H).abs() <= E * (1 + 3 * np.log(V + 1)) + 4 * U * np.log(V + 1)).all()
+
+
+@gpu
 @pytest.mark.parametrize("weights", ["int8", "w8a8", "w8a16", "mixed"])
 @pytest.mark.parametrize("B,k,H,V,slots,rank", [(1, 4, 256, 3001, 3, 16), (16, 5, 1024, 8000, 4, 8), (64, 5, 512, 9000, 8, 24),
                                                 (90, 5, 256, 5000, 64, 16)])

@@ -202,21 +202,19 @@ struct LpRow {
   }
   __device__ __noinline__ LpGroup<T> get_ragged(int j) const {
     LpGroup<T> g;
-    {
-      const uint32_t none = none_bits();
+    const uint32_t none = none_bits();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g.w[i] = 0;
+    for (int i = 0; i < 8; ++i) g.w[i] = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const long long v = static_cast<long long>(j) * E - off + i;
-        uint32_t bits = none;
-        if (v >= 0 && v < V) {
-          if (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t*>(base)[v + off];
-          else bits = reinterpret_cast<const uint16_t*>(base)[v + off];
-        }
-        if (sizeof(T) == 4) g.w[i & 7] = bits;
-        else g.w[(i >> 1) & 7] |= bits << (16 * (i & 1));
+    for (int i = 0; i < E; ++i) {
+      const long long v = static_cast<long long>(j) * E - off + i;
+      uint32_t bits = none;
+      if (v >= 0 && v < V) {
+        if (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t*>(base)[v + off];
+        else bits = reinterpret_cast<const uint16_t*>(base)[v + off];
       }
+      if (sizeof(T) == 4) g.w[i & 7] = bits;
+      else g.w[(i >> 1) & 7] |= bits << (16 * (i & 1));
     }
     return g;
   }
@@ -349,7 +347,10 @@ struct LpThread {
         shift = fabsf(most) < 5e5f ? -most * kLog2e : CUDART_NAN_F;
         if (ref != -CUDART_INF_F) {
           float dx = shift - old;
-          if (!(dx == dx)) dx = (ref - most) * kLog2e;
+          if (!(dx == dx)) {                             // one of them from differences: x of the same logit, now less then
+            const float now = shift == shift ? fmaf(ref, kLog2e, shift) : (ref - most) * kLog2e;
+            dx = now - (old == old ? fmaf(ref, kLog2e, old) : 0.f);
+          }
           dx = fmaxf(dx, -1e28f);
           const float e = ex2_approx(dx);
           const uint64_t e2 = pack2(e, e);

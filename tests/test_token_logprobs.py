@@ -176,6 +176,19 @@ def test_masks_of_any_depth_and_logits_of_any_size(dtype, V):
 
 
 @gpu
+@pytest.mark.parametrize("span", [12.0, 40.0, 2e5, 2e6])
+def test_a_maximum_that_rises_through_large_numbers(span):
+    """Rows that climb, a little in every group of a thread, from below a large number (of either sign) to above it."""
+    rows, V = 230, 66000
+    g = torch.Generator(device="cuda").manual_seed(7)
+    ramp = torch.arange(V, device="cuda") / V - 0.5
+    centre = 5e5 + (torch.rand((rows, 1), generator=g, device="cuda") - 0.5) * 10
+    centre[::2] *= -1
+    l = centre + span * ramp + torch.randn((rows, V), generator=g, device="cuda")
+    check(binding.hola_token_logprobs(l, some_tokens(l, 1, 5), n_top=5), reference(l, some_tokens(l, 1, 5), 5), l, V, some_tokens(l, 1, 5), 5)
+
+
+@gpu
 @pytest.mark.parametrize("rows", [6, 230])          # a cluster per row; one CTA, long rows of which are taken two groups at a time
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_best_entries_gathered_in_few_threads(dtype, rows):

@@ -379,13 +379,7 @@ struct LpThread {
     const uint64_t both = add2(pt[0], pt[1]);
     float a, b;
     unpack2(both, a, b);
-    const bool fine = a + b == a + b;
-    if (__all_sync(0xffffffffu, fine)) {
-      s2 = add2(s2, add2(ps[0], ps[1]));
-      t2 = add2(t2, both);
-      return;
-    }
-    if (fine) {
+    if (a + b == a + b) {
       s2 = add2(s2, add2(ps[0], ps[1]));
       t2 = add2(t2, both);
       return;

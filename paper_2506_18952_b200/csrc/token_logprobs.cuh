@@ -509,12 +509,18 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
   // Rounds in which every thread has N whole groups, and some for what is left; the row's first group, where it lacks entries, has one
   // of its own.  The first groups are on their way while the tokens and their logits are looked up.
   const int j_first = max(j_begin, min(r.whole_begin, j_end)), rounds = max(0, min(j_end, r.whole_end) - j_first) / (N * kLpThreads);
-  LpGroup<T> next[N];
+  // What is on the way stays in its registers until it is used (a copy waits for it): rounds by turns.  384 x 32000 fp32, one / two on
+  // the way: 15.1 / 13.3 us out of HBM, 10.3 / 10.6 out of the L2; two of two groups each, 384 x 128256: 42.5 / 48.6, no registers left
+  // for it; 16-bit logits, 192 x 32000: 12.7 / 13.1.  Bulk prefetches into the L2 instead: 13.4 and 11.4 us, 42.5 -> 48.1.
+  constexpr int D = sizeof(T) == 4 && N == 1 ? 2 : 1;
+  LpGroup<T> next[D][N];
   const T* ptr = r.base + static_cast<size_t>(j_first + tid) * E;
-  if (rounds > 0) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) next[u].load(ptr + u * kLpThreads * E);
-  }
+  for (int d = 0; d < D; ++d)
+    if (d < rounds) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) next[d][u].load(ptr + (d * N + u) * kLpThreads * E);
+    }
 
   LpToken<T> tok[kRank ? kRank : 1];
   float l_min = CUDART_INF_F;
@@ -533,16 +539,21 @@ __global__ void __launch_bounds__(kLpThreads, lp_per_sm<T>(kSums, kTop)) token_l
   int j = j_first + tid;
   LpThread<T, kSums, kTop, kRank> th(j);
 #pragma unroll 1
-  for (int i = 0; i < rounds; ++i, j += N * kLpThreads) {
-    LpGroup<T> g[N];
+  for (int i = 0; i < rounds; i += D) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) g[u] = next[u];
-    ptr += N * kLpThreads * E;
-    if (i + 1 < rounds) {
+    for (int d = 0; d < D; ++d) {
+      if (d > 0 && i + d >= rounds) break;
+      LpGroup<T> g[N];
 #pragma unroll
-      for (int u = 0; u < N; ++u) next[u].load(ptr + u * kLpThreads * E);
+      for (int u = 0; u < N; ++u) g[u] = next[d][u];
+      if (i + d + D < rounds) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) next[d][u].load(ptr + (D * N + u) * kLpThreads * E);
+      }
+      ptr += N * kLpThreads * E;
+      th.template take<true, N>(g, j, r.first(j), tok, l_min, false);
+      j += N * kLpThreads;
     }
-    th.template take<true, N>(g, j, r.first(j), tok, l_min, false);
   }
 #pragma unroll 1
   for (int i = 0; i <= N; ++i, j += kLpThreads) {        // (less than N groups a thread and a ragged one; the first)
@@ -901,7 +912,8 @@ cudaError_t launch_logprobs(const LpParams& p, int C, cudaStream_t stream) {
 
 // One token per row is the rule: the pass then carries one comparison instead of kLpTok.  Long rows of fp32 are taken two groups at a
 // time, which halves what each costs beside its sums and doubles what is on the way (us, one / two: 384 x 128256, one CTA a row,
-// 63 groups a thread 49.7 / 42.5; 32000 entries, 16 groups a thread 10.3 / 11.3; 16-bit logits 116 / 142).
+// 63 groups a thread 46.2 / 42.5; 32000 entries, 16 groups a thread 10.6 / 11.3 out of the L2, 13.3 / 13.1 out of HBM; 16-bit logits
+// 116 / 142).
 template <typename T, bool kSums, bool kTop, int N>
 cudaError_t launch_logprobs_of(const LpParams& p, bool rank, int C, cudaStream_t stream) {
   return !rank ? launch_logprobs<T, kSums, kTop, 0, N>(p, C, stream)

@@ -393,7 +393,8 @@ struct LpThread {
         float s = 0.f, t = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          const float x = lp_below(g[u].entry(i), ref) * kLog2e, e = ex2_approx(x);
+          const float l = g[u].entry(i);                 // (about the same point as everything else)
+          const float x = shift == shift ? fmaxf(fmaf(l, kLog2e, shift), -1e30f) : lp_below(l, ref) * kLog2e, e = ex2_approx(x);
           s += e;
           t = fmaf(e, x, t);
         }

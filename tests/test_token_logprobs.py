@@ -176,6 +176,21 @@ def test_masks_of_any_depth_and_logits_of_any_size(dtype, V):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [62, 3001, 70001])
+@pytest.mark.parametrize("kept", [1.0, 0.99, 0.5])
+def test_masked_entries_among_logits_far_from_zero(dtype, V, kept):
+    """Groups that hold a masked entry, or a row's end, add up with those that hold none, about one and the same point."""
+    centre = torch.tensor([-4e5, -1e5, -1e4, -300.0, 300.0, 1e4, 4e4, 1e5, 4e5], device="cuda")[:, None]
+    centre = centre.clamp(-6e4, 6e4) if dtype == torch.float16 else centre
+    g = torch.Generator(device="cuda").manual_seed(V)
+    l = (centre + 3 * torch.randn((len(centre), V), generator=g, device="cuda")).to(dtype)
+    l[torch.rand(l.shape, generator=g, device="cuda") > kept] = -torch.inf
+    t = some_tokens(l, 2, 8)
+    check(binding.hola_token_logprobs(l, t, n_top=5), reference(l, t, 5), l, V, t, 5)
+
+
+@gpu
 @pytest.mark.parametrize("span", [12.0, 40.0, 2e5, 2e6])
 def test_a_maximum_that_rises_through_large_numbers(span):
     """Rows that climb, a little in every group of a thread, from below a large number (of either sign) to above it."""

@@ -385,6 +385,7 @@ struct LpThread {
       return;
     }
     // 0 * -inf: entries that are masked (-inf, or as low as the type goes), or too large for x; or there is no distribution
+    const float from = shift == shift ? fmaf(ref, kLog2e, shift) : 0.f;       // (about the same point as everything else)
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       if (!(top[u] < CUDART_INF_F)) {
@@ -393,8 +394,7 @@ struct LpThread {
         float s = 0.f, t = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          const float l = g[u].entry(i);                 // (about the same point as everything else)
-          const float x = shift == shift ? fmaxf(fmaf(l, kLog2e, shift), -1e30f) : lp_below(l, ref) * kLog2e, e = ex2_approx(x);
+          const float x = fmaf(lp_below(g[u].entry(i), ref), kLog2e, from), e = ex2_approx(x);
           s += e;
           t = fmaf(e, x, t);
         }

@@ -88,6 +88,7 @@ class hola_sample_info(ctypes.Structure):
 _lib = None
 _host = None            # the native helper (csrc/host_call.cpp), or None: arguments are then filled from Python
 _entry = {}             # addresses of the entry points that it calls
+_ADAPTER_ENTRIES = ("hola_lm_head_adapters", "hola_verify_adapters")     # those whose function takes a hola_adapters as well
 
 
 def _load_host(lib: ctypes.CDLL):
@@ -728,7 +729,7 @@ class HolaVerify:
                 return None
             wmix, w_scale = ctypes.addressof(W_lm.struct), W_lm.w_scale
             W_lm = W_lm.W8 if W_lm.W8 is not None else (W_lm.W4 if W_lm.W4 is not None else W_lm.W16)
-        if bank is not None:
+        if entry in _ADAPTER_ENTRIES:                            # (the form of the call is the entry point's, whatever it is given)
             if type(bank) is not AdapterBank or bank.H != self.H or bank.V != self.V or bank.device != self._dev:
                 return None
             return _host.call(_entry[entry], self._ctx.value, self.H, self.V, hidden, W_lm, draft_tok, draft_q, uniforms, tau, out,
@@ -787,6 +788,11 @@ class HolaVerify:
             _check(self.lib, self._ctx, st, "hola_lm_head_entropy")
         return out
 
+    @staticmethod
+    def _check_adapters(bank, ids):
+        if not isinstance(bank, AdapterBank) or not isinstance(ids, torch.Tensor):
+            raise HolaError("adapters must be an AdapterBank and adapter_ids a tensor; hola_lm_head_entropy and hola_verify take the bare head")
+
     def _with_adapters(self, bank: AdapterBank, ids: torch.Tensor, hidden) -> hola_adapters:
         if bank.H != self.H or bank.V != self.V or bank.device != self._dev:
             raise HolaError("the adapter bank must be made for the context's H and V, on its device")
@@ -800,6 +806,7 @@ class HolaVerify:
                               want_logits: bool = True, stream=None, w_scale=None, a8: bool = False) -> VerifyOutputs:
         """hola_lm_head_entropy with low-rank adapters beside the head: adapter_ids int32 [B] names each sequence's slot of the
         bank, -1 the bare head."""
+        self._check_adapters(adapters, adapter_ids)
         fresh = not out
         if fresh:
             B, k1 = hidden.shape[:2]
@@ -822,6 +829,7 @@ class HolaVerify:
                              gate_source: int = HOLA_GATE_TARGET_ENTROPY, fallback: int = HOLA_FALLBACK_SAMPLE, w_scale=None,
                              a8: bool = False) -> VerifyOutputs:
         """hola_verify with low-rank adapters beside the head (see hola_lm_head_adapters)."""
+        self._check_adapters(adapters, adapter_ids)
         fresh = not out
         if fresh:
             B, k1 = hidden.shape[:2]

@@ -461,6 +461,42 @@ def test_refused_by_the_binding():
             ctx.hola_verify_adapters(d["hidden"], d["W"], None, None, None, 1.0, bank, d["ids"])
 
 
+class _NoDevice(binding.HolaVerify):
+    """A context that is never asked for anything on a device."""
+
+    def __init__(self, H, V):
+        self.H, self.V, self.device, self._dev, self._ctx = H, V, 0, torch.device("cpu"), ctypes.c_void_p()
+        self.lib = binding.load_library()
+
+    def close(self):
+        pass
+
+
+@pytest.mark.parametrize("adapters,ids", [(None, True), ("bank", None), ("bank", [0, 1]), ("struct", True), (object(), True), (None, None)])
+def test_what_is_no_bank_is_refused_before_anything_native_is_called(monkeypatch, adapters, ids):
+    """The library's functions for adapters take one argument more than the others: none of them may be called without a bank."""
+    calls = []
+    ctx = _NoDevice(64, 40)
+    monkeypatch.setattr(binding, "_host", type("Host", (), {"call": staticmethod(lambda *a: calls.append(a) or 1),
+                                                            "outputs": staticmethod(lambda *a: calls.append(a))}))
+    bank = binding.AdapterBank.empty(2, 8, 64, 40, "cpu")
+    adapters = {"bank": bank, "struct": bank.struct}.get(adapters, adapters) if isinstance(adapters, str) else adapters
+    ids = torch.zeros(2, dtype=torch.int32) if ids is True else ids
+    hidden, W = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(40, 64, dtype=torch.bfloat16)
+    out = ctx.alloc_outputs(2, 3, device="cpu")
+    q, u, t = torch.zeros(2, 3, 40), torch.zeros(2, 4), torch.zeros(2, 3, dtype=torch.int32)
+    stream = type("Stream", (), {"cuda_stream": 4096})()
+    for o in (out, None):
+        with pytest.raises(binding.HolaError):
+            ctx.hola_lm_head_adapters(hidden, W, adapters, ids, out=o, stream=stream)
+        with pytest.raises(binding.HolaError):
+            ctx.hola_verify_adapters(hidden, W, t, q, u, 1.5, adapters, ids, out=o, stream=stream)
+    assert not calls
+    for entry in ("hola_lm_head_adapters", "hola_verify_adapters"):      # (nor by the short way itself)
+        assert ctx._native(entry, hidden, W, t, q, u, 1.5, out, 1, 0, 0, 0, None, False, stream, None, ids) is None
+    assert not calls
+
+
 @gpu
 def test_decode_loop_with_adapters_and_scores():
     """The driver's loop on adapted heads: log probabilities as the records' logits have them, tokens as a bare loop's without adapters."""

@@ -207,6 +207,24 @@ def _stream_ptr(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
+def _make_on(stream, dev, make):
+    """make(), whose tensors a call fills that was given none: made on the stream that the call was given, since the allocator
+    orders uses of a block on the stream it was made on only.  What the caller's current stream still has to read of them when they
+    are dropped is waited for as well."""
+    if stream is None:
+        return make()
+    if not isinstance(stream, torch.cuda.Stream):                # (whatever has a cuda_stream)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=dev)
+    here = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        made = make()
+    if here != stream:
+        for t in (made.__dict__.values() if hasattr(made, "__dict__") else made):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(here)
+    return made
+
+
 def hola_quantize_w8(W_lm: torch.Tensor, stream=None):
     """8-bit form of a bf16 W_lm [V, H] on the device: returns (q int8 [V, H], scale fp32 [V]).  The integers and the
     scales are computed by the library's kernel; torch only provides the two output buffers."""
@@ -214,8 +232,8 @@ def hola_quantize_w8(W_lm: torch.Tensor, stream=None):
         raise HolaError("hola_quantize_w8 takes a contiguous bfloat16 device tensor")
     lib = load_library()
     V, H = W_lm.shape
-    q = torch.empty((V, H), dtype=torch.int8, device=W_lm.device)
-    scale = torch.empty((V,), dtype=torch.float32, device=W_lm.device)
+    q, scale = _make_on(stream, W_lm.device, lambda: (torch.empty((V, H), dtype=torch.int8, device=W_lm.device),
+                                                      torch.empty((V,), dtype=torch.float32, device=W_lm.device)))
     with torch.cuda.device(W_lm.device):
         _check(lib, None, lib.hola_quantize_w8(_dptr(W_lm), V, H, _dptr(q), _dptr(scale), _stream_ptr(stream)),
                "hola_quantize_w8")
@@ -418,7 +436,8 @@ def hola_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None
     [B], next_tok [B]) of a verify call instead, for logits [B, k + 1, V]: position j holds draft_tok[b, j] up to accept_len[b],
     then next_tok[b], nothing behind.  logZ: fp32 [...] where it is known (a verify call's): entropy and logZ are not made then;
     the emitted form needs it.  Without ranks and alternatives nothing but the tokens' entries is read in that case.
-    status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  out: an earlier call's result of the same form, filled again."""
+    status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  out: an earlier call's result of the same form, filled again.
+    stream: where the call runs, and where its fresh outputs are made (see HolaVerify)."""
     lib = load_library()
     if _host is not None and stream is None and out is None:
         draft_tok, accept_len, next_tok = emitted if emitted is not None else (None, None, None)
@@ -473,10 +492,13 @@ def hola_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None
         setattr(a, name, t.data_ptr() if out is None else check(t, dtype, size, name))
         return t
 
-    got = TokenLogprobs(field("logprob", torch.float32, per_row, some), field("rank", torch.int32, per_row, some and want_rank),
-                        field("entropy", torch.float32, shape, sums), field("logZ", torch.float32, shape, sums),
-                        field("top_ids", torch.int32, (*shape, n_top), n_top > 0),
-                        field("top_logprobs", torch.float32, (*shape, n_top), n_top > 0))
+    def fields():
+        return TokenLogprobs(field("logprob", torch.float32, per_row, some), field("rank", torch.int32, per_row, some and want_rank),
+                             field("entropy", torch.float32, shape, sums), field("logZ", torch.float32, shape, sums),
+                             field("top_ids", torch.int32, (*shape, n_top), n_top > 0),
+                             field("top_logprobs", torch.float32, (*shape, n_top), n_top > 0))
+
+    got = fields() if out is not None else _make_on(stream, dev, fields)
     if status is not None:
         a.status_word = check(status, torch.int32, (1,), "status")
     if a.rows == 0 or not (sums or some or n_top):
@@ -522,10 +544,12 @@ for _name in ("accept_len", "next_tok", "draft_entropy"):
     setattr(VerifyOutputs, _name, _FieldOnDemand(_name))
 
 
-def _fresh_outputs(ctx: "HolaVerify", B: int, k1: int, want_logits: bool, draws: bool, draft_gate: bool) -> VerifyOutputs:
+def _fresh_outputs(ctx: "HolaVerify", B: int, k1: int, want_logits: bool, draws: bool, draft_gate: bool, stream=None) -> VerifyOutputs:
     """Outputs a call makes for itself: only the tensors that it fills are allocated (one allocation costs the host as
     much as a fifth of a call), the others when somebody asks for them.  The status word is cleared by the call
     (HOLA_ARG_CLEAR_STATUS)."""
+    if stream is not None:
+        return _make_on(stream, ctx._dev, lambda: _fresh_outputs(ctx, B, k1, want_logits, draws, draft_gate))
     out = VerifyOutputs.__new__(VerifyOutputs)
     dev = ctx._dev
     out._lazy = (B, k1 - 1, dev)
@@ -546,7 +570,10 @@ def _fresh_outputs(ctx: "HolaVerify", B: int, k1: int, want_logits: bool, draws:
 
 
 class HolaVerify:
-    """Owns one hola_ctx.  Methods are named after the C entry points they call."""
+    """Owns one hola_ctx.  Methods are named after the C entry points they call.
+
+    stream=: the call runs there, in no order with the current stream, which is the caller's to make; outputs that the call makes for
+    itself belong to that stream, and may be read on the current one (behind a wait for the other) and dropped at any time."""
 
     def __init__(self, maxB: int, maxK: int, H: int, V: int, device: int | None = None):
         if not torch.cuda.is_available():
@@ -589,8 +616,7 @@ class HolaVerify:
         """Runs the bounded-wait self-test; returns (status word, threads that reached the end, waits that gave up)
         after synchronising the stream."""
         dev = torch.device("cuda", self.device)
-        status = torch.zeros(1, dtype=torch.int32, device=dev)
-        counters = torch.zeros(2, dtype=torch.int32, device=dev)
+        status, counters = _make_on(stream, dev, lambda: [torch.zeros(n, dtype=torch.int32, device=dev) for n in (1, 2)])
         st = self.lib.hola_selftest_bounded_wait(self._ctx, int(limit_cycles), _dptr(status), _dptr(counters),
                                                  _stream_ptr(stream))
         _check(self.lib, self._ctx, st, "hola_selftest_bounded_wait")
@@ -600,8 +626,7 @@ class HolaVerify:
     def hola_selftest_staged_wait(self, limit_cycles: int = 100000, stream=None) -> tuple[int, int, int, int]:
         """Runs the self-test of the wait on staged rows; returns (status word, threads that reached the end, waits that gave
         up, flags that the other CTA reported) after synchronising the stream."""
-        status = torch.zeros(1, dtype=torch.int32, device=self._dev)
-        counters = torch.zeros(3, dtype=torch.int32, device=self._dev)
+        status, counters = _make_on(stream, self._dev, lambda: [torch.zeros(n, dtype=torch.int32, device=self._dev) for n in (1, 3)])
         st = self.lib.hola_selftest_staged_wait(self._ctx, int(limit_cycles), _dptr(status), _dptr(counters),
                                                 _stream_ptr(stream))
         _check(self.lib, self._ctx, st, "hola_selftest_staged_wait")
@@ -611,8 +636,7 @@ class HolaVerify:
     def hola_selftest_mass_wait(self, limit_cycles: int = 100000, stream=None) -> tuple[int, int, int, int, int]:
         """Runs the self-test of the wait on the other CTAs' sums; returns (status word, threads that reached the end, waits
         that gave up, flags that the first CTA reported, CTAs that all sums had reached) after synchronising the stream."""
-        status = torch.zeros(1, dtype=torch.int32, device=self._dev)
-        counters = torch.zeros(4, dtype=torch.int32, device=self._dev)
+        status, counters = _make_on(stream, self._dev, lambda: [torch.zeros(n, dtype=torch.int32, device=self._dev) for n in (1, 4)])
         st = self.lib.hola_selftest_mass_wait(self._ctx, int(limit_cycles), _dptr(status), _dptr(counters), _stream_ptr(stream))
         _check(self.lib, self._ctx, st, "hola_selftest_mass_wait")
         (torch.cuda.current_stream() if stream is None else stream).synchronize()
@@ -620,7 +644,7 @@ class HolaVerify:
 
     def hola_selftest_pace(self, stream=None) -> torch.Tensor:
         """The pace counters of launches that hold several passes, behind what is queued on the stream: zeros between calls."""
-        words = torch.empty(HOLA_PACE_WORDS, dtype=torch.int32, device=self._dev)
+        words, = _make_on(stream, self._dev, lambda: (torch.empty(HOLA_PACE_WORDS, dtype=torch.int32, device=self._dev),))
         _check(self.lib, self._ctx, self.lib.hola_selftest_pace(self._ctx, _dptr(words), _stream_ptr(stream)), "hola_selftest_pace")
         return words
 
@@ -629,7 +653,7 @@ class HolaVerify:
         for x in (t, s):
             if x.dtype != torch.float32 or x.device != self._dev or not x.is_contiguous() or x.numel() != t.numel():
                 raise HolaError("hola_selftest_quotient takes two contiguous fp32 tensors of one size on the context's device")
-        out = torch.empty_like(t)
+        out, = _make_on(stream, self._dev, lambda: (torch.empty_like(t),))
         st = self.lib.hola_selftest_quotient(self._ctx, _dptr(t), _dptr(s), t.numel(), _dptr(out), _stream_ptr(stream))
         _check(self.lib, self._ctx, st, "hola_selftest_quotient")
         return out
@@ -757,7 +781,7 @@ class HolaVerify:
         fresh = not out
         if fresh:
             B, k1 = hidden.shape[:2]
-            out = _fresh_outputs(self, B, k1, want_logits, True, gate_source == HOLA_GATE_DRAFT_ENTROPY)
+            out = _fresh_outputs(self, B, k1, want_logits, True, gate_source == HOLA_GATE_DRAFT_ENTROPY, stream)
         st = self._native("hola_verify", hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, 1,
                           HOLA_ARG_CLEAR_STATUS if fresh else 0, gate_source, fallback, w_scale, a8, stream)
         if st is None:
@@ -775,7 +799,7 @@ class HolaVerify:
         fresh = not out
         if fresh:
             B, k1 = hidden.shape[:2]
-            out = _fresh_outputs(self, B, k1, want_logits, False, False)
+            out = _fresh_outputs(self, B, k1, want_logits, False, False, stream)
         st = self._native("hola_lm_head_entropy", hidden, W_lm, None, None, None, 0.0, out, 0,
                           HOLA_ARG_CLEAR_STATUS if fresh else 0, 0, 0, w_scale, a8, stream)
         if st is None:
@@ -810,7 +834,7 @@ class HolaVerify:
         fresh = not out
         if fresh:
             B, k1 = hidden.shape[:2]
-            out = _fresh_outputs(self, B, k1, want_logits, False, False)
+            out = _fresh_outputs(self, B, k1, want_logits, False, False, stream)
         st = self._native("hola_lm_head_adapters", hidden, W_lm, None, None, None, 0.0, out, 0, HOLA_ARG_CLEAR_STATUS if fresh else 0, 0,
                           0, w_scale, a8, stream, adapters, adapter_ids)
         if st is None:
@@ -833,7 +857,7 @@ class HolaVerify:
         fresh = not out
         if fresh:
             B, k1 = hidden.shape[:2]
-            out = _fresh_outputs(self, B, k1, want_logits, True, gate_source == HOLA_GATE_DRAFT_ENTROPY)
+            out = _fresh_outputs(self, B, k1, want_logits, True, gate_source == HOLA_GATE_DRAFT_ENTROPY, stream)
         st = self._native("hola_verify_adapters", hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, 1,
                           HOLA_ARG_CLEAR_STATUS if fresh else 0, gate_source, fallback, w_scale, a8, stream, adapters, adapter_ids)
         if st is None:
@@ -850,10 +874,15 @@ class HolaVerify:
     def hola_accept_sample(self, logits, entropy, logZ, draft_tok, draft_q, uniforms, tau, stream=None) -> VerifyOutputs:
         """Steps 3-5 from given fp32 logits [B, k+1, V] and their entropy / logZ."""
         B, k = logits.shape[0], logits.shape[1] - 1
-        out = self.alloc_outputs(B, k, False)
+
+        def made():
+            out = self.alloc_outputs(B, k, False)
+            out.entropy.copy_(entropy)
+            out.logZ.copy_(logZ)
+            return out
+
+        out = _make_on(stream, self._dev, made)
         out.logits = logits
-        out.entropy.copy_(entropy)
-        out.logZ.copy_(logZ)
         a = hola_verify_args()
         a.B, a.k, a.H, a.V = B, k, self.H, self.V
         a.draft_tok = _dptr(draft_tok) if k > 0 else None

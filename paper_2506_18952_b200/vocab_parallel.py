@@ -94,16 +94,18 @@ class ShardedHolaVerify:
         B, k = hidden.shape[0], hidden.shape[1] - 1
         if W_lm.shape[0] != self.V_local or (k > 0 and draft_q.shape[-1] != self.V_local):
             raise binding.HolaError("W_lm and draft_q must be this rank's vocabulary range")
-        out = out or self.ctx.alloc_outputs(B, k, False)
+        dev = hidden.device
+        out = out or binding._make_on(stream, dev, lambda: self.ctx.alloc_outputs(B, k, False))
         a = self.ctx._args(hidden, W_lm, draft_tok, draft_q, uniforms, tau, out, B, k,
                            binding.HOLA_GATE_TARGET_ENTROPY, fallback, w_scale, a8)
         sh = binding.hola_shard_args()
         sh.world, sh.rank, sh.v_offset, sh.V_global = self.world, self.rank, self.v_offset, self.V_global
-        qt = q_tok.to(torch.float32).contiguous() if k > 0 else None
+        qt, record, mass = binding._make_on(stream, dev, lambda: (
+            q_tok.to(torch.float32).contiguous() if k > 0 else None,
+            torch.empty(int(self.ctx.lib.hola_shard_record_bytes(B, k)), dtype=torch.uint8, device=dev),
+            torch.zeros((B, 2), dtype=torch.float64, device=dev)))
         sh.q_tok = binding._dptr(qt)
-        record = torch.empty(int(self.ctx.lib.hola_shard_record_bytes(B, k)), dtype=torch.uint8, device=hidden.device)
         sh.record_out = binding._dptr(record)
-        mass = torch.zeros((B, 2), dtype=torch.float64, device=hidden.device)
         sh.mass_out = binding._dptr(mass)
         self.ctx.hola_shard_call("hola_shard_lm_head", a, sh, stream)
         # the argument structs point into these tensors: keep them until the step is over

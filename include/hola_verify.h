@@ -289,7 +289,8 @@ hola_status hola_lm_head_entropy_static(const hola_verify_args* args, void* cuda
  * the requests of many fine-tunes):  for a sequence that uses adapter a, position by position,
  *   l[r][v] = sum_h W[v][h] x[r][h] + sum_i B[a][v][i] u[r][i],   u[r][i] = scale[a] * sum_h A[a][i][h] x[r][h],   i < rank,
  * and entropy, logZ and everything behind are those of these logits.  W_lm in any of its storage forms; A, B and x are bf16, u and the
- * logits fp32.  An adapter of a lower rank is filled up with zeros.
+ * logits fp32.  An adapter of a lower rank is filled up with zeros.  An infinite factor counts as the formula has it: an entry of -inf
+ * has probability 0, and a row with NaN or +inf has no distribution (logZ NaN); the rows of other sequences are not touched by it.
  * hola_lm_head_adapters is hola_lm_head_entropy, hola_verify_adapters is hola_verify, with the same arguments, checks, streams and
  * outputs; the arrays of `adapters` (a host struct, not looked at after the call) are resident on the device. */
 typedef struct hola_adapters {

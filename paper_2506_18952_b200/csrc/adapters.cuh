@@ -9,7 +9,9 @@
 //       rows' softmax statistics anew, in the form in which the GEMM's epilogue leaves them (partials of each row), so that
 //       everything behind reads them as before.  Rows without an adapter are left alone.
 // Both products run on bf16 operands with fp32 accumulation; u, which is fp32, enters the second one as three bf16 planes that
-// add up to it exactly (8 significant bits each), so that no rounding is added to what an fp32 product would have.
+// add up to it exactly (8 significant bits each), so that no rounding is added to what an fp32 product would have.  That holds for
+// finite factors; where one is not (an entry of B masks with -inf, say), a zero in one plane or planes of opposite signs make NaN of a
+// product that is infinite: entries that come out as NaN are taken again as fp32 products.
 //
 // (Why not inside the GEMM, as further K blocks [B_0 B_1 ...] against rows that are zero but for their own slot's columns: a number
 // that is not finite in one slot would reach the rows of every other request as 0 * inf, and each block costs all rows' MMAs.)
@@ -221,6 +223,13 @@ struct RowStats {
       t2 = fma2(e, x, t2);
     }
   }
+  // Entries of -inf, which the sums are not kept clear of in whole steps, have made NaN (0 * -inf) of t.
+  __device__ __forceinline__ bool lost() const {
+    float a, b, c, d;
+    unpack2(s2, a, b);
+    unpack2(t2, c, d);
+    return a + b > 0.f && a + b < CUDART_INF_F && c + d != c + d;
+  }
   __device__ __forceinline__ Stats stats() const {
     float a, b, c, d;
     unpack2(s2, a, b);
@@ -232,6 +241,14 @@ struct RowStats {
     return Stats{m, s * e, kLn2 * (e * fmaf(-x, s, c + d)), arg};
   }
 };
+
+// One entry of the second product, rank by rank; b: the entry's row of B.
+__device__ __noinline__ float adapter_product(const uint16_t* b, const float* u, int rank) {
+  float s = 0.f;
+#pragma unroll 1
+  for (int i = 0; i < rank && s == s; ++i) s = fmaf(__uint_as_float(static_cast<uint32_t>(b[i]) << 16), u[i], s);
+  return s;
+}
 
 // A warp step covers 64 vocabulary entries, the M of four MMAs, and the tile's eight rows, their N.  Lane (g, q) holds entries g, 8 + g,
 // 16 + g ... of rows 2 q and 2 q + 1.  Rows of the logits that start on 16-byte boundaries (kVec) are loaded and stored 16 bytes a lane,
@@ -416,9 +433,26 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kAdUpCtas) adapter_up_kernel(
           for (int e = 0; e < 8; ++e)
             if (vg + 8 * e >= p.V) l[h][e] = -CUDART_INF_F;
         }
-        top[h] = fmaxf(max3(max3(l[h][0], l[h][1], l[h][2]), max3(l[h][3], l[h][4], l[h][5]), l[h][6]), l[h][7]);
+        top[h] = max3_nan(max3_nan(max3_nan(l[h][0], l[h][1], l[h][2]), max3_nan(l[h][3], l[h][4], l[h][5]), l[h][6]), l[h][7], l[h][7]);
       }
-      if (__any_sync(0xffffffffu, p.want_arg || top[0] > st[0].rise() || top[1] > st[1].rise())) {
+      if (__any_sync(0xffffffffu, p.want_arg || !(top[0] <= st[0].rise()) || !(top[1] <= st[1].rise()))) {
+        if (top[0] != top[0] || top[1] != top[1]) {
+          unsigned which = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) which |= l[i >> 3][i & 7] != l[i >> 3][i & 7] && have[i >> 3] ? 1u << i : 0u;
+#pragma unroll 1
+          for (; which; which &= which - 1u) {
+            const int at_i = __ffs(which) - 1, h = at_i >> 3, e = at_i & 7;
+            float x = (h ? at[1] : at[0])[v0 + 8 * e - (kVec ? 3 * g : 0)];
+            if (x == x) x += adapter_product(row(c, e), p.u + static_cast<size_t>(tile.row[2 * q + h]) * kAdMaxRank, rank);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (i == at_i) l[i >> 3][i & 7] = x;
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h)                    // (the largest of those that are numbers)
+            top[h] = fmaxf(max3(max3(l[h][0], l[h][1], l[h][2]), max3(l[h][3], l[h][4], l[h][5]), l[h][6]), l[h][7]);
+        }
         st[0].rises(l[0], top[0], p.want_arg, [&](int e) { return vg + 8 * e; });
         st[1].rises(l[1], top[1], p.want_arg, [&](int e) { return vg + 8 * e; });
       }
@@ -449,6 +483,28 @@ __global__ void __launch_bounds__(kAdUpWarps * 32, kAdUpCtas) adapter_up_kernel(
           for (int e = 0; e < 8; ++e)
             if (have[h] && (whole || vg + 8 * e < p.V)) at[h][v0 + 8 * e - (kVec ? 3 * g : 0)] = l[h][e];
       }
+    }
+    // (rows with entries of -inf: the sums once more, clear of them, from what has been stored)
+    if (__any_sync(0xffffffffu, st[0].lost() || st[1].lost())) {
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!st[h].lost() || !have[h]) continue;
+        st[h].clear();
+#pragma unroll 1
+        for (int c = c_begin; c < c_end; c += kAdUpWarps) {
+          const int vg = c * kAdChunk + g;
+          float l[8], top = -CUDART_INF_F;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            l[e] = vg + 8 * e < p.V ? at[h][vg + 8 * e - (kVec ? 4 * g : g)] : -CUDART_INF_F;
+            top = fmaxf(top, l[e]);
+          }
+          st[h].rises(l, top, p.want_arg, [&](int e) { return vg + 8 * e; });
+          st[h].template add<true>(l, top);
+        }
+      }
+      __syncwarp();
     }
     // a row's statistics over the eight lanes that hold it, then over the warps
 #pragma unroll

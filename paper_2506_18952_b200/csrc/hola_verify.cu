@@ -657,6 +657,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {     // NaN where one of them is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 
 // stats_fold16<true> with half the issue slots: the maximum by three-input comparisons, the exponents' arguments
 // x = (l - m) log2 e, the sum of the exponentials and the sum of e * x two at a time.  The centred sum is ln 2 times the

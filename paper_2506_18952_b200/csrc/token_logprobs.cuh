@@ -111,11 +111,6 @@ __device__ __forceinline__ uint64_t lp_merge_warps(uint64_t a, uint64_t* lists, 
   return a;
 }
 
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {     // NaN where one of them is
-  float d;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ float lp_float(float x) { return x; }
 __device__ __forceinline__ float lp_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float lp_float(__half x) { return __half2float(x); }

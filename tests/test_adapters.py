@@ -247,6 +247,56 @@ def test_what_is_not_finite_stays_in_its_requests():
 
 
 @gpu
+@pytest.mark.parametrize("V", [2052, 2051, 9000])
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 64, 104])
+def test_infinite_factors(rank, V):
+    """An infinite factor makes of its entries what the formula says: infinities (-inf: an entry of probability 0) or, with a factor of
+    zero or another infinity, NaN.  The other entries are bounded as everywhere: the product's own bound and one addition in fp32."""
+    B, k, H, inf = 12, 2, 128, float("inf")
+    d = make(B, k, H, V, 6, rank, seed=rank + V)
+    d["ids"].copy_(torch.tensor([0, 1, 2, 3, 4, -1, 0, 1, 2, 5, 5, 0]))
+    d["hidden"][:, :, 0] = 1.0
+    for s in (0, 5):                                          # u[0] is positive: masks
+        d["A"][s, 0], d["A"][s, 0, 0] = 0.0, 1.0
+    d["Bup"][0, 5::3, 0] = -inf
+    d["Bup"][5, : V - 7, rank - 1 if rank > 8 else 0] = -inf  # (of either sign where the rank is not u[0])
+    d["Bup"][5, V - 3, 0] = -inf
+    d["Bup"][1, 7, 2], d["Bup"][1, V - 1, 3] = inf, -inf
+    d["Bup"][2, 11, 1], d["Bup"][2, 11, 5], d["Bup"][2, 64:80, 4] = inf, -inf, -inf
+    d["A"][3, 1] = 0.0                                        # u[1] is zero
+    d["Bup"][3, 300, 1] = -inf
+    d["A"][4, 0, 0] = inf                                     # u[0] is infinite
+    d["Bup"][4, 100, 0] = 0.0
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        base = ctx.hola_lm_head_entropy(d["hidden"], d["W"])
+        out = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"])
+        one = [t[:, :1].contiguous() for t in (d["hidden"], torch.rand((B, 1), device="cuda"))]
+        greedy = ctx.hola_verify_adapters(one[0], d["W"], None, None, one[1], 1.5, bank, d["ids"], want_logits=True, fallback=1)
+        for f in ("logits", "logZ", "entropy"):
+            assert torch.equal(getattr(out, f)[5], getattr(base, f)[5])
+    delta, bound = delta64(d)
+    want = base.logits.double() + delta
+    fine = want.isfinite()
+    got = out.logits.double()
+    assert torch.equal(got.isfinite(), fine) and torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got[want.isinf()], want[want.isinf()])
+    assert ((got - want).abs() <= bound + 2 * U * (base.logits.double().abs() + want.abs()))[fine].all()
+    # rows without NaN and +inf have a distribution
+    row = (got < inf).all(dim=-1)
+    assert row[[0, 5, 6, 11]].all() and not row[4].any()
+    assert out.logZ[~row].isnan().all()
+    m = got[row].amax(dim=-1, keepdim=True)
+    ln_s = (got[row] - m).exp().sum(dim=-1).log()
+    lp = got[row] - m - ln_s[:, None]
+    want_H = -torch.where(lp > -inf, lp.exp() * lp, 0.0).sum(dim=-1)
+    E = (V / 1000 + 40) * U + 2.0 ** -22 + 4 * U * float(got[row].abs().nan_to_num(posinf=0.0).max())
+    assert ((out.logZ[row].double() - m[:, 0] - ln_s).abs() <= E + 2 * U * m[:, 0].abs()).all()
+    assert ((out.entropy[row].double() - want_H).abs() <= E * (1 + 3 * np.log(V + 1)) + 4 * U * np.log(V + 1)).all()
+    assert torch.equal(greedy.next_tok[row[:, 0]].long(), greedy.logits[row[:, 0], 0].argmax(dim=-1))
+
+
+@gpu
 def test_an_empty_batch():
     bank = binding.AdapterBank.empty(2, 8, 64, 500, "cuda")
     with binding.HolaVerify(2, 1, 64, 500) as ctx:

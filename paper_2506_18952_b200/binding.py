@@ -451,6 +451,8 @@ def hola_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None
         raise HolaError("hola_token_logprobs takes fp32, bf16 or fp16 logits on a device")
     shape, dev = logits.shape[:-1], logits.device
     a = hola_logprobs_args()
+    if max(shape.numel(), logits.shape[-1], 0 if tokens is None or tokens.dim() == 0 else tokens.shape[-1]) > 2 ** 31 - 1:
+        raise HolaError("hola_token_logprobs: more rows, entries or tokens per row than 32 bits count")       # (ctypes would cut them off)
     a.rows, a.V, a.n_top = shape.numel(), logits.shape[-1], n_top
     a.logits, a.row_stride, a.l_dtype = logits.data_ptr(), _row_stride(logits), _L_DTYPES[logits.dtype]
 

@@ -353,6 +353,17 @@ def test_offsets_beyond_32_bits():
 
 
 @gpu
+def test_counts_beyond_32_bits_are_refused():
+    """(2^32 + 4 rows or entries are not 4.)"""
+    many = 2 ** 32 + 4
+    for l, t in ((torch.zeros((1, 9), device="cuda").expand(many, 9), torch.zeros(1, dtype=torch.int32, device="cuda").expand(many)),
+                 (torch.zeros(many, dtype=torch.bfloat16, device="cuda"), torch.zeros((), dtype=torch.int32, device="cuda")),
+                 (torch.zeros((2 ** 31, 1), dtype=torch.bfloat16, device="cuda"), None)):
+        with pytest.raises(binding.HolaError, match="32 bits"):
+            binding.hola_token_logprobs(l, t)
+
+
+@gpu
 def test_nothing_outside_the_outputs_is_written():
     rows, V, n = 9, 3001, 5
     l = make(rows, V, torch.float32, 5)

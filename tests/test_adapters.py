@@ -103,6 +103,64 @@ def test_logits_and_statistics(B, k, H, V, slots, rank):
 
 
 @gpu
+@pytest.mark.parametrize("B,k,H,V,slots,rank", [(23, 3, 128, 5003, 8, 24), (17, 2, 256, 9000, 64, 16), (12, 5, 64, 3004, 5, 64), (9, 5, 128, 4099, 3, 128),
+                                                (6, 2, 64, 2001, 4, 8), (12, 5, 256, 3003, 5, 32)])
+def test_logits_within_the_two_products_own_bounds(B, k, H, V, slots, rank):
+    """The second product is made apart from the head's and added once, in fp32: what bounds a logit's error are the steps of its own
+    sequence's two products (delta64's, but for u, which enters with all its bits) and that addition, however many slots there are."""
+    d = make(B, k, H, V, slots, rank, seed=B + V + 1)
+    bank = binding.AdapterBank(d["A"], d["Bup"], d["scale"])
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        base = ctx.hola_lm_head_entropy(d["hidden"], d["W"], want_logits=True).logits.double()
+        got = ctx.hola_lm_head_adapters(d["hidden"], d["W"], bank, d["ids"]).logits.double()
+    delta, _ = delta64(d)
+    for b in range(B):
+        a = int(d["ids"][b])
+        if a < 0:
+            continue
+        x, A, Bu, s = d["hidden"][b].double(), d["A"][a].double(), d["Bup"][a].double(), d["scale"][a].double()
+        u, u_abs = s * (x @ A.T), s * (x.abs() @ A.abs().T)
+        e_u = u_abs * (-(-H // 16) * 2.0 ** -22 + 17 * U) + u.abs() * U
+        tol = e_u @ Bu.abs().T + (u.abs() @ Bu.abs().T) * (3 * -(-rank // 16) + 3) * 2.0 ** -22 + U * (base[b] + delta[b]).abs()
+        assert ((got[b] - base[b] - delta[b]).abs() <= tol).all()
+
+
+@gpu
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 64, 128])
+@pytest.mark.parametrize("V", [1000, 1003])
+def test_u_enters_the_second_product_with_all_its_bits(rank, V):
+    """u = scale exactly (one channel of x and of A is 1, the others 0), every entry of the vocabulary has one rank, with a power of two,
+    and W = 0: a logit is that power times a number of 24 bits.  The tensor cores add the planes smallest first and cut a sum off at the
+    larger operand's last place.  Where the largest plane lies below the next power of two above u that is u's own last place and
+    nothing is lost; where u rounds up to that power (u from 2 - 2^-8 on, say), less than 2^-22 beside 2 is: 2^-23 of u and a little.
+    (Without the third plane up to 2^-17 would be.)"""
+    n = 48
+    g = torch.Generator(device="cuda").manual_seed(rank)
+    scale = 1 + torch.randint(0, 2 ** 23, (n,), generator=g, device="cuda").float() * 2.0 ** -23           # (exact)
+    scale[:6] = torch.tensor([2 - 2.0 ** -23, 1 + 2.0 ** -23, 1 + 2.0 ** -8 + 2.0 ** -23, 2 - 2.0 ** -8 - 2.0 ** -23, 1 + 2.0 ** -9 + 2.0 ** -17 + 2.0 ** -23,
+                              2 - 2.0 ** -16 - 2.0 ** -23])
+    scale[::3] *= -1
+    scale[1::4] *= 2.0 ** -20
+    hidden = torch.zeros((n, 1, 64), dtype=torch.bfloat16, device="cuda")
+    hidden[:, :, 0] = 1.0
+    A = torch.zeros((n, rank, 64), dtype=torch.bfloat16, device="cuda")
+    A[:, :, 0] = 1.0
+    at = torch.arange(V, device="cuda")
+    power = 2.0 ** ((at % 7) - 3).float() * (1 - 2 * (at // 7 % 2)).float()
+    Bup = torch.zeros((n, V, rank), dtype=torch.bfloat16, device="cuda")
+    Bup[:, at, at % rank] = power.bfloat16()
+    with binding.HolaVerify(n, 0, 64, V) as ctx:
+        W = torch.zeros((V, 64), dtype=torch.bfloat16, device="cuda")
+        out = ctx.hola_lm_head_adapters(hidden, W, binding.AdapterBank(A, Bup, scale), torch.arange(n, dtype=torch.int32, device="cuda"))
+    want = scale.double()[:, None] * power.double()
+    up = (scale.abs().bfloat16().float() >= 2.0 ** (scale.abs().log2().floor() + 1))[:, None]              # (u rounds up to a power of two)
+    assert up.any() and not up.all()
+    err = (out.logits[:, 0].double() - want).abs()
+    assert (err[~up.expand_as(err)] == 0).all()
+    assert (err <= 2.0 ** -23 * (1 + 2.0 ** -7) * want.abs()).all()
+
+
+@gpu
 @pytest.mark.parametrize("V", [1000, 9003])
 def test_statistics_of_logits_far_from_zero(V):
     """A logit's distance to the maximum counts, not where the maximum is.  Sums of differences, which are rounded once: relative to

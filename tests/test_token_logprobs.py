@@ -177,6 +177,40 @@ def test_masks_of_any_depth_and_logits_of_any_size(dtype, V):
 
 @gpu
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [40, 3000, 70001])
+def test_entries_beside_masks_of_any_depth_keep_their_precision(dtype, V):
+    """How deep a mask is puts nothing on the entries beside it.  A log probability is (l - m) - ln s: ln s is off by s's relative error E,
+    by 2^-22 for each exponential that a thread's sums pass through afterwards (to its own maximum, the warp's, the CTA's, the row's) and
+    by logf's 2 x 2^-24 of itself (<= ln V); two more roundings are relative to the result, which is no smaller than either operand
+    but for ln s.  logZ = m + ln s: one rounding of the result."""
+    U = 2.0 ** -24
+    sizes = [0.0, 1e4, 4e5, 1e7, 1e9, 1e20, 1e38, torch.finfo(torch.float32).max, math.inf]
+    if dtype == torch.float16:
+        sizes = [0.0, 300.0, 1e4, 65504.0, math.inf]
+    l = make(4 * len(sizes), V, dtype, V + 1)
+    for i, big in enumerate(sizes):
+        big = min(big, torch.finfo(dtype).max) if big < math.inf else big
+        if big:
+            l[4 * i, 1::2] = -big
+            l[4 * i + 1, V // 3:] = -big
+            l[4 * i + 2, torch.arange(V, device="cuda") % 16 != 5] = -big          # one entry in a group or two
+            l[4 * i + 3, :V - 3] = -big                                            # three entries left
+    t = some_tokens(l, 3, 4)
+    out, ref = binding.hola_token_logprobs(l, t, n_top=min(20, V)), reference(l, t, min(20, V))
+    ln_V = math.log(V + 1)
+    E = slack(l, V)[0] + 4 * 2.0 ** -22 + 2 * U * ln_V
+    big = torch.finfo(torch.float32).max
+    for name in ("logZ", "logprob", "top_logprobs"):
+        got, want = getattr(out, name).double().cpu().reshape(ref[name].shape), ref[name]
+        want = torch.where(want < -big, -math.inf, want)
+        fine = want.isfinite()
+        assert torch.equal(got[~fine], want[~fine])
+        assert ((got - want).abs() <= E + (1 if name == "logZ" else 2) * U * (want.abs() + ln_V))[fine].all(), name
+    assert torch.equal(out.rank.cpu().long(), ref["rank"]) and torch.equal(out.top_ids.cpu().long(), ref["top_ids"])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("V", [62, 3001, 70001])
 @pytest.mark.parametrize("kept", [1.0, 0.99, 0.5])
 def test_masked_entries_among_logits_far_from_zero(dtype, V, kept):

@@ -62,8 +62,9 @@ __device__ __forceinline__ int adapter_of(const AdapterParams& p, int b) {
 }
 
 // The batch's rows by adapter, in tiles of eight, by one CTA.  Sequences with the same adapter keep their order; a sequence finds its
-// place by looking at all others (B^2 comparisons: 256 sequences take as long as the loads of the other CTAs).  Beyond kAdMaxSorted
-// sequences every one has tiles of its own.
+// place by looking at all others: B^2 comparisons, which up to some 100 sequences are hidden behind the loads of the other CTAs and
+// beyond are what the kernel takes (us, H = 1024, two rows each: 64 sequences 5.3, 256 16, 512 42, 1024 140, 2048 516).  Beyond
+// kAdMaxSorted sequences every one has tiles of its own (2049: 48).
 __device__ __forceinline__ void adapter_tiles(const AdapterParams& p) {
   __shared__ int ids[kAdMaxSorted], users[kAdMaxSorted];
   const int tid = threadIdx.x, nthr = blockDim.x, k1 = p.rows_per_seq, B = p.B;
@@ -264,10 +265,12 @@ __device__ __forceinline__ int adapter_rank(int k, int q) {      // first of the
 }
 constexpr int kAdPitch = kAdChunk + 4;                           // (floats from row to row: no two rows of a step on the same banks)
 
-// What bounds it: memory.  64 adapters of rank 16, 384 rows, V = 128256: 262 MB of B and the logits in and out, 197 MB each, 132 us from
-// the first CTA's start to the last one's end, 5.0 TB/s; 48 tiles of 16 adapters, V = 32000 26 us (18 of them the steps, 87 MB at
-// 4.9 TB/s out of the L2, the rest start and end); 16 adapters of rank 32 for 28 rows, V = 128256 35 us, 4.6 TB/s.  Without the stores
-// 5 us less of 26, without the sums 1, without two of the three planes 1.
+// What bounds it: at V = 128256 memory, short of its limit.  64 adapters of rank 16, 384 rows: 262 MB of B and the logits in and out,
+// 197 MB each, 132 us from the first CTA's start to the last one's end, 5.0 TB/s; 16 adapters of rank 32 for 28 rows 35 us, 4.6 TB/s.
+// At V = 32000 the latency of a warp's step, load -> shared memory -> MMA -> sums -> shared memory -> store with one step asked for ahead:
+// 48 tiles of 16 adapters 26 us, 18 of them the steps (87 MB at 4.9 TB/s out of the L2, with 24 % of the warps, 34 % of the issue slots
+// and 21 % of DRAM's rate in use under a profiler), the rest start and end.  Without the stores 5 us less of 26, without the sums 1,
+// without two of the three planes 1.
 constexpr int kAdUpCtas = 4;                                     // per SM, by registers
 template <bool kVec, int kR>
 __global__ void __launch_bounds__(kAdUpWarps * 32, kAdUpCtas) adapter_up_kernel(const AdapterParams p) {

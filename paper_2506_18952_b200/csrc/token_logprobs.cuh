@@ -886,7 +886,8 @@ __global__ void __launch_bounds__(128) gather_logprobs_kernel(const LpParams p) 
 // CTAs per row: up to three on an SM, as long as a thread keeps a group or two of its own.  Start, merges and the second look are
 // latency, some 4 us a CTA, which more CTAs only add to, and a second wave for a few of them costs as much as the first.  us with 1 /
 // 2 / 4 / 8: 69 x 50003 fp16 18.3 / 14.8 / 15.4 / 23.0; 192 x 32000 bf16 13.7 / 12.7 / 18.4 / 30.3; 384 x 128256 fp32 42.5 / 49.5 /
-// 63.2 / 99.9; 5 x 32000 fp32 9.5 / 7.8 / 6.7 / 7.0.
+// 63.2 / 99.9; 5 x 32000 fp32 9.5 / 7.8 / 6.7 / 7.0.  The rule takes the best of them for the second and third, one doubling too many
+// for the first and the last (four and eight: 4 % above the best).  Rows of the emitted form that return at once count like the others.
 int lp_cluster(int num_sms, int rows, int V) {
   int C = 1;
   while (C < kLpMaxCluster && 2ll * rows * C <= 3ll * num_sms && V / (2 * C) >= 8 * kLpThreads) C <<= 1;

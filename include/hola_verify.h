@@ -108,7 +108,8 @@ typedef struct hola_wmix {
 #define HOLA_FLAG_TIMEOUT 4u     /* an on-chip wait ran out of iterations; outputs of this call are invalid  */
 #define HOLA_FLAG_R_ZERO 8u      /* residual mass was zero (p <= q everywhere): token drawn from p instead   */
 #define HOLA_FLAG_BAD_ADAPTER 16u /* an adapter index outside [-1,slots): that sequence gets the bare head         */
-#define HOLA_FLAG_BAD_LOGIT 32u  /* hola_token_logprobs: a row of logits holds NaN or +inf                     */
+#define HOLA_FLAG_BAD_LOGIT 32u  /* hola_token_logprobs, hola_beam_select: a row of logits holds NaN or +inf   */
+#define HOLA_FLAG_BAD_BEAM 64u   /* hola_beam_reorder: a parent outside [-1,W): that beam is left as it was       */
 
 /* Bits of hola_verify_args::flags. */
 #define HOLA_ARG_CLEAR_STATUS 1 /* the call stores 0 to status_word before it OR-s anything in, so the caller need not  */
@@ -345,6 +346,134 @@ typedef struct hola_logprobs_args {
   uint32_t* status_word;    /* in/out [1], optional: HOLA_FLAG_* bits are OR-ed in                        */
 } hola_logprobs_args;
 hola_status hola_token_logprobs(const hola_logprobs_args* args, void* cuda_stream);
+
+/* One step of a beam search: the best continuations over all beams and the vocabulary.  The paper decodes by draft and verification;
+ * this is the other search that a server runs on the same LM head (hola_lm_head_entropy with the W beams of a sequence in the place
+ * of its k + 1 positions leaves the logits and logZ that are read here).  For beam w of a sequence and token v
+ *   c(w, v) = (score[w] - logZ[w]) + l[w][v],   key = c * weight[w],   both evaluated in 64 bits,
+ * and the first n candidates in the order (key descending, beam ascending, logit descending, id ascending) are written: c rounded to fp32,
+ * w, v.  An ended beam (finished[w] != 0) has one candidate, end_token with c = score[w]; its logits are not read.  A score of -inf is no beam, an
+ * entry of -inf no candidate.  Where fewer than n candidates are left: score -inf, parent and token -1.  A row that holds NaN or +inf,
+ * a score or logZ that is NaN or +inf, or a weight that is not positive and finite: that beam has no candidates, and HOLA_FLAG_BAD_LOGIT is set.
+ * keep_slots (n = W): instead of by rank, the best child of a beam is written at that beam's own place, so that its state need not
+ * move; the other candidates take the free places in their order.
+ * finished_out: 1 where the parent had ended or the token is end_token.
+ * Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing, needs no context,
+ * and launched like hola_verify (programmatic stream serialization, waits before it reads). */
+#define HOLA_MAX_BEAMS 32
+typedef struct hola_beam_args {
+  int32_t B;                /* sequences, >= 0                                                            */
+  int32_t W;                /* beams of a sequence, 1 .. 32                                               */
+  int32_t V;                /* entries per row, 1 .. 2^27                                                 */
+  int32_t n;                /* candidates that are kept, 1 .. 32                                          */
+  const void* logits;       /* row (b, w) starts at entry b * seq_stride + w * beam_stride; any alignment of the element type */
+  int64_t seq_stride;       /* entries, >= 0                                                              */
+  int64_t beam_stride;      /* entries, >= 0                                                              */
+  int32_t l_dtype;          /* hola_l_dtype                                                               */
+  int32_t end_token;        /* -1: none                                                                   */
+  const float* logZ;        /* [B][W]                                                                     */
+  const float* score;       /* [B][W] log probabilities of the beams so far                               */
+  const uint8_t* finished;  /* [B][W], optional (needs end_token)                                         */
+  const float* weight;      /* [B][W], optional (1): for keys normalised by length, say                   */
+  int32_t keep_slots;
+  int32_t reserved_;
+  float* score_out;         /* out [B][n]                                                                 */
+  int32_t* parent;          /* out [B][n]                                                                 */
+  int32_t* token;           /* out [B][n]                                                                 */
+  uint8_t* finished_out;    /* out [B][n], optional                                                       */
+  uint32_t* status_word;    /* in/out [1], optional: HOLA_FLAG_* bits are OR-ed in                        */
+} hola_beam_args;
+hola_status hola_beam_select(const hola_beam_args* args, void* cuda_stream);
+
+/* The beams' states in the order of their parents: new[b][i] = old[b][parent[b][i]] for i < n, for any number of states at once
+ * (token histories, keys and values, page tables).  parent -1: that place is left as it was.  In place (src = dst, for all states or
+ * none) any order of the parents is allowed, and beams that stay where they are cost nothing.  From one buffer into another (which may not overlap) every
+ * place is written.  A run is what lies side by side of one beam, for one index of the outer axes; with `used`, states whose `position`
+ * is not 0 are moved up to used[b] positions only (at most the run; negative counts as 0), and the bytes behind are left as they were.
+ * Beams may not share bytes (beam_stride >= run), nor may sequences or outer indices.  `states` is a host array, not looked at after the call; its pointers, parent
+ * and used are DEVICE pointers of the current device.  One launch for every 24 states.  Asynchronous on cuda_stream, allocates nothing, launched like hola_verify. */
+typedef struct hola_beam_state {
+  const void* src;
+  void* dst;
+  int64_t seq_stride, beam_stride;   /* of src, bytes                                                     */
+  int64_t outer_stride[2];
+  int64_t dst_seq_stride, dst_beam_stride;   /* of dst (in place: the same)                                */
+  int64_t dst_outer_stride[2];
+  int64_t outer[2];                  /* sizes of the outer axes (1 where there is none)                   */
+  int64_t run;                       /* bytes                                                             */
+  int64_t position;                  /* bytes of a position inside the run, 0: the run is moved whole     */
+} hola_beam_state;
+typedef struct hola_reorder_args {
+  int32_t B, W, n;                   /* n: beams behind the step (in place: at most W)                    */
+  int32_t count;                     /* states                                                            */
+  const hola_beam_state* states;     /* HOST pointer                                                      */
+  const int32_t* parent;             /* [b * parent_stride + i], -1 .. W - 1                               */
+  int64_t parent_stride;
+  const int32_t* used;               /* [B], optional                                                     */
+  uint32_t* status_word;             /* in/out [1], optional                                              */
+} hola_reorder_args;
+hola_status hola_beam_reorder(const hola_reorder_args* args, void* cuda_stream);
+
+/* Rows of a table by token:  out[r] = add[r] + scale * W[tokens[r]],  the table in any storage form of the LM head (tied weights) or
+ * fp32 / fp16.  Every operation is one rounding in fp32 (for the quantised forms w_scale * code first), the result is rounded once more where out is 16 bits wide.
+ * A token of -1 is none: out[r] = add[r], or 0.  Any other token outside the vocabulary: the same, and HOLA_FLAG_BAD_TOKEN.  Of a
+ * vocabulary that is split over several tables this is one part: rows v_offset .. v_offset + V - 1 of V_global (0: V, the whole); tokens of
+ * the other parts count as none, so that the parts' results add up.
+ * Every pointer but wmix is a DEVICE pointer of the current device, rows at any distance.  add may be out.  Asynchronous on cuda_stream,
+ * allocates nothing, needs no context, launched like hola_verify. */
+typedef enum { HOLA_T_F32 = 0, HOLA_T_BF16 = 1, HOLA_T_F16 = 2, HOLA_T_INT8 = 3, HOLA_T_MIXED = 4 } hola_t_dtype;
+typedef struct hola_embed_args {
+  int64_t N;                /* tokens, >= 0                                                               */
+  int32_t V, H;             /* rows and channels of the table                                             */
+  int32_t v_offset, V_global;
+  const void* tokens;       /* int32 [N], or int64 (wide_tokens)                                          */
+  int32_t wide_tokens;
+  int32_t t_dtype;          /* hola_t_dtype                                                               */
+  const void* table;        /* HOLA_T_MIXED: not read                                                     */
+  int64_t row_stride;       /* channels                                                                   */
+  const float* w_scale;     /* [V], HOLA_T_INT8 and HOLA_T_MIXED                                          */
+  const hola_wmix* wmix;    /* HOST pointer, HOLA_T_MIXED (H a multiple of 128)                           */
+  float scale;
+  int32_t out_dtype;        /* HOLA_T_F32, HOLA_T_BF16 or HOLA_T_F16, of add as well                      */
+  const void* add;          /* [N][H], optional                                                           */
+  int64_t add_stride;
+  void* out;                /* [N][H]                                                                     */
+  int64_t out_stride;
+  uint32_t* status_word;    /* in/out [1], optional                                                       */
+} hola_embed_args;
+hola_status hola_embed(const hola_embed_args* args, void* cuda_stream);
+
+/* The gradient of such a table:  dW[v] = scale * sum of grad[r] over the r with tokens[r] = v.  Sums are held in fp32, in pieces of rising r (at most 1024 rows) that are
+ * added up in their order: the same inputs give the same bits.  Tokens count as for hola_embed.
+ *   the whole table: out [V][H], rows of tokens that do not occur are zero; or with accumulate: added to what out holds, other rows left as they are.
+ *   by rows (ids_out and count_out given): the distinct tokens in rising order, out[i] the row of ids_out[i], count_out their number;
+ *   what lies behind is left as it was.  out and ids_out have room for N.
+ * workspace: hola_embed_grad_workspace_bytes(N, V, H) bytes on the device, 16-byte aligned, of this call alone until it has run (the
+ * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs no context, two launches like
+ * hola_verify's. */
+typedef struct hola_embed_grad_args {
+  int64_t N;                /* >= 0, < 2^31 - 1                                                           */
+  int32_t V, H;
+  int32_t v_offset, V_global;
+  const void* tokens;
+  int32_t wide_tokens;
+  int32_t g_dtype;          /* HOLA_T_F32, HOLA_T_BF16 or HOLA_T_F16                                      */
+  const void* grad;         /* [N][H]                                                                     */
+  int64_t grad_stride;      /* channels                                                                   */
+  float scale;
+  int32_t out_dtype;        /* HOLA_T_F32, HOLA_T_BF16 or HOLA_T_F16                                      */
+  void* out;
+  int64_t out_stride;
+  int32_t accumulate;
+  int32_t reserved_;
+  int32_t* ids_out;         /* [N], by rows                                                               */
+  int32_t* count_out;       /* [1], by rows                                                               */
+  void* workspace;
+  uint64_t workspace_bytes;
+  uint32_t* status_word;    /* in/out [1], optional                                                       */
+} hola_embed_grad_args;
+size_t hola_embed_grad_workspace_bytes(long long N, int V, int H);
+hola_status hola_embed_grad(const hola_embed_grad_args* args, void* cuda_stream);
 
 /* Quantises a bf16 W_lm [V][H] (device) to the HOLA_W_INT8 form, on the current device, asynchronously on the
  * stream: scale[v] = max_h |W[v][h]| / 127 (1 for an all-zero row), q = clip(rint(W / scale), -127, 127), evaluated in

@@ -25,14 +25,15 @@ HOLA_W_BF16, HOLA_W_INT8, HOLA_W8A8, HOLA_W8A16, HOLA_W_MIXED = 0, 1, 2, 3, 4
 HOLA_HIDDEN_IN_PLACE, HOLA_HIDDEN_ON_LINES, HOLA_HIDDEN_8BIT = 0, 1, 2
 HOLA_ARG_CLEAR_STATUS = 1
 GROUP_ROWS, SUB_BLOCK, HOLA_PACE_WORDS = 256, 128, 256
-FLAG_BAD_TOKEN, FLAG_BAD_UNIFORM, FLAG_TIMEOUT, FLAG_R_ZERO, FLAG_BAD_ADAPTER, FLAG_BAD_LOGIT = 1, 2, 4, 8, 16, 32
+FLAG_BAD_TOKEN, FLAG_BAD_UNIFORM, FLAG_TIMEOUT, FLAG_R_ZERO, FLAG_BAD_ADAPTER, FLAG_BAD_LOGIT, FLAG_BAD_BEAM = 1, 2, 4, 8, 16, 32, 64
 HOLA_L_F32, HOLA_L_BF16, HOLA_L_F16 = 0, 1, 2
-HOLA_MAX_TOP, HOLA_MAX_RANK = 32, 128
+HOLA_T_F32, HOLA_T_BF16, HOLA_T_F16, HOLA_T_INT8, HOLA_T_MIXED = 0, 1, 2, 3, 4
+HOLA_MAX_TOP, HOLA_MAX_RANK, HOLA_MAX_BEAMS = 32, 128, 32
 HOLA_OPT_RING_SLOTS, HOLA_OPT_ROTATING_UNITS, HOLA_OPT_HOST_OVERLAP, HOLA_OPT_HOST_ROWS_ON_DEMAND, HOLA_OPT_PASSES, HOLA_OPT_PAIR_MMA, HOLA_OPT_HOST_IN_PLACE, HOLA_OPT_CONVERTER_GROUP, HOLA_OPT_FUSED_PASSES = 1, 2, 3, 4, 5, 6, 7, 8, 9
 
 EXPORTS = ["hola_create", "hola_destroy", "hola_workspace_bytes", "hola_verify", "hola_verify_host",
            "hola_lm_head_entropy", "hola_accept_sample", "hola_host_traffic", "hola_shard_record_bytes", "hola_shard_lm_head",
-           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_lm_head_adapters", "hola_verify_adapters", "hola_token_logprobs", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
+           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_lm_head_adapters", "hola_verify_adapters", "hola_token_logprobs", "hola_beam_select", "hola_beam_reorder", "hola_embed", "hola_embed_grad", "hola_embed_grad_workspace_bytes", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
            "hola_version"]
 
 
@@ -75,6 +76,45 @@ class hola_logprobs_args(ctypes.Structure):
                 ("next_tok", ctypes.c_void_p), ("logZ_in", ctypes.c_void_p), ("logprob", ctypes.c_void_p),
                 ("rank", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("logZ", ctypes.c_void_p),
                 ("top_ids", ctypes.c_void_p), ("top_logprobs", ctypes.c_void_p), ("status_word", ctypes.c_void_p)]
+
+
+class hola_beam_args(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("W", ctypes.c_int32), ("V", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("beam_stride", ctypes.c_int64),
+                ("l_dtype", ctypes.c_int32), ("end_token", ctypes.c_int32), ("logZ", ctypes.c_void_p), ("score", ctypes.c_void_p),
+                ("finished", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("keep_slots", ctypes.c_int32),
+                ("reserved_", ctypes.c_int32), ("score_out", ctypes.c_void_p), ("parent", ctypes.c_void_p),
+                ("token", ctypes.c_void_p), ("finished_out", ctypes.c_void_p), ("status_word", ctypes.c_void_p)]
+
+
+class hola_beam_state(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("beam_stride", ctypes.c_int64),
+                ("outer_stride", ctypes.c_int64 * 2), ("dst_seq_stride", ctypes.c_int64), ("dst_beam_stride", ctypes.c_int64),
+                ("dst_outer_stride", ctypes.c_int64 * 2), ("outer", ctypes.c_int64 * 2), ("run", ctypes.c_int64),
+                ("position", ctypes.c_int64)]
+
+
+class hola_reorder_args(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("W", ctypes.c_int32), ("n", ctypes.c_int32), ("count", ctypes.c_int32),
+                ("states", ctypes.c_void_p), ("parent", ctypes.c_void_p), ("parent_stride", ctypes.c_int64),
+                ("used", ctypes.c_void_p), ("status_word", ctypes.c_void_p)]
+
+
+class hola_embed_args(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int32), ("H", ctypes.c_int32), ("v_offset", ctypes.c_int32),
+                ("V_global", ctypes.c_int32), ("tokens", ctypes.c_void_p), ("wide_tokens", ctypes.c_int32), ("t_dtype", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("w_scale", ctypes.c_void_p), ("wmix", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("out_dtype", ctypes.c_int32), ("add", ctypes.c_void_p), ("add_stride", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64), ("status_word", ctypes.c_void_p)]
+
+
+class hola_embed_grad_args(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int32), ("H", ctypes.c_int32), ("v_offset", ctypes.c_int32),
+                ("V_global", ctypes.c_int32), ("tokens", ctypes.c_void_p), ("wide_tokens", ctypes.c_int32), ("g_dtype", ctypes.c_int32),
+                ("grad", ctypes.c_void_p), ("grad_stride", ctypes.c_int64), ("scale", ctypes.c_float), ("out_dtype", ctypes.c_int32),
+                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64), ("accumulate", ctypes.c_int32), ("reserved_", ctypes.c_int32),
+                ("ids_out", ctypes.c_void_p), ("count_out", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_uint64), ("status_word", ctypes.c_void_p)]
 
 
 class hola_plan_info(ctypes.Structure):
@@ -131,6 +171,13 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         fn.argtypes = [ctypes.c_void_p, ctypes.POINTER(hola_verify_args), ctypes.POINTER(hola_adapters), ctypes.c_void_p]
     lib.hola_token_logprobs.restype = ctypes.c_int
     lib.hola_token_logprobs.argtypes = [ctypes.POINTER(hola_logprobs_args), ctypes.c_void_p]
+    for name, args in (("hola_beam_select", hola_beam_args), ("hola_beam_reorder", hola_reorder_args), ("hola_embed", hola_embed_args),
+                       ("hola_embed_grad", hola_embed_grad_args)):
+        fn = getattr(lib, name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
+    lib.hola_embed_grad_workspace_bytes.restype = ctypes.c_size_t
+    lib.hola_embed_grad_workspace_bytes.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
     lib.hola_quantize_w8.restype = ctypes.c_int
     lib.hola_quantize_w8.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                      ctypes.c_void_p]
@@ -508,6 +555,339 @@ def hola_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None
     with torch.cuda.device(dev):
         _check(lib, None, lib.hola_token_logprobs(ctypes.byref(a), _stream_ptr(stream)), "hola_token_logprobs")
     return got
+
+
+# ------------------------------------------------------------------------------------------------ beams
+@dataclass
+class BeamSelection:
+    """What hola_beam_select fills."""
+    score: torch.Tensor                 # fp32 [B, n]
+    parent: torch.Tensor                # int32 [B, n]
+    token: torch.Tensor                 # int32 [B, n]
+    finished: torch.Tensor | None       # bool [B, n], where beams can end
+
+
+def _same(what, t, dtype, size, dev, name):
+    """Pointer of an operand that has to be a contiguous tensor of this type and shape on this device."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(size) or not t.is_contiguous():
+        raise HolaError(f"{what}: {name} must be a contiguous {dtype} tensor of shape {tuple(size)} on {dev}")
+    return t.data_ptr()
+
+
+def hola_beam_select(logits: torch.Tensor, logZ: torch.Tensor, score: torch.Tensor, n: int | None = None, finished: torch.Tensor | None = None,
+                     end_token: int = -1, weight: torch.Tensor | None = None, keep_slots: bool = False, out: BeamSelection | None = None,
+                     status: torch.Tensor | None = None, stream=None) -> BeamSelection:
+    """The `n` best continuations (None: as many as there are beams) over the beams of each sequence and the vocabulary.
+
+    logits: fp32, bf16 or fp16 [B, W, V], a row's entries side by side; logZ: fp32 [B, W], their log-sum-exp (hola_lm_head_entropy and
+    hola_token_logprobs have it); score: fp32 [B, W], the beams' log probabilities so far, -inf for none.  Candidates are ordered by
+    (score - logZ + logit) * weight in 64 bits, equal ones by beam, logit and id; out.score is score - logZ + logit.  finished: bool [B, W],
+    beams that have ended: one candidate each, end_token at the score they have.  weight: fp32 [B, W], positive (length-normalised keys).
+    keep_slots (n = W): the best child of a beam is put at the beam's own place instead of by rank, so that hola_beam_reorder has
+    least to move.  Places without a candidate: score -inf, parent and token -1.
+    status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  out: an earlier call's result, filled again.  stream: see HolaVerify."""
+    lib = load_library()
+    what = "hola_beam_select"
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in _L_DTYPES or not logits.is_cuda or logits.dim() != 3:
+        raise HolaError(f"{what} takes fp32, bf16 or fp16 logits [B, W, V] on a device")
+    B, W, V = logits.shape
+    dev = logits.device
+    n = W if n is None else n
+    if not 1 <= W <= HOLA_MAX_BEAMS or not 1 <= n <= HOLA_MAX_BEAMS or not 1 <= V <= 1 << 27 or (keep_slots and n != W):
+        raise HolaError(f"{what}: 1 .. {HOLA_MAX_BEAMS} beams and candidates, 1 .. 2^27 entries; keep_slots with as many candidates as beams")
+    if V > 1 and logits.stride(2) != 1:
+        raise HolaError(f"{what}: the entries of a row must lie side by side")
+    if not -1 <= end_token < V or (finished is not None and end_token < 0):
+        raise HolaError(f"{what}: end_token must be -1 .. V - 1, and a token where beams are finished")
+    a = hola_beam_args()
+    a.B, a.W, a.V, a.n, a.l_dtype, a.end_token, a.keep_slots = B, W, V, n, _L_DTYPES[logits.dtype], end_token, bool(keep_slots)
+    a.logits, a.seq_stride, a.beam_stride = logits.data_ptr(), logits.stride(0), logits.stride(1)
+    a.logZ, a.score = _same(what, logZ, torch.float32, (B, W), dev, "logZ"), _same(what, score, torch.float32, (B, W), dev, "score")
+    if finished is not None:
+        a.finished = _same(what, finished, torch.bool, (B, W), dev, "finished")
+    if weight is not None:
+        a.weight = _same(what, weight, torch.float32, (B, W), dev, "weight")
+    if status is not None:
+        a.status_word = _same(what, status, torch.int32, (1,), dev, "status")
+    ends = end_token >= 0
+    if out is None:
+        out = _make_on(stream, dev, lambda: BeamSelection(
+            torch.empty((B, n), dtype=torch.float32, device=dev), torch.empty((B, n), dtype=torch.int32, device=dev),
+            torch.empty((B, n), dtype=torch.int32, device=dev), torch.empty((B, n), dtype=torch.bool, device=dev) if ends else None))
+    a.score_out = _same(what, out.score, torch.float32, (B, n), dev, "out.score")
+    a.parent, a.token = (_same(what, t, torch.int32, (B, n), dev, "out") for t in (out.parent, out.token))
+    if ends:
+        a.finished_out = _same(what, out.finished, torch.bool, (B, n), dev, "out.finished")
+    with torch.cuda.device(dev):
+        _check(lib, None, lib.hola_beam_select(ctypes.byref(a), _stream_ptr(stream)), what)
+    return out
+
+
+class BeamStates:
+    """States of the beams for hola_beam_reorder, laid out once: tensors [..., B, W, ...] (token histories, keys and values, page tables).
+
+    axes: the axis of the sequences in each tensor (one number: in all), the beams' is the next one.  positions: for each tensor the axis that counts
+    positions, of which only the first used[b] are moved, or None.  into: tensors that take the reordered states (double buffers; perhaps with
+    another number of beams), None: the tensors themselves.  Keep the object alive while calls that use it are in flight."""
+
+    def __init__(self, tensors, axes=0, positions=None, into=None):
+        tensors = list(tensors)
+        axes = [axes] * len(tensors) if isinstance(axes, int) else list(axes)
+        positions = [None] * len(tensors) if positions is None else list(positions)
+        targets = tensors if into is None else list(into)
+        if not len(tensors) == len(axes) == len(positions) == len(targets) or not tensors:
+            raise HolaError("BeamStates takes tensors and one axis, one position axis or None, and one target for each")
+        if not all(isinstance(t, torch.Tensor) and t.layout == torch.strided for t in (*tensors, *targets)):
+            raise HolaError("BeamStates takes strided tensors")
+        self.tensors, self.into, self.device = tensors, targets, tensors[0].device
+        first = tensors[0].shape[axes[0]:axes[0] + 2] if 0 <= axes[0] <= tensors[0].dim() - 2 else (0, 0)
+        self.B, self.W = first
+        self.n = targets[0].shape[axes[0] + 1] if into is not None and targets[0].dim() == tensors[0].dim() else self.W
+        self.in_place = into is None
+        if not 1 <= self.W <= HOLA_MAX_BEAMS or not 1 <= self.n <= HOLA_MAX_BEAMS:
+            raise HolaError(f"BeamStates: 1 .. {HOLA_MAX_BEAMS} beams")
+        self.states = (hola_beam_state * len(tensors))()
+        for st, x, y, axis, at in zip(self.states, tensors, targets, axes, positions):
+            self._lay_out(st, x, y, axis, at)
+        if into is not None:
+            spans = lambda ts: [(t.data_ptr(), t.data_ptr() + (sum((s - 1) * d for s, d in zip(t.shape, t.stride())) + 1) * t.element_size())   # noqa: E731
+                                for t in ts if t.numel()]
+            written = spans(targets)
+            if any(a < d and c < b for a, b in written for c, d in spans(tensors)):
+                raise HolaError("BeamStates: a target overlaps a source")
+        self.address = ctypes.addressof(self.states)
+
+    def _lay_out(self, st, x, y, axis, at):
+        if not 0 <= axis <= x.dim() - 2 or tuple(x.shape[axis:axis + 2]) != (self.B, self.W):
+            raise HolaError(f"BeamStates: every tensor must have {self.B} sequences and {self.W} beams at its axis")
+        if y.dtype != x.dtype or x.device != self.device or y.device != self.device or tuple(y.shape) != (*x.shape[:axis + 1], self.n, *x.shape[axis + 2:]):
+            raise HolaError("BeamStates: a target must be like its tensor, but for the number of beams")
+        rest = [d for d in range(x.dim()) if d not in (axis, axis + 1)]
+        if at is not None and at not in rest:
+            raise HolaError("BeamStates: the positions' axis must be one besides those of sequences and beams")
+        for t in (x, y):                                         # (indices that share memory)
+            if any(t.shape[d] > 1 and t.stride(d) == 0 for d in range(t.dim())):
+                raise HolaError("BeamStates: expanded tensors hold no states of their own")
+        size, outer, closed, position = 1, [], False, 0          # what lies side by side, from the last axis on
+        for d in reversed(rest):
+            if x.shape[d] == 1 and d != at:
+                continue
+            inside = not closed and all(t.stride(d) == size or t.shape[d] == 1 for t in (x, y))
+            if d == at:
+                if not inside:
+                    raise HolaError("BeamStates: what belongs to a position must lie side by side, and the positions as well")
+                position, closed = size, True                    # (axes outside the positions' are outer ones)
+                size *= x.shape[d]
+            elif inside:
+                size *= x.shape[d]
+            else:
+                closed = True
+                if outer and all(s == o * n for s, o, n in ((x.stride(d), outer[-1][1], outer[-1][0]), (y.stride(d), outer[-1][2], outer[-1][0]))):
+                    outer[-1] = (outer[-1][0] * x.shape[d], *outer[-1][1:])
+                else:
+                    outer.append((x.shape[d], x.stride(d), y.stride(d)))
+        if len(outer) > 2:
+            raise HolaError("BeamStates: more than two axes beside the ones that lie side by side")
+        e = x.element_size()
+        beams = [(t.shape[axis + 1], t.stride(axis + 1)) for t in (x, y)]
+        if any(count > 1 and stride < size for count, stride in beams):
+            raise HolaError("BeamStates: beams must not share memory")
+        outer += [(1, 0, 0)] * (2 - len(outer))
+        st.src, st.dst, st.run, st.position = x.data_ptr(), y.data_ptr(), size * e, position * e
+        st.seq_stride, st.beam_stride, st.dst_seq_stride, st.dst_beam_stride = (
+            t.stride(d) * e for t, d in ((x, axis), (x, axis + 1), (y, axis), (y, axis + 1)))
+        for i, (count, s, to) in enumerate(outer):
+            st.outer[i], st.outer_stride[i], st.dst_outer_stride[i] = count, s * e, to * e
+
+
+def hola_beam_reorder(states: BeamStates, parent: torch.Tensor, used: torch.Tensor | None = None, status: torch.Tensor | None = None,
+                      stream=None) -> None:
+    """new[b, i] = old[b, parent[b, i]] for all states.  parent: int32 [B, n], -1 .. W - 1, rows at any distance (n columns of a wider
+    selection, say); -1 leaves a place as it was.  used: int32 [B], positions that hold something (states with a positions' axis)."""
+    lib = load_library()
+    what = "hola_beam_reorder"
+    if not isinstance(states, BeamStates):
+        raise HolaError(f"{what} takes BeamStates")
+    dev = states.device
+    if (not isinstance(parent, torch.Tensor) or parent.dtype != torch.int32 or parent.device != dev or parent.dim() != 2 or parent.shape[0] != states.B
+            or not 1 <= parent.shape[1] <= states.n or (parent.shape[1] > 1 and parent.stride(1) != 1) or dev.type != "cuda"):
+        raise HolaError(f"{what}: parent must be an int32 tensor of {states.B} rows of up to {states.n} places side by side, on the states' device")
+    a = hola_reorder_args()
+    a.B, a.W, a.n, a.count, a.states = states.B, states.W, parent.shape[1], len(states.states), states.address
+    a.parent, a.parent_stride = parent.data_ptr(), parent.stride(0)
+    if used is not None:
+        a.used = _same(what, used, torch.int32, (states.B,), dev, "used")
+    if status is not None:
+        a.status_word = _same(what, status, torch.int32, (1,), dev, "status")
+    with torch.cuda.device(dev):
+        _check(lib, None, lib.hola_beam_reorder(ctypes.byref(a), _stream_ptr(stream)), what)
+
+
+# ------------------------------------------------------------------------------------------------ embeddings
+_T_DTYPES = {torch.float32: HOLA_T_F32, torch.bfloat16: HOLA_T_BF16, torch.float16: HOLA_T_F16}
+_TOKENS = {torch.int32: 0, torch.int64: 1}
+
+
+def _rows_apart(what, t, shape, name):
+    """(pointer, distance of the rows) of a tensor [*shape, H] whose rows lie at one distance."""
+    if tuple(t.shape[:-1]) != tuple(shape) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise HolaError(f"{what}: {name} must have the tokens' shape and channels side by side")
+    stride, rows = None, 1
+    for size, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if stride is None:
+            stride = s
+        elif s != stride * rows:
+            raise HolaError(f"{what}: the rows of {name} must lie at one distance from each other")
+        rows *= size
+    return t.data_ptr(), t.shape[-1] if stride is None else stride
+
+
+def _ids(what, tokens):
+    if not isinstance(tokens, torch.Tensor) or tokens.dtype not in _TOKENS or not tokens.is_cuda or not tokens.is_contiguous():
+        raise HolaError(f"{what} takes contiguous int32 or int64 tokens on a device")
+
+
+def _part(what, a, v_offset, V_global):
+    if v_offset < 0 or (V_global and v_offset + a.V > V_global) or (not V_global and v_offset) or not 0 <= V_global < 2 ** 31:
+        raise HolaError(f"{what}: rows v_offset .. v_offset + V - 1 must be part of the V_global rows")
+    a.v_offset, a.V_global = v_offset, V_global
+
+
+def hola_embed(tokens: torch.Tensor, table, scale: float = 1.0, add: torch.Tensor | None = None, w_scale: torch.Tensor | None = None,
+               out: torch.Tensor | None = None, dtype: torch.dtype | None = None, v_offset: int = 0, V_global: int = 0,
+               status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """add + scale * table[tokens], [..., H] for tokens [...] (int32 or int64, -1: none).
+
+    table: fp32, bf16, fp16 [V, H], int8 [V, H] with w_scale (hola_quantize_w8) or a MixedHead.  Evaluated in fp32; dtype: of the result
+    (None: of out, of add, of the table, bf16 for the quantised ones).  add: the same type, [..., H]; it may be out.  v_offset, V_global: the table
+    is rows v_offset .. of a vocabulary of V_global; tokens of other parts count as none.
+    status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  stream: see HolaVerify."""
+    lib = load_library()
+    what = "hola_embed"
+    _ids(what, tokens)
+    dev, shape = tokens.device, tokens.shape
+    a = hola_embed_args()
+    if isinstance(table, MixedHead):
+        if w_scale is not None or table.w_scale.device != dev:
+            raise HolaError(f"{what}: a MixedHead carries its own scales, on the tokens' device")
+        a.V, a.H, a.t_dtype, a.wmix, a.w_scale = table.V, table.H, HOLA_T_MIXED, ctypes.addressof(table.struct), table.w_scale.data_ptr()
+        own = torch.bfloat16
+    else:
+        if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.device != dev or (table.dtype not in _T_DTYPES and table.dtype != torch.int8):
+            raise HolaError(f"{what} takes a table [V, H] of fp32, bf16, fp16 or int8 on the tokens' device, or a MixedHead")
+        if (table.dtype == torch.int8) != (w_scale is not None):
+            raise HolaError(f"{what}: an int8 table goes with w_scale (fp32 per row), another one without")
+        if max(table.shape) >= 2 ** 31:
+            raise HolaError(f"{what}: more rows or channels than 32 bits count")
+        a.V, a.H = table.shape
+        a.table, a.row_stride = _rows_apart(what, table, (a.V,), "table")
+        a.t_dtype = HOLA_T_INT8 if w_scale is not None else _T_DTYPES[table.dtype]
+        if w_scale is not None:
+            a.w_scale = _same(what, w_scale, torch.float32, (a.V,), dev, "w_scale")
+        own = torch.bfloat16 if w_scale is not None else table.dtype
+    _part(what, a, v_offset, V_global)
+    for t in (out, add):
+        dtype = t.dtype if dtype is None and t is not None else dtype
+    dtype = own if dtype is None else dtype
+    if dtype not in _T_DTYPES or any(t is not None and (t.dtype != dtype or t.device != dev or t.shape[-1:] != (a.H,)) for t in (out, add)):
+        raise HolaError(f"{what}: fp32, bf16 or fp16 results; out and add of that type, with the table's channels, on the tokens' device")
+    if tokens.numel() >= 2 ** 31:
+        raise HolaError(f"{what}: more tokens than 32 bits count")
+    a.N, a.tokens, a.wide_tokens, a.scale, a.out_dtype = tokens.numel(), tokens.data_ptr(), _TOKENS[tokens.dtype], scale, _T_DTYPES[dtype]
+    if add is not None:
+        a.add, a.add_stride = _rows_apart(what, add, shape, "add")
+    if out is None:
+        out, = _make_on(stream, dev, lambda: (torch.empty((*shape, a.H), dtype=dtype, device=dev),))
+    a.out, a.out_stride = _rows_apart(what, out, shape, "out")
+    if status is not None:
+        a.status_word = _same(what, status, torch.int32, (1,), dev, "status")
+    if a.N:
+        with torch.cuda.device(dev):
+            _check(lib, None, lib.hola_embed(ctypes.byref(a), _stream_ptr(stream)), what)
+    return out
+
+
+@dataclass
+class TokenRows:
+    """The gradient of a table by rows: what hola_embed_grad_rows fills.  The first count[0] entries hold something."""
+    ids: torch.Tensor        # int32 [N], the distinct tokens, rising
+    rows: torch.Tensor       # [N, H]
+    count: torch.Tensor      # int32 [1]
+
+
+def _embed_grad(what, tokens, grad, V, scale, v_offset, V_global, status, stream, fill):
+    lib = load_library()
+    _ids(what, tokens)
+    dev, N = tokens.device, tokens.numel()
+    if not isinstance(grad, torch.Tensor) or grad.dtype not in _T_DTYPES or grad.device != dev or grad.dim() < 1:
+        raise HolaError(f"{what} takes an fp32, bf16 or fp16 gradient on the tokens' device")
+    H = grad.shape[-1]
+    if not 1 <= V < 2 ** 31 - 2 or not 1 <= H < 2 ** 31 or N >= 2 ** 31 - 1:
+        raise HolaError(f"{what}: sizes must be positive and fit 32 bits")
+    a = hola_embed_grad_args()
+    a.N, a.V, a.H, a.scale = N, V, H, scale
+    _part(what, a, v_offset, V_global)
+    a.tokens, a.wide_tokens, a.g_dtype = tokens.data_ptr(), _TOKENS[tokens.dtype], _T_DTYPES[grad.dtype]
+    a.grad, a.grad_stride = _rows_apart(what, grad, tokens.shape, "grad")
+    if status is not None:
+        a.status_word = _same(what, status, torch.int32, (1,), dev, "status")
+    a.workspace_bytes = lib.hola_embed_grad_workspace_bytes(N, V, H)
+    out = _make_on(stream, dev, lambda: fill(a, dev, N, H))
+    workspace, = _make_on(stream, dev, lambda: (torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev),))
+    a.workspace = workspace.data_ptr()
+    with torch.cuda.device(dev):
+        _check(lib, None, lib.hola_embed_grad(ctypes.byref(a), _stream_ptr(stream)), what)
+    return out
+
+
+def hola_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, V: int, scale: float = 1.0, out: torch.Tensor | None = None,
+                    accumulate: bool = False, dtype: torch.dtype = torch.float32, v_offset: int = 0, V_global: int = 0,
+                    status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient of a table [V, H] through hola_embed: row v is scale times the sum of grad[r] over the tokens r that are v (-1: none),
+    in fp32, the same bits every time.  grad: fp32, bf16 or fp16 [..., H] for tokens [...].  out: fp32, bf16 or fp16 [V, H], filled (rows of
+    tokens that do not occur: zeros), or with accumulate added to.  dtype: of a fresh result.  status, stream, v_offset, V_global: as
+    for hola_embed."""
+    what = "hola_embed_grad"
+    if accumulate and out is None:
+        raise HolaError(f"{what}: accumulate needs out")
+
+    def fill(a, dev, N, H):
+        if (dtype if out is None else out.dtype) not in _T_DTYPES:
+            raise HolaError(f"{what}: fp32, bf16 or fp16 results")
+        t = torch.empty((V, H), dtype=dtype, device=dev) if out is None else out
+        if tuple(t.shape) != (V, H) or t.device != dev:
+            raise HolaError(f"{what}: out must be [V, H] on the tokens' device")
+        a.out, a.out_stride = _rows_apart(what, t, (V,), "out")
+        a.out_dtype, a.accumulate = _T_DTYPES[t.dtype], bool(accumulate)
+        return (t,)
+
+    return _embed_grad(what, tokens, grad, V, scale, v_offset, V_global, status, stream, fill)[0]
+
+
+def hola_embed_grad_rows(tokens: torch.Tensor, grad: torch.Tensor, V: int, scale: float = 1.0, out: TokenRows | None = None,
+                         dtype: torch.dtype = torch.float32, v_offset: int = 0, V_global: int = 0, status: torch.Tensor | None = None,
+                         stream=None) -> TokenRows:
+    """The same by rows: the distinct tokens in rising order, and the gradient's row of each.  out: an earlier call's result, or buffers
+    with room for as many rows as there are tokens; what lies behind the distinct ones is left as it was."""
+    what = "hola_embed_grad_rows"
+
+    def fill(a, dev, N, H):
+        got = out
+        if got is None:
+            if dtype not in _T_DTYPES:
+                raise HolaError(f"{what}: fp32, bf16 or fp16 results")
+            got = TokenRows(torch.empty((N,), dtype=torch.int32, device=dev), torch.empty((N, H), dtype=dtype, device=dev),
+                            torch.empty((1,), dtype=torch.int32, device=dev))
+        if got.rows.dtype not in _T_DTYPES or got.rows.device != dev or tuple(got.rows.shape) != (N, H):
+            raise HolaError(f"{what}: out.rows must be fp32, bf16 or fp16, a row for each token, on the tokens' device")
+        a.ids_out, a.count_out = _same(what, got.ids, torch.int32, (N,), dev, "out.ids"), _same(what, got.count, torch.int32, (1,), dev, "out.count")
+        a.out, a.out_stride = _rows_apart(what, got.rows, (N,), "out.rows")
+        a.out_dtype = _T_DTYPES[got.rows.dtype]
+        return got
+
+    return _embed_grad(what, tokens, grad, V, scale, v_offset, V_global, status, stream, fill)
 
 
 @dataclass

@@ -1,0 +1,577 @@
+// beams.cuh - one step of a beam search around the LM head: the best continuations over all beams and the vocabulary, and the beams'
+// states put in the order of their parents.  Part of hola_verify.cu (inside its anonymous namespace, behind token_logprobs.cuh, whose
+// groups of 32 bytes and rows it uses).
+//
+// Selection.  Candidate (w, v) of a sequence has c = (score[w] - logZ[w]) + l[w][v] and the key c * weight[w], both in 64 bits; the n
+// first in the order (key descending, beam ascending, logit descending, id ascending) are kept.  One pass over the logits in 32 bits:
+// a = fma(l, weight, b), b = (score - logZ) weight rounded, is within 2^-24 (|a| + |b|) of the key.  A cluster of CTAs takes a sequence,
+// every CTA a part of each row; a thread keeps the largest a of its groups, the group, and the largest of its other groups.  Every
+// eight threads put the best of theirs on a board of 32 (every four on one of 64, for more than twenty candidates); let the n-th best
+// there be w.  At least n candidates have a >= w, so each of the part's n best has a >= w - 2^-22 (|w| + max |b|): twice the bound
+// above for either side, and the roundings of this line.  Only threads whose own largest is that large hold such entries; their groups are read again, out of the L2,
+// and what qualifies goes, with its key in 64 bits, to the sequence's first CTA, which places each by counting those before it.
+
+constexpr int kBsThreads = 256;
+constexpr int kBsWarps = kBsThreads / 32;
+constexpr int kBsMaxBeams = 32, kBsMaxKept = 32;
+constexpr int kBsMaxCluster = 16;
+constexpr int kBsSpots = 128;          // candidates that a part may send unsorted; beyond that it sends its 32 best
+constexpr int kBsAhead = 4;            // groups of a thread that are on the way
+constexpr int kBsMaxV = 1 << 27;       // ids share a word with a beam and a logit
+
+struct BsParams {
+  const void* logits;
+  long long seq_stride, beam_stride;   // entries
+  int B, W, V, n;
+  const float* logZ;                   // [B][W]
+  const float* score;                  // [B][W]
+  const uint8_t* finished;             // [B][W], or null
+  const float* weight;                 // [B][W], or null: 1
+  int end_token, keep_slots;
+  float* score_out;                    // [B][n]
+  int* parent;
+  int* token;
+  uint8_t* finished_out;               // or null
+  unsigned* status;                    // or null
+};
+
+// A candidate in its order: the larger (hi, lo) comes first.  hi: the key; lo: beam (5 bits, reversed), logit (32), id (27, reversed).
+struct BsCand {
+  uint64_t hi, lo;
+};
+__device__ __forceinline__ bool bs_before(const BsCand& a, const BsCand& b) { return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo); }
+__device__ __forceinline__ uint64_t bs_order(double x) {
+  const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));
+  return b >> 63 ? ~b : b | 0x8000000000000000ull;
+}
+__device__ __forceinline__ uint64_t bs_low(int beam, float l, int id) {
+  return static_cast<uint64_t>(31 - beam) << 59 | static_cast<uint64_t>(lp_order(l)) << 27 | static_cast<uint32_t>(kBsMaxV - 1 - id);
+}
+__device__ __forceinline__ int bs_beam(uint64_t lo) { return 31 - static_cast<int>(lo >> 59); }
+__device__ __forceinline__ float bs_logit(uint64_t lo) { return lp_value(static_cast<uint32_t>(lo >> 27)); }
+__device__ __forceinline__ int bs_id(uint64_t lo) { return kBsMaxV - 1 - static_cast<int>(lo & (kBsMaxV - 1)); }
+
+// Sorted lists across a warp, as in token_logprobs.cuh, of candidates; {0, 0}: none.
+__device__ __forceinline__ BsCand bs_exchange(const BsCand& a, int stride, bool first) {
+  const BsCand b = {__shfl_xor_sync(0xffffffffu, a.hi, stride), __shfl_xor_sync(0xffffffffu, a.lo, stride)};
+  return bs_before(a, b) == first ? a : b;
+}
+__device__ __noinline__ BsCand bs_take_in(BsCand best, const BsCand* waiting, int n) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  BsCand a = {0, 0};
+  if (lane < n) a = waiting[lane];
+#pragma unroll 1
+  for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll 1
+    for (int stride = size >> 1; stride > 0; stride >>= 1) a = bs_exchange(a, stride, ((lane & size) == 0) == ((lane & stride) == 0));
+  const BsCand r = {__shfl_sync(0xffffffffu, a.hi, 31 - lane), __shfl_sync(0xffffffffu, a.lo, 31 - lane)};
+  if (bs_before(r, best)) best = r;
+#pragma unroll 1
+  for (int stride = 16; stride > 0; stride >>= 1) best = bs_exchange(best, stride, (lane & stride) == 0);
+  __syncwarp();
+  return best;
+}
+
+// A live beam's row, and this CTA's part of it.
+struct BsRow {
+  double off, weight;
+  const void* row;
+  float b, w32;
+  int beam, j_begin, j_end;
+};
+
+template <typename T>
+struct BsShared {
+  BsRow rows[kBsMaxBeams];
+  BsCand own[kBsWarps * 32];           // what this part sends (kBsSpots), or the warps' sorted lists
+  BsCand all[kBsMaxCluster * kBsSpots + kBsMaxBeams];      // first CTA: what the parts have sent, and the ended beams
+  int before_it[kBsMaxCluster * kBsSpots + kBsMaxBeams];
+  BsCand waiting[kBsWarps][32];
+  BsCand kept[kBsMaxKept];
+  uint64_t board[64];
+  uint8_t looked_at[kBsWarps][32];
+  unsigned bad_from[kBsMaxCluster];    // rows that hold NaN or +inf, as every CTA of the cluster has found them
+  unsigned bad_here;
+  int live, n_own, n_all;
+  float b_max;
+};
+
+// a: the key in 32 bits.  (Kept finite: a mask may be as low as the type goes.  -inf is no candidate; NaN stays.)
+__device__ __forceinline__ float bs_approx(float l, float w32, float b) {
+  const float a = fmaf(l, w32, b);
+  return fabsf(a) == CUDART_INF_F && fabsf(l) != CUDART_INF_F ? copysignf(3.402823466e38f, a) : a;
+}
+
+// Walks a part: rounds of kBsThreads groups of one row, row after row.  The same for all threads but for j.
+template <typename T>
+struct BsWalk {
+  const BsRow* rows;
+  int live, li, j, j_end, round_end;
+  LpRow<T> r;
+  __device__ __forceinline__ BsWalk(const BsRow* rows_, int live_, int V) : rows(rows_), live(live_), li(-1), j(0), j_end(0), round_end(0),
+                                                                          r(nullptr, V) { row(V); }
+  // On to the next row that has groups in this part.
+  __device__ __forceinline__ void row(int V) {
+    while (++li < live) {
+      if (rows[li].j_begin >= rows[li].j_end) continue;
+      r = LpRow<T>(static_cast<const T*>(rows[li].row), V);
+      j_end = rows[li].j_end;
+      j = rows[li].j_begin + static_cast<int>(threadIdx.x);
+      round_end = rows[li].j_begin + kBsThreads;
+      return;
+    }
+  }
+  __device__ __forceinline__ bool done() const { return li >= live; }
+  __device__ __forceinline__ LpGroup<T> get() const { return j < j_end ? r.get(j) : LpRow<T>::none(); }
+  __device__ __forceinline__ void next(int V) {
+    if (round_end >= j_end) { row(V); return; }
+    j += kBsThreads;
+    round_end += kBsThreads;
+  }
+};
+
+// Entries of group j of a row whose a is at least thr, as candidates.
+template <typename T>
+__device__ __forceinline__ void bs_send(BsShared<T>& s, const BsRow& row, int V, int j, float thr) {
+  const LpRow<T> r(static_cast<const T*>(row.row), V);
+  const LpGroup<T> g = r.get(j);
+  unsigned which = 0;
+#pragma unroll
+  for (int e = 0; e < LpGroup<T>::kEntries; ++e) {
+    const float l = g.entry(e);
+    which |= l > -CUDART_INF_F && bs_approx(l, row.w32, row.b) >= thr ? 1u << e : 0u;
+  }
+  if (!which) return;
+  int spot = atomicAdd(&s.n_own, __popc(which));
+  const int v0 = r.first(j);
+#pragma unroll
+  for (int e = 0; e < LpGroup<T>::kEntries; ++e)
+    if (which >> e & 1u) {
+      if (spot < kBsSpots) {
+        const float l = g.entry(e);
+        s.own[spot] = {bs_order((row.off + static_cast<double>(l)) * row.weight), bs_low(row.beam, l, v0 + e)};
+      }
+      ++spot;
+    }
+}
+
+// What bounds it: HBM for large batches; for a few rows the chain beams -> pass -> board -> second look -> cluster -> counting.
+template <typename T>
+__global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsParams p, int C) {
+  extern __shared__ __align__(16) unsigned char bs_smem[];
+  BsShared<T>& s = *reinterpret_cast<BsShared<T>*>(bs_smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int seq = blockIdx.x / C, part = blockIdx.x - seq * C;
+  if (tid == 0) { s.n_own = 0; s.n_all = 0; s.bad_here = 0; }
+  if (tid < kBsMaxCluster) s.bad_from[tid] = 0;
+  // (the other CTAs of the cluster have started, and their counters stand at zero: looked at before anything is sent)
+  if (C > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  grid_dependency_wait();
+  grid_dependency_release();
+
+  // The beams, by every warp for itself; warp 0 writes them down.
+  unsigned flags = 0;
+  float score = -CUDART_INF_F, logZ = 0.f, weight = 1.f;
+  bool ended = false;
+  if (lane < p.W) {
+    const size_t at = static_cast<size_t>(seq) * p.W + lane;
+    score = p.score[at];
+    ended = p.finished && p.finished[at];
+    if (p.weight) weight = p.weight[at];
+    if (!ended) logZ = p.logZ[at];
+  }
+  const bool bad_beam = !(score < CUDART_INF_F) || !(logZ < CUDART_INF_F) || !(weight > 0.f && weight < CUDART_INF_F);
+  const bool there = !bad_beam && score != -CUDART_INF_F, reads = there && !ended && logZ != -CUDART_INF_F;
+  if (__any_sync(0xffffffffu, bad_beam)) flags |= HOLA_FLAG_BAD_LOGIT;
+  const unsigned ended_mask = __ballot_sync(0xffffffffu, there && ended);
+  unsigned excluded = 0;                                 // rows that have turned out to hold NaN or +inf
+
+  for (;;) {
+    const unsigned live_mask = __ballot_sync(0xffffffffu, reads && !(excluded >> lane & 1u));
+    const int live = __popc(live_mask);
+    if (warp == 0) {
+      const double off = static_cast<double>(score) - static_cast<double>(logZ);
+      const float b = static_cast<float>(off * static_cast<double>(weight));
+      if (live_mask >> lane & 1u) {
+        BsRow& row = s.rows[__popc(live_mask & ((1u << lane) - 1u))];
+        const T* at = static_cast<const T*>(p.logits) + static_cast<size_t>(seq) * p.seq_stride + static_cast<size_t>(lane) * p.beam_stride;
+        const LpRow<T> r(at, p.V);
+        const int per = (r.groups + C - 1) / C;
+        row.off = off; row.weight = weight; row.row = at; row.b = b; row.w32 = weight; row.beam = lane;
+        row.j_end = min(r.groups, (part + 1) * per);
+        row.j_begin = min(part * per, row.j_end);
+      }
+      const float most = warp_max_f32(live_mask >> lane & 1u ? fabsf(b) : 0.f);
+      if (lane == 0) s.b_max = most;
+    }
+    __syncthreads();
+
+    // The pass.
+    float m = -CUDART_INF_F, second = -CUDART_INF_F;
+    int at_li = 0, at_j = 0, steps = 0;                  // steps: rounds of this part
+    {
+      BsWalk<T> ahead(s.rows, live, p.V), here(s.rows, live, p.V);
+      LpGroup<T> next[kBsAhead];
+#pragma unroll
+      for (int d = 0; d < kBsAhead; ++d)
+        if (!ahead.done()) { next[d] = ahead.get(); ahead.next(p.V); }
+#pragma unroll 1
+      while (!here.done()) {
+#pragma unroll
+        for (int d = 0; d < kBsAhead; ++d) {
+          if (here.done()) break;
+          const float top = next[d].largest();
+          if (!ahead.done()) { next[d] = ahead.get(); ahead.next(p.V); }
+          const BsRow& row = s.rows[here.li];
+          const float a = bs_approx(top, row.w32, row.b);
+          if (!(top < CUDART_INF_F)) atomicOr(&s.bad_here, 1u << row.beam);
+          second = fmaxf(second, fminf(a, m));
+          if (a > m) { at_li = here.li; at_j = here.j; }
+          m = fmaxf(m, a);
+          here.next(p.V);
+          ++steps;
+        }
+      }
+    }
+
+    // The board: the n-th best of the threads' largest, taken together by eight or four.
+    {
+      uint64_t a = m > -CUDART_INF_F ? lp_key(m, tid) : 0;
+      const int board = p.n > 20 ? 64 : 32, share = kBsThreads / board;
+      for (int o = 1; o < share; o <<= 1) {
+        const uint64_t b = __shfl_xor_sync(0xffffffffu, a, o);
+        if (b > a) a = b;
+      }
+      if ((lane & (share - 1)) == 0) s.board[tid / share] = a;
+      __syncthreads();
+      uint64_t lim = 0;
+      for (int at = 0; at < board; at += 32) {
+        const uint64_t key = s.board[at + lane];
+        int before = 0;
+#pragma unroll 8
+        for (int i = 0; i < board; ++i) before += s.board[i] > key ? 1 : 0;
+        const unsigned nth = __ballot_sync(0xffffffffu, key != 0 && before == p.n - 1);
+        if (nth) lim = __shfl_sync(0xffffffffu, key, __ffs(nth) - 1);
+      }
+      // (offsets beyond 1e30, where the bound on a would run over: everything qualifies)
+      float thr = -CUDART_INF_F;
+      if (lim != 0 && s.b_max < 1e30f) {
+        const float w = lp_value(static_cast<uint32_t>(lim >> 32));
+        thr = w - (2.384185791015625e-7f * (fabsf(w) + s.b_max) + 1e-37f);
+      }
+      const bool mine = m > -CUDART_INF_F && m >= thr, again = mine && second >= thr && second > -CUDART_INF_F;
+      if (mine && !again) bs_send(s, s.rows[at_li], p.V, at_j, thr);
+      // threads with more than one such group: all of theirs, dealt out to the warp's lanes
+      const unsigned look = __ballot_sync(0xffffffffu, again);
+      if (look) {
+        if (again) s.looked_at[warp][__popc(look & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
+        __syncwarp();
+        const int who = __popc(look);
+        // (step by step over the rows' rounds: lane i takes thread i % who of round i / who)
+        for (int li = 0; li < live; ++li) {
+          const int n_rounds = (s.rows[li].j_end - s.rows[li].j_begin + kBsThreads - 1) / kBsThreads, total = n_rounds * who;
+          for (int i = lane; i < total; i += 32) {
+            const int jj = s.rows[li].j_begin + (i / who) * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
+            if (jj < s.rows[li].j_end) bs_send(s, s.rows[li], p.V, jj, thr);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    if (s.n_own > kBsSpots) {
+      // More than there is room for (equal or masked entries, or the best crowd together): the part's 32 best by sorted lists, from
+      // every entry's key in 64 bits.
+      __syncthreads();                                   // (everyone has seen n_own)
+      BsCand best = {0, 0};
+      int waiting = 0;
+#pragma unroll 1
+      for (int li = 0; li < live; ++li) {
+        const BsRow& row = s.rows[li];
+        const LpRow<T> r(static_cast<const T*>(row.row), p.V);
+#pragma unroll 1
+        for (int j0 = row.j_begin + warp * 32; j0 < row.j_end; j0 += kBsThreads) {
+          const int jj = j0 + lane;
+          LpGroup<T> g = LpRow<T>::none();
+          if (jj < row.j_end) g = r.get(jj);
+          const int v0 = r.first(jj);
+          BsCand worst = {__shfl_sync(0xffffffffu, best.hi, p.n - 1), __shfl_sync(0xffffffffu, best.lo, p.n - 1)};
+          const float top = g.largest();
+          const bool any = jj < row.j_end && top > -CUDART_INF_F &&
+                           bs_order((row.off + static_cast<double>(top)) * row.weight) >= worst.hi;
+          if (!__any_sync(0xffffffffu, any)) continue;
+#pragma unroll 1
+          for (int e = 0; e < LpGroup<T>::kEntries; ++e) {
+            float l = -CUDART_INF_F;
+#pragma unroll
+            for (int i = 0; i < LpGroup<T>::kEntries; ++i) l = i == e ? g.entry(i) : l;
+            const BsCand c = {bs_order((row.off + static_cast<double>(l)) * row.weight), bs_low(row.beam, l, v0 + e)};
+            const bool in = any && l > -CUDART_INF_F && bs_before(c, worst);
+            const unsigned mask = __ballot_sync(0xffffffffu, in);
+            if (!mask) continue;
+            const int fit = __popc(mask);
+            if (waiting + fit > 32) {
+              best = bs_take_in(best, s.waiting[warp], waiting);
+              waiting = 0;
+              worst = {__shfl_sync(0xffffffffu, best.hi, p.n - 1), __shfl_sync(0xffffffffu, best.lo, p.n - 1)};
+            }
+            if (in) s.waiting[warp][waiting + __popc(mask & ((1u << lane) - 1u))] = c;
+            waiting += fit;
+          }
+        }
+      }
+      best = bs_take_in(best, s.waiting[warp], waiting);
+      s.own[tid] = best;
+      __syncthreads();
+      int before = 0;
+      for (int i = 0; i < kBsWarps * 32; ++i) before += bs_before(s.own[i], best) ? 1 : 0;
+      __syncthreads();
+      if (best.hi != 0 && before < 32) s.own[before] = best;       // (candidates differ, so their places do)
+      const int some = __syncthreads_count(best.hi != 0 && before < 32);
+      if (tid == 0) s.n_own = some;
+      __syncthreads();
+    }
+
+    // To the sequence's first CTA: the candidates; to every CTA: the rows found bad.
+    if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+    const int mine = s.n_own;
+    if (warp == 0) {
+      int* n_all = C > 1 ? cg::this_cluster().map_shared_rank(&s.n_all, 0) : &s.n_all;
+      int first = 0;
+      if (lane == 0 && mine > 0) first = atomicAdd(n_all, mine);
+      first = __shfl_sync(0xffffffffu, first, 0);
+      BsCand* all = C > 1 ? cg::this_cluster().map_shared_rank(s.all, 0) : s.all;
+      for (int i = lane; i < mine; i += 32) all[first + i] = s.own[i];
+    } else if (warp == 1 && lane < C) {
+      unsigned* to = C > 1 ? cg::this_cluster().map_shared_rank(&s.bad_from[part], lane) : &s.bad_from[part];
+      *to = s.bad_here;
+    }
+    if (C > 1) cluster_sync_all();
+    else __syncthreads();
+    const unsigned found = __reduce_or_sync(0xffffffffu, lane < C ? s.bad_from[lane] : 0u) & ~excluded;
+    if (!found) break;
+    // Seldom: the limits may stem from rows that have no distribution.  Once more without them.
+    excluded |= found;
+    flags |= HOLA_FLAG_BAD_LOGIT;
+    __syncthreads();
+    if (tid == 0) { s.n_own = 0; s.n_all = 0; }
+    if (C > 1) {
+      cluster_sync_all();
+      asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+    } else {
+      __syncthreads();
+    }
+  }
+  if (part != 0) return;
+
+  // Ended beams have one candidate each.
+  const int sent = s.n_all;
+  const int total = sent + __popc(ended_mask);
+  if (warp == 0 && (ended_mask >> lane & 1u))
+    s.all[sent + __popc(ended_mask & ((1u << lane) - 1u))] = {bs_order(static_cast<double>(score) * weight), bs_low(lane, 0.f, p.end_token)};
+  if (tid < kBsMaxKept) s.kept[tid] = {0, 0};
+  for (int i = tid; i < total; i += kBsThreads) s.before_it[i] = 0;
+  __syncthreads();
+  // Every candidate's place is the number of those before it: a warp compares all of them with an eighth of them.
+  const int slice = (total + kBsWarps - 1) / kBsWarps, from = warp * slice, to = min(total, from + slice);
+  if (from < to) {
+#pragma unroll 1
+    for (int i = lane; i < total; i += 32) {
+      const BsCand c = s.all[i];
+      int before = 0;
+#pragma unroll 4
+      for (int k = from; k < to; ++k) before += bs_before(s.all[k], c) ? 1 : 0;
+      atomicAdd(&s.before_it[i], before);
+    }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = tid; i < total; i += kBsThreads) {
+    const int place = s.before_it[i];
+    if (place < p.n) s.kept[place] = s.all[i];
+  }
+  __syncthreads();
+  if (warp != 0) return;
+
+  // Lane i: the i-th kept.
+  const BsCand c = s.kept[lane];
+  const bool have = lane < p.n && c.hi != 0;
+  const int beam = have ? bs_beam(c.lo) : 0;
+  const float from_score = __shfl_sync(0xffffffffu, score, beam), from_logZ = __shfl_sync(0xffffffffu, logZ, beam);
+  const bool was_ended = have && (ended_mask >> beam & 1u);
+  const float out_score = !have ? -CUDART_INF_F
+                          : was_ended ? from_score
+                          : static_cast<float>((static_cast<double>(from_score) - static_cast<double>(from_logZ)) + static_cast<double>(bs_logit(c.lo)));
+  const int token = have ? bs_id(c.lo) : -1;
+  int slot = lane;
+  if (p.keep_slots) {
+    // the first child of a beam goes to its slot, the others take the free ones in order
+    const unsigned same = __match_any_sync(0xffffffffu, have ? beam : -1 - lane);
+    const bool stays = have && __ffs(same) - 1 == lane;
+    unsigned free = ~__reduce_or_sync(0xffffffffu, stays ? 1u << beam : 0u);
+    const unsigned waits = __ballot_sync(0xffffffffu, lane < p.n && !stays);
+    if (stays) {
+      slot = beam;
+    } else {
+      for (int i = __popc(waits & ((1u << lane) - 1u)); i > 0; --i) free &= free - 1u;
+      slot = __ffs(free) - 1;
+    }
+  }
+  if (lane < p.n) {
+    const size_t at = static_cast<size_t>(seq) * p.n + slot;
+    p.score_out[at] = out_score;
+    p.parent[at] = have ? beam : -1;
+    p.token[at] = token;
+    if (p.finished_out) p.finished_out[at] = have && (was_ended || (p.end_token >= 0 && token == p.end_token)) ? 1 : 0;
+  }
+  if (p.status && lane == 0 && flags) atomicOr(p.status, flags);
+}
+
+// CTAs per sequence: up to three on an SM, as long as a thread keeps two groups or so of the sequence's rows.
+int bs_cluster(int num_sms, int B, int W, int V, int elem) {
+  const long long groups = static_cast<long long>(W) * V / (kLpGroupBytes / elem);
+  int C = 1;
+  while (C < kBsMaxCluster && 2ll * B * C <= 3ll * num_sms && groups / (2 * C) >= kBsThreads) C <<= 1;
+  return C;
+}
+
+template <typename T>
+cudaError_t launch_beam_select(const BsParams& p, int num_sms, cudaStream_t stream) {
+  const int C = bs_cluster(num_sms, p.B, p.W, p.V, static_cast<int>(sizeof(T)));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(p.B) * C); cfg.blockDim = dim3(kBsThreads); cfg.stream = stream;
+  cfg.dynamicSmemBytes = sizeof(BsShared<T>);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(C); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
+  cudaError_t e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(BsShared<T>)));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  return cudaLaunchKernelEx(&cfg, beam_select_kernel<T>, p, C);
+}
+
+// ------------------------------------------------------------------------------------------------ reordering
+// new[b][i] = old[b][parent[b][i]], any number of states.  A CTA takes a piece of the bytes of all beams of one sequence (of one
+// layer, one head); a thread takes 16 bytes of every beam that changes into registers and then writes them, so that the same buffer
+// may be read and written in any order of the parents: no other thread touches these bytes.  In place, beams that stay (parent[i] = i)
+// are neither read, but for their children, nor written.  Bound by HBM, whose latency 16 words of 16 bytes a thread on the way hide.
+constexpr int kBrThreads = 128;
+constexpr int kBrStates = 24;          // states of one launch (launch parameters)
+
+struct BrState {
+  const unsigned char* src;
+  unsigned char* dst;
+  long long seq, beam, outer0, outer1; // strides in bytes
+  long long to_seq, to_beam, to_outer0, to_outer1;
+  long long run, position;             // bytes that lie side by side; bytes of a position (0: all of the run is moved)
+  unsigned n0, n1;                     // outer axes
+  unsigned pieces;                     // of a run
+  unsigned first_cta;
+};
+struct BrParams {
+  BrState s[kBrStates];
+  int count, B, W, n, in_place;
+  long long parent_stride;
+  const int* parent;
+  const int* used;
+  unsigned* status;
+};
+constexpr int kBrPiece = 8 * 16 * kBrThreads;      // bytes of a beam that a CTA takes at most
+
+// M: beams that change at most; U: words of each that a thread has on the way.
+template <typename V, int M, int U>
+__device__ __forceinline__ void br_move(const BrState& st, const unsigned char* src, unsigned char* dst, long long begin, long long end,
+                                        const int* to, const int* from, int moves) {
+  constexpr long long kStep = static_cast<long long>(kBrThreads) * sizeof(V);
+#pragma unroll 1
+  for (long long at = begin + static_cast<long long>(threadIdx.x) * sizeof(V); at < end; at += U * kStep) {
+    V v[U][M];
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      if (i < moves) {
+        const unsigned char* x = src + from[i] * st.beam + at;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (at + u * kStep < end) v[u][i] = *reinterpret_cast<const V*>(x + u * kStep);
+      }
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      if (i < moves) {
+        unsigned char* x = dst + to[i] * st.to_beam + at;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (at + u * kStep < end) *reinterpret_cast<V*>(x + u * kStep) = v[u][i];
+      }
+  }
+}
+template <typename V>
+__device__ __forceinline__ void br_move_any(const BrState& st, const unsigned char* src, unsigned char* dst, long long begin, long long end,
+                                            const int* to, const int* from, int moves) {
+  if (moves <= 2) br_move<V, 2, 8>(st, src, dst, begin, end, to, from, moves);
+  else if (moves <= 4) br_move<V, 4, 4>(st, src, dst, begin, end, to, from, moves);
+  else if (moves <= 8) br_move<V, 8, 2>(st, src, dst, begin, end, to, from, moves);
+  else if (moves <= 16) br_move<V, 16, 1>(st, src, dst, begin, end, to, from, moves);
+  else br_move<V, 32, 1>(st, src, dst, begin, end, to, from, moves);
+}
+
+__global__ void __launch_bounds__(kBrThreads) beam_reorder_kernel(const __grid_constant__ BrParams p) {
+  __shared__ int to[32], from[32];
+  __shared__ int n_moves;
+  grid_dependency_wait();
+  grid_dependency_release();
+  int k = 0;
+  while (k + 1 < p.count && blockIdx.x >= p.s[k + 1].first_cta) ++k;
+  const BrState& st = p.s[k];
+  unsigned x = blockIdx.x - st.first_cta;
+  const unsigned piece = x % st.pieces; x /= st.pieces;
+  const unsigned b = x % static_cast<unsigned>(p.B); x /= static_cast<unsigned>(p.B);
+  const unsigned i1 = x % st.n1, i0 = x / st.n1;
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    int from_beam = -1;
+    bool bad = false;
+    if (lane < p.n) {
+      from_beam = p.parent[static_cast<long long>(b) * p.parent_stride + lane];
+      bad = from_beam < -1 || from_beam >= p.W;
+    }
+    const bool moves = !bad && from_beam >= 0 && !(p.in_place && from_beam == lane);
+    const unsigned mask = __ballot_sync(0xffffffffu, moves);
+    if (moves) {
+      const int at = __popc(mask & ((1u << lane) - 1u));
+      to[at] = lane;
+      from[at] = from_beam;
+    }
+    if (lane == 0) n_moves = __popc(mask);
+    if (__any_sync(0xffffffffu, bad) && lane == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_BEAM);
+  }
+  __syncthreads();
+  const int moves = n_moves;
+  long long run = st.run;
+  if (p.used && st.position > 0) {
+    const long long filled = static_cast<long long>(max(p.used[b], 0)) * st.position;
+    run = filled < run ? filled : run;
+  }
+  const long long begin = static_cast<long long>(piece) * kBrPiece, end = begin + kBrPiece < run ? begin + kBrPiece : run;
+  if (moves == 0 || begin >= end) return;
+  const unsigned char* src = st.src + (b * st.seq + i0 * st.outer0 + i1 * st.outer1);
+  unsigned char* dst = st.dst + (b * st.to_seq + i0 * st.to_outer0 + i1 * st.to_outer1);
+  // what every address of the piece has in common
+  const unsigned align = static_cast<unsigned>(reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) |
+                                               static_cast<uintptr_t>(st.beam | st.to_beam | end));
+  if (align % 16 == 0) br_move_any<uint4>(st, src, dst, begin, end, to, from, moves);
+  else if (align % 4 == 0) br_move_any<uint32_t>(st, src, dst, begin, end, to, from, moves);
+  else br_move_any<unsigned char>(st, src, dst, begin, end, to, from, moves);
+}
+
+cudaError_t launch_beam_reorder(const BrParams& p, unsigned ctas, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(kBrThreads); cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, beam_reorder_kernel, p);
+}

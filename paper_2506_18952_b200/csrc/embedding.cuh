@@ -1,0 +1,626 @@
+// embedding.cuh - rows of a table by token, and the gradient of the table.  Part of hola_verify.cu (inside its anonymous namespace).
+
+// ------------------------------------------------------------------------------------------------ lookup
+// out[r] = add[r] + scale * W[tok[r]], every operation one rounding in fp32 (the scale of a quantised row first), the result rounded
+// once more where it is stored in 16 bits.  A thread takes 8 neighbouring channels of kEmRows rows.
+constexpr int kEmThreads = 256;
+constexpr int kEmRows = 4;             // rows of a CTA, loads of which are on the way together
+
+// Types of rows in memory (hola_t_dtype).
+enum { kTabF32 = HOLA_T_F32, kTabBf16 = HOLA_T_BF16, kTabF16 = HOLA_T_F16, kTabInt8 = HOLA_T_INT8, kTabMixed = HOLA_T_MIXED };
+__host__ __device__ constexpr int tab_bytes(int t) { return t == kTabF32 ? 4 : t == kTabInt8 ? 1 : 2; }
+
+struct EmParams {
+  const void* tokens;
+  int wide;                            // 64-bit ids
+  long long N;
+  int V, H;
+  long long v_offset, V_global;
+  const void* table;
+  long long row_stride;                // channels
+  const float* w_scale;
+  hola_wmix mix;
+  float scale;
+  const void* add;
+  long long add_stride;
+  void* out;
+  long long out_stride;
+  unsigned* status;
+};
+
+// Row of the table that a token names; -1: none.  `bad`: no token at all.
+__device__ __forceinline__ int em_row(const void* tokens, int wide, long long r, int V, long long v_offset, long long V_global, bool* bad) {
+  const long long t = wide ? static_cast<const long long*>(tokens)[r] : static_cast<const int*>(tokens)[r];
+  *bad = t < -1 || t >= V_global;
+  const long long v = t - v_offset;
+  return t >= 0 && v >= 0 && v < V ? static_cast<int>(v) : -1;
+}
+
+// n (8 or 1) channels as loaded, and as fp32.
+template <int kType, int n>
+struct EmWord {
+  static constexpr int kBytes = tab_bytes(kType) * n;
+  uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
+  __device__ __forceinline__ void load(const void* p) {
+    if (kBytes == 32) {
+      const uint4 a = static_cast<const uint4*>(p)[0], b = static_cast<const uint4*>(p)[1];
+      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+      w[4 % (kBytes < 4 ? 1 : kBytes / 4)] = b.x; w[5 % (kBytes < 4 ? 1 : kBytes / 4)] = b.y;
+      w[6 % (kBytes < 4 ? 1 : kBytes / 4)] = b.z; w[7 % (kBytes < 4 ? 1 : kBytes / 4)] = b.w;
+    } else if (kBytes == 16) {
+      const uint4 a = *static_cast<const uint4*>(p);
+      w[0] = a.x; w[1 % (kBytes < 4 ? 1 : kBytes / 4)] = a.y; w[2 % (kBytes < 4 ? 1 : kBytes / 4)] = a.z;
+      w[3 % (kBytes < 4 ? 1 : kBytes / 4)] = a.w;
+    } else if (kBytes == 8) {
+      const uint2 a = *static_cast<const uint2*>(p);
+      w[0] = a.x; w[1 % (kBytes < 4 ? 1 : kBytes / 4)] = a.y;
+    } else if (kBytes == 4) {
+      w[0] = *static_cast<const uint32_t*>(p);
+    } else if (kBytes == 2) {
+      w[0] = *static_cast<const uint16_t*>(p);
+    } else {
+      w[0] = *static_cast<const uint8_t*>(p);
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if (kType == kTabF32) return __uint_as_float(w[i]);
+    if (kType == kTabBf16) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    if (kType == kTabF16) return __half2float(__ushort_as_half(static_cast<unsigned short>(w[i / 2] >> (16 * (i & 1)))));
+    return static_cast<float>(static_cast<int>(w[i / 4] << (24 - 8 * (i & 3))) >> 24);
+  }
+};
+
+// n channels to memory, rounded to nearest even.
+template <int kType, int n>
+__device__ __forceinline__ void em_store(void* p, const float* x) {
+  if (kType == kTabF32) {
+    if (n == 8) {
+      static_cast<float4*>(p)[0] = make_float4(x[0], x[1 % n], x[2 % n], x[3 % n]);
+      static_cast<float4*>(p)[1] = make_float4(x[4 % n], x[5 % n], x[6 % n], x[7 % n]);
+    } else {
+      *static_cast<float*>(p) = x[0];
+    }
+    return;
+  }
+  uint32_t h[n];
+#pragma unroll
+  for (int i = 0; i < n; ++i)
+    h[i] = kType == kTabBf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x[i])) : __half_as_ushort(__float2half_rn(x[i]));
+  if (n == 8)
+    *static_cast<uint4*>(p) = make_uint4(h[0] | h[1 % n] << 16, h[2 % n] | h[3 % n] << 16, h[4 % n] | h[5 % n] << 16, h[6 % n] | h[7 % n] << 16);
+  else
+    *static_cast<uint16_t*>(p) = static_cast<uint16_t>(h[0]);
+}
+template <int n>
+__device__ __forceinline__ void em_store_as(int type, void* base, long long at, const float* x) {
+  if (type == kTabF32) em_store<kTabF32, n>(static_cast<float*>(base) + at, x);
+  else if (type == kTabBf16) em_store<kTabBf16, n>(static_cast<uint16_t*>(base) + at, x);
+  else em_store<kTabF16, n>(static_cast<uint16_t*>(base) + at, x);
+}
+template <int n>
+__device__ __forceinline__ void em_load_as(int type, const void* base, long long at, float* x) {
+  if (type == kTabF32) {
+    EmWord<kTabF32, n> w;
+    w.load(static_cast<const float*>(base) + at);
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = w.get(i);
+  } else {
+    EmWord<kTabBf16, n> w;
+    w.load(static_cast<const uint16_t*>(base) + at);
+    EmWord<kTabF16, n> f;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof w.w / 4); ++i) f.w[i] = w.w[i];
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = type == kTabBf16 ? w.get(i) : f.get(i);
+  }
+}
+
+// n channels of a row of a mixed-width head: group of 256 rows -> its width and its place among the rows of that width.
+template <int n>
+__device__ __forceinline__ void em_mixed(const hola_wmix& mix, int H, int v, int h, float* x) {
+  const int width = mix.group_width[v >> 8];
+  const size_t row = static_cast<size_t>(mix.group_row[v >> 8]) + (v & 255);
+  if (width == 16) {
+    EmWord<kTabBf16, n> w;
+    w.load(static_cast<const uint16_t*>(mix.W16) + row * H + h);
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = w.get(i);
+  } else if (width == 8) {
+    EmWord<kTabInt8, n> w;
+    w.load(static_cast<const uint8_t*>(mix.W8) + row * H + h);
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = w.get(i);
+  } else {
+    // two codes a byte, the even channel in the low nibble; a power of two for every 128 channels
+    const uint8_t* at = static_cast<const uint8_t*>(mix.W4) + (row * H + h) / 2;
+    const uint32_t codes = n == 8 ? *reinterpret_cast<const uint32_t*>(at) : static_cast<uint32_t>(*at) >> (4 * (h & 1));
+    const int e = mix.shift4[static_cast<size_t>(h / 128) * mix.rows4 + row];
+#pragma unroll
+    for (int i = 0; i < n; ++i) x[i] = static_cast<float>((static_cast<int>(codes << (28 - 4 * i)) >> 28) << e);
+  }
+}
+
+// n: channels of a thread, 8 where everything is aligned.  Bound by HBM: rows in, rows out.
+template <int kType, int n>
+__global__ void __launch_bounds__(kEmThreads) embed_kernel(const __grid_constant__ EmParams p, int out_type, int rows_per_cta) {
+  grid_dependency_wait();
+  grid_dependency_release();
+  const long long r0 = static_cast<long long>(blockIdx.x) * rows_per_cta;
+  const int rows = static_cast<int>(p.N - r0 < rows_per_cta ? p.N - r0 : rows_per_cta);
+  int v[kEmRows];
+  float ws[kEmRows];
+  bool any_bad = false;
+#pragma unroll
+  for (int i = 0; i < kEmRows; ++i) {
+    v[i] = -1;
+    ws[i] = 1.f;
+    if (i < rows) {
+      bool bad;
+      v[i] = em_row(p.tokens, p.wide, r0 + i, p.V, p.v_offset, p.V_global, &bad);
+      any_bad = any_bad || bad;
+      if ((kType == kTabInt8 || kType == kTabMixed) && v[i] >= 0) ws[i] = p.w_scale[v[i]];
+    }
+  }
+  if (any_bad && p.status && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  const int step = static_cast<int>(gridDim.y) * kEmThreads * n;
+#pragma unroll 1
+  for (int h = (static_cast<int>(blockIdx.y) * kEmThreads + static_cast<int>(threadIdx.x)) * n; h < p.H; h += step) {
+    float x[kEmRows][n];
+    if (kType == kTabMixed) {
+#pragma unroll
+      for (int i = 0; i < kEmRows; ++i)
+        if (v[i] >= 0) em_mixed<n>(p.mix, p.H, v[i], h, x[i]);
+    } else {
+      constexpr int kWord = kType == kTabMixed ? kTabBf16 : kType;
+      EmWord<kWord, n> w[kEmRows];
+#pragma unroll
+      for (int i = 0; i < kEmRows; ++i)
+        if (v[i] >= 0) w[i].load(static_cast<const unsigned char*>(p.table) + (v[i] * p.row_stride + h) * tab_bytes(kWord));
+#pragma unroll
+      for (int i = 0; i < kEmRows; ++i)
+#pragma unroll
+        for (int c = 0; c < n; ++c) x[i][c] = v[i] >= 0 ? w[i].get(c) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kEmRows; ++i) {
+      if (i >= rows) break;
+      float y[n];
+#pragma unroll
+      for (int c = 0; c < n; ++c) {
+        y[c] = 0.f;
+        if (v[i] >= 0) {
+          y[c] = x[i][c];
+          if (kType == kTabInt8 || kType == kTabMixed) y[c] = __fmul_rn(y[c], ws[i]);
+          y[c] = __fmul_rn(y[c], p.scale);
+        }
+      }
+      if (p.add) {
+        float a[n];
+        em_load_as<n>(out_type, p.add, (r0 + i) * p.add_stride + h, a);
+#pragma unroll
+        for (int c = 0; c < n; ++c) y[c] = __fadd_rn(a[c], y[c]);
+      }
+      em_store_as<n>(out_type, p.out, (r0 + i) * p.out_stride + h, y);
+    }
+  }
+}
+
+template <int kType, int n>
+cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
+  const long long slices = (p.H + kEmThreads * n - 1) / (kEmThreads * n);
+  // several rows of a CTA where there are CTAs enough all the same
+  const int rows = p.N * slices >= 8ll * kEmRows * num_sms ? kEmRows : 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((p.N + rows - 1) / rows), static_cast<unsigned>(slices > 65535 ? 65535 : slices));
+  cfg.blockDim = dim3(kEmThreads); cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, embed_kernel<kType, n>, p, out_type, rows);
+}
+template <int n>
+cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_sms, cudaStream_t stream) {
+  switch (type) {
+    case kTabF32: return launch_embed<kTabF32, n>(p, out_type, num_sms, stream);
+    case kTabBf16: return launch_embed<kTabBf16, n>(p, out_type, num_sms, stream);
+    case kTabF16: return launch_embed<kTabF16, n>(p, out_type, num_sms, stream);
+    case kTabInt8: return launch_embed<kTabInt8, n>(p, out_type, num_sms, stream);
+    default: return launch_embed<kTabMixed, n>(p, out_type, num_sms, stream);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+// dW[v] = scale * sum of g[r] over the rows r with tok[r] = v, in rising r, in fp32.  Two launches.
+//
+// 1. Tokens sorted (stable), with nothing exchanged between the CTAs: each takes a range of `R` ids and reads all tokens, every warp a
+//    stretch of them.  It counts what lies below its range (where its part of the sorted order begins) and, per id and warp, what lies
+//    inside; a scan over (id, warp) gives every warp the place of its first occurrence of every id, and a second look at the tokens
+//    puts them there.  Bound by latency; N x 4 or 8 bytes per CTA out of the L2.
+// 2. Sums.  The sorted order is cut into windows; the rows of a token lie side by side there, in pieces of at most `S`.  A CTA adds up
+//    the pieces that begin in its window, for a slice of kEgSlice channels.  A token with one piece is finished by it; the pieces of the others
+//    go to the workspace, and the CTA that comes last adds them up in their order.  So the result does not depend on the schedule.
+//    The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
+constexpr int kEsThreads = 1024, kEsWarps = 32;
+constexpr int kEsMaxIds = 1536;        // ids of a CTA of the sort: counters of 4 bytes per id and warp
+constexpr int kEgThreads = 128, kEgEach = 8;
+constexpr int kEgSlice = kEgThreads * kEgEach;
+constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
+constexpr int kEgAhead = 8;            // rows of a thread on the way
+constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspace has to be known without a device)
+
+struct EgParams {
+  const void* tokens;
+  int wide;
+  long long N;                         // < 2^31
+  int V, H;
+  long long v_offset, V_global;
+  int R, buckets, warps, chunk;        // sort: ids per CTA, CTAs, warps that count, tokens of a warp
+  int S, window, slices;
+  const void* grad;
+  long long g_stride;
+  float scale;
+  void* out;
+  long long out_stride;
+  int accumulate, by_rows;
+  int* ids_out;                        // by_rows: the distinct tokens, rising
+  int* count_out;
+  // workspace
+  int* perm;                           // [N] rows in sorted order
+  int* sorted;                         // [N] their ids
+  int* first;                          // [V + 1] where an id's rows begin
+  int* place;                          // [V] by_rows: rank of an id among the CTA's distinct ones
+  int* distinct;                       // [buckets]
+  unsigned* done;                      // [ceil(N / S)][slices] pieces of a token that have arrived
+  float* partial;                      // [2 ceil(N / S)][slices * kEgSlice]
+  unsigned* status;
+};
+
+__global__ void __launch_bounds__(kEsThreads) embed_sort_kernel(const __grid_constant__ EgParams p) {
+  extern __shared__ int es_counts[];                     // [R][warps]
+  __shared__ int warp_sum[kEsWarps], warp_below[kEsWarps], warp_distinct[kEsWarps];
+  __shared__ int base;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int lo = blockIdx.x * p.R, R = min(p.R, p.V - lo), cells = R * p.warps;
+  for (int i = tid; i < cells; i += kEsThreads) es_counts[i] = 0;
+  grid_dependency_wait();
+  grid_dependency_release();
+  // (counters of the second launch)
+  const long long pieces = (p.N + p.S - 1) / p.S * p.slices;
+  for (long long i = static_cast<long long>(blockIdx.x) * kEsThreads + tid; i < pieces; i += static_cast<long long>(p.buckets) * kEsThreads) p.done[i] = 0;
+  __syncthreads();
+
+  const long long begin = static_cast<long long>(warp) * p.chunk, end = begin + p.chunk < p.N ? begin + p.chunk : p.N;
+  int below = 0;
+  bool any_bad = false;
+  if (warp < p.warps) {
+#pragma unroll 4
+    for (long long r0 = begin; r0 < end; r0 += 32) {
+      bool bad = false;
+      int v = -1;
+      if (r0 + lane < end) v = em_row(p.tokens, p.wide, r0 + lane, p.V, p.v_offset, p.V_global, &bad);
+      any_bad = any_bad || bad;
+      below += v >= 0 && v < lo ? 1 : 0;
+      const unsigned at = static_cast<unsigned>(v - lo);
+      const unsigned in = __ballot_sync(0xffffffffu, v >= 0 && at < static_cast<unsigned>(R));
+      if (in >> lane & 1u) {
+        const unsigned same = __match_any_sync(in, at);
+        if (__ffs(same) - 1 == lane) es_counts[at * p.warps + warp] += __popc(same);
+      }
+      __syncwarp();
+    }
+  }
+  below = __reduce_add_sync(0xffffffffu, below);
+  if (lane == 0) warp_below[warp] = below;
+  if (__any_sync(0xffffffffu, any_bad) && lane == 0 && blockIdx.x == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  __syncthreads();
+
+  // Exclusive scan over (id, warp): a thread's cells lie side by side.
+  const int each = (cells + kEsThreads - 1) / kEsThreads, c0 = min(tid * each, cells), c1 = min(c0 + each, cells);
+  int sum = 0;
+  for (int i = c0; i < c1; ++i) sum += es_counts[i];
+  int upto = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) warp_sum[warp] = upto;
+  __syncthreads();
+  if (warp == 0) {
+    const int mine = warp_sum[lane];
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    warp_sum[lane] = x - mine;
+    const int all_below = __reduce_add_sync(0xffffffffu, warp_below[lane]);
+    if (lane == 0) base = all_below;
+  }
+  __syncthreads();
+  int at = base + warp_sum[warp] + upto - sum;
+  for (int i = c0; i < c1; ++i) {
+    const int n = es_counts[i];
+    es_counts[i] = at;
+    at += n;
+  }
+  __syncthreads();
+  const int last = blockIdx.x + 1 == gridDim.x ? 1 : 0;
+  // Where the ids begin; the distinct ones numbered.  (The end of the range: base plus everything inside.)
+  __shared__ int range_end;
+  if (tid == kEsThreads - 1) range_end = at;             // (the last thread's cells are the last, or none)
+  __syncthreads();
+  int distinct_before = 0;
+#pragma unroll 1
+  for (int v0 = 0; v0 < R; v0 += kEsThreads) {
+    const int v = v0 + tid;
+    bool some = false;
+    if (v < R) {
+      const int b = es_counts[v * p.warps], e = v + 1 < R ? es_counts[(v + 1) * p.warps] : range_end;
+      p.first[lo + v] = b;
+      some = e > b;
+    }
+    if (last && v == R) p.first[p.V] = range_end;
+    if (p.by_rows) {
+      const unsigned have = __ballot_sync(0xffffffffu, some);
+      if (lane == 0) warp_distinct[warp] = __popc(have);
+      __syncthreads();
+      int mine = warp_distinct[lane], x = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      const int before = __shfl_sync(0xffffffffu, x - mine, warp), all = __shfl_sync(0xffffffffu, x, 31);
+      if (some) p.place[lo + v] = distinct_before + before + __popc(have & ((1u << lane) - 1u));
+      distinct_before += all;
+      __syncthreads();
+    }
+  }
+  if (last && tid == 0) p.first[p.V] = range_end;
+  if (p.by_rows && tid == 0) p.distinct[blockIdx.x] = distinct_before;
+  __syncthreads();                                       // (the counters move on below)
+
+  if (warp < p.warps) {
+#pragma unroll 4
+    for (long long r0 = begin; r0 < end; r0 += 32) {
+      bool bad;
+      int v = -1;
+      if (r0 + lane < end) v = em_row(p.tokens, p.wide, r0 + lane, p.V, p.v_offset, p.V_global, &bad);
+      const unsigned id = static_cast<unsigned>(v - lo);
+      const unsigned in = __ballot_sync(0xffffffffu, v >= 0 && id < static_cast<unsigned>(R));
+      if (in >> lane & 1u) {
+        const unsigned same = __match_any_sync(in, id);
+        const int to = es_counts[id * p.warps + warp] + __popc(same & ((1u << lane) - 1u));
+        __syncwarp(same);
+        if (__ffs(same) - 1 == lane) es_counts[id * p.warps + warp] += __popc(same);
+        p.perm[to] = static_cast<int>(r0 + lane);
+        p.sorted[to] = v;
+      }
+      __syncwarp();
+    }
+  }
+}
+
+// Eight channels of a thread: side by side (kVec), or kEgThreads apart where rows start anywhere.
+template <bool kVec>
+__device__ __forceinline__ int eg_channel(int slice, int i) {
+  return slice * kEgSlice + (kVec ? static_cast<int>(threadIdx.x) * kEgEach + i : static_cast<int>(threadIdx.x) + i * kEgThreads);
+}
+template <int kType, bool kVec>
+struct EgRow {
+  EmWord<kType, kVec ? kEgEach : 1> w[kVec ? 1 : kEgEach];
+  __device__ __forceinline__ void load(const EgParams& p, int row, int slice) {
+    const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row) * p.g_stride * tab_bytes(kType);
+#pragma unroll
+    for (int i = 0; i < (kVec ? 1 : kEgEach); ++i) {
+      const int h = eg_channel<kVec>(slice, i);
+      if (h < p.H) w[i].load(at + static_cast<long long>(h) * tab_bytes(kType));
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return kVec ? w[0].get(i) : w[kVec ? 0 : i].get(0); }
+};
+
+template <bool kVec>
+__device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long long row, int slice, const float* sum) {
+  float x[kEgEach];
+#pragma unroll
+  for (int i = 0; i < kEgEach; ++i) x[i] = __fmul_rn(sum[i], p.scale);
+  if (kVec) {
+    const int h = eg_channel<true>(slice, 0);
+    if (h >= p.H) return;
+    const long long at = row * p.out_stride + h;
+    if (p.accumulate) {
+      float a[kEgEach];
+      em_load_as<kEgEach>(out_type, p.out, at, a);
+#pragma unroll
+      for (int i = 0; i < kEgEach; ++i) x[i] = __fadd_rn(a[i], x[i]);
+    }
+    em_store_as<kEgEach>(out_type, p.out, at, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEgEach; ++i) {
+      const int h = eg_channel<false>(slice, i);
+      if (h >= p.H) continue;
+      const long long at = row * p.out_stride + h;
+      float a[1] = {0.f};
+      if (p.accumulate) em_load_as<1>(out_type, p.out, at, a);
+      a[0] = __fadd_rn(a[0], x[i]);
+      em_store_as<1>(out_type, p.out, at, a);
+    }
+  }
+}
+
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
+  __shared__ int rows[kEgMaxWindow + kEgMaxPiece];       // of the gradient, for the places of the pieces that begin in the window
+  __shared__ int ids[kEgMaxWindow], firsts[kEgMaxWindow + 1], ends[kEgMaxWindow], out_rows[kEgMaxWindow];
+  __shared__ int part_sum[kEgThreads / 32];
+  __shared__ int last_here;
+  grid_dependency_wait();
+  grid_dependency_release();
+  const int slice = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.slices)), tid = threadIdx.x;
+  const int w = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.slices));
+  if (w >= windows) {
+    // The whole table: zeros to the rows of ids that do not occur.
+    const float zero[kEgEach] = {};
+    const int v0 = (w - windows) * kEgMaxWindow, n = min(kEgMaxWindow, p.V - v0);
+    if (tid <= n) firsts[tid] = p.first[v0 + tid];
+    __syncthreads();
+    for (int i = 0; i < n; ++i)
+      if (firsts[i] == firsts[i + 1]) eg_write<kVec>(p, out_type, v0 + i, slice, zero);
+    return;
+  }
+  const int valid = p.first[p.V];
+  if (w == 0 && slice == 0 && p.by_rows && tid < 32) {
+    int n = 0;
+    for (int i = tid; i < p.buckets; i += 32) n += p.distinct[i];
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (tid == 0) *p.count_out = n;
+  }
+  const int w0 = w * p.window, w1 = min(w0 + p.window, valid);
+  if (w0 >= w1) return;
+  if (tid < w1 - w0) {
+    const int v = p.sorted[w0 + tid];
+    ids[tid] = v;
+    firsts[tid] = p.first[v];
+    ends[tid] = p.first[v + 1];
+  }
+  __syncthreads();
+  // Places x0 .. x1 - 1: from the first piece that begins in the window to the end of the last one that does.
+  int x0 = w0, x1 = w1;
+  {
+    const int in = (w0 - firsts[0]) % p.S;
+    if (in != 0) x0 = min(w0 + p.S - in, ends[0]);
+    if (x0 >= w1) return;                                // (all of the window inside one piece)
+    const int b = firsts[w1 - 1 - w0];
+    x1 = min(b + ((w1 - 1 - b) / p.S + 1) * p.S, ends[w1 - 1 - w0]);
+  }
+  for (int i = tid; i < x1 - x0; i += kEgThreads) rows[i] = p.perm[x0 + i];
+  if (p.by_rows) {
+    // The distinct ids ahead of an id's own range of ids, and ahead of it there.
+    const int bucket0 = ids[0] / p.R;
+    int n = 0;
+    for (int i = tid; i < bucket0; i += kEgThreads) n += p.distinct[i];
+    n = __reduce_add_sync(0xffffffffu, n);
+    if ((tid & 31) == 0) part_sum[tid >> 5] = n;
+    __syncthreads();
+    if (tid < w1 - w0) {
+      n = 0;
+      for (int i = 0; i < kEgThreads / 32; ++i) n += part_sum[i];
+      const int v = ids[tid], bucket = v / p.R;
+#pragma unroll 4
+      for (int i = bucket0; i < bucket; ++i) n += p.distinct[i];
+      out_rows[tid] = n + p.place[v];
+    }
+  } else if (tid < w1 - w0) {
+    out_rows[tid] = ids[tid];
+  }
+  __syncthreads();
+
+  float sum[kEgEach] = {};
+#pragma unroll 1
+  for (int x = x0; x < x1; x += kEgAhead) {
+    EgRow<kType, kVec> g[kEgAhead];
+#pragma unroll
+    for (int u = 0; u < kEgAhead; ++u)
+      if (x + u < x1) g[u].load(p, rows[x + u - x0], slice);
+#pragma unroll
+    for (int u = 0; u < kEgAhead; ++u) {
+      if (x + u >= x1) break;
+#pragma unroll
+      for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u].get(i));
+      // (places behind the window belong to the last piece)
+      const int k = min(x + u, w1 - 1) - w0, begin = firsts[k], end = ends[k], next = x + u + 1;
+      if (next != end && (next - begin) % p.S != 0) continue;
+      if (end - begin > p.S) {
+        // One of several pieces.
+        const int from = begin + (x + u - begin) / p.S * p.S;
+        const long long width = static_cast<long long>(p.slices) * kEgSlice;
+        float* mine = p.partial + (2ll * (from / p.S) + (from == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
+#pragma unroll
+        for (int i = 0; i < kEgEach; ++i) { mine[i * kEgThreads] = sum[i]; sum[i] = 0.f; }
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+          const unsigned n = static_cast<unsigned>((end - begin + p.S - 1) / p.S);
+          last_here = atomicAdd(&p.done[static_cast<long long>(begin / p.S) * p.slices + slice], 1u) == n - 1 ? 1 : 0;
+        }
+        __syncthreads();
+        const bool all_there = last_here != 0;
+        __syncthreads();
+        if (!all_there) continue;
+        __threadfence();
+#pragma unroll 4
+        for (int b = begin; b < end; b += p.S) {
+          const float* y = p.partial + (2ll * (b / p.S) + (b == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
+#pragma unroll
+          for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], __ldcg(y + i * kEgThreads));
+        }
+      }
+      if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(ids[k] + p.v_offset);
+      eg_write<kVec>(p, out_type, out_rows[k], slice, sum);
+#pragma unroll
+      for (int i = 0; i < kEgEach; ++i) sum[i] = 0.f;
+    }
+  }
+}
+
+struct EgLayout {
+  size_t perm, sorted, first, place, distinct, done, partial, total;
+};
+
+// Host: the cut of the work.  False: sizes that are not served.
+bool eg_plan(long long N, int V, int H, int num_sms, EgParams* p, EgLayout* l) {
+  if (N < 0 || N >= INT32_MAX || V <= 0 || H <= 0 || V > INT32_MAX - 2) return false;
+  int R = (V + num_sms - 1) / num_sms;
+  if (R > kEsMaxIds) R = kEsMaxIds;
+  p->R = R;
+  p->buckets = (V + R - 1) / R;
+  int warps = 1;
+  while (warps < kEsWarps && N > 64ll * warps) warps <<= 1;      // a warp's stretch: 64 tokens, or more once all count
+  p->warps = warps;
+  p->chunk = static_cast<int>(((N + warps - 1) / warps + 31) / 32 * 32);
+  if (p->chunk == 0) p->chunk = 32;
+  int S = 64;
+  while (S < kEgMaxPiece && N > 256ll * S) S <<= 1;
+  p->S = S;
+  p->slices = (H + kEgSlice - 1) / kEgSlice;
+  int window = kEgMaxWindow;
+  while (window > 4 && (N + window - 1) / window * p->slices < 4ll * num_sms) window >>= 1;
+  p->window = window;
+  const size_t pieces = static_cast<size_t>((N + S - 1) / S);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  l->perm = take(static_cast<size_t>(N) * 4);
+  l->sorted = take(static_cast<size_t>(N) * 4);
+  l->first = take((static_cast<size_t>(V) + 1) * 4);
+  l->place = take(static_cast<size_t>(V) * 4);
+  l->distinct = take(static_cast<size_t>(p->buckets) * 4);
+  l->done = take(pieces * p->slices * 4);
+  l->partial = take(2 * pieces * p->slices * kEgSlice * 4);
+  l->total = at;
+  return true;
+}
+
+template <int kType>
+cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStream_t stream) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
+  cfg.gridDim = dim3(static_cast<unsigned>(p.buckets)); cfg.blockDim = dim3(kEsThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(p.R) * p.warps * 4;
+  cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsMaxIds * kEsWarps * 4);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, embed_sort_kernel, p);
+  if (e != cudaSuccess) return e;
+  const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
+  const long long blank = p.by_rows || p.accumulate ? 0 : (static_cast<long long>(p.V) + kEgMaxWindow - 1) / kEgMaxWindow;
+  cfg.gridDim = dim3(static_cast<unsigned>((windows + blank) * p.slices)); cfg.blockDim = dim3(kEgThreads);
+  cfg.dynamicSmemBytes = 0;
+  return vec ? cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, true>, p, out_type, static_cast<int>(windows))
+             : cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, false>, p, out_type, static_cast<int>(windows));
+}

@@ -1,0 +1,410 @@
+"""Rows of a table by token, equal to the bit with the same operations in fp32, and the gradient of the table against 64 bits."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2506_18952_b200 import binding
+
+gpu = pytest.mark.gpu
+FLOATS = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def rnd(shape, dtype, seed, std=1.0):
+    return (torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda") * std).to(dtype)
+
+
+def some_tokens(N, V, seed, dtype=torch.int32, absent=0.1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = torch.exp(torch.rand((N,), generator=g, device="cuda", dtype=torch.float64) * math.log(V + 1.0)) - 1.0
+    t = torch.where(torch.rand((N,), generator=g, device="cuda") < absent, -1, t.long().clamp_(0, V - 1))
+    return t.to(dtype)
+
+
+def looked_up(tokens, rows32, scale, add, dtype):
+    """rows32: the table in fp32.  One rounding for the product, one for the sum, one for the result's type."""
+    t = tokens.long()
+    inside = (t >= 0) & (t < rows32.shape[0])
+    y = torch.where(inside[..., None], rows32[t.clamp(0, rows32.shape[0] - 1)] * scale, 0.0)
+    return (y if add is None else add.float() + y).to(dtype)
+
+
+# ------------------------------------------------------------------------------------------------ lookup
+@gpu
+@pytest.mark.parametrize("table_dtype", [*FLOATS, torch.int8])
+@pytest.mark.parametrize("N,V,H", [(1, 1, 1), (1, 5, 8), (3, 7, 5), (2, 100, 64), (5, 1000, 4096), (17, 33, 1000), (130, 500, 2056), (9, 50, 8200),
+                                   (4000, 3000, 128), (2500, 100, 2048)])
+def test_rows_of_every_type(N, V, H, table_dtype):
+    t32 = some_tokens(N, V, N)
+    scale = rnd((V,), torch.float32, 1).abs() * 0.01 if table_dtype == torch.int8 else None
+    table = rnd((V, H), torch.float32, 2, 30.0).to(table_dtype) if scale is not None else rnd((V, H), table_dtype, 2)
+    rows32 = table.float() * scale[:, None] if scale is not None else table.float()
+    for dtype in FLOATS:
+        for s, with_add, wide in ((1.0, False, False), (math.sqrt(H), False, True), (0.35, True, False)):
+            tokens = t32.long() if wide else t32
+            add = rnd((N, H), dtype, 3) if with_add else None
+            got = binding.hola_embed(tokens, table, scale=s, add=add, w_scale=scale, dtype=dtype)
+            assert got.dtype == dtype and torch.equal(got, looked_up(tokens, rows32, s, add, dtype))
+
+
+@gpu
+@pytest.mark.parametrize("V,H", [(256, 128), (700, 256), (3000, 1024)])
+def test_rows_of_a_head_of_mixed_widths(V, H):
+    W = rnd((V, H), torch.bfloat16, 4)
+    groups = -(-V // 256)
+    for widths in ([(4, 8, 16)[i % 3] for i in range(groups)], [4] * groups, [8] * groups, [16] * groups):
+        head = binding.hola_quantize_mixed(W, widths)
+        codes = torch.empty((V, H), device="cuda")
+        at = {4: 0, 8: 0, 16: 0}
+        for g, width in enumerate(widths):
+            n = min(256, V - 256 * g)
+            r = slice(at[width], at[width] + n)
+            if width == 16:
+                part = head.W16[r].float()
+            elif width == 8:
+                part = head.W8[r].float()
+            else:
+                b = head.W4[r].int()
+                both = torch.stack([(b << 28) >> 28, (b << 24) >> 28], dim=2).reshape(n, H)
+                part = (both << head.shift4[:, r].t().int().repeat_interleave(128, dim=1)).float()
+            codes[256 * g:256 * g + n] = part
+            at[width] += n
+        rows32 = codes * head.w_scale[:, None]
+        tokens = torch.arange(-1, V, device="cuda", dtype=torch.int32)
+        assert torch.equal(binding.hola_embed(tokens, head, scale=1.7), looked_up(tokens, rows32, 1.7, None, torch.bfloat16))
+        # rows on odd addresses: channel by channel
+        out = torch.zeros((V + 1, H + 1), device="cuda")
+        binding.hola_embed(tokens, head, scale=0.3, out=out[:, 1:])
+        assert torch.equal(out[:, 1:], looked_up(tokens, rows32, 0.3, None, torch.float32)) and (out[:, 0] == 0).all()
+    # and those that the LM head itself multiplies with: W8 is the quantiser's
+    q, scale = binding.hola_quantize_w8(W)
+    tokens = torch.arange(V, device="cuda", dtype=torch.int32)
+    assert torch.equal(binding.hola_embed(tokens, q, w_scale=scale), binding.hola_embed(tokens, binding.hola_quantize_mixed(W, [8] * groups)))
+
+
+@gpu
+@pytest.mark.parametrize("H", [7, 64, 1000])
+def test_strides_shapes_and_results_in_place(H):
+    V = 90
+    table = rnd((V, H + 3), torch.float32, 1)[:, :H]          # rows further apart
+    tokens = some_tokens(24, V, 2).view(2, 3, 4)
+    want = looked_up(tokens, table, 2.0, None, torch.float32)
+    assert torch.equal(binding.hola_embed(tokens, table, 2.0), want)
+    buf = torch.full((2, 3, 4, H + 5), math.nan, device="cuda")
+    got = binding.hola_embed(tokens, table, 2.0, out=buf[..., :H])
+    assert got.data_ptr() == buf.data_ptr() and torch.equal(buf[..., :H], want) and buf[..., H:].isnan().all()
+    x = rnd((2, 3, 4, H), torch.float32, 5)
+    want = looked_up(tokens, table, 2.0, x, torch.float32)
+    binding.hola_embed(tokens, table, 2.0, add=x, out=x)      # onto what is there
+    assert torch.equal(x, want)
+    row = rnd((1, 1, 1, H), torch.float32, 6).expand(2, 3, 4, H)                  # one row for all
+    assert torch.equal(binding.hola_embed(tokens, table, 2.0, add=row), looked_up(tokens, table, 2.0, row, torch.float32))
+    assert binding.hola_embed(tokens[:0], table).shape == (0, 3, 4, H)
+    assert binding.hola_embed(tokens[0, 0, 0], table).shape == (H,)
+
+
+@gpu
+def test_tokens_that_there_are_not():
+    V, H = 50, 40
+    table = rnd((V, H), torch.float32, 1)
+    for dtype in (torch.int32, torch.int64):
+        t = torch.tensor([0, -1, 49, 50, -2, 2 ** 31 - 1, -2 ** 31, 7], device="cuda").to(dtype)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        got = binding.hola_embed(t, table, status=status)
+        assert torch.equal(got, looked_up(t, table, 1.0, None, torch.float32)) and (got[[1, 3, 4, 5, 6]] == 0).all()
+        assert status.item() == binding.FLAG_BAD_TOKEN
+        status.zero_()
+        binding.hola_embed(t[:3].contiguous(), table, status=status)
+        assert status.item() == 0
+        status.zero_()
+        got = binding.hola_embed_grad(t, torch.ones((8, H), device="cuda"), V, status=status)
+        assert status.item() == binding.FLAG_BAD_TOKEN and got.sum().item() == 3 * H and (got[[0, 49, 7]] == 1).all()
+    big = torch.tensor([2 ** 32, 2 ** 32 + 3, 2 ** 40 - 1], device="cuda")        # not 0, 3, -1 cut off
+    status.zero_()
+    assert (binding.hola_embed(big, table, status=status) == 0).all() and status.item() == binding.FLAG_BAD_TOKEN
+    assert (binding.hola_embed_grad(big, torch.ones((3, H), device="cuda"), V) == 0).all()
+
+
+@gpu
+def test_parts_of_a_vocabulary_add_up():
+    V, H, cuts = 1000, 72, [0, 130, 131, 600, 1000]
+    table = rnd((V, H), torch.bfloat16, 3)
+    tokens = some_tokens(300, V, 4)
+    grad = rnd((300, H), torch.float32, 5)
+    whole, dense = binding.hola_embed(tokens, table, 3.0), binding.hola_embed_grad(tokens, grad, V, 3.0)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = torch.zeros((300, H), dtype=torch.bfloat16, device="cuda")
+    ids = []
+    for a, b in zip(cuts, cuts[1:]):
+        got = binding.hola_embed(tokens, table[a:b], 3.0, add=got, v_offset=a, V_global=V, status=status)
+        assert torch.equal(binding.hola_embed_grad(tokens, grad, b - a, 3.0, v_offset=a, V_global=V, status=status), dense[a:b])
+        rows = binding.hola_embed_grad_rows(tokens, grad, b - a, 3.0, v_offset=a, V_global=V, status=status)
+        n = rows.count.item()
+        ids += rows.ids[:n].tolist()
+        assert torch.equal(rows.rows[:n], dense[rows.ids[:n].long()])
+    assert torch.equal(got, whole) and status.item() == 0
+    assert ids == sorted(set(tokens.tolist()) - {-1})
+
+
+# ------------------------------------------------------------------------------------------------ gradient
+def check_grad(tokens, grad, V, scale, got, before=None, rows=None):
+    """|error| <= (c + 2) 2^-24 scale sum |g| for c rows: at most c additions in fp32 (the pieces' own ones among them) and the product;
+    with what was there before, one more rounding of the sum; and half a step of the result's type."""
+    t, H = tokens.reshape(-1).long(), grad.shape[-1]
+    g = grad.reshape(-1, H).double()
+    inside = (t >= 0) & (t < V)
+    t, g = t[inside], g[inside]
+    want = torch.zeros((V, H), dtype=torch.float64, device="cuda").index_add_(0, t, g) * scale
+    size = torch.zeros((V, H), dtype=torch.float64, device="cuda").index_add_(0, t, g.abs()) * abs(scale)
+    count = torch.bincount(t, minlength=V).double()[:, None]
+    tol = (count + 2) * 2.0 ** -24 * size
+    if before is not None:
+        want = want + before.double()
+        tol = tol + 2.0 ** -24 * (want.abs() + size)
+    if rows is not None:
+        want, tol = want[rows], tol[rows]
+    eps = torch.finfo(got.dtype).eps / 2
+    tiny = torch.finfo(got.dtype).smallest_normal * eps       # (steps below the smallest normal number)
+    over = (got.double() - want).abs() - (tol * (1 + eps) + eps * want.abs() + (tiny if got.dtype != torch.float32 else 0))
+    assert float(over.max()) <= 0, float(over.max())
+    if before is None and rows is None:
+        assert (got[count[:, 0] == 0] == 0).all()
+
+
+SIZES = [(1, 1, 1), (1, 300, 8), (2, 5, 7), (33, 4, 64), (65, 2, 1000), (320, 5000, 4096), (200, 7, 1032), (1000, 1000, 72), (5000, 40, 128), (3000, 128256, 256),
+         (20000, 3, 16), (70000, 500, 8)]
+
+
+@gpu
+@pytest.mark.parametrize("g_dtype", FLOATS)
+@pytest.mark.parametrize("N,V,H", SIZES)
+def test_gradients_of_all_sizes(N, V, H, g_dtype):
+    tokens, grad = some_tokens(N, V, N + V), rnd((N, H), g_dtype, H)
+    for dtype, scale, wide in ((torch.float32, 1.0, False), (torch.bfloat16, math.sqrt(H), True), (torch.float16, 0.01, False)):
+        t = tokens.long() if wide else tokens
+        got = binding.hola_embed_grad(t, grad, V, scale, dtype=dtype)
+        check_grad(t, grad, V, scale, got)
+        assert torch.equal(got, binding.hola_embed_grad(t, grad, V, scale, dtype=dtype))          # the same bits
+        base = rnd((V, H), dtype, 9)
+        more = base.clone()
+        binding.hola_embed_grad(t, grad, V, scale, out=more, accumulate=True)
+        check_grad(t, grad, V, scale, more, before=base)
+        untouched = torch.ones(V, dtype=torch.bool, device="cuda")
+        untouched[tokens[tokens >= 0].long()] = False
+        assert torch.equal(more[untouched], base[untouched])
+        mark = binding.TokenRows(torch.full((N,), -7, dtype=torch.int32, device="cuda"), torch.full((N, H), -7.0, dtype=dtype, device="cuda"),
+                                 torch.full((1,), -7, dtype=torch.int32, device="cuda"))
+        rows = binding.hola_embed_grad_rows(t, grad, V, scale, out=mark)
+        n = rows.count.item()
+        want = sorted(set(tokens.tolist()) - {-1})
+        assert rows.ids[:n].tolist() == want and (rows.ids[n:] == -7).all() and (rows.rows[n:] == -7).all()
+        assert torch.equal(rows.rows[:n], got[rows.ids[:n].long()])
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["one", "two", "all", "none", "last", "runs"])
+def test_tokens_that_occur_never_once_and_always(kind):
+    """One token throughout (many pieces, the last CTA adds them up), tokens at the borders of ranges and pieces."""
+    N, V, H = 40000, 3001, 40
+    g = torch.Generator(device="cuda").manual_seed(1)
+    t = {"one": lambda: torch.full((N,), 1234), "two": lambda: torch.arange(N) % 2 * 3000, "all": lambda: torch.arange(N) % V,
+         "none": lambda: torch.full((N,), -1), "last": lambda: torch.where(torch.arange(N) < N - 1, -1, 3000),
+         "runs": lambda: torch.repeat_interleave(torch.arange(V), torch.randint(0, 27, (V,), generator=torch.Generator().manual_seed(2)))[:N]}[kind]()
+    t = t.cuda().to(torch.int32)
+    grad = torch.randn((t.numel(), H), generator=g, device="cuda")
+    got = binding.hola_embed_grad(t, grad, V)
+    check_grad(t, grad, V, 1.0, got)
+    rows = binding.hola_embed_grad_rows(t, grad, V)
+    n = rows.count.item()
+    assert rows.ids[:n].tolist() == sorted(set(t.tolist()) - {-1})
+    assert torch.equal(rows.rows[:n], got[rows.ids[:n].long()])
+
+
+@gpu
+def test_pieces_of_every_length():
+    """Runs of 1 .. 300 equal tokens, so that pieces end inside and at the ends of windows; whole numbers: exact sums."""
+    V, H = 300, 24
+    t = torch.repeat_interleave(torch.arange(V), torch.arange(1, V + 1)).cuda().to(torch.int32)
+    t = t[torch.randperm(t.numel(), generator=torch.Generator().manual_seed(3)).cuda()]
+    grad = torch.randint(-8, 9, (t.numel(), H), device="cuda", generator=torch.Generator(device="cuda").manual_seed(4)).float()
+    want = torch.zeros((V, H), dtype=torch.float64, device="cuda").index_add_(0, t.long(), grad.double()).float()
+    assert torch.equal(binding.hola_embed_grad(t, grad, V), want)
+    assert torch.equal(binding.hola_embed_grad(t, grad.bfloat16(), V), want)
+
+
+@gpu
+def test_vocabularies_of_any_size():
+    for V in (1, 2, 147, 148, 149, 1536 * 148, 1536 * 148 + 1, 3000001):
+        t = torch.tensor([0, V - 1, V // 2, V - 1, 0, max(0, V - 2)], device="cuda")
+        grad = torch.arange(12.0, device="cuda").view(6, 2)
+        rows = binding.hola_embed_grad_rows(t, grad, V)
+        n = rows.count.item()
+        want = sorted(set(t.tolist()))
+        assert rows.ids[:n].tolist() == want
+        for i, v in enumerate(want):
+            assert torch.equal(rows.rows[i], grad[t == v].sum(dim=0))
+        if V < 10 ** 6:
+            assert torch.equal(binding.hola_embed_grad(t, grad, V), torch.zeros((V, 2), device="cuda").index_add_(0, t, grad))
+
+
+@gpu
+def test_strides_of_gradients():
+    N, V = 100, 30
+    t = some_tokens(N, V, 1).view(4, 25)
+    for H in (8, 9, 1024):
+        wide = rnd((4, 25, H + 8), torch.bfloat16, 2)
+        for grad in (wide[..., :H], wide[..., 1:H + 1], wide[:1, :1, :H].expand(4, 25, H)):       # (a broadcast one)
+            got = binding.hola_embed_grad(t, grad, V)
+            check_grad(t, grad, V, 1.0, got)
+            out = torch.full((V, H + 3), 7.0, device="cuda")
+            binding.hola_embed_grad(t, grad, V, out=out[:, 1:H + 1])
+            assert torch.equal(out[:, 1:H + 1], got) and (out[:, 0] == 7).all() and (out[:, H + 1:] == 7).all()
+    for N in (0, 1):
+        t, grad = torch.zeros(N, dtype=torch.int32, device="cuda"), torch.ones((N, 16), device="cuda")
+        assert binding.hola_embed_grad(t, grad, 5).sum().item() == 16 * N
+        assert binding.hola_embed_grad_rows(t, grad, 5).count.item() == N
+
+
+@gpu
+@pytest.mark.parametrize("H", [24, 25])
+def test_gradient_against_differences(H):
+    """f(W) = sum r * sin(lookup): its derivative along D, from the gradient and from (f(W + h D) - f(W - h D)) / 2 h with lookups in fp32,
+    everything behind them in 64.  The difference's own error is h^2 / 6 sum |r D^3| (the third derivative of sin is at most 1), the
+    lookups' roundings 2^-24 (|scale W| + h |scale D|) |r| / h, the gradient's 2^-24 (c + 3) of the sum of its terms."""
+    N, V, scale, h = 400, 60, 1.5, 2.0 ** -8
+    t, W, D = some_tokens(N, V, 1), rnd((V, H), torch.float32, 2), rnd((V, H), torch.float32, 3)
+    r = rnd((N, H), torch.float64, 4)
+    f = lambda w: float((r * torch.sin(binding.hola_embed(t, w.float(), scale).double())).sum())          # noqa: E731
+    x = binding.hola_embed(t, W, scale).double()
+    g = (r * torch.cos(x)).float()
+    got = float((binding.hola_embed_grad(t, g, V, scale).double() * D.double()).sum())
+    want = (f(W.double() + h * D.double()) - f(W.double() - h * D.double())) / (2 * h)
+    d = scale * D[t.long().clamp_min(0)].double().abs() * (t >= 0)[:, None]
+    w = scale * W[t.long().clamp_min(0)].double().abs()
+    tol = h * h / 6 * (r.abs() * d ** 3).sum() + 2 * 2.0 ** -24 / h * (r.abs() * (w + h * d)).sum() + 2.0 ** -24 * (N + 3) * (r.abs() * d).sum()
+    assert abs(got - want) <= float(tol) and abs(want) > 4 * float(tol)
+
+
+@gpu
+def test_streams_graphs_and_two_calls_at_once():
+    N, V, H = 5000, 700, 256
+    tokens = [some_tokens(N, V, i) for i in (1, 2)]
+    grads = [rnd((N, H), torch.bfloat16, i) for i in (3, 4)]
+    table = rnd((V, H), torch.bfloat16, 5)
+    want = [(binding.hola_embed_grad(t, g, V), binding.hola_embed(t, table)) for t, g in zip(tokens, grads)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [(i, binding.hola_embed_grad(tokens[i], grads[i], V, stream=streams[i]), binding.hola_embed(tokens[i], table, stream=streams[i]))
+           for _ in range(10) for i in (0, 1)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want[i][0]) and torch.equal(b, want[i][1]) for i, a, b in got)
+    # two graphs of the same kind, replayed by turns and together
+    graphs = []
+    for i in (0, 1):
+        t, g, out = tokens[i].clone(), grads[i].clone(), torch.zeros((V, H), device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            binding.hola_embed_grad(t, g, V, out=out)
+        graphs.append((graph, t, g, out))
+    for swap in (0, 1):
+        for i, (graph, t, g, out) in enumerate(graphs):
+            t.copy_(tokens[i ^ swap])
+            g.copy_(grads[i ^ swap])
+        torch.cuda.synchronize()
+        for (graph, _, _, _), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, want[i ^ swap][0]) for i, (_, _, _, out) in enumerate(graphs))
+
+
+@gpu
+def test_tables_and_gradients_beyond_32_bits():
+    """Rows that begin more than 2^32 bytes into a table or a gradient."""
+    V, H = 300001, 8192
+    table = torch.empty((V, H), dtype=torch.bfloat16, device="cuda")
+    t = torch.tensor([0, V - 1, 262144, 131072, V // 2], device="cuda")
+    table[t] = rnd((5, H), torch.bfloat16, 1)
+    assert torch.equal(binding.hola_embed(t, table), table[t])
+    grad = torch.as_strided(table, (5, H), (75000 * H, 1))                        # rows 0, 75000 .. 300000 of the same memory
+    grad.copy_(rnd((5, H), torch.bfloat16, 2))
+    rows = binding.hola_embed_grad_rows(t, grad, V)
+    order = torch.argsort(t)
+    assert rows.ids.tolist() == t[order].tolist() and torch.equal(rows.rows, grad[order].float())
+    del rows
+    out = binding.hola_embed_grad(t, grad, V, dtype=torch.bfloat16)
+    assert torch.equal(out[t], grad) and int(out.count_nonzero()) == int(grad.count_nonzero())
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+def _embed_args(**kw):
+    a = binding.hola_embed_args()
+    a.N, a.V, a.H, a.row_stride, a.out_stride = 4, 10, 16, 16, 16
+    a.tokens = a.table = a.out = 4096
+    for name, v in kw.items():
+        setattr(a, name, v)
+    return a
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(N=-1), 1), (dict(V=0), 1), (dict(H=0), 1), (dict(t_dtype=5), 1), (dict(out_dtype=3), 1), (dict(row_stride=-1), 1), (dict(out_stride=15), 1),
+    (dict(tokens=None), 1), (dict(table=None), 1), (dict(out=None), 1), (dict(t_dtype=3), 1), (dict(w_scale=4096), 1), (dict(t_dtype=4, w_scale=4096), 2),
+    (dict(t_dtype=4, w_scale=4096, H=128, out_stride=128), 1), (dict(v_offset=1), 1), (dict(v_offset=1, V_global=10), 1), (dict(v_offset=-1, V_global=20), 1),
+    (dict(tokens=4098), 1), (dict(tokens=4100, wide_tokens=1), 1), (dict(out=4098), 1), (dict(add=4097), 1), (dict(N=2 ** 31), 2), (dict(N=0), 0)])
+def test_lookups_that_are_refused(kw, status):
+    lib = binding.load_library()
+    assert lib.hola_embed(ctypes.byref(_embed_args(**kw)), None) == status
+    assert lib.hola_embed(None, None) == 1
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(N=-1), 1), (dict(V=0), 1), (dict(H=0), 1), (dict(g_dtype=3), 1), (dict(out_dtype=3), 1), (dict(out_stride=15), 1), (dict(tokens=None), 1),
+    (dict(grad=None), 1), (dict(out=None), 1), (dict(workspace=None), 1), (dict(workspace=4097), 1), (dict(workspace_bytes=100), 1), (dict(ids_out=4096), 1),
+    (dict(count_out=4096), 1), (dict(ids_out=4096, count_out=4096, accumulate=1), 1), (dict(N=2 ** 31 - 1), 2), (dict(V=2 ** 31 - 1), 2), (dict(grad=4098), 1),
+    (dict(v_offset=1), 1), (dict(v_offset=5, V_global=12), 1)])
+def test_gradients_that_are_refused(kw, status):
+    lib = binding.load_library()
+    a = binding.hola_embed_grad_args()
+    a.N, a.V, a.H, a.grad_stride, a.out_stride, a.workspace_bytes = 4, 10, 16, 16, 16, lib.hola_embed_grad_workspace_bytes(4, 10, 16)
+    a.tokens = a.grad = a.out = a.workspace = 4096
+    for name, v in kw.items():
+        setattr(a, name, v)
+    assert lib.hola_embed_grad(ctypes.byref(a), None) == status
+    assert lib.hola_embed_grad(None, None) == 1
+    assert lib.hola_embed_grad_workspace_bytes(-1, 10, 16) == 0 and lib.hola_embed_grad_workspace_bytes(4, 0, 16) == 0
+
+
+def test_layout_of_the_structs():
+    assert ctypes.sizeof(binding.hola_embed_args) == 8 + 16 + 8 + 8 + 4 * 8 + 8 + 5 * 8
+    assert ctypes.sizeof(binding.hola_embed_grad_args) == 8 + 16 + 8 + 8 + 2 * 8 + 8 + 2 * 8 + 8 + 5 * 8
+
+
+def test_tensors_without_a_device_are_refused():
+    t, w = torch.zeros(3, dtype=torch.int32), torch.zeros((5, 8))
+    for call in (lambda: binding.hola_embed(t, w), lambda: binding.hola_embed_grad(t, torch.zeros((3, 8)), 5),
+                 lambda: binding.hola_embed_grad_rows(t, torch.zeros((3, 8)), 5), lambda: binding.hola_embed([1, 2], w)):
+        with pytest.raises(binding.HolaError):
+            call()
+
+
+@gpu
+def test_operands_that_are_refused():
+    t, w = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros((5, 8), device="cuda")
+    g = torch.zeros((3, 8), device="cuda")
+    s = torch.ones(5, device="cuda")
+    for kw in (dict(tokens=t.short()), dict(tokens=t.cpu()), dict(tokens=torch.zeros(6, dtype=torch.int32, device="cuda")[::2]), dict(table=w.double()),
+               dict(table=w[0]), dict(table=w.cpu()), dict(table=w.t()), dict(w_scale=s), dict(table=w.to(torch.int8)), dict(table=w.to(torch.int8), w_scale=s[:4]),
+               dict(add=g[:2]), dict(add=g.half(), dtype=torch.float32), dict(out=g[:, :7]), dict(out=g.t().contiguous().t()), dict(dtype=torch.int32),
+               dict(v_offset=1), dict(v_offset=2, V_global=6), dict(status=torch.zeros(1, device="cuda")), dict(add=g.cpu())):
+        with pytest.raises(binding.HolaError):
+            binding.hola_embed(**{"tokens": t, "table": w, **kw})
+    for kw in (dict(tokens=t.cpu()), dict(grad=g.double()), dict(grad=g[:2]), dict(grad=g[:, :1].expand(3, 8)), dict(V=0), dict(accumulate=True), dict(out=w[:4]),
+               dict(out=w.to(torch.int32)), dict(out=w.cpu()), dict(dtype=torch.int64), dict(out=w[:1].expand(5, 8))):
+        with pytest.raises(binding.HolaError):
+            binding.hola_embed_grad(**{"tokens": t, "grad": g, "V": 5, **kw})
+    ids, rows, count = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros((3, 8), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for out in (binding.TokenRows(ids[:2], rows, count), binding.TokenRows(ids, rows[:2], count), binding.TokenRows(ids, rows, ids),
+                binding.TokenRows(ids.long(), rows, count), binding.TokenRows(ids, rows.cpu(), count)):
+        with pytest.raises(binding.HolaError):
+            binding.hola_embed_grad_rows(t, g, 5, out=out)

@@ -11,14 +11,15 @@ import sys
 import sysconfig
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(_PKG, "csrc", "hola_verify.cu")
-PARTS = [os.path.join(_PKG, "csrc", name) for name in ("adapters.cuh", "token_logprobs.cuh", "beams.cuh", "embedding.cuh")]      # what it includes
+SRC = [os.path.join(_PKG, "csrc", name) for name in ("hola_verify.cu", "decode_ops.cu")]
+PARTS = [os.path.join(_PKG, "csrc", name) for name in ("device_util.cuh", "logit_rows.cuh", "adapters.cuh", "token_logprobs.cuh", "beams.cuh",
+                                                       "embedding.cuh")]      # what they include
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "hola_verify.h")
 LIB = os.path.join(_PKG, "libhola_verify.so")
 HOST_SRC = os.path.join(_PKG, "csrc", "host_call.cpp")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC"]
+              "-shared", "-Xcompiler", "-fPIC", "--threads", "2"]
 
 
 def _older(out: str, *sources: str) -> bool:
@@ -58,7 +59,7 @@ def _link(cmd: list, out: str, wanted) -> None:
 
 
 def needs_build() -> bool:
-    return _older(LIB, SRC, *PARTS, HEADER)
+    return _older(LIB, *SRC, *PARTS, HEADER)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -66,7 +67,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return force or needs_build()
     if wanted():
         nvcc = os.environ.get("NVCC", "nvcc")
-        _link([nvcc, *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), SRC], LIB, wanted)
+        _link([nvcc, *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []), *SRC], LIB, wanted)
     return LIB
 
 

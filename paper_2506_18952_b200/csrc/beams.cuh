@@ -1,6 +1,5 @@
 // beams.cuh - one step of a beam search around the LM head: the best continuations over all beams and the vocabulary, and the beams'
-// states put in the order of their parents.  Part of hola_verify.cu (inside its anonymous namespace, behind token_logprobs.cuh, whose
-// groups of 32 bytes and rows it uses).
+// states put in the order of their parents.  Part of decode_ops.cu (inside its anonymous namespace).
 //
 // Selection.  Candidate (w, v) of a sequence has c = (score[w] - logZ[w]) + l[w][v] and the key c * weight[w], both in 64 bits; the n
 // first in the order (key descending, beam ascending, logit descending, id ascending) are kept.  One pass over the logits in 32 bits:
@@ -73,12 +72,15 @@ __device__ __noinline__ BsCand bs_take_in(BsCand best, const BsCand* waiting, in
   return best;
 }
 
-// A live beam's row, and this CTA's part of it.
+// A live beam's row, and this CTA's part of its whole groups of 32 bytes.  The first and the last group, where they lack entries, are the
+// first CTA's (`edge`, or -1).
 struct BsRow {
   double off, weight;
   const void* row;
+  const unsigned char* at;             // group `begin`
   float b, w32;
-  int beam, j_begin, j_end;
+  int beam, begin, count, rounds;      // rounds of kBsThreads groups
+  int edge[2];
 };
 
 template <typename T>
@@ -93,7 +95,7 @@ struct BsShared {
   uint8_t looked_at[kBsWarps][32];
   unsigned bad_from[kBsMaxCluster];    // rows that hold NaN or +inf, as every CTA of the cluster has found them
   unsigned bad_here;
-  int live, n_own, n_all;
+  int rounds, n_own, n_all;
   float b_max;
 };
 
@@ -102,34 +104,6 @@ __device__ __forceinline__ float bs_approx(float l, float w32, float b) {
   const float a = fmaf(l, w32, b);
   return fabsf(a) == CUDART_INF_F && fabsf(l) != CUDART_INF_F ? copysignf(3.402823466e38f, a) : a;
 }
-
-// Walks a part: rounds of kBsThreads groups of one row, row after row.  The same for all threads but for j.
-template <typename T>
-struct BsWalk {
-  const BsRow* rows;
-  int live, li, j, j_end, round_end;
-  LpRow<T> r;
-  __device__ __forceinline__ BsWalk(const BsRow* rows_, int live_, int V) : rows(rows_), live(live_), li(-1), j(0), j_end(0), round_end(0),
-                                                                          r(nullptr, V) { row(V); }
-  // On to the next row that has groups in this part.
-  __device__ __forceinline__ void row(int V) {
-    while (++li < live) {
-      if (rows[li].j_begin >= rows[li].j_end) continue;
-      r = LpRow<T>(static_cast<const T*>(rows[li].row), V);
-      j_end = rows[li].j_end;
-      j = rows[li].j_begin + static_cast<int>(threadIdx.x);
-      round_end = rows[li].j_begin + kBsThreads;
-      return;
-    }
-  }
-  __device__ __forceinline__ bool done() const { return li >= live; }
-  __device__ __forceinline__ LpGroup<T> get() const { return j < j_end ? r.get(j) : LpRow<T>::none(); }
-  __device__ __forceinline__ void next(int V) {
-    if (round_end >= j_end) { row(V); return; }
-    j += kBsThreads;
-    round_end += kBsThreads;
-  }
-};
 
 // Entries of group j of a row whose a is at least thr, as candidates.
 template <typename T>
@@ -197,42 +171,76 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
         BsRow& row = s.rows[__popc(live_mask & ((1u << lane) - 1u))];
         const T* at = static_cast<const T*>(p.logits) + static_cast<size_t>(seq) * p.seq_stride + static_cast<size_t>(lane) * p.beam_stride;
         const LpRow<T> r(at, p.V);
-        const int per = (r.groups + C - 1) / C;
+        const int whole = max(r.whole_end - r.whole_begin, 0), per = (whole + C - 1) / C, first = min(part * per, whole);
         row.off = off; row.weight = weight; row.row = at; row.b = b; row.w32 = weight; row.beam = lane;
-        row.j_end = min(r.groups, (part + 1) * per);
-        row.j_begin = min(part * per, row.j_end);
+        row.begin = r.whole_begin + first;
+        row.count = min(per, whole - first);
+        row.rounds = (row.count + kBsThreads - 1) / kBsThreads;
+        row.at = reinterpret_cast<const unsigned char*>(r.base) + static_cast<size_t>(row.begin) * kLpGroupBytes;
+        row.edge[0] = part == 0 && r.whole_begin == 1 ? 0 : -1;
+        row.edge[1] = part == 0 && r.whole_end < r.groups && r.whole_end >= r.whole_begin ? r.whole_end : -1;
       }
       const float most = warp_max_f32(live_mask >> lane & 1u ? fabsf(b) : 0.f);
       if (lane == 0) s.b_max = most;
+      __syncwarp();
+      const int rounds = __reduce_add_sync(0xffffffffu, lane < live ? s.rows[lane].rounds : 0);
+      if (lane == 0) s.rounds = rounds;
     }
     __syncthreads();
 
-    // The pass.
+    // The pass, all rows' rounds one after the other: kBsAhead of them on the way.  (A thread without a group in a round takes the
+    // part's last one again and sets it aside: no lane waits for another's load.)
     float m = -CUDART_INF_F, second = -CUDART_INF_F;
-    int at_li = 0, at_j = 0, steps = 0;                  // steps: rounds of this part
+    int at = 0;                                          // round of the largest; from s.rounds on: an edge
+    const int rounds = s.rounds;
+    auto take = [&](float top, float w32, float b, bool have, int beam, int where) {
+      if (!(top < CUDART_INF_F)) atomicOr(&s.bad_here, 1u << beam);
+      const float a = have ? bs_approx(top, w32, b) : -CUDART_INF_F;
+      second = fmaxf(second, fminf(a, m));
+      if (a > m) at = where;
+      m = fmaxf(m, a);
+    };
     {
-      BsWalk<T> ahead(s.rows, live, p.V), here(s.rows, live, p.V);
+      int li_a = -1, left_a = 0, j_a = 0, last_a = 0;      // the round that is loaded next
+      int li = -1, left = 0, spare = 0, beam = 0;          // the one that is looked at; spare > 0: this thread has a group in it
+      float w32 = 1.f, b = 0.f;
+      const unsigned char* row_at = nullptr;
       LpGroup<T> next[kBsAhead];
+      auto load = [&](LpGroup<T>& g) {
+        if (left_a == 0) {
+          do ++li_a; while (s.rows[li_a].rounds == 0);
+          left_a = s.rows[li_a].rounds; last_a = s.rows[li_a].count - 1; row_at = s.rows[li_a].at;
+          j_a = tid;
+        }
+        g.load(reinterpret_cast<const T*>(row_at + static_cast<size_t>(min(j_a, last_a)) * kLpGroupBytes));
+        j_a += kBsThreads;
+        --left_a;
+      };
 #pragma unroll
       for (int d = 0; d < kBsAhead; ++d)
-        if (!ahead.done()) { next[d] = ahead.get(); ahead.next(p.V); }
+        if (d < rounds) load(next[d]);
 #pragma unroll 1
-      while (!here.done()) {
+      for (int i = 0; i < rounds; i += kBsAhead) {
 #pragma unroll
         for (int d = 0; d < kBsAhead; ++d) {
-          if (here.done()) break;
+          if (i + d >= rounds) break;
           const float top = next[d].largest();
-          if (!ahead.done()) { next[d] = ahead.get(); ahead.next(p.V); }
-          const BsRow& row = s.rows[here.li];
-          const float a = bs_approx(top, row.w32, row.b);
-          if (!(top < CUDART_INF_F)) atomicOr(&s.bad_here, 1u << row.beam);
-          second = fmaxf(second, fminf(a, m));
-          if (a > m) { at_li = here.li; at_j = here.j; }
-          m = fmaxf(m, a);
-          here.next(p.V);
-          ++steps;
+          if (i + d + kBsAhead < rounds) load(next[d]);
+          if (left == 0) {
+            do ++li; while (s.rows[li].rounds == 0);
+            left = s.rows[li].rounds; spare = s.rows[li].count - tid; w32 = s.rows[li].w32; b = s.rows[li].b; beam = s.rows[li].beam;
+          }
+          take(top, w32, b, spare > 0, beam, i + d);
+          spare -= kBsThreads;
+          --left;
         }
       }
+    }
+    // (a thread of the first CTA for each edge)
+    const int my_edge = tid < 2 * live ? s.rows[tid >> 1].edge[tid & 1] : -1;
+    if (my_edge >= 0) {
+      const BsRow& row = s.rows[tid >> 1];
+      take(LpRow<T>(static_cast<const T*>(row.row), p.V).get_ragged(my_edge).largest(), row.w32, row.b, true, row.beam, rounds);
     }
 
     // The board: the n-th best of the threads' largest, taken together by eight or four.
@@ -261,7 +269,16 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
         thr = w - (2.384185791015625e-7f * (fabsf(w) + s.b_max) + 1e-37f);
       }
       const bool mine = m > -CUDART_INF_F && m >= thr, again = mine && second >= thr && second > -CUDART_INF_F;
-      if (mine && !again) bs_send(s, s.rows[at_li], p.V, at_j, thr);
+      if (mine && !again) {
+        if (at == rounds) {
+          bs_send(s, s.rows[tid >> 1], p.V, my_edge, thr);
+        } else {
+          int li = 0;
+          for (; at >= s.rows[li].rounds; ++li) at -= s.rows[li].rounds;
+          bs_send(s, s.rows[li], p.V, s.rows[li].begin + at * kBsThreads + tid, thr);
+        }
+      }
+      if (again && my_edge >= 0) bs_send(s, s.rows[tid >> 1], p.V, my_edge, thr);
       // threads with more than one such group: all of theirs, dealt out to the warp's lanes
       const unsigned look = __ballot_sync(0xffffffffu, again);
       if (look) {
@@ -270,10 +287,10 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
         const int who = __popc(look);
         // (step by step over the rows' rounds: lane i takes thread i % who of round i / who)
         for (int li = 0; li < live; ++li) {
-          const int n_rounds = (s.rows[li].j_end - s.rows[li].j_begin + kBsThreads - 1) / kBsThreads, total = n_rounds * who;
+          const int total = s.rows[li].rounds * who;
           for (int i = lane; i < total; i += 32) {
-            const int jj = s.rows[li].j_begin + (i / who) * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
-            if (jj < s.rows[li].j_end) bs_send(s, s.rows[li], p.V, jj, thr);
+            const int j = (i / who) * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
+            if (j < s.rows[li].count) bs_send(s, s.rows[li], p.V, s.rows[li].begin + j, thr);
           }
         }
       }
@@ -285,41 +302,42 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
       __syncthreads();                                   // (everyone has seen n_own)
       BsCand best = {0, 0};
       int waiting = 0;
+      // (a warp's lanes bring a group each, of one row or, edges, of several)
+      auto look = [&](const BsRow& row, int j) {
+        LpGroup<T> g = LpRow<T>::none();
+        const LpRow<T> r(static_cast<const T*>(row.row), p.V);
+        if (j >= 0) g = r.get(j);
+        const int v0 = r.first(j);
+        BsCand worst = {__shfl_sync(0xffffffffu, best.hi, p.n - 1), __shfl_sync(0xffffffffu, best.lo, p.n - 1)};
+        const float top = g.largest();
+        const bool any = j >= 0 && top > -CUDART_INF_F && bs_order((row.off + static_cast<double>(top)) * row.weight) >= worst.hi;
+        if (!__any_sync(0xffffffffu, any)) return;
+#pragma unroll 1
+        for (int e = 0; e < LpGroup<T>::kEntries; ++e) {
+          float l = -CUDART_INF_F;
+#pragma unroll
+          for (int i = 0; i < LpGroup<T>::kEntries; ++i) l = i == e ? g.entry(i) : l;
+          const BsCand c = {bs_order((row.off + static_cast<double>(l)) * row.weight), bs_low(row.beam, l, v0 + e)};
+          const bool in = any && l > -CUDART_INF_F && bs_before(c, worst);
+          const unsigned mask = __ballot_sync(0xffffffffu, in);
+          if (!mask) continue;
+          const int fit = __popc(mask);
+          if (waiting + fit > 32) {
+            best = bs_take_in(best, s.waiting[warp], waiting);
+            waiting = 0;
+            worst = {__shfl_sync(0xffffffffu, best.hi, p.n - 1), __shfl_sync(0xffffffffu, best.lo, p.n - 1)};
+          }
+          if (in) s.waiting[warp][waiting + __popc(mask & ((1u << lane) - 1u))] = c;
+          waiting += fit;
+        }
+      };
 #pragma unroll 1
       for (int li = 0; li < live; ++li) {
-        const BsRow& row = s.rows[li];
-        const LpRow<T> r(static_cast<const T*>(row.row), p.V);
 #pragma unroll 1
-        for (int j0 = row.j_begin + warp * 32; j0 < row.j_end; j0 += kBsThreads) {
-          const int jj = j0 + lane;
-          LpGroup<T> g = LpRow<T>::none();
-          if (jj < row.j_end) g = r.get(jj);
-          const int v0 = r.first(jj);
-          BsCand worst = {__shfl_sync(0xffffffffu, best.hi, p.n - 1), __shfl_sync(0xffffffffu, best.lo, p.n - 1)};
-          const float top = g.largest();
-          const bool any = jj < row.j_end && top > -CUDART_INF_F &&
-                           bs_order((row.off + static_cast<double>(top)) * row.weight) >= worst.hi;
-          if (!__any_sync(0xffffffffu, any)) continue;
-#pragma unroll 1
-          for (int e = 0; e < LpGroup<T>::kEntries; ++e) {
-            float l = -CUDART_INF_F;
-#pragma unroll
-            for (int i = 0; i < LpGroup<T>::kEntries; ++i) l = i == e ? g.entry(i) : l;
-            const BsCand c = {bs_order((row.off + static_cast<double>(l)) * row.weight), bs_low(row.beam, l, v0 + e)};
-            const bool in = any && l > -CUDART_INF_F && bs_before(c, worst);
-            const unsigned mask = __ballot_sync(0xffffffffu, in);
-            if (!mask) continue;
-            const int fit = __popc(mask);
-            if (waiting + fit > 32) {
-              best = bs_take_in(best, s.waiting[warp], waiting);
-              waiting = 0;
-              worst = {__shfl_sync(0xffffffffu, best.hi, p.n - 1), __shfl_sync(0xffffffffu, best.lo, p.n - 1)};
-            }
-            if (in) s.waiting[warp][waiting + __popc(mask & ((1u << lane) - 1u))] = c;
-            waiting += fit;
-          }
-        }
+        for (int j0 = warp * 32; j0 < s.rows[li].count; j0 += kBsThreads)
+          look(s.rows[li], j0 + lane < s.rows[li].count ? s.rows[li].begin + j0 + lane : -1);
       }
+      if (warp * 32 < 2 * live) look(s.rows[min(tid >> 1, live - 1)], my_edge);
       best = bs_take_in(best, s.waiting[warp], waiting);
       s.own[tid] = best;
       __syncthreads();

@@ -1,0 +1,216 @@
+// decode_ops.cu - sm_100a kernels and C ABI for what stands around the LM head in a decoder: a beam search's step, token embeddings and
+// their gradient.  See include/hola_verify.h for the contract.
+//
+// Kernels
+//   beam_select_kernel, beam_reorder_kernel  (beams.cuh) the best continuations of all beams of a sequence, and the beams' states in the
+//       order of their parents.
+//   embed_kernel                (embedding.cuh) rows of a table, the head's own storage forms among them, by token; embed_sort_kernel,
+//       embed_grad_kernel, the gradient of a table by sorted tokens.
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math_constants.h>
+#include <stdint.h>
+
+#include <cooperative_groups.h>
+
+#include <type_traits>
+
+#include "../../include/hola_verify.h"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+#include "device_util.cuh"
+#include "logit_rows.cuh"
+#include "beams.cuh"
+#include "embedding.cuh"
+
+}  // namespace
+
+extern "C" {
+
+// The current device's SM count; 0: no device that runs these kernels.
+static int current_sms() {
+  int dev = 0, sms = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10)
+    return 0;
+  return sms;
+}
+
+hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
+  if (!a || a->B < 0 || a->W <= 0 || a->V <= 0 || a->n <= 0 || a->seq_stride < 0 || a->beam_stride < 0) return HOLA_ERR_INVALID_ARG;
+  if (a->l_dtype < HOLA_L_F32 || a->l_dtype > HOLA_L_F16) return HOLA_ERR_INVALID_ARG;
+  if (a->W > kBsMaxBeams || a->n > kBsMaxKept || a->V > kBsMaxV || a->B > INT32_MAX / kBsMaxCluster) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (a->keep_slots && a->n != a->W) return HOLA_ERR_INVALID_ARG;
+  if (a->end_token < -1 || a->end_token >= a->V || (a->finished && a->end_token < 0)) return HOLA_ERR_INVALID_ARG;
+  if (a->B == 0) return HOLA_OK;
+  if (!a->logits || !a->logZ || !a->score || !a->score_out || !a->parent || !a->token) return HOLA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(a->logits) % (a->l_dtype == HOLA_L_F32 ? 4 : 2)) return HOLA_ERR_INVALID_ARG;
+  const int sms = current_sms();
+  if (!sms) return HOLA_ERR_NO_DEVICE;
+  BsParams p = {};
+  p.logits = a->logits; p.seq_stride = a->seq_stride; p.beam_stride = a->beam_stride; p.B = a->B; p.W = a->W; p.V = a->V; p.n = a->n;
+  p.logZ = a->logZ; p.score = a->score; p.finished = a->finished; p.weight = a->weight; p.end_token = a->end_token;
+  p.keep_slots = a->keep_slots; p.score_out = a->score_out; p.parent = a->parent; p.token = a->token; p.finished_out = a->finished_out;
+  p.status = a->status_word;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = a->l_dtype == HOLA_L_F32 ? launch_beam_select<float>(p, sms, stream)
+                        : a->l_dtype == HOLA_L_BF16 ? launch_beam_select<__nv_bfloat16>(p, sms, stream) : launch_beam_select<__half>(p, sms, stream);
+  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
+}
+
+hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
+  if (!a || a->B < 0 || a->W <= 0 || a->n <= 0 || a->count < 0 || a->parent_stride < 0) return HOLA_ERR_INVALID_ARG;
+  if (a->W > kBsMaxBeams || a->n > kBsMaxBeams) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (a->B == 0 || a->count == 0) return HOLA_OK;
+  if (!a->states || !a->parent) return HOLA_ERR_INVALID_ARG;
+  // (all states are looked at before the first launch)
+  int in_place = -1;
+  for (int i = 0; i < a->count; ++i) {
+    const hola_beam_state& s = a->states[i];
+    if (s.run < 0 || s.position < 0 || s.outer[0] < 0 || s.outer[1] < 0) return HOLA_ERR_INVALID_ARG;
+    if (s.run == 0 || s.outer[0] == 0 || s.outer[1] == 0) continue;
+    if (!s.src || !s.dst || s.seq_stride < 0 || s.beam_stride < 0 || s.outer_stride[0] < 0 || s.outer_stride[1] < 0 || s.dst_seq_stride < 0 ||
+        s.dst_beam_stride < 0 || s.dst_outer_stride[0] < 0 || s.dst_outer_stride[1] < 0)
+      return HOLA_ERR_INVALID_ARG;
+    const bool here = s.src == s.dst;
+    if (in_place >= 0 && in_place != static_cast<int>(here)) return HOLA_ERR_INVALID_ARG;
+    in_place = here;
+    if (here && (a->n > a->W || s.seq_stride != s.dst_seq_stride || s.beam_stride != s.dst_beam_stride ||
+                 s.outer_stride[0] != s.dst_outer_stride[0] || s.outer_stride[1] != s.dst_outer_stride[1]))
+      return HOLA_ERR_INVALID_ARG;
+    if ((a->n > 1 && s.dst_beam_stride < s.run) || (a->W > 1 && s.beam_stride < s.run)) return HOLA_ERR_INVALID_ARG;      // beams that share bytes
+    const long long pieces = (s.run - 1) / kBrPiece + 1;
+    if (pieces > INT32_MAX || s.outer[0] > INT32_MAX || s.outer[1] > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
+    const double ctas = static_cast<double>(pieces) * a->B * static_cast<double>(s.outer[0]) * static_cast<double>(s.outer[1]);
+    if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  }
+  if (in_place < 0) return HOLA_OK;
+  if (!current_sms()) return HOLA_ERR_NO_DEVICE;
+  BrParams p = {};
+  p.B = a->B; p.W = a->W; p.n = a->n; p.parent = a->parent; p.parent_stride = a->parent_stride; p.used = a->used; p.status = a->status_word;
+  p.in_place = in_place;
+  long long ctas = 0;
+  for (int i = 0; i <= a->count; ++i) {
+    long long more = 0, pieces = 0;
+    const hola_beam_state* s = i < a->count ? &a->states[i] : nullptr;
+    if (s) {
+      if (s->run == 0 || s->outer[0] == 0 || s->outer[1] == 0) continue;
+      pieces = (s->run - 1) / kBrPiece + 1;
+      more = pieces * a->B * s->outer[0] * s->outer[1];
+    }
+    if (p.count > 0 && (!s || p.count == kBrStates || ctas + more > INT32_MAX)) {
+      const cudaError_t e = launch_beam_reorder(p, static_cast<unsigned>(ctas), static_cast<cudaStream_t>(cuda_stream));
+      if (e != cudaSuccess) return HOLA_ERR_CUDA;
+      p.count = 0;
+      ctas = 0;
+    }
+    if (!s) break;
+    BrState& o = p.s[p.count++];
+    o.src = static_cast<const unsigned char*>(s->src); o.dst = static_cast<unsigned char*>(s->dst);
+    o.seq = s->seq_stride; o.beam = s->beam_stride; o.outer0 = s->outer_stride[0]; o.outer1 = s->outer_stride[1];
+    o.to_seq = s->dst_seq_stride; o.to_beam = s->dst_beam_stride; o.to_outer0 = s->dst_outer_stride[0]; o.to_outer1 = s->dst_outer_stride[1];
+    o.run = s->run; o.position = s->position;
+    o.n0 = static_cast<unsigned>(s->outer[0]); o.n1 = static_cast<unsigned>(s->outer[1]);
+    o.pieces = static_cast<unsigned>(pieces); o.first_cta = static_cast<unsigned>(ctas);
+    ctas += more;
+  }
+  return HOLA_OK;
+}
+
+// Whether n bytes at a time can be read or written of rows of `stride` elements.
+static bool in_words(const void* base, long long stride, int elem, unsigned bytes) {
+  return reinterpret_cast<uintptr_t>(base) % bytes == 0 && stride * elem % bytes == 0;
+}
+
+hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
+  if (!a || a->N < 0 || a->V <= 0 || a->H <= 0 || a->row_stride < 0 || a->add_stride < 0 || a->out_stride < 0) return HOLA_ERR_INVALID_ARG;
+  if (a->t_dtype < HOLA_T_F32 || a->t_dtype > HOLA_T_MIXED || a->out_dtype < HOLA_T_F32 || a->out_dtype > HOLA_T_F16) return HOLA_ERR_INVALID_ARG;
+  if (a->v_offset < 0 || a->V_global < 0 || (a->V_global > 0 && static_cast<long long>(a->v_offset) + a->V > a->V_global)) return HOLA_ERR_INVALID_ARG;
+  if (a->V_global == 0 && a->v_offset != 0) return HOLA_ERR_INVALID_ARG;
+  const bool mixed = a->t_dtype == HOLA_T_MIXED;
+  if (a->N > INT32_MAX || a->H > INT32_MAX - 65536 || (mixed && a->H % 128 != 0)) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (a->N == 0) return HOLA_OK;
+  if (!a->tokens || !a->out || (a->N > 1 && a->out_stride < a->H)) return HOLA_ERR_INVALID_ARG;
+  if (mixed) {
+    const hola_wmix* m = a->wmix;
+    if (!m || !m->group_width || !m->group_row || m->rows4 < 0 || m->rows8 < 0 || m->rows16 < 0 ||
+        static_cast<long long>(m->rows4) + m->rows8 + m->rows16 != a->V)
+      return HOLA_ERR_INVALID_ARG;
+    if ((m->rows4 > 0 && (!m->W4 || !m->shift4)) || (m->rows8 > 0 && !m->W8) || (m->rows16 > 0 && !m->W16)) return HOLA_ERR_INVALID_ARG;
+  } else if (!a->table) {
+    return HOLA_ERR_INVALID_ARG;
+  }
+  if ((mixed || a->t_dtype == HOLA_T_INT8) != (a->w_scale != nullptr)) return HOLA_ERR_INVALID_ARG;
+  const int te = mixed ? 1 : tab_bytes(a->t_dtype), oe = tab_bytes(a->out_dtype);
+  if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
+      reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
+    return HOLA_ERR_INVALID_ARG;
+  const int sms = current_sms();
+  if (!sms) return HOLA_ERR_NO_DEVICE;
+  EmParams p = {};
+  p.tokens = a->tokens; p.wide = a->wide_tokens; p.N = a->N; p.V = a->V; p.H = a->H; p.v_offset = a->v_offset;
+  p.V_global = a->V_global ? a->V_global : a->V;
+  p.table = a->table; p.row_stride = a->row_stride; p.w_scale = a->w_scale;
+  if (mixed) p.mix = *a->wmix;
+  p.scale = a->scale; p.add = a->add; p.add_stride = a->add_stride; p.out = a->out; p.out_stride = a->out_stride; p.status = a->status_word;
+  // (eight channels at a time: 8, 16 or 32 bytes)
+  bool words = a->H % 8 == 0 && in_words(a->out, a->out_stride, oe, 8 * oe) && (!a->add || in_words(a->add, a->add_stride, oe, 8 * oe));
+  if (mixed) words = words && in_words(p.mix.W16, 0, 1, 16) && in_words(p.mix.W8, 0, 1, 8) && in_words(p.mix.W4, 0, 1, 4);
+  else words = words && in_words(a->table, a->row_stride, te, 8 * te);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, sms, stream)
+                              : launch_embed_of<1>(p, a->t_dtype, a->out_dtype, sms, stream);
+  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
+}
+
+size_t hola_embed_grad_workspace_bytes(long long N, int V, int H) {
+  EgParams p = {};
+  EgLayout l;
+  return eg_plan(N, V, H, &p, &l) ? l.total : 0;
+}
+
+hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
+  if (!a || a->N < 0 || a->V <= 0 || a->H <= 0 || a->grad_stride < 0 || a->out_stride < 0) return HOLA_ERR_INVALID_ARG;
+  if (a->g_dtype < HOLA_T_F32 || a->g_dtype > HOLA_T_F16 || a->out_dtype < HOLA_T_F32 || a->out_dtype > HOLA_T_F16) return HOLA_ERR_INVALID_ARG;
+  if (a->v_offset < 0 || a->V_global < 0 || (a->V_global > 0 && static_cast<long long>(a->v_offset) + a->V > a->V_global)) return HOLA_ERR_INVALID_ARG;
+  if (a->V_global == 0 && a->v_offset != 0) return HOLA_ERR_INVALID_ARG;
+  const bool by_rows = a->ids_out || a->count_out;
+  if (by_rows && (!a->count_out || a->accumulate)) return HOLA_ERR_INVALID_ARG;
+  EgParams p = {};
+  EgLayout l;
+  if (!eg_plan(a->N, a->V, a->H, &p, &l)) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (a->N > 0 && (!a->tokens || !a->grad || (by_rows && (!a->ids_out || !a->out)))) return HOLA_ERR_INVALID_ARG;
+  if (!by_rows && !a->out) return HOLA_ERR_INVALID_ARG;
+  if (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 16 || a->workspace_bytes < l.total) return HOLA_ERR_INVALID_ARG;
+  if ((by_rows ? a->N : static_cast<long long>(a->V)) > 1 && a->out_stride < a->H) return HOLA_ERR_INVALID_ARG;
+  const int ge = tab_bytes(a->g_dtype), oe = tab_bytes(a->out_dtype);
+  if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->grad) % ge ||
+      reinterpret_cast<uintptr_t>(a->out) % oe)
+    return HOLA_ERR_INVALID_ARG;
+  const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + kEgMaxWindow - 1) / kEgMaxWindow) * p.slices;
+  if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (!current_sms()) return HOLA_ERR_NO_DEVICE;
+  p.tokens = a->tokens; p.wide = a->wide_tokens; p.v_offset = a->v_offset;
+  p.V_global = a->V_global ? a->V_global : a->V;
+  p.grad = a->grad; p.g_stride = a->grad_stride; p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;
+  p.accumulate = a->accumulate; p.by_rows = by_rows; p.ids_out = a->ids_out; p.count_out = a->count_out; p.status = a->status_word;
+  unsigned char* ws = static_cast<unsigned char*>(a->workspace);
+  p.places = reinterpret_cast<int4*>(ws + l.places); p.numbers = reinterpret_cast<int2*>(ws + l.numbers);
+  p.first = by_rows || a->accumulate ? nullptr : reinterpret_cast<int*>(ws + l.first);
+  p.distinct = reinterpret_cast<int*>(ws + l.distinct); p.valid = reinterpret_cast<int*>(ws + l.valid);
+  p.done = reinterpret_cast<unsigned*>(ws + l.done);
+  p.partial = reinterpret_cast<float*>(ws + l.partial);
+  const bool words = a->H % 8 == 0 && in_words(a->grad, a->grad_stride, ge, 8 * ge) && in_words(a->out, a->out_stride, oe, 8 * oe);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = a->g_dtype == HOLA_T_F32 ? launch_embed_grad<kTabF32>(p, a->out_dtype, words, stream)
+                        : a->g_dtype == HOLA_T_BF16 ? launch_embed_grad<kTabBf16>(p, a->out_dtype, words, stream)
+                                                    : launch_embed_grad<kTabF16>(p, a->out_dtype, words, stream);
+  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
+}
+
+}  // extern "C"

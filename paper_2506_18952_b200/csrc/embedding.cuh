@@ -1,4 +1,4 @@
-// embedding.cuh - rows of a table by token, and the gradient of the table.  Part of hola_verify.cu (inside its anonymous namespace).
+// embedding.cuh - rows of a table by token, and the gradient of the table.  Part of decode_ops.cu (inside its anonymous namespace).
 
 // ------------------------------------------------------------------------------------------------ lookup
 // out[r] = add[r] + scale * W[tok[r]], every operation one rounding in fp32 (the scale of a quantised row first), the result rounded
@@ -43,10 +43,10 @@ struct EmWord {
   uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
   __device__ __forceinline__ void load(const void* p) {
     if (kBytes == 32) {
-      const uint4 a = static_cast<const uint4*>(p)[0], b = static_cast<const uint4*>(p)[1];
-      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-      w[4 % (kBytes < 4 ? 1 : kBytes / 4)] = b.x; w[5 % (kBytes < 4 ? 1 : kBytes / 4)] = b.y;
-      w[6 % (kBytes < 4 ? 1 : kBytes / 4)] = b.z; w[7 % (kBytes < 4 ? 1 : kBytes / 4)] = b.w;
+      constexpr int k = kBytes < 4 ? 1 : kBytes / 4;
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1 % k]), "=r"(w[2 % k]), "=r"(w[3 % k]), "=r"(w[4 % k]), "=r"(w[5 % k]), "=r"(w[6 % k]), "=r"(w[7 % k])
+                   : "l"(p) : "memory");
     } else if (kBytes == 16) {
       const uint4 a = *static_cast<const uint4*>(p);
       w[0] = a.x; w[1 % (kBytes < 4 ? 1 : kBytes / 4)] = a.y; w[2 % (kBytes < 4 ? 1 : kBytes / 4)] = a.z;
@@ -75,8 +75,9 @@ template <int kType, int n>
 __device__ __forceinline__ void em_store(void* p, const float* x) {
   if (kType == kTabF32) {
     if (n == 8) {
-      static_cast<float4*>(p)[0] = make_float4(x[0], x[1 % n], x[2 % n], x[3 % n]);
-      static_cast<float4*>(p)[1] = make_float4(x[4 % n], x[5 % n], x[6 % n], x[7 % n]);
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(p), "f"(x[0]), "f"(x[1 % n]), "f"(x[2 % n]), "f"(x[3 % n]), "f"(x[4 % n]), "f"(x[5 % n]), "f"(x[6 % n]), "f"(x[7 % n])
+                   : "memory");
     } else {
       *static_cast<float*>(p) = x[0];
     }
@@ -233,16 +234,22 @@ cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_s
 // ------------------------------------------------------------------------------------------------ gradient
 // dW[v] = scale * sum of g[r] over the rows r with tok[r] = v, in rising r, in fp32.  Two launches.
 //
-// 1. Tokens sorted (stable), with nothing exchanged between the CTAs: each takes a range of `R` ids and reads all tokens, every warp a
-//    stretch of them.  It counts what lies below its range (where its part of the sorted order begins) and, per id and warp, what lies
-//    inside; a scan over (id, warp) gives every warp the place of its first occurrence of every id, and a second look at the tokens
-//    puts them there.  Bound by latency; N x 4 or 8 bytes per CTA out of the L2.
+// 1. Tokens sorted (stable), with nothing exchanged between the CTAs: each takes a range of ids and reads all tokens, every warp a
+//    stretch of them, lists those inside its range, and counts those below it (where its part of the sorted order begins).  Counts per
+//    (id, warp), and a scan over them, give every warp the place of its first occurrence of every id.  Ranges are cut at the even
+//    marks V j / U and at the marks (V + 1)^(i / Z) together, for vocabularies are numbered by falling frequency: no range holds more than
+//    1 / U of the ids nor, where p(id) is about 1 / (id + 1), much more than 1 / Z of the tokens (or one id).  Bound by latency;
+//    N x 4 or 8 bytes per CTA out of the L2.
 // 2. Sums.  The sorted order is cut into windows; the rows of a token lie side by side there, in pieces of at most `S`.  A CTA adds up
 //    the pieces that begin in its window, for a slice of kEgSlice channels.  A token with one piece is finished by it; the pieces of the others
 //    go to the workspace, and the CTA that comes last adds them up in their order.  So the result does not depend on the schedule.
 //    The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
 constexpr int kEsThreads = 1024, kEsWarps = 32;
-constexpr int kEsMaxIds = 1536;        // ids of a CTA of the sort: counters of 4 bytes per id and warp
+constexpr int kEsZipf = 74;            // Z
+constexpr int kEsList = 256;           // tokens that a warp lists before it counts them
+constexpr int kEsLoads = 4;            // 32 tokens each that a warp has on the way
+constexpr int kEsCellBytes = 128 * 1024;       // counters of a CTA
+constexpr int kEsIdBits = 11;          // ids of a range (with what is left of 32 bits for places in a warp's stretch)
 constexpr int kEgThreads = 128, kEgEach = 8;
 constexpr int kEgSlice = kEgThreads * kEgEach;
 constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
@@ -252,10 +259,9 @@ constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspac
 struct EgParams {
   const void* tokens;
   int wide;
-  long long N;                         // < 2^31
-  int V, H;
+  int N, V, H;
   long long v_offset, V_global;
-  int R, buckets, warps, chunk;        // sort: ids per CTA, CTAs, warps that count, tokens of a warp
+  int even, buckets, warps, chunk;     // sort: U, ranges of ids, warps that count, tokens of a warp
   int S, window, slices;
   const void* grad;
   long long g_stride;
@@ -266,142 +272,190 @@ struct EgParams {
   int* ids_out;                        // by_rows: the distinct tokens, rising
   int* count_out;
   // workspace
-  int* perm;                           // [N] rows in sorted order
-  int* sorted;                         // [N] their ids
-  int* first;                          // [V + 1] where an id's rows begin
-  int* place;                          // [V] by_rows: rank of an id among the CTA's distinct ones
+  int4* places;                        // [N] in sorted order: row, id, where the id's rows begin and end
+  int2* numbers;                       // [N] by_rows: the id's range, its number among the distinct ones there
+  int* first;                          // [V + 1] the whole table: where an id's rows begin
   int* distinct;                       // [buckets]
+  int* valid;                          // tokens that have a row
   unsigned* done;                      // [ceil(N / S)][slices] pieces of a token that have arrived
   float* partial;                      // [2 ceil(N / S)][slices * kEgSlice]
   unsigned* status;
 };
 
-__global__ void __launch_bounds__(kEsThreads) embed_sort_kernel(const __grid_constant__ EgParams p) {
-  extern __shared__ int es_counts[];                     // [R][warps]
-  __shared__ int warp_sum[kEsWarps], warp_below[kEsWarps], warp_distinct[kEsWarps];
-  __shared__ int base;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int lo = blockIdx.x * p.R, R = min(p.R, p.V - lo), cells = R * p.warps;
-  for (int i = tid; i < cells; i += kEsThreads) es_counts[i] = 0;
+// Number of even marks V j / U (1 <= j < U) that are at most x.
+__device__ __forceinline__ int es_even_upto(int x, int V, int U) {
+  const long long j = ((static_cast<long long>(x) + 1) * U - 1) / V;
+  return static_cast<int>(j < U - 1 ? j : U - 1);
+}
+
+// Cell: counters of a warp's tokens per id, 16 bits where there are few enough tokens.
+template <typename Cell>
+__global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_constant__ EgParams p) {
+  extern __shared__ __align__(16) unsigned char es_smem[];
+  __shared__ uint32_t list[kEsWarps][kEsList];
+  __shared__ int warp_below[kEsWarps];
+  __shared__ uint64_t warp_sum[kEsWarps];
+  __shared__ int mark[kEsZipf], range[2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = blockIdx.x;
+  // The range: marks g and g + 1 of both kinds together (even ones before equal others).
+  int place = 0;
+  if (tid < kEsZipf - 1) {
+    const float x = exp2f(log2f(static_cast<float>(p.V) + 1.f) * (static_cast<float>(tid + 1) / kEsZipf));
+    mark[tid] = static_cast<int>(fminf(x, static_cast<float>(p.V)));
+    mark[tid] = min(mark[tid], p.V);
+    place = tid + 1 + es_even_upto(mark[tid], p.V, p.even);
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int r = g + e;
+    const int before = __syncthreads_count(tid < kEsZipf - 1 && place < r);
+    if (tid == 0) range[e] = r == 0 ? 0 : r == p.buckets ? p.V : static_cast<int>(static_cast<long long>(p.V) * (r - before) / p.even);
+    __syncthreads();
+    if (tid < kEsZipf - 1 && place == r && r < p.buckets) range[e] = mark[tid];
+  }
+  __syncthreads();
+  const int lo = range[0], R = range[1] - lo;
+  // [warp][id] counters, then per id where its rows begin and how many distinct ids lie before it
+  Cell* cells = reinterpret_cast<Cell*>(es_smem);
+  int2* heads = reinterpret_cast<int2*>(es_smem + kEsCellBytes);
+  for (int i = tid; i < (R * p.warps * static_cast<int>(sizeof(Cell)) + 15) / 16; i += kEsThreads) reinterpret_cast<uint4*>(es_smem)[i] = make_uint4(0, 0, 0, 0);
   grid_dependency_wait();
   grid_dependency_release();
   // (counters of the second launch)
-  const long long pieces = (p.N + p.S - 1) / p.S * p.slices;
-  for (long long i = static_cast<long long>(blockIdx.x) * kEsThreads + tid; i < pieces; i += static_cast<long long>(p.buckets) * kEsThreads) p.done[i] = 0;
+  const long long pieces = static_cast<long long>((p.N + p.S - 1) / p.S) * p.slices;
+  for (long long i = static_cast<long long>(g) * kEsThreads + tid; i < pieces; i += static_cast<long long>(p.buckets) * kEsThreads) p.done[i] = 0;
   __syncthreads();
 
-  const long long begin = static_cast<long long>(warp) * p.chunk, end = begin + p.chunk < p.N ? begin + p.chunk : p.N;
-  int below = 0;
+  const long long begin = static_cast<long long>(warp) * p.chunk;
+  const int len = warp < p.warps ? static_cast<int>(min(static_cast<long long>(p.chunk), max(p.N - begin, 0ll))) : 0;
+  int below = 0, n = 0;
   bool any_bad = false;
-  if (warp < p.warps) {
-#pragma unroll 4
-    for (long long r0 = begin; r0 < end; r0 += 32) {
-      bool bad = false;
-      int v = -1;
-      if (r0 + lane < end) v = em_row(p.tokens, p.wide, r0 + lane, p.V, p.v_offset, p.V_global, &bad);
-      any_bad = any_bad || bad;
-      below += v >= 0 && v < lo ? 1 : 0;
-      const unsigned at = static_cast<unsigned>(v - lo);
-      const unsigned in = __ballot_sync(0xffffffffu, v >= 0 && at < static_cast<unsigned>(R));
-      if (in >> lane & 1u) {
-        const unsigned same = __match_any_sync(in, at);
-        if (__ffs(same) - 1 == lane) es_counts[at * p.warps + warp] += __popc(same);
+  // One pass over the warp's stretch; full(): the list may not hold the next tokens, last() at the end.
+  auto stream = [&](bool count, auto&& full) {
+#pragma unroll 1
+    for (int r0 = 0; r0 < len; r0 += 32 * kEsLoads) {
+      long long t[kEsLoads];
+#pragma unroll
+      for (int u = 0; u < kEsLoads; ++u) {
+        const int r = r0 + 32 * u + lane;
+        t[u] = -1;
+        if (r < len) t[u] = p.wide ? static_cast<const long long*>(p.tokens)[begin + r] : static_cast<const int*>(p.tokens)[begin + r];
       }
+#pragma unroll
+      for (int u = 0; u < kEsLoads; ++u) {
+        const long long v = t[u] - p.v_offset;
+        const bool there = t[u] >= 0 && v >= 0 && v < p.V;
+        const unsigned id = static_cast<unsigned>(static_cast<int>(v) - lo);
+        if (count) {
+          any_bad = any_bad || t[u] < -1 || t[u] >= p.V_global;
+          below += there && v < lo ? 1 : 0;
+        }
+        const bool mine = there && v >= lo && id < static_cast<unsigned>(R);
+        const unsigned in = __ballot_sync(0xffffffffu, mine);
+        if (in) {
+          if (mine) list[warp][n + __popc(in & ((1u << lane) - 1u))] = static_cast<uint32_t>(r0 + 32 * u + lane) << kEsIdBits | id;
+          n += __popc(in);
+        }
+      }
+      if (n > kEsList - 32 * kEsLoads) full();
+    }
+  };
+  auto count_list = [&]() {
+    __syncwarp();
+    for (int i = 0; i < n; i += 32) {
+      // (lanes without a token: an id that there is not)
+      const unsigned id = i + lane < n ? list[warp][i + lane] & ((1u << kEsIdBits) - 1u) : 0xffffffffu;
+      const unsigned same = __match_any_sync(0xffffffffu, id);
+      if (i + lane < n && __ffs(same) - 1 == lane) cells[warp * R + id] += static_cast<Cell>(__popc(same));
       __syncwarp();
     }
-  }
+  };
+  bool again = false;                                    // the list did not hold all
+  stream(true, [&]() { count_list(); n = 0; again = true; });
+  count_list();
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) warp_below[warp] = below;
-  if (__any_sync(0xffffffffu, any_bad) && lane == 0 && blockIdx.x == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  if (__any_sync(0xffffffffu, any_bad) && lane == 0 && g == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
   __syncthreads();
 
-  // Exclusive scan over (id, warp): a thread's cells lie side by side.
-  const int each = (cells + kEsThreads - 1) / kEsThreads, c0 = min(tid * each, cells), c1 = min(c0 + each, cells);
-  int sum = 0;
-  for (int i = c0; i < c1; ++i) sum += es_counts[i];
-  int upto = sum;
+  // Per id: exclusive sums over the warps.  Over the ids: a thread's ids lie side by side; tokens in the upper half, distinct ids in the lower.
+  const int each = (R + kEsThreads - 1) / kEsThreads, i0 = min(tid * each, R), i1 = min(i0 + each, R);
+  uint64_t sum = 0;
+  for (int i = i0; i < i1; ++i) {
+    unsigned all = 0;
+    for (int w = 0; w < p.warps; ++w) {
+      const unsigned c = cells[w * R + i];
+      cells[w * R + i] = static_cast<Cell>(all);
+      all += c;
+    }
+    heads[i] = make_int2(static_cast<int>(all), 0);
+    sum += static_cast<uint64_t>(all) << 32 | (all ? 1u : 0u);
+  }
+  uint64_t upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, upto, o);
+    const uint64_t x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
   if (lane == 31) warp_sum[warp] = upto;
+  const int base = __reduce_add_sync(0xffffffffu, warp_below[lane]);
   __syncthreads();
-  if (warp == 0) {
-    const int mine = warp_sum[lane];
-    int x = mine;
+  uint64_t before = 0, total = 0;
+  {
+    const uint64_t mine = warp_sum[lane];
+    uint64_t x = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      const uint64_t y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
-    warp_sum[lane] = x - mine;
-    const int all_below = __reduce_add_sync(0xffffffffu, warp_below[lane]);
-    if (lane == 0) base = all_below;
+    before = __shfl_sync(0xffffffffu, x - mine, warp);
+    total = __shfl_sync(0xffffffffu, x, 31);
+  }
+  uint64_t at = before + upto - sum;
+  for (int i = i0; i < i1; ++i) {
+    const unsigned all = static_cast<unsigned>(heads[i].x);
+    heads[i] = make_int2(base + static_cast<int>(at >> 32), static_cast<int>(at & 0xffffffffu));
+    at += static_cast<uint64_t>(all) << 32 | (all ? 1u : 0u);
+  }
+  const int end = base + static_cast<int>(total >> 32);
+  if (tid == 0) {
+    heads[R] = make_int2(end, 0);
+    p.distinct[g] = static_cast<int>(total & 0xffffffffu);
+    if (g + 1 == p.buckets) *p.valid = end;
   }
   __syncthreads();
-  int at = base + warp_sum[warp] + upto - sum;
-  for (int i = c0; i < c1; ++i) {
-    const int n = es_counts[i];
-    es_counts[i] = at;
-    at += n;
+  if (p.first) {
+    for (int i = tid; i < R; i += kEsThreads) p.first[lo + i] = heads[i].x;
+    if (g + 1 == p.buckets && tid == 0) p.first[p.V] = end;
   }
-  __syncthreads();
-  const int last = blockIdx.x + 1 == gridDim.x ? 1 : 0;
-  // Where the ids begin; the distinct ones numbered.  (The end of the range: base plus everything inside.)
-  __shared__ int range_end;
-  if (tid == kEsThreads - 1) range_end = at;             // (the last thread's cells are the last, or none)
-  __syncthreads();
-  int distinct_before = 0;
-#pragma unroll 1
-  for (int v0 = 0; v0 < R; v0 += kEsThreads) {
-    const int v = v0 + tid;
-    bool some = false;
-    if (v < R) {
-      const int b = es_counts[v * p.warps], e = v + 1 < R ? es_counts[(v + 1) * p.warps] : range_end;
-      p.first[lo + v] = b;
-      some = e > b;
-    }
-    if (last && v == R) p.first[p.V] = range_end;
-    if (p.by_rows) {
-      const unsigned have = __ballot_sync(0xffffffffu, some);
-      if (lane == 0) warp_distinct[warp] = __popc(have);
-      __syncthreads();
-      int mine = warp_distinct[lane], x = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      const int before = __shfl_sync(0xffffffffu, x - mine, warp), all = __shfl_sync(0xffffffffu, x, 31);
-      if (some) p.place[lo + v] = distinct_before + before + __popc(have & ((1u << lane) - 1u));
-      distinct_before += all;
-      __syncthreads();
-    }
-  }
-  if (last && tid == 0) p.first[p.V] = range_end;
-  if (p.by_rows && tid == 0) p.distinct[blockIdx.x] = distinct_before;
-  __syncthreads();                                       // (the counters move on below)
 
-  if (warp < p.warps) {
-#pragma unroll 4
-    for (long long r0 = begin; r0 < end; r0 += 32) {
-      bool bad;
-      int v = -1;
-      if (r0 + lane < end) v = em_row(p.tokens, p.wide, r0 + lane, p.V, p.v_offset, p.V_global, &bad);
-      const unsigned id = static_cast<unsigned>(v - lo);
-      const unsigned in = __ballot_sync(0xffffffffu, v >= 0 && id < static_cast<unsigned>(R));
-      if (in >> lane & 1u) {
-        const unsigned same = __match_any_sync(in, id);
-        const int to = es_counts[id * p.warps + warp] + __popc(same & ((1u << lane) - 1u));
-        __syncwarp(same);
-        if (__ffs(same) - 1 == lane) es_counts[id * p.warps + warp] += __popc(same);
-        p.perm[to] = static_cast<int>(r0 + lane);
-        p.sorted[to] = v;
+  // The places.
+  auto put_list = [&]() {
+    __syncwarp();
+    for (int i = 0; i < n; i += 32) {
+      const bool have = i + lane < n;
+      const uint32_t entry = have ? list[warp][i + lane] : 0;
+      const unsigned id = have ? entry & ((1u << kEsIdBits) - 1u) : 0xffffffffu;
+      const unsigned same = __match_any_sync(0xffffffffu, id);
+      unsigned ahead = 0;
+      if (have) ahead = cells[warp * R + id];
+      __syncwarp();
+      if (have) {
+        if (__ffs(same) - 1 == lane) cells[warp * R + id] = static_cast<Cell>(ahead + __popc(same));
+        const int2 head = heads[id];
+        const int to = head.x + static_cast<int>(ahead) + __popc(same & ((1u << lane) - 1u));
+        p.places[to] = make_int4(static_cast<int>(begin + (entry >> kEsIdBits)), lo + static_cast<int>(id), head.x, heads[id + 1].x);
+        if (p.by_rows) p.numbers[to] = make_int2(g, head.y);
       }
       __syncwarp();
     }
+  };
+  if (again) {
+    n = 0;
+    stream(false, [&]() { put_list(); n = 0; });
   }
+  put_list();
 }
 
 // Eight channels of a thread: side by side (kVec), or kEgThreads apart where rows start anywhere.
@@ -456,13 +510,14 @@ __device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long l
 template <int kType, bool kVec>
 __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
   __shared__ int rows[kEgMaxWindow + kEgMaxPiece];       // of the gradient, for the places of the pieces that begin in the window
-  __shared__ int ids[kEgMaxWindow], firsts[kEgMaxWindow + 1], ends[kEgMaxWindow], out_rows[kEgMaxWindow];
+  __shared__ int4 spots[kEgMaxWindow];
+  __shared__ int firsts[kEgMaxWindow + 1], out_rows[kEgMaxWindow];
   __shared__ int part_sum[kEgThreads / 32];
   __shared__ int last_here;
-  grid_dependency_wait();
-  grid_dependency_release();
   const int slice = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.slices)), tid = threadIdx.x;
   const int w = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.slices));
+  grid_dependency_wait();
+  grid_dependency_release();
   if (w >= windows) {
     // The whole table: zeros to the rows of ids that do not occur.
     const float zero[kEgEach] = {};
@@ -473,50 +528,53 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
       if (firsts[i] == firsts[i + 1]) eg_write<kVec>(p, out_type, v0 + i, slice, zero);
     return;
   }
-  const int valid = p.first[p.V];
+  // (behind the last valid place there is something to read, which is not used)
+  const int w0 = w * p.window;
+  int4 spot = make_int4(0, 0, 0, 0);
+  int2 number = make_int2(0, 0);
+  if (tid < p.window && w0 + tid < p.N) {
+    spot = p.places[w0 + tid];
+    if (p.by_rows) number = p.numbers[w0 + tid];
+    spots[tid] = spot;
+  }
+  const int w1 = min(w0 + p.window, *p.valid);
   if (w == 0 && slice == 0 && p.by_rows && tid < 32) {
     int n = 0;
     for (int i = tid; i < p.buckets; i += 32) n += p.distinct[i];
     n = __reduce_add_sync(0xffffffffu, n);
     if (tid == 0) *p.count_out = n;
   }
-  const int w0 = w * p.window, w1 = min(w0 + p.window, valid);
   if (w0 >= w1) return;
-  if (tid < w1 - w0) {
-    const int v = p.sorted[w0 + tid];
-    ids[tid] = v;
-    firsts[tid] = p.first[v];
-    ends[tid] = p.first[v + 1];
-  }
   __syncthreads();
   // Places x0 .. x1 - 1: from the first piece that begins in the window to the end of the last one that does.
   int x0 = w0, x1 = w1;
   {
-    const int in = (w0 - firsts[0]) % p.S;
-    if (in != 0) x0 = min(w0 + p.S - in, ends[0]);
+    const int in = (w0 - spots[0].z) % p.S;
+    if (in != 0) x0 = min(w0 + p.S - in, spots[0].w);
     if (x0 >= w1) return;                                // (all of the window inside one piece)
-    const int b = firsts[w1 - 1 - w0];
-    x1 = min(b + ((w1 - 1 - b) / p.S + 1) * p.S, ends[w1 - 1 - w0]);
+    const int4 last = spots[w1 - 1 - w0];
+    x1 = min(last.z + ((w1 - 1 - last.z) / p.S + 1) * p.S, last.w);
   }
-  for (int i = tid; i < x1 - x0; i += kEgThreads) rows[i] = p.perm[x0 + i];
+  for (int i = tid; i < x1 - x0; i += kEgThreads) rows[i] = x0 + i < w1 ? spots[x0 + i - w0].x : p.places[x0 + i].x;
   if (p.by_rows) {
-    // The distinct ids ahead of an id's own range of ids, and ahead of it there.
-    const int bucket0 = ids[0] / p.R;
+    // The distinct ids ahead of an id's own range, and ahead of it there.
+    __shared__ int range0;
+    if (tid == 0) range0 = number.x;
+    __syncthreads();
     int n = 0;
-    for (int i = tid; i < bucket0; i += kEgThreads) n += p.distinct[i];
+    for (int i = tid; i < range0; i += kEgThreads) n += p.distinct[i];
     n = __reduce_add_sync(0xffffffffu, n);
     if ((tid & 31) == 0) part_sum[tid >> 5] = n;
     __syncthreads();
     if (tid < w1 - w0) {
       n = 0;
       for (int i = 0; i < kEgThreads / 32; ++i) n += part_sum[i];
-      const int v = ids[tid], bucket = v / p.R;
 #pragma unroll 4
-      for (int i = bucket0; i < bucket; ++i) n += p.distinct[i];
-      out_rows[tid] = n + p.place[v];
+      for (int i = range0; i < number.x; ++i) n += p.distinct[i];
+      out_rows[tid] = n + number.y;
     }
   } else if (tid < w1 - w0) {
-    out_rows[tid] = ids[tid];
+    out_rows[tid] = spot.y;
   }
   __syncthreads();
 
@@ -533,7 +591,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
 #pragma unroll
       for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u].get(i));
       // (places behind the window belong to the last piece)
-      const int k = min(x + u, w1 - 1) - w0, begin = firsts[k], end = ends[k], next = x + u + 1;
+      const int k = min(x + u, w1 - 1) - w0, begin = spots[k].z, end = spots[k].w, next = x + u + 1;
       if (next != end && (next - begin) % p.S != 0) continue;
       if (end - begin > p.S) {
         // One of several pieces.
@@ -560,7 +618,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
           for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], __ldcg(y + i * kEgThreads));
         }
       }
-      if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(ids[k] + p.v_offset);
+      if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(spots[k].y + p.v_offset);
       eg_write<kVec>(p, out_type, out_rows[k], slice, sum);
 #pragma unroll
       for (int i = 0; i < kEgEach; ++i) sum[i] = 0.f;
@@ -569,41 +627,44 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
 }
 
 struct EgLayout {
-  size_t perm, sorted, first, place, distinct, done, partial, total;
+  size_t places, numbers, first, distinct, valid, done, partial, total;
 };
 
 // Host: the cut of the work.  False: sizes that are not served.
-bool eg_plan(long long N, int V, int H, int num_sms, EgParams* p, EgLayout* l) {
-  if (N < 0 || N >= INT32_MAX || V <= 0 || H <= 0 || V > INT32_MAX - 2) return false;
-  int R = (V + num_sms - 1) / num_sms;
-  if (R > kEsMaxIds) R = kEsMaxIds;
-  p->R = R;
-  p->buckets = (V + R - 1) / R;
+bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
+  if (N < 0 || N > 1 << 26 || V <= 0 || H <= 0 || V > 1 << 30 || H > INT32_MAX - kEgSlice) return false;
+  p->N = static_cast<int>(N); p->V = V; p->H = H;
   int warps = 1;
   while (warps < kEsWarps && N > 64ll * warps) warps <<= 1;      // a warp's stretch: 64 tokens, or more once all count
   p->warps = warps;
   p->chunk = static_cast<int>(((N + warps - 1) / warps + 31) / 32 * 32);
-  if (p->chunk == 0) p->chunk = 32;
+  // Ranges: one per SM where their counters fit, else as many as it takes.
+  const int cell = N <= UINT16_MAX ? 2 : 4, ids = min(kEsCellBytes / (cell * warps), (1 << kEsIdBits) - 2);
+  const int even = (V + ids - 1) / ids + 1;
+  p->even = even > kEgPlanSms - kEsZipf + 1 ? even : kEgPlanSms - kEsZipf + 1;
+  p->buckets = p->even + kEsZipf - 1;
   int S = 64;
   while (S < kEgMaxPiece && N > 256ll * S) S <<= 1;
   p->S = S;
   p->slices = (H + kEgSlice - 1) / kEgSlice;
   int window = kEgMaxWindow;
-  while (window > 4 && (N + window - 1) / window * p->slices < 4ll * num_sms) window >>= 1;
+  while (window > 4 && (N + window - 1) / window * p->slices < 4ll * kEgPlanSms) window >>= 1;
   p->window = window;
   const size_t pieces = static_cast<size_t>((N + S - 1) / S);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-  l->perm = take(static_cast<size_t>(N) * 4);
-  l->sorted = take(static_cast<size_t>(N) * 4);
+  l->places = take(static_cast<size_t>(N) * 16);
+  l->numbers = take(static_cast<size_t>(N) * 8);
   l->first = take((static_cast<size_t>(V) + 1) * 4);
-  l->place = take(static_cast<size_t>(V) * 4);
   l->distinct = take(static_cast<size_t>(p->buckets) * 4);
+  l->valid = take(4);
   l->done = take(pieces * p->slices * 4);
   l->partial = take(2 * pieces * p->slices * kEgSlice * 4);
   l->total = at;
   return true;
 }
+
+constexpr int kEsDynamic = kEsCellBytes + (1 << kEsIdBits) * 8;
 
 template <int kType>
 cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStream_t stream) {
@@ -613,12 +674,13 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
   cudaLaunchConfig_t cfg = {};
   cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
   cfg.gridDim = dim3(static_cast<unsigned>(p.buckets)); cfg.blockDim = dim3(kEsThreads);
-  cfg.dynamicSmemBytes = static_cast<size_t>(p.R) * p.warps * 4;
-  cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsMaxIds * kEsWarps * 4);
-  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, embed_sort_kernel, p);
+  cfg.dynamicSmemBytes = kEsDynamic;
+  auto* sort = p.N <= UINT16_MAX ? embed_sort_kernel<uint16_t> : embed_sort_kernel<uint32_t>;
+  cudaError_t e = cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsDynamic);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, sort, p);
   if (e != cudaSuccess) return e;
   const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
-  const long long blank = p.by_rows || p.accumulate ? 0 : (static_cast<long long>(p.V) + kEgMaxWindow - 1) / kEgMaxWindow;
+  const long long blank = p.first ? (static_cast<long long>(p.V) + kEgMaxWindow - 1) / kEgMaxWindow : 0;
   cfg.gridDim = dim3(static_cast<unsigned>((windows + blank) * p.slices)); cfg.blockDim = dim3(kEgThreads);
   cfg.dynamicSmemBytes = 0;
   return vec ? cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, true>, p, out_type, static_cast<int>(windows))

@@ -26,10 +26,6 @@
 //   adapter_down_kernel, adapter_up_kernel  (adapters.cuh) low-rank adapters of many requests beside the LM head.
 //   token_logprobs_kernel       (token_logprobs.cuh) log probabilities and ranks of given tokens, entropy and top alternatives, from
 //       logits in memory; gather_logprobs_kernel, the tokens' entries alone.
-//   beam_select_kernel, beam_reorder_kernel  (beams.cuh) a step of a beam search: the best continuations of all beams, and the beams'
-//       states in the order of their parents.
-//   embed_kernel                (embedding.cuh) rows of a table, the head's own storage forms among them, by token; embed_sort_kernel,
-//       embed_grad_kernel, the gradient of a table by sorted tokens.
 //   bounded_wait_selftest_kernel, staged_wait_selftest_kernel  waits that are made to run out, to exercise the give-up paths
 //       without breaking anything; quotient_selftest_kernel, the division behind every entropy.
 //   draft_entropy_kernel        H(q_j) of the draft rows, for the gate on the draft distribution.
@@ -64,6 +60,8 @@
 namespace cg = cooperative_groups;
 
 namespace {
+
+#include "device_util.cuh"
 
 // ------------------------------------------------------------------------------------------------ constants
 constexpr int kBlockK = 64;                      // bf16 elements per K block = one 128-byte swizzle row
@@ -223,10 +221,6 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
   return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 // Execution barrier only: orders no memory operations.  For the end of the kernel, where the point is that the peer CTA
 // has stopped using this CTA's barriers and tensor memory; a release here would make every thread wait until its last
@@ -436,12 +430,6 @@ __device__ __forceinline__ void leave_pace(unsigned* counter, unsigned members) 
     *counter = 0u;
   }
 }
-
-// Programmatic dependent launch: the grid may have been started while the kernel before it in the stream was still
-// running.  grid_dependency_wait returns once that kernel has completed and its writes are visible; it must precede
-// every global-memory access of the calling thread that could touch what that kernel reads or writes.
-__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_dependency_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -661,12 +649,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {     // NaN where one of them is
-  float d;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
 // stats_fold16<true> with half the issue slots: the maximum by three-input comparisons, the exponents' arguments
 // x = (l - m) log2 e, the sum of the exponentials and the sum of e * x two at a time.  The centred sum is ln 2 times the
 // last one.  What the rounding of m log2 e puts on every x (up to 2^-24 |m|) then counts as a shift of the reference in s and
@@ -771,11 +753,6 @@ __device__ __forceinline__ float scaled(float acc, float w_scale, const float* h
   return acc;
 }
 
-__device__ __forceinline__ float warp_max_f32(float x) {       // (of numbers; -inf among them)
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));       // (volatile: whole warps, stays where it is)
-  return r;
-}
 __device__ __forceinline__ double warp_sum_f64(double x) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
@@ -2472,9 +2449,8 @@ __global__ void __launch_bounds__(kSoloWarps ? kSoloThreads : kK3Threads, kSoloW
 
 // ------------------------------------------------------------------------------------------------ adapters, token log probabilities
 #include "adapters.cuh"
+#include "logit_rows.cuh"
 #include "token_logprobs.cuh"
-#include "beams.cuh"
-#include "embedding.cuh"
 
 // ------------------------------------------------------------------------------------------------ 8-bit quantiser
 // The 8-bit case of the Lo-Bi quantiser on the LM head (Lo-Bi Optimization section; the quantiser itself is not
@@ -4581,185 +4557,6 @@ hola_status hola_token_logprobs(const hola_logprobs_args* a, void* cuda_stream) 
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = a->l_dtype == HOLA_L_F32 ? run_logprobs<float>(p, sms, stream)
                         : a->l_dtype == HOLA_L_BF16 ? run_logprobs<__nv_bfloat16>(p, sms, stream) : run_logprobs<__half>(p, sms, stream);
-  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
-}
-
-// The current device's SM count; 0: no device that runs these kernels.
-static int current_sms() {
-  int dev = 0, sms = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10)
-    return 0;
-  return sms;
-}
-
-hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
-  if (!a || a->B < 0 || a->W <= 0 || a->V <= 0 || a->n <= 0 || a->seq_stride < 0 || a->beam_stride < 0) return HOLA_ERR_INVALID_ARG;
-  if (a->l_dtype < HOLA_L_F32 || a->l_dtype > HOLA_L_F16) return HOLA_ERR_INVALID_ARG;
-  if (a->W > kBsMaxBeams || a->n > kBsMaxKept || a->V > kBsMaxV || a->B > INT32_MAX / kBsMaxCluster) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (a->keep_slots && a->n != a->W) return HOLA_ERR_INVALID_ARG;
-  if (a->end_token < -1 || a->end_token >= a->V || (a->finished && a->end_token < 0)) return HOLA_ERR_INVALID_ARG;
-  if (a->B == 0) return HOLA_OK;
-  if (!a->logits || !a->logZ || !a->score || !a->score_out || !a->parent || !a->token) return HOLA_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(a->logits) % (a->l_dtype == HOLA_L_F32 ? 4 : 2)) return HOLA_ERR_INVALID_ARG;
-  const int sms = current_sms();
-  if (!sms) return HOLA_ERR_NO_DEVICE;
-  BsParams p = {};
-  p.logits = a->logits; p.seq_stride = a->seq_stride; p.beam_stride = a->beam_stride; p.B = a->B; p.W = a->W; p.V = a->V; p.n = a->n;
-  p.logZ = a->logZ; p.score = a->score; p.finished = a->finished; p.weight = a->weight; p.end_token = a->end_token;
-  p.keep_slots = a->keep_slots; p.score_out = a->score_out; p.parent = a->parent; p.token = a->token; p.finished_out = a->finished_out;
-  p.status = a->status_word;
-  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = a->l_dtype == HOLA_L_F32 ? launch_beam_select<float>(p, sms, stream)
-                        : a->l_dtype == HOLA_L_BF16 ? launch_beam_select<__nv_bfloat16>(p, sms, stream) : launch_beam_select<__half>(p, sms, stream);
-  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
-}
-
-hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
-  if (!a || a->B < 0 || a->W <= 0 || a->n <= 0 || a->count < 0 || a->parent_stride < 0) return HOLA_ERR_INVALID_ARG;
-  if (a->W > kBsMaxBeams || a->n > kBsMaxBeams) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (a->B == 0 || a->count == 0) return HOLA_OK;
-  if (!a->states || !a->parent) return HOLA_ERR_INVALID_ARG;
-  // (all states are looked at before the first launch)
-  int in_place = -1;
-  for (int i = 0; i < a->count; ++i) {
-    const hola_beam_state& s = a->states[i];
-    if (s.run < 0 || s.position < 0 || s.outer[0] < 0 || s.outer[1] < 0) return HOLA_ERR_INVALID_ARG;
-    if (s.run == 0 || s.outer[0] == 0 || s.outer[1] == 0) continue;
-    if (!s.src || !s.dst || s.seq_stride < 0 || s.beam_stride < 0 || s.outer_stride[0] < 0 || s.outer_stride[1] < 0 || s.dst_seq_stride < 0 ||
-        s.dst_beam_stride < 0 || s.dst_outer_stride[0] < 0 || s.dst_outer_stride[1] < 0)
-      return HOLA_ERR_INVALID_ARG;
-    const bool here = s.src == s.dst;
-    if (in_place >= 0 && in_place != static_cast<int>(here)) return HOLA_ERR_INVALID_ARG;
-    in_place = here;
-    if (here && (a->n > a->W || s.seq_stride != s.dst_seq_stride || s.beam_stride != s.dst_beam_stride ||
-                 s.outer_stride[0] != s.dst_outer_stride[0] || s.outer_stride[1] != s.dst_outer_stride[1]))
-      return HOLA_ERR_INVALID_ARG;
-    if ((a->n > 1 && s.dst_beam_stride < s.run) || (a->W > 1 && s.beam_stride < s.run)) return HOLA_ERR_INVALID_ARG;      // beams that share bytes
-    const long long pieces = (s.run - 1) / kBrPiece + 1;
-    if (pieces > INT32_MAX || s.outer[0] > INT32_MAX || s.outer[1] > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
-    const double ctas = static_cast<double>(pieces) * a->B * static_cast<double>(s.outer[0]) * static_cast<double>(s.outer[1]);
-    if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  }
-  if (in_place < 0) return HOLA_OK;
-  if (!current_sms()) return HOLA_ERR_NO_DEVICE;
-  BrParams p = {};
-  p.B = a->B; p.W = a->W; p.n = a->n; p.parent = a->parent; p.parent_stride = a->parent_stride; p.used = a->used; p.status = a->status_word;
-  p.in_place = in_place;
-  long long ctas = 0;
-  for (int i = 0; i <= a->count; ++i) {
-    long long more = 0, pieces = 0;
-    const hola_beam_state* s = i < a->count ? &a->states[i] : nullptr;
-    if (s) {
-      if (s->run == 0 || s->outer[0] == 0 || s->outer[1] == 0) continue;
-      pieces = (s->run - 1) / kBrPiece + 1;
-      more = pieces * a->B * s->outer[0] * s->outer[1];
-    }
-    if (p.count > 0 && (!s || p.count == kBrStates || ctas + more > INT32_MAX)) {
-      const cudaError_t e = launch_beam_reorder(p, static_cast<unsigned>(ctas), static_cast<cudaStream_t>(cuda_stream));
-      if (e != cudaSuccess) return HOLA_ERR_CUDA;
-      p.count = 0;
-      ctas = 0;
-    }
-    if (!s) break;
-    BrState& o = p.s[p.count++];
-    o.src = static_cast<const unsigned char*>(s->src); o.dst = static_cast<unsigned char*>(s->dst);
-    o.seq = s->seq_stride; o.beam = s->beam_stride; o.outer0 = s->outer_stride[0]; o.outer1 = s->outer_stride[1];
-    o.to_seq = s->dst_seq_stride; o.to_beam = s->dst_beam_stride; o.to_outer0 = s->dst_outer_stride[0]; o.to_outer1 = s->dst_outer_stride[1];
-    o.run = s->run; o.position = s->position;
-    o.n0 = static_cast<unsigned>(s->outer[0]); o.n1 = static_cast<unsigned>(s->outer[1]);
-    o.pieces = static_cast<unsigned>(pieces); o.first_cta = static_cast<unsigned>(ctas);
-    ctas += more;
-  }
-  return HOLA_OK;
-}
-
-// Whether n bytes at a time can be read or written of rows of `stride` elements.
-static bool in_words(const void* base, long long stride, int elem, unsigned bytes) {
-  return reinterpret_cast<uintptr_t>(base) % bytes == 0 && stride * elem % bytes == 0;
-}
-
-hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
-  if (!a || a->N < 0 || a->V <= 0 || a->H <= 0 || a->row_stride < 0 || a->add_stride < 0 || a->out_stride < 0) return HOLA_ERR_INVALID_ARG;
-  if (a->t_dtype < HOLA_T_F32 || a->t_dtype > HOLA_T_MIXED || a->out_dtype < HOLA_T_F32 || a->out_dtype > HOLA_T_F16) return HOLA_ERR_INVALID_ARG;
-  if (a->v_offset < 0 || a->V_global < 0 || (a->V_global > 0 && static_cast<long long>(a->v_offset) + a->V > a->V_global)) return HOLA_ERR_INVALID_ARG;
-  if (a->V_global == 0 && a->v_offset != 0) return HOLA_ERR_INVALID_ARG;
-  const bool mixed = a->t_dtype == HOLA_T_MIXED;
-  if (a->N > INT32_MAX || a->H > INT32_MAX - 65536 || (mixed && a->H % kSubBlock != 0)) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (a->N == 0) return HOLA_OK;
-  if (!a->tokens || !a->out || (a->N > 1 && a->out_stride < a->H)) return HOLA_ERR_INVALID_ARG;
-  if (mixed) {
-    const hola_wmix* m = a->wmix;
-    if (!m || !m->group_width || !m->group_row || m->rows4 < 0 || m->rows8 < 0 || m->rows16 < 0 ||
-        static_cast<long long>(m->rows4) + m->rows8 + m->rows16 != a->V)
-      return HOLA_ERR_INVALID_ARG;
-    if ((m->rows4 > 0 && (!m->W4 || !m->shift4)) || (m->rows8 > 0 && !m->W8) || (m->rows16 > 0 && !m->W16)) return HOLA_ERR_INVALID_ARG;
-  } else if (!a->table) {
-    return HOLA_ERR_INVALID_ARG;
-  }
-  if ((mixed || a->t_dtype == HOLA_T_INT8) != (a->w_scale != nullptr)) return HOLA_ERR_INVALID_ARG;
-  const int te = mixed ? 1 : tab_bytes(a->t_dtype), oe = tab_bytes(a->out_dtype);
-  if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
-      reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
-    return HOLA_ERR_INVALID_ARG;
-  const int sms = current_sms();
-  if (!sms) return HOLA_ERR_NO_DEVICE;
-  EmParams p = {};
-  p.tokens = a->tokens; p.wide = a->wide_tokens; p.N = a->N; p.V = a->V; p.H = a->H; p.v_offset = a->v_offset;
-  p.V_global = a->V_global ? a->V_global : a->V;
-  p.table = a->table; p.row_stride = a->row_stride; p.w_scale = a->w_scale;
-  if (mixed) p.mix = *a->wmix;
-  p.scale = a->scale; p.add = a->add; p.add_stride = a->add_stride; p.out = a->out; p.out_stride = a->out_stride; p.status = a->status_word;
-  bool words = a->H % 8 == 0 && in_words(a->out, a->out_stride, oe, 16) && (!a->add || in_words(a->add, a->add_stride, oe, 16));
-  if (mixed) words = words && in_words(p.mix.W16, 0, 1, 16) && in_words(p.mix.W8, 0, 1, 8) && in_words(p.mix.W4, 0, 1, 4);
-  else words = words && in_words(a->table, a->row_stride, te, te == 1 ? 8 : 16);
-  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, sms, stream)
-                              : launch_embed_of<1>(p, a->t_dtype, a->out_dtype, sms, stream);
-  return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
-}
-
-size_t hola_embed_grad_workspace_bytes(long long N, int V, int H) {
-  EgParams p = {};
-  EgLayout l;
-  return eg_plan(N, V, H, kEgPlanSms, &p, &l) ? l.total : 0;
-}
-
-hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
-  if (!a || a->N < 0 || a->V <= 0 || a->H <= 0 || a->grad_stride < 0 || a->out_stride < 0) return HOLA_ERR_INVALID_ARG;
-  if (a->g_dtype < HOLA_T_F32 || a->g_dtype > HOLA_T_F16 || a->out_dtype < HOLA_T_F32 || a->out_dtype > HOLA_T_F16) return HOLA_ERR_INVALID_ARG;
-  if (a->v_offset < 0 || a->V_global < 0 || (a->V_global > 0 && static_cast<long long>(a->v_offset) + a->V > a->V_global)) return HOLA_ERR_INVALID_ARG;
-  if (a->V_global == 0 && a->v_offset != 0) return HOLA_ERR_INVALID_ARG;
-  const bool by_rows = a->ids_out || a->count_out;
-  if (by_rows && (!a->count_out || a->accumulate)) return HOLA_ERR_INVALID_ARG;
-  EgParams p = {};
-  EgLayout l;
-  if (!eg_plan(a->N, a->V, a->H, kEgPlanSms, &p, &l)) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (a->N > 0 && (!a->tokens || !a->grad || (by_rows && (!a->ids_out || !a->out)))) return HOLA_ERR_INVALID_ARG;
-  if (!by_rows && !a->out) return HOLA_ERR_INVALID_ARG;
-  if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < l.total) return HOLA_ERR_INVALID_ARG;
-  if ((by_rows ? a->N : static_cast<long long>(a->V)) > 1 && a->out_stride < a->H) return HOLA_ERR_INVALID_ARG;
-  const int ge = tab_bytes(a->g_dtype), oe = tab_bytes(a->out_dtype);
-  if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->grad) % ge ||
-      reinterpret_cast<uintptr_t>(a->out) % oe)
-    return HOLA_ERR_INVALID_ARG;
-  const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + kEgMaxWindow - 1) / kEgMaxWindow) * p.slices;
-  if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (!current_sms()) return HOLA_ERR_NO_DEVICE;
-  p.tokens = a->tokens; p.wide = a->wide_tokens; p.N = a->N; p.V = a->V; p.H = a->H; p.v_offset = a->v_offset;
-  p.V_global = a->V_global ? a->V_global : a->V;
-  p.grad = a->grad; p.g_stride = a->grad_stride; p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;
-  p.accumulate = a->accumulate; p.by_rows = by_rows; p.ids_out = a->ids_out; p.count_out = a->count_out; p.status = a->status_word;
-  unsigned char* ws = static_cast<unsigned char*>(a->workspace);
-  p.perm = reinterpret_cast<int*>(ws + l.perm); p.sorted = reinterpret_cast<int*>(ws + l.sorted);
-  p.first = reinterpret_cast<int*>(ws + l.first); p.place = reinterpret_cast<int*>(ws + l.place);
-  p.distinct = reinterpret_cast<int*>(ws + l.distinct); p.done = reinterpret_cast<unsigned*>(ws + l.done);
-  p.partial = reinterpret_cast<float*>(ws + l.partial);
-  const bool words = a->H % 8 == 0 && in_words(a->grad, a->grad_stride, ge, 16) && in_words(a->out, a->out_stride, oe, 16);
-  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = a->g_dtype == HOLA_T_F32 ? launch_embed_grad<kTabF32>(p, a->out_dtype, words, stream)
-                        : a->g_dtype == HOLA_T_BF16 ? launch_embed_grad<kTabBf16>(p, a->out_dtype, words, stream)
-                                                    : launch_embed_grad<kTabF16>(p, a->out_dtype, words, stream);
   return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }
 

@@ -140,7 +140,8 @@ def _load_host(lib: ctypes.CDLL):
         warnings.warn(f"host-side helper not available, calls cost a few microseconds more: {e}")
         return
     for name in ("hola_verify", "hola_verify_host", "hola_lm_head_entropy", "hola_quantize_mixed_widths", "hola_lm_head_adapters",
-                 "hola_verify_adapters", "hola_token_logprobs"):
+                 "hola_verify_adapters", "hola_token_logprobs", "hola_beam_select", "hola_beam_reorder", "hola_embed", "hola_embed_grad",
+                 "hola_embed_grad_workspace_bytes"):
         _entry[name] = ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
     _host = helper
 
@@ -588,6 +589,13 @@ def hola_beam_select(logits: torch.Tensor, logZ: torch.Tensor, score: torch.Tens
     status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  out: an earlier call's result, filled again.  stream: see HolaVerify."""
     lib = load_library()
     what = "hola_beam_select"
+    if _host is not None and stream is None and out is None and getattr(logits, "is_cuda", False):
+        got = _host.beam_select(_entry[what], logits, logZ, score, n, finished, end_token, weight, keep_slots, status, torch._C._cuda_getDevice(),
+                                _stream_ptr(None))
+        if got is not None:
+            if got[0]:
+                _check(lib, None, got[0], what)
+            return BeamSelection(*got[1:])
     if not isinstance(logits, torch.Tensor) or logits.dtype not in _L_DTYPES or not logits.is_cuda or logits.dim() != 3:
         raise HolaError(f"{what} takes fp32, bf16 or fp16 logits [B, W, V] on a device")
     B, W, V = logits.shape
@@ -655,7 +663,7 @@ class BeamStates:
             written = spans(targets)
             if any(a < d and c < b for a, b in written for c, d in spans(tensors)):
                 raise HolaError("BeamStates: a target overlaps a source")
-        self.address = ctypes.addressof(self.states)
+        self.address, self.count = ctypes.addressof(self.states), len(tensors)
 
     def _lay_out(self, st, x, y, axis, at):
         if not 0 <= axis <= x.dim() - 2 or tuple(x.shape[axis:axis + 2]) != (self.B, self.W):
@@ -709,11 +717,18 @@ def hola_beam_reorder(states: BeamStates, parent: torch.Tensor, used: torch.Tens
     if not isinstance(states, BeamStates):
         raise HolaError(f"{what} takes BeamStates")
     dev = states.device
+    if _host is not None and dev.type == "cuda" and dev.index == (device := torch._C._cuda_getDevice()):
+        got = _host.beam_reorder(_entry[what], states.address, states.count, states.B, states.W, states.n, parent, used, status, device,
+                                 _stream_ptr(stream))
+        if got is not None:
+            if got:
+                _check(lib, None, got, what)
+            return
     if (not isinstance(parent, torch.Tensor) or parent.dtype != torch.int32 or parent.device != dev or parent.dim() != 2 or parent.shape[0] != states.B
             or not 1 <= parent.shape[1] <= states.n or (parent.shape[1] > 1 and parent.stride(1) != 1) or dev.type != "cuda"):
         raise HolaError(f"{what}: parent must be an int32 tensor of {states.B} rows of up to {states.n} places side by side, on the states' device")
     a = hola_reorder_args()
-    a.B, a.W, a.n, a.count, a.states = states.B, states.W, parent.shape[1], len(states.states), states.address
+    a.B, a.W, a.n, a.count, a.states = states.B, states.W, parent.shape[1], states.count, states.address
     a.parent, a.parent_stride = parent.data_ptr(), parent.stride(0)
     if used is not None:
         a.used = _same(what, used, torch.int32, (states.B,), dev, "used")
@@ -766,6 +781,15 @@ def hola_embed(tokens: torch.Tensor, table, scale: float = 1.0, add: torch.Tenso
     status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  stream: see HolaVerify."""
     lib = load_library()
     what = "hola_embed"
+    if _host is not None and stream is None and out is None and getattr(tokens, "is_cuda", False) and (dtype is None or dtype in _T_DTYPES):
+        mixed = type(table) is MixedHead and w_scale is None and table.w_scale is not None
+        got = _host.embed(_entry[what], tokens, table, ctypes.addressof(table.struct) if mixed else 0, table.V if mixed else 0, table.H if mixed else 0,
+                          scale, add, table.w_scale if mixed else w_scale, -1 if dtype is None else _T_DTYPES[dtype], v_offset, V_global, status,
+                          torch._C._cuda_getDevice(), _stream_ptr(None))
+        if got is not None:
+            if got[0]:
+                _check(lib, None, got[0], what)
+            return got[1]
     _ids(what, tokens)
     dev, shape = tokens.device, tokens.shape
     a = hola_embed_args()
@@ -817,6 +841,18 @@ class TokenRows:
     count: torch.Tensor      # int32 [1]
 
 
+def _embed_grad_native(what, tokens, grad, V, scale, dtype, v_offset, V_global, by_rows, out, status):
+    """(result or rows, ids, count) through the native helper, None where the arguments have to be made from Python."""
+    if _host is None or dtype not in _T_DTYPES or not getattr(tokens, "is_cuda", False):
+        return None
+    ids, rows, count = (out.ids, out.rows, out.count) if type(out) is TokenRows else (None, None, None)
+    got = _host.embed_grad(_entry["hola_embed_grad"], _entry["hola_embed_grad_workspace_bytes"], tokens, grad, V, scale, _T_DTYPES[dtype], v_offset,
+                           V_global, by_rows, ids, rows, count, status, torch._C._cuda_getDevice(), _stream_ptr(None))
+    if got is not None and got[0]:
+        _check(load_library(), None, got[0], what)
+    return None if got is None else got[1:]
+
+
 def _embed_grad(what, tokens, grad, V, scale, v_offset, V_global, status, stream, fill):
     lib = load_library()
     _ids(what, tokens)
@@ -852,6 +888,11 @@ def hola_embed_grad(tokens: torch.Tensor, grad: torch.Tensor, V: int, scale: flo
     what = "hola_embed_grad"
     if accumulate and out is None:
         raise HolaError(f"{what}: accumulate needs out")
+    load_library()
+    if stream is None and out is None:
+        got = _embed_grad_native(what, tokens, grad, V, scale, dtype, v_offset, V_global, False, None, status)
+        if got is not None:
+            return got[0]
 
     def fill(a, dev, N, H):
         if (dtype if out is None else out.dtype) not in _T_DTYPES:
@@ -872,6 +913,11 @@ def hola_embed_grad_rows(tokens: torch.Tensor, grad: torch.Tensor, V: int, scale
     """The same by rows: the distinct tokens in rising order, and the gradient's row of each.  out: an earlier call's result, or buffers
     with room for as many rows as there are tokens; what lies behind the distinct ones is left as it was."""
     what = "hola_embed_grad_rows"
+    load_library()
+    if stream is None and (out is None or type(out) is TokenRows):
+        got = _embed_grad_native(what, tokens, grad, V, scale, dtype, v_offset, V_global, True, out, status)
+        if got is not None:
+            return out if out is not None else TokenRows(got[1], got[0], got[2])
 
     def fill(a, dev, N, H):
         got = out

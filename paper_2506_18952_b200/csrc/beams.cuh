@@ -38,7 +38,10 @@ struct BsParams {
 struct BsCand {
   uint64_t hi, lo;
 };
-__device__ __forceinline__ bool bs_before(const BsCand& a, const BsCand& b) { return a.hi > b.hi || (a.hi == b.hi && a.lo > b.lo); }
+// (without branches: 103 candidates against one another 4.1 us with them)
+__device__ __forceinline__ bool bs_before(const BsCand& a, const BsCand& b) {
+  return static_cast<bool>(static_cast<int>(a.hi > b.hi) | (static_cast<int>(a.hi == b.hi) & static_cast<int>(a.lo > b.lo)));
+}
 __device__ __forceinline__ uint64_t bs_order(double x) {
   const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
@@ -284,14 +287,12 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
       if (look) {
         if (again) s.looked_at[warp][__popc(look & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);
         __syncwarp();
-        const int who = __popc(look);
-        // (step by step over the rows' rounds: lane i takes thread i % who of round i / who)
-        for (int li = 0; li < live; ++li) {
-          const int total = s.rows[li].rounds * who;
-          for (int i = lane; i < total; i += 32) {
-            const int j = (i / who) * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
-            if (j < s.rows[li].count) bs_send(s, s.rows[li], p.V, s.rows[li].begin + j, thr);
-          }
+        const int who = __popc(look), total = rounds * who;
+        for (int i = lane; i < total; i += 32) {
+          int t = i / who, li = 0;
+          for (; t >= s.rows[li].rounds; ++li) t -= s.rows[li].rounds;
+          const int j = t * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
+          if (j < s.rows[li].count) bs_send(s, s.rows[li], p.V, s.rows[li].begin + j, thr);
         }
       }
     }
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
     for (int i = lane; i < total; i += 32) {
       const BsCand c = s.all[i];
       int before = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (int k = from; k < to; ++k) before += bs_before(s.all[k], c) ? 1 : 0;
       atomicAdd(&s.before_it[i], before);
     }
@@ -465,10 +466,18 @@ cudaError_t launch_beam_select(const BsParams& p, int num_sms, cudaStream_t stre
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = static_cast<unsigned>(C); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
-  cudaError_t e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(BsShared<T>)));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e != cudaSuccess) return e;
   return cudaLaunchKernelEx(&cfg, beam_select_kernel<T>, p, C);
+}
+
+template <typename T>
+cudaError_t configure_select() {
+  const cudaError_t e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(BsShared<T>)));
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+}
+cudaError_t configure_beams() {
+  cudaError_t e = configure_select<float>();
+  if (e == cudaSuccess) e = configure_select<__nv_bfloat16>();
+  return e == cudaSuccess ? configure_select<__half>() : e;
 }
 
 // ------------------------------------------------------------------------------------------------ reordering

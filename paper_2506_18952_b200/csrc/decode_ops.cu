@@ -15,6 +15,7 @@
 
 #include <cooperative_groups.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "../../include/hola_verify.h"
@@ -32,12 +33,19 @@ namespace {
 
 extern "C" {
 
-// The current device's SM count; 0: no device that runs these kernels.
+// The current device's SM count; 0: no device that runs these kernels.  What a device is does not change: asked for once (the first call
+// on a device also tells the runtime how much shared memory the kernels use, which the calls behind it need not say again).
 static int current_sms() {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];
   int dev = 0, sms = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  if (dev < kDevices && (sms = known[dev].load(std::memory_order_acquire)) != 0) return sms;
+  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10)
     return 0;
+  if (configure_beams() != cudaSuccess || configure_embedding() != cudaSuccess) return 0;
+  if (dev < kDevices) known[dev].store(sms, std::memory_order_release);
   return sms;
 }
 

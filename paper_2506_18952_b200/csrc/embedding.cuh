@@ -2,9 +2,8 @@
 
 // ------------------------------------------------------------------------------------------------ lookup
 // out[r] = add[r] + scale * W[tok[r]], every operation one rounding in fp32 (the scale of a quantised row first), the result rounded
-// once more where it is stored in 16 bits.  A thread takes 8 neighbouring channels of kEmRows rows.
+// once more where it is stored in 16 bits.  A thread takes 8 neighbouring channels of some rows.
 constexpr int kEmThreads = 256;
-constexpr int kEmRows = 4;             // rows of a CTA, loads of which are on the way together
 
 // Types of rows in memory (hola_t_dtype).
 enum { kTabF32 = HOLA_T_F32, kTabBf16 = HOLA_T_BF16, kTabF16 = HOLA_T_F16, kTabInt8 = HOLA_T_INT8, kTabMixed = HOLA_T_MIXED };
@@ -62,6 +61,16 @@ struct EmWord {
       w[0] = *static_cast<const uint8_t*>(p);
     }
   }
+  __device__ __forceinline__ void store(void* p) const {
+    constexpr int k = kBytes < 4 ? 1 : kBytes / 4;
+    if (kBytes == 32)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(p), "r"(w[0]), "r"(w[1 % k]), "r"(w[2 % k]), "r"(w[3 % k]), "r"(w[4 % k]), "r"(w[5 % k]), "r"(w[6 % k]), "r"(w[7 % k])
+                   : "memory");
+    else if (kBytes == 16) *static_cast<uint4*>(p) = make_uint4(w[0], w[1 % k], w[2 % k], w[3 % k]);
+    else if (kBytes == 4) *static_cast<uint32_t*>(p) = w[0];
+    else if (kBytes == 2) *static_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
+  }
   __device__ __forceinline__ float get(int i) const {
     if (kType == kTabF32) return __uint_as_float(w[i]);
     if (kType == kTabBf16) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
@@ -83,14 +92,23 @@ __device__ __forceinline__ void em_store(void* p, const float* x) {
     }
     return;
   }
-  uint32_t h[n];
+  if (n == 8) {
+    uint32_t h[4];
 #pragma unroll
-  for (int i = 0; i < n; ++i)
-    h[i] = kType == kTabBf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x[i])) : __half_as_ushort(__float2half_rn(x[i]));
-  if (n == 8)
-    *static_cast<uint4*>(p) = make_uint4(h[0] | h[1 % n] << 16, h[2 % n] | h[3 % n] << 16, h[4 % n] | h[5 % n] << 16, h[6 % n] | h[7 % n] << 16);
-  else
-    *static_cast<uint16_t*>(p) = static_cast<uint16_t>(h[0]);
+    for (int i = 0; i < 4; ++i) {
+      const float a = x[(2 * i) % n], b = x[(2 * i + 1) % n];
+      if (kType == kTabBf16) {
+        const __nv_bfloat162 y = __floats2bfloat162_rn(a, b);
+        h[i] = *reinterpret_cast<const uint32_t*>(&y);
+      } else {
+        const __half2 y = __floats2half2_rn(a, b);
+        h[i] = *reinterpret_cast<const uint32_t*>(&y);
+      }
+    }
+    *static_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
+  } else {
+    *static_cast<uint16_t*>(p) = kType == kTabBf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x[0])) : __half_as_ushort(__float2half_rn(x[0]));
+  }
 }
 template <int n>
 __device__ __forceinline__ void em_store_as(int type, void* base, long long at, const float* x) {
@@ -141,76 +159,93 @@ __device__ __forceinline__ void em_mixed(const hola_wmix& mix, int H, int v, int
   }
 }
 
-// n: channels of a thread, 8 where everything is aligned.  Bound by HBM: rows in, rows out.
-template <int kType, int n>
-__global__ void __launch_bounds__(kEmThreads) embed_kernel(const __grid_constant__ EmParams p, int out_type, int rows_per_cta) {
+// n: channels of a thread, 8 where everything is aligned; kWide: results of 32 bits, else of 16 (`f16`: which).  Bound by HBM: rows in, rows out.
+template <int kType>
+__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed ? 2 : 4; }       // rows of a CTA, on the way together
+
+template <int kType, bool kWide, bool kAdd, int n>
+__global__ void __launch_bounds__(kEmThreads, 4) embed_kernel(const __grid_constant__ EmParams p, int f16, int rows_per_cta) {
+  constexpr bool kCodes = kType == kTabInt8 || kType == kTabMixed, kMixed = kType == kTabMixed;
+  constexpr int kWord = kMixed ? kTabBf16 : kType, kRows = em_rows<kType>(), kOut = kWide ? kTabF32 : kTabBf16;
   grid_dependency_wait();
   grid_dependency_release();
   const long long r0 = static_cast<long long>(blockIdx.x) * rows_per_cta;
   const int rows = static_cast<int>(p.N - r0 < rows_per_cta ? p.N - r0 : rows_per_cta);
-  int v[kEmRows];
-  float ws[kEmRows];
+  int v[kRows];
+  float ws[kRows];
   bool any_bad = false;
 #pragma unroll
-  for (int i = 0; i < kEmRows; ++i) {
+  for (int i = 0; i < kRows; ++i) {
     v[i] = -1;
     ws[i] = 1.f;
     if (i < rows) {
       bool bad;
       v[i] = em_row(p.tokens, p.wide, r0 + i, p.V, p.v_offset, p.V_global, &bad);
       any_bad = any_bad || bad;
-      if ((kType == kTabInt8 || kType == kTabMixed) && v[i] >= 0) ws[i] = p.w_scale[v[i]];
+      if (kCodes && v[i] >= 0) ws[i] = p.w_scale[v[i]];
     }
   }
   if (any_bad && p.status && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  // (what is neither scaled nor added to nor converted is passed on as it is)
+  const bool as_is = !kAdd && p.scale == 1.f && (kWide ? kType == kTabF32 : kType == (f16 ? kTabF16 : kTabBf16));
   const int step = static_cast<int>(gridDim.y) * kEmThreads * n;
 #pragma unroll 1
   for (int h = (static_cast<int>(blockIdx.y) * kEmThreads + static_cast<int>(threadIdx.x)) * n; h < p.H; h += step) {
-    float x[kEmRows][n];
-    if (kType == kTabMixed) {
+    EmWord<kWord, n> w[kRows];
+    float x[kMixed ? kRows : 1][n];
+    EmWord<kOut, n> add[kAdd ? kRows : 1];
 #pragma unroll
-      for (int i = 0; i < kEmRows; ++i)
-        if (v[i] >= 0) em_mixed<n>(p.mix, p.H, v[i], h, x[i]);
-    } else {
-      constexpr int kWord = kType == kTabMixed ? kTabBf16 : kType;
-      EmWord<kWord, n> w[kEmRows];
-#pragma unroll
-      for (int i = 0; i < kEmRows; ++i)
-        if (v[i] >= 0) w[i].load(static_cast<const unsigned char*>(p.table) + (v[i] * p.row_stride + h) * tab_bytes(kWord));
-#pragma unroll
-      for (int i = 0; i < kEmRows; ++i)
-#pragma unroll
-        for (int c = 0; c < n; ++c) x[i][c] = v[i] >= 0 ? w[i].get(c) : 0.f;
+    for (int i = 0; i < kRows; ++i) {
+      if (v[i] >= 0) {
+        if (kMixed) em_mixed<n>(p.mix, p.H, v[i], h, x[kMixed ? i : 0]);
+        else w[i].load(static_cast<const unsigned char*>(p.table) + (v[i] * p.row_stride + h) * tab_bytes(kWord));
+      }
+      if (kAdd && i < rows) add[kAdd ? i : 0].load(static_cast<const unsigned char*>(p.add) + ((r0 + i) * p.add_stride + h) * tab_bytes(kOut));
     }
 #pragma unroll
-    for (int i = 0; i < kEmRows; ++i) {
+    for (int i = 0; i < kRows; ++i) {
       if (i >= rows) break;
+      unsigned char* to = static_cast<unsigned char*>(p.out) + ((r0 + i) * p.out_stride + h) * tab_bytes(kOut);
       float y[n];
+      if (v[i] >= 0) {
+        if (as_is) {
+          w[i].store(to);
+          continue;
+        }
 #pragma unroll
-      for (int c = 0; c < n; ++c) {
-        y[c] = 0.f;
-        if (v[i] >= 0) {
-          y[c] = x[i][c];
-          if (kType == kTabInt8 || kType == kTabMixed) y[c] = __fmul_rn(y[c], ws[i]);
+        for (int c = 0; c < n; ++c) {
+          y[c] = kMixed ? x[kMixed ? i : 0][c] : w[i].get(c);
+          if (kCodes) y[c] = __fmul_rn(y[c], ws[i]);
           y[c] = __fmul_rn(y[c], p.scale);
         }
-      }
-      if (p.add) {
-        float a[n];
-        em_load_as<n>(out_type, p.add, (r0 + i) * p.add_stride + h, a);
+      } else {
 #pragma unroll
-        for (int c = 0; c < n; ++c) y[c] = __fadd_rn(a[c], y[c]);
+        for (int c = 0; c < n; ++c) y[c] = 0.f;
       }
-      em_store_as<n>(out_type, p.out, (r0 + i) * p.out_stride + h, y);
+      if (kAdd) {
+        const EmWord<kOut, n>& a = add[kAdd ? i : 0];
+        if (!kWide && f16) {
+          EmWord<kTabF16, n> b;
+#pragma unroll
+          for (int c = 0; c < static_cast<int>(sizeof a.w / 4); ++c) b.w[c] = a.w[c];
+#pragma unroll
+          for (int c = 0; c < n; ++c) y[c] = __fadd_rn(b.get(c), y[c]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < n; ++c) y[c] = __fadd_rn(a.get(c), y[c]);
+        }
+      }
+      if (!kWide && f16) em_store<kTabF16, n>(to, y);
+      else em_store<kOut, n>(to, y);
     }
   }
 }
 
-template <int kType, int n>
+template <int kType, bool kWide, bool kAdd, int n>
 cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
   const long long slices = (p.H + kEmThreads * n - 1) / (kEmThreads * n);
   // several rows of a CTA where there are CTAs enough all the same
-  const int rows = p.N * slices >= 8ll * kEmRows * num_sms ? kEmRows : 1;
+  const int rows = p.N * slices >= 8ll * em_rows<kType>() * num_sms ? em_rows<kType>() : 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((p.N + rows - 1) / rows), static_cast<unsigned>(slices > 65535 ? 65535 : slices));
   cfg.blockDim = dim3(kEmThreads); cfg.stream = stream;
@@ -218,16 +253,22 @@ cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStrea
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, embed_kernel<kType, n>, p, out_type, rows);
+  return cudaLaunchKernelEx(&cfg, embed_kernel<kType, kWide, kAdd, n>, p, out_type == kTabF16 ? 1 : 0, rows);
+}
+template <int kType, int n>
+cudaError_t launch_embed_as(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
+  if (out_type == kTabF32)
+    return p.add ? launch_embed<kType, true, true, n>(p, out_type, num_sms, stream) : launch_embed<kType, true, false, n>(p, out_type, num_sms, stream);
+  return p.add ? launch_embed<kType, false, true, n>(p, out_type, num_sms, stream) : launch_embed<kType, false, false, n>(p, out_type, num_sms, stream);
 }
 template <int n>
 cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_sms, cudaStream_t stream) {
   switch (type) {
-    case kTabF32: return launch_embed<kTabF32, n>(p, out_type, num_sms, stream);
-    case kTabBf16: return launch_embed<kTabBf16, n>(p, out_type, num_sms, stream);
-    case kTabF16: return launch_embed<kTabF16, n>(p, out_type, num_sms, stream);
-    case kTabInt8: return launch_embed<kTabInt8, n>(p, out_type, num_sms, stream);
-    default: return launch_embed<kTabMixed, n>(p, out_type, num_sms, stream);
+    case kTabF32: return launch_embed_as<kTabF32, n>(p, out_type, num_sms, stream);
+    case kTabBf16: return launch_embed_as<kTabBf16, n>(p, out_type, num_sms, stream);
+    case kTabF16: return launch_embed_as<kTabF16, n>(p, out_type, num_sms, stream);
+    case kTabInt8: return launch_embed_as<kTabInt8, n>(p, out_type, num_sms, stream);
+    default: return launch_embed_as<kTabMixed, n>(p, out_type, num_sms, stream);
   }
 }
 
@@ -509,7 +550,9 @@ __device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long l
 
 template <int kType, bool kVec>
 __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
-  __shared__ int rows[kEgMaxWindow + kEgMaxPiece];       // of the gradient, for the places of the pieces that begin in the window
+  // for the places of the pieces that begin in the window: rows of the gradient, and whether a piece ends there
+  __shared__ __align__(16) int rows[kEgMaxWindow + kEgMaxPiece + kEgAhead];
+  __shared__ __align__(16) uint8_t piece_ends[kEgMaxWindow + kEgMaxPiece + kEgAhead];
   __shared__ int4 spots[kEgMaxWindow];
   __shared__ int firsts[kEgMaxWindow + 1], out_rows[kEgMaxWindow];
   __shared__ int part_sum[kEgThreads / 32];
@@ -555,7 +598,18 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     const int4 last = spots[w1 - 1 - w0];
     x1 = min(last.z + ((w1 - 1 - last.z) / p.S + 1) * p.S, last.w);
   }
-  for (int i = tid; i < x1 - x0; i += kEgThreads) rows[i] = x0 + i < w1 ? spots[x0 + i - w0].x : p.places[x0 + i].x;
+  for (int i = tid; i < x1 - x0; i += kEgThreads) {
+    // (places behind the window belong to the last piece)
+    bool ends = x0 + i + 1 == x1;
+    if (x0 + i < w1) {
+      const int4 here = spots[x0 + i - w0];
+      rows[i] = here.x;
+      ends = x0 + i + 1 == here.w || (x0 + i + 1 - here.z) % p.S == 0;
+    } else {
+      rows[i] = p.places[x0 + i].x;
+    }
+    piece_ends[i] = ends ? 1 : 0;
+  }
   if (p.by_rows) {
     // The distinct ids ahead of an id's own range, and ahead of it there.
     __shared__ int range0;
@@ -582,17 +636,20 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
 #pragma unroll 1
   for (int x = x0; x < x1; x += kEgAhead) {
     EgRow<kType, kVec> g[kEgAhead];
+    const int n = min(kEgAhead, x1 - x);
+    const int4 some = *reinterpret_cast<const int4*>(rows + (x - x0)), more = *reinterpret_cast<const int4*>(rows + (x - x0) + 4);
+    const int at[kEgAhead] = {some.x, some.y, some.z, some.w, more.x, more.y, more.z, more.w};
+    const uint64_t last = *reinterpret_cast<const uint64_t*>(piece_ends + (x - x0));
 #pragma unroll
     for (int u = 0; u < kEgAhead; ++u)
-      if (x + u < x1) g[u].load(p, rows[x + u - x0], slice);
+      if (u < n) g[u].load(p, at[u], slice);
 #pragma unroll
     for (int u = 0; u < kEgAhead; ++u) {
-      if (x + u >= x1) break;
+      if (u >= n) break;
 #pragma unroll
       for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u].get(i));
-      // (places behind the window belong to the last piece)
-      const int k = min(x + u, w1 - 1) - w0, begin = spots[k].z, end = spots[k].w, next = x + u + 1;
-      if (next != end && (next - begin) % p.S != 0) continue;
+      if (!(last >> (8 * u) & 1u)) continue;
+      const int k = min(x + u, w1 - 1) - w0, begin = spots[k].z, end = spots[k].w;
       if (end - begin > p.S) {
         // One of several pieces.
         const int from = begin + (x + u - begin) / p.S * p.S;
@@ -675,9 +732,7 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
   cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
   cfg.gridDim = dim3(static_cast<unsigned>(p.buckets)); cfg.blockDim = dim3(kEsThreads);
   cfg.dynamicSmemBytes = kEsDynamic;
-  auto* sort = p.N <= UINT16_MAX ? embed_sort_kernel<uint16_t> : embed_sort_kernel<uint32_t>;
-  cudaError_t e = cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsDynamic);
-  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, sort, p);
+  const cudaError_t e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t>, p);
   if (e != cudaSuccess) return e;
   const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
   const long long blank = p.first ? (static_cast<long long>(p.V) + kEgMaxWindow - 1) / kEgMaxWindow : 0;
@@ -685,4 +740,9 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
   cfg.dynamicSmemBytes = 0;
   return vec ? cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, true>, p, out_type, static_cast<int>(windows))
              : cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, false>, p, out_type, static_cast<int>(windows));
+}
+
+cudaError_t configure_embedding() {
+  const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel<uint16_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsDynamic);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_sort_kernel<uint32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsDynamic);
 }

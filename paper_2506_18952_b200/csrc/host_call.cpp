@@ -22,6 +22,11 @@ namespace {
 typedef hola_status (*EntryFn)(hola_ctx*, const hola_verify_args*, void*);
 typedef hola_status (*AdapterFn)(hola_ctx*, const hola_verify_args*, const hola_adapters*, void*);
 typedef hola_status (*ScoreFn)(const hola_logprobs_args*, void*);
+typedef hola_status (*SelectFn)(const hola_beam_args*, void*);
+typedef hola_status (*ReorderFn)(const hola_reorder_args*, void*);
+typedef hola_status (*EmbedFn)(const hola_embed_args*, void*);
+typedef hola_status (*GradFn)(const hola_embed_grad_args*, void*);
+typedef size_t (*WorkspaceFn)(long long, int, int);
 
 // A tensor whose memory can be handed over as it is: null for anything else.
 const at::Tensor* plain(PyObject* o) {
@@ -376,10 +381,263 @@ PyObject* quantize(PyObject*, PyObject* const* v, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// What the calls below have in common: operands on the current device, of a given type, contiguous and of a given shape.
+struct Operands {
+  int32_t device;
+  const at::Tensor* on_device(PyObject* o) const {
+    const at::Tensor* x = plain(o);
+    return x && x->is_cuda() && x->get_device() == device ? x : nullptr;
+  }
+  // Pointer, or null for anything else.
+  void* of(PyObject* o, at::ScalarType t, at::IntArrayRef size) const {
+    const at::Tensor* x = on_device(o);
+    return x && x->scalar_type() == t && x->is_contiguous() && x->sizes() == size ? x->data_ptr() : nullptr;
+  }
+  // The same of an optional one: false for anything that is neither.
+  template <typename P>
+  bool perhaps(PyObject* o, at::ScalarType t, at::IntArrayRef size, P** p) const {
+    if (o == Py_None) return true;
+    *p = static_cast<P*>(of(o, t, size));
+    return *p != nullptr;
+  }
+};
+
+// Rows of `t` [..., H] at one distance, of the leading shape `shape`: the distance, -1 where they are not.
+int64_t rows_apart(const at::Tensor& t, at::IntArrayRef shape) {
+  const int64_t axes = t.dim() - 1;
+  if (axes < 0 || t.sizes().slice(0, axes) != shape || (t.size(axes) > 1 && t.stride(axes) != 1)) return -1;
+  int64_t rows = 1, stride = -1;
+  for (int64_t i = axes - 1; i >= 0; --i) {
+    if (t.size(i) == 1) continue;
+    if (stride < 0) stride = t.stride(i);
+    else if (t.stride(i) != stride * rows) return -1;
+    rows *= t.size(i);
+  }
+  return stride < 0 ? t.size(axes) : stride;
+}
+
+int float_type(at::ScalarType t) { return t == at::kFloat ? HOLA_T_F32 : t == at::kBFloat16 ? HOLA_T_BF16 : t == at::kHalf ? HOLA_T_F16 : -1; }
+
+bool truth(PyObject* o, int32_t* v) {
+  if (o != Py_True && o != Py_False) return false;
+  *v = o == Py_True;
+  return true;
+}
+bool number(PyObject* o, float* v) {
+  long long whole = 0;
+  if (PyFloat_CheckExact(o)) *v = static_cast<float>(PyFloat_AS_DOUBLE(o));
+  else if (integer(o, &whole)) *v = static_cast<float>(static_cast<double>(whole));
+  else return false;
+  return true;
+}
+PyObject* wrapped(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); }
+
+// beam_select(function, logits, logZ, score, n or None, finished, end_token, weight, keep_slots, status, current device, stream) ->
+// (status, score, parent, token, finished), or None where the caller has to go the long way.
+PyObject* beam_select(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 12) { PyErr_SetString(PyExc_TypeError, "beam_select() takes 12 arguments"); return nullptr; }
+  void *fn = nullptr, *stream = nullptr;
+  Operands in;
+  hola_beam_args a = {};
+  if (!address(v[0], &fn) || !fn || !int32(v[10], &in.device) || !address(v[11], &stream) || !int32(v[6], &a.end_token) || !truth(v[8], &a.keep_slots))
+    Py_RETURN_NONE;
+  const at::Tensor* l = in.on_device(v[1]);
+  if (!l || l->dim() != 3 || l->numel() == 0 || l->size(0) > INT32_MAX || l->size(1) > HOLA_MAX_BEAMS || l->size(2) > 1 << 27 ||
+      (l->size(2) > 1 && l->stride(2) != 1))
+    Py_RETURN_NONE;
+  const int type = float_type(l->scalar_type());
+  if (type < 0) Py_RETURN_NONE;
+  a.l_dtype = type == HOLA_T_F32 ? HOLA_L_F32 : type == HOLA_T_BF16 ? HOLA_L_BF16 : HOLA_L_F16;
+  a.B = static_cast<int32_t>(l->size(0)); a.W = static_cast<int32_t>(l->size(1)); a.V = static_cast<int32_t>(l->size(2));
+  a.logits = l->data_ptr(); a.seq_stride = l->stride(0); a.beam_stride = l->stride(1);
+  if (v[4] == Py_None) a.n = a.W;
+  else if (!int32(v[4], &a.n)) Py_RETURN_NONE;
+  if (a.n < 1 || a.n > HOLA_MAX_BEAMS || (a.keep_slots && a.n != a.W) || a.end_token < -1 || a.end_token >= a.V) Py_RETURN_NONE;
+  const at::IntArrayRef beams = l->sizes().slice(0, 2);
+  if (!(a.logZ = static_cast<const float*>(in.of(v[2], at::kFloat, beams))) || !(a.score = static_cast<const float*>(in.of(v[3], at::kFloat, beams))) ||
+      !in.perhaps(v[5], at::kBool, beams, &a.finished) || (a.finished && a.end_token < 0) || !in.perhaps(v[7], at::kFloat, beams, &a.weight) ||
+      !in.perhaps(v[9], at::kInt, {1}, &a.status_word))
+    Py_RETURN_NONE;
+  at::Tensor score, parent, token, finished;
+  hola_status s = HOLA_OK;
+  Py_BEGIN_ALLOW_THREADS
+  try {
+    const auto f32 = at::TensorOptions().dtype(at::kFloat).device(l->device());
+    const auto i32 = f32.dtype(at::kInt);
+    score = at::empty({a.B, a.n}, f32); a.score_out = static_cast<float*>(score.data_ptr());
+    parent = at::empty({a.B, a.n}, i32); a.parent = static_cast<int32_t*>(parent.data_ptr());
+    token = at::empty({a.B, a.n}, i32); a.token = static_cast<int32_t*>(token.data_ptr());
+    if (a.end_token >= 0) { finished = at::empty({a.B, a.n}, f32.dtype(at::kBool)); a.finished_out = static_cast<uint8_t*>(finished.data_ptr()); }
+    s = reinterpret_cast<SelectFn>(fn)(&a, stream);
+  } catch (...) {
+    Py_BLOCK_THREADS
+    throw;
+  }
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("iNNNN", static_cast<int>(s), wrapped(score), wrapped(parent), wrapped(token), wrapped(finished));
+  END_HANDLE_TH_ERRORS
+}
+
+// beam_reorder(function, address of the states, their number, B, W, beams behind the step, parent, used, status, current device, stream)
+// -> status, or None where the caller has to go the long way.
+PyObject* beam_reorder(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11) { PyErr_SetString(PyExc_TypeError, "beam_reorder() takes 11 arguments"); return nullptr; }
+  void *fn = nullptr, *stream = nullptr, *states = nullptr;
+  Operands in;
+  int32_t most = 0;
+  hola_reorder_args a = {};
+  if (!address(v[0], &fn) || !fn || !address(v[1], &states) || !states || !int32(v[2], &a.count) || !int32(v[3], &a.B) || !int32(v[4], &a.W) ||
+      !int32(v[5], &most) || !int32(v[9], &in.device) || !address(v[10], &stream))
+    Py_RETURN_NONE;
+  const at::Tensor* t = in.on_device(v[6]);
+  if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != a.B || t->size(1) < 1 || t->size(1) > most ||
+      (t->size(1) > 1 && t->stride(1) != 1))
+    Py_RETURN_NONE;
+  a.states = static_cast<const hola_beam_state*>(states);
+  a.n = static_cast<int32_t>(t->size(1)); a.parent = static_cast<const int32_t*>(t->data_ptr()); a.parent_stride = t->stride(0);
+  if (!in.perhaps(v[7], at::kInt, {a.B}, &a.used) || !in.perhaps(v[8], at::kInt, {1}, &a.status_word)) Py_RETURN_NONE;
+  hola_status s;
+  Py_BEGIN_ALLOW_THREADS
+  s = reinterpret_cast<ReorderFn>(fn)(&a, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(s);
+  END_HANDLE_TH_ERRORS
+}
+
+// The tokens of a lookup or its gradient.
+template <typename Args>
+const at::Tensor* token_ids(const Operands& in, PyObject* o, Args* a) {
+  const at::Tensor* t = in.on_device(o);
+  if (!t || !t->is_contiguous() || t->numel() == 0 || t->numel() >= INT32_MAX || (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong)) return nullptr;
+  a->N = t->numel(); a->tokens = t->data_ptr(); a->wide_tokens = t->scalar_type() == at::kLong;
+  return t;
+}
+
+// embed(function, tokens, table, address of the hola_wmix of a head of mixed widths or 0, its V, its H, scale, add, w_scale, type of the
+// result (hola_t_dtype, -1: the table's), v_offset, V_global, status, current device, stream) -> (status, result), or None where the caller
+// has to go the long way.
+PyObject* embed(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 15) { PyErr_SetString(PyExc_TypeError, "embed() takes 15 arguments"); return nullptr; }
+  void *fn = nullptr, *stream = nullptr, *mix = nullptr;
+  Operands in;
+  hola_embed_args a = {};
+  if (!address(v[0], &fn) || !fn || !address(v[3], &mix) || !int32(v[4], &a.V) || !int32(v[5], &a.H) || !number(v[6], &a.scale) ||
+      !int32(v[9], &a.out_dtype) || !int32(v[10], &a.v_offset) || !int32(v[11], &a.V_global) || !int32(v[13], &in.device) || !address(v[14], &stream))
+    Py_RETURN_NONE;
+  const at::Tensor* t = token_ids(in, v[1], &a);
+  if (!t) Py_RETURN_NONE;
+  int own = HOLA_T_BF16;
+  if (mix) {
+    a.t_dtype = HOLA_T_MIXED; a.wmix = static_cast<const hola_wmix*>(mix);
+  } else {
+    const at::Tensor* w = in.on_device(v[2]);
+    if (!w || w->dim() != 2 || w->numel() == 0 || w->size(0) > INT32_MAX || w->size(1) > INT32_MAX) Py_RETURN_NONE;
+    a.V = static_cast<int32_t>(w->size(0)); a.H = static_cast<int32_t>(w->size(1));
+    a.row_stride = rows_apart(*w, w->sizes().slice(0, 1));
+    a.table = w->data_ptr();
+    if (w->scalar_type() == at::kChar) a.t_dtype = HOLA_T_INT8;
+    else a.t_dtype = own = float_type(w->scalar_type());
+    if (a.row_stride < 0 || a.t_dtype < 0) Py_RETURN_NONE;
+  }
+  if ((a.t_dtype >= HOLA_T_INT8) != (v[8] != Py_None) || !in.perhaps(v[8], at::kFloat, {a.V}, &a.w_scale)) Py_RETURN_NONE;
+  const at::Tensor* add = nullptr;
+  if (v[7] != Py_None) {
+    add = in.on_device(v[7]);
+    if (!add || add->dim() < 1 || add->size(-1) != a.H || float_type(add->scalar_type()) < 0) Py_RETURN_NONE;
+    own = float_type(add->scalar_type());
+    a.add = add->data_ptr(); a.add_stride = rows_apart(*add, t->sizes());
+    if (a.add_stride < 0) Py_RETURN_NONE;
+  }
+  if (a.out_dtype < 0) a.out_dtype = own;
+  if (add && a.out_dtype != own) Py_RETURN_NONE;
+  if (a.v_offset < 0 || a.V_global < 0 || (a.V_global ? static_cast<int64_t>(a.v_offset) + a.V > a.V_global : a.v_offset != 0) ||
+      !in.perhaps(v[12], at::kInt, {1}, &a.status_word))
+    Py_RETURN_NONE;
+  at::Tensor out;
+  hola_status s = HOLA_OK;
+  Py_BEGIN_ALLOW_THREADS
+  try {
+    at::DimVector size(t->sizes().begin(), t->sizes().end());
+    size.push_back(a.H);
+    out = at::empty(size, at::TensorOptions().dtype(a.out_dtype == HOLA_T_F32 ? at::kFloat : a.out_dtype == HOLA_T_BF16 ? at::kBFloat16 : at::kHalf)
+                              .device(t->device()));
+    a.out = out.data_ptr(); a.out_stride = a.H;
+    s = reinterpret_cast<EmbedFn>(fn)(&a, stream);
+  } catch (...) {
+    Py_BLOCK_THREADS
+    throw;
+  }
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("iN", static_cast<int>(s), wrapped(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// embed_grad(function, that of the workspace's size, tokens, grad, V, scale, type of the result (hola_t_dtype), v_offset, V_global, by rows, ids,
+// rows, count (None: made here), status, current device, stream) -> (status, the table's gradient or the rows, ids, count), or None where
+// the caller has to go the long way.
+PyObject* embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 16) { PyErr_SetString(PyExc_TypeError, "embed_grad() takes 16 arguments"); return nullptr; }
+  void *fn = nullptr, *size_fn = nullptr, *stream = nullptr;
+  Operands in;
+  int32_t by_rows = 0;
+  hola_embed_grad_args a = {};
+  if (!address(v[0], &fn) || !fn || !address(v[1], &size_fn) || !size_fn || !int32(v[4], &a.V) || !number(v[5], &a.scale) || !int32(v[6], &a.out_dtype) ||
+      !int32(v[7], &a.v_offset) || !int32(v[8], &a.V_global) || !truth(v[9], &by_rows) || !int32(v[14], &in.device) || !address(v[15], &stream))
+    Py_RETURN_NONE;
+  const at::Tensor *t = token_ids(in, v[2], &a), *g = in.on_device(v[3]);
+  if (!t || !g || g->dim() < 1 || g->size(-1) < 1 || g->size(-1) > INT32_MAX || a.V < 1 || float_type(g->scalar_type()) < 0) Py_RETURN_NONE;
+  a.H = static_cast<int32_t>(g->size(-1)); a.g_dtype = float_type(g->scalar_type());
+  a.grad = g->data_ptr(); a.grad_stride = rows_apart(*g, t->sizes());
+  if (a.grad_stride < 0 || a.out_dtype < 0 || a.out_dtype > HOLA_T_F16 || a.v_offset < 0 || a.V_global < 0 ||
+      (a.V_global ? static_cast<int64_t>(a.v_offset) + a.V > a.V_global : a.v_offset != 0) || !in.perhaps(v[13], at::kInt, {1}, &a.status_word))
+    Py_RETURN_NONE;
+  at::Tensor out, ids, count, workspace;
+  const bool given = v[11] != Py_None;
+  if (given) {
+    const at::Tensor* x = in.on_device(v[11]);
+    if (!by_rows || !x || x->dim() != 2 || x->size(0) != a.N || x->size(1) != a.H || float_type(x->scalar_type()) < 0) Py_RETURN_NONE;
+    a.out_dtype = float_type(x->scalar_type());
+    a.out = x->data_ptr(); a.out_stride = rows_apart(*x, x->sizes().slice(0, 1));
+    a.ids_out = static_cast<int32_t*>(in.of(v[10], at::kInt, {a.N})); a.count_out = static_cast<int32_t*>(in.of(v[12], at::kInt, {1}));
+    if (a.out_stride < 0 || !a.ids_out || !a.count_out) Py_RETURN_NONE;
+  }
+  hola_status s = HOLA_OK;
+  Py_BEGIN_ALLOW_THREADS
+  try {
+    const auto on = at::TensorOptions().device(t->device());
+    if (!given) {
+      out = at::empty({by_rows ? a.N : a.V, a.H}, on.dtype(a.out_dtype == HOLA_T_F32 ? at::kFloat : a.out_dtype == HOLA_T_BF16 ? at::kBFloat16 : at::kHalf));
+      a.out = out.data_ptr(); a.out_stride = a.H;
+      if (by_rows) {
+        ids = at::empty({a.N}, on.dtype(at::kInt)); a.ids_out = static_cast<int32_t*>(ids.data_ptr());
+        count = at::empty({1}, on.dtype(at::kInt)); a.count_out = static_cast<int32_t*>(count.data_ptr());
+      }
+    }
+    a.workspace_bytes = reinterpret_cast<WorkspaceFn>(size_fn)(a.N, a.V, a.H);
+    workspace = at::empty({static_cast<int64_t>(a.workspace_bytes)}, on.dtype(at::kByte));
+    a.workspace = workspace.data_ptr();
+    s = reinterpret_cast<GradFn>(fn)(&a, stream);
+  } catch (...) {
+    Py_BLOCK_THREADS
+    throw;
+  }
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("iNNN", static_cast<int>(s), wrapped(out), wrapped(ids), wrapped(count));
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL, nullptr},
     {"outputs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(outputs)), METH_FASTCALL, nullptr},
     {"score", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(score)), METH_FASTCALL, nullptr},
+    {"beam_select", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(beam_select)), METH_FASTCALL, nullptr},
+    {"beam_reorder", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(beam_reorder)), METH_FASTCALL, nullptr},
+    {"embed", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embed)), METH_FASTCALL, nullptr},
+    {"embed_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embed_grad)), METH_FASTCALL, nullptr},
     {"quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantize)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -551,3 +551,33 @@ def test_operands_that_are_refused():
                          (p.t().contiguous().t(), None), (p, p[0]), (p, torch.zeros(2, device="cuda"))):
         with pytest.raises(binding.HolaError):
             binding.hola_beam_reorder(states, parent, used)
+
+
+@gpu
+def test_calls_through_the_native_helper_and_without_it(monkeypatch):
+    """The same results and the same refusals either way."""
+    l, z, s = make(3, 4, 500, torch.float16, 6, pad=3)
+    f = torch.zeros((3, 4), dtype=torch.bool, device="cuda")
+    f[1, 2] = True
+    w = torch.rand((3, 4), device="cuda") + 0.5
+    calls = [lambda: binding.hola_beam_select(l, z, s), lambda: binding.hola_beam_select(l, z, s, 7, f, 9, w),
+             lambda: binding.hola_beam_select(l, z, s, 4, f, 9, keep_slots=True), lambda: binding.hola_beam_select(l[:0], z[:0], s[:0], 3),
+             lambda: binding.hola_beam_select(l, z.half(), s), lambda: binding.hola_beam_select(l, z, s, 33), lambda: binding.hola_beam_select(l, z, s, 5, f)]
+
+    def run():
+        got = []
+        for call in calls:
+            try:
+                o = call()
+                got.append((o.score.cpu(), o.parent.cpu(), o.token.cpu(), None if o.finished is None else o.finished.cpu()))
+            except binding.HolaError as e:
+                got.append(str(e))
+        x = anything((3, 4, 50), torch.int32, 1)
+        binding.hola_beam_reorder(binding.BeamStates([x]), got[0][1].cuda())
+        return [*got, (x.cpu(),)]
+
+    assert binding._host is not None
+    with_it = run()
+    monkeypatch.setattr(binding, "_host", None)
+    for a, b in zip(with_it, run(), strict=True):
+        assert a == b if isinstance(a, str) else all((x is None and y is None) or torch.equal(x, y) for x, y in zip(a, b, strict=True))

@@ -408,3 +408,72 @@ def test_operands_that_are_refused():
                 binding.TokenRows(ids.long(), rows, count), binding.TokenRows(ids, rows.cpu(), count)):
         with pytest.raises(binding.HolaError):
             binding.hola_embed_grad_rows(t, g, 5, out=out)
+
+
+@gpu
+def test_calls_through_the_native_helper_and_without_it(monkeypatch):
+    """The same results and the same refusals either way."""
+    V, H = 300, 128
+    t = some_tokens(40, V, 1).view(5, 8)
+    W, add, g = rnd((V, H), torch.bfloat16, 2), rnd((5, 8, H), torch.float32, 3), rnd((5, 8, H), torch.float16, 4)
+    q, scale = binding.hola_quantize_w8(W)
+    head = binding.hola_quantize_mixed(W, [4, 8])
+    rows = lambda r: (lambda n: [r.ids[:n], r.rows[:n], r.count])(r.count.item())          # noqa: E731
+    calls = [lambda: binding.hola_embed(t, W), lambda: binding.hola_embed(t.long(), W, 2, add=add), lambda: binding.hola_embed(t, q, 0.5, w_scale=scale),
+             lambda: binding.hola_embed(t, head, dtype=torch.float32), lambda: binding.hola_embed(t, head, 3.0, add=add), lambda: binding.hola_embed(t[:0], W),
+             lambda: binding.hola_embed(t, W[5:], v_offset=5, V_global=V), lambda: binding.hola_embed(t, W.float().t()),
+             lambda: binding.hola_embed(t, W, add=add, dtype=torch.bfloat16), lambda: binding.hola_embed(t, W, dtype=torch.int32),
+             lambda: binding.hola_embed(t, W, v_offset=5), lambda: binding.hola_embed_grad(t, g, V, 2.0), lambda: binding.hola_embed_grad(t, g, V, dtype=torch.bfloat16),
+             lambda: binding.hola_embed_grad(t[:0], g[:0], V), lambda: binding.hola_embed_grad(t, g[:2], V), lambda: rows(binding.hola_embed_grad_rows(t, g, V)),
+             lambda: rows(binding.hola_embed_grad_rows(t, g, 50, v_offset=10, V_global=V, dtype=torch.float16)), lambda: binding.hola_embed_grad_rows(t, g, 0)]
+
+    def run():
+        got = []
+        for call in calls:
+            try:
+                o = call()
+                got.append([x.cpu() for x in (o if isinstance(o, list) else [o])])
+            except binding.HolaError as e:
+                got.append(str(e))
+        return got
+
+    assert binding._host is not None
+    with_it = run()
+    monkeypatch.setattr(binding, "_host", None)
+    for a, b in zip(with_it, run(), strict=True):
+        assert a == b if isinstance(a, str) else all(x.dtype == y.dtype and torch.equal(x, y) for x, y in zip(a, b, strict=True))
+
+
+@gpu
+def test_outputs_on_another_stream_are_not_written_over():
+    """Results of a call on another stream, dropped while the current one has still to read them, and the other way round."""
+    N, V, H = 3000, 400, 512
+    table = rnd((V, H), torch.float32, 1)
+    tokens, grads = [some_tokens(N, V, i) for i in (2, 3)], [rnd((N, H), torch.float32, i) for i in (4, 5)]
+    scores = [rnd((4, 3, 3000), torch.float32, i) for i in (6, 7)]
+    logZ, score = [torch.logsumexp(x, 2) for x in scores], torch.zeros((4, 3), device="cuda")
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    calls = [lambda i, s: [binding.hola_embed(tokens[i], table, stream=s)], lambda i, s: [binding.hola_embed_grad(tokens[i], grads[i], V, stream=s)],
+             lambda i, s: [binding.hola_embed_grad_rows(tokens[i], grads[i], V, stream=s).count],
+             lambda i, s: list(vars(binding.hola_beam_select(scores[i], logZ[i], score, stream=s)).values())[:3]]
+
+    def busy(stream):
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(40_000_000)
+    for call in calls:
+        want = [[t.clone() for t in call(i, None)] for i in (0, 1)]
+        torch.cuda.synchronize()
+        got = call(0, side)
+        here.wait_stream(side)
+        busy(here)
+        kept = [t.clone() for t in got]
+        del got
+        other = call(1, side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(kept, want[0])) and all(torch.equal(a, b) for a, b in zip(other, want[1]))
+        busy(side)
+        call(0, side)                                         # dropped at once
+        fresh = [torch.full_like(t, 7) for t in want[0]]
+        torch.cuda.synchronize()
+        assert all((t == 7).all() for t in fresh)
+        del kept, other, fresh

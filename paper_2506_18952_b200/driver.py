@@ -6,14 +6,18 @@ verifier's test) and which token follows them, and the context grows by accept_l
 claim is that verifier invocations drop from one per token to one per round; the loop reports exactly that ratio
 (tokens emitted per verifier call) together with the time spent inside the verify step.
 
+Beside it, beam_decode searches with W beams per sequence on the same verifier: its LM head on the beams' positions, the best
+continuations of all beams, their states in the order of the parents, the next embeddings.
+
 The two models are seeded synthetic stand-ins (the paper's trained draft / verifier checkpoints are not used): both
 read the context through embedding tables and share the LM head; the verifier sees two tokens back, the draft only
 one, so q is close to p but not equal.  They are harness code in stock torch; every step of the verify path itself
 runs in the CUDA library.  Everything stays on the device: no host read-back inside the loop.
 
-Two options of the serving path: `score` has the emitted tokens' log probabilities under the verifier (hola_token_logprobs, on the
+Three options of the serving path: `score` has the emitted tokens' log probabilities under the verifier (hola_token_logprobs, on the
 logits and logZ that the verify call leaves), and a bank of low-rank adapters gives every sequence its own LM head
-(hola_verify_adapters).
+(hola_verify_adapters), and `distill` moves the draft's embedding table towards the verifier after every round, by the gradient of the
+tokens that the round was drawn from (hola_embed_grad_rows).
 """
 from __future__ import annotations
 
@@ -47,12 +51,32 @@ class SyntheticPair:
 
     def target_hidden(self, prev1: torch.Tensor, prev2: torch.Tensor) -> torch.Tensor:
         """Verifier trunk stand-in: hidden state for the position that follows (..., prev2, prev1).  bf16 [..., H]."""
-        return self._norm(self.E1[prev1] + 0.35 * self.E2[prev2], prev1).to(torch.bfloat16)
+        return self.target_hidden_from(prev1, binding.hola_embed(prev2.contiguous(), self.E2, scale=0.35))
 
-    def draft_probs(self, prev1: torch.Tensor) -> torch.Tensor:
-        """Draft model stand-in: q(. | prev1), fp32 [..., V]."""
-        h = self._norm(self.E1[prev1], prev1).to(torch.bfloat16).float()
+    def target_hidden_from(self, prev1: torch.Tensor, state: torch.Tensor) -> torch.Tensor:
+        """The same from what the trunk keeps of the token before, 0.35 E2[prev2], fp32 [..., H]."""
+        return self._norm(binding.hola_embed(prev1.contiguous(), self.E1, add=state), prev1).to(torch.bfloat16)
+
+    def draft_table(self) -> torch.Tensor:
+        """The draft's own copy of its embedding table, for hsd_decode's distill."""
+        return self.E1.clone()
+
+    def draft_probs(self, prev1: torch.Tensor, table: torch.Tensor | None = None) -> torch.Tensor:
+        """Draft model stand-in: q(. | prev1), fp32 [..., V].  table: the draft's own embedding table."""
+        e = binding.hola_embed(prev1.contiguous(), self.E1 if table is None else table)
+        h = self._norm(e, prev1).to(torch.bfloat16).float()
         return torch.softmax(h @ self.W_lm.float().T, dim=-1)
+
+    def draft_grad(self, prev1: torch.Tensor, table: torch.Tensor, p: torch.Tensor) -> binding.TokenRows:
+        """Gradient of the mean KL(p || q(. | prev1)) over the positions prev1 [...] by the draft's table, p fp32 [..., V]: (q - p) / n
+        through the head and the normalisation, and by tokens into rows of the table.  (The roundings of h to 16 bits are passed over.)"""
+        prev1 = prev1.reshape(-1)
+        e = binding.hola_embed(prev1, table)
+        norm, gain = e.norm(dim=-1, keepdim=True), self.gain[prev1].unsqueeze(-1)
+        d = (self.draft_probs(prev1, table) - p.reshape(-1, self.V)) / prev1.numel()
+        dh = d @ self.W_lm.float()
+        unit = e / norm
+        return binding.hola_embed_grad_rows(prev1, gain / norm * (dh - unit * (unit * dh).sum(dim=-1, keepdim=True)), self.V)
 
 
 def seeded_adapters(models: SyntheticPair, slots: int, rank: int, seed: int, strength: float = 0.25) -> binding.AdapterBank:
@@ -86,13 +110,16 @@ class DecodeResult:
     accepted: torch.Tensor      # int64 [B]: draft tokens kept, summed over the rounds
     logprob: torch.Tensor | None = None   # fp64 [B]: log probability of a sequence's emitted tokens under the verifier (score)
     records: list = field(default_factory=list)
+    draft_table: torch.Tensor | None = None   # fp32 [V, H]: the draft's embedding table as it has been moved (distill)
 
 
 def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Tensor, k: int, tau: float, rounds: int,
                seed: int, gate_source: int = 0, fallback: int = 0, keep_records: bool = False, score: bool = False,
-               adapters: binding.AdapterBank | None = None, adapter_ids: torch.Tensor | None = None) -> DecodeResult:
+               adapters: binding.AdapterBank | None = None, adapter_ids: torch.Tensor | None = None,
+               distill: float = 0.0) -> DecodeResult:
     """Runs `rounds` draft-and-verify rounds for a batch of sequences.  prompt: int64 [B, 2] (two context tokens).  score: the
-    emitted tokens' log probabilities are summed up.  adapters, adapter_ids: the sequences' LM-head adapters."""
+    emitted tokens' log probabilities are summed up.  adapters, adapter_ids: the sequences' LM-head adapters.  distill: step size by which
+    the draft's own copy of its embedding table follows the gradient of KL(verifier || draft) over each round's draft positions."""
     dev = prompt.device
     B = prompt.shape[0]
     g = torch.Generator(device=dev)
@@ -104,7 +131,8 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
     accepted = torch.zeros((B,), dtype=torch.int64, device=dev)
     rows = torch.arange(B, device=dev)
     steps = torch.arange(k + 1, device=dev)
-    out = ctx.alloc_outputs(B, k, score)
+    table = models.draft_table() if distill else None
+    out = ctx.alloc_outputs(B, k, score or bool(distill))
     options = dict(out=out, gate_source=gate_source, fallback=fallback)
     logprob = torch.zeros((B,), dtype=torch.float64, device=dev) if score else None
     records = []
@@ -118,7 +146,7 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
         draft_q = torch.empty((B, k, models.V), dtype=torch.bfloat16, device=dev)
         prev = last1
         for j in range(k):
-            q = models.draft_probs(prev).to(torch.bfloat16)
+            q = models.draft_probs(prev, table).to(torch.bfloat16)
             draft_q[:, j] = q
             prev = torch.multinomial(q.float(), 1, generator=g).squeeze(1)
             draft_tok[:, j] = prev
@@ -137,6 +165,11 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
         if score:
             scored = binding.hola_token_logprobs(out.logits, logZ=out.logZ, emitted=(tok32, out.accept_len, out.next_tok), want_rank=False)
             logprob += scored.logprob.double().sum(dim=1)
+        if distill and k > 0:
+            # distinct tokens' rows alone; what lies behind them goes, times zero, to row 0
+            got = models.draft_grad(c1[:, :k], table, torch.exp(out.logits[:, :k] - out.logZ[:, :k, None]))
+            have = torch.arange(got.ids.numel(), device=dev) < got.count
+            table.index_add_(0, torch.where(have, got.ids, 0), torch.where(have[:, None], got.rows, 0.0), alpha=-distill)
         # the context grows by the accepted drafts and the verifier's token (no host read-back)
         n = out.accept_len.to(torch.int64)
         new = torch.cat([draft_tok, torch.zeros((B, 1), dtype=torch.int64, device=dev)], dim=1)
@@ -153,7 +186,44 @@ def hsd_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Ten
     ev[-1].record()
     torch.cuda.synchronize()
     verify_ms = sum(ev[2 * r].elapsed_time(ev[2 * r + 1]) for r in range(rounds))
-    return DecodeResult(tokens, lengths, rounds, verify_ms, ev[-2].elapsed_time(ev[-1]), accepted, logprob, records)
+    return DecodeResult(tokens, lengths, rounds, verify_ms, ev[-2].elapsed_time(ev[-1]), accepted, logprob, records, table)
+
+
+@dataclass
+class BeamResult:
+    tokens: torch.Tensor        # int32 [B, W, 2 + steps], the first two are the prompt; best beam first
+    score: torch.Tensor         # fp32 [B, W]: log probability of what was emitted, under the verifier
+    steps: int
+    total_ms: float             # CUDA-event time of the whole loop
+
+
+def beam_decode(ctx: binding.HolaVerify, models: SyntheticPair, prompt: torch.Tensor, W: int, steps: int, end_token: int = -1) -> BeamResult:
+    """Beam search with W beams per sequence on the verifier.  ctx: for at least W - 1 draft positions, whose rows the beams take.
+    prompt: int64 [B, 2].  end_token: beams that emit it have ended and keep their score (their places are filled with it)."""
+    dev, B = prompt.device, prompt.shape[0]
+    history = torch.zeros((B, W, 2 + steps), dtype=torch.int32, device=dev)
+    history[:, :, :2] = prompt[:, None]
+    tok = prompt[:, 1:].expand(B, W).to(torch.int32)
+    # what the trunk keeps between steps: the token before the last, embedded
+    trunk = binding.hola_embed(prompt[:, :1].expand(B, W).contiguous(), models.E2, scale=0.35)
+    states = binding.BeamStates([history, trunk], positions=[2, None])
+    score = torch.full((B, W), -math.inf, device=dev)
+    score[:, 0] = 0.0                                            # (the beams are alike: one of them is alive)
+    finished = torch.zeros((B, W), dtype=torch.bool, device=dev) if end_token >= 0 else None
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    ev[0].record()
+    for t in range(2, 2 + steps):
+        hidden = models.target_hidden_from(tok, trunk).contiguous()                    # [B, W, H]
+        out = ctx.hola_lm_head_entropy(hidden, models.W_lm)
+        sel = binding.hola_beam_select(out.logits, out.logZ, score, finished=finished, end_token=end_token, keep_slots=True)
+        trunk.copy_(binding.hola_embed(tok.contiguous(), models.E2, scale=0.35))       # (the parents' last tokens, then by parent)
+        binding.hola_beam_reorder(states, sel.parent, used=torch.full((B,), t, dtype=torch.int32, device=dev))
+        history[:, :, t] = sel.token
+        tok, score, finished = sel.token.clamp_min(0), sel.score, sel.finished
+    order = torch.argsort(score, dim=1, descending=True, stable=True)
+    ev[1].record()
+    torch.cuda.synchronize()
+    return BeamResult(history.gather(1, order[:, :, None].expand_as(history)), score.gather(1, order), steps, ev[0].elapsed_time(ev[1]))
 
 
 def main():
@@ -170,14 +240,25 @@ def main():
     ap.add_argument("--score", action="store_true", help="report the emitted tokens' mean log probability under the verifier")
     ap.add_argument("--adapters", type=int, default=0, help="seeded low-rank adapters beside the LM head, dealt out to the sequences")
     ap.add_argument("--rank", type=int, default=4, help="rank of the adapters")
+    ap.add_argument("--distill", type=float, default=0.0, help="step size by which the draft's embedding table follows the verifier, round by round")
+    ap.add_argument("--beams", type=int, default=0, help="beam search with this many beams per sequence instead, --rounds steps of it")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         raise SystemExit("driver: no CUDA device; the verify path has no CPU fallback")
     dev = torch.device("cuda", torch.cuda.current_device())
     models = SyntheticPair(args.V, args.H, args.seed, dev)
     prompt = torch.randint(0, args.V, (args.B, 2), device=dev, generator=torch.Generator(device=dev).manual_seed(args.seed + 1))
+    if args.beams:
+        with binding.HolaVerify(args.B, args.beams - 1, args.H, args.V) as ctx:
+            beam_decode(ctx, models, prompt, args.beams, 3)                                      # warm-up
+            res = beam_decode(ctx, models, prompt, args.beams, args.rounds)
+        print(json.dumps({
+            "workload": f"beam search: B={args.B} beams={args.beams} H={args.H} V={args.V}, synthetic verifier", "steps": res.steps,
+            "mean_logprob_best": float(res.score[:, 0].mean()) / res.steps, "mean_logprob_last": float(res.score[:, -1].mean()) / res.steps,
+            "loop_ms_per_step": res.total_ms / res.steps, "tokens_per_s": args.B * res.steps / (res.total_ms * 1e-3), "data": "synthetic"}))
+        return
     gs, fb = int(args.gate == "draft"), int(args.fallback == "greedy")
-    more = {"score": args.score}
+    more = {"score": args.score, "distill": args.distill}
     if args.adapters > 0:
         more["adapters"] = seeded_adapters(models, args.adapters, args.rank, args.seed + 2)
         more["adapter_ids"] = torch.arange(args.B, device=dev, dtype=torch.int32) % args.adapters
@@ -186,6 +267,8 @@ def main():
         res = hsd_decode(ctx, models, prompt, args.k, args.tau, args.rounds, args.seed, gs, fb, **more)
     emitted = int((res.lengths - 2).sum().item())
     extra = {"mean_logprob": float(res.logprob.sum().item()) / emitted} if args.score else {}
+    if args.distill:
+        extra["distill"] = args.distill
     if args.adapters > 0:
         extra.update(adapters=args.adapters, rank=args.rank)
     print(json.dumps({

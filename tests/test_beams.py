@@ -581,3 +581,40 @@ def test_calls_through_the_native_helper_and_without_it(monkeypatch):
     monkeypatch.setattr(binding, "_host", None)
     for a, b in zip(with_it, run(), strict=True):
         assert a == b if isinstance(a, str) else all((x is None and y is None) or torch.equal(x, y) for x, y in zip(a, b, strict=True))
+
+
+@gpu
+def test_the_drivers_beam_search():
+    """Scores are the log probabilities of the emitted tokens; one beam is the greedy decoder; more beams never score less than the
+    prefix of fewer would allow at the last step, and ended beams keep what they have."""
+    from paper_2506_18952_b200 import driver
+    B, H, V, steps, W = 4, 256, 2000, 7, 5
+    models = driver.SyntheticPair(V, H, 5, torch.device("cuda", torch.cuda.current_device()))
+    prompt = torch.randint(0, V, (B, 2), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+
+    def logprobs(tokens):                                     # of every position behind the prompt, in 64 bits from the head's bf16 rows
+        c1, c2 = tokens[..., 1:-1].long(), tokens[..., :-2].long()
+        h = models._norm(models.E1[c1] + 0.35 * models.E2[c2], c1).bfloat16().double()
+        lp = torch.log_softmax(h @ models.W_lm.double().T, dim=-1)
+        return lp.gather(-1, tokens[..., 2:].long()[..., None])[..., 0], lp
+
+    with binding.HolaVerify(B, W - 1, H, V) as ctx:
+        res = driver.beam_decode(ctx, models, prompt, W, steps)
+        lp, _ = logprobs(res.tokens)
+        # logits to 1e-5 of their size (tens), sums of `steps` of them in fp32
+        assert (res.score.double() - lp.sum(-1)).abs().max() <= steps * 1e-3
+        assert (res.score[:, :-1] >= res.score[:, 1:]).all()
+        assert len({tuple(t.tolist()) for t in res.tokens.reshape(-1, 2 + steps)}) == B * W
+        one = driver.beam_decode(ctx, models, prompt, 1, steps)
+        lp, every = logprobs(one.tokens)
+        assert (every.amax(-1)[:, 0] - lp[:, 0]).max() <= 1e-3
+        end = int(res.tokens[0, 0, 4])                        # a token that comes up
+        ended = driver.beam_decode(ctx, models, prompt, W, steps, end_token=end)
+        lp, _ = logprobs(ended.tokens)
+        for b in range(B):
+            for w in range(W):
+                where = (ended.tokens[b, w, 2:] == end).nonzero()
+                n = int(where[0]) + 1 if len(where) else steps
+                assert abs(float(ended.score[b, w]) - float(lp[b, w, :n].sum())) <= steps * 1e-3
+                assert (ended.tokens[b, w, 2 + n:] == end).all()
+        assert (ended.tokens[0, :, 2:] == end).any()

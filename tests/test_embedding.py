@@ -477,3 +477,50 @@ def test_outputs_on_another_stream_are_not_written_over():
         torch.cuda.synchronize()
         assert all((t == 7).all() for t in fresh)
         del kept, other, fresh
+
+
+@gpu
+def test_distillation_of_the_drivers_draft():
+    """The gradient of KL(verifier || draft) by the draft's table against differences in 64 bits; the decode loop runs with it."""
+    from paper_2506_18952_b200 import driver
+    B, k, H, V, rounds = 4, 3, 64, 400, 3
+    dev = torch.device("cuda", torch.cuda.current_device())
+    models = driver.SyntheticPair(V, H, 7, dev, sharpness=0.5)
+    t = torch.tensor([3, 9, 3, 399, 0, 9, 3, 12], device="cuda")
+    p = torch.softmax(rnd((8, V), torch.float32, 1), dim=-1)
+    got = models.draft_grad(t, models.E1, p)
+    n = got.count.item()
+    assert got.ids[:n].tolist() == [0, 3, 9, 12, 399]
+
+    def loss(E):
+        e = E[t]
+        h = e / e.norm(dim=-1, keepdim=True) * models.gain[t].double()[:, None]
+        return float(-(p.double() * torch.log_softmax(h @ models.W_lm.double().T, dim=-1)).sum() / 8)
+
+    E, D, eps = models.E1.double(), rnd((V, H), torch.float64, 2), 1e-4
+    want = (loss(E + eps * D) - loss(E - eps * D)) / (2 * eps)
+    mine = float((got.rows[:n].double() * D[got.ids[:n].long()]).sum())
+    # the draft's rows h are rounded to bf16 (2^-8 of each), which moves q by up to 2^-8 |h W| of itself, logits of about 0.5 here: some
+    # 2^-9 of the gradient's terms, whose sizes are those of |dE D|
+    size = float((got.rows[:n].double().abs() * D[got.ids[:n].long()].abs()).sum())
+    assert abs(mine - want) <= 2.0 ** -8 * size and abs(want) > 2.0 ** -6 * size
+    prompt = torch.randint(0, V, (B, 2), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    with binding.HolaVerify(B, k, H, V) as ctx:
+        bare = driver.hsd_decode(ctx, models, prompt, k, 1.5, rounds, 3, keep_records=True)
+        res = driver.hsd_decode(ctx, models, prompt, k, 1.5, rounds, 3, keep_records=True, distill=0.5)
+    # (a round's q depends on the table through the rows of its own tokens alone, so what has moved shows in the table)
+    assert torch.equal(res.records[0].draft_q, bare.records[0].draft_q) and bare.draft_table is None
+    last = [prompt[:, 1], *(r.out.next_tok.long() for r in res.records)]
+    used = {v for i, r in enumerate(res.records) for v in (*last[i].tolist(), *r.draft_tok[:, :k - 1].flatten().tolist())}
+    assert set((res.draft_table != models.E1).any(dim=1).nonzero()[:, 0].tolist()) == used
+    assert all(torch.isfinite(r.draft_q.float()).all() for r in res.records)
+
+
+@gpu
+def test_the_drivers_lookups_are_those_of_the_tables():
+    from paper_2506_18952_b200 import driver
+    models = driver.SyntheticPair(500, 96, 3, torch.device("cuda", torch.cuda.current_device()))
+    a, b = some_tokens(60, 500, 1, torch.int64, 0.0).view(20, 3), some_tokens(60, 500, 2, torch.int64, 0.0).view(20, 3)
+    assert torch.equal(models.target_hidden(a, b), models._norm(models.E1[a] + 0.35 * models.E2[b], a).to(torch.bfloat16))
+    h = models._norm(models.E1[a], a).to(torch.bfloat16).float()
+    assert torch.equal(models.draft_probs(a), torch.softmax(h @ models.W_lm.float().T, dim=-1))

@@ -8,14 +8,15 @@
 // eight threads put the best of theirs on a board of 32 (every four on one of 64, for more than twenty candidates); let the n-th best
 // there be w.  At least n candidates have a >= w, so each of the part's n best has a >= w - 2^-22 (|w| + max |b|): twice the bound
 // above for either side, and the roundings of this line.  Only threads whose own largest is that large hold such entries; their groups are read again, out of the L2,
-// and what qualifies goes, with its key in 64 bits, to the sequence's first CTA, which places each by counting those before it.
+// and what qualifies is placed, by keys in 64 bits, by counting those before it.  The n best go to the sequence's first CTA in their
+// order, which merges the parts' lists.
 
 constexpr int kBsThreads = 256;
 constexpr int kBsWarps = kBsThreads / 32;
 constexpr int kBsMaxBeams = 32, kBsMaxKept = 32;
 constexpr int kBsMaxCluster = 16;
-constexpr int kBsSpots = 128;          // candidates that a part may send unsorted; beyond that it sends its 32 best
-constexpr int kBsAhead = 4;            // groups of a thread that are on the way
+constexpr int kBsSpots = 64;           // candidates that a part may send unsorted; beyond that it sends its 32 best
+constexpr int kBsAhead = 6;            // groups of a thread that are on the way
 constexpr int kBsMaxV = 1 << 27;       // ids share a word with a beam and a logit
 
 struct BsParams {
@@ -58,6 +59,13 @@ __device__ __forceinline__ BsCand bs_exchange(const BsCand& a, int stride, bool 
   const BsCand b = {__shfl_xor_sync(0xffffffffu, a.hi, stride), __shfl_xor_sync(0xffffffffu, a.lo, stride)};
   return bs_before(a, b) == first ? a : b;
 }
+// The 32 first of two sorted lists, sorted; `reversed`: the second one from its end.
+__device__ __forceinline__ BsCand bs_merge(BsCand a, const BsCand& reversed, int lane) {
+  if (bs_before(reversed, a)) a = reversed;
+#pragma unroll
+  for (int stride = 16; stride > 0; stride >>= 1) a = bs_exchange(a, stride, (lane & stride) == 0);
+  return a;
+}
 __device__ __noinline__ BsCand bs_take_in(BsCand best, const BsCand* waiting, int n) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
@@ -68,9 +76,7 @@ __device__ __noinline__ BsCand bs_take_in(BsCand best, const BsCand* waiting, in
 #pragma unroll 1
     for (int stride = size >> 1; stride > 0; stride >>= 1) a = bs_exchange(a, stride, ((lane & size) == 0) == ((lane & stride) == 0));
   const BsCand r = {__shfl_sync(0xffffffffu, a.hi, 31 - lane), __shfl_sync(0xffffffffu, a.lo, 31 - lane)};
-  if (bs_before(r, best)) best = r;
-#pragma unroll 1
-  for (int stride = 16; stride > 0; stride >>= 1) best = bs_exchange(best, stride, (lane & stride) == 0);
+  best = bs_merge(best, r, lane);
   __syncwarp();
   return best;
 }
@@ -86,19 +92,19 @@ struct BsRow {
   int edge[2];
 };
 
-template <typename T>
 struct BsShared {
   BsRow rows[kBsMaxBeams];
-  BsCand own[kBsWarps * 32];           // what this part sends (kBsSpots), or the warps' sorted lists
-  BsCand all[kBsMaxCluster * kBsSpots + kBsMaxBeams];      // first CTA: what the parts have sent, and the ended beams
-  int before_it[kBsMaxCluster * kBsSpots + kBsMaxBeams];
-  BsCand waiting[kBsWarps][32];
-  BsCand kept[kBsMaxKept];
+  uint2 spots[kBsSpots];               // entries of this part: logit; row (5 bits) and id (27)
+  BsCand own[kBsWarps * 32];           // this part's candidates (the ended beams among the first part's), or the warps' sorted lists
+  int before_it[kBsSpots + kBsMaxBeams];
+  BsCand sent[kBsMaxCluster][32];      // first CTA: every part's best, sorted
+  int sent_by[kBsMaxCluster];          // their number
+  BsCand waiting[kBsWarps][32];        // also: lists on their way through the merge
   uint64_t board[64];
   uint8_t looked_at[kBsWarps][32];
   unsigned bad_from[kBsMaxCluster];    // rows that hold NaN or +inf, as every CTA of the cluster has found them
   unsigned bad_here;
-  int rounds, n_own, n_all;
+  int rounds, n_own;
   float b_max;
 };
 
@@ -108,9 +114,10 @@ __device__ __forceinline__ float bs_approx(float l, float w32, float b) {
   return fabsf(a) == CUDART_INF_F && fabsf(l) != CUDART_INF_F ? copysignf(3.402823466e38f, a) : a;
 }
 
-// Entries of group j of a row whose a is at least thr, as candidates.
+// Entries of group j of a row whose a is at least thr, to the part's spots.
 template <typename T>
-__device__ __forceinline__ void bs_send(BsShared<T>& s, const BsRow& row, int V, int j, float thr) {
+__device__ __forceinline__ void bs_note(BsShared& s, int li, int V, int j, float thr) {
+  const BsRow& row = s.rows[li];
   const LpRow<T> r(static_cast<const T*>(row.row), V);
   const LpGroup<T> g = r.get(j);
   unsigned which = 0;
@@ -121,28 +128,27 @@ __device__ __forceinline__ void bs_send(BsShared<T>& s, const BsRow& row, int V,
   }
   if (!which) return;
   int spot = atomicAdd(&s.n_own, __popc(which));
-  const int v0 = r.first(j);
+  const uint32_t at = static_cast<uint32_t>(li) << 27 | static_cast<uint32_t>(r.first(j) & (kBsMaxV - 1));
 #pragma unroll
   for (int e = 0; e < LpGroup<T>::kEntries; ++e)
     if (which >> e & 1u) {
-      if (spot < kBsSpots) {
-        const float l = g.entry(e);
-        s.own[spot] = {bs_order((row.off + static_cast<double>(l)) * row.weight), bs_low(row.beam, l, v0 + e)};
-      }
+      // (a row's first group may begin before entry 0: added up within 27 bits)
+      if (spot < kBsSpots)
+        s.spots[spot] = make_uint2(__float_as_uint(g.entry(e)), static_cast<uint32_t>(li) << 27 | ((at + static_cast<uint32_t>(e)) & (kBsMaxV - 1)));
       ++spot;
     }
 }
 
 // What bounds it: HBM for large batches; for a few rows the chain beams -> pass -> board -> second look -> cluster -> counting.
 template <typename T>
-__global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsParams p, int C) {
+__global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsParams p, int C) {
   extern __shared__ __align__(16) unsigned char bs_smem[];
-  BsShared<T>& s = *reinterpret_cast<BsShared<T>*>(bs_smem);
+  BsShared& s = *reinterpret_cast<BsShared*>(bs_smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int seq = blockIdx.x / C, part = blockIdx.x - seq * C;
-  if (tid == 0) { s.n_own = 0; s.n_all = 0; s.bad_here = 0; }
+  if (tid == 0) { s.n_own = 0; s.bad_here = 0; }
   if (tid < kBsMaxCluster) s.bad_from[tid] = 0;
-  // (the other CTAs of the cluster have started, and their counters stand at zero: looked at before anything is sent)
+  // (the other CTAs of the cluster have started, and their words stand at zero: looked at before anything is sent)
   if (C > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   grid_dependency_wait();
   grid_dependency_release();
@@ -273,15 +279,14 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
       }
       const bool mine = m > -CUDART_INF_F && m >= thr, again = mine && second >= thr && second > -CUDART_INF_F;
       if (mine && !again) {
-        if (at == rounds) {
-          bs_send(s, s.rows[tid >> 1], p.V, my_edge, thr);
-        } else {
-          int li = 0;
-          for (; at >= s.rows[li].rounds; ++li) at -= s.rows[li].rounds;
-          bs_send(s, s.rows[li], p.V, s.rows[li].begin + at * kBsThreads + tid, thr);
+        int li = tid >> 1, j = my_edge;
+        if (at < rounds) {
+          for (li = 0; at >= s.rows[li].rounds; ++li) at -= s.rows[li].rounds;
+          j = s.rows[li].begin + at * kBsThreads + tid;
         }
+        bs_note<T>(s, li, p.V, j, thr);
       }
-      if (again && my_edge >= 0) bs_send(s, s.rows[tid >> 1], p.V, my_edge, thr);
+      if (again && my_edge >= 0) bs_note<T>(s, tid >> 1, p.V, my_edge, thr);
       // threads with more than one such group: all of theirs, dealt out to the warp's lanes
       const unsigned look = __ballot_sync(0xffffffffu, again);
       if (look) {
@@ -292,12 +297,20 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
           int t = i / who, li = 0;
           for (; t >= s.rows[li].rounds; ++li) t -= s.rows[li].rounds;
           const int j = t * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
-          if (j < s.rows[li].count) bs_send(s, s.rows[li], p.V, s.rows[li].begin + j, thr);
+          if (j < s.rows[li].count) bs_note<T>(s, li, p.V, s.rows[li].begin + j, thr);
         }
       }
     }
     __syncthreads();
-    if (s.n_own > kBsSpots) {
+    int mine = s.n_own;
+    if (mine <= kBsSpots) {
+      if (tid < mine) {
+        const uint2 e = s.spots[tid];
+        const BsRow& row = s.rows[e.y >> 27];
+        const float l = __uint_as_float(e.x);
+        s.own[tid] = {bs_order((row.off + static_cast<double>(l)) * row.weight), bs_low(row.beam, l, static_cast<int>(e.y & (kBsMaxV - 1)))};
+      }
+    } else {
       // More than there is room for (equal or masked entries, or the best crowd together): the part's 32 best by sorted lists, from
       // every entry's key in 64 bits.
       __syncthreads();                                   // (everyone has seen n_own)
@@ -346,25 +359,38 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
       for (int i = 0; i < kBsWarps * 32; ++i) before += bs_before(s.own[i], best) ? 1 : 0;
       __syncthreads();
       if (best.hi != 0 && before < 32) s.own[before] = best;       // (candidates differ, so their places do)
-      const int some = __syncthreads_count(best.hi != 0 && before < 32);
-      if (tid == 0) s.n_own = some;
-      __syncthreads();
+      mine = __syncthreads_count(best.hi != 0 && before < 32);
     }
 
-    // To the sequence's first CTA: the candidates; to every CTA: the rows found bad.
-    if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
-    const int mine = s.n_own;
-    if (warp == 0) {
-      int* n_all = C > 1 ? cg::this_cluster().map_shared_rank(&s.n_all, 0) : &s.n_all;
-      int first = 0;
-      if (lane == 0 && mine > 0) first = atomicAdd(n_all, mine);
-      first = __shfl_sync(0xffffffffu, first, 0);
-      BsCand* all = C > 1 ? cg::this_cluster().map_shared_rank(s.all, 0) : s.all;
-      for (int i = lane; i < mine; i += 32) all[first + i] = s.own[i];
-    } else if (warp == 1 && lane < C) {
-      unsigned* to = C > 1 ? cg::this_cluster().map_shared_rank(&s.bad_from[part], lane) : &s.bad_from[part];
-      *to = s.bad_here;
+    // Ended beams have one candidate each: the first part's.
+    if (part == 0) {
+      if (warp == kBsWarps - 1 && (ended_mask >> lane & 1u))
+        s.own[mine + __popc(ended_mask & ((1u << lane) - 1u))] = {bs_order(static_cast<double>(score) * weight), bs_low(lane, 0.f, p.end_token)};
+      mine += __popc(ended_mask);
     }
+    if (tid < mine) s.before_it[tid] = 0;
+    __syncthreads();
+    // Every candidate's place is the number of those before it: half of the threads look at half of them each.
+    constexpr int kHalf = kBsThreads / 2;
+    static_assert(kBsSpots + kBsMaxBeams <= kHalf, "a thread for each candidate");
+    BsCand c = {0, 0};
+    if ((tid & (kHalf - 1)) < mine) {
+      c = s.own[tid & (kHalf - 1)];
+      const int half = (mine + 1) / 2, from = tid < kHalf ? 0 : half, to = tid < kHalf ? half : mine;
+      int before = 0;
+#pragma unroll 8
+      for (int k = from; k < to; ++k) before += bs_before(s.own[k], c) ? 1 : 0;
+      atomicAdd(&s.before_it[tid & (kHalf - 1)], before);
+    }
+    __syncthreads();
+    // To the sequence's first CTA: the best; to every CTA: the rows found bad.
+    if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+    if (tid < mine) {
+      const int place = s.before_it[tid];
+      if (place < p.n) (C > 1 ? cg::this_cluster().map_shared_rank(&s.sent[part][0], 0) : &s.sent[part][0])[place] = c;
+    }
+    if (tid == kBsThreads - 1) *(C > 1 ? cg::this_cluster().map_shared_rank(&s.sent_by[part], 0) : &s.sent_by[part]) = min(mine, p.n);
+    if (warp == 3 && lane < C) *(C > 1 ? cg::this_cluster().map_shared_rank(&s.bad_from[part], lane) : &s.bad_from[part]) = s.bad_here;
     if (C > 1) cluster_sync_all();
     else __syncthreads();
     const unsigned found = __reduce_or_sync(0xffffffffu, lane < C ? s.bad_from[lane] : 0u) & ~excluded;
@@ -373,7 +399,7 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
     excluded |= found;
     flags |= HOLA_FLAG_BAD_LOGIT;
     __syncthreads();
-    if (tid == 0) { s.n_own = 0; s.n_all = 0; }
+    if (tid == 0) s.n_own = 0;
     if (C > 1) {
       cluster_sync_all();
       asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
@@ -383,37 +409,22 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
   }
   if (part != 0) return;
 
-  // Ended beams have one candidate each.
-  const int sent = s.n_all;
-  const int total = sent + __popc(ended_mask);
-  if (warp == 0 && (ended_mask >> lane & 1u))
-    s.all[sent + __popc(ended_mask & ((1u << lane) - 1u))] = {bs_order(static_cast<double>(score) * weight), bs_low(lane, 0.f, p.end_token)};
-  if (tid < kBsMaxKept) s.kept[tid] = {0, 0};
-  for (int i = tid; i < total; i += kBsThreads) s.before_it[i] = 0;
-  __syncthreads();
-  // Every candidate's place is the number of those before it: a warp compares all of them with an eighth of them.
-  const int slice = (total + kBsWarps - 1) / kBsWarps, from = warp * slice, to = min(total, from + slice);
-  if (from < to) {
-#pragma unroll 1
-    for (int i = lane; i < total; i += 32) {
-      const BsCand c = s.all[i];
-      int before = 0;
-#pragma unroll 8
-      for (int k = from; k < to; ++k) before += bs_before(s.all[k], c) ? 1 : 0;
-      atomicAdd(&s.before_it[i], before);
-    }
+  // The parts' lists, merged: warp w takes those of parts w and w + 8, then the other warps'.  Lane i: the i-th kept.
+  BsCand c = {0, 0};
+  if (warp < C && lane < s.sent_by[warp]) c = s.sent[warp][lane];
+  if (warp + kBsWarps < C) {
+    BsCand r = {0, 0};
+    if (31 - lane < s.sent_by[warp + kBsWarps]) r = s.sent[warp + kBsWarps][31 - lane];
+    c = bs_merge(c, r, lane);
   }
-  __syncthreads();
 #pragma unroll 1
-  for (int i = tid; i < total; i += kBsThreads) {
-    const int place = s.before_it[i];
-    if (place < p.n) s.kept[place] = s.all[i];
+  for (int step = 1; step < min(C, kBsWarps); step <<= 1) {
+    if ((warp & (2 * step - 1)) == step) s.waiting[warp][lane] = c;
+    __syncthreads();
+    if ((warp & (2 * step - 1)) == 0 && warp + step < C) c = bs_merge(c, s.waiting[warp + step][31 - lane], lane);
   }
-  __syncthreads();
   if (warp != 0) return;
 
-  // Lane i: the i-th kept.
-  const BsCand c = s.kept[lane];
   const bool have = lane < p.n && c.hi != 0;
   const int beam = have ? bs_beam(c.lo) : 0;
   const float from_score = __shfl_sync(0xffffffffu, score, beam), from_logZ = __shfl_sync(0xffffffffu, logZ, beam);
@@ -446,20 +457,23 @@ __global__ void __launch_bounds__(kBsThreads, 3) beam_select_kernel(const BsPara
   if (p.status && lane == 0 && flags) atomicOr(p.status, flags);
 }
 
-// CTAs per sequence: up to three on an SM, as long as a thread keeps two groups or so of the sequence's rows.
-int bs_cluster(int num_sms, int B, int W, int V, int elem) {
+// CTAs per sequence: as many as leave all clusters of the call room on the chip at once (`fit`: clusters of so many CTAs that it holds; up to
+// fifteen sixteenths of them, for the last ones share SMs), and a thread three groups or more.  us with 1 / 2 / 4 / 8 / 16: 1 x 4 x 32000
+// fp32 12.5 / 9.4 / 7.8 / 7.1 / 6.8; 23 x 3 x 50003 fp16 14.0 / 10.9 / 10.4 / 10.2 / 16.8 (two waves); 64 x 6 x 32000 fp32 27.7 / 19.1 /
+// 15.7 / 26.3 / 41.2; 32 x 5 x 128256 bf16 41.3 / 25.3 / 18.4 / 18.1 (with 7: 16.1); 4 x 2 x 5000 fp32 5.0 / 5.3 / 5.4 / 6.1 / 11.2.
+int bs_cluster(int B, int W, int V, int elem, const int* fit) {
   const long long groups = static_cast<long long>(W) * V / (kLpGroupBytes / elem);
-  int C = 1;
-  while (C < kBsMaxCluster && 2ll * B * C <= 3ll * num_sms && groups / (2 * C) >= kBsThreads) C <<= 1;
-  return C;
+  for (int C = kBsMaxCluster; C > 1; C = C > 8 ? 8 : C - 1)
+    if (16ll * B <= 15ll * fit[C] && groups / C >= 3 * kBsThreads) return C;
+  return 1;
 }
 
 template <typename T>
-cudaError_t launch_beam_select(const BsParams& p, int num_sms, cudaStream_t stream) {
-  const int C = bs_cluster(num_sms, p.B, p.W, p.V, static_cast<int>(sizeof(T)));
+cudaError_t launch_beam_select(const BsParams& p, const int* fit, cudaStream_t stream) {
+  const int C = bs_cluster(p.B, p.W, p.V, static_cast<int>(sizeof(T)), fit);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.B) * C); cfg.blockDim = dim3(kBsThreads); cfg.stream = stream;
-  cfg.dynamicSmemBytes = sizeof(BsShared<T>);
+  cfg.dynamicSmemBytes = sizeof(BsShared);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -471,13 +485,26 @@ cudaError_t launch_beam_select(const BsParams& p, int num_sms, cudaStream_t stre
 
 template <typename T>
 cudaError_t configure_select() {
-  const cudaError_t e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(BsShared<T>)));
+  const cudaError_t e = cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(BsShared)));
   return e != cudaSuccess ? e : cudaFuncSetAttribute(beam_select_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
-cudaError_t configure_beams() {
+// Also: how many clusters of 1 .. kBsMaxCluster CTAs the device holds at once (the types' kernels are alike in what they need).
+cudaError_t configure_beams(int* fit) {
   cudaError_t e = configure_select<float>();
   if (e == cudaSuccess) e = configure_select<__nv_bfloat16>();
-  return e == cudaSuccess ? configure_select<__half>() : e;
+  if (e == cudaSuccess) e = configure_select<__half>();
+  for (int C = 1; e == cudaSuccess && C <= kBsMaxCluster; ++C) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(C)); cfg.blockDim = dim3(kBsThreads); cfg.dynamicSmemBytes = sizeof(BsShared);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(C); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    fit[C] = 0;
+    // (a size that the device does not hold at all is none that is taken)
+    if (cudaOccupancyMaxActiveClusters(&fit[C], beam_select_kernel<float>, &cfg) != cudaSuccess) { fit[C] = 0; cudaGetLastError(); }
+  }
+  return e;
 }
 
 // ------------------------------------------------------------------------------------------------ reordering

@@ -16,6 +16,7 @@
 #include <cooperative_groups.h>
 
 #include <atomic>
+#include <mutex>
 #include <type_traits>
 
 #include "../../include/hola_verify.h"
@@ -33,20 +34,31 @@ namespace {
 
 extern "C" {
 
-// The current device's SM count; 0: no device that runs these kernels.  What a device is does not change: asked for once (the first call
-// on a device also tells the runtime how much shared memory the kernels use, which the calls behind it need not say again).
-static int current_sms() {
+// What the launches need to know of a device, asked for once (the first call on a device also tells the runtime how much shared memory
+// the kernels use, which the calls behind it need not say again).
+struct DeviceFacts {
+  int sms;
+  int fit[kBsMaxCluster + 1];          // see bs_cluster
+};
+// The current device's; null: no device that runs these kernels.
+static const DeviceFacts* device_facts() {
   constexpr int kDevices = 64;
-  static std::atomic<int> known[kDevices];
-  int dev = 0, sms = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  if (dev < kDevices && (sms = known[dev].load(std::memory_order_acquire)) != 0) return sms;
+  static DeviceFacts facts[kDevices];
+  static std::atomic<bool> known[kDevices];
+  static std::mutex first;
+  int dev = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return nullptr;
+  if (known[dev].load(std::memory_order_acquire)) return &facts[dev];
+  std::lock_guard<std::mutex> lock(first);
+  if (known[dev].load(std::memory_order_acquire)) return &facts[dev];
+  DeviceFacts f = {};
   if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10)
-    return 0;
-  if (configure_beams() != cudaSuccess || configure_embedding() != cudaSuccess) return 0;
-  if (dev < kDevices) known[dev].store(sms, std::memory_order_release);
-  return sms;
+      cudaDeviceGetAttribute(&f.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || major != 10 || f.sms <= 0)
+    return nullptr;
+  if (configure_beams(f.fit) != cudaSuccess || configure_embedding() != cudaSuccess) return nullptr;
+  facts[dev] = f;
+  known[dev].store(true, std::memory_order_release);
+  return &facts[dev];
 }
 
 hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
@@ -58,16 +70,16 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   if (a->B == 0) return HOLA_OK;
   if (!a->logits || !a->logZ || !a->score || !a->score_out || !a->parent || !a->token) return HOLA_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(a->logits) % (a->l_dtype == HOLA_L_F32 ? 4 : 2)) return HOLA_ERR_INVALID_ARG;
-  const int sms = current_sms();
-  if (!sms) return HOLA_ERR_NO_DEVICE;
+  const DeviceFacts* dev = device_facts();
+  if (!dev) return HOLA_ERR_NO_DEVICE;
   BsParams p = {};
   p.logits = a->logits; p.seq_stride = a->seq_stride; p.beam_stride = a->beam_stride; p.B = a->B; p.W = a->W; p.V = a->V; p.n = a->n;
   p.logZ = a->logZ; p.score = a->score; p.finished = a->finished; p.weight = a->weight; p.end_token = a->end_token;
   p.keep_slots = a->keep_slots; p.score_out = a->score_out; p.parent = a->parent; p.token = a->token; p.finished_out = a->finished_out;
   p.status = a->status_word;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = a->l_dtype == HOLA_L_F32 ? launch_beam_select<float>(p, sms, stream)
-                        : a->l_dtype == HOLA_L_BF16 ? launch_beam_select<__nv_bfloat16>(p, sms, stream) : launch_beam_select<__half>(p, sms, stream);
+  const cudaError_t e = a->l_dtype == HOLA_L_F32 ? launch_beam_select<float>(p, dev->fit, stream)
+                        : a->l_dtype == HOLA_L_BF16 ? launch_beam_select<__nv_bfloat16>(p, dev->fit, stream) : launch_beam_select<__half>(p, dev->fit, stream);
   return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }
 
@@ -98,7 +110,7 @@ hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
     if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
   }
   if (in_place < 0) return HOLA_OK;
-  if (!current_sms()) return HOLA_ERR_NO_DEVICE;
+  if (!device_facts()) return HOLA_ERR_NO_DEVICE;
   BrParams p = {};
   p.B = a->B; p.W = a->W; p.n = a->n; p.parent = a->parent; p.parent_stride = a->parent_stride; p.used = a->used; p.status = a->status_word;
   p.in_place = in_place;
@@ -158,8 +170,8 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
       reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
     return HOLA_ERR_INVALID_ARG;
-  const int sms = current_sms();
-  if (!sms) return HOLA_ERR_NO_DEVICE;
+  const DeviceFacts* dev = device_facts();
+  if (!dev) return HOLA_ERR_NO_DEVICE;
   EmParams p = {};
   p.tokens = a->tokens; p.wide = a->wide_tokens; p.N = a->N; p.V = a->V; p.H = a->H; p.v_offset = a->v_offset;
   p.V_global = a->V_global ? a->V_global : a->V;
@@ -171,8 +183,8 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (mixed) words = words && in_words(p.mix.W16, 0, 1, 16) && in_words(p.mix.W8, 0, 1, 8) && in_words(p.mix.W4, 0, 1, 4);
   else words = words && in_words(a->table, a->row_stride, te, 8 * te);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, sms, stream)
-                              : launch_embed_of<1>(p, a->t_dtype, a->out_dtype, sms, stream);
+  const cudaError_t e = words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, dev->sms, stream)
+                              : launch_embed_of<1>(p, a->t_dtype, a->out_dtype, dev->sms, stream);
   return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }
 
@@ -202,7 +214,7 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
     return HOLA_ERR_INVALID_ARG;
   const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + kEgMaxWindow - 1) / kEgMaxWindow) * p.slices;
   if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
-  if (!current_sms()) return HOLA_ERR_NO_DEVICE;
+  if (!device_facts()) return HOLA_ERR_NO_DEVICE;
   p.tokens = a->tokens; p.wide = a->wide_tokens; p.v_offset = a->v_offset;
   p.V_global = a->V_global ? a->V_global : a->V;
   p.grad = a->grad; p.g_stride = a->grad_stride; p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;

@@ -509,9 +509,10 @@ cudaError_t configure_beams(int* fit) {
 
 // ------------------------------------------------------------------------------------------------ reordering
 // new[b][i] = old[b][parent[b][i]], any number of states.  A CTA takes a piece of the bytes of all beams of one sequence (of one
-// layer, one head); a thread takes 16 bytes of every beam that changes into registers and then writes them, so that the same buffer
-// may be read and written in any order of the parents: no other thread touches these bytes.  In place, beams that stay (parent[i] = i)
-// are neither read, but for their children, nor written.  Bound by HBM, whose latency 16 words of 16 bytes a thread on the way hide.
+// layer, one head).  Where no place that changes has children of its own (copies into another buffer; a selection that keeps slots), every
+// parent's words are read once and written to all of its children.  Else, in place, a thread takes its words of every beam that changes into
+// registers and then writes them, so that any order of the parents will do: no other thread touches these bytes.  In place, beams that
+// stay (parent[i] = i) are neither read, but for their children, nor written.  Bound by HBM, whose latency eight words of 16 bytes a thread on the way hide.
 constexpr int kBrThreads = 128;
 constexpr int kBrStates = 24;          // states of one launch (launch parameters)
 
@@ -535,13 +536,42 @@ struct BrParams {
 };
 constexpr int kBrPiece = 8 * 16 * kBrThreads;      // bytes of a beam that a CTA takes at most
 
-// M: beams that change at most; U: words of each that a thread has on the way.
+// Every parent's words to its children: `sources` parents, children[k] as bits.
+template <typename V>
+__device__ __forceinline__ void br_spread(const BrState& st, const unsigned char* src, unsigned char* dst, long long begin, long long end,
+                                          const int* from, const unsigned* children, int sources) {
+  constexpr int U = 8;
+  constexpr int kStep = kBrThreads * sizeof(V);
+  // (a piece is 8 words of 16 bytes a thread; of narrower ones it takes several rounds)
+#pragma unroll 1
+  for (long long at = begin + static_cast<long long>(threadIdx.x) * sizeof(V); at < end; at += U * kStep) {
+    const int left = static_cast<int>(end - at);
+#pragma unroll 1
+    for (int k = 0; k < sources; ++k) {
+      V v[U];
+      const unsigned char* x = src + from[k] * st.beam + at;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (u * kStep < left) v[u] = *reinterpret_cast<const V*>(x + u * kStep);
+#pragma unroll 1
+      for (unsigned c = children[k]; c; c &= c - 1u) {
+        unsigned char* y = dst + (__ffs(c) - 1) * st.to_beam + at;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u * kStep < left) *reinterpret_cast<V*>(y + u * kStep) = v[u];
+      }
+    }
+  }
+}
+
+// In any order: M beams that change at most; U words of each that a thread has on the way.
 template <typename V, int M, int U>
 __device__ __forceinline__ void br_move(const BrState& st, const unsigned char* src, unsigned char* dst, long long begin, long long end,
                                         const int* to, const int* from, int moves) {
-  constexpr long long kStep = static_cast<long long>(kBrThreads) * sizeof(V);
+  constexpr int kStep = kBrThreads * sizeof(V);
 #pragma unroll 1
   for (long long at = begin + static_cast<long long>(threadIdx.x) * sizeof(V); at < end; at += U * kStep) {
+    const int left = static_cast<int>(end - at);
     V v[U][M];
 #pragma unroll
     for (int i = 0; i < M; ++i)
@@ -549,7 +579,7 @@ __device__ __forceinline__ void br_move(const BrState& st, const unsigned char* 
         const unsigned char* x = src + from[i] * st.beam + at;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (at + u * kStep < end) v[u][i] = *reinterpret_cast<const V*>(x + u * kStep);
+          if (u * kStep < left) v[u][i] = *reinterpret_cast<const V*>(x + u * kStep);
       }
 #pragma unroll
     for (int i = 0; i < M; ++i)
@@ -557,23 +587,23 @@ __device__ __forceinline__ void br_move(const BrState& st, const unsigned char* 
         unsigned char* x = dst + to[i] * st.to_beam + at;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (at + u * kStep < end) *reinterpret_cast<V*>(x + u * kStep) = v[u][i];
+          if (u * kStep < left) *reinterpret_cast<V*>(x + u * kStep) = v[u][i];
       }
   }
 }
 template <typename V>
 __device__ __forceinline__ void br_move_any(const BrState& st, const unsigned char* src, unsigned char* dst, long long begin, long long end,
                                             const int* to, const int* from, int moves) {
-  if (moves <= 2) br_move<V, 2, 8>(st, src, dst, begin, end, to, from, moves);
-  else if (moves <= 4) br_move<V, 4, 4>(st, src, dst, begin, end, to, from, moves);
+  if (moves <= 4) br_move<V, 4, 4>(st, src, dst, begin, end, to, from, moves);
   else if (moves <= 8) br_move<V, 8, 2>(st, src, dst, begin, end, to, from, moves);
   else if (moves <= 16) br_move<V, 16, 1>(st, src, dst, begin, end, to, from, moves);
-  else br_move<V, 32, 1>(st, src, dst, begin, end, to, from, moves);
+  else br_move<std::conditional_t<sizeof(V) == 16, uint2, V>, 32, 1>(st, src, dst, begin, end, to, from, moves);       // (64 registers)
 }
 
-__global__ void __launch_bounds__(kBrThreads) beam_reorder_kernel(const __grid_constant__ BrParams p) {
+__global__ void __launch_bounds__(kBrThreads, 5) beam_reorder_kernel(const __grid_constant__ BrParams p) {
   __shared__ int to[32], from[32];
-  __shared__ int n_moves;
+  __shared__ unsigned children[32];
+  __shared__ int n_moves, n_sources;                     // n_sources 0: in any order
   grid_dependency_wait();
   grid_dependency_release();
   int k = 0;
@@ -592,13 +622,21 @@ __global__ void __launch_bounds__(kBrThreads) beam_reorder_kernel(const __grid_c
       bad = from_beam < -1 || from_beam >= p.W;
     }
     const bool moves = !bad && from_beam >= 0 && !(p.in_place && from_beam == lane);
-    const unsigned mask = __ballot_sync(0xffffffffu, moves);
-    if (moves) {
-      const int at = __popc(mask & ((1u << lane) - 1u));
-      to[at] = lane;
+    const unsigned mask = __ballot_sync(0xffffffffu, moves), below = (1u << lane) - 1u;
+    const unsigned parents = __reduce_or_sync(0xffffffffu, moves ? 1u << from_beam : 0u);
+    const unsigned same = __match_any_sync(0xffffffffu, moves ? from_beam : -1);
+    const bool any_order = p.in_place && (mask & parents) != 0;
+    if (any_order) {
+      if (moves) {
+        to[__popc(mask & below)] = lane;
+        from[__popc(mask & below)] = from_beam;
+      }
+    } else if (moves && __ffs(same) - 1 == lane) {
+      const int at = __popc(parents & ((1u << from_beam) - 1u));
       from[at] = from_beam;
+      children[at] = same;
     }
-    if (lane == 0) n_moves = __popc(mask);
+    if (lane == 0) { n_moves = __popc(mask); n_sources = any_order ? 0 : __popc(parents); }
     if (__any_sync(0xffffffffu, bad) && lane == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_BEAM);
   }
   __syncthreads();
@@ -615,9 +653,15 @@ __global__ void __launch_bounds__(kBrThreads) beam_reorder_kernel(const __grid_c
   // what every address of the piece has in common
   const unsigned align = static_cast<unsigned>(reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) |
                                                static_cast<uintptr_t>(st.beam | st.to_beam | end));
-  if (align % 16 == 0) br_move_any<uint4>(st, src, dst, begin, end, to, from, moves);
-  else if (align % 4 == 0) br_move_any<uint32_t>(st, src, dst, begin, end, to, from, moves);
-  else br_move_any<unsigned char>(st, src, dst, begin, end, to, from, moves);
+  if (n_sources) {
+    if (align % 16 == 0) br_spread<uint4>(st, src, dst, begin, end, from, children, n_sources);
+    else if (align % 4 == 0) br_spread<uint32_t>(st, src, dst, begin, end, from, children, n_sources);
+    else br_spread<unsigned char>(st, src, dst, begin, end, from, children, n_sources);
+  } else {
+    if (align % 16 == 0) br_move_any<uint4>(st, src, dst, begin, end, to, from, moves);
+    else if (align % 4 == 0) br_move_any<uint32_t>(st, src, dst, begin, end, to, from, moves);
+    else br_move_any<unsigned char>(st, src, dst, begin, end, to, from, moves);
+  }
 }
 
 cudaError_t launch_beam_reorder(const BrParams& p, unsigned ctas, cudaStream_t stream) {

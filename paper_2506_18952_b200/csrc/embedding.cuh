@@ -3,7 +3,7 @@
 // ------------------------------------------------------------------------------------------------ lookup
 // out[r] = add[r] + scale * W[tok[r]], every operation one rounding in fp32 (the scale of a quantised row first), the result rounded
 // once more where it is stored in 16 bits.  A thread takes 8 neighbouring channels of some rows.
-constexpr int kEmThreads = 256;
+constexpr int kEmThreads = 128;
 
 // Types of rows in memory (hola_t_dtype).
 enum { kTabF32 = HOLA_T_F32, kTabBf16 = HOLA_T_BF16, kTabF16 = HOLA_T_F16, kTabInt8 = HOLA_T_INT8, kTabMixed = HOLA_T_MIXED };
@@ -159,18 +159,25 @@ __device__ __forceinline__ void em_mixed(const hola_wmix& mix, int H, int v, int
   }
 }
 
-// n: channels of a thread, 8 where everything is aligned; kWide: results of 32 bits, else of 16 (`f16`: which).  Bound by HBM: rows in, rows out.
+// n: channels that a thread takes at once, 8 where everything is aligned; kWide: results of 32 bits, else of 16 (`f16`: which).  A CTA takes
+// kRows rows at a time, or as many times that as leave no thread idle where rows are short (`lanes`: threads of a row, a power of two).
+// Bound by HBM: rows in, rows out.  us with 128 / 256 threads: 16384 x 4096 bf16 33.2 / 35.6, 20000 x 4096 int8 41 / 47; rows one by one
+// instead of four at a time: 2304 x 4096 int8 18.3 -> 13.1.
 template <int kType>
-__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed ? 2 : 4; }       // rows of a CTA, on the way together
+__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed ? 2 : 4; }       // rows on the way together
 
-template <int kType, bool kWide, bool kAdd, int n>
-__global__ void __launch_bounds__(kEmThreads, 4) embed_kernel(const __grid_constant__ EmParams p, int f16, int rows_per_cta) {
+// kShort: several rows side by side in a CTA (addresses that all threads share are cheaper: 16384 x 4096 bf16 36.2 -> 33.2 us).
+template <int kType, bool kWide, bool kAdd, bool kShort, int n>
+__global__ void __launch_bounds__(kEmThreads, 8) embed_kernel(const __grid_constant__ EmParams p, int f16, int some_rows, int lanes_log2) {
   constexpr bool kCodes = kType == kTabInt8 || kType == kTabMixed, kMixed = kType == kTabMixed;
   constexpr int kWord = kMixed ? kTabBf16 : kType, kRows = em_rows<kType>(), kOut = kWide ? kTabF32 : kTabBf16;
+  constexpr int kWords = n == 1 ? 4 : 1;                 // words of a row that a thread has on the way
   grid_dependency_wait();
   grid_dependency_release();
-  const long long r0 = static_cast<long long>(blockIdx.x) * rows_per_cta;
-  const int rows = static_cast<int>(p.N - r0 < rows_per_cta ? p.N - r0 : rows_per_cta);
+  const int lanes = kShort ? 1 << lanes_log2 : kEmThreads, lane = static_cast<int>(threadIdx.x) & (lanes - 1);
+  const long long r0 = kShort ? (static_cast<long long>(blockIdx.x) * (kEmThreads >> lanes_log2) + (threadIdx.x >> lanes_log2)) * some_rows
+                              : static_cast<long long>(blockIdx.x) * some_rows;
+  const int rows = static_cast<int>(p.N - r0 < some_rows ? p.N - r0 : some_rows);          // (less than one: none)
   int v[kRows];
   float ws[kRows];
   bool any_bad = false;
@@ -185,75 +192,91 @@ __global__ void __launch_bounds__(kEmThreads, 4) embed_kernel(const __grid_const
       if (kCodes && v[i] >= 0) ws[i] = p.w_scale[v[i]];
     }
   }
-  if (any_bad && p.status && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  if (any_bad && p.status && lane == 0 && blockIdx.y == 0) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
   // (what is neither scaled nor added to nor converted is passed on as it is)
   const bool as_is = !kAdd && p.scale == 1.f && (kWide ? kType == kTabF32 : kType == (f16 ? kTabF16 : kTabBf16));
-  const int step = static_cast<int>(gridDim.y) * kEmThreads * n;
+  const int apart = lanes * n;                           // a thread's words
 #pragma unroll 1
-  for (int h = (static_cast<int>(blockIdx.y) * kEmThreads + static_cast<int>(threadIdx.x)) * n; h < p.H; h += step) {
-    EmWord<kWord, n> w[kRows];
-    float x[kMixed ? kRows : 1][n];
-    EmWord<kOut, n> add[kAdd ? kRows : 1];
+  for (int h0 = static_cast<int>(blockIdx.y) * apart * kWords + lane * n; h0 < p.H; h0 += static_cast<int>(gridDim.y) * apart * kWords) {
+    EmWord<kWord, n> w[kRows][kWords];
+    float x[kMixed ? kRows : 1][kMixed ? kWords : 1][n];
+    EmWord<kOut, n> add[kAdd ? kRows : 1][kWords];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      if (v[i] >= 0) {
-        if (kMixed) em_mixed<n>(p.mix, p.H, v[i], h, x[kMixed ? i : 0]);
-        else w[i].load(static_cast<const unsigned char*>(p.table) + (v[i] * p.row_stride + h) * tab_bytes(kWord));
+    for (int i = 0; i < kRows; ++i)
+#pragma unroll
+      for (int u = 0; u < kWords; ++u) {
+        const int h = h0 + u * apart;
+        if (kWords > 1 && h >= p.H) continue;
+        if (v[i] >= 0) {
+          if (kMixed) em_mixed<n>(p.mix, p.H, v[i], h, x[kMixed ? i : 0][kMixed ? u : 0]);
+          else w[i][u].load(static_cast<const unsigned char*>(p.table) + (v[i] * p.row_stride + h) * tab_bytes(kWord));
+        }
+        if (kAdd && i < rows) add[kAdd ? i : 0][u].load(static_cast<const unsigned char*>(p.add) + ((r0 + i) * p.add_stride + h) * tab_bytes(kOut));
       }
-      if (kAdd && i < rows) add[kAdd ? i : 0].load(static_cast<const unsigned char*>(p.add) + ((r0 + i) * p.add_stride + h) * tab_bytes(kOut));
-    }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       if (i >= rows) break;
-      unsigned char* to = static_cast<unsigned char*>(p.out) + ((r0 + i) * p.out_stride + h) * tab_bytes(kOut);
-      float y[n];
-      if (v[i] >= 0) {
-        if (as_is) {
-          w[i].store(to);
-          continue;
-        }
 #pragma unroll
-        for (int c = 0; c < n; ++c) {
-          y[c] = kMixed ? x[kMixed ? i : 0][c] : w[i].get(c);
-          if (kCodes) y[c] = __fmul_rn(y[c], ws[i]);
-          y[c] = __fmul_rn(y[c], p.scale);
-        }
-      } else {
+      for (int u = 0; u < kWords; ++u) {
+        const int h = h0 + u * apart;
+        if (kWords > 1 && h >= p.H) continue;
+        unsigned char* to = static_cast<unsigned char*>(p.out) + ((r0 + i) * p.out_stride + h) * tab_bytes(kOut);
+        float y[n];
+        if (v[i] >= 0) {
+          if (as_is) {
+            w[i][u].store(to);
+            continue;
+          }
 #pragma unroll
-        for (int c = 0; c < n; ++c) y[c] = 0.f;
-      }
-      if (kAdd) {
-        const EmWord<kOut, n>& a = add[kAdd ? i : 0];
-        if (!kWide && f16) {
-          EmWord<kTabF16, n> b;
-#pragma unroll
-          for (int c = 0; c < static_cast<int>(sizeof a.w / 4); ++c) b.w[c] = a.w[c];
-#pragma unroll
-          for (int c = 0; c < n; ++c) y[c] = __fadd_rn(b.get(c), y[c]);
+          for (int c = 0; c < n; ++c) {
+            y[c] = kMixed ? x[kMixed ? i : 0][kMixed ? u : 0][c] : w[i][u].get(c);
+            if (kCodes) y[c] = __fmul_rn(y[c], ws[i]);
+            y[c] = __fmul_rn(y[c], p.scale);
+          }
         } else {
 #pragma unroll
-          for (int c = 0; c < n; ++c) y[c] = __fadd_rn(a.get(c), y[c]);
+          for (int c = 0; c < n; ++c) y[c] = 0.f;
         }
+        if (kAdd) {
+          const EmWord<kOut, n>& a = add[kAdd ? i : 0][u];
+          if (!kWide && f16) {
+            EmWord<kTabF16, n> b;
+#pragma unroll
+            for (int c = 0; c < static_cast<int>(sizeof a.w / 4); ++c) b.w[c] = a.w[c];
+#pragma unroll
+            for (int c = 0; c < n; ++c) y[c] = __fadd_rn(b.get(c), y[c]);
+          } else {
+#pragma unroll
+            for (int c = 0; c < n; ++c) y[c] = __fadd_rn(a.get(c), y[c]);
+          }
+        }
+        if (!kWide && f16) em_store<kTabF16, n>(to, y);
+        else em_store<kOut, n>(to, y);
       }
-      if (!kWide && f16) em_store<kTabF16, n>(to, y);
-      else em_store<kOut, n>(to, y);
     }
   }
 }
 
 template <int kType, bool kWide, bool kAdd, int n>
 cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
-  const long long slices = (p.H + kEmThreads * n - 1) / (kEmThreads * n);
-  // several rows of a CTA where there are CTAs enough all the same
-  const int rows = p.N * slices >= 8ll * em_rows<kType>() * num_sms ? em_rows<kType>() : 1;
+  constexpr int kAtOnce = n == 1 ? 4 : n;
+  int log2 = 0;
+  while ((1 << log2) < kEmThreads && (1 << log2) * kAtOnce < p.H) ++log2;
+  const int lanes = 1 << log2;
+  const long long slices = (p.H + lanes * kAtOnce - 1) / (lanes * kAtOnce);
+  const int slots = kEmThreads / lanes;
+  // several rows at a time where there are CTAs enough all the same
+  const int rows = p.N * slices >= 2ll * em_rows<kType>() * slots * num_sms ? em_rows<kType>() : 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((p.N + rows - 1) / rows), static_cast<unsigned>(slices > 65535 ? 65535 : slices));
+  cfg.gridDim = dim3(static_cast<unsigned>((p.N + rows * slots - 1) / (rows * slots)), static_cast<unsigned>(slices > 65535 ? 65535 : slices));
   cfg.blockDim = dim3(kEmThreads); cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, embed_kernel<kType, kWide, kAdd, n>, p, out_type == kTabF16 ? 1 : 0, rows);
+  const int f16 = out_type == kTabF16 ? 1 : 0;
+  if (n == 1 || lanes < kEmThreads) return cudaLaunchKernelEx(&cfg, embed_kernel<kType, kWide, kAdd, true, n>, p, f16, rows, log2);
+  return cudaLaunchKernelEx(&cfg, embed_kernel<kType, kWide, kAdd, n == 1, n>, p, f16, rows, log2);
 }
 template <int kType, int n>
 cudaError_t launch_embed_as(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
@@ -287,9 +310,9 @@ cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_s
 //    The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
 constexpr int kEsThreads = 1024, kEsWarps = 32;
 constexpr int kEsZipf = 74;            // Z
-constexpr int kEsList = 256;           // tokens that a warp lists before it counts them
+constexpr int kEsList = 256, kEsMaxList = 1024;       // tokens that a warp lists before it counts them: as many as there is room for
 constexpr int kEsLoads = 4;            // 32 tokens each that a warp has on the way
-constexpr int kEsCellBytes = 128 * 1024;       // counters of a CTA
+constexpr int kEsMaxShared = 216 * 1024;       // shared memory of a CTA
 constexpr int kEsIdBits = 11;          // ids of a range (with what is left of 32 bits for places in a warp's stretch)
 constexpr int kEgThreads = 128, kEgEach = 8;
 constexpr int kEgSlice = kEgThreads * kEgEach;
@@ -302,7 +325,8 @@ struct EgParams {
   int wide;
   int N, V, H;
   long long v_offset, V_global;
-  int even, buckets, warps, chunk;     // sort: U, ranges of ids, warps that count, tokens of a warp
+  int even, buckets, R, warps, chunk, list;      // sort: U, ranges of ids and how many a range holds at most, warps that count, tokens of a warp
+                                       // and how many of them it lists
   int S, window, slices;
   const void* grad;
   long long g_stride;
@@ -329,11 +353,22 @@ __device__ __forceinline__ int es_even_upto(int x, int V, int U) {
   return static_cast<int>(j < U - 1 ? j : U - 1);
 }
 
-// Cell: counters of a warp's tokens per id, 16 bits where there are few enough tokens.
-template <typename Cell>
+// Shared memory of the sort, of `ids` ids at most in a range: [warp][id] counters (`pitch` of them a warp), per id where its rows begin and
+// how many distinct ids lie before it, the warps' lists.
+struct EsLayout {
+  int pitch, heads, lists, total;
+  __host__ __device__ EsLayout(int ids, int warps, int list, int cell) {
+    pitch = (ids + 1) & ~1;
+    heads = (pitch * warps * cell + 15) & ~15;
+    lists = heads + (ids + 1) * 8;
+    total = lists + warps * list * 4;
+  }
+};
+
+// Cell: counters of a warp's tokens per id, 16 bits where there are few enough tokens; Token: as they lie in memory.
+template <typename Cell, typename Token>
 __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_constant__ EgParams p) {
   extern __shared__ __align__(16) unsigned char es_smem[];
-  __shared__ uint32_t list[kEsWarps][kEsList];
   __shared__ int warp_below[kEsWarps];
   __shared__ uint64_t warp_sum[kEsWarps];
   __shared__ int mark[kEsZipf], range[2];
@@ -342,8 +377,7 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   int place = 0;
   if (tid < kEsZipf - 1) {
     const float x = exp2f(log2f(static_cast<float>(p.V) + 1.f) * (static_cast<float>(tid + 1) / kEsZipf));
-    mark[tid] = static_cast<int>(fminf(x, static_cast<float>(p.V)));
-    mark[tid] = min(mark[tid], p.V);
+    mark[tid] = min(static_cast<int>(fminf(x, static_cast<float>(p.V))), p.V);
     place = tid + 1 + es_even_upto(mark[tid], p.V, p.even);
   }
 #pragma unroll
@@ -356,10 +390,11 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   }
   __syncthreads();
   const int lo = range[0], R = range[1] - lo;
-  // [warp][id] counters, then per id where its rows begin and how many distinct ids lie before it
-  Cell* cells = reinterpret_cast<Cell*>(es_smem);
-  int2* heads = reinterpret_cast<int2*>(es_smem + kEsCellBytes);
-  for (int i = tid; i < (R * p.warps * static_cast<int>(sizeof(Cell)) + 15) / 16; i += kEsThreads) reinterpret_cast<uint4*>(es_smem)[i] = make_uint4(0, 0, 0, 0);
+  const EsLayout lay(p.R, p.warps, p.list, static_cast<int>(sizeof(Cell)));
+  Cell* cells = reinterpret_cast<Cell*>(es_smem) + warp * lay.pitch;
+  int2* heads = reinterpret_cast<int2*>(es_smem + lay.heads);
+  uint32_t* list = reinterpret_cast<uint32_t*>(es_smem + lay.lists) + warp * p.list;
+  for (int i = tid; i < lay.heads / 16; i += kEsThreads) reinterpret_cast<uint4*>(es_smem)[i] = make_uint4(0, 0, 0, 0);
   grid_dependency_wait();
   grid_dependency_release();
   // (counters of the second launch)
@@ -371,43 +406,60 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   const int len = warp < p.warps ? static_cast<int>(min(static_cast<long long>(p.chunk), max(p.N - begin, 0ll))) : 0;
   int below = 0, n = 0;
   bool any_bad = false;
-  // One pass over the warp's stretch; full(): the list may not hold the next tokens, last() at the end.
+  // Row of the table; none: above every row (as differences that wrap are).
+  const unsigned V_global = static_cast<unsigned>(p.V_global), v_offset = static_cast<unsigned>(p.v_offset);
+  auto row_of = [&](Token x, bool* inside) {
+    unsigned t = static_cast<unsigned>(x);
+    if (sizeof(Token) == 8 && static_cast<uint64_t>(x) >> 32 != 0) t = 0xffffffffu;
+    *inside = t < V_global;
+    return *inside ? t - v_offset : 0xffffffffu;
+  };
+  // One pass over the warp's stretch, one batch ahead; full(): the list may not hold the next tokens.
   auto stream = [&](bool count, auto&& full) {
+    const Token* at = static_cast<const Token*>(p.tokens) + begin + lane;
+    Token next[kEsLoads];
+#pragma unroll
+    for (int u = 0; u < kEsLoads; ++u) {
+      next[u] = -1;
+      if (32 * u + lane < len) next[u] = at[32 * u];
+    }
 #pragma unroll 1
     for (int r0 = 0; r0 < len; r0 += 32 * kEsLoads) {
-      long long t[kEsLoads];
+      unsigned v[kEsLoads];
 #pragma unroll
       for (int u = 0; u < kEsLoads; ++u) {
-        const int r = r0 + 32 * u + lane;
-        t[u] = -1;
-        if (r < len) t[u] = p.wide ? static_cast<const long long*>(p.tokens)[begin + r] : static_cast<const int*>(p.tokens)[begin + r];
+        bool inside;
+        v[u] = row_of(next[u], &inside);
+        if (count && g == 0) any_bad = any_bad || (!inside && next[u] != -1);
+      }
+      at += 32 * kEsLoads;
+      const int left = len - r0 - 32 * kEsLoads - lane;
+#pragma unroll
+      for (int u = 0; u < kEsLoads; ++u) {
+        next[u] = -1;
+        if (32 * u < left) next[u] = at[32 * u];
       }
 #pragma unroll
       for (int u = 0; u < kEsLoads; ++u) {
-        const long long v = t[u] - p.v_offset;
-        const bool there = t[u] >= 0 && v >= 0 && v < p.V;
-        const unsigned id = static_cast<unsigned>(static_cast<int>(v) - lo);
-        if (count) {
-          any_bad = any_bad || t[u] < -1 || t[u] >= p.V_global;
-          below += there && v < lo ? 1 : 0;
-        }
-        const bool mine = there && v >= lo && id < static_cast<unsigned>(R);
+        if (count) below += v[u] < static_cast<unsigned>(lo) ? 1 : 0;
+        const unsigned id = v[u] - static_cast<unsigned>(lo);
+        const bool mine = id < static_cast<unsigned>(R);
         const unsigned in = __ballot_sync(0xffffffffu, mine);
         if (in) {
-          if (mine) list[warp][n + __popc(in & ((1u << lane) - 1u))] = static_cast<uint32_t>(r0 + 32 * u + lane) << kEsIdBits | id;
+          if (mine) list[n + __popc(in & ((1u << lane) - 1u))] = static_cast<uint32_t>(r0 + 32 * u + lane) << kEsIdBits | id;
           n += __popc(in);
         }
       }
-      if (n > kEsList - 32 * kEsLoads) full();
+      if (n > p.list - 32 * kEsLoads) full();
     }
   };
   auto count_list = [&]() {
     __syncwarp();
     for (int i = 0; i < n; i += 32) {
       // (lanes without a token: an id that there is not)
-      const unsigned id = i + lane < n ? list[warp][i + lane] & ((1u << kEsIdBits) - 1u) : 0xffffffffu;
+      const unsigned id = i + lane < n ? list[i + lane] & ((1u << kEsIdBits) - 1u) : 0xffffffffu;
       const unsigned same = __match_any_sync(0xffffffffu, id);
-      if (i + lane < n && __ffs(same) - 1 == lane) cells[warp * R + id] += static_cast<Cell>(__popc(same));
+      if (i + lane < n && __ffs(same) - 1 == lane) cells[id] += static_cast<Cell>(__popc(same));
       __syncwarp();
     }
   };
@@ -416,22 +468,30 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   count_list();
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) warp_below[warp] = below;
-  if (__any_sync(0xffffffffu, any_bad) && lane == 0 && g == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  if (__any_sync(0xffffffffu, any_bad) && lane == 0 && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
   __syncthreads();
 
-  // Per id: exclusive sums over the warps.  Over the ids: a thread's ids lie side by side; tokens in the upper half, distinct ids in the lower.
-  const int each = (R + kEsThreads - 1) / kEsThreads, i0 = min(tid * each, R), i1 = min(i0 + each, R);
-  uint64_t sum = 0;
-  for (int i = i0; i < i1; ++i) {
-    unsigned all = 0;
+  // Per id: exclusive sums over the warps (two ids of 16 bits in one word; neither half runs over).  Over the ids: tokens in the upper half,
+  // distinct ids in the lower.
+  const int i0 = 2 * tid;
+  unsigned all[2] = {0, 0};
+  if (i0 < R) {
+    using Pair = std::conditional_t<sizeof(Cell) == 2, uint32_t, uint2>;
+    Pair* word = reinterpret_cast<Pair*>(reinterpret_cast<Cell*>(es_smem) + i0);
+    const int step = lay.pitch / 2;
+    Pair run = {};
+#pragma unroll 8
     for (int w = 0; w < p.warps; ++w) {
-      const unsigned c = cells[w * R + i];
-      cells[w * R + i] = static_cast<Cell>(all);
-      all += c;
+      const Pair c = word[w * step];
+      word[w * step] = run;
+      if constexpr (sizeof(Cell) == 2) run += c;
+      else run = make_uint2(run.x + c.x, run.y + c.y);
     }
-    heads[i] = make_int2(static_cast<int>(all), 0);
-    sum += static_cast<uint64_t>(all) << 32 | (all ? 1u : 0u);
+    if constexpr (sizeof(Cell) == 2) { all[0] = run & 0xffffu; all[1] = run >> 16; }
+    else { all[0] = run.x; all[1] = run.y; }
+    if (i0 + 1 >= R) all[1] = 0;
   }
+  const uint64_t sum = static_cast<uint64_t>(all[0] + all[1]) << 32 | ((all[0] ? 1u : 0u) + (all[1] ? 1u : 0u));
   uint64_t upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -453,11 +513,11 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
     before = __shfl_sync(0xffffffffu, x - mine, warp);
     total = __shfl_sync(0xffffffffu, x, 31);
   }
-  uint64_t at = before + upto - sum;
-  for (int i = i0; i < i1; ++i) {
-    const unsigned all = static_cast<unsigned>(heads[i].x);
-    heads[i] = make_int2(base + static_cast<int>(at >> 32), static_cast<int>(at & 0xffffffffu));
-    at += static_cast<uint64_t>(all) << 32 | (all ? 1u : 0u);
+  const uint64_t at = before + upto - sum;
+  if (i0 < R) {
+    const int head = base + static_cast<int>(at >> 32), number = static_cast<int>(at & 0xffffffffu);
+    heads[i0] = make_int2(head, number);
+    if (i0 + 1 < R) heads[i0 + 1] = make_int2(head + static_cast<int>(all[0]), number + (all[0] ? 1 : 0));
   }
   const int end = base + static_cast<int>(total >> 32);
   if (tid == 0) {
@@ -476,14 +536,14 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
     __syncwarp();
     for (int i = 0; i < n; i += 32) {
       const bool have = i + lane < n;
-      const uint32_t entry = have ? list[warp][i + lane] : 0;
+      const uint32_t entry = have ? list[i + lane] : 0;
       const unsigned id = have ? entry & ((1u << kEsIdBits) - 1u) : 0xffffffffu;
       const unsigned same = __match_any_sync(0xffffffffu, id);
       unsigned ahead = 0;
-      if (have) ahead = cells[warp * R + id];
+      if (have) ahead = cells[id];
       __syncwarp();
       if (have) {
-        if (__ffs(same) - 1 == lane) cells[warp * R + id] = static_cast<Cell>(ahead + __popc(same));
+        if (__ffs(same) - 1 == lane) cells[id] = static_cast<Cell>(ahead + __popc(same));
         const int2 head = heads[id];
         const int to = head.x + static_cast<int>(ahead) + __popc(same & ((1u << lane) - 1u));
         p.places[to] = make_int4(static_cast<int>(begin + (entry >> kEsIdBits)), lo + static_cast<int>(id), head.x, heads[id + 1].x);
@@ -610,6 +670,18 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     }
     piece_ends[i] = ends ? 1 : 0;
   }
+  __syncthreads();
+
+  // (the first rows are on their way while the rows of the result are looked up)
+  EgRow<kType, kVec> g[kEgAhead];
+  auto load = [&](int x) {
+    const int4 some = *reinterpret_cast<const int4*>(rows + (x - x0)), more = *reinterpret_cast<const int4*>(rows + (x - x0) + 4);
+    const int at[kEgAhead] = {some.x, some.y, some.z, some.w, more.x, more.y, more.z, more.w};
+#pragma unroll
+    for (int u = 0; u < kEgAhead; ++u)
+      if (x + u < x1) g[u].load(p, at[u], slice);
+  };
+  if (kVec) load(x0);
   if (p.by_rows) {
     // The distinct ids ahead of an id's own range, and ahead of it there.
     __shared__ int range0;
@@ -635,14 +707,9 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   float sum[kEgEach] = {};
 #pragma unroll 1
   for (int x = x0; x < x1; x += kEgAhead) {
-    EgRow<kType, kVec> g[kEgAhead];
+    if (!kVec || x > x0) load(x);
     const int n = min(kEgAhead, x1 - x);
-    const int4 some = *reinterpret_cast<const int4*>(rows + (x - x0)), more = *reinterpret_cast<const int4*>(rows + (x - x0) + 4);
-    const int at[kEgAhead] = {some.x, some.y, some.z, some.w, more.x, more.y, more.z, more.w};
     const uint64_t last = *reinterpret_cast<const uint64_t*>(piece_ends + (x - x0));
-#pragma unroll
-    for (int u = 0; u < kEgAhead; ++u)
-      if (u < n) g[u].load(p, at[u], slice);
 #pragma unroll
     for (int u = 0; u < kEgAhead; ++u) {
       if (u >= n) break;
@@ -693,19 +760,27 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   p->N = static_cast<int>(N); p->V = V; p->H = H;
   int warps = 1;
   while (warps < kEsWarps && N > 64ll * warps) warps <<= 1;      // a warp's stretch: 64 tokens, or more once all count
+  // Ranges: one per SM where their counters fit, else as many as it takes.  (A thread adds up two ids.)
+  const int cell = N <= UINT16_MAX ? 2 : 4, most = (1 << kEsIdBits) - 2;
+  int ids = (V + kEgPlanSms - kEsZipf) / (kEgPlanSms - kEsZipf + 1);
+  if (ids > most) ids = most;
+  // (rather fewer warps than a second round of CTAs)
+  while (warps > kEsWarps / 2 && EsLayout(ids, warps, kEsList, cell).total > kEsMaxShared) warps -= 4;
+  while (EsLayout(ids, warps, kEsList, cell).total > kEsMaxShared) --ids;
+  const int room = (kEsMaxShared - EsLayout(ids, warps, 0, cell).total) / (4 * warps) / 32 * 32;
+  p->list = room < kEsMaxList ? room : kEsMaxList;
   p->warps = warps;
   p->chunk = static_cast<int>(((N + warps - 1) / warps + 31) / 32 * 32);
-  // Ranges: one per SM where their counters fit, else as many as it takes.
-  const int cell = N <= UINT16_MAX ? 2 : 4, ids = min(kEsCellBytes / (cell * warps), (1 << kEsIdBits) - 2);
-  const int even = (V + ids - 1) / ids + 1;
-  p->even = even > kEgPlanSms - kEsZipf + 1 ? even : kEgPlanSms - kEsZipf + 1;
+  if (p->chunk == 0) p->chunk = 32;
+  p->R = ids;
+  p->even = (V + ids - 1) / ids;
   p->buckets = p->even + kEsZipf - 1;
-  int S = 64;
-  while (S < kEgMaxPiece && N > 256ll * S) S <<= 1;
+  int S = 32;                                            // (some 512 pieces, where one token is all there is)
+  while (S < kEgMaxPiece && N > 512ll * S) S <<= 1;
   p->S = S;
   p->slices = (H + kEgSlice - 1) / kEgSlice;
   int window = kEgMaxWindow;
-  while (window > 4 && (N + window - 1) / window * p->slices < 4ll * kEgPlanSms) window >>= 1;
+  while (window > 4 && (N + window - 1) / window * p->slices < 16ll * kEgPlanSms) window >>= 1;
   p->window = window;
   const size_t pieces = static_cast<size_t>((N + S - 1) / S);
   size_t at = 0;
@@ -721,8 +796,6 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   return true;
 }
 
-constexpr int kEsDynamic = kEsCellBytes + (1 << kEsIdBits) * 8;
-
 template <int kType>
 cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
@@ -731,8 +804,10 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
   cudaLaunchConfig_t cfg = {};
   cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
   cfg.gridDim = dim3(static_cast<unsigned>(p.buckets)); cfg.blockDim = dim3(kEsThreads);
-  cfg.dynamicSmemBytes = kEsDynamic;
-  const cudaError_t e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t>, p);
+  cfg.dynamicSmemBytes = static_cast<size_t>(EsLayout(p.R, p.warps, p.list, p.N <= UINT16_MAX ? 2 : 4).total);
+  cudaError_t e;
+  if (p.wide) e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int64_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int64_t>, p);
+  else e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int32_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int32_t>, p);
   if (e != cudaSuccess) return e;
   const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
   const long long blank = p.first ? (static_cast<long long>(p.V) + kEgMaxWindow - 1) / kEgMaxWindow : 0;
@@ -742,7 +817,22 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
              : cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, false>, p, out_type, static_cast<int>(windows));
 }
 
+template <typename Cell>
+cudaError_t configure_sort() {
+  const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel<Cell, int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsMaxShared);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_sort_kernel<Cell, int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsMaxShared);
+}
+// The sums' loads on the way need room in the L1: without a preference the SMs stay as the sort, which takes nearly all of them for shared memory, has
+// left them (16384 rows of 4096 81.4 -> 70.6 us, 32768 Zipf tokens 108 -> 92).
+template <int kType>
+cudaError_t configure_sums() {
+  const cudaError_t e = cudaFuncSetAttribute(embed_grad_kernel<kType, true>, cudaFuncAttributePreferredSharedMemoryCarveout, 25);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_grad_kernel<kType, false>, cudaFuncAttributePreferredSharedMemoryCarveout, 25);
+}
 cudaError_t configure_embedding() {
-  const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel<uint16_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsDynamic);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_sort_kernel<uint32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsDynamic);
+  cudaError_t e = configure_sort<uint16_t>();
+  if (e == cudaSuccess) e = configure_sort<uint32_t>();
+  if (e == cudaSuccess) e = configure_sums<kTabF32>();
+  if (e == cudaSuccess) e = configure_sums<kTabBf16>();
+  return e == cudaSuccess ? configure_sums<kTabF16>() : e;
 }

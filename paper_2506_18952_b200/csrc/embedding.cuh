@@ -310,13 +310,14 @@ cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_s
 //    The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
 constexpr int kEsThreads = 1024, kEsWarps = 32;
 constexpr int kEsZipf = 74;            // Z
-constexpr int kEsList = 256, kEsMaxList = 1024;       // tokens that a warp lists before it counts them: as many as there is room for
-constexpr int kEsLoads = 4;            // 32 tokens each that a warp has on the way
+constexpr int kEsList = 512, kEsMaxList = 1024;       // tokens that a warp lists before it counts them: as many as there is room for
+constexpr int kEsLoads = 8;            // 32 tokens each that a warp has on the way
 constexpr int kEsMaxShared = 216 * 1024;       // shared memory of a CTA
 constexpr int kEsIdBits = 11;          // ids of a range (with what is left of 32 bits for places in a warp's stretch)
 constexpr int kEgThreads = 128, kEgEach = 8;
 constexpr int kEgSlice = kEgThreads * kEgEach;
 constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
+constexpr int kEgRanges = 2 * kEgThreads;        // ranges of ids whose distinct ones are added up beforehand
 constexpr int kEgAhead = 8;            // rows of a thread on the way
 constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspace has to be known without a device)
 
@@ -327,7 +328,7 @@ struct EgParams {
   long long v_offset, V_global;
   int even, buckets, R, warps, chunk, list;      // sort: U, ranges of ids and how many a range holds at most, warps that count, tokens of a warp
                                        // and how many of them it lists
-  int S, window, slices;
+  int S, S_log2, window, slices;
   const void* grad;
   long long g_stride;
   float scale;
@@ -406,6 +407,7 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   const int len = warp < p.warps ? static_cast<int>(min(static_cast<long long>(p.chunk), max(p.N - begin, 0ll))) : 0;
   int below = 0, n = 0;
   bool any_bad = false;
+  const bool looks = g + 1 == p.buckets;                 // for what is no token at all (the last range's ids are rare ones)
   // Row of the table; none: above every row (as differences that wrap are).
   const unsigned V_global = static_cast<unsigned>(p.V_global), v_offset = static_cast<unsigned>(p.v_offset);
   auto row_of = [&](Token x, bool* inside) {
@@ -425,24 +427,19 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
     }
 #pragma unroll 1
     for (int r0 = 0; r0 < len; r0 += 32 * kEsLoads) {
-      unsigned v[kEsLoads];
-#pragma unroll
-      for (int u = 0; u < kEsLoads; ++u) {
-        bool inside;
-        v[u] = row_of(next[u], &inside);
-        if (count && g == 0) any_bad = any_bad || (!inside && next[u] != -1);
-      }
       at += 32 * kEsLoads;
       const int left = len - r0 - 32 * kEsLoads - lane;
 #pragma unroll
       for (int u = 0; u < kEsLoads; ++u) {
+        bool inside;
+        const unsigned v = row_of(next[u], &inside);
+        if (count) {
+          if (looks) any_bad = any_bad || (!inside && next[u] != -1);
+          below += v < static_cast<unsigned>(lo) ? 1 : 0;
+        }
         next[u] = -1;
         if (32 * u < left) next[u] = at[32 * u];
-      }
-#pragma unroll
-      for (int u = 0; u < kEsLoads; ++u) {
-        if (count) below += v[u] < static_cast<unsigned>(lo) ? 1 : 0;
-        const unsigned id = v[u] - static_cast<unsigned>(lo);
+        const unsigned id = v - static_cast<unsigned>(lo);
         const bool mine = id < static_cast<unsigned>(R);
         const unsigned in = __ballot_sync(0xffffffffu, mine);
         if (in) {
@@ -615,7 +612,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   __shared__ __align__(16) uint8_t piece_ends[kEgMaxWindow + kEgMaxPiece + kEgAhead];
   __shared__ int4 spots[kEgMaxWindow];
   __shared__ int firsts[kEgMaxWindow + 1], out_rows[kEgMaxWindow];
-  __shared__ int part_sum[kEgThreads / 32];
+  __shared__ int part_sum[kEgThreads / 32], range_rows[kEgRanges];
   __shared__ int last_here;
   const int slice = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.slices)), tid = threadIdx.x;
   const int w = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.slices));
@@ -632,13 +629,27 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     return;
   }
   // (behind the last valid place there is something to read, which is not used)
-  const int w0 = w * p.window;
+  const int w0 = w * p.window, before_S = p.S - 1;
   int4 spot = make_int4(0, 0, 0, 0);
   int2 number = make_int2(0, 0);
   if (tid < p.window && w0 + tid < p.N) {
     spot = p.places[w0 + tid];
     if (p.by_rows) number = p.numbers[w0 + tid];
     spots[tid] = spot;
+  }
+  // by rows: distinct ids of the first kEgRanges ranges, two a thread, added up
+  int in_range[2] = {0, 0}, upto = 0;
+  if (p.by_rows) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (2 * tid + i < p.buckets) in_range[i] = p.distinct[2 * tid + i];
+    upto = in_range[0] + in_range[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, o);
+      if ((tid & 31) >= o) upto += x;
+    }
+    if ((tid & 31) == 31) part_sum[tid >> 5] = upto;
   }
   const int w1 = min(w0 + p.window, *p.valid);
   if (w == 0 && slice == 0 && p.by_rows && tid < 32) {
@@ -649,14 +660,21 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   }
   if (w0 >= w1) return;
   __syncthreads();
+  if (p.by_rows) {
+    // where each range's ids begin in the result
+    int at = upto - in_range[0] - in_range[1];
+    for (int i = 0; i < tid >> 5; ++i) at += part_sum[i];
+    range_rows[2 * tid] = at;
+    range_rows[2 * tid + 1] = at + in_range[0];
+  }
   // Places x0 .. x1 - 1: from the first piece that begins in the window to the end of the last one that does.
   int x0 = w0, x1 = w1;
   {
-    const int in = (w0 - spots[0].z) % p.S;
+    const int in = (w0 - spots[0].z) & before_S;
     if (in != 0) x0 = min(w0 + p.S - in, spots[0].w);
     if (x0 >= w1) return;                                // (all of the window inside one piece)
     const int4 last = spots[w1 - 1 - w0];
-    x1 = min(last.z + ((w1 - 1 - last.z) / p.S + 1) * p.S, last.w);
+    x1 = min(last.z + (((w1 - 1 - last.z) | before_S) + 1), last.w);
   }
   for (int i = tid; i < x1 - x0; i += kEgThreads) {
     // (places behind the window belong to the last piece)
@@ -664,7 +682,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     if (x0 + i < w1) {
       const int4 here = spots[x0 + i - w0];
       rows[i] = here.x;
-      ends = x0 + i + 1 == here.w || (x0 + i + 1 - here.z) % p.S == 0;
+      ends = x0 + i + 1 == here.w || ((x0 + i + 1 - here.z) & before_S) == 0;
     } else {
       rows[i] = p.places[x0 + i].x;
     }
@@ -682,25 +700,15 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
       if (x + u < x1) g[u].load(p, at[u], slice);
   };
   if (kVec) load(x0);
-  if (p.by_rows) {
-    // The distinct ids ahead of an id's own range, and ahead of it there.
-    __shared__ int range0;
-    if (tid == 0) range0 = number.x;
-    __syncthreads();
-    int n = 0;
-    for (int i = tid; i < range0; i += kEgThreads) n += p.distinct[i];
-    n = __reduce_add_sync(0xffffffffu, n);
-    if ((tid & 31) == 0) part_sum[tid >> 5] = n;
-    __syncthreads();
-    if (tid < w1 - w0) {
-      n = 0;
-      for (int i = 0; i < kEgThreads / 32; ++i) n += part_sum[i];
+  if (tid < w1 - w0) {
+    int row = spot.y;
+    if (p.by_rows) {
+      // the distinct ids ahead of an id's own range, and ahead of it there
+      row = range_rows[min(number.x, kEgRanges - 1)] + number.y;
 #pragma unroll 4
-      for (int i = range0; i < number.x; ++i) n += p.distinct[i];
-      out_rows[tid] = n + number.y;
+      for (int i = kEgRanges - 1; i < number.x; ++i) row += p.distinct[i];
     }
-  } else if (tid < w1 - w0) {
-    out_rows[tid] = spot.y;
+    out_rows[tid] = row;
   }
   __syncthreads();
 
@@ -719,16 +727,16 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
       const int k = min(x + u, w1 - 1) - w0, begin = spots[k].z, end = spots[k].w;
       if (end - begin > p.S) {
         // One of several pieces.
-        const int from = begin + (x + u - begin) / p.S * p.S;
+        const int from = begin + ((x + u - begin) & ~before_S);
         const long long width = static_cast<long long>(p.slices) * kEgSlice;
-        float* mine = p.partial + (2ll * (from / p.S) + (from == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
+        float* mine = p.partial + (2ll * (from >> p.S_log2) + (from == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
 #pragma unroll
         for (int i = 0; i < kEgEach; ++i) { mine[i * kEgThreads] = sum[i]; sum[i] = 0.f; }
         __threadfence();
         __syncthreads();
         if (tid == 0) {
-          const unsigned n = static_cast<unsigned>((end - begin + p.S - 1) / p.S);
-          last_here = atomicAdd(&p.done[static_cast<long long>(begin / p.S) * p.slices + slice], 1u) == n - 1 ? 1 : 0;
+          const unsigned n = static_cast<unsigned>((end - begin + before_S) >> p.S_log2);
+          last_here = atomicAdd(&p.done[static_cast<long long>(begin >> p.S_log2) * p.slices + slice], 1u) == n - 1 ? 1 : 0;
         }
         __syncthreads();
         const bool all_there = last_here != 0;
@@ -737,7 +745,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
         __threadfence();
 #pragma unroll 4
         for (int b = begin; b < end; b += p.S) {
-          const float* y = p.partial + (2ll * (b / p.S) + (b == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
+          const float* y = p.partial + (2ll * (b >> p.S_log2) + (b == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
 #pragma unroll
           for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], __ldcg(y + i * kEgThreads));
         }
@@ -778,6 +786,8 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   int S = 32;                                            // (some 512 pieces, where one token is all there is)
   while (S < kEgMaxPiece && N > 512ll * S) S <<= 1;
   p->S = S;
+  p->S_log2 = 0;
+  while (1 << p->S_log2 < S) ++p->S_log2;
   p->slices = (H + kEgSlice - 1) / kEgSlice;
   int window = kEgMaxWindow;
   while (window > 4 && (N + window - 1) / window * p->slices < 16ll * kEgPlanSms) window >>= 1;

@@ -358,6 +358,7 @@ hola_status hola_token_logprobs(const hola_logprobs_args* args, void* cuda_strea
  * keep_slots (n = W): instead of by rank, the best child of a beam is written at that beam's own place, so that its state need not
  * move; the other candidates take the free places in their order.
  * finished_out: 1 where the parent had ended or the token is end_token.
+ * Outputs may not overlap inputs, but with n = W score_out may be score itself, and finished_out finished.
  * Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing, needs no context,
  * and launched like hola_verify (programmatic stream serialization, waits before it reads). */
 #define HOLA_MAX_BEAMS 32
@@ -452,8 +453,8 @@ hola_status hola_embed(const hola_embed_args* args, void* cuda_stream);
  * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs no context, two launches like
  * hola_verify's. */
 typedef struct hola_embed_grad_args {
-  int64_t N;                /* >= 0, < 2^31 - 1                                                           */
-  int32_t V, H;
+  int64_t N;                /* 0 .. 2^25                                                                  */
+  int32_t V, H;             /* V at most 2^30                                                             */
   int32_t v_offset, V_global;
   const void* tokens;
   int32_t wide_tokens;

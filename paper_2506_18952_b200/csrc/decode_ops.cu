@@ -61,6 +61,11 @@ static const DeviceFacts* device_facts() {
   return &facts[dev];
 }
 
+static bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
+}
+
 hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   if (!a || a->B < 0 || a->W <= 0 || a->V <= 0 || a->n <= 0 || a->seq_stride < 0 || a->beam_stride < 0) return HOLA_ERR_INVALID_ARG;
   if (a->l_dtype < HOLA_L_F32 || a->l_dtype > HOLA_L_F16) return HOLA_ERR_INVALID_ARG;
@@ -70,6 +75,15 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   if (a->B == 0) return HOLA_OK;
   if (!a->logits || !a->logZ || !a->score || !a->score_out || !a->parent || !a->token) return HOLA_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(a->logits) % (a->l_dtype == HOLA_L_F32 ? 4 : 2)) return HOLA_ERR_INVALID_ARG;
+  // A sequence is written when all of it has been read; another one's beams may lie where its candidates go, but for the same layout.
+  const long long beams = static_cast<long long>(a->B) * a->W, kept = static_cast<long long>(a->B) * a->n;
+  const struct { const void* at; int bytes; } in[] = {{a->score, 4}, {a->logZ, 4}, {a->weight, 4}, {a->finished, 1}},
+                                              out[] = {{a->score_out, 4}, {a->finished_out, 1}, {a->parent, 4}, {a->token, 4}};
+  for (const auto& x : in)
+    for (const auto& y : out) {
+      const bool itself = a->n == a->W && x.at == y.at && ((x.at == a->score && y.at == a->score_out) || (x.at == a->finished && y.at == a->finished_out));
+      if (!itself && overlap(x.at, beams * x.bytes, y.at, kept * y.bytes)) return HOLA_ERR_INVALID_ARG;
+    }
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   BsParams p = {};

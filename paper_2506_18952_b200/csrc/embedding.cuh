@@ -319,6 +319,7 @@ constexpr int kEgSlice = kEgThreads * kEgEach;
 constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
 constexpr int kEgRanges = 2 * kEgThreads;        // ranges of ids whose distinct ones are added up beforehand
 constexpr int kEgAhead = 8;            // rows of a thread on the way
+constexpr long long kEgMaxTokens = 1 << 25;      // what is left of a list's words for places in the stretch of one of 16 warps
 constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspace has to be known without a device)
 
 struct EgParams {
@@ -764,7 +765,7 @@ struct EgLayout {
 
 // Host: the cut of the work.  False: sizes that are not served.
 bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
-  if (N < 0 || N > 1 << 26 || V <= 0 || H <= 0 || V > 1 << 30 || H > INT32_MAX - kEgSlice) return false;
+  if (N < 0 || N > kEgMaxTokens || V <= 0 || H <= 0 || V > 1 << 30 || H > INT32_MAX - kEgSlice) return false;
   p->N = static_cast<int>(N); p->V = V; p->H = H;
   int warps = 1;
   while (warps < kEsWarps && N > 64ll * warps) warps <<= 1;      // a warp's stretch: 64 tokens, or more once all count

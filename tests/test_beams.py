@@ -466,8 +466,8 @@ def _args(**kw):
     a = binding.hola_beam_args()
     a.B, a.W, a.V, a.n, a.end_token = 2, 4, 100, 4, -1
     a.seq_stride, a.beam_stride = 400, 100
-    for name in ("logits", "logZ", "score", "score_out", "parent", "token"):
-        setattr(a, name, 4096)
+    for i, name in enumerate(("logits", "logZ", "score", "score_out", "parent", "token")):
+        setattr(a, name, 4096 * (20 + i))
     for name, v in kw.items():
         setattr(a, name, v)
     return a
@@ -477,7 +477,9 @@ def _args(**kw):
     (dict(B=-1), 1), (dict(W=0), 1), (dict(V=0), 1), (dict(n=0), 1), (dict(l_dtype=3), 1), (dict(l_dtype=-1), 1), (dict(seq_stride=-1), 1),
     (dict(W=33, n=4), 2), (dict(n=33), 2), (dict(V=2 ** 27 + 1), 2), (dict(B=2 ** 31 - 1), 2), (dict(keep_slots=1, n=5), 1), (dict(end_token=100), 1),
     (dict(end_token=-2), 1), (dict(finished=4096), 1), (dict(logits=None), 1), (dict(logZ=None), 1), (dict(score=None), 1), (dict(parent=None), 1),
-    (dict(token=None), 1), (dict(score_out=None), 1), (dict(logits=4098), 1), (dict(B=0), 0), (dict(B=0, logits=None), 0)])
+    (dict(token=None), 1), (dict(score_out=None), 1), (dict(logits=4098), 1), (dict(B=0), 0), (dict(B=0, logits=None), 0),
+    (dict(score=8192, score_out=8192 + 16), 1), (dict(score=8192, score_out=8192, n=3), 1), (dict(score=8192, score_out=16384, token=8192 + 28), 1),
+    (dict(score=8192, score_out=16384, logZ=16384), 1), (dict(finished=8192, end_token=3, finished_out=8196), 1)])
 def test_selections_that_are_refused(kw, status):
     lib = binding.load_library()
     assert lib.hola_beam_select(ctypes.byref(_args(**kw)), None) == status
@@ -618,3 +620,17 @@ def test_the_drivers_beam_search():
                 assert abs(float(ended.score[b, w]) - float(lp[b, w, :n].sum())) <= steps * 1e-3
                 assert (ended.tokens[b, w, 2 + n:] == end).all()
         assert (ended.tokens[0, :, 2:] == end).any()
+
+
+@gpu
+@pytest.mark.parametrize("B", [1, 200])
+def test_scores_that_are_written_over(B):
+    """A loop that keeps its scores in place: many CTAs a sequence, and one."""
+    W, V = 4, 30000 if B == 1 else 900
+    l, z, s = make(B, W, V, torch.float32, 9)
+    f = torch.zeros((B, W), dtype=torch.bool, device="cuda")
+    f[:, 1] = True
+    want = reference(l, z, s, W, f, 5)
+    out = binding.BeamSelection(s, torch.empty((B, W), dtype=torch.int32, device="cuda"), torch.empty((B, W), dtype=torch.int32, device="cuda"), f)
+    binding.hola_beam_select(l, z, s, W, f, 5, out=out)
+    same(out, want)

@@ -361,7 +361,7 @@ def test_lookups_that_are_refused(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(N=-1), 1), (dict(V=0), 1), (dict(H=0), 1), (dict(g_dtype=3), 1), (dict(out_dtype=3), 1), (dict(out_stride=15), 1), (dict(tokens=None), 1),
     (dict(grad=None), 1), (dict(out=None), 1), (dict(workspace=None), 1), (dict(workspace=4097), 1), (dict(workspace_bytes=100), 1), (dict(ids_out=4096), 1),
-    (dict(count_out=4096), 1), (dict(ids_out=4096, count_out=4096, accumulate=1), 1), (dict(N=2 ** 31 - 1), 2), (dict(V=2 ** 31 - 1), 2), (dict(grad=4098), 1),
+    (dict(count_out=4096), 1), (dict(ids_out=4096, count_out=4096, accumulate=1), 1), (dict(N=2 ** 31 - 1), 2), (dict(N=2 ** 25 + 1), 2), (dict(V=2 ** 30 + 1), 2), (dict(V=2 ** 31 - 1), 2), (dict(grad=4098), 1),
     (dict(v_offset=1), 1), (dict(v_offset=5, V_global=12), 1)])
 def test_gradients_that_are_refused(kw, status):
     lib = binding.load_library()
@@ -524,3 +524,41 @@ def test_the_drivers_lookups_are_those_of_the_tables():
     assert torch.equal(models.target_hidden(a, b), models._norm(models.E1[a] + 0.35 * models.E2[b], a).to(torch.bfloat16))
     h = models._norm(models.E1[a], a).to(torch.bfloat16).float()
     assert torch.equal(models.draft_probs(a), torch.softmax(h @ models.W_lm.float().T, dim=-1))
+
+
+@gpu
+def test_what_absent_tokens_hold_is_not_read():
+    """NaN and infinities in gradients of places without a token; in a table's rows that nobody names; in a row, for its own token alone."""
+    N, V, H = 500, 90, 64
+    t = some_tokens(N, V, 1, absent=0.3)
+    grad = rnd((N, H), torch.float32, 2)
+    want = binding.hola_embed_grad(t, grad, V)
+    dirty = grad.clone()
+    dirty[t < 0] = math.nan
+    assert torch.equal(binding.hola_embed_grad(t, dirty, V), want)
+    one = int(t[t >= 0][7])
+    dirty[t == one] = math.inf
+    got = binding.hola_embed_grad(t, dirty, V)
+    assert (got[one] == math.inf).all()
+    got[one] = want[one]
+    assert torch.equal(got, want)
+    table = rnd((V, H), torch.float32, 3)
+    clean = binding.hola_embed(t, table, 2.0)
+    table[[v for v in range(V) if v not in set(t.tolist())]] = math.nan
+    assert torch.equal(binding.hola_embed(t, table, 2.0), clean)
+
+
+@gpu
+def test_the_most_tokens_of_a_call():
+    """2^25 of them, whole numbers: every sum is exact."""
+    N, V, H = 2 ** 25, 1000, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    t = torch.randint(-1, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    t[N - 5:] = 7
+    grad = torch.randint(-1, 2, (N, H), generator=g, device="cuda", dtype=torch.int8).bfloat16()
+    want = torch.zeros((V + 1, H), dtype=torch.float64, device="cuda")
+    for a in range(0, N, 1 << 22):
+        want.index_add_(0, t[a:a + (1 << 22)].long() + 1, grad[a:a + (1 << 22)].double())
+    assert torch.equal(binding.hola_embed_grad(t, grad, V).double(), want[1:])
+    with pytest.raises(binding.HolaError):
+        binding.hola_embed_grad(torch.zeros(N + 1, dtype=torch.int32, device="cuda"), grad[:1].expand(N + 1, H), V)

@@ -4,10 +4,10 @@
 // Selection.  Candidate (w, v) of a sequence has c = (score[w] - logZ[w]) + l[w][v] and the key c * weight[w], both in 64 bits; the n
 // first in the order (key descending, beam ascending, logit descending, id ascending) are kept.  One pass over the logits in 32 bits:
 // a = fma(l, weight, b), b = (score - logZ) weight rounded, is within 2^-24 (|a| + |b|) of the key.  A cluster of CTAs takes a sequence,
-// every CTA a part of each row; a thread keeps the largest a of its groups, the group, and the largest of its other groups.  Every
+// every CTA a part of each row; a thread keeps the two largest a of its groups, those groups, and the largest of its other groups.  Every
 // eight threads put the best of theirs on a board of 32 (every four on one of 64, for more than twenty candidates); let the n-th best
 // there be w.  At least n candidates have a >= w, so each of the part's n best has a >= w - 2^-22 (|w| + max |b|): twice the bound
-// above for either side, and the roundings of this line.  Only threads whose own largest is that large hold such entries; their groups are read again, out of the L2,
+// above for either side, and the roundings of this line.  Only threads whose own largest is that large hold such entries; their two groups (all of theirs, where a third is as large) are read again, out of the L2,
 // and what qualifies is placed, by keys in 64 bits, by counting those before it.  The n best go to the sequence's first CTA in their
 // order, which merges the parts' lists.
 
@@ -199,12 +199,14 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
 
     // The pass, all rows' rounds one after the other: kBsAhead of them on the way.  (A thread without a group in a round takes the
     // part's last one again and sets it aside: no lane waits for another's load.)
-    float m = -CUDART_INF_F, second = -CUDART_INF_F;
-    int at = 0;                                          // round of the largest; from s.rounds on: an edge
+    float m = -CUDART_INF_F, second = -CUDART_INF_F, third = -CUDART_INF_F;
+    int at = 0, at_second = 0;                           // rounds of the two largest; s.rounds: an edge
     const int rounds = s.rounds;
     auto take = [&](float top, float w32, float b, bool have, int beam, int where) {
       if (!(top < CUDART_INF_F)) atomicOr(&s.bad_here, 1u << beam);
       const float a = have ? bs_approx(top, w32, b) : -CUDART_INF_F;
+      third = fmaxf(third, fminf(a, second));
+      if (a > second) at_second = a > m ? at : where;
       second = fmaxf(second, fminf(a, m));
       if (a > m) at = where;
       m = fmaxf(m, a);
@@ -277,17 +279,21 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
         const float w = lp_value(static_cast<uint32_t>(lim >> 32));
         thr = w - (2.384185791015625e-7f * (fabsf(w) + s.b_max) + 1e-37f);
       }
-      const bool mine = m > -CUDART_INF_F && m >= thr, again = mine && second >= thr && second > -CUDART_INF_F;
+      const bool mine = m > -CUDART_INF_F && m >= thr, again = mine && third >= thr && third > -CUDART_INF_F;
       if (mine && !again) {
-        int li = tid >> 1, j = my_edge;
-        if (at < rounds) {
-          for (li = 0; at >= s.rows[li].rounds; ++li) at -= s.rows[li].rounds;
-          j = s.rows[li].begin + at * kBsThreads + tid;
+        const int groups = second > -CUDART_INF_F && second >= thr ? 2 : 1;
+#pragma unroll 1
+        for (int q = 0; q < groups; ++q) {
+          int li = tid >> 1, j = my_edge, t = q ? at_second : at;
+          if (t < rounds) {
+            for (li = 0; t >= s.rows[li].rounds; ++li) t -= s.rows[li].rounds;
+            j = s.rows[li].begin + t * kBsThreads + tid;
+          }
+          bs_note<T>(s, li, p.V, j, thr);
         }
-        bs_note<T>(s, li, p.V, j, thr);
       }
       if (again && my_edge >= 0) bs_note<T>(s, tid >> 1, p.V, my_edge, thr);
-      // threads with more than one such group: all of theirs, dealt out to the warp's lanes
+      // (seldom) threads with more than two such groups: all of theirs, dealt out to the warp's lanes
       const unsigned look = __ballot_sync(0xffffffffu, again);
       if (look) {
         if (again) s.looked_at[warp][__popc(look & ((1u << lane) - 1u))] = static_cast<uint8_t>(lane);

@@ -197,7 +197,10 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (mixed) words = words && in_words(p.mix.W16, 0, 1, 16) && in_words(p.mix.W8, 0, 1, 8) && in_words(p.mix.W4, 0, 1, 4);
   else words = words && in_words(a->table, a->row_stride, te, 8 * te);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, dev->sms, stream)
+  const bool wide = words && a->H % 16 == 0 && oe == 2 && !mixed && te <= 2 && in_words(a->out, a->out_stride, oe, 32) &&
+                    (!a->add || in_words(a->add, a->add_stride, oe, 32)) && in_words(a->table, a->row_stride, te, 16 * te);
+  const cudaError_t e = wide ? launch_embed_16(p, a->t_dtype, a->out_dtype, dev->sms, stream)
+                        : words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, dev->sms, stream)
                               : launch_embed_of<1>(p, a->t_dtype, a->out_dtype, dev->sms, stream);
   return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }

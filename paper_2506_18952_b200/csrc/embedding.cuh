@@ -2,7 +2,7 @@
 
 // ------------------------------------------------------------------------------------------------ lookup
 // out[r] = add[r] + scale * W[tok[r]], every operation one rounding in fp32 (the scale of a quantised row first), the result rounded
-// once more where it is stored in 16 bits.  A thread takes 8 neighbouring channels of some rows.
+// once more where it is stored in 16 bits.
 constexpr int kEmThreads = 128;
 
 // Types of rows in memory (hola_t_dtype).
@@ -92,10 +92,11 @@ __device__ __forceinline__ void em_store(void* p, const float* x) {
     }
     return;
   }
-  if (n == 8) {
-    uint32_t h[4];
+  if (n >= 8) {
+    constexpr int kPairs = n / 2 < 4 ? 4 : n / 2;
+    uint32_t h[kPairs];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kPairs; ++i) {
       const float a = x[(2 * i) % n], b = x[(2 * i + 1) % n];
       if (kType == kTabBf16) {
         const __nv_bfloat162 y = __floats2bfloat162_rn(a, b);
@@ -105,7 +106,11 @@ __device__ __forceinline__ void em_store(void* p, const float* x) {
         h[i] = *reinterpret_cast<const uint32_t*>(&y);
       }
     }
-    *static_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
+    if (n == 16)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(p), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]), "r"(h[4 % kPairs]), "r"(h[5 % kPairs]), "r"(h[6 % kPairs]), "r"(h[7 % kPairs])
+                   : "memory");
+    else *static_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
   } else {
     *static_cast<uint16_t*>(p) = kType == kTabBf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x[0])) : __half_as_ushort(__float2half_rn(x[0]));
   }
@@ -159,18 +164,18 @@ __device__ __forceinline__ void em_mixed(const hola_wmix& mix, int H, int v, int
   }
 }
 
-// n: channels that a thread takes at once, 8 where everything is aligned; kWide: results of 32 bits, else of 16 (`f16`: which).  A CTA takes
-// kRows rows at a time, or as many times that as leave no thread idle where rows are short (`lanes`: threads of a row, a power of two).
-// Bound by HBM: rows in, rows out.  us with 128 / 256 threads: 16384 x 4096 bf16 33.2 / 35.6, 20000 x 4096 int8 41 / 47; rows one by one
-// instead of four at a time: 2304 x 4096 int8 18.3 -> 13.1.
-template <int kType>
-__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed ? 2 : 4; }       // rows on the way together
+// n: channels that a thread takes at once, 8 where everything is aligned, 16 where rows of 8 or 16 bits become results of 16; kWide: results
+// of 32 bits, else of 16 (`f16`: which).  A CTA takes kRows rows at a time, or as many times that as leave no thread idle where rows are
+// short (`lanes`: threads of a row, a power of two).  Bound by HBM: rows in, rows out.  us: 128 / 256 threads 16384 x 4096 bf16 33.2 /
+// 35.6; 8 / 16 channels 33.1 / 31.8, 20000 x 4096 int8 41 / 34; rows one by one instead of four at a time 2304 x 4096 int8 18.3 -> 13.1.
+template <int kType, int n>
+__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed || (n == 16 && kType != kTabInt8) ? 2 : 4; }       // rows on the way together
 
 // kShort: several rows side by side in a CTA (addresses that all threads share are cheaper: 16384 x 4096 bf16 36.2 -> 33.2 us).
 template <int kType, bool kWide, bool kAdd, bool kShort, int n>
 __global__ void __launch_bounds__(kEmThreads, 8) embed_kernel(const __grid_constant__ EmParams p, int f16, int some_rows, int lanes_log2) {
   constexpr bool kCodes = kType == kTabInt8 || kType == kTabMixed, kMixed = kType == kTabMixed;
-  constexpr int kWord = kMixed ? kTabBf16 : kType, kRows = em_rows<kType>(), kOut = kWide ? kTabF32 : kTabBf16;
+  constexpr int kWord = kMixed ? kTabBf16 : kType, kRows = em_rows<kType, n>(), kOut = kWide ? kTabF32 : kTabBf16;
   constexpr int kWords = n == 1 ? 4 : 1;                 // words of a row that a thread has on the way
   grid_dependency_wait();
   grid_dependency_release();
@@ -266,7 +271,7 @@ cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStrea
   const long long slices = (p.H + lanes * kAtOnce - 1) / (lanes * kAtOnce);
   const int slots = kEmThreads / lanes;
   // several rows at a time where there are CTAs enough all the same
-  const int rows = p.N * slices >= 2ll * em_rows<kType>() * slots * num_sms ? em_rows<kType>() : 1;
+  const int rows = p.N * slices >= 2ll * em_rows<kType, n>() * slots * num_sms ? em_rows<kType, n>() : 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((p.N + rows * slots - 1) / (rows * slots)), static_cast<unsigned>(slices > 65535 ? 65535 : slices));
   cfg.blockDim = dim3(kEmThreads); cfg.stream = stream;
@@ -283,6 +288,12 @@ cudaError_t launch_embed_as(const EmParams& p, int out_type, int num_sms, cudaSt
   if (out_type == kTabF32)
     return p.add ? launch_embed<kType, true, true, n>(p, out_type, num_sms, stream) : launch_embed<kType, true, false, n>(p, out_type, num_sms, stream);
   return p.add ? launch_embed<kType, false, true, n>(p, out_type, num_sms, stream) : launch_embed<kType, false, false, n>(p, out_type, num_sms, stream);
+}
+// Sixteen channels at once: results of 16 bits from rows of 8 or 16.
+cudaError_t launch_embed_16(const EmParams& p, int type, int out_type, int num_sms, cudaStream_t stream) {
+  if (type == kTabInt8) return p.add ? launch_embed<kTabInt8, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabInt8, false, false, 16>(p, out_type, num_sms, stream);
+  if (type == kTabBf16) return p.add ? launch_embed<kTabBf16, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabBf16, false, false, 16>(p, out_type, num_sms, stream);
+  return p.add ? launch_embed<kTabF16, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabF16, false, false, 16>(p, out_type, num_sms, stream);
 }
 template <int n>
 cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_sms, cudaStream_t stream) {

@@ -87,12 +87,14 @@ __device__ __forceinline__ void em_store(void* p, const float* x) {
       asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                    ::"l"(p), "f"(x[0]), "f"(x[1 % n]), "f"(x[2 % n]), "f"(x[3 % n]), "f"(x[4 % n]), "f"(x[5 % n]), "f"(x[6 % n]), "f"(x[7 % n])
                    : "memory");
+    } else if (n == 4) {
+      *static_cast<float4*>(p) = make_float4(x[0], x[1 % n], x[2 % n], x[3 % n]);
     } else {
       *static_cast<float*>(p) = x[0];
     }
     return;
   }
-  if (n >= 8) {
+  if (n >= 4) {
     constexpr int kPairs = n / 2 < 4 ? 4 : n / 2;
     uint32_t h[kPairs];
 #pragma unroll
@@ -110,7 +112,8 @@ __device__ __forceinline__ void em_store(void* p, const float* x) {
       asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                    ::"l"(p), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]), "r"(h[4 % kPairs]), "r"(h[5 % kPairs]), "r"(h[6 % kPairs]), "r"(h[7 % kPairs])
                    : "memory");
-    else *static_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
+    else if (n == 8) *static_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
+    else *static_cast<uint2*>(p) = make_uint2(h[0], h[1]);
   } else {
     *static_cast<uint16_t*>(p) = kType == kTabBf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x[0])) : __half_as_ushort(__float2half_rn(x[0]));
   }
@@ -329,7 +332,7 @@ constexpr int kEgThreads = 128, kEgEach = 8;
 constexpr int kEgSlice = kEgThreads * kEgEach;
 constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
 constexpr int kEgRanges = 2 * kEgThreads;        // ranges of ids whose distinct ones are added up beforehand
-constexpr int kEgAhead = 8;            // rows of a thread on the way
+constexpr int kEgAhead = 8;            // rows of a thread on the way (those that start anywhere)
 constexpr long long kEgMaxTokens = 1 << 25;      // what is left of a list's words for places in the stretch of one of 16 warps
 constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspace has to be known without a device)
 
@@ -568,60 +571,42 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   put_list();
 }
 
-// Eight channels of a thread: side by side (kVec), or kEgThreads apart where rows start anywhere.
-template <bool kVec>
+// Eight channels of a thread, in runs that lie side by side: of 16 bytes of the gradient, or single ones where rows start anywhere.
+template <int kRun>
 __device__ __forceinline__ int eg_channel(int slice, int i) {
-  return slice * kEgSlice + (kVec ? static_cast<int>(threadIdx.x) * kEgEach + i : static_cast<int>(threadIdx.x) + i * kEgThreads);
+  return slice * kEgSlice + (i / kRun) * (kEgThreads * kRun) + static_cast<int>(threadIdx.x) * kRun + i % kRun;
 }
-template <int kType, bool kVec>
-struct EgRow {
-  EmWord<kType, kVec ? kEgEach : 1> w[kVec ? 1 : kEgEach];
-  __device__ __forceinline__ void load(const EgParams& p, int row, int slice) {
-    const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row) * p.g_stride * tab_bytes(kType);
-#pragma unroll
-    for (int i = 0; i < (kVec ? 1 : kEgEach); ++i) {
-      const int h = eg_channel<kVec>(slice, i);
-      if (h < p.H) w[i].load(at + static_cast<long long>(h) * tab_bytes(kType));
-    }
-  }
-  __device__ __forceinline__ float get(int i) const { return kVec ? w[0].get(i) : w[kVec ? 0 : i].get(0); }
-};
+template <int kType>
+using EgWord = EmWord<kType, kEgEach>;
+// Rows of a thread in the ring: 24 KB of a CTA.
+template <int kType>
+__host__ __device__ constexpr int eg_stages() { return 24 * 1024 / (kEgThreads * kEgEach * tab_bytes(kType)); }
 
-template <bool kVec>
+template <int kRun>
 __device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long long row, int slice, const float* sum) {
-  float x[kEgEach];
 #pragma unroll
-  for (int i = 0; i < kEgEach; ++i) x[i] = __fmul_rn(sum[i], p.scale);
-  if (kVec) {
-    const int h = eg_channel<true>(slice, 0);
-    if (h >= p.H) return;
+  for (int i = 0; i < kEgEach; i += kRun) {
+    const int h = eg_channel<kRun>(slice, i);
+    if (h >= p.H) continue;
     const long long at = row * p.out_stride + h;
+    float x[kRun];
+#pragma unroll
+    for (int c = 0; c < kRun; ++c) x[c] = __fmul_rn(sum[i + c], p.scale);
     if (p.accumulate) {
-      float a[kEgEach];
-      em_load_as<kEgEach>(out_type, p.out, at, a);
+      float a[kRun];
+      em_load_as<kRun>(out_type, p.out, at, a);
 #pragma unroll
-      for (int i = 0; i < kEgEach; ++i) x[i] = __fadd_rn(a[i], x[i]);
+      for (int c = 0; c < kRun; ++c) x[c] = __fadd_rn(a[c], x[c]);
     }
-    em_store_as<kEgEach>(out_type, p.out, at, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kEgEach; ++i) {
-      const int h = eg_channel<false>(slice, i);
-      if (h >= p.H) continue;
-      const long long at = row * p.out_stride + h;
-      float a[1] = {0.f};
-      if (p.accumulate) em_load_as<1>(out_type, p.out, at, a);
-      a[0] = __fadd_rn(a[0], x[i]);
-      em_store_as<1>(out_type, p.out, at, a);
-    }
+    em_store_as<kRun>(out_type, p.out, at, x);
   }
 }
 
 template <int kType, bool kVec>
-__global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
-  // for the places of the pieces that begin in the window: rows of the gradient, and whether a piece ends there
-  __shared__ __align__(16) int rows[kEgMaxWindow + kEgMaxPiece + kEgAhead];
-  __shared__ __align__(16) uint8_t piece_ends[kEgMaxWindow + kEgMaxPiece + kEgAhead];
+__global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
+  constexpr int kRun = kVec ? 16 / tab_bytes(kType) : 1;
+  __shared__ __align__(16) unsigned char eg_ring[kVec ? eg_stages<kType>() * kEgThreads * kEgEach * tab_bytes(kType) : 16];
+  __shared__ int rows[kEgMaxWindow + kEgMaxPiece];       // of the gradient, by place from x0 on; complemented where a piece ends
   __shared__ int4 spots[kEgMaxWindow];
   __shared__ int firsts[kEgMaxWindow + 1], out_rows[kEgMaxWindow];
   __shared__ int part_sum[kEgThreads / 32], range_rows[kEgRanges];
@@ -637,7 +622,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     if (tid <= n) firsts[tid] = p.first[v0 + tid];
     __syncthreads();
     for (int i = 0; i < n; ++i)
-      if (firsts[i] == firsts[i + 1]) eg_write<kVec>(p, out_type, v0 + i, slice, zero);
+      if (firsts[i] == firsts[i + 1]) eg_write<kRun>(p, out_type, v0 + i, slice, zero);
     return;
   }
   // (behind the last valid place there is something to read, which is not used)
@@ -691,27 +676,41 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   for (int i = tid; i < x1 - x0; i += kEgThreads) {
     // (places behind the window belong to the last piece)
     bool ends = x0 + i + 1 == x1;
+    int row;
     if (x0 + i < w1) {
       const int4 here = spots[x0 + i - w0];
-      rows[i] = here.x;
+      row = here.x;
       ends = x0 + i + 1 == here.w || ((x0 + i + 1 - here.z) & before_S) == 0;
     } else {
-      rows[i] = p.places[x0 + i].x;
+      row = p.places[x0 + i].x;
     }
-    piece_ends[i] = ends ? 1 : 0;
+    rows[i] = ends ? ~row : row;
   }
   __syncthreads();
 
-  // (the first rows are on their way while the rows of the result are looked up)
-  EgRow<kType, kVec> g[kEgAhead];
-  auto load = [&](int x) {
-    const int4 some = *reinterpret_cast<const int4*>(rows + (x - x0)), more = *reinterpret_cast<const int4*>(rows + (x - x0) + 4);
-    const int at[kEgAhead] = {some.x, some.y, some.z, some.w, more.x, more.y, more.z, more.w};
+  // The first rows are on their way while the rows of the result are looked up.  Aligned ones: through a ring in shared memory, of which a
+  // thread reads what it has copied itself.
+  constexpr int kWords = kEgEach / kRun;                 // 16-byte words of a row that a thread takes
+  const uint32_t ring = kVec ? static_cast<uint32_t>(__cvta_generic_to_shared(eg_ring)) + tid * 16 : 0;
+  auto copy = [&](int x, int slot) {                     // the row at place x, into a slot of the ring
+    if (x < x1) {
+      const int row = rows[x - x0];
+      const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row < 0 ? ~row : row) * p.g_stride * tab_bytes(kType);
 #pragma unroll
-    for (int u = 0; u < kEgAhead; ++u)
-      if (x + u < x1) g[u].load(p, at[u], slice);
+      for (int i = 0; i < kWords; ++i) {
+        const int h = eg_channel<kRun>(slice, i * kRun);
+        if (h < p.H)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                       ::"r"(ring + (slot * kWords + i) * kEgThreads * 16), "l"(at + static_cast<long long>(h) * tab_bytes(kType)) : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (kVec) load(x0);
+  constexpr int kStages = eg_stages<kType>();
+  if (kVec) {
+#pragma unroll 1
+    for (int s = 0; s < kStages - 1; ++s) copy(x0 + s, s);
+  }
   if (tid < w1 - w0) {
     int row = spot.y;
     if (p.by_rows) {
@@ -725,35 +724,26 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   __syncthreads();
 
   float sum[kEgEach] = {};
-#pragma unroll 1
-  for (int x = x0; x < x1; x += kEgAhead) {
-    if (!kVec || x > x0) load(x);
-    const int n = min(kEgAhead, x1 - x);
-    const uint64_t last = *reinterpret_cast<const uint64_t*>(piece_ends + (x - x0));
+  // The piece that ends at place x: written, or put with the token's other ones.
+  auto finish = [&](int x) {
+    const int k = min(x, w1 - 1) - w0, begin = spots[k].z, end = spots[k].w;
+    bool whole = true;
+    if (end - begin > p.S) {
+      const int from = begin + ((x - begin) & ~before_S);
+      const long long width = static_cast<long long>(p.slices) * kEgSlice;
+      float* mine = p.partial + (2ll * (from >> p.S_log2) + (from == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
 #pragma unroll
-    for (int u = 0; u < kEgAhead; ++u) {
-      if (u >= n) break;
-#pragma unroll
-      for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u].get(i));
-      if (!(last >> (8 * u) & 1u)) continue;
-      const int k = min(x + u, w1 - 1) - w0, begin = spots[k].z, end = spots[k].w;
-      if (end - begin > p.S) {
-        // One of several pieces.
-        const int from = begin + ((x + u - begin) & ~before_S);
-        const long long width = static_cast<long long>(p.slices) * kEgSlice;
-        float* mine = p.partial + (2ll * (from >> p.S_log2) + (from == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
-#pragma unroll
-        for (int i = 0; i < kEgEach; ++i) { mine[i * kEgThreads] = sum[i]; sum[i] = 0.f; }
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-          const unsigned n = static_cast<unsigned>((end - begin + before_S) >> p.S_log2);
-          last_here = atomicAdd(&p.done[static_cast<long long>(begin >> p.S_log2) * p.slices + slice], 1u) == n - 1 ? 1 : 0;
-        }
-        __syncthreads();
-        const bool all_there = last_here != 0;
-        __syncthreads();
-        if (!all_there) continue;
+      for (int i = 0; i < kEgEach; ++i) { mine[i * kEgThreads] = sum[i]; sum[i] = 0.f; }
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const unsigned n = static_cast<unsigned>((end - begin + before_S) >> p.S_log2);
+        last_here = atomicAdd(&p.done[static_cast<long long>(begin >> p.S_log2) * p.slices + slice], 1u) == n - 1 ? 1 : 0;
+      }
+      __syncthreads();
+      whole = last_here != 0;
+      __syncthreads();
+      if (whole) {
         __threadfence();
 #pragma unroll 4
         for (int b = begin; b < end; b += p.S) {
@@ -762,10 +752,55 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
           for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], __ldcg(y + i * kEgThreads));
         }
       }
-      if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(spots[k].y + p.v_offset);
-      eg_write<kVec>(p, out_type, out_rows[k], slice, sum);
+    }
+    if (!whole) return;
+    if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(spots[k].y + p.v_offset);
+    eg_write<kRun>(p, out_type, out_rows[k], slice, sum);
 #pragma unroll
-      for (int i = 0; i < kEgEach; ++i) sum[i] = 0.f;
+    for (int i = 0; i < kEgEach; ++i) sum[i] = 0.f;
+  };
+  if (kVec) {
+    int slot = 0, before = kStages - 1;                  // of place x, and of the one before it, which is free
+#pragma unroll 1
+    for (int x = x0; x < x1; ++x) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      EgWord<kType> g;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        const uint4 y = *reinterpret_cast<const uint4*>(eg_ring + ((slot * kWords + i) * kEgThreads + tid) * 16);
+        g.w[4 * i] = y.x; g.w[4 * i + 1] = y.y; g.w[4 * i + 2] = y.z; g.w[4 * i + 3] = y.w;
+      }
+      const bool ends = rows[x - x0] < 0;
+      copy(x + kStages - 1, before);
+      before = slot;
+      slot = slot + 1 == kStages ? 0 : slot + 1;
+#pragma unroll
+      for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g.get(i));
+      if (ends) finish(x);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+#pragma unroll 1
+    for (int x = x0; x < x1; x += kEgAhead) {
+      EmWord<kType, 1> g[kEgAhead][kEgEach];
+      int row[kEgAhead];
+#pragma unroll
+      for (int u = 0; u < kEgAhead; ++u) {
+        row[u] = x + u < x1 ? rows[x + u - x0] : 0;
+        const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride * tab_bytes(kType);
+#pragma unroll
+        for (int i = 0; i < kEgEach; ++i) {
+          const int h = eg_channel<1>(slice, i);
+          if (x + u < x1 && h < p.H) g[u][i].load(at + static_cast<long long>(h) * tab_bytes(kType));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kEgAhead; ++u) {
+        if (x + u >= x1) break;
+#pragma unroll
+        for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u][i].get(0));
+        if (row[u] < 0) finish(x + u);
+      }
     }
   }
 }
@@ -844,11 +879,11 @@ cudaError_t configure_sort() {
   const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel<Cell, int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsMaxShared);
   return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_sort_kernel<Cell, int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEsMaxShared);
 }
-// The sums' loads on the way need room in the L1: without a preference the SMs stay as the sort, which takes nearly all of them for shared memory, has
-// left them (16384 rows of 4096 81.4 -> 70.6 us, 32768 Zipf tokens 108 -> 92).
+// What the sums have on the way is in shared memory, as many CTAs of it as there is room for; where rows start anywhere, in the L1, which
+// the sort has left next to nothing of (16384 aligned rows that way: 81.4 us, 70.6 with room for them).
 template <int kType>
 cudaError_t configure_sums() {
-  const cudaError_t e = cudaFuncSetAttribute(embed_grad_kernel<kType, true>, cudaFuncAttributePreferredSharedMemoryCarveout, 25);
+  const cudaError_t e = cudaFuncSetAttribute(embed_grad_kernel<kType, true>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
   return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_grad_kernel<kType, false>, cudaFuncAttributePreferredSharedMemoryCarveout, 25);
 }
 cudaError_t configure_embedding() {

@@ -191,6 +191,10 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   p.V_global = a->V_global ? a->V_global : a->V;
   p.table = a->table; p.row_stride = a->row_stride; p.w_scale = a->w_scale;
   if (mixed) p.mix = *a->wmix;
+  auto end = [&](const void* base, long long rows, long long stride, int elem) {
+    return base ? static_cast<const unsigned char*>(base) + ((rows - 1) * stride + a->H) * elem : nullptr;
+  };
+  p.table_end = end(a->table, a->V, a->row_stride, te); p.add_end = end(a->add, a->N, a->add_stride, oe);
   p.scale = a->scale; p.add = a->add; p.add_stride = a->add_stride; p.out = a->out; p.out_stride = a->out_stride; p.status = a->status_word;
   // (eight channels at a time: 8, 16 or 32 bytes)
   bool words = a->H % 8 == 0 && in_words(a->out, a->out_stride, oe, 8 * oe) && (!a->add || in_words(a->add, a->add_stride, oe, 8 * oe));
@@ -200,8 +204,7 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   const bool wide = words && a->H % 16 == 0 && oe == 2 && !mixed && te <= 2 && in_words(a->out, a->out_stride, oe, 32) &&
                     (!a->add || in_words(a->add, a->add_stride, oe, 32)) && in_words(a->table, a->row_stride, te, 16 * te);
   const cudaError_t e = wide ? launch_embed_16(p, a->t_dtype, a->out_dtype, dev->sms, stream)
-                        : words ? launch_embed_of<8>(p, a->t_dtype, a->out_dtype, dev->sms, stream)
-                              : launch_embed_of<1>(p, a->t_dtype, a->out_dtype, dev->sms, stream);
+                             : launch_embed_of(p, a->t_dtype, a->out_dtype, words, dev->sms, stream);
   return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }
 
@@ -234,7 +237,9 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
   if (!device_facts()) return HOLA_ERR_NO_DEVICE;
   p.tokens = a->tokens; p.wide = a->wide_tokens; p.v_offset = a->v_offset;
   p.V_global = a->V_global ? a->V_global : a->V;
-  p.grad = a->grad; p.g_stride = a->grad_stride; p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;
+  p.grad = a->grad; p.g_stride = a->grad_stride;
+  p.grad_end = static_cast<const unsigned char*>(a->grad) + (a->N > 0 ? ((a->N - 1) * a->grad_stride + a->H) * ge : 0);
+  p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;
   p.accumulate = a->accumulate; p.by_rows = by_rows; p.ids_out = a->ids_out; p.count_out = a->count_out; p.status = a->status_word;
   unsigned char* ws = static_cast<unsigned char*>(a->workspace);
   p.places = reinterpret_cast<int4*>(ws + l.places); p.numbers = reinterpret_cast<int2*>(ws + l.numbers);

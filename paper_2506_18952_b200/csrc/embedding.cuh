@@ -15,7 +15,7 @@ struct EmParams {
   long long N;
   int V, H;
   long long v_offset, V_global;
-  const void* table;
+  const void *table, *table_end, *add_end;      // (ends of what may be read)
   long long row_stride;                // channels
   const float* w_scale;
   hola_wmix mix;
@@ -141,6 +141,57 @@ __device__ __forceinline__ void em_load_as(int type, const void* base, long long
     for (int i = 0; i < n; ++i) x[i] = type == kTabBf16 ? w.get(i) : f.get(i);
   }
 }
+
+// Eight channels from any address: the aligned 16 bytes that hold them, on their way, and shifted into place later.  What else these hold is of
+// the same tensor; at its ends, where it would not be, channel by channel.
+template <int kType>
+struct EmRaw {
+  static constexpr int kSize = tab_bytes(kType), kNeed = 8 * kSize, kGranules = (kNeed + 15) / 16 + 1;
+  uint32_t w[4 * kGranules];
+  unsigned shift;
+  // Channels h .. h + 7 of a row of H (those outside it are not used) of a tensor from begin to end.
+  __device__ __forceinline__ void load(const void* begin, const void* end, long long row, int h, int H) {
+    const unsigned char* at = static_cast<const unsigned char*>(begin) + (row + h) * kSize;
+    shift = static_cast<unsigned>(reinterpret_cast<uintptr_t>(at) & 15u);
+    const unsigned char* first = at - shift;
+    const int granules = static_cast<int>(shift + kNeed + 15) / 16;
+    if (first >= static_cast<const unsigned char*>(begin) && first + 16 * granules <= static_cast<const unsigned char*>(end)) {
+#pragma unroll
+      for (int i = 0; i < kGranules; ++i)
+        if (i < granules) {
+          const uint4 y = *reinterpret_cast<const uint4*>(first + 16 * i);
+          w[4 * i] = y.x; w[4 * i + 1] = y.y; w[4 * i + 2] = y.z; w[4 * i + 3] = y.w;
+        }
+    } else {
+      ragged(at, h, H);
+    }
+  }
+  __device__ __forceinline__ void ragged(const unsigned char* at, int h, int H) {
+    uint32_t y[kNeed / 4];
+#pragma unroll
+    for (int i = 0; i < kNeed / 4; ++i) y[i] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (h + e >= 0 && h + e < H) {
+        if (kSize == 4) y[e * kSize / 4] = *reinterpret_cast<const uint32_t*>(at + e * kSize);
+        else if (kSize == 2) y[e * kSize / 4] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(at + e * kSize)) << (16 * (e & 1));
+        else y[e * kSize / 4] |= static_cast<uint32_t>(at[e]) << (8 * (e & 3));
+      }
+#pragma unroll
+    for (int i = 0; i < kNeed / 4; ++i) w[i] = y[i];
+    shift = 0;
+  }
+  __device__ __forceinline__ EmWord<kType, 8> get() {
+#pragma unroll
+    for (int i = 0; i + 1 < 4 * kGranules; ++i) w[i] = shift & 4u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i + 2 < 4 * kGranules; ++i) w[i] = shift & 8u ? w[i + 2] : w[i];
+    EmWord<kType, 8> x;
+#pragma unroll
+    for (int i = 0; i < kNeed / 4; ++i) x.w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (shift & 3u));
+    return x;
+  }
+};
 
 // n channels of a row of a mixed-width head: group of 256 rows -> its width and its place among the rows of that width.
 template <int n>
@@ -286,6 +337,107 @@ cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStrea
   if (n == 1 || lanes < kEmThreads) return cudaLaunchKernelEx(&cfg, embed_kernel<kType, kWide, kAdd, true, n>, p, f16, rows, log2);
   return cudaLaunchKernelEx(&cfg, embed_kernel<kType, kWide, kAdd, n == 1, n>, p, f16, rows, log2);
 }
+// The same where rows start anywhere: a thread takes 8 channels that lie side by side on an aligned address of the result (or, at a row's ends,
+// what there is of them), out of the aligned words that hold them in the table.  us, channel by channel / so: 3000 x 4097 bf16 18.7 / 12.7,
+// 5000 x 1001 8.6 / 6.0.
+template <int kType, bool kWide, bool kAdd>
+__global__ void __launch_bounds__(kEmThreads, 8) embed_any_kernel(const __grid_constant__ EmParams p, int f16, int lanes_log2) {
+  constexpr int kRows = kType == kTabF32 || kAdd ? 1 : 2, kOut = kWide ? kTabF32 : kTabBf16, kOutSize = tab_bytes(kOut);
+  grid_dependency_wait();
+  grid_dependency_release();
+  const int lanes = 1 << lanes_log2, lane = static_cast<int>(threadIdx.x) & (lanes - 1);
+  const long long r0 = (static_cast<long long>(blockIdx.x) * (kEmThreads >> lanes_log2) + (threadIdx.x >> lanes_log2)) * kRows;
+  const int rows = static_cast<int>(p.N - r0 < kRows ? p.N - r0 : kRows);
+  int v[kRows], lead[kRows];                             // lead: channels ahead of the first aligned address of the result
+  float ws[kRows];
+  bool any_bad = false;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    v[i] = -1;
+    ws[i] = 1.f;
+    lead[i] = 0;
+    if (i < rows) {
+      bool bad;
+      v[i] = em_row(p.tokens, p.wide, r0 + i, p.V, p.v_offset, p.V_global, &bad);
+      any_bad = any_bad || bad;
+      if (kType == kTabInt8 && v[i] >= 0) ws[i] = p.w_scale[v[i]];
+      lead[i] = static_cast<int>((0 - (reinterpret_cast<uintptr_t>(p.out) + static_cast<uintptr_t>((r0 + i) * p.out_stride) * kOutSize)) & (8 * kOutSize - 1)) / kOutSize;
+    }
+  }
+  if (any_bad && p.status && lane == 0 && blockIdx.y == 0) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+#pragma unroll 1
+  for (int c = static_cast<int>(blockIdx.y) * lanes + lane; 8 * (c - 1) < p.H; c += static_cast<int>(gridDim.y) * lanes) {
+    EmRaw<kType> w[kRows];
+    EmRaw<kOut> add[kAdd ? kRows : 1];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int h = lead[i] + 8 * (c - 1);
+      if (h <= -8 || h >= p.H) continue;
+      if (v[i] >= 0) w[i].load(p.table, p.table_end, v[i] * p.row_stride, h, p.H);
+      if (kAdd && i < rows) add[kAdd ? i : 0].load(p.add, p.add_end, (r0 + i) * p.add_stride, h, p.H);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int h = lead[i] + 8 * (c - 1);
+      if (i >= rows || h <= -8 || h >= p.H) continue;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = 0.f;
+      if (v[i] >= 0) {
+        const EmWord<kType, 8> x = w[i].get();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] = x.get(e);
+          if (kType == kTabInt8) y[e] = __fmul_rn(y[e], ws[i]);
+          y[e] = __fmul_rn(y[e], p.scale);
+        }
+      }
+      if (kAdd) {
+        const EmWord<kOut, 8> a = add[kAdd ? i : 0].get();
+        EmWord<kTabF16, 8> b;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b.w[k] = a.w[k];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __fadd_rn(!kWide && f16 ? b.get(e) : a.get(e), y[e]);
+      }
+      unsigned char* to = static_cast<unsigned char*>(p.out) + ((r0 + i) * p.out_stride + h) * kOutSize;
+      if (h >= 0 && h + 8 <= p.H) {
+        if (!kWide && f16) em_store<kTabF16, 8>(to, y);
+        else em_store<kOut, 8>(to, y);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (h + e >= 0 && h + e < p.H) {
+            if (!kWide && f16) em_store<kTabF16, 1>(to + e * kOutSize, y + e);
+            else em_store<kOut, 1>(to + e * kOutSize, y + e);
+          }
+      }
+    }
+  }
+}
+
+template <int kType, bool kWide, bool kAdd>
+cudaError_t launch_embed_any(const EmParams& p, int out_type, cudaStream_t stream) {
+  constexpr int kRows = kType == kTabF32 || kAdd ? 1 : 2;
+  const int chunks = static_cast<int>((static_cast<long long>(p.H) + 15) / 8);
+  int log2 = 0;
+  while ((1 << log2) < kEmThreads && 1 << log2 < chunks) ++log2;
+  const int lanes = 1 << log2, slots = kEmThreads / lanes * kRows, slices = (chunks + lanes - 1) / lanes;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((p.N + slots - 1) / slots), static_cast<unsigned>(slices > 65535 ? 65535 : slices));
+  cfg.blockDim = dim3(kEmThreads); cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, embed_any_kernel<kType, kWide, kAdd>, p, out_type == kTabF16 ? 1 : 0, log2);
+}
+template <int kType>
+cudaError_t launch_embed_any_of(const EmParams& p, int out_type, cudaStream_t stream) {
+  if (out_type == kTabF32) return p.add ? launch_embed_any<kType, true, true>(p, out_type, stream) : launch_embed_any<kType, true, false>(p, out_type, stream);
+  return p.add ? launch_embed_any<kType, false, true>(p, out_type, stream) : launch_embed_any<kType, false, false>(p, out_type, stream);
+}
+
 template <int kType, int n>
 cudaError_t launch_embed_as(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
   if (out_type == kTabF32)
@@ -298,14 +450,14 @@ cudaError_t launch_embed_16(const EmParams& p, int type, int out_type, int num_s
   if (type == kTabBf16) return p.add ? launch_embed<kTabBf16, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabBf16, false, false, 16>(p, out_type, num_sms, stream);
   return p.add ? launch_embed<kTabF16, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabF16, false, false, 16>(p, out_type, num_sms, stream);
 }
-template <int n>
-cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, int num_sms, cudaStream_t stream) {
+// words: eight channels of every row start on an aligned address.
+cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, bool words, int num_sms, cudaStream_t stream) {
   switch (type) {
-    case kTabF32: return launch_embed_as<kTabF32, n>(p, out_type, num_sms, stream);
-    case kTabBf16: return launch_embed_as<kTabBf16, n>(p, out_type, num_sms, stream);
-    case kTabF16: return launch_embed_as<kTabF16, n>(p, out_type, num_sms, stream);
-    case kTabInt8: return launch_embed_as<kTabInt8, n>(p, out_type, num_sms, stream);
-    default: return launch_embed_as<kTabMixed, n>(p, out_type, num_sms, stream);
+    case kTabF32: return words ? launch_embed_as<kTabF32, 8>(p, out_type, num_sms, stream) : launch_embed_any_of<kTabF32>(p, out_type, stream);
+    case kTabBf16: return words ? launch_embed_as<kTabBf16, 8>(p, out_type, num_sms, stream) : launch_embed_any_of<kTabBf16>(p, out_type, stream);
+    case kTabF16: return words ? launch_embed_as<kTabF16, 8>(p, out_type, num_sms, stream) : launch_embed_any_of<kTabF16>(p, out_type, stream);
+    case kTabInt8: return words ? launch_embed_as<kTabInt8, 8>(p, out_type, num_sms, stream) : launch_embed_any_of<kTabInt8>(p, out_type, stream);
+    default: return words ? launch_embed_as<kTabMixed, 8>(p, out_type, num_sms, stream) : launch_embed_as<kTabMixed, 1>(p, out_type, num_sms, stream);
   }
 }
 
@@ -332,7 +484,7 @@ constexpr int kEgThreads = 128, kEgEach = 8;
 constexpr int kEgSlice = kEgThreads * kEgEach;
 constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
 constexpr int kEgRanges = 2 * kEgThreads;        // ranges of ids whose distinct ones are added up beforehand
-constexpr int kEgAhead = 8;            // rows of a thread on the way (those that start anywhere)
+constexpr int kEgAhead = 6;            // rows of a thread on the way (those that start anywhere)
 constexpr long long kEgMaxTokens = 1 << 25;      // what is left of a list's words for places in the stretch of one of 16 warps
 constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspace has to be known without a device)
 
@@ -344,7 +496,7 @@ struct EgParams {
   int even, buckets, R, warps, chunk, list;      // sort: U, ranges of ids and how many a range holds at most, warps that count, tokens of a warp
                                        // and how many of them it lists
   int S, S_log2, window, slices;
-  const void* grad;
+  const void *grad, *grad_end;
   long long g_stride;
   float scale;
   void* out;
@@ -571,7 +723,7 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   put_list();
 }
 
-// Eight channels of a thread, in runs that lie side by side: of 16 bytes of the gradient, or single ones where rows start anywhere.
+// Eight channels of a thread, in runs that lie side by side: of 16 bytes of the gradient, or all of them where rows start anywhere.
 template <int kRun>
 __device__ __forceinline__ int eg_channel(int slice, int i) {
   return slice * kEgSlice + (i / kRun) * (kEgThreads * kRun) + static_cast<int>(threadIdx.x) * kRun + i % kRun;
@@ -582,29 +734,31 @@ using EgWord = EmWord<kType, kEgEach>;
 template <int kType>
 __host__ __device__ constexpr int eg_stages() { return 24 * 1024 / (kEgThreads * kEgEach * tab_bytes(kType)); }
 
-template <int kRun>
+// The sums, scaled, to a row of the result (added to what is there); kVec: runs are aligned, else channel by channel.
+template <int kRun, bool kVec>
 __device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long long row, int slice, const float* sum) {
+  constexpr int kOnce = kVec ? kRun : 1;
 #pragma unroll
-  for (int i = 0; i < kEgEach; i += kRun) {
+  for (int i = 0; i < kEgEach; i += kOnce) {
     const int h = eg_channel<kRun>(slice, i);
     if (h >= p.H) continue;
     const long long at = row * p.out_stride + h;
-    float x[kRun];
+    float x[kOnce];
 #pragma unroll
-    for (int c = 0; c < kRun; ++c) x[c] = __fmul_rn(sum[i + c], p.scale);
+    for (int c = 0; c < kOnce; ++c) x[c] = __fmul_rn(sum[i + c], p.scale);
     if (p.accumulate) {
-      float a[kRun];
-      em_load_as<kRun>(out_type, p.out, at, a);
+      float a[kOnce];
+      em_load_as<kOnce>(out_type, p.out, at, a);
 #pragma unroll
-      for (int c = 0; c < kRun; ++c) x[c] = __fadd_rn(a[c], x[c]);
+      for (int c = 0; c < kOnce; ++c) x[c] = __fadd_rn(a[c], x[c]);
     }
-    em_store_as<kRun>(out_type, p.out, at, x);
+    em_store_as<kOnce>(out_type, p.out, at, x);
   }
 }
 
 template <int kType, bool kVec>
 __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
-  constexpr int kRun = kVec ? 16 / tab_bytes(kType) : 1;
+  constexpr int kRun = kVec ? 16 / tab_bytes(kType) : kEgEach;
   __shared__ __align__(16) unsigned char eg_ring[kVec ? eg_stages<kType>() * kEgThreads * kEgEach * tab_bytes(kType) : 16];
   __shared__ int rows[kEgMaxWindow + kEgMaxPiece];       // of the gradient, by place from x0 on; complemented where a piece ends
   __shared__ int4 spots[kEgMaxWindow];
@@ -622,7 +776,7 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
     if (tid <= n) firsts[tid] = p.first[v0 + tid];
     __syncthreads();
     for (int i = 0; i < n; ++i)
-      if (firsts[i] == firsts[i + 1]) eg_write<kRun>(p, out_type, v0 + i, slice, zero);
+      if (firsts[i] == firsts[i + 1]) eg_write<kRun, kVec>(p, out_type, v0 + i, slice, zero);
     return;
   }
   // (behind the last valid place there is something to read, which is not used)
@@ -755,7 +909,7 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
     }
     if (!whole) return;
     if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(spots[k].y + p.v_offset);
-    eg_write<kRun>(p, out_type, out_rows[k], slice, sum);
+    eg_write<kRun, kVec>(p, out_type, out_rows[k], slice, sum);
 #pragma unroll
     for (int i = 0; i < kEgEach; ++i) sum[i] = 0.f;
   };
@@ -782,23 +936,21 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
   } else {
 #pragma unroll 1
     for (int x = x0; x < x1; x += kEgAhead) {
-      EmWord<kType, 1> g[kEgAhead][kEgEach];
+      EmRaw<kType> g[kEgAhead];
       int row[kEgAhead];
+      const int h = eg_channel<kEgEach>(slice, 0);
 #pragma unroll
       for (int u = 0; u < kEgAhead; ++u) {
         row[u] = x + u < x1 ? rows[x + u - x0] : 0;
-        const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride * tab_bytes(kType);
-#pragma unroll
-        for (int i = 0; i < kEgEach; ++i) {
-          const int h = eg_channel<1>(slice, i);
-          if (x + u < x1 && h < p.H) g[u][i].load(at + static_cast<long long>(h) * tab_bytes(kType));
-        }
+        if (x + u < x1 && h < p.H)
+          g[u].load(p.grad, p.grad_end, static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride, h, p.H);
       }
 #pragma unroll
       for (int u = 0; u < kEgAhead; ++u) {
         if (x + u >= x1) break;
+        const EmWord<kType, kEgEach> y = g[u].get();
 #pragma unroll
-        for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u][i].get(0));
+        for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], y.get(i));
         if (row[u] < 0) finish(x + u);
       }
     }

@@ -562,3 +562,43 @@ def test_the_most_tokens_of_a_call():
     assert torch.equal(binding.hola_embed_grad(t, grad, V).double(), want[1:])
     with pytest.raises(binding.HolaError):
         binding.hola_embed_grad(torch.zeros(N + 1, dtype=torch.int32, device="cuda"), grad[:1].expand(N + 1, H), V)
+
+
+@gpu
+@pytest.mark.parametrize("table_dtype", [*FLOATS, torch.int8])
+@pytest.mark.parametrize("H", [1, 3, 15, 17, 333, 1001, 2050])
+def test_rows_that_start_anywhere(H, table_dtype):
+    """Tables, results and what is added on every address of their type, first and last rows of their buffers among them."""
+    V, N = 41, 83
+    tokens = some_tokens(N, V, H)
+    tokens[:3] = torch.tensor([0, V - 1, 0], dtype=torch.int32)
+    scale = rnd((V,), torch.float32, 1).abs() if table_dtype == torch.int8 else None
+    for lead in range(0, 9):
+        wide = H + lead % 3
+        buf = rnd((lead + V * wide,), torch.float32, lead, 20.0).to(table_dtype)[lead:]
+        table = buf.view(V, wide)[:, :H]
+        rows32 = table.float() * scale[:, None] if scale is not None else table.float()
+        for dtype in FLOATS:
+            out = torch.full((N * (H + 1) + 9,), -3.0, dtype=dtype, device="cuda")
+            view = out[lead:lead + N * (H + 1)].view(N, H + 1)[:, :H]
+            add = rnd((N * H + lead,), dtype, 5)[lead:].view(N, H) if lead % 2 else None
+            binding.hola_embed(tokens, table, 1.25, add=add, w_scale=scale, out=view)
+            assert torch.equal(view, looked_up(tokens, rows32, 1.25, add, dtype))
+            view.fill_(-3.0)
+            assert (out == -3.0).all()                        # (nothing beside the rows has been written)
+
+
+@gpu
+@pytest.mark.parametrize("g_dtype", FLOATS)
+@pytest.mark.parametrize("H", [1, 3, 15, 17, 333, 1001, 2050])
+def test_gradients_that_start_anywhere(H, g_dtype):
+    V, N = 60, 700
+    tokens = some_tokens(N, V, H)
+    for lead in (0, 1, 2, 5, 8):
+        grad = rnd((N * (H + lead % 3) + lead,), g_dtype, lead)[lead:].view(N, -1)[:, :H]
+        out = torch.full((V * (H + 1) + 9,), -3.0, device="cuda")
+        view = out[lead:lead + V * (H + 1)].view(V, H + 1)[:, :H]
+        binding.hola_embed_grad(tokens, grad, V, 0.5, out=view)
+        check_grad(tokens, grad, V, 0.5, view)
+        view.fill_(-3.0)
+        assert (out == -3.0).all()

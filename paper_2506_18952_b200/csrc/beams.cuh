@@ -88,7 +88,7 @@ struct BsRow {
   const void* row;
   const unsigned char* at;             // group `begin`
   float b, w32;
-  int beam, begin, count, rounds;      // rounds of kBsThreads groups
+  int beam, begin, count;
   int edge[2];
 };
 
@@ -104,7 +104,7 @@ struct BsShared {
   uint8_t looked_at[kBsWarps][32];
   unsigned bad_from[kBsMaxCluster];    // rows that hold NaN or +inf, as every CTA of the cluster has found them
   unsigned bad_here;
-  int rounds, n_own;
+  int width, n_own;                    // width: groups of the row that has most of them in this part
   float b_max;
 };
 
@@ -184,7 +184,6 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
         row.off = off; row.weight = weight; row.row = at; row.b = b; row.w32 = weight; row.beam = lane;
         row.begin = r.whole_begin + first;
         row.count = min(per, whole - first);
-        row.rounds = (row.count + kBsThreads - 1) / kBsThreads;
         row.at = reinterpret_cast<const unsigned char*>(r.base) + static_cast<size_t>(row.begin) * kLpGroupBytes;
         row.edge[0] = part == 0 && r.whole_begin == 1 ? 0 : -1;
         row.edge[1] = part == 0 && r.whole_end < r.groups && r.whole_end >= r.whole_begin ? r.whole_end : -1;
@@ -192,18 +191,19 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
       const float most = warp_max_f32(live_mask >> lane & 1u ? fabsf(b) : 0.f);
       if (lane == 0) s.b_max = most;
       __syncwarp();
-      const int rounds = __reduce_add_sync(0xffffffffu, lane < live ? s.rows[lane].rounds : 0);
-      if (lane == 0) s.rounds = rounds;
+      const int width = __reduce_max_sync(0xffffffffu, lane < live ? s.rows[lane].count : 0);
+      if (lane == 0) s.width = width;
     }
     __syncthreads();
 
-    // The pass, all rows' rounds one after the other: kBsAhead of them on the way.  (A thread without a group in a round takes the
-    // part's last one again and sets it aside: no lane waits for another's load.)
+    // The pass: the part's groups, `width` places for those of every row, dealt out to the threads in rounds, kBsAhead of them on the way.  (So
+    // short rows, or many CTAs to a sequence, leave no thread idle: 2 x 16 x 10864 fp16 95.8 us with rounds of one row each, and too few on the
+    // board for a limit.)
     float m = -CUDART_INF_F, second = -CUDART_INF_F, third = -CUDART_INF_F;
-    int at = 0, at_second = 0;                           // rounds of the two largest; s.rounds: an edge
-    const int rounds = s.rounds;
+    int at = 0, at_second = 0;                           // rounds of the two largest; `rounds`: an edge
+    const int width = s.width, rounds = static_cast<int>((static_cast<long long>(live) * width + kBsThreads - 1) / kBsThreads);
     auto take = [&](float top, float w32, float b, bool have, int beam, int where) {
-      if (!(top < CUDART_INF_F)) atomicOr(&s.bad_here, 1u << beam);
+      if (have && !(top < CUDART_INF_F)) atomicOr(&s.bad_here, 1u << beam);
       const float a = have ? bs_approx(top, w32, b) : -CUDART_INF_F;
       third = fmaxf(third, fminf(a, second));
       if (a > second) at_second = a > m ? at : where;
@@ -211,21 +211,38 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
       if (a > m) at = where;
       m = fmaxf(m, a);
     };
-    {
-      int li_a = -1, left_a = 0, j_a = 0, last_a = 0;      // the round that is loaded next
-      int li = -1, left = 0, spare = 0, beam = 0;          // the one that is looked at; spare > 0: this thread has a group in it
+    // Group of this thread in a round: row and place in it (row `live` or a place that the row lacks: none).
+    auto group_of = [&](int round, int thread, int* j) {
+      const int f = round * kBsThreads + thread, li = f / width;
+      *j = f - li * width;
+      return li;
+    };
+    if (rounds > 0) {
+      const int q = kBsThreads / width, r = kBsThreads - q * width;
+      int j_a = 0, li_a = group_of(0, tid, &j_a), j = j_a, li = li_a;        // of the round that is loaded next, and of the one that is looked at
+      int count_a = 0, count = 0, beam = 0;
       float w32 = 1.f, b = 0.f;
       const unsigned char* row_at = nullptr;
+      auto reload_a = [&]() {
+        count_a = 0;
+        if (li_a < live) { row_at = s.rows[li_a].at; count_a = s.rows[li_a].count; }
+      };
+      auto reload = [&]() {
+        count = 0;
+        if (li < live) { count = s.rows[li].count; w32 = s.rows[li].w32; b = s.rows[li].b; beam = s.rows[li].beam; }
+      };
+      reload_a();
+      reload();
       LpGroup<T> next[kBsAhead];
       auto load = [&](LpGroup<T>& g) {
-        if (left_a == 0) {
-          do ++li_a; while (s.rows[li_a].rounds == 0);
-          left_a = s.rows[li_a].rounds; last_a = s.rows[li_a].count - 1; row_at = s.rows[li_a].at;
-          j_a = tid;
+        if (j_a < count_a) g.load(reinterpret_cast<const T*>(row_at + static_cast<size_t>(j_a) * kLpGroupBytes));
+        j_a += r;
+        const bool over = j_a >= width;
+        if (over) j_a -= width;
+        if (over || q > 0) {
+          li_a += q + (over ? 1 : 0);
+          reload_a();
         }
-        g.load(reinterpret_cast<const T*>(row_at + static_cast<size_t>(min(j_a, last_a)) * kLpGroupBytes));
-        j_a += kBsThreads;
-        --left_a;
       };
 #pragma unroll
       for (int d = 0; d < kBsAhead; ++d)
@@ -237,13 +254,14 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
           if (i + d >= rounds) break;
           const float top = next[d].largest();
           if (i + d + kBsAhead < rounds) load(next[d]);
-          if (left == 0) {
-            do ++li; while (s.rows[li].rounds == 0);
-            left = s.rows[li].rounds; spare = s.rows[li].count - tid; w32 = s.rows[li].w32; b = s.rows[li].b; beam = s.rows[li].beam;
+          take(top, w32, b, j < count, beam, i + d);
+          j += r;
+          const bool over = j >= width;
+          if (over) j -= width;
+          if (over || q > 0) {
+            li += q + (over ? 1 : 0);
+            reload();
           }
-          take(top, w32, b, spare > 0, beam, i + d);
-          spare -= kBsThreads;
-          --left;
         }
       }
     }
@@ -257,12 +275,15 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
     // The board: the n-th best of the threads' largest, taken together by eight or four.
     {
       uint64_t a = m > -CUDART_INF_F ? lp_key(m, tid) : 0;
-      const int board = p.n > 20 ? 64 : 32, share = kBsThreads / board;
+      // (fewer threads to a place of the board where not all of them have groups)
+      const int board = p.n > 20 ? 64 : 32, held = static_cast<int>(min(static_cast<long long>(live) * width, static_cast<long long>(kBsThreads)));
+      int share = kBsThreads / board;
+      while (share > 1 && held <= share / 2 * board) share >>= 1;
       for (int o = 1; o < share; o <<= 1) {
         const uint64_t b = __shfl_xor_sync(0xffffffffu, a, o);
         if (b > a) a = b;
       }
-      if ((lane & (share - 1)) == 0) s.board[tid / share] = a;
+      if ((lane & (share - 1)) == 0 && tid < board * share) s.board[tid / share] = a;
       __syncthreads();
       uint64_t lim = 0;
       for (int at = 0; at < board; at += 32) {
@@ -284,10 +305,11 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
         const int groups = second > -CUDART_INF_F && second >= thr ? 2 : 1;
 #pragma unroll 1
         for (int q = 0; q < groups; ++q) {
-          int li = tid >> 1, j = my_edge, t = q ? at_second : at;
+          const int t = q ? at_second : at;
+          int li = tid >> 1, j = my_edge;
           if (t < rounds) {
-            for (li = 0; t >= s.rows[li].rounds; ++li) t -= s.rows[li].rounds;
-            j = s.rows[li].begin + t * kBsThreads + tid;
+            li = group_of(t, tid, &j);
+            j += s.rows[li].begin;
           }
           bs_note<T>(s, li, p.V, j, thr);
         }
@@ -300,10 +322,9 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
         __syncwarp();
         const int who = __popc(look), total = rounds * who;
         for (int i = lane; i < total; i += 32) {
-          int t = i / who, li = 0;
-          for (; t >= s.rows[li].rounds; ++li) t -= s.rows[li].rounds;
-          const int j = t * kBsThreads + warp * 32 + s.looked_at[warp][i % who];
-          if (j < s.rows[li].count) bs_note<T>(s, li, p.V, s.rows[li].begin + j, thr);
+          int j;
+          const int li = group_of(i / who, warp * 32 + s.looked_at[warp][i % who], &j);
+          if (li < live && j < s.rows[li].count) bs_note<T>(s, li, p.V, s.rows[li].begin + j, thr);
         }
       }
     }

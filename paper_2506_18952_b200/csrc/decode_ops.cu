@@ -232,14 +232,12 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->grad) % ge ||
       reinterpret_cast<uintptr_t>(a->out) % oe)
     return HOLA_ERR_INVALID_ARG;
-  const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + kEgMaxWindow - 1) / kEgMaxWindow) * p.slices;
+  const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + p.blank - 1) / p.blank) * p.slices;
   if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (!device_facts()) return HOLA_ERR_NO_DEVICE;
   p.tokens = a->tokens; p.wide = a->wide_tokens; p.v_offset = a->v_offset;
   p.V_global = a->V_global ? a->V_global : a->V;
-  p.grad = a->grad; p.g_stride = a->grad_stride;
-  p.grad_end = static_cast<const unsigned char*>(a->grad) + (a->N > 0 ? ((a->N - 1) * a->grad_stride + a->H) * ge : 0);
-  p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;
+  p.grad = a->grad; p.g_stride = a->grad_stride; p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride;
   p.accumulate = a->accumulate; p.by_rows = by_rows; p.ids_out = a->ids_out; p.count_out = a->count_out; p.status = a->status_word;
   unsigned char* ws = static_cast<unsigned char*>(a->workspace);
   p.places = reinterpret_cast<int4*>(ws + l.places); p.numbers = reinterpret_cast<int2*>(ws + l.numbers);

@@ -471,7 +471,7 @@ cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, bool word
 //    1 / U of the ids nor, where p(id) is about 1 / (id + 1), much more than 1 / Z of the tokens (or one id).  Bound by latency;
 //    N x 4 or 8 bytes per CTA out of the L2.
 // 2. Sums.  The sorted order is cut into windows; the rows of a token lie side by side there, in pieces of at most `S`.  A CTA adds up
-//    the pieces that begin in its window, for a slice of kEgSlice channels.  A token with one piece is finished by it; the pieces of the others
+//    the pieces that begin in its window, for a slice of 1024 channels (256 where there are no more).  A token with one piece is finished by it; the pieces of the others
 //    go to the workspace, and the CTA that comes last adds them up in their order.  So the result does not depend on the schedule.
 //    The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
 constexpr int kEsThreads = 1024, kEsWarps = 32;
@@ -480,11 +480,10 @@ constexpr int kEsList = 512, kEsMaxList = 1024;       // tokens that a warp list
 constexpr int kEsLoads = 8;            // 32 tokens each that a warp has on the way
 constexpr int kEsMaxShared = 216 * 1024;       // shared memory of a CTA
 constexpr int kEsIdBits = 11;          // ids of a range (with what is left of 32 bits for places in a warp's stretch)
-constexpr int kEgThreads = 128, kEgEach = 8;
-constexpr int kEgSlice = kEgThreads * kEgEach;
+constexpr int kEgThreads = 128, kEgFewThreads = 32, kEgEach = 8;       // threads of a CTA of the sums; where a row has at most 256 channels
 constexpr int kEgMaxWindow = 64, kEgMaxPiece = 1024;
-constexpr int kEgRanges = 2 * kEgThreads;        // ranges of ids whose distinct ones are added up beforehand
-constexpr int kEgAhead = 6;            // rows of a thread on the way (those that start anywhere)
+constexpr int kEgRanges = 256;         // ranges of ids whose distinct ones are added up beforehand
+constexpr int kEgAhead = 8;            // rows of a thread on the way (those that start anywhere)
 constexpr long long kEgMaxTokens = 1 << 25;      // what is left of a list's words for places in the stretch of one of 16 warps
 constexpr int kEgPlanSms = 148;        // what the work is cut for (the workspace has to be known without a device)
 
@@ -495,8 +494,8 @@ struct EgParams {
   long long v_offset, V_global;
   int even, buckets, R, warps, chunk, list;      // sort: U, ranges of ids and how many a range holds at most, warps that count, tokens of a warp
                                        // and how many of them it lists
-  int S, S_log2, window, slices;
-  const void *grad, *grad_end;
+  int S, S_log2, window, slices, blank;      // sums: piece, window, slices of the channels; rows of a CTA that writes zeros
+  const void* grad;
   long long g_stride;
   float scale;
   void* out;
@@ -511,7 +510,7 @@ struct EgParams {
   int* distinct;                       // [buckets]
   int* valid;                          // tokens that have a row
   unsigned* done;                      // [ceil(N / S)][slices] pieces of a token that have arrived
-  float* partial;                      // [2 ceil(N / S)][slices * kEgSlice]
+  float* partial;                      // [2 ceil(N / S)][slices x channels of a slice]
   unsigned* status;
 };
 
@@ -723,47 +722,49 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
   put_list();
 }
 
-// Eight channels of a thread, in runs that lie side by side: of 16 bytes of the gradient, or all of them where rows start anywhere.
-template <int kRun>
+// Eight channels of a thread, in runs that lie side by side: of 16 bytes of the gradient, or single ones where rows start anywhere.
+// (Eight at once out of the aligned words that hold them, as lookups take them, and turned round for the result: 9000 x 1001 bf16 26.3 -> 32.8 us.)
+template <int kRun, int kThreads>
 __device__ __forceinline__ int eg_channel(int slice, int i) {
-  return slice * kEgSlice + (i / kRun) * (kEgThreads * kRun) + static_cast<int>(threadIdx.x) * kRun + i % kRun;
+  return slice * (kThreads * kEgEach) + (i / kRun) * (kThreads * kRun) + static_cast<int>(threadIdx.x) * kRun + i % kRun;
 }
 template <int kType>
 using EgWord = EmWord<kType, kEgEach>;
-// Rows of a thread in the ring: 24 KB of a CTA.
+// Rows of a thread in the ring: 24 KB of a CTA of 128 threads.
 template <int kType>
 __host__ __device__ constexpr int eg_stages() { return 24 * 1024 / (kEgThreads * kEgEach * tab_bytes(kType)); }
 
-// The sums, scaled, to a row of the result (added to what is there); kVec: runs are aligned, else channel by channel.
-template <int kRun, bool kVec>
+// The sums, scaled, to a row of the result (added to what is there), run by run.
+template <int kRun, int kThreads>
 __device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long long row, int slice, const float* sum) {
-  constexpr int kOnce = kVec ? kRun : 1;
 #pragma unroll
-  for (int i = 0; i < kEgEach; i += kOnce) {
-    const int h = eg_channel<kRun>(slice, i);
+  for (int i = 0; i < kEgEach; i += kRun) {
+    const int h = eg_channel<kRun, kThreads>(slice, i);
     if (h >= p.H) continue;
     const long long at = row * p.out_stride + h;
-    float x[kOnce];
+    float x[kRun];
 #pragma unroll
-    for (int c = 0; c < kOnce; ++c) x[c] = __fmul_rn(sum[i + c], p.scale);
+    for (int c = 0; c < kRun; ++c) x[c] = __fmul_rn(sum[i + c], p.scale);
     if (p.accumulate) {
-      float a[kOnce];
-      em_load_as<kOnce>(out_type, p.out, at, a);
+      float a[kRun];
+      em_load_as<kRun>(out_type, p.out, at, a);
 #pragma unroll
-      for (int c = 0; c < kOnce; ++c) x[c] = __fadd_rn(a[c], x[c]);
+      for (int c = 0; c < kRun; ++c) x[c] = __fadd_rn(a[c], x[c]);
     }
-    em_store_as<kOnce>(out_type, p.out, at, x);
+    em_store_as<kRun>(out_type, p.out, at, x);
   }
 }
 
-template <int kType, bool kVec>
-__global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
-  constexpr int kRun = kVec ? 16 / tab_bytes(kType) : kEgEach;
-  __shared__ __align__(16) unsigned char eg_ring[kVec ? eg_stages<kType>() * kEgThreads * kEgEach * tab_bytes(kType) : 16];
+// kVec: everything is aligned.
+template <int kType, bool kVec, int kThreads>
+__global__ void __launch_bounds__(kThreads, kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
+  constexpr int kRun = kVec ? 16 / tab_bytes(kType) : 1, kSlice = kThreads * kEgEach;
+  constexpr int kMine = kEgRanges / kThreads;            // ranges that a thread adds up
+  __shared__ __align__(16) unsigned char eg_ring[kVec ? eg_stages<kType>() * kSlice * tab_bytes(kType) : 16];
   __shared__ int rows[kEgMaxWindow + kEgMaxPiece];       // of the gradient, by place from x0 on; complemented where a piece ends
   __shared__ int4 spots[kEgMaxWindow];
   __shared__ int firsts[kEgMaxWindow + 1], out_rows[kEgMaxWindow];
-  __shared__ int part_sum[kEgThreads / 32], range_rows[kEgRanges];
+  __shared__ int part_sum[kThreads / 32], range_rows[kEgRanges];
   __shared__ int last_here;
   const int slice = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.slices)), tid = threadIdx.x;
   const int w = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.slices));
@@ -772,29 +773,25 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
   if (w >= windows) {
     // The whole table: zeros to the rows of ids that do not occur.
     const float zero[kEgEach] = {};
-    const int v0 = (w - windows) * kEgMaxWindow, n = min(kEgMaxWindow, p.V - v0);
-    if (tid <= n) firsts[tid] = p.first[v0 + tid];
+    const int v0 = (w - windows) * p.blank, n = min(p.blank, p.V - v0);
+    for (int i = tid; i <= n; i += kThreads) firsts[i] = p.first[v0 + i];
     __syncthreads();
     for (int i = 0; i < n; ++i)
-      if (firsts[i] == firsts[i + 1]) eg_write<kRun, kVec>(p, out_type, v0 + i, slice, zero);
+      if (firsts[i] == firsts[i + 1]) eg_write<kRun, kThreads>(p, out_type, v0 + i, slice, zero);
     return;
   }
   // (behind the last valid place there is something to read, which is not used)
   const int w0 = w * p.window, before_S = p.S - 1;
-  int4 spot = make_int4(0, 0, 0, 0);
-  int2 number = make_int2(0, 0);
-  if (tid < p.window && w0 + tid < p.N) {
-    spot = p.places[w0 + tid];
-    if (p.by_rows) number = p.numbers[w0 + tid];
-    spots[tid] = spot;
-  }
-  // by rows: distinct ids of the first kEgRanges ranges, two a thread, added up
-  int in_range[2] = {0, 0}, upto = 0;
+  for (int i = tid; i < p.window && w0 + i < p.N; i += kThreads) spots[i] = p.places[w0 + i];
+  // by rows: distinct ids of the first kEgRanges ranges, added up
+  int in_ranges = 0, upto = 0, in_range[kMine];
   if (p.by_rows) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (2 * tid + i < p.buckets) in_range[i] = p.distinct[2 * tid + i];
-    upto = in_range[0] + in_range[1];
+    for (int i = 0; i < kMine; ++i) {
+      in_range[i] = kMine * tid + i < p.buckets ? p.distinct[kMine * tid + i] : 0;
+      in_ranges += in_range[i];
+    }
+    upto = in_ranges;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, upto, o);
@@ -813,10 +810,13 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
   __syncthreads();
   if (p.by_rows) {
     // where each range's ids begin in the result
-    int at = upto - in_range[0] - in_range[1];
+    int at = upto - in_ranges;
     for (int i = 0; i < tid >> 5; ++i) at += part_sum[i];
-    range_rows[2 * tid] = at;
-    range_rows[2 * tid + 1] = at + in_range[0];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      range_rows[kMine * tid + i] = at;
+      at += in_range[i];
+    }
   }
   // Places x0 .. x1 - 1: from the first piece that begins in the window to the end of the last one that does.
   int x0 = w0, x1 = w1;
@@ -827,7 +827,7 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
     const int4 last = spots[w1 - 1 - w0];
     x1 = min(last.z + (((w1 - 1 - last.z) | before_S) + 1), last.w);
   }
-  for (int i = tid; i < x1 - x0; i += kEgThreads) {
+  for (int i = tid; i < x1 - x0; i += kThreads) {
     // (places behind the window belong to the last piece)
     bool ends = x0 + i + 1 == x1;
     int row;
@@ -852,10 +852,10 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
       const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row < 0 ? ~row : row) * p.g_stride * tab_bytes(kType);
 #pragma unroll
       for (int i = 0; i < kWords; ++i) {
-        const int h = eg_channel<kRun>(slice, i * kRun);
+        const int h = eg_channel<kRun, kThreads>(slice, i * kRun);
         if (h < p.H)
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                       ::"r"(ring + (slot * kWords + i) * kEgThreads * 16), "l"(at + static_cast<long long>(h) * tab_bytes(kType)) : "memory");
+                       ::"r"(ring + (slot * kWords + i) * kThreads * 16), "l"(at + static_cast<long long>(h) * tab_bytes(kType)) : "memory");
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -865,15 +865,16 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
 #pragma unroll 1
     for (int s = 0; s < kStages - 1; ++s) copy(x0 + s, s);
   }
-  if (tid < w1 - w0) {
-    int row = spot.y;
+  for (int k = tid; k < w1 - w0; k += kThreads) {
+    int row = spots[k].y;
     if (p.by_rows) {
       // the distinct ids ahead of an id's own range, and ahead of it there
+      const int2 number = p.numbers[w0 + k];
       row = range_rows[min(number.x, kEgRanges - 1)] + number.y;
 #pragma unroll 4
       for (int i = kEgRanges - 1; i < number.x; ++i) row += p.distinct[i];
     }
-    out_rows[tid] = row;
+    out_rows[k] = row;
   }
   __syncthreads();
 
@@ -884,10 +885,10 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
     bool whole = true;
     if (end - begin > p.S) {
       const int from = begin + ((x - begin) & ~before_S);
-      const long long width = static_cast<long long>(p.slices) * kEgSlice;
-      float* mine = p.partial + (2ll * (from >> p.S_log2) + (from == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
+      const long long width = static_cast<long long>(p.slices) * kSlice;
+      float* mine = p.partial + (2ll * (from >> p.S_log2) + (from == begin ? 1 : 0)) * width + slice * kSlice + tid;
 #pragma unroll
-      for (int i = 0; i < kEgEach; ++i) { mine[i * kEgThreads] = sum[i]; sum[i] = 0.f; }
+      for (int i = 0; i < kEgEach; ++i) { mine[i * kThreads] = sum[i]; sum[i] = 0.f; }
       __threadfence();
       __syncthreads();
       if (tid == 0) {
@@ -901,15 +902,15 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
         __threadfence();
 #pragma unroll 4
         for (int b = begin; b < end; b += p.S) {
-          const float* y = p.partial + (2ll * (b >> p.S_log2) + (b == begin ? 1 : 0)) * width + slice * kEgSlice + tid;
+          const float* y = p.partial + (2ll * (b >> p.S_log2) + (b == begin ? 1 : 0)) * width + slice * kSlice + tid;
 #pragma unroll
-          for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], __ldcg(y + i * kEgThreads));
+          for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], __ldcg(y + i * kThreads));
         }
       }
     }
     if (!whole) return;
     if (p.by_rows && slice == 0 && tid == 0) p.ids_out[out_rows[k]] = static_cast<int>(spots[k].y + p.v_offset);
-    eg_write<kRun, kVec>(p, out_type, out_rows[k], slice, sum);
+    eg_write<kRun, kThreads>(p, out_type, out_rows[k], slice, sum);
 #pragma unroll
     for (int i = 0; i < kEgEach; ++i) sum[i] = 0.f;
   };
@@ -921,7 +922,7 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
       EgWord<kType> g;
 #pragma unroll
       for (int i = 0; i < kWords; ++i) {
-        const uint4 y = *reinterpret_cast<const uint4*>(eg_ring + ((slot * kWords + i) * kEgThreads + tid) * 16);
+        const uint4 y = *reinterpret_cast<const uint4*>(eg_ring + ((slot * kWords + i) * kThreads + tid) * 16);
         g.w[4 * i] = y.x; g.w[4 * i + 1] = y.y; g.w[4 * i + 2] = y.z; g.w[4 * i + 3] = y.w;
       }
       const bool ends = rows[x - x0] < 0;
@@ -936,21 +937,23 @@ __global__ void __launch_bounds__(kEgThreads, kVec ? 7 : 4) embed_grad_kernel(co
   } else {
 #pragma unroll 1
     for (int x = x0; x < x1; x += kEgAhead) {
-      EmRaw<kType> g[kEgAhead];
+      EmWord<kType, 1> g[kEgAhead][kEgEach];
       int row[kEgAhead];
-      const int h = eg_channel<kEgEach>(slice, 0);
 #pragma unroll
       for (int u = 0; u < kEgAhead; ++u) {
         row[u] = x + u < x1 ? rows[x + u - x0] : 0;
-        if (x + u < x1 && h < p.H)
-          g[u].load(p.grad, p.grad_end, static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride, h, p.H);
+        const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride * tab_bytes(kType);
+#pragma unroll
+        for (int i = 0; i < kEgEach; ++i) {
+          const int h = eg_channel<1, kThreads>(slice, i);
+          if (x + u < x1 && h < p.H) g[u][i].load(at + static_cast<long long>(h) * tab_bytes(kType));
+        }
       }
 #pragma unroll
       for (int u = 0; u < kEgAhead; ++u) {
         if (x + u >= x1) break;
-        const EmWord<kType, kEgEach> y = g[u].get();
 #pragma unroll
-        for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], y.get(i));
+        for (int i = 0; i < kEgEach; ++i) sum[i] = __fadd_rn(sum[i], g[u][i].get(0));
         if (row[u] < 0) finish(x + u);
       }
     }
@@ -963,7 +966,7 @@ struct EgLayout {
 
 // Host: the cut of the work.  False: sizes that are not served.
 bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
-  if (N < 0 || N > kEgMaxTokens || V <= 0 || H <= 0 || V > 1 << 30 || H > INT32_MAX - kEgSlice) return false;
+  if (N < 0 || N > kEgMaxTokens || V <= 0 || H <= 0 || V > 1 << 30 || H > INT32_MAX - 4096) return false;
   p->N = static_cast<int>(N); p->V = V; p->H = H;
   int warps = 1;
   while (warps < kEsWarps && N > 64ll * warps) warps <<= 1;      // a warp's stretch: 64 tokens, or more once all count
@@ -987,7 +990,10 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   p->S = S;
   p->S_log2 = 0;
   while (1 << p->S_log2 < S) ++p->S_log2;
-  p->slices = (H + kEgSlice - 1) / kEgSlice;
+  const int slice = (H <= kEgFewThreads * kEgEach ? kEgFewThreads : kEgThreads) * kEgEach;
+  p->slices = (H + slice - 1) / slice;
+  p->blank = kEgMaxWindow;
+  while (p->blank > 1 && static_cast<long long>(V) / p->blank * p->slices < 16ll * kEgPlanSms) p->blank >>= 1;
   int window = kEgMaxWindow;
   while (window > 4 && (N + window - 1) / window * p->slices < 16ll * kEgPlanSms) window >>= 1;
   p->window = window;
@@ -1000,7 +1006,7 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   l->distinct = take(static_cast<size_t>(p->buckets) * 4);
   l->valid = take(4);
   l->done = take(pieces * p->slices * 4);
-  l->partial = take(2 * pieces * p->slices * kEgSlice * 4);
+  l->partial = take(2 * pieces * p->slices * slice * 4);
   l->total = at;
   return true;
 }
@@ -1019,11 +1025,16 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
   else e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int32_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int32_t>, p);
   if (e != cudaSuccess) return e;
   const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
-  const long long blank = p.first ? (static_cast<long long>(p.V) + kEgMaxWindow - 1) / kEgMaxWindow : 0;
-  cfg.gridDim = dim3(static_cast<unsigned>((windows + blank) * p.slices)); cfg.blockDim = dim3(kEgThreads);
+  const long long blank = p.first ? (static_cast<long long>(p.V) + p.blank - 1) / p.blank : 0;
+  const bool few = p.H <= kEgFewThreads * kEgEach;
+  cfg.gridDim = dim3(static_cast<unsigned>((windows + blank) * p.slices)); cfg.blockDim = dim3(few ? kEgFewThreads : kEgThreads);
   cfg.dynamicSmemBytes = 0;
-  return vec ? cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, true>, p, out_type, static_cast<int>(windows))
-             : cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, false>, p, out_type, static_cast<int>(windows));
+  const int n = static_cast<int>(windows);
+  if (few)
+    return vec ? cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, true, kEgFewThreads>, p, out_type, n)
+               : cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, false, kEgFewThreads>, p, out_type, n);
+  return vec ? cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, true, kEgThreads>, p, out_type, n)
+             : cudaLaunchKernelEx(&cfg, embed_grad_kernel<kType, false, kEgThreads>, p, out_type, n);
 }
 
 template <typename Cell>
@@ -1033,10 +1044,15 @@ cudaError_t configure_sort() {
 }
 // What the sums have on the way is in shared memory, as many CTAs of it as there is room for; where rows start anywhere, in the L1, which
 // the sort has left next to nothing of (16384 aligned rows that way: 81.4 us, 70.6 with room for them).
+template <int kType, int kThreads>
+cudaError_t configure_sums_of() {
+  const cudaError_t e = cudaFuncSetAttribute(embed_grad_kernel<kType, true, kThreads>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_grad_kernel<kType, false, kThreads>, cudaFuncAttributePreferredSharedMemoryCarveout, 25);
+}
 template <int kType>
 cudaError_t configure_sums() {
-  const cudaError_t e = cudaFuncSetAttribute(embed_grad_kernel<kType, true>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_grad_kernel<kType, false>, cudaFuncAttributePreferredSharedMemoryCarveout, 25);
+  const cudaError_t e = configure_sums_of<kType, kEgThreads>();
+  return e != cudaSuccess ? e : configure_sums_of<kType, kEgFewThreads>();
 }
 cudaError_t configure_embedding() {
   cudaError_t e = configure_sort<uint16_t>();

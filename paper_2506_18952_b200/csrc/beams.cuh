@@ -4,12 +4,12 @@
 // Selection.  Candidate (w, v) of a sequence has c = (score[w] - logZ[w]) + l[w][v] and the key c * weight[w], both in 64 bits; the n
 // first in the order (key descending, beam ascending, logit descending, id ascending) are kept.  One pass over the logits in 32 bits:
 // a = fma(l, weight, b), b = (score - logZ) weight rounded, is within 2^-24 (|a| + |b|) of the key.  A cluster of CTAs takes a sequence,
-// every CTA a part of each row; a thread keeps the two largest a of its groups, those groups, and the largest of its other groups.  Every
-// eight threads put the best of theirs on a board of 32 (every four on one of 64, for more than twenty candidates); let the n-th best
-// there be w.  At least n candidates have a >= w, so each of the part's n best has a >= w - 2^-22 (|w| + max |b|): twice the bound
-// above for either side, and the roundings of this line.  Only threads whose own largest is that large hold such entries; their two groups (all of theirs, where a third is as large) are read again, out of the L2,
-// and what qualifies is placed, by keys in 64 bits, by counting those before it.  The n best go to the sequence's first CTA in their
-// order, which merges the parts' lists.
+// every CTA a part of each row; a thread keeps the two largest a of its groups, those groups, and the largest of its other groups.
+// Eight threads each put the best of theirs on a place of a board of 32 (four each on one of 64, for more than twenty candidates); let
+// the n-th best there be w.  At least n candidates have a >= w, so each of the part's n best has a >= w - 2^-22 (|w| + max |b|): twice
+// the bound above for either side, and the roundings of this line.  Only threads whose own largest is that large hold such entries;
+// their two groups (all of theirs, where a third is as large) are read again, out of the L2, and what qualifies is placed, by keys in
+// 64 bits, by counting those before it.  The n best go to the sequence's first CTA in their order, which merges the parts' lists.
 
 constexpr int kBsThreads = 256;
 constexpr int kBsWarps = kBsThreads / 32;
@@ -100,7 +100,8 @@ struct BsShared {
   BsCand sent[kBsMaxCluster][32];      // first CTA: every part's best, sorted
   int sent_by[kBsMaxCluster];          // their number
   BsCand waiting[kBsWarps][32];        // also: lists on their way through the merge
-  uint64_t board[64];
+  uint64_t keys[kBsThreads];           // the threads' largest
+  uint64_t board[kBsWarps][64];
   uint8_t looked_at[kBsWarps][32];
   unsigned bad_from[kBsMaxCluster];    // rows that hold NaN or +inf, as every CTA of the cluster has found them
   unsigned bad_here;
@@ -272,25 +273,29 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
       take(LpRow<T>(static_cast<const T*>(row.row), p.V).get_ragged(my_edge).largest(), row.w32, row.b, true, row.beam, rounds);
     }
 
-    // The board: the n-th best of the threads' largest, taken together by eight or four.
+    // The board: the n-th best of the threads' largest, taken together by eight or four that lie apart.  (Neighbouring threads have neighbouring groups,
+    // and one beam's groups may hold all that is good: with neighbours on one place the limit would be another beam's, and far too low.)
     {
-      uint64_t a = m > -CUDART_INF_F ? lp_key(m, tid) : 0;
-      // (fewer threads to a place of the board where not all of them have groups)
-      const int board = p.n > 20 ? 64 : 32, held = static_cast<int>(min(static_cast<long long>(live) * width, static_cast<long long>(kBsThreads)));
-      int share = kBsThreads / board;
-      while (share > 1 && held <= share / 2 * board) share >>= 1;
-      for (int o = 1; o < share; o <<= 1) {
-        const uint64_t b = __shfl_xor_sync(0xffffffffu, a, o);
-        if (b > a) a = b;
-      }
-      if ((lane & (share - 1)) == 0 && tid < board * share) s.board[tid / share] = a;
+      const int board = p.n > 20 ? 64 : 32;
+      s.keys[tid] = m > -CUDART_INF_F ? lp_key(m, tid) : 0;
       __syncthreads();
+      // (by every warp for itself)
+      uint64_t place[2] = {0, 0};
+#pragma unroll
+      for (int w = 0; w < kBsWarps; ++w) {
+        const uint64_t a = s.keys[w * 32 + lane];
+        if (board == 64 && (w & 1)) place[1] = a > place[1] ? a : place[1];
+        else place[0] = a > place[0] ? a : place[0];
+      }
+      s.board[warp][lane] = place[0];
+      s.board[warp][32 + lane] = place[1];
+      __syncwarp();
       uint64_t lim = 0;
       for (int at = 0; at < board; at += 32) {
-        const uint64_t key = s.board[at + lane];
+        const uint64_t key = at ? place[1] : place[0];
         int before = 0;
 #pragma unroll 8
-        for (int i = 0; i < board; ++i) before += s.board[i] > key ? 1 : 0;
+        for (int i = 0; i < board; ++i) before += s.board[warp][i] > key ? 1 : 0;
         const unsigned nth = __ballot_sync(0xffffffffu, key != 0 && before == p.n - 1);
         if (nth) lim = __shfl_sync(0xffffffffu, key, __ffs(nth) - 1);
       }
@@ -551,30 +556,31 @@ struct BrState {
   long long run, position;             // bytes that lie side by side; bytes of a position (0: all of the run is moved)
   unsigned n0, n1;                     // outer axes
   unsigned pieces;                     // of a run
+  unsigned piece;                      // bytes of one: 8 words a thread, of 16 bytes, 4, 2 or 1, as the state's addresses allow
   unsigned first_cta;
 };
 struct BrParams {
   BrState s[kBrStates];
   int count, B, W, n, in_place;
+  int split;                           // CTAs that share the parents of a piece
   long long parent_stride;
   const int* parent;
   const int* used;
   unsigned* status;
 };
-constexpr int kBrPiece = 8 * 16 * kBrThreads;      // bytes of a beam that a CTA takes at most
+constexpr int kBrWords = 8;            // words of a piece that a thread takes
 
 // Every parent's words to its children: `sources` parents, children[k] as bits.
 template <typename V>
 __device__ __forceinline__ void br_spread(const BrState& st, const unsigned char* src, unsigned char* dst, long long begin, long long end,
-                                          const int* from, const unsigned* children, int sources) {
-  constexpr int U = 8;
+                                          const int* from, const unsigned* children, int first, int sources, int split) {
+  constexpr int U = kBrWords;
   constexpr int kStep = kBrThreads * sizeof(V);
-  // (a piece is 8 words of 16 bytes a thread; of narrower ones it takes several rounds)
 #pragma unroll 1
   for (long long at = begin + static_cast<long long>(threadIdx.x) * sizeof(V); at < end; at += U * kStep) {
     const int left = static_cast<int>(end - at);
 #pragma unroll 1
-    for (int k = 0; k < sources; ++k) {
+    for (int k = first; k < sources; k += split) {
       V v[U];
       const unsigned char* x = src + from[k] * st.beam + at;
 #pragma unroll
@@ -634,9 +640,11 @@ __global__ void __launch_bounds__(kBrThreads, 5) beam_reorder_kernel(const __gri
   grid_dependency_wait();
   grid_dependency_release();
   int k = 0;
-  while (k + 1 < p.count && blockIdx.x >= p.s[k + 1].first_cta) ++k;
+  const unsigned cta = blockIdx.x / static_cast<unsigned>(p.split);
+  const int share = static_cast<int>(blockIdx.x - cta * static_cast<unsigned>(p.split));
+  while (k + 1 < p.count && cta >= p.s[k + 1].first_cta) ++k;
   const BrState& st = p.s[k];
-  unsigned x = blockIdx.x - st.first_cta;
+  unsigned x = cta - st.first_cta;
   const unsigned piece = x % st.pieces; x /= st.pieces;
   const unsigned b = x % static_cast<unsigned>(p.B); x /= static_cast<unsigned>(p.B);
   const unsigned i1 = x % st.n1, i0 = x / st.n1;
@@ -673,22 +681,36 @@ __global__ void __launch_bounds__(kBrThreads, 5) beam_reorder_kernel(const __gri
     const long long filled = static_cast<long long>(max(p.used[b], 0)) * st.position;
     run = filled < run ? filled : run;
   }
-  const long long begin = static_cast<long long>(piece) * kBrPiece, end = begin + kBrPiece < run ? begin + kBrPiece : run;
+  const long long begin = static_cast<long long>(piece) * st.piece, end = begin + st.piece < run ? begin + st.piece : run;
   if (moves == 0 || begin >= end) return;
   const unsigned char* src = st.src + (b * st.seq + i0 * st.outer0 + i1 * st.outer1);
   unsigned char* dst = st.dst + (b * st.to_seq + i0 * st.to_outer0 + i1 * st.to_outer1);
-  // what every address of the piece has in common
-  const unsigned align = static_cast<unsigned>(reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) |
-                                               static_cast<uintptr_t>(st.beam | st.to_beam | end));
-  if (n_sources) {
-    if (align % 16 == 0) br_spread<uint4>(st, src, dst, begin, end, from, children, n_sources);
-    else if (align % 4 == 0) br_spread<uint32_t>(st, src, dst, begin, end, from, children, n_sources);
-    else br_spread<unsigned char>(st, src, dst, begin, end, from, children, n_sources);
-  } else {
-    if (align % 16 == 0) br_move_any<uint4>(st, src, dst, begin, end, to, from, moves);
-    else if (align % 4 == 0) br_move_any<uint32_t>(st, src, dst, begin, end, to, from, moves);
-    else br_move_any<unsigned char>(st, src, dst, begin, end, to, from, moves);
+  // whole words, and what is left of the last one byte by byte (a last position may end anywhere)
+  const int word = static_cast<int>(st.piece / (kBrWords * kBrThreads));
+  const long long words_end = end - (end - begin) % word;
+  const int sources = n_sources;
+  if (sources) {
+    if (word == 16) br_spread<uint4>(st, src, dst, begin, words_end, from, children, share, sources, p.split);
+    else if (word == 4) br_spread<uint32_t>(st, src, dst, begin, words_end, from, children, share, sources, p.split);
+    else if (word == 2) br_spread<uint16_t>(st, src, dst, begin, words_end, from, children, share, sources, p.split);
+    else br_spread<unsigned char>(st, src, dst, begin, words_end, from, children, share, sources, p.split);
+    br_spread<unsigned char>(st, src, dst, words_end, end, from, children, share, sources, p.split);
+  } else if (share == 0) {
+    if (word == 16) br_move_any<uint4>(st, src, dst, begin, words_end, to, from, moves);
+    else if (word == 4) br_move_any<uint32_t>(st, src, dst, begin, words_end, to, from, moves);
+    else if (word == 2) br_move_any<uint16_t>(st, src, dst, begin, words_end, to, from, moves);
+    else br_move_any<unsigned char>(st, src, dst, begin, words_end, to, from, moves);
+    br_move_any<unsigned char>(st, src, dst, words_end, end, to, from, moves);
   }
+}
+
+// Bytes of a piece of a state: by the widest word that all its addresses are multiples of.
+unsigned br_piece(const hola_beam_state& s) {
+  uintptr_t all = reinterpret_cast<uintptr_t>(s.src) | reinterpret_cast<uintptr_t>(s.dst) | static_cast<uintptr_t>(s.seq_stride | s.beam_stride | s.dst_seq_stride |
+                                                                                                                 s.dst_beam_stride);
+  for (int i = 0; i < 2; ++i)
+    if (s.outer[i] > 1) all |= static_cast<uintptr_t>(s.outer_stride[i] | s.dst_outer_stride[i]);
+  return kBrWords * kBrThreads * (all % 16 == 0 ? 16u : all % 4 == 0 ? 4u : all % 2 == 0 ? 2u : 1u);
 }
 
 cudaError_t launch_beam_reorder(const BrParams& p, unsigned ctas, cudaStream_t stream) {

@@ -118,13 +118,15 @@ hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
                  s.outer_stride[0] != s.dst_outer_stride[0] || s.outer_stride[1] != s.dst_outer_stride[1]))
       return HOLA_ERR_INVALID_ARG;
     if ((a->n > 1 && s.dst_beam_stride < s.run) || (a->W > 1 && s.beam_stride < s.run)) return HOLA_ERR_INVALID_ARG;      // beams that share bytes
-    const long long pieces = (s.run - 1) / kBrPiece + 1;
+    const long long pieces = (s.run - 1) / br_piece(s) + 1;
     if (pieces > INT32_MAX || s.outer[0] > INT32_MAX || s.outer[1] > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
     const double ctas = static_cast<double>(pieces) * a->B * static_cast<double>(s.outer[0]) * static_cast<double>(s.outer[1]);
     if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
   }
   if (in_place < 0) return HOLA_OK;
-  if (!device_facts()) return HOLA_ERR_NO_DEVICE;
+  const DeviceFacts* dev = device_facts();
+  if (!dev) return HOLA_ERR_NO_DEVICE;
+  const int sms = dev->sms;
   BrParams p = {};
   p.B = a->B; p.W = a->W; p.n = a->n; p.parent = a->parent; p.parent_stride = a->parent_stride; p.used = a->used; p.status = a->status_word;
   p.in_place = in_place;
@@ -134,11 +136,13 @@ hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
     const hola_beam_state* s = i < a->count ? &a->states[i] : nullptr;
     if (s) {
       if (s->run == 0 || s->outer[0] == 0 || s->outer[1] == 0) continue;
-      pieces = (s->run - 1) / kBrPiece + 1;
+      pieces = (s->run - 1) / br_piece(*s) + 1;
       more = pieces * a->B * s->outer[0] * s->outer[1];
     }
     if (p.count > 0 && (!s || p.count == kBrStates || ctas + more > INT32_MAX)) {
-      const cudaError_t e = launch_beam_reorder(p, static_cast<unsigned>(ctas), static_cast<cudaStream_t>(cuda_stream));
+      // (parents one after the other take a microsecond each: shared out where there are CTAs to spare)
+      for (p.split = 1; p.split < a->W && 2 * p.split * ctas <= 8ll * sms; p.split <<= 1) {}
+      const cudaError_t e = launch_beam_reorder(p, static_cast<unsigned>(ctas * p.split), static_cast<cudaStream_t>(cuda_stream));
       if (e != cudaSuccess) return HOLA_ERR_CUDA;
       p.count = 0;
       ctas = 0;
@@ -150,7 +154,7 @@ hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
     o.to_seq = s->dst_seq_stride; o.to_beam = s->dst_beam_stride; o.to_outer0 = s->dst_outer_stride[0]; o.to_outer1 = s->dst_outer_stride[1];
     o.run = s->run; o.position = s->position;
     o.n0 = static_cast<unsigned>(s->outer[0]); o.n1 = static_cast<unsigned>(s->outer[1]);
-    o.pieces = static_cast<unsigned>(pieces); o.first_cta = static_cast<unsigned>(ctas);
+    o.pieces = static_cast<unsigned>(pieces); o.piece = br_piece(*s); o.first_cta = static_cast<unsigned>(ctas);
     ctas += more;
   }
   return HOLA_OK;

@@ -755,6 +755,23 @@ __device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long l
   }
 }
 
+// Zeros to the bytes from `at` to `end`, whole elements of `size` bytes: 16 at a time where these are aligned.
+template <int kThreads>
+__device__ __forceinline__ void eg_zeros(unsigned char* at, unsigned char* end, int size) {
+  unsigned char* first = at + ((0 - reinterpret_cast<uintptr_t>(at)) & 15u);
+  unsigned char* last = end - (reinterpret_cast<uintptr_t>(end) & 15u);
+  if (first > last) first = last = end;                  // (less than one such)
+  for (unsigned char* x = first + threadIdx.x * 16; x < last; x += kThreads * 16) *reinterpret_cast<uint4*>(x) = make_uint4(0, 0, 0, 0);
+  for (unsigned char* x = at + threadIdx.x * size; x < first; x += kThreads * size) {
+    if (size == 4) *reinterpret_cast<uint32_t*>(x) = 0;
+    else *reinterpret_cast<uint16_t*>(x) = 0;
+  }
+  for (unsigned char* x = last + threadIdx.x * size; x < end; x += kThreads * size) {
+    if (size == 4) *reinterpret_cast<uint32_t*>(x) = 0;
+    else *reinterpret_cast<uint16_t*>(x) = 0;
+  }
+}
+
 // kVec: everything is aligned.
 template <int kType, bool kVec, int kThreads>
 __global__ void __launch_bounds__(kThreads, kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
@@ -776,8 +793,16 @@ __global__ void __launch_bounds__(kThreads, kVec ? 7 : 4) embed_grad_kernel(cons
     const int v0 = (w - windows) * p.blank, n = min(p.blank, p.V - v0);
     for (int i = tid; i <= n; i += kThreads) firsts[i] = p.first[v0 + i];
     __syncthreads();
-    for (int i = 0; i < n; ++i)
-      if (firsts[i] == firsts[i + 1]) eg_write<kRun, kThreads>(p, out_type, v0 + i, slice, zero);
+    const int size = tab_bytes(out_type), h0 = slice * kSlice, h1 = min(h0 + kSlice, p.H);
+    for (int i = 0; i < n; ++i) {
+      if (firsts[i] != firsts[i + 1]) continue;
+      if (kVec) {
+        eg_write<kRun, kThreads>(p, out_type, v0 + i, slice, zero);
+      } else {
+        unsigned char* row = static_cast<unsigned char*>(p.out) + (v0 + i) * p.out_stride * size;
+        eg_zeros<kThreads>(row + static_cast<long long>(h0) * size, row + static_cast<long long>(h1) * size, size);
+      }
+    }
     return;
   }
   // (behind the last valid place there is something to read, which is not used)

@@ -319,8 +319,12 @@ __global__ void __launch_bounds__(kEmThreads, 8) embed_kernel(const __grid_const
 template <int kType, bool kWide, bool kAdd, int n>
 cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
   constexpr int kAtOnce = n == 1 ? 4 : n;
+  // (fewer threads to a row where the last of several slices would leave more than an eighth of them idle)
   int log2 = 0;
   while ((1 << log2) < kEmThreads && (1 << log2) * kAtOnce < p.H) ++log2;
+  const long long chunks = (static_cast<long long>(p.H) + kAtOnce - 1) / kAtOnce;
+  auto idle = [&](int log) { return ((chunks + (1 << log) - 1) >> log << log) - chunks; };
+  while (log2 > 5 && 8 * idle(log2) > chunks && idle(log2 - 1) < idle(log2)) --log2;
   const int lanes = 1 << log2;
   const long long slices = (p.H + lanes * kAtOnce - 1) / (lanes * kAtOnce);
   const int slots = kEmThreads / lanes;
@@ -774,7 +778,7 @@ __device__ __forceinline__ void eg_zeros(unsigned char* at, unsigned char* end, 
 
 // kVec: everything is aligned.
 template <int kType, bool kVec, int kThreads>
-__global__ void __launch_bounds__(kThreads, kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
+__global__ void __launch_bounds__(kThreads, kThreads == kEgFewThreads ? 16 : kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
   constexpr int kRun = kVec ? 16 / tab_bytes(kType) : 1, kSlice = kThreads * kEgEach;
   constexpr int kMine = kEgRanges / kThreads;            // ranges that a thread adds up
   __shared__ __align__(16) unsigned char eg_ring[kVec ? eg_stages<kType>() * kSlice * tab_bytes(kType) : 16];
@@ -794,13 +798,18 @@ __global__ void __launch_bounds__(kThreads, kVec ? 7 : 4) embed_grad_kernel(cons
     for (int i = tid; i <= n; i += kThreads) firsts[i] = p.first[v0 + i];
     __syncthreads();
     const int size = tab_bytes(out_type), h0 = slice * kSlice, h1 = min(h0 + kSlice, p.H);
+    // (rows without a gap between them are one stretch)
+    const bool joined = !kVec && p.slices == 1 && p.out_stride == p.H;
     for (int i = 0; i < n; ++i) {
       if (firsts[i] != firsts[i + 1]) continue;
       if (kVec) {
         eg_write<kRun, kThreads>(p, out_type, v0 + i, slice, zero);
       } else {
-        unsigned char* row = static_cast<unsigned char*>(p.out) + (v0 + i) * p.out_stride * size;
-        eg_zeros<kThreads>(row + static_cast<long long>(h0) * size, row + static_cast<long long>(h1) * size, size);
+        int last = i;
+        while (joined && last + 1 < n && firsts[last + 1] == firsts[last + 2]) ++last;
+        unsigned char* out = static_cast<unsigned char*>(p.out);
+        eg_zeros<kThreads>(out + ((v0 + i) * p.out_stride + h0) * size, out + ((v0 + last) * p.out_stride + h1) * size, size);
+        i = last;
       }
     }
     return;

@@ -348,19 +348,18 @@ typedef struct hola_logprobs_args {
 hola_status hola_token_logprobs(const hola_logprobs_args* args, void* cuda_stream);
 
 /* One step of a beam search: the best continuations over all beams and the vocabulary.  The paper decodes by draft and verification;
- * this is the other search that a server runs on the same LM head (hola_lm_head_entropy with the W beams of a sequence in the place
- * of its k + 1 positions leaves the logits and logZ that are read here).  For beam w of a sequence and token v
+ * this is the other search that a server runs on the same LM head (hola_lm_head_entropy with the W beams of a sequence in the place of
+ * its k + 1 positions leaves the logits and logZ that are read here).  For beam w of a sequence and token v
  *   c(w, v) = (score[w] - logZ[w]) + l[w][v],   key = c * weight[w],   both evaluated in 64 bits,
- * and the first n candidates in the order (key descending, beam ascending, logit descending, id ascending) are written: c rounded to fp32,
- * w, v.  An ended beam (finished[w] != 0) has one candidate, end_token with c = score[w]; its logits are not read.  A score of -inf is no beam, an
- * entry of -inf no candidate.  Where fewer than n candidates are left: score -inf, parent and token -1.  A row that holds NaN or +inf,
- * a score or logZ that is NaN or +inf, or a weight that is not positive and finite: that beam has no candidates, and HOLA_FLAG_BAD_LOGIT is set.
- * keep_slots (n = W): instead of by rank, the best child of a beam is written at that beam's own place, so that its state need not
- * move; the other candidates take the free places in their order.
- * finished_out: 1 where the parent had ended or the token is end_token.
- * Outputs may not overlap inputs, but with n = W score_out may be score itself, and finished_out finished.
- * Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing, needs no context,
- * and launched like hola_verify (programmatic stream serialization, waits before it reads). */
+ * and the first n candidates in the order (key descending, beam ascending, logit descending, id ascending) are written: c rounded to
+ * fp32, w, v.  An ended beam (finished[w] != 0) has one candidate, end_token with c = score[w]; its logits are not read.  A score of
+ * -inf is no beam, an entry of -inf no candidate.  Where fewer than n candidates are left: score -inf, parent and token -1.  A row
+ * that holds NaN or +inf, a score or logZ that is NaN or +inf, or a weight that is not positive and finite: that beam has no
+ * candidates, and HOLA_FLAG_BAD_LOGIT is set. keep_slots (n = W): instead of by rank, the best child of a beam is written at that
+ * beam's own place, so that its state need not move; the other candidates take the free places in their order. finished_out: 1 where
+ * the parent had ended or the token is end_token. Outputs may not overlap inputs, but with n = W score_out may be score itself, and
+ * finished_out finished. Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing,
+ * needs no context, and launched like hola_verify (programmatic stream serialization, waits before it reads). */
 #define HOLA_MAX_BEAMS 32
 typedef struct hola_beam_args {
   int32_t B;                /* sequences, >= 0                                                            */
@@ -386,13 +385,14 @@ typedef struct hola_beam_args {
 } hola_beam_args;
 hola_status hola_beam_select(const hola_beam_args* args, void* cuda_stream);
 
-/* The beams' states in the order of their parents: new[b][i] = old[b][parent[b][i]] for i < n, for any number of states at once
- * (token histories, keys and values, page tables).  parent -1: that place is left as it was.  In place (src = dst, for all states or
- * none) any order of the parents is allowed, and beams that stay where they are cost nothing.  From one buffer into another (which may not overlap) every
- * place is written.  A run is what lies side by side of one beam, for one index of the outer axes; with `used`, states whose `position`
- * is not 0 are moved up to used[b] positions only (at most the run; negative counts as 0), and the bytes behind are left as they were.
- * Beams may not share bytes (beam_stride >= run), nor may sequences or outer indices.  `states` is a host array, not looked at after the call; its pointers, parent
- * and used are DEVICE pointers of the current device.  One launch for every 24 states.  Asynchronous on cuda_stream, allocates nothing, launched like hola_verify. */
+/* The beams' states in the order of their parents: new[b][i] = old[b][parent[b][i]] for i < n, for any number of states at once (token
+ * histories, keys and values, page tables).  parent -1: that place is left as it was.  In place (src = dst, for all states or none)
+ * any order of the parents is allowed, and beams that stay where they are cost nothing.  From one buffer into another (which may not
+ * overlap) every place is written.  A run is what lies side by side of one beam, for one index of the outer axes; with `used`, states
+ * whose `position` is not 0 are moved up to used[b] positions only (at most the run; negative counts as 0), and the bytes behind are
+ * left as they were. Beams may not share bytes (beam_stride >= run), nor may sequences or outer indices.  `states` is a host array,
+ * not looked at after the call; its pointers, parent and used are DEVICE pointers of the current device.  One launch for every 24
+ * states.  Asynchronous on cuda_stream, allocates nothing, launched like hola_verify. */
 typedef struct hola_beam_state {
   const void* src;
   void* dst;
@@ -416,12 +416,12 @@ typedef struct hola_reorder_args {
 hola_status hola_beam_reorder(const hola_reorder_args* args, void* cuda_stream);
 
 /* Rows of a table by token:  out[r] = add[r] + scale * W[tokens[r]],  the table in any storage form of the LM head (tied weights) or
- * fp32 / fp16.  Every operation is one rounding in fp32 (for the quantised forms w_scale * code first), the result is rounded once more where out is 16 bits wide.
- * A token of -1 is none: out[r] = add[r], or 0.  Any other token outside the vocabulary: the same, and HOLA_FLAG_BAD_TOKEN.  Of a
- * vocabulary that is split over several tables this is one part: rows v_offset .. v_offset + V - 1 of V_global (0: V, the whole); tokens of
- * the other parts count as none, so that the parts' results add up.
- * Every pointer but wmix is a DEVICE pointer of the current device, rows at any distance.  add may be out.  Asynchronous on cuda_stream,
- * allocates nothing, needs no context, launched like hola_verify. */
+ * fp32 / fp16.  Every operation is one rounding in fp32 (for the quantised forms w_scale * code first), the result is rounded once
+ * more where out is 16 bits wide. A token of -1 is none: out[r] = add[r], or 0.  Any other token outside the vocabulary: the same, and
+ * HOLA_FLAG_BAD_TOKEN.  Of a vocabulary that is split over several tables this is one part: rows v_offset .. v_offset + V - 1 of
+ * V_global (0: V, the whole); tokens of the other parts count as none, so that the parts' results add up. Every pointer but wmix is a
+ * DEVICE pointer of the current device, rows at any distance.  add may be out.  Asynchronous on cuda_stream, allocates nothing, needs
+ * no context, launched like hola_verify. */
 typedef enum { HOLA_T_F32 = 0, HOLA_T_BF16 = 1, HOLA_T_F16 = 2, HOLA_T_INT8 = 3, HOLA_T_MIXED = 4 } hola_t_dtype;
 typedef struct hola_embed_args {
   int64_t N;                /* tokens, >= 0                                                               */
@@ -444,14 +444,15 @@ typedef struct hola_embed_args {
 } hola_embed_args;
 hola_status hola_embed(const hola_embed_args* args, void* cuda_stream);
 
-/* The gradient of such a table:  dW[v] = scale * sum of grad[r] over the r with tokens[r] = v.  Sums are held in fp32, in pieces of rising r (at most 1024 rows) that are
- * added up in their order: the same inputs give the same bits.  Tokens count as for hola_embed.
- *   the whole table: out [V][H], rows of tokens that do not occur are zero; or with accumulate: added to what out holds, other rows left as they are.
- *   by rows (ids_out and count_out given): the distinct tokens in rising order, out[i] the row of ids_out[i], count_out their number;
- *   what lies behind is left as it was.  out and ids_out have room for N.
+/* The gradient of such a table:  dW[v] = scale * sum of grad[r] over the r with tokens[r] = v.  Sums are held in fp32, in pieces of
+ * rising r (at most 1024 rows) that are added up in their order: the same inputs give the same bits.  Tokens count as for hola_embed.
+ *   the whole table: out [V][H], rows of tokens that do not occur are zero; or with accumulate: added to what out holds, other rows
+ *     left as they are.
+ *   by rows (ids_out and count_out given): the distinct tokens in rising order, out[i] the row of ids_out[i], count_out their
+ *     number; what lies behind is left as it was.  out and ids_out have room for N.
  * workspace: hola_embed_grad_workspace_bytes(N, V, H) bytes on the device, 16-byte aligned, of this call alone until it has run (the
- * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs no context, two launches like
- * hola_verify's. */
+ * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs
+ * no context, two launches like hola_verify's. */
 typedef struct hola_embed_grad_args {
   int64_t N;                /* 0 .. 2^25                                                                  */
   int32_t V, H;             /* V at most 2^30                                                             */

@@ -197,9 +197,9 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
     }
     __syncthreads();
 
-    // The pass: the part's groups, `width` places for those of every row, dealt out to the threads in rounds, kBsAhead of them on the way.  (So
-    // short rows, or many CTAs to a sequence, leave no thread idle: 2 x 16 x 10864 fp16 95.8 us with rounds of one row each, and too few on the
-    // board for a limit.)
+    // The pass: the part's groups, `width` places for those of every row, dealt out to the threads in rounds, kBsAhead of them on the
+    // way.  (So short rows, or many CTAs to a sequence, leave no thread idle: 2 x 16 x 10864 fp16 95.8 us with rounds of one row each,
+    // and too few on the board for a limit.)
     float m = -CUDART_INF_F, second = -CUDART_INF_F, third = -CUDART_INF_F;
     int at = 0, at_second = 0;                           // rounds of the two largest; `rounds`: an edge
     const int width = s.width, rounds = static_cast<int>((static_cast<long long>(live) * width + kBsThreads - 1) / kBsThreads);
@@ -273,8 +273,9 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
       take(LpRow<T>(static_cast<const T*>(row.row), p.V).get_ragged(my_edge).largest(), row.w32, row.b, true, row.beam, rounds);
     }
 
-    // The board: the n-th best of the threads' largest, taken together by eight or four that lie apart.  (Neighbouring threads have neighbouring groups,
-    // and one beam's groups may hold all that is good: with neighbours on one place the limit would be another beam's, and far too low.)
+    // The board: the n-th best of the threads' largest, taken together by eight or four that lie apart.  (Neighbouring threads have
+    // neighbouring groups, and one beam's groups may hold all that is good: with neighbours on one place the limit would be another
+    // beam's, and far too low.)
     {
       const int board = p.n > 20 ? 64 : 32;
       s.keys[tid] = m > -CUDART_INF_F ? lp_key(m, tid) : 0;
@@ -540,11 +541,12 @@ cudaError_t configure_beams(int* fit) {
 }
 
 // ------------------------------------------------------------------------------------------------ reordering
-// new[b][i] = old[b][parent[b][i]], any number of states.  A CTA takes a piece of the bytes of all beams of one sequence (of one
-// layer, one head).  Where no place that changes has children of its own (copies into another buffer; a selection that keeps slots), every
-// parent's words are read once and written to all of its children.  Else, in place, a thread takes its words of every beam that changes into
-// registers and then writes them, so that any order of the parents will do: no other thread touches these bytes.  In place, beams that
-// stay (parent[i] = i) are neither read, but for their children, nor written.  Bound by HBM, whose latency eight words of 16 bytes a thread on the way hide.
+// new[b][i] = old[b][parent[b][i]], any number of states.  A CTA takes a piece of the bytes of all beams of one sequence (of one layer,
+// one head).  Where no place that changes has children of its own (copies into another buffer; a selection that keeps slots), every
+// parent's words are read once and written to all of its children.  Else, in place, a thread takes its words of every beam that changes
+// into registers and then writes them, so that any order of the parents will do: no other thread touches these bytes.  In place, beams
+// that stay (parent[i] = i) are neither read, but for their children, nor written.  Bound by HBM, whose latency eight words of 16 bytes a
+// thread on the way hide.
 constexpr int kBrThreads = 128;
 constexpr int kBrStates = 24;          // states of one launch (launch parameters)
 

@@ -222,8 +222,8 @@ __device__ __forceinline__ void em_mixed(const hola_wmix& mix, int H, int v, int
 // of 32 bits, else of 16 (`f16`: which).  A CTA takes kRows rows at a time, or as many times that as leave no thread idle where rows are
 // short (`lanes`: threads of a row, a power of two).  Bound by HBM: rows in, rows out.  us: 128 / 256 threads 16384 x 4096 bf16 33.2 /
 // 35.6; 8 / 16 channels 33.1 / 31.8, 20000 x 4096 int8 41 / 34; rows one by one instead of four at a time 2304 x 4096 int8 18.3 -> 13.1.
-template <int kType, int n>
-__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed || (n == 16 && kType != kTabInt8) ? 2 : 4; }       // rows on the way together
+template <int kType, int n>                            // rows on the way together
+__host__ __device__ constexpr int em_rows() { return kType == kTabF32 || kType == kTabMixed || (n == 16 && kType != kTabInt8) ? 2 : 4; }
 
 // kShort: several rows side by side in a CTA (addresses that all threads share are cheaper: 16384 x 4096 bf16 36.2 -> 33.2 us).
 template <int kType, bool kWide, bool kAdd, bool kShort, int n>
@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(kEmThreads, 8) embed_any_kernel(const __grid_c
       v[i] = em_row(p.tokens, p.wide, r0 + i, p.V, p.v_offset, p.V_global, &bad);
       any_bad = any_bad || bad;
       if (kType == kTabInt8 && v[i] >= 0) ws[i] = p.w_scale[v[i]];
-      lead[i] = static_cast<int>((0 - (reinterpret_cast<uintptr_t>(p.out) + static_cast<uintptr_t>((r0 + i) * p.out_stride) * kOutSize)) & (8 * kOutSize - 1)) / kOutSize;
+      const uintptr_t to = reinterpret_cast<uintptr_t>(p.out) + static_cast<uintptr_t>((r0 + i) * p.out_stride) * kOutSize;
+      lead[i] = static_cast<int>((0 - to) & (8 * kOutSize - 1)) / kOutSize;
     }
   }
   if (any_bad && p.status && lane == 0 && blockIdx.y == 0) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
@@ -438,7 +439,8 @@ cudaError_t launch_embed_any(const EmParams& p, int out_type, cudaStream_t strea
 }
 template <int kType>
 cudaError_t launch_embed_any_of(const EmParams& p, int out_type, cudaStream_t stream) {
-  if (out_type == kTabF32) return p.add ? launch_embed_any<kType, true, true>(p, out_type, stream) : launch_embed_any<kType, true, false>(p, out_type, stream);
+  if (out_type == kTabF32)
+    return p.add ? launch_embed_any<kType, true, true>(p, out_type, stream) : launch_embed_any<kType, true, false>(p, out_type, stream);
   return p.add ? launch_embed_any<kType, false, true>(p, out_type, stream) : launch_embed_any<kType, false, false>(p, out_type, stream);
 }
 
@@ -449,10 +451,13 @@ cudaError_t launch_embed_as(const EmParams& p, int out_type, int num_sms, cudaSt
   return p.add ? launch_embed<kType, false, true, n>(p, out_type, num_sms, stream) : launch_embed<kType, false, false, n>(p, out_type, num_sms, stream);
 }
 // Sixteen channels at once: results of 16 bits from rows of 8 or 16.
+template <int kType>
+cudaError_t launch_embed_16_of(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
+  return p.add ? launch_embed<kType, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kType, false, false, 16>(p, out_type, num_sms, stream);
+}
 cudaError_t launch_embed_16(const EmParams& p, int type, int out_type, int num_sms, cudaStream_t stream) {
-  if (type == kTabInt8) return p.add ? launch_embed<kTabInt8, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabInt8, false, false, 16>(p, out_type, num_sms, stream);
-  if (type == kTabBf16) return p.add ? launch_embed<kTabBf16, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabBf16, false, false, 16>(p, out_type, num_sms, stream);
-  return p.add ? launch_embed<kTabF16, false, true, 16>(p, out_type, num_sms, stream) : launch_embed<kTabF16, false, false, 16>(p, out_type, num_sms, stream);
+  return type == kTabInt8 ? launch_embed_16_of<kTabInt8>(p, out_type, num_sms, stream)
+         : type == kTabBf16 ? launch_embed_16_of<kTabBf16>(p, out_type, num_sms, stream) : launch_embed_16_of<kTabF16>(p, out_type, num_sms, stream);
 }
 // words: eight channels of every row start on an aligned address.
 cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, bool words, int num_sms, cudaStream_t stream) {
@@ -470,14 +475,14 @@ cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, bool word
 //
 // 1. Tokens sorted (stable), with nothing exchanged between the CTAs: each takes a range of ids and reads all tokens, every warp a
 //    stretch of them, lists those inside its range, and counts those below it (where its part of the sorted order begins).  Counts per
-//    (id, warp), and a scan over them, give every warp the place of its first occurrence of every id.  Ranges are cut at the even
-//    marks V j / U and at the marks (V + 1)^(i / Z) together, for vocabularies are numbered by falling frequency: no range holds more than
-//    1 / U of the ids nor, where p(id) is about 1 / (id + 1), much more than 1 / Z of the tokens (or one id).  Bound by latency;
-//    N x 4 or 8 bytes per CTA out of the L2.
+//    (id, warp), and a scan over them, give every warp the place of its first occurrence of every id.  Ranges are cut at the even marks
+//    V j / U and at the marks (V + 1)^(i / Z) together, for vocabularies are numbered by falling frequency: no range holds more than 1 / U
+//    of the ids nor, where p(id) is about 1 / (id + 1), much more than 1 / Z of the tokens (or one id).  Bound by latency; N x 4 or 8
+//    bytes per CTA out of the L2.
 // 2. Sums.  The sorted order is cut into windows; the rows of a token lie side by side there, in pieces of at most `S`.  A CTA adds up
-//    the pieces that begin in its window, for a slice of 1024 channels (256 where there are no more).  A token with one piece is finished by it; the pieces of the others
-//    go to the workspace, and the CTA that comes last adds them up in their order.  So the result does not depend on the schedule.
-//    The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
+//    the pieces that begin in its window, for a slice of 1024 channels (256 where there are no more).  A token with one piece is finished
+//    by it; the pieces of the others go to the workspace, and the CTA that comes last adds them up in their order.  So the result does
+//    not depend on the schedule. The whole table's gradient: further CTAs write zeros to the rows that no token names.  Bound by HBM.
 constexpr int kEsThreads = 1024, kEsWarps = 32;
 constexpr int kEsZipf = 74;            // Z
 constexpr int kEsList = 512, kEsMaxList = 1024;       // tokens that a warp lists before it counts them: as many as there is room for
@@ -778,7 +783,8 @@ __device__ __forceinline__ void eg_zeros(unsigned char* at, unsigned char* end, 
 
 // kVec: everything is aligned.
 template <int kType, bool kVec, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == kEgFewThreads ? 16 : kVec ? 7 : 4) embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
+__global__ void __launch_bounds__(kThreads, kThreads == kEgFewThreads ? 16 : kVec ? 7 : 4)
+    embed_grad_kernel(const __grid_constant__ EgParams p, int out_type, int windows) {
   constexpr int kRun = kVec ? 16 / tab_bytes(kType) : 1, kSlice = kThreads * kEgEach;
   constexpr int kMine = kEgRanges / kThreads;            // ranges that a thread adds up
   __shared__ __align__(16) unsigned char eg_ring[kVec ? eg_stages<kType>() * kSlice * tab_bytes(kType) : 16];
@@ -883,7 +889,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == kEgFewThreads ? 16 : kVe
   auto copy = [&](int x, int slot) {                     // the row at place x, into a slot of the ring
     if (x < x1) {
       const int row = rows[x - x0];
-      const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row < 0 ? ~row : row) * p.g_stride * tab_bytes(kType);
+      const unsigned char* at =
+          static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row < 0 ? ~row : row) * p.g_stride * tab_bytes(kType);
 #pragma unroll
       for (int i = 0; i < kWords; ++i) {
         const int h = eg_channel<kRun, kThreads>(slice, i * kRun);
@@ -976,7 +983,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == kEgFewThreads ? 16 : kVe
 #pragma unroll
       for (int u = 0; u < kEgAhead; ++u) {
         row[u] = x + u < x1 ? rows[x + u - x0] : 0;
-        const unsigned char* at = static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride * tab_bytes(kType);
+        const unsigned char* at =
+            static_cast<const unsigned char*>(p.grad) + static_cast<long long>(row[u] < 0 ? ~row[u] : row[u]) * p.g_stride * tab_bytes(kType);
 #pragma unroll
         for (int i = 0; i < kEgEach; ++i) {
           const int h = eg_channel<1, kThreads>(slice, i);
@@ -1054,9 +1062,14 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
   cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
   cfg.gridDim = dim3(static_cast<unsigned>(p.buckets)); cfg.blockDim = dim3(kEsThreads);
   cfg.dynamicSmemBytes = static_cast<size_t>(EsLayout(p.R, p.warps, p.list, p.N <= UINT16_MAX ? 2 : 4).total);
+  const bool few_tokens = p.N <= UINT16_MAX;
   cudaError_t e;
-  if (p.wide) e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int64_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int64_t>, p);
-  else e = p.N <= UINT16_MAX ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int32_t>, p) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int32_t>, p);
+  if (p.wide)
+    e = few_tokens ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int64_t>, p)
+                   : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int64_t>, p);
+  else
+    e = few_tokens ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int32_t>, p)
+                   : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int32_t>, p);
   if (e != cudaSuccess) return e;
   const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
   const long long blank = p.first ? (static_cast<long long>(p.V) + p.blank - 1) / p.blank : 0;

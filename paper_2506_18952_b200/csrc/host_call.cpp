@@ -1,8 +1,9 @@
-// The host side of a call on torch tensors, in native code: reads the tensors, fills hola_verify_args and calls the C ABI;
-// makes the output tensors of a call that is given none (scores: all of it in one).  What a call costs the host bounds small problems.  us, Python -> native:
-// arguments filled and a call that is refused 3.5 -> 0.8, five output tensors 8.2 -> 5.1, seven 11.7 -> 7.0, beside 5 for the two
-// launches; whole calls: one sequence, V = 1000 10.45 -> 9.75; three, V = 5000, fresh outputs 19.75 -> 13.2; host entry, two sequences,
-// V = 10000 42.1 -> 37.4; mixed-width quantiser, 1000 x 128 50 -> 13.8.
+// The host side of a call on torch tensors, in native code: reads the tensors, fills hola_verify_args and calls the C ABI; makes
+// the output tensors of a call that is given none (scores, and the calls around the head: all of it in one).  What a call costs
+// the host bounds small problems.  us, Python -> native: arguments filled and a call that is refused 3.5 -> 0.8, five output
+// tensors 8.2 -> 5.1, seven 11.7 -> 7.0, beside 5 for the two launches; whole calls: one sequence, V = 1000 10.45 -> 9.75; three,
+// V = 5000, fresh outputs 19.75 -> 13.2; host entry, two sequences, V = 10000 42.1 -> 37.4; mixed-width quantiser, 1000 x 128 50
+// -> 13.8.
 //
 // call() takes the plain forms only (torch.Tensor or Parameter objects with storage, strided, contiguous, of the types that
 // the entry points know) and answers None for everything else, before it has done anything: the caller then goes the long
@@ -510,7 +511,8 @@ PyObject* beam_reorder(PyObject*, PyObject* const* v, Py_ssize_t n) {
 template <typename Args>
 const at::Tensor* token_ids(const Operands& in, PyObject* o, Args* a) {
   const at::Tensor* t = in.on_device(o);
-  if (!t || !t->is_contiguous() || t->numel() == 0 || t->numel() >= INT32_MAX || (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong)) return nullptr;
+  if (!t || !t->is_contiguous() || t->numel() == 0 || t->numel() >= INT32_MAX || (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong))
+    return nullptr;
   a->N = t->numel(); a->tokens = t->data_ptr(); a->wide_tokens = t->scalar_type() == at::kLong;
   return t;
 }

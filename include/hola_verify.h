@@ -357,8 +357,8 @@ hola_status hola_token_logprobs(const hola_logprobs_args* args, void* cuda_strea
  * that holds NaN or +inf, a score or logZ that is NaN or +inf, or a weight that is not positive and finite: that beam has no
  * candidates, and HOLA_FLAG_BAD_LOGIT is set. keep_slots (n = W): instead of by rank, the best child of a beam is written at that
  * beam's own place, so that its state need not move; the other candidates take the free places in their order. finished_out: 1 where
- * the parent had ended or the token is end_token. Outputs may not overlap inputs, but with n = W score_out may be score itself, and
- * finished_out finished. Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing,
+ * the parent had ended or the token is end_token. Outputs may not overlap inputs nor one another, but with n = W score_out may be score
+ * itself, and finished_out finished. Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing,
  * needs no context, and launched like hola_verify (programmatic stream serialization, waits before it reads). */
 #define HOLA_MAX_BEAMS 32
 typedef struct hola_beam_args {
@@ -390,7 +390,8 @@ hola_status hola_beam_select(const hola_beam_args* args, void* cuda_stream);
  * any order of the parents is allowed, and beams that stay where they are cost nothing.  From one buffer into another (which may not
  * overlap) every place is written.  A run is what lies side by side of one beam, for one index of the outer axes; with `used`, states
  * whose `position` is not 0 are moved up to used[b] positions only (at most the run; negative counts as 0), and the bytes behind are
- * left as they were. Beams may not share bytes (beam_stride >= run), nor may sequences or outer indices.  `states` is a host array,
+ * left as they were. Beams may not share bytes (beam_stride >= run), nor may sequences, outer indices or the
+ * states that are written.  `states` is a host array,
  * not looked at after the call; its pointers, parent and used are DEVICE pointers of the current device.  One launch for every 24
  * states.  Asynchronous on cuda_stream, allocates nothing, launched like hola_verify. */
 typedef struct hola_beam_state {
@@ -420,7 +421,8 @@ hola_status hola_beam_reorder(const hola_reorder_args* args, void* cuda_stream);
  * more where out is 16 bits wide. A token of -1 is none: out[r] = add[r], or 0.  Any other token outside the vocabulary: the same, and
  * HOLA_FLAG_BAD_TOKEN.  Of a vocabulary that is split over several tables this is one part: rows v_offset .. v_offset + V - 1 of
  * V_global (0: V, the whole); tokens of the other parts count as none, so that the parts' results add up. Every pointer but wmix is a
- * DEVICE pointer of the current device, rows at any distance.  add may be out.  Asynchronous on cuda_stream, allocates nothing, needs
+ * DEVICE pointer of the current device, rows at any distance.  add may be out; else out overlaps
+ * nothing that is read.  Asynchronous on cuda_stream, allocates nothing, needs
  * no context, launched like hola_verify. */
 typedef enum { HOLA_T_F32 = 0, HOLA_T_BF16 = 1, HOLA_T_F16 = 2, HOLA_T_INT8 = 3, HOLA_T_MIXED = 4 } hola_t_dtype;
 typedef struct hola_embed_args {
@@ -452,7 +454,7 @@ hola_status hola_embed(const hola_embed_args* args, void* cuda_stream);
  *     number; what lies behind is left as it was.  out and ids_out have room for N.
  * workspace: hola_embed_grad_workspace_bytes(N, V, H) bytes on the device, 16-byte aligned, of this call alone until it has run (the
  * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs
- * no context, two launches like hola_verify's. */
+ * no context, two launches like hola_verify's.  out overlaps neither grad nor tokens. */
 typedef struct hola_embed_grad_args {
   int64_t N;                /* 0 .. 2^25                                                                  */
   int32_t V, H;             /* V at most 2^30                                                             */

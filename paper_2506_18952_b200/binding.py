@@ -636,7 +636,8 @@ class BeamStates:
 
     axes: the axis of the sequences in each tensor (one number: in all), the beams' is the next one.  positions: for each tensor the axis that counts
     positions, of which only the first used[b] are moved, or None.  into: tensors that take the reordered states (double buffers; perhaps with
-    another number of beams), None: the tensors themselves.  Keep the object alive while calls that use it are in flight."""
+    another number of beams), None: the tensors themselves.  Tensors that are written share no memory.  Keep the object alive while calls
+    that use it are in flight."""
 
     def __init__(self, tensors, axes=0, positions=None, into=None):
         tensors = list(tensors)
@@ -657,6 +658,8 @@ class BeamStates:
         self.states = (hola_beam_state * len(tensors))()
         for st, x, y, axis, at in zip(self.states, tensors, targets, axes, positions):
             self._lay_out(st, x, y, axis, at)
+        if len({t.data_ptr() for t in targets if t.numel()}) != sum(t.numel() > 0 for t in targets):
+            raise HolaError("BeamStates: a tensor that would be reordered twice")
         if into is not None:
             spans = lambda ts: [(t.data_ptr(), t.data_ptr() + (sum((s - 1) * d for s, d in zip(t.shape, t.stride())) + 1) * t.element_size())   # noqa: E731
                                 for t in ts if t.numel()]

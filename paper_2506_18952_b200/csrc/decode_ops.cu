@@ -66,6 +66,17 @@ static bool overlap(const void* a, long long a_bytes, const void* b, long long b
   return a && b && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
 }
 
+// Whether rows of a_bytes and of b_bytes, each at one distance from the next, share a byte.  Two views that lie side by side in the rows of
+// one buffer do not; views of one stretch at different distances count as if they did.
+static bool rows_meet(const void* a, long long a_rows, long long a_apart, long long a_bytes, const void* b, long long b_rows, long long b_apart,
+                      long long b_bytes) {
+  if (!overlap(a, (a_rows - 1) * a_apart + a_bytes, b, (b_rows - 1) * b_apart + b_bytes)) return false;
+  if (a_rows <= 1 || b_rows <= 1 || a_apart != b_apart || a_apart == 0) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const long long d = static_cast<long long>((x < y ? y - x : x - y) % static_cast<uintptr_t>(a_apart));
+  return d < (x < y ? a_bytes : b_bytes) || d + (x < y ? b_bytes : a_bytes) > a_apart;
+}
+
 hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   if (!a || a->B < 0 || a->W <= 0 || a->V <= 0 || a->n <= 0 || a->seq_stride < 0 || a->beam_stride < 0) return HOLA_ERR_INVALID_ARG;
   if (a->l_dtype < HOLA_L_F32 || a->l_dtype > HOLA_L_F16) return HOLA_ERR_INVALID_ARG;
@@ -84,6 +95,9 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
       const bool itself = a->n == a->W && x.at == y.at && ((x.at == a->score && y.at == a->score_out) || (x.at == a->finished && y.at == a->finished_out));
       if (!itself && overlap(x.at, beams * x.bytes, y.at, kept * y.bytes)) return HOLA_ERR_INVALID_ARG;
     }
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].at, kept * out[i].bytes, out[j].at, kept * out[j].bytes)) return HOLA_ERR_INVALID_ARG;
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   BsParams p = {};
@@ -188,6 +202,12 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
       reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
     return HOLA_ERR_INVALID_ARG;
+  const long long apart = a->out_stride * oe, bytes = static_cast<long long>(a->H) * oe;
+  const bool itself = a->add == a->out && (a->N == 1 || a->add_stride == a->out_stride);
+  if ((!itself && rows_meet(a->add, a->N, a->add_stride * oe, bytes, a->out, a->N, apart, bytes)) ||
+      (!mixed && rows_meet(a->table, a->V, a->row_stride * te, static_cast<long long>(a->H) * te, a->out, a->N, apart, bytes)) ||
+      rows_meet(a->tokens, 1, 0, a->N * (a->wide_tokens ? 8 : 4), a->out, a->N, apart, bytes))
+    return HOLA_ERR_INVALID_ARG;
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   EmParams p = {};
@@ -236,6 +256,12 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->grad) % ge ||
       reinterpret_cast<uintptr_t>(a->out) % oe)
     return HOLA_ERR_INVALID_ARG;
+  if (a->N > 0) {
+    const long long rows = by_rows ? a->N : a->V, apart = a->out_stride * oe, bytes = static_cast<long long>(a->H) * oe;
+    if (rows_meet(a->grad, a->N, a->grad_stride * ge, static_cast<long long>(a->H) * ge, a->out, rows, apart, bytes) ||
+        rows_meet(a->tokens, 1, 0, a->N * (a->wide_tokens ? 8 : 4), a->out, rows, apart, bytes))
+      return HOLA_ERR_INVALID_ARG;
+  }
   const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + p.blank - 1) / p.blank) * p.slices;
   if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (!device_facts()) return HOLA_ERR_NO_DEVICE;

@@ -634,3 +634,23 @@ def test_scores_that_are_written_over(B):
     out = binding.BeamSelection(s, torch.empty((B, W), dtype=torch.int32, device="cuda"), torch.empty((B, W), dtype=torch.int32, device="cuda"), f)
     binding.hola_beam_select(l, z, s, W, f, 5, out=out)
     same(out, want)
+
+
+def test_outputs_on_one_another_and_states_twice_are_refused():
+    lib = binding.load_library()
+    a = binding.hola_beam_args()
+    a.B, a.W, a.V, a.n, a.seq_stride, a.beam_stride, a.end_token = 2, 4, 100, 4, 400, 100, 7
+    a.logits, a.logZ, a.score, a.score_out, a.parent, a.token, a.finished_out = 1 << 20, 4096, 8192, 12288, 16384, 20480, 24576
+    for name, at in (("parent", 12288), ("token", 16384), ("token", 20480 - 4096 + 28), ("finished_out", 12288 + 31), ("parent", 20480 + 28)):
+        kept = getattr(a, name)
+        setattr(a, name, at)
+        assert lib.hola_beam_select(ctypes.byref(a), None) == 1, name
+        setattr(a, name, kept)
+    x, y = torch.zeros((2, 4, 6)), torch.zeros((2, 4, 6))
+    for twice in (lambda: binding.BeamStates([x, x]), lambda: binding.BeamStates([x, x.view(2, 4, 3, 2)]),
+                  lambda: binding.BeamStates([x, x.clone()], into=[y, y])):
+        with pytest.raises(binding.HolaError):
+            twice()
+    kv = torch.zeros((2, 4, 2, 6))
+    binding.BeamStates(list(kv.unbind(2)) + [kv[:, :, :0], kv[:, :, :0]])            # (side by side in one buffer; nothing at all)
+    binding.BeamStates([x, x], into=[y, y.clone()])

@@ -602,3 +602,46 @@ def test_gradients_that_start_anywhere(H, g_dtype):
         check_grad(tokens, grad, V, 0.5, view)
         view.fill_(-3.0)
         assert (out == -3.0).all()
+
+
+def test_results_on_what_is_read_are_refused():
+    """Rows that share a byte with the table, the addend, the gradient or the tokens; views side by side in one buffer do not."""
+    lib = binding.load_library()
+    e = dict(table=1 << 20, tokens=1 << 16, out=1 << 24, out_stride=40, add_stride=40)
+    for kw in (dict(out=1 << 20, out_stride=16), dict(out=(1 << 20) - 4), dict(out=(1 << 20) + 9 * 64 + 60), dict(tokens=(1 << 24) + 64 - 4),
+               dict(add=(1 << 24) + 60), dict(add=(1 << 24) - 60), dict(add=(1 << 24) + 160 - 60), dict(add=1 << 24, add_stride=0),
+               dict(add=1 << 24, add_stride=16), dict(add=(1 << 24) + 160 + 60)):
+        assert lib.hola_embed(ctypes.byref(_embed_args(**{**e, **kw})), None) == 1, kw
+    beside = lib.hola_embed(ctypes.byref(_embed_args(**{**e, "add": (1 << 24) + 64})), None) if not torch.cuda.is_available() else 5
+    assert beside != 1                                        # (no device here: nothing runs)
+    a = binding.hola_embed_grad_args()
+    a.N, a.V, a.H, a.grad_stride, a.out_stride, a.workspace_bytes = 4, 10, 16, 16, 16, lib.hola_embed_grad_workspace_bytes(4, 10, 16)
+    a.tokens, a.grad, a.out, a.workspace = 1 << 16, 1 << 20, 1 << 24, 1 << 26
+    for kw in (dict(out=1 << 20), dict(out=(1 << 20) + 3 * 64 + 60), dict(out=(1 << 20) - 9 * 64 - 60), dict(tokens=(1 << 24) + 636), dict(out=(1 << 16) + 12)):
+        kept = {name: getattr(a, name) for name in kw}
+        for name, at in kw.items():
+            setattr(a, name, at)
+        assert lib.hola_embed_grad(ctypes.byref(a), None) == 1, kw
+        for name, at in kept.items():
+            setattr(a, name, at)
+
+
+@gpu
+def test_results_beside_what_is_read():
+    """Both halves of the rows of one buffer: the addend in one, the result in the other; and the addend itself."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for H in (64, 33):
+        table = torch.randn((50, H), generator=g, device="cuda")
+        t = torch.randint(50, (37,), generator=g, device="cuda")
+        buf = torch.randn((37, 2 * H), generator=g, device="cuda")
+        kept = buf.clone()
+        binding.hola_embed(t, table, 0.5, add=buf[:, H:], out=buf[:, :H])
+        assert torch.equal(buf[:, :H], kept[:, H:] + 0.5 * table[t]) and torch.equal(buf[:, H:], kept[:, H:])
+        binding.hola_embed(t, table, add=buf[:, H:], out=buf[:, H:])
+        assert torch.equal(buf[:, H:], kept[:, H:] + table[t])
+        with pytest.raises(binding.HolaError):
+            binding.hola_embed(t, table, add=buf[:, H:], out=buf[:, H - 1:-1])
+        with pytest.raises(binding.HolaError):
+            binding.hola_embed(t, table, out=table[:37])
+        with pytest.raises(binding.HolaError):
+            binding.hola_embed_grad(t[:20], buf[:20, :H], 37, out=buf[:, 1:H + 1])

@@ -262,7 +262,8 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
         rows_meet(a->tokens, 1, 0, a->N * (a->wide_tokens ? 8 : 4), a->out, rows, apart, bytes))
       return HOLA_ERR_INVALID_ARG;
   }
-  const long long ctas = ((a->N + p.window - 1) / p.window + 1 + (static_cast<long long>(a->V) + p.blank - 1) / p.blank) * p.slices;
+  const long long blank = (static_cast<long long>(a->V) + p.blank - 1) / p.blank;
+  const long long ctas = p.few ? blank + kEfPerSm * kEgPlanSms : ((a->N + p.window - 1) / p.window + 1 + blank) * p.slices;
   if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (!device_facts()) return HOLA_ERR_NO_DEVICE;
   p.tokens = a->tokens; p.wide = a->wide_tokens; p.v_offset = a->v_offset;

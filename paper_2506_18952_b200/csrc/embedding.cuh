@@ -471,7 +471,7 @@ cudaError_t launch_embed_of(const EmParams& p, int type, int out_type, bool word
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// dW[v] = scale * sum of g[r] over the rows r with tok[r] = v, in rising r, in fp32.  Two launches.
+// dW[v] = scale * sum of g[r] over the rows r with tok[r] = v, in rising r, in fp32.  Two launches (few tokens: embed_grad_few_kernel).
 //
 // 1. Tokens sorted (stable), with nothing exchanged between the CTAs: each takes a range of ids and reads all tokens, every warp a
 //    stretch of them, lists those inside its range, and counts those below it (where its part of the sorted order begins).  Counts per
@@ -503,6 +503,7 @@ struct EgParams {
   long long v_offset, V_global;
   int even, buckets, R, warps, chunk, list;      // sort: U, ranges of ids and how many a range holds at most, warps that count, tokens of a warp
                                        // and how many of them it lists
+  int few;                             // one launch does it, see embed_grad_few_kernel
   int S, S_log2, window, slices, blank;      // sums: piece, window, slices of the channels; rows of a CTA that writes zeros
   const void* grad;
   long long g_stride;
@@ -734,8 +735,8 @@ __global__ void __launch_bounds__(kEsThreads, 1) embed_sort_kernel(const __grid_
 // Eight channels of a thread, in runs that lie side by side: of 16 bytes of the gradient, or single ones where rows start anywhere.
 // (Eight at once out of the aligned words that hold them, as lookups take them, and turned round for the result: 9000 x 1001 bf16 26.3 -> 32.8 us.)
 template <int kRun, int kThreads>
-__device__ __forceinline__ int eg_channel(int slice, int i) {
-  return slice * (kThreads * kEgEach) + (i / kRun) * (kThreads * kRun) + static_cast<int>(threadIdx.x) * kRun + i % kRun;
+__device__ __forceinline__ int eg_channel(int slice, int i, int thread = static_cast<int>(threadIdx.x)) {
+  return slice * (kThreads * kEgEach) + (i / kRun) * (kThreads * kRun) + thread * kRun + i % kRun;
 }
 template <int kType>
 using EgWord = EmWord<kType, kEgEach>;
@@ -745,10 +746,11 @@ __host__ __device__ constexpr int eg_stages() { return 24 * 1024 / (kEgThreads *
 
 // The sums, scaled, to a row of the result (added to what is there), run by run.
 template <int kRun, int kThreads>
-__device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long long row, int slice, const float* sum) {
+__device__ __forceinline__ void eg_write(const EgParams& p, int out_type, long long row, int slice, const float* sum,
+                                         int thread = static_cast<int>(threadIdx.x)) {
 #pragma unroll
   for (int i = 0; i < kEgEach; i += kRun) {
-    const int h = eg_channel<kRun, kThreads>(slice, i);
+    const int h = eg_channel<kRun, kThreads>(slice, i, thread);
     if (h >= p.H) continue;
     const long long at = row * p.out_stride + h;
     float x[kRun];
@@ -1002,6 +1004,214 @@ __global__ void __launch_bounds__(kThreads, kThreads == kEgFewThreads ? 16 : kVe
   }
 }
 
+// Few tokens: all of it in one launch, without a workspace.  Every CTA reads all tokens and finds out, by a table in shared memory, which
+// are the first of their id and which ids have more than kEfAlone rows.  A token's row in the result is, by rows, the number of first ones
+// with smaller ids.  The other ids: a CTA takes every `groups`-th token, where it is the first of its id, for a share of the slices of 256
+// channels; votes say where the id occurs, and a warp adds up its rows in rising r.  Those with many rows are dealt out to all CTAs by 64
+// channels; eight lanes take a stretch of the rows, and the stretches are added up in their order.  Bound by latency: launch, tokens,
+// table, votes, rows.  us, sorted / so, V = 32000, by rows, fp32: 64 x 4096 9.4 / 3.5, 320 x 4096 9.7 / 6.1, 512 x 4096 10.3 / 8.7, tokens by
+// falling frequency 11.8 / 11.4, 512 x 1024 9.6 / 6.3, one id 13.9 / 9.2, 512 x 8192 11.7 / 11.6; beyond 512 tokens the votes and tables
+// of all CTAs cost more than a sort (1024 x 4096 11.8 / 14.8).  Whole table, 64 x 4096 80.4 / 73.5.
+constexpr int kEfMost = 512;           // tokens
+constexpr int kEfThreads = 256, kEfWarps = 8, kEfSlots = 2 * kEfMost;
+constexpr int kEfPerSm = 3;            // CTAs
+constexpr int kEfAlone = 16;            // rows of an id that a warp adds up by itself
+constexpr int kEfLanes = 8, kEfStretches = kEfThreads / kEfLanes;      // of an id with many rows
+
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(kEfThreads, kEfPerSm) embed_grad_few_kernel(const __grid_constant__ EgParams p, int out_type, int groups,
+                                                                                     int shares) {
+  constexpr int kRun = kVec ? kEgEach : 1, kAhead = kType == kTabF32 || !kVec ? 4 : 8, kNone = INT32_MAX, kMine = kEfMost / kEfThreads;
+  __shared__ int ids[kEfMost], distinct[kEfMost];        // rows of the table, -1: none; those of the tokens that are the first of their id
+  __shared__ int keys[kEfSlots], seen[kEfSlots], times[kEfSlots];      // ids, the first tokens that have them, how many do
+  __shared__ unsigned many[kEfMost / 32];                // bits: first tokens of ids with many rows
+  __shared__ unsigned short list[kEfMost];               // rows of the ids that this CTA adds up
+  __shared__ int at_of[kEfMost], row_of[kEfMost];        // the CTA's ids: places in the list, rows of the result
+  __shared__ int n_of[kEfMost];                          // rows of the ids of the tokens that are their first
+  __shared__ float part[kEfStretches][kEfLanes * kEgEach];
+  __shared__ int used;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  grid_dependency_wait();
+  grid_dependency_release();
+  if (blockIdx.x >= static_cast<unsigned>(groups * shares)) {
+    // The whole table: zeros to the rows of ids that do not occur, rows without a gap between them as one stretch.
+    const int v0 = (static_cast<int>(blockIdx.x) - groups * shares) * p.blank, n = min(p.blank, p.V - v0);
+    if (tid < n) n_of[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < p.N; i += kEfThreads) {
+      bool bad;
+      const int v = em_row(p.tokens, p.wide, i, p.V, p.v_offset, p.V_global, &bad);
+      if (v >= v0 && v < v0 + n) n_of[v - v0] = 1;
+    }
+    __syncthreads();
+    const int size = tab_bytes(out_type);
+    unsigned char* out = static_cast<unsigned char*>(p.out);
+    for (int i = 0; i < n; ++i) {
+      if (n_of[i]) continue;
+      int last = i;
+      while (p.out_stride == p.H && last + 1 < n && !n_of[last + 1]) ++last;
+      eg_zeros<kEfThreads>(out + (v0 + i) * p.out_stride * size, out + ((v0 + last) * p.out_stride + p.H) * size, size);
+      i = last;
+    }
+    return;
+  }
+  const int group = static_cast<int>(blockIdx.x) / shares, share = static_cast<int>(blockIdx.x) - group * shares;
+  const int slices = (p.slices + shares - 1) / shares, s0 = share * slices, s1 = min(s0 + slices, p.slices);
+  int id_of[kMine], slot[kMine];
+  bool bad_here = false;
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = tid + k * kEfThreads;
+    bool bad = false;
+    id_of[k] = i < p.N ? em_row(p.tokens, p.wide, i, p.V, p.v_offset, p.V_global, &bad) : -1;
+    ids[i] = id_of[k];
+    bad_here = bad_here || bad;
+  }
+  if (blockIdx.x == 0 && bad_here && p.status) atomicOr(p.status, HOLA_FLAG_BAD_TOKEN);
+  if (tid == 0) used = 0;
+  for (int i = tid; i < kEfSlots; i += kEfThreads) { keys[i] = -1; seen[i] = kNone; times[i] = 0; }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int id = id_of[k];
+    slot[k] = static_cast<int>((static_cast<uint32_t>(id) * 2654435761u) / (0x100000000ull / kEfSlots));
+    if (id < 0) continue;
+    for (int had = atomicCAS(&keys[slot[k]], -1, id); had != -1 && had != id; had = atomicCAS(&keys[slot[k]], -1, id))
+      slot[k] = (slot[k] + 1) & (kEfSlots - 1);          // (half of the places stay free)
+    atomicMin(&seen[slot[k]], tid + k * kEfThreads);
+    atomicAdd(&times[slot[k]], 1);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = tid + k * kEfThreads;
+    const bool first = id_of[k] >= 0 && seen[slot[k]] == i;
+    distinct[i] = first ? id_of[k] : kNone;
+    n_of[i] = first ? times[slot[k]] : 0;
+    const unsigned bits = __ballot_sync(0xffffffffu, first && times[slot[k]] > kEfAlone);
+    if (lane == 0) many[i >> 5] = bits;
+  }
+  __syncthreads();
+
+  // For a whole warp: the row of the result of the id of token i; its rows to the list from `at` on (-1: not).
+  auto find = [&](int id, int at) {
+    unsigned mask = 0;                                   // lane w: of tokens 32 w .. 32 w + 31
+    int smaller = 0;
+    for (int w = 0; w * 32 < p.N; ++w) {
+      const unsigned same = __ballot_sync(0xffffffffu, ids[w * 32 + lane] == id);
+      if (lane == w) mask = same;
+      smaller += distinct[w * 32 + lane] < id ? 1 : 0;
+    }
+    if (at >= 0) {
+      const int here = __popc(mask);
+      int upto = here;
+#pragma unroll
+      for (int o = 1; o < kEfMost / 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      for (int to = at + upto - here; mask; mask &= mask - 1u) list[to++] = static_cast<unsigned short>(lane * 32 + __ffs(mask) - 1);
+    }
+    return p.by_rows ? __reduce_add_sync(0xffffffffu, smaller) : id;
+  };
+  // A thread's eight channels of some rows of the list, `lanes` threads to a row, summed.
+  float sum[kEgEach];
+  auto add_up = [&](auto lanes, int slice, int thread, int from, int to) {
+#pragma unroll
+    for (int c = 0; c < kEgEach; ++c) sum[c] = 0.f;
+#pragma unroll 1
+    for (int x = from; x < to; x += kAhead) {
+      EmWord<kType, kRun> g[kAhead][kEgEach / kRun];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (x + u >= to) break;
+        const unsigned char* at = static_cast<const unsigned char*>(p.grad) + list[x + u] * p.g_stride * tab_bytes(kType);
+#pragma unroll
+        for (int i = 0; i < kEgEach / kRun; ++i) {
+          const int h = eg_channel<kRun, decltype(lanes)::value>(slice, i * kRun, thread);
+          if (h < p.H) g[u][i].load(at + static_cast<long long>(h) * tab_bytes(kType));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (x + u >= to) break;
+#pragma unroll
+        for (int c = 0; c < kEgEach; ++c) sum[c] = __fadd_rn(sum[c], g[u][c / kRun].get(c % kRun));
+      }
+    }
+  };
+
+  // Ids with many rows.
+  int items = 0, word = 0, passed = 0;
+  for (int w = 0; w < kEfMost / 32; ++w) items += __popc(many[w]);
+  const int cuts = (p.H + kEfLanes * kEgEach - 1) / (kEfLanes * kEgEach);
+  int found = -1, n = 0, row = 0;
+  for (long long item = blockIdx.x; item < static_cast<long long>(items) * cuts; item += groups * shares) {
+    const int which = static_cast<int>(item / cuts), cut = static_cast<int>(item - static_cast<long long>(which) * cuts);
+    if (which != found) {
+      for (; passed + __popc(many[word]) <= which; ++word) passed += __popc(many[word]);
+      unsigned bits = many[word];
+      for (int i = passed; i < which; ++i) bits &= bits - 1u;
+      const int i = word * 32 + __ffs(bits) - 1;
+      found = which;
+      n = n_of[i];
+      __syncthreads();                                   // (the list before it has been read)
+      row = find(ids[i], warp == 0 ? 0 : -1);
+      __syncthreads();
+    }
+    const int stretch = tid / kEfLanes, thread = tid % kEfLanes, each = (n + kEfStretches - 1) / kEfStretches;
+    add_up(std::integral_constant<int, kEfLanes>(), cut, thread, min(stretch * each, n), min((stretch + 1) * each, n));
+#pragma unroll
+    for (int c = 0; c < kEgEach; ++c) part[stretch][c * kEfLanes + thread] = sum[c];
+    __syncthreads();
+    if (tid < kEfLanes * kEgEach) {
+      float x = part[0][tid];
+#pragma unroll
+      for (int q = 1; q < kEfStretches; ++q) x = __fadd_rn(x, part[q][tid]);
+      part[0][tid] = x;
+    }
+    __syncthreads();
+    if (tid < kEfLanes) {
+#pragma unroll
+      for (int c = 0; c < kEgEach; ++c) sum[c] = part[0][c * kEfLanes + tid];
+      eg_write<kRun, kEfLanes>(p, out_type, row, cut, sum, tid);
+    }
+    __syncthreads();
+  }
+
+  // The CTA's other ids; whose row of the result holds which id.
+  const int mine = group < p.N ? (p.N - 1 - group) / groups + 1 : 0;
+  for (int k = warp; k < mine; k += kEfWarps) {
+    const int i = group + k * groups, id = ids[i], rows = n_of[i];
+    if (rows == 0) continue;
+    const bool here = rows <= kEfAlone;
+    if (!here && (!p.by_rows || share != 0)) continue;
+    int at = -1;
+    if (here) {
+      if (lane == 0) at = atomicAdd(&used, rows);
+      at = __shfl_sync(0xffffffffu, at, 0);
+    }
+    const int to = find(id, at);
+    if (p.by_rows && share == 0 && lane == 0) p.ids_out[to] = static_cast<int>(id + p.v_offset);
+    if (lane == 0) { at_of[k] = at; row_of[k] = to; }
+  }
+  __syncthreads();
+  // (a slice at a time to a warp, so that the slices of an id with several rows lie with several warps)
+  const int pieces = mine * (s1 - s0);
+  for (int x = warp; x < pieces; x += kEfWarps) {
+    const int k = x / (s1 - s0), s = s0 + (x - k * (s1 - s0)), rows = n_of[group + k * groups];
+    if (rows == 0 || rows > kEfAlone) continue;
+    add_up(std::integral_constant<int, 32>(), s, lane, at_of[k], at_of[k] + rows);
+    eg_write<kRun, 32>(p, out_type, row_of[k], s, sum, lane);
+  }
+  if (blockIdx.x == 0 && p.by_rows && warp == kEfWarps - 1) {
+    int count = 0;
+    for (int i = lane; i < kEfMost; i += 32) count += distinct[i] != kNone ? 1 : 0;
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (lane == 0) *p.count_out = count;
+  }
+}
+
 struct EgLayout {
   size_t places, numbers, first, distinct, valid, done, partial, total;
 };
@@ -1010,8 +1220,16 @@ struct EgLayout {
 bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   if (N < 0 || N > kEgMaxTokens || V <= 0 || H <= 0 || V > 1 << 30 || H > INT32_MAX - 4096) return false;
   p->N = static_cast<int>(N); p->V = V; p->H = H;
-  int warps = 1;
-  while (warps < kEsWarps && N > 64ll * warps) warps <<= 1;      // a warp's stretch: 64 tokens, or more once all count
+  p->few = N <= kEfMost;
+  if (p->few) {
+    *l = {};
+    l->total = 256;
+    p->slices = (H + 32 * kEgEach - 1) / (32 * kEgEach);
+    p->blank = kEgMaxWindow;
+    while (p->blank > 1 && V / p->blank < 16 * kEgPlanSms) p->blank >>= 1;
+    return true;
+  }
+  int warps = N > 2 * kEfMost ? kEsWarps : kEsWarps / 2;
   // Ranges: one per SM where their counters fit, else as many as it takes.  (A thread adds up two ids.)
   const int cell = N <= UINT16_MAX ? 2 : 4, most = (1 << kEsIdBits) - 2;
   int ids = (V + kEgPlanSms - kEsZipf) / (kEgPlanSms - kEsZipf + 1);
@@ -1023,7 +1241,6 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   p->list = room < kEsMaxList ? room : kEsMaxList;
   p->warps = warps;
   p->chunk = static_cast<int>(((N + warps - 1) / warps + 31) / 32 * 32);
-  if (p->chunk == 0) p->chunk = 32;
   p->R = ids;
   p->even = (V + ids - 1) / ids;
   p->buckets = p->even + kEsZipf - 1;
@@ -1054,7 +1271,25 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
 }
 
 template <int kType>
+cudaError_t launch_embed_grad_few(const EgParams& p, int out_type, bool vec, cudaStream_t stream) {
+  // (a token for every warp, and as many CTAs as there is room for: a share of the slices to each)
+  constexpr int kRoom = kEfPerSm * kEgPlanSms;
+  const int groups = p.N > kEfWarps ? (p.N + kEfWarps - 1) / kEfWarps : 1;
+  const int shares = kRoom / groups < p.slices ? kRoom / groups : p.slices;
+  const long long blank = p.by_rows || p.accumulate ? 0 : (static_cast<long long>(p.V) + p.blank - 1) / p.blank;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
+  cfg.gridDim = dim3(static_cast<unsigned>(static_cast<long long>(groups) * shares + blank)); cfg.blockDim = dim3(kEfThreads);
+  return vec ? cudaLaunchKernelEx(&cfg, embed_grad_few_kernel<kType, true>, p, out_type, groups, shares)
+             : cudaLaunchKernelEx(&cfg, embed_grad_few_kernel<kType, false>, p, out_type, groups, shares);
+}
+
+template <int kType>
 cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStream_t stream) {
+  if (p.few) return launch_embed_grad_few<kType>(p, out_type, vec, stream);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1071,7 +1306,7 @@ cudaError_t launch_embed_grad(const EgParams& p, int out_type, bool vec, cudaStr
     e = few_tokens ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint16_t, int32_t>, p)
                    : cudaLaunchKernelEx(&cfg, embed_sort_kernel<uint32_t, int32_t>, p);
   if (e != cudaSuccess) return e;
-  const long long windows = p.N > 0 ? (p.N + p.window - 1) / p.window : 1;      // (the first one reports the count)
+  const long long windows = (p.N + p.window - 1) / p.window;
   const long long blank = p.first ? (static_cast<long long>(p.V) + p.blank - 1) / p.blank : 0;
   const bool few = p.H <= kEgFewThreads * kEgEach;
   cfg.gridDim = dim3(static_cast<unsigned>((windows + blank) * p.slices)); cfg.blockDim = dim3(few ? kEgFewThreads : kEgThreads);

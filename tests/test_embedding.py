@@ -645,3 +645,57 @@ def test_results_beside_what_is_read():
             binding.hola_embed(t, table, out=table[:37])
         with pytest.raises(binding.HolaError):
             binding.hola_embed_grad(t[:20], buf[:20, :H], 37, out=buf[:, 1:H + 1])
+
+
+@gpu
+@pytest.mark.parametrize("g_dtype", FLOATS)
+@pytest.mark.parametrize("N", [0, 1, 17, 511, 512, 513, 700])
+def test_gradients_of_few_tokens_and_of_some_more(N, g_dtype):
+    """Ids with 15, 16, 17 and with most of the rows, absent and wrong tokens, results that lie apart, all forms of the result."""
+    V, wrong = 90, 3 if N > 17 else 0
+    for H in (5, 64, 72, 257, 2056):
+        t = torch.arange(N) % 5 * 18
+        for i, n in enumerate((15, 16, 17, 1, 2, 63, 64, 65)):
+            if N > 400:
+                t[sum((15, 16, 17, 1, 2, 63, 64, 65)[:i]):][:n] = 80 + i
+        t[N // 2:N // 2 + N // 7] = -1
+        if wrong:
+            t[:wrong] = torch.tensor([V, -2, 2 ** 31 - 1])
+        t = t[torch.randperm(N, generator=torch.Generator().manual_seed(N + H))].cuda()
+        t = t if H == 64 else t.int()
+        wide = rnd((N, H + 11), g_dtype, H)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        for grad in (wide[:, :H].contiguous(), wide[:, :H], wide[:, 3:H + 3]):
+            got = binding.hola_embed_grad(t, grad, V, 0.7, status=status)
+            check_grad(t, grad, V, 0.7, got)
+            base = rnd((V, H + 5), torch.float32, 6)
+            for lead in (0, 1):
+                out = base.clone()
+                binding.hola_embed_grad(t, grad, V, 0.7, out=out[:, lead:lead + H])
+                assert torch.equal(out[:, lead:lead + H], got)
+                out[:, lead:lead + H] = base[:, lead:lead + H]
+                assert torch.equal(out, base)
+                binding.hola_embed_grad(t, grad, V, 0.7, out=out[:, lead:lead + H], accumulate=True)
+                check_grad(t, grad, V, 0.7, out[:, lead:lead + H], before=base[:, lead:lead + H])
+            rows = binding.TokenRows(torch.full((N,), -7, dtype=torch.int32, device="cuda"), torch.full((N, H), -7.0, device="cuda"),
+                                     torch.full((1,), -7, dtype=torch.int32, device="cuda"))
+            binding.hola_embed_grad_rows(t, grad, V, 0.7, out=rows)
+            ids = sorted({v for v in t.tolist() if 0 <= v < V})
+            n = rows.count.item()
+            assert rows.ids[:n].tolist() == ids and (rows.ids[n:] == -7).all() and (rows.rows[n:] == -7).all()
+            assert torch.equal(rows.rows[:n], got[rows.ids[:n].long()])
+        assert status.item() == (binding.FLAG_BAD_TOKEN if wrong else 0)
+
+
+@gpu
+@pytest.mark.parametrize("N", [300, 600])
+def test_ids_of_few_tokens_that_share_places_of_the_table(N):
+    """Ids at equal distances of 2^20 and the largest ones, each some times, in a falling order."""
+    V = 2 ** 30
+    t = torch.cat([torch.arange(N // 3) * 2 ** 20, V - 1 - torch.arange(N // 3), torch.arange(N // 3) * 2 ** 20]).flip(0).cuda() % V
+    grad = torch.randint(-8, 9, (t.numel(), 8), device="cuda", generator=torch.Generator(device="cuda").manual_seed(4)).float()
+    rows = binding.hola_embed_grad_rows(t, grad, V)
+    ids, which = torch.unique(t, return_inverse=True)
+    n = rows.count.item()
+    assert torch.equal(rows.ids[:n].long(), ids)
+    assert torch.equal(rows.rows[:n], torch.zeros((n, 8), dtype=torch.float64, device="cuda").index_add_(0, which, grad.double()).float())

@@ -454,7 +454,8 @@ hola_status hola_embed(const hola_embed_args* args, void* cuda_stream);
  *     number; what lies behind is left as it was.  out and ids_out have room for N.
  * workspace: hola_embed_grad_workspace_bytes(N, V, H) bytes on the device, 16-byte aligned, of this call alone until it has run (the
  * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs
- * no context, one launch (up to 512 tokens) or two like hola_verify's.  out overlaps neither grad nor tokens. */
+ * no context, one launch (up to 512 tokens) or two like hola_verify's.  out, ids_out, count_out and the workspace overlap neither grad
+ * nor tokens nor one another. */
 typedef struct hola_embed_grad_args {
   int64_t N;                /* 0 .. 2^25                                                                  */
   int32_t V, H;             /* V at most 2^30                                                             */

@@ -61,20 +61,52 @@ static const DeviceFacts* device_facts() {
   return &facts[dev];
 }
 
-static bool overlap(const void* a, long long a_bytes, const void* b, long long b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
-}
+// Bytes of an operand: runs that start at every index of some axes, by falling stride.
+struct Bytes {
+  static constexpr int kAxes = 4;
+  uintptr_t at;                        // 0: no bytes
+  int axes = 0;
+  long long size[kAxes], stride[kAxes];
+  long long extent[kAxes + 1];         // from the first byte to behind the last one of what the axes from here on span
+  Bytes(const void* base, long long run) : at(run > 0 ? reinterpret_cast<uintptr_t>(base) : 0) { extent[0] = run; }
+  Bytes& along(long long n, long long apart) {           // (at most kAxes times; sizes of 1 are no axis)
+    if (n <= 0) at = 0;
+    if (n <= 1) return *this;
+    int i = axes++;
+    for (; i > 0 && stride[i - 1] < apart; --i) { size[i] = size[i - 1]; stride[i] = stride[i - 1]; }
+    size[i] = n;
+    stride[i] = apart;
+    long long run = extent[axes - 1];
+    for (i = axes; i >= 0; --i) {
+      extent[i] = run;
+      if (i > 0) run += (size[i - 1] - 1) * stride[i - 1];
+    }
+    return *this;
+  }
+};
 
-// Whether rows of a_bytes and of b_bytes, each at one distance from the next, share a byte.  Two views that lie side by side in the rows of
-// one buffer do not; views of one stretch at different distances count as if they did.
-static bool rows_meet(const void* a, long long a_rows, long long a_apart, long long a_bytes, const void* b, long long b_rows, long long b_apart,
-                      long long b_bytes) {
-  if (!overlap(a, (a_rows - 1) * a_apart + a_bytes, b, (b_rows - 1) * b_apart + b_bytes)) return false;
-  if (a_rows <= 1 || b_rows <= 1 || a_apart != b_apart || a_apart == 0) return true;
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  const long long d = static_cast<long long>((x < y ? y - x : x - y) % static_cast<uintptr_t>(a_apart));
-  return d < (x < y ? a_bytes : b_bytes) || d + (x < y ? b_bytes : a_bytes) > a_apart;
+// Whether a, from axis i on, and b, from axis j on, which begins d bytes behind it, share a byte: the longest stride left is taken first, of which
+// only indices matter whose spans meet (one or two, where strides are larger than what they step over).  Layouts for which
+// more than a few thousand pairs would have to be looked at count as if they did.
+static bool meet(const Bytes& a, int i, const Bytes& b, int j, long long d, int* looks) {
+  if (d >= a.extent[i] || d <= -b.extent[j]) return false;
+  if (i == a.axes && j == b.axes) return true;
+  if (++*looks > 4096) return true;
+  const long long s = i < a.axes ? a.stride[i] : -1, t = j < b.axes ? b.stride[j] : -1, step = s > t ? s : t;
+  if (step == 0) return meet(a, a.axes, b, b.axes, d, looks);
+  // (places of b behind those of a, in steps)
+  long long first = s == step ? -(a.size[i] - 1) : 0, last = t == step ? b.size[j] - 1 : 0;
+  if (s == step) ++i;
+  if (t == step) ++j;
+  auto down = [](long long x, long long y) { return x >= 0 ? x / y : -((y - 1 - x) / y); };
+  const long long from = down(-b.extent[j] - d, step) + 1, to = down(a.extent[i] - 1 - d, step);
+  for (long long k = first > from ? first : from; k <= (last < to ? last : to); ++k)
+    if (meet(a, i, b, j, d + k * step, looks)) return true;
+  return false;
+}
+static bool share(const Bytes& a, const Bytes& b) {
+  int looks = 0;
+  return a.at && b.at && meet(a, 0, b, 0, static_cast<long long>(b.at - a.at), &looks);
 }
 
 hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
@@ -93,11 +125,11 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   for (const auto& x : in)
     for (const auto& y : out) {
       const bool itself = a->n == a->W && x.at == y.at && ((x.at == a->score && y.at == a->score_out) || (x.at == a->finished && y.at == a->finished_out));
-      if (!itself && overlap(x.at, beams * x.bytes, y.at, kept * y.bytes)) return HOLA_ERR_INVALID_ARG;
+      if (!itself && share({x.at, beams * x.bytes}, {y.at, kept * y.bytes})) return HOLA_ERR_INVALID_ARG;
     }
   for (int i = 0; i < 4; ++i)
     for (int j = 0; j < i; ++j)
-      if (overlap(out[i].at, kept * out[i].bytes, out[j].at, kept * out[j].bytes)) return HOLA_ERR_INVALID_ARG;
+      if (share({out[i].at, kept * out[i].bytes}, {out[j].at, kept * out[j].bytes})) return HOLA_ERR_INVALID_ARG;
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   BsParams p = {};
@@ -202,11 +234,11 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
       reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
     return HOLA_ERR_INVALID_ARG;
-  const long long apart = a->out_stride * oe, bytes = static_cast<long long>(a->H) * oe;
+  const Bytes out = Bytes(a->out, static_cast<long long>(a->H) * oe).along(a->N, a->out_stride * oe);
   const bool itself = a->add == a->out && (a->N == 1 || a->add_stride == a->out_stride);
-  if ((!itself && rows_meet(a->add, a->N, a->add_stride * oe, bytes, a->out, a->N, apart, bytes)) ||
-      (!mixed && rows_meet(a->table, a->V, a->row_stride * te, static_cast<long long>(a->H) * te, a->out, a->N, apart, bytes)) ||
-      rows_meet(a->tokens, 1, 0, a->N * (a->wide_tokens ? 8 : 4), a->out, a->N, apart, bytes))
+  if ((!itself && share(Bytes(a->add, static_cast<long long>(a->H) * oe).along(a->N, a->add_stride * oe), out)) ||
+      (!mixed && share(Bytes(a->table, static_cast<long long>(a->H) * te).along(a->V, a->row_stride * te), out)) ||
+      share({a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, out))
     return HOLA_ERR_INVALID_ARG;
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
@@ -256,11 +288,16 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->grad) % ge ||
       reinterpret_cast<uintptr_t>(a->out) % oe)
     return HOLA_ERR_INVALID_ARG;
-  if (a->N > 0) {
-    const long long rows = by_rows ? a->N : a->V, apart = a->out_stride * oe, bytes = static_cast<long long>(a->H) * oe;
-    if (rows_meet(a->grad, a->N, a->grad_stride * ge, static_cast<long long>(a->H) * ge, a->out, rows, apart, bytes) ||
-        rows_meet(a->tokens, 1, 0, a->N * (a->wide_tokens ? 8 : 4), a->out, rows, apart, bytes))
-      return HOLA_ERR_INVALID_ARG;
+  // (CTAs read tokens and rows while others write results, and the sort's lists lie in the workspace)
+  const long long rows = by_rows ? a->N : a->V, width = a->H;
+  const Bytes in[] = {{a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, Bytes(a->grad, width * ge).along(a->N, a->grad_stride * ge)},
+              out[] = {Bytes(a->out, width * oe).along(rows, a->out_stride * oe), {a->ids_out, a->N * 4}, {a->count_out, 4},
+                       {a->workspace, static_cast<long long>(l.total)}};
+  for (int i = 0; i < 4; ++i) {
+    for (const Bytes& x : in)
+      if (share(x, out[i])) return HOLA_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (share(out[j], out[i])) return HOLA_ERR_INVALID_ARG;
   }
   const long long blank = (static_cast<long long>(a->V) + p.blank - 1) / p.blank;
   const long long ctas = p.few ? blank + kEfPerSm * kEgPlanSms : ((a->N + p.window - 1) / p.window + 1 + blank) * p.slices;

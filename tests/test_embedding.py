@@ -699,3 +699,47 @@ def test_ids_of_few_tokens_that_share_places_of_the_table(N):
     n = rows.count.item()
     assert torch.equal(rows.ids[:n].long(), ids)
     assert torch.equal(rows.rows[:n], torch.zeros((n, 8), dtype=torch.float64, device="cuda").index_add_(0, which, grad.double()).float())
+
+
+def test_gradients_by_rows_on_what_is_read_or_on_one_another_are_refused():
+    """CTAs read the tokens and the gradient while others write ids, rows and their number."""
+    lib = binding.load_library()
+    a = binding.hola_embed_grad_args()
+    for N in (4, 600):                                        # (one launch, and two)
+        need = lib.hola_embed_grad_workspace_bytes(N, 10, 16)
+        a.N, a.V, a.H, a.grad_stride, a.out_stride, a.workspace_bytes = N, 10, 16, 16, 20, need
+        ok = dict(tokens=1 << 16, grad=1 << 20, out=1 << 24, ids_out=1 << 28, count_out=1 << 29, workspace=1 << 30)
+        for name, at in ok.items():
+            setattr(a, name, at)
+        row, last = 4 * N, (1 << 24) + 80 * (N - 1)
+        for kw in (dict(ids_out=1 << 16), dict(ids_out=(1 << 16) + row - 4), dict(ids_out=(1 << 16) - row + 4), dict(ids_out=1 << 20),
+                   dict(ids_out=(1 << 20) + 64 * N - 4), dict(ids_out=1 << 24), dict(count_out=1 << 16), dict(count_out=(1 << 16) + row - 4),
+                   dict(count_out=(1 << 20) + 60), dict(count_out=last + 60), dict(count_out=1 << 28), dict(count_out=(1 << 28) + row - 4),
+                   dict(workspace=1 << 16), dict(workspace=1 << 20), dict(workspace=1 << 24), dict(workspace=1 << 28), dict(tokens=(1 << 30) + need - 4),
+                   dict(count_out=(1 << 30) + 8), dict(grad=(1 << 30) + need - 4), dict(out=(1 << 30) - last + (1 << 24) - 60)):
+            for name, at in kw.items():
+                setattr(a, name, at)
+            assert lib.hola_embed_grad(ctypes.byref(a), None) == 1, (N, kw)
+            for name in kw:
+                setattr(a, name, ok[name])
+        if not torch.cuda.is_available():                     # (no device here: nothing runs)
+            for kw in ({}, dict(count_out=last + 64), dict(ids_out=(1 << 16) + row), dict(count_out=(1 << 28) + row)):
+                for name, at in kw.items():
+                    setattr(a, name, at)
+                assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1), (N, kw)
+                for name in kw:
+                    setattr(a, name, ok[name])
+
+
+@gpu
+@pytest.mark.parametrize("N", [300, 600])
+def test_ids_in_the_tokens_place_are_refused(N, monkeypatch):
+    t, grad = some_tokens(N, 50, 1), rnd((N, 16), torch.float32, 2)
+    kept = t.clone()
+    rows, count = torch.zeros((N, 16), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for _ in range(2):                                        # through the native helper and without it
+        for out in (binding.TokenRows(t, rows, count), binding.TokenRows(torch.zeros_like(t), grad, count), binding.TokenRows(torch.zeros_like(t), rows, t[:1])):
+            with pytest.raises(binding.HolaError):
+                binding.hola_embed_grad_rows(t, grad, 50, out=out)
+        monkeypatch.setattr(binding, "_host", None)
+    assert torch.equal(t, kept)

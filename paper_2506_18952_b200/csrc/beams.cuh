@@ -176,7 +176,8 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
     const int live = __popc(live_mask);
     if (warp == 0) {
       const double off = static_cast<double>(score) - static_cast<double>(logZ);
-      const float b = static_cast<float>(off * static_cast<double>(weight));
+      // (kept finite: an entry of -inf stays -inf beside it)
+      const float b = fminf(fmaxf(static_cast<float>(off * static_cast<double>(weight)), -3.402823466e38f), 3.402823466e38f);
       if (live_mask >> lane & 1u) {
         BsRow& row = s.rows[__popc(live_mask & ((1u << lane) - 1u))];
         const T* at = static_cast<const T*>(p.logits) + static_cast<size_t>(seq) * p.seq_stride + static_cast<size_t>(lane) * p.beam_stride;

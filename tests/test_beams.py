@@ -654,3 +654,25 @@ def test_outputs_on_one_another_and_states_twice_are_refused():
     kv = torch.zeros((2, 4, 2, 6))
     binding.BeamStates(list(kv.unbind(2)) + [kv[:, :, :0], kv[:, :, :0]])            # (side by side in one buffer; nothing at all)
     binding.BeamStates([x, x], into=[y, y.clone()])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,seen", [(4096, 3), (4096, 9), (8192, 5), (3000, 2), (30000, 3)])
+def test_masks_of_both_kinds_beside_offsets_beyond_fp32(V, seen, dtype):
+    """A few entries at the lowest value of fp32 and -inf behind them: the logZ is that low too, and an offset times a weight above 1 is more
+    than fp32 holds.  (Only entries that are there count, and each of them once.)"""
+    low = torch.finfo(torch.float32).min
+    for W, n in ((1, 4), (3, 7), (2, 32)):
+        l = torch.full((4, W, V), -math.inf, device="cuda", dtype=dtype)
+        l[..., :seen] = torch.finfo(dtype).min
+        l[1, ..., V // 2:V // 2 + seen] = 0.5 * torch.finfo(dtype).min
+        l[2, ..., ::8] = torch.finfo(dtype).min
+        z = torch.full((4, W), low, device="cuda")
+        s = torch.full((4, W), -3.0, device="cuda")
+        z[3] = -low                                           # (and far above what is there)
+        for weight in (1.0, 1.5, 3.0, 1e30):
+            w = torch.full((4, W), weight, device="cuda")
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            same(binding.hola_beam_select(l, z, s, n, weight=w, status=status), reference(l, z, s, n, weight=w))
+            assert status.item() == 0

@@ -427,7 +427,7 @@ hola_status hola_beam_reorder(const hola_reorder_args* args, void* cuda_stream);
 typedef enum { HOLA_T_F32 = 0, HOLA_T_BF16 = 1, HOLA_T_F16 = 2, HOLA_T_INT8 = 3, HOLA_T_MIXED = 4 } hola_t_dtype;
 typedef struct hola_embed_args {
   int64_t N;                /* tokens, >= 0                                                               */
-  int32_t V, H;             /* rows and channels of the table                                             */
+  int32_t V, H;             /* rows and channels of the table, H at most 2^30                              */
   int32_t v_offset, V_global;
   const void* tokens;       /* int32 [N], or int64 (wide_tokens)                                          */
   int32_t wide_tokens;

@@ -217,7 +217,7 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (a->v_offset < 0 || a->V_global < 0 || (a->V_global > 0 && static_cast<long long>(a->v_offset) + a->V > a->V_global)) return HOLA_ERR_INVALID_ARG;
   if (a->V_global == 0 && a->v_offset != 0) return HOLA_ERR_INVALID_ARG;
   const bool mixed = a->t_dtype == HOLA_T_MIXED;
-  if (a->N > INT32_MAX || a->H > INT32_MAX - 65536 || (mixed && a->H % 128 != 0)) return HOLA_ERR_UNSUPPORTED_SHAPE;
+  if (a->N > INT32_MAX || a->H > kEmMaxH || (mixed && a->H % 128 != 0)) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (a->N == 0) return HOLA_OK;
   if (!a->tokens || !a->out || (a->N > 1 && a->out_stride < a->H)) return HOLA_ERR_INVALID_ARG;
   if (mixed) {

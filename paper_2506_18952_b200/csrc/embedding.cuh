@@ -4,6 +4,7 @@
 // out[r] = add[r] + scale * W[tok[r]], every operation one rounding in fp32 (the scale of a quantised row first), the result rounded
 // once more where it is stored in 16 bits.
 constexpr int kEmThreads = 128;
+constexpr int kEmMaxH = 1 << 30;       // channels: 32 bits count them, and a step of 65535 slices (at most 2^27 channels) beyond the last one
 
 // Types of rows in memory (hola_t_dtype).
 enum { kTabF32 = HOLA_T_F32, kTabBf16 = HOLA_T_BF16, kTabF16 = HOLA_T_F16, kTabInt8 = HOLA_T_INT8, kTabMixed = HOLA_T_MIXED };
@@ -319,6 +320,7 @@ __global__ void __launch_bounds__(kEmThreads, 8) embed_kernel(const __grid_const
 template <int kType, bool kWide, bool kAdd, int n>
 cudaError_t launch_embed(const EmParams& p, int out_type, int num_sms, cudaStream_t stream) {
   constexpr int kAtOnce = n == 1 ? 4 : n;
+  static_assert(65535ll * kEmThreads * kAtOnce <= INT32_MAX - kEmMaxH, "a channel behind the row still fits 32 bits");
   // (fewer threads to a row where the last of several slices would leave more than an eighth of them idle)
   int log2 = 0;
   while ((1 << log2) < kEmThreads && (1 << log2) * kAtOnce < p.H) ++log2;

@@ -743,3 +743,29 @@ def test_ids_in_the_tokens_place_are_refused(N, monkeypatch):
                 binding.hola_embed_grad_rows(t, grad, 50, out=out)
         monkeypatch.setattr(binding, "_host", None)
     assert torch.equal(t, kept)
+
+
+def test_channels_that_32_bits_do_not_step_over_are_refused():
+    """Every type of the table, rows on aligned addresses and on others."""
+    lib = binding.load_library()
+    for H, refused in ((2 ** 31 - 65537, True), (2 ** 31 - 65536, True), (2010000000, True), (2 ** 30 + 128, True), (2 ** 30, False), (2 ** 30 - 1, False)):
+        for t_dtype, lead in ((0, 0), (1, 0), (2, 4), (3, 0), (3, 1)):
+            a = _embed_args(N=1, V=2, H=H, t_dtype=t_dtype, row_stride=H, out_stride=H, table=(1 << 20) + lead, out=1 << 44, w_scale=1 << 45 if t_dtype == 3 else None)
+            if refused:
+                assert lib.hola_embed(ctypes.byref(a), None) == 2, (H, t_dtype)
+            elif not torch.cuda.is_available():               # (no device here: nothing runs)
+                assert lib.hola_embed(ctypes.byref(a), None) not in (0, 1, 2), (H, t_dtype)
+
+
+@gpu
+@pytest.mark.parametrize("H,lead", [(2 ** 27 + 24, 0), (2 ** 26 + 1001, 1)])
+def test_rows_of_more_channels_than_slices_of_a_launch(H, lead):
+    table = torch.randint(-20000, 20000, (2 * H + lead,), device="cuda", dtype=torch.int16, generator=torch.Generator(device="cuda").manual_seed(1))
+    table = table.view(torch.bfloat16)[lead:].view(2, H)
+    out = torch.zeros((3, H), dtype=torch.bfloat16, device="cuda")
+    binding.hola_embed(torch.tensor([1, -1, 0], device="cuda"), table, out=out)
+    # (the bits of -127 .. -1 are NaN, which comes out as a NaN, perhaps another one; everything else bit by bit)
+    for got, want in ((out[0], table[1]), (out[2], table[0])):
+        nan = want.isnan()
+        assert bool((got.isnan() == nan).all()) and bool(((got.view(torch.int16) == want.view(torch.int16)) | nan).all())
+    assert int(out[1].count_nonzero()) == 0

@@ -452,8 +452,9 @@ hola_status hola_embed(const hola_embed_args* args, void* cuda_stream);
  *     left as they are.
  *   by rows (ids_out and count_out given): the distinct tokens in rising order, out[i] the row of ids_out[i], count_out their
  *     number; what lies behind is left as it was.  out and ids_out have room for N.
- * workspace: hola_embed_grad_workspace_bytes(N, V, H) bytes on the device, 16-byte aligned, of this call alone until it has run (the
- * library is not told what it holds; nothing is kept there from call to call).  Asynchronous on cuda_stream, allocates nothing, needs
+ * workspace: hola_embed_grad_workspace_bytes(N, V, H) bytes on the device, 16-byte aligned, which serve any smaller number of tokens of
+ * the same V and H as well; of this call alone until it has run (the library is not told what it holds; nothing is kept there from
+ * call to call).  Asynchronous on cuda_stream, allocates nothing, needs
  * no context, one launch (up to 512 tokens) or two like hola_verify's.  out, ids_out, count_out and the workspace overlap neither grad
  * nor tokens nor one another. */
 typedef struct hola_embed_grad_args {

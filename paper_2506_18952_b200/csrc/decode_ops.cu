@@ -267,7 +267,7 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
 size_t hola_embed_grad_workspace_bytes(long long N, int V, int H) {
   EgParams p = {};
   EgLayout l;
-  return eg_plan(N, V, H, &p, &l) ? l.total : 0;
+  return eg_plan(N, V, H, &p, &l) ? l.enough : 0;
 }
 
 hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {

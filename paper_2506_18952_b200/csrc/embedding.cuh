@@ -1216,6 +1216,7 @@ __global__ void __launch_bounds__(kEfThreads, kEfPerSm) embed_grad_few_kernel(co
 
 struct EgLayout {
   size_t places, numbers, first, distinct, valid, done, partial, total;
+  size_t enough;                       // for as many tokens and for any smaller number
 };
 
 // Host: the cut of the work.  False: sizes that are not served.
@@ -1225,7 +1226,7 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   p->few = N <= kEfMost;
   if (p->few) {
     *l = {};
-    l->total = 256;
+    l->total = l->enough = 256;
     p->slices = (H + 32 * kEgEach - 1) / (32 * kEgEach);
     p->blank = kEgMaxWindow;
     while (p->blank > 1 && V / p->blank < 16 * kEgPlanSms) p->blank >>= 1;
@@ -1266,9 +1267,17 @@ bool eg_plan(long long N, int V, int H, EgParams* p, EgLayout* l) {
   l->first = take((static_cast<size_t>(V) + 1) * 4);
   l->distinct = take(static_cast<size_t>(p->buckets) * 4);
   l->valid = take(4);
-  l->done = take(pieces * p->slices * 4);
-  l->partial = take(2 * pieces * p->slices * slice * 4);
-  l->total = at;
+  const size_t lists = at;
+  auto sums = [&](size_t n) {                            // what n pieces need, behind the lists
+    at = lists;
+    l->done = take(n * p->slices * 4);
+    l->partial = take(2 * n * p->slices * slice * 4);
+    return at;
+  };
+  // (pieces double in length where there would be more than 512, so that fewer tokens may have more of them; the lists only grow)
+  const size_t by_32 = static_cast<size_t>((N + 31) / 32);
+  l->enough = sums(by_32 < 512 ? by_32 : pieces < 512 ? 512 : pieces);
+  l->total = sums(pieces);
   return true;
 }
 

@@ -769,3 +769,20 @@ def test_rows_of_more_channels_than_slices_of_a_launch(H, lead):
         nan = want.isnan()
         assert bool((got.isnan() == nan).all()) and bool(((got.view(torch.int16) == want.view(torch.int16)) | nan).all())
     assert int(out[1].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("V,H", [(1, 1), (300, 16), (32000, 4096), (128256, 256), (128256, 257), (2 ** 30, 64)])
+def test_a_workspace_for_many_tokens_serves_fewer(V, H):
+    """The size that is asked for rises with the number of tokens, across all borders of the plan, and the call takes the size for more."""
+    lib = binding.load_library()
+    borders = [1, 512, 1024, 65535, *(512 * 32 * 2 ** i for i in range(6)), 2 ** 25 - 1]
+    counts = sorted({n for b in borders for n in (b - 1, b, b + 1, b + 40)} | {int(1.03 ** i) for i in range(1, 586)})
+    sizes = [lib.hola_embed_grad_workspace_bytes(n, V, H) for n in counts if n <= 2 ** 25]
+    assert sizes == sorted(sizes) and min(sizes) > 0
+    a = binding.hola_embed_grad_args()
+    a.V, a.H, a.grad_stride, a.out_stride, a.tokens, a.grad, a.out, a.workspace = V, H, 0, H, 1 << 40, 1 << 41, 1 << 50, 1 << 45
+    a.ids_out, a.count_out = 1 << 42, 1 << 43
+    for n, more in zip(counts, sizes[1:]):
+        a.N, a.workspace_bytes = n, more
+        if not torch.cuda.is_available():                     # (no device here: nothing runs)
+            assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1), n

@@ -387,11 +387,12 @@ hola_status hola_beam_select(const hola_beam_args* args, void* cuda_stream);
 
 /* The beams' states in the order of their parents: new[b][i] = old[b][parent[b][i]] for i < n, for any number of states at once (token
  * histories, keys and values, page tables).  parent -1: that place is left as it was.  In place (src = dst, for all states or none)
- * any order of the parents is allowed, and beams that stay where they are cost nothing.  From one buffer into another (which may not
- * overlap) every place is written.  A run is what lies side by side of one beam, for one index of the outer axes; with `used`, states
+ * any order of the parents is allowed, and beams that stay where they are cost nothing.  From one buffer into another every place is
+ * written.  A run is what lies side by side of one beam, for one index of the outer axes; with `used`, states
  * whose `position` is not 0 are moved up to used[b] positions only (at most the run; negative counts as 0), and the bytes behind are
- * left as they were. Beams may not share bytes (beam_stride >= run), nor may sequences, outer indices or the
- * states that are written.  `states` is a host array,
+ * left as they were.  No byte that is written is another one's: beams (beam_stride >= run), sequences and outer indices of a state
+ * share none, nor does a state's dst with its src (but in place), parent or used, all of which are refused; that different states
+ * share none with what another one writes is the caller's part, and hola_beam_states_check looks at it.  `states` is a host array,
  * not looked at after the call; its pointers, parent and used are DEVICE pointers of the current device.  One launch for every 24
  * states.  Asynchronous on cuda_stream, allocates nothing, launched like hola_verify. */
 typedef struct hola_beam_state {
@@ -415,6 +416,9 @@ typedef struct hola_reorder_args {
   uint32_t* status_word;             /* in/out [1], optional                                              */
 } hola_reorder_args;
 hola_status hola_beam_reorder(const hola_reorder_args* args, void* cuda_stream);
+/* Whether hola_beam_reorder can take these states (B, W, n, count and states of args; the others are not looked at), and whether what one of
+ * them writes is no part of another one: HOLA_ERR_INVALID_ARG where it is.  On the host alone, once for states that stay where they are. */
+hola_status hola_beam_states_check(const hola_reorder_args* args);
 
 /* Rows of a table by token:  out[r] = add[r] + scale * W[tokens[r]],  the table in any storage form of the LM head (tied weights) or
  * fp32 / fp16.  Every operation is one rounding in fp32 (for the quantised forms w_scale * code first), the result is rounded once

@@ -17,7 +17,7 @@ import torch
 
 from . import build as _build
 
-HOLA_OK = 0
+HOLA_OK, HOLA_ERR_INVALID_ARG = 0, 1
 HOLA_Q_BF16, HOLA_Q_F32 = 0, 1
 HOLA_GATE_TARGET_ENTROPY, HOLA_GATE_DRAFT_ENTROPY = 0, 1
 HOLA_FALLBACK_SAMPLE, HOLA_FALLBACK_GREEDY = 0, 1
@@ -33,7 +33,7 @@ HOLA_OPT_RING_SLOTS, HOLA_OPT_ROTATING_UNITS, HOLA_OPT_HOST_OVERLAP, HOLA_OPT_HO
 
 EXPORTS = ["hola_create", "hola_destroy", "hola_workspace_bytes", "hola_verify", "hola_verify_host",
            "hola_lm_head_entropy", "hola_accept_sample", "hola_host_traffic", "hola_shard_record_bytes", "hola_shard_lm_head",
-           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_lm_head_adapters", "hola_verify_adapters", "hola_token_logprobs", "hola_beam_select", "hola_beam_reorder", "hola_embed", "hola_embed_grad", "hola_embed_grad_workspace_bytes", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
+           "hola_shard_accept", "hola_shard_sample", "hola_lm_head_entropy_static", "hola_lm_head_adapters", "hola_verify_adapters", "hola_token_logprobs", "hola_beam_select", "hola_beam_reorder", "hola_beam_states_check", "hola_embed", "hola_embed_grad", "hola_embed_grad_workspace_bytes", "hola_quantize_w8", "hola_quantize_w4", "hola_quantize_mixed", "hola_quantize_mixed_widths", "hola_plan", "hola_plan_ex", "hola_plan_for_shape", "hola_hidden_form_for_shape", "hola_sample_plan_for_shape", "hola_set_option", "hola_selftest_bounded_wait", "hola_selftest_staged_wait", "hola_selftest_mass_wait", "hola_selftest_pace", "hola_selftest_quotient", "hola_profile_begin", "hola_profile_end", "hola_strerror", "hola_last_cuda_error",
            "hola_version"]
 
 
@@ -177,6 +177,8 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = [ctypes.POINTER(args), ctypes.c_void_p]
+    lib.hola_beam_states_check.restype = ctypes.c_int
+    lib.hola_beam_states_check.argtypes = [ctypes.POINTER(hola_reorder_args)]
     lib.hola_embed_grad_workspace_bytes.restype = ctypes.c_size_t
     lib.hola_embed_grad_workspace_bytes.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
     lib.hola_quantize_w8.restype = ctypes.c_int
@@ -636,8 +638,8 @@ class BeamStates:
 
     axes: the axis of the sequences in each tensor (one number: in all), the beams' is the next one.  positions: for each tensor the axis that counts
     positions, of which only the first used[b] are moved, or None.  into: tensors that take the reordered states (double buffers; perhaps with
-    another number of beams), None: the tensors themselves.  Tensors that are written share no memory.  Keep the object alive while calls
-    that use it are in flight."""
+    another number of beams), None: the tensors themselves.  Tensors that are written share no byte with one another nor with what is read;
+    views side by side in one buffer do not.  Keep the object alive while calls that use it are in flight."""
 
     def __init__(self, tensors, axes=0, positions=None, into=None):
         tensors = list(tensors)
@@ -658,15 +660,16 @@ class BeamStates:
         self.states = (hola_beam_state * len(tensors))()
         for st, x, y, axis, at in zip(self.states, tensors, targets, axes, positions):
             self._lay_out(st, x, y, axis, at)
-        if len({t.data_ptr() for t in targets if t.numel()}) != sum(t.numel() > 0 for t in targets):
-            raise HolaError("BeamStates: a tensor that would be reordered twice")
-        if into is not None:
-            spans = lambda ts: [(t.data_ptr(), t.data_ptr() + (sum((s - 1) * d for s, d in zip(t.shape, t.stride())) + 1) * t.element_size())   # noqa: E731
-                                for t in ts if t.numel()]
-            written = spans(targets)
-            if any(a < d and c < b for a, b in written for c, d in spans(tensors)):
-                raise HolaError("BeamStates: a target overlaps a source")
         self.address, self.count = ctypes.addressof(self.states), len(tensors)
+        a = hola_reorder_args()
+        a.B, a.W, a.n, a.count, a.states = self.B, self.W, self.n, self.count, self.address
+        if into is not None and any(x.data_ptr() == y.data_ptr() and x.numel() for x, y in zip(tensors, targets)):
+            raise HolaError("BeamStates: a target overlaps its source")
+        lib = load_library()
+        status = lib.hola_beam_states_check(ctypes.byref(a))
+        if status == HOLA_ERR_INVALID_ARG:
+            raise HolaError("BeamStates: what is written shares memory with itself, with another state or with what is read")
+        _check(lib, None, status, "BeamStates")
 
     def _lay_out(self, st, x, y, axis, at):
         if not 0 <= axis <= x.dim() - 2 or tuple(x.shape[axis:axis + 2]) != (self.B, self.W):

@@ -30,6 +30,67 @@ namespace {
 #include "beams.cuh"
 #include "embedding.cuh"
 
+// ------------------------------------------------------------------------------------------------ bytes that operands share
+// Bytes of an operand: runs that start at every index of some axes, by falling stride.
+struct Bytes {
+  static constexpr int kAxes = 4;
+  uintptr_t at;                        // 0: no bytes
+  int axes = 0;
+  long long size[kAxes], stride[kAxes];
+  long long extent[kAxes + 1];         // from the first byte to behind the last one of what the axes from here on span
+  struct Axis { long long size, apart; };
+  Bytes(const void* base, long long run) : Bytes(base, run, nullptr, 0) {}
+  template <int n>
+  Bytes(const void* base, long long run, const Axis (&along)[n]) : Bytes(base, run, along, n) { static_assert(n <= kAxes, "axes"); }
+
+ private:
+  Bytes(const void* base, long long run, const Axis* along, int n) : at(run > 0 ? reinterpret_cast<uintptr_t>(base) : 0) {
+    for (int k = 0; k < n; ++k) {
+      if (along[k].size <= 0) at = 0;
+      if (along[k].size <= 1) continue;
+      int i = axes++;
+      for (; i > 0 && stride[i - 1] < along[k].apart; --i) { size[i] = size[i - 1]; stride[i] = stride[i - 1]; }
+      size[i] = along[k].size;
+      stride[i] = along[k].apart;
+    }
+    extent[axes] = run;
+    for (int i = axes; i > 0; --i) extent[i - 1] = extent[i] + (size[i - 1] - 1) * stride[i - 1];
+  }
+};
+
+// Whether a, from axis i on, and b, from axis j on, which begins d bytes behind it, share a byte: the longest stride left is taken first, of which
+// only indices matter whose spans meet (one or two, where strides are larger than what they step over).  Layouts for which
+// more than a few thousand pairs would have to be looked at count as if they did.
+bool meet(const Bytes& a, int i, const Bytes& b, int j, long long d, int* looks) {
+  if (d >= a.extent[i] || d <= -b.extent[j]) return false;
+  if (i == a.axes && j == b.axes) return true;
+  if (++*looks > 4096) return true;
+  const long long s = i < a.axes ? a.stride[i] : -1, t = j < b.axes ? b.stride[j] : -1, step = s > t ? s : t;
+  if (step == 0) return meet(a, a.axes, b, b.axes, d, looks);
+  // (places of b behind those of a, in steps)
+  long long first = s == step ? -(a.size[i] - 1) : 0, last = t == step ? b.size[j] - 1 : 0;
+  if (s == step) ++i;
+  if (t == step) ++j;
+  auto down = [](long long x, long long y) { return x >= 0 ? x / y : -((y - 1 - x) / y); };
+  const long long from = down(-b.extent[j] - d, step) + 1, to = down(a.extent[i] - 1 - d, step);
+  for (long long k = first > from ? first : from; k <= (last < to ? last : to); ++k)
+    if (meet(a, i, b, j, d + k * step, looks)) return true;
+  return false;
+}
+bool share(const Bytes& a, const Bytes& b) {
+  int looks = 0;
+  return a.at && b.at && meet(a, 0, b, 0, static_cast<long long>(b.at - a.at), &looks);
+}
+
+// Whether two indices of a's axes from i on have a byte in common.
+bool shares_with_itself(const Bytes& a) {
+  int looks = 0;
+  for (int i = 0; i < a.axes; ++i)
+    for (long long k = 1; k < a.size[i] && k * a.stride[i] < a.extent[i + 1]; ++k)       // (nothing to do where strides are larger than what they step over)
+      if (meet(a, i + 1, a, i + 1, k * a.stride[i], &looks)) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -59,54 +120,6 @@ static const DeviceFacts* device_facts() {
   facts[dev] = f;
   known[dev].store(true, std::memory_order_release);
   return &facts[dev];
-}
-
-// Bytes of an operand: runs that start at every index of some axes, by falling stride.
-struct Bytes {
-  static constexpr int kAxes = 4;
-  uintptr_t at;                        // 0: no bytes
-  int axes = 0;
-  long long size[kAxes], stride[kAxes];
-  long long extent[kAxes + 1];         // from the first byte to behind the last one of what the axes from here on span
-  Bytes(const void* base, long long run) : at(run > 0 ? reinterpret_cast<uintptr_t>(base) : 0) { extent[0] = run; }
-  Bytes& along(long long n, long long apart) {           // (at most kAxes times; sizes of 1 are no axis)
-    if (n <= 0) at = 0;
-    if (n <= 1) return *this;
-    int i = axes++;
-    for (; i > 0 && stride[i - 1] < apart; --i) { size[i] = size[i - 1]; stride[i] = stride[i - 1]; }
-    size[i] = n;
-    stride[i] = apart;
-    long long run = extent[axes - 1];
-    for (i = axes; i >= 0; --i) {
-      extent[i] = run;
-      if (i > 0) run += (size[i - 1] - 1) * stride[i - 1];
-    }
-    return *this;
-  }
-};
-
-// Whether a, from axis i on, and b, from axis j on, which begins d bytes behind it, share a byte: the longest stride left is taken first, of which
-// only indices matter whose spans meet (one or two, where strides are larger than what they step over).  Layouts for which
-// more than a few thousand pairs would have to be looked at count as if they did.
-static bool meet(const Bytes& a, int i, const Bytes& b, int j, long long d, int* looks) {
-  if (d >= a.extent[i] || d <= -b.extent[j]) return false;
-  if (i == a.axes && j == b.axes) return true;
-  if (++*looks > 4096) return true;
-  const long long s = i < a.axes ? a.stride[i] : -1, t = j < b.axes ? b.stride[j] : -1, step = s > t ? s : t;
-  if (step == 0) return meet(a, a.axes, b, b.axes, d, looks);
-  // (places of b behind those of a, in steps)
-  long long first = s == step ? -(a.size[i] - 1) : 0, last = t == step ? b.size[j] - 1 : 0;
-  if (s == step) ++i;
-  if (t == step) ++j;
-  auto down = [](long long x, long long y) { return x >= 0 ? x / y : -((y - 1 - x) / y); };
-  const long long from = down(-b.extent[j] - d, step) + 1, to = down(a.extent[i] - 1 - d, step);
-  for (long long k = first > from ? first : from; k <= (last < to ? last : to); ++k)
-    if (meet(a, i, b, j, d + k * step, looks)) return true;
-  return false;
-}
-static bool share(const Bytes& a, const Bytes& b) {
-  int looks = 0;
-  return a.at && b.at && meet(a, 0, b, 0, static_cast<long long>(b.at - a.at), &looks);
 }
 
 hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
@@ -143,13 +156,23 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   return e == cudaSuccess ? HOLA_OK : HOLA_ERR_CUDA;
 }
 
-hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
-  if (!a || a->B < 0 || a->W <= 0 || a->n <= 0 || a->count < 0 || a->parent_stride < 0) return HOLA_ERR_INVALID_ARG;
+// What is read of a state, and what is written (in place: the same).
+static Bytes state_read(const hola_reorder_args* a, const hola_beam_state& s) {
+  return {s.src, s.run, {{a->B, s.seq_stride}, {a->W, s.beam_stride}, {s.outer[0], s.outer_stride[0]}, {s.outer[1], s.outer_stride[1]}}};
+}
+static Bytes state_written(const hola_reorder_args* a, const hola_beam_state& s) {
+  return {s.dst, s.run, {{a->B, s.dst_seq_stride}, {s.src == s.dst ? a->W : a->n, s.dst_beam_stride}, {s.outer[0], s.dst_outer_stride[0]},
+                         {s.outer[1], s.dst_outer_stride[1]}}};
+}
+
+// Every state by itself, and beside what a call reads.  in_place: -1 where there is nothing to move.
+static hola_status look_at_states(const hola_reorder_args* a, bool call, int* in_place) {
+  *in_place = -1;
+  if (!a || a->B < 0 || a->W <= 0 || a->n <= 0 || a->count < 0 || (call && a->parent_stride < 0)) return HOLA_ERR_INVALID_ARG;
   if (a->W > kBsMaxBeams || a->n > kBsMaxBeams) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (a->B == 0 || a->count == 0) return HOLA_OK;
-  if (!a->states || !a->parent) return HOLA_ERR_INVALID_ARG;
-  // (all states are looked at before the first launch)
-  int in_place = -1;
+  if (!a->states || (call && !a->parent)) return HOLA_ERR_INVALID_ARG;
+  const Bytes parent(call ? a->parent : nullptr, a->n * 4ll, {{a->B, a->parent_stride * 4}}), used(call ? a->used : nullptr, a->B * 4ll);
   for (int i = 0; i < a->count; ++i) {
     const hola_beam_state& s = a->states[i];
     if (s.run < 0 || s.position < 0 || s.outer[0] < 0 || s.outer[1] < 0) return HOLA_ERR_INVALID_ARG;
@@ -158,8 +181,8 @@ hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
         s.dst_beam_stride < 0 || s.dst_outer_stride[0] < 0 || s.dst_outer_stride[1] < 0)
       return HOLA_ERR_INVALID_ARG;
     const bool here = s.src == s.dst;
-    if (in_place >= 0 && in_place != static_cast<int>(here)) return HOLA_ERR_INVALID_ARG;
-    in_place = here;
+    if (*in_place >= 0 && *in_place != static_cast<int>(here)) return HOLA_ERR_INVALID_ARG;
+    *in_place = here;
     if (here && (a->n > a->W || s.seq_stride != s.dst_seq_stride || s.beam_stride != s.dst_beam_stride ||
                  s.outer_stride[0] != s.dst_outer_stride[0] || s.outer_stride[1] != s.dst_outer_stride[1]))
       return HOLA_ERR_INVALID_ARG;
@@ -168,8 +191,30 @@ hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
     if (pieces > INT32_MAX || s.outer[0] > INT32_MAX || s.outer[1] > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
     const double ctas = static_cast<double>(pieces) * a->B * static_cast<double>(s.outer[0]) * static_cast<double>(s.outer[1]);
     if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
+    const Bytes to = state_written(a, s);
+    if (shares_with_itself(to) || (!here && share(state_read(a, s), to)) || share(parent, to) || share(used, to)) return HOLA_ERR_INVALID_ARG;
   }
-  if (in_place < 0) return HOLA_OK;
+  return HOLA_OK;
+}
+
+hola_status hola_beam_states_check(const hola_reorder_args* a) {
+  int in_place;
+  const hola_status status = look_at_states(a, false, &in_place);
+  if (status != HOLA_OK || in_place < 0) return status;
+  for (int i = 0; i < a->count; ++i) {
+    const Bytes to = state_written(a, a->states[i]);
+    for (int j = 0; j < a->count; ++j)
+      if ((j < i && share(state_written(a, a->states[j]), to)) || (j != i && !in_place && share(state_read(a, a->states[j]), to)))
+        return HOLA_ERR_INVALID_ARG;
+  }
+  return HOLA_OK;
+}
+
+hola_status hola_beam_reorder(const hola_reorder_args* a, void* cuda_stream) {
+  // (all states are looked at before the first launch)
+  int in_place;
+  const hola_status status = look_at_states(a, true, &in_place);
+  if (status != HOLA_OK || in_place < 0) return status;
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   const int sms = dev->sms;
@@ -234,10 +279,10 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
       reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
     return HOLA_ERR_INVALID_ARG;
-  const Bytes out = Bytes(a->out, static_cast<long long>(a->H) * oe).along(a->N, a->out_stride * oe);
+  const Bytes out(a->out, static_cast<long long>(a->H) * oe, {{a->N, a->out_stride * oe}});
   const bool itself = a->add == a->out && (a->N == 1 || a->add_stride == a->out_stride);
-  if ((!itself && share(Bytes(a->add, static_cast<long long>(a->H) * oe).along(a->N, a->add_stride * oe), out)) ||
-      (!mixed && share(Bytes(a->table, static_cast<long long>(a->H) * te).along(a->V, a->row_stride * te), out)) ||
+  if ((!itself && share({a->add, static_cast<long long>(a->H) * oe, {{a->N, a->add_stride * oe}}}, out)) ||
+      (!mixed && share({a->table, static_cast<long long>(a->H) * te, {{a->V, a->row_stride * te}}}, out)) ||
       share({a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, out))
     return HOLA_ERR_INVALID_ARG;
   const DeviceFacts* dev = device_facts();
@@ -290,8 +335,8 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
     return HOLA_ERR_INVALID_ARG;
   // (CTAs read tokens and rows while others write results, and the sort's lists lie in the workspace)
   const long long rows = by_rows ? a->N : a->V, width = a->H;
-  const Bytes in[] = {{a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, Bytes(a->grad, width * ge).along(a->N, a->grad_stride * ge)},
-              out[] = {Bytes(a->out, width * oe).along(rows, a->out_stride * oe), {a->ids_out, a->N * 4}, {a->count_out, 4},
+  const Bytes in[] = {{a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, {a->grad, width * ge, {{a->N, a->grad_stride * ge}}}},
+              out[] = {{a->out, width * oe, {{rows, a->out_stride * oe}}}, {a->ids_out, a->N * 4}, {a->count_out, 4},
                        {a->workspace, static_cast<long long>(l.total)}};
   for (int i = 0; i < 4; ++i) {
     for (const Bytes& x : in)

@@ -676,3 +676,77 @@ def test_masks_of_both_kinds_beside_offsets_beyond_fp32(V, seen, dtype):
             status = torch.zeros(1, dtype=torch.int32, device="cuda")
             same(binding.hola_beam_select(l, z, s, n, weight=w, status=status), reference(l, z, s, n, weight=w))
             assert status.item() == 0
+
+
+def test_states_that_share_bytes_are_refused():
+    """Parts of one buffer: side by side they are states of their own, in place and from one half into the other; with a byte in common they
+    are not."""
+    buf = torch.zeros((3, 4, 2, 12))
+    x, y = buf[:, :, 0], buf[:, :, 1]
+    binding.BeamStates([x], into=[y])                         # (interleaved)
+    binding.BeamStates([buf[..., :6], buf[..., 6:]])
+    binding.BeamStates([x, y])
+    binding.BeamStates([buf[:, :, 0, :4], buf[:, :, 1, 6:]], into=[buf[:, :, 0, 4:8], buf[:, :, 1, :6]])
+    halves = torch.zeros((3, 8, 12))
+    binding.BeamStates([halves[:, :4]], into=[halves[:, 4:]])
+    turns = torch.zeros((2, 12, 3, 4))                        # layers first, time-major
+    binding.BeamStates([torch.zeros(99).as_strided((3, 4, 2, 2), (4, 12, 2, 1))])       # (4 b + 12 w: a fourth sequence would be on the next beam)
+    binding.BeamStates([turns[0], turns[1]], axes=1)
+    binding.BeamStates([turns[0]], axes=1, into=[turns[1]])
+    for bad in (lambda: binding.BeamStates([buf[:, :, 0, :4], buf[:, :, 1, 4:]], into=[buf[:, :, 0, 4:8], buf[:, :, 1, :8]]),       # (4 .. 7 of the second)
+                lambda: binding.BeamStates([buf[..., :8], buf[..., 4:]]), lambda: binding.BeamStates([x, buf[:, :, 0, 11:]]),
+                lambda: binding.BeamStates([x, y.clone()], into=[x.clone(), x]), lambda: binding.BeamStates([x], into=[buf.view(3, 4, 24)[..., 11:23]]),
+                lambda: binding.BeamStates([x, y], into=[torch.zeros_like(x), x]), lambda: binding.BeamStates([x, y], into=[y, torch.zeros_like(x)]),
+                lambda: binding.BeamStates([x.clone(), y.clone()], into=[buf[..., 0, :8], buf[..., 0, 4:]]),
+                lambda: binding.BeamStates([halves[:, :4]], into=[halves[:, 3:7]]), lambda: binding.BeamStates([torch.zeros(99).unfold(0, 12, 1)[:12].view(3, 4, 12)]),
+                lambda: binding.BeamStates([torch.zeros(99).as_strided((4, 4, 2, 2), (4, 12, 2, 1))])):
+        with pytest.raises(binding.HolaError):
+            bad()
+
+
+def test_calls_on_states_that_share_bytes_are_refused():
+    """The C entry: a state's own two sides, its own sequences, and what the call reads besides."""
+    lib = binding.load_library()
+    a = binding.hola_reorder_args()
+    a.B, a.W, a.n, a.count, a.parent, a.parent_stride, a.used = 2, 4, 4, 1, 1 << 20, 4, 1 << 21
+
+    def status(check=False, parent=1 << 20, used=1 << 21, **kw):
+        s = (binding.hola_beam_state * 1)(_state(**{"src": 1 << 24, "dst": 1 << 25, **kw}))
+        a.states, a.parent, a.used = ctypes.addressof(s), parent, used
+        return lib.hola_beam_states_check(ctypes.byref(a)) if check else lib.hola_beam_reorder(ctypes.byref(a), None)
+
+    src = 1 << 24
+    for kw in (dict(dst=src + 100), dict(dst=src + 99), dict(dst=src - 1), dict(dst=src + 799), dict(dst=src + 50, beam_stride=200, seq_stride=800),
+               dict(dst=src, dst_seq_stride=500), dict(dst_seq_stride=399), dict(dst=src, seq_stride=399, dst_seq_stride=399)):
+        assert status(**kw) == 1 and status(True, **kw) == 1, kw
+    for kw in (dict(parent=1 << 25), dict(parent=(1 << 25) + 799), dict(parent=(1 << 25) - 31), dict(used=(1 << 25) + 796), dict(used=(1 << 25) - 4)):
+        assert status(**kw) == 1, kw
+    fine = [dict(), dict(dst=src), dict(dst=src + 800), dict(dst=src - 800), dict(parent=(1 << 25) + 800), dict(used=(1 << 25) - 8),
+            dict(dst=src + 100, beam_stride=200, seq_stride=800, dst_beam_stride=200, dst_seq_stride=800)]
+    for kw in fine:
+        if "parent" not in kw and "used" not in kw:
+            assert status(True, **kw) == 0, kw
+        if not torch.cuda.is_available():                     # (no device here: nothing runs)
+            assert status(**kw) not in (0, 1), kw
+    both = (binding.hola_beam_state * 2)(_state(src=src, dst=src), _state(src=src + 800, dst=src + 800))
+    a.states, a.count = ctypes.addressof(both), 2
+    assert lib.hola_beam_states_check(ctypes.byref(a)) == 0
+    both[1].src = both[1].dst = src + 799
+    assert lib.hola_beam_states_check(ctypes.byref(a)) == 1
+    assert lib.hola_beam_states_check(None) == 1
+
+
+@gpu
+def test_states_side_by_side_in_one_buffer():
+    B, W, T = 3, 5, 37
+    for used in (None, torch.tensor([4, 37, 0], dtype=torch.int32, device="cuda")):
+        buf = anything((B, W, 2, T, 3), torch.float16, 1)
+        parent = some_parents(B, W, W, 2)
+        want = reordered([buf[:, :, 0]], [buf[:, :, 1]], [0], [2], parent, used)
+        kept = buf[:, :, 0].clone()
+        binding.hola_beam_reorder(binding.BeamStates([buf[:, :, 0]], 0, [2], [buf[:, :, 1]]), parent, used)
+        assert equal([buf[:, :, 1]], want) and equal([buf[:, :, 0]], [kept.cpu()])
+        xs = [buf[..., :1], buf[..., 1:]]                     # (channels)
+        want = reordered(xs, xs, [0, 0], [None, None], parent)
+        binding.hola_beam_reorder(binding.BeamStates(xs), parent)
+        assert equal(xs, want)

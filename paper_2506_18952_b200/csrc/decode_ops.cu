@@ -78,8 +78,10 @@ bool meet(const Bytes& a, int i, const Bytes& b, int j, long long d, int* looks)
   return false;
 }
 bool share(const Bytes& a, const Bytes& b) {
+  const long long d = static_cast<long long>(b.at - a.at);
+  if (!a.at || !b.at || d >= a.extent[0] || d <= -b.extent[0]) return false;
   int looks = 0;
-  return a.at && b.at && meet(a, 0, b, 0, static_cast<long long>(b.at - a.at), &looks);
+  return meet(a, 0, b, 0, d, &looks);
 }
 
 // Whether two indices of a's axes from i on have a byte in common.
@@ -130,7 +132,8 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   if (a->end_token < -1 || a->end_token >= a->V || (a->finished && a->end_token < 0)) return HOLA_ERR_INVALID_ARG;
   if (a->B == 0) return HOLA_OK;
   if (!a->logits || !a->logZ || !a->score || !a->score_out || !a->parent || !a->token) return HOLA_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(a->logits) % (a->l_dtype == HOLA_L_F32 ? 4 : 2)) return HOLA_ERR_INVALID_ARG;
+  const int entry = a->l_dtype == HOLA_L_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(a->logits) % entry) return HOLA_ERR_INVALID_ARG;
   // A sequence is written when all of it has been read; another one's beams may lie where its candidates go, but for the same layout.
   const long long beams = static_cast<long long>(a->B) * a->W, kept = static_cast<long long>(a->B) * a->n;
   const struct { const void* at; int bytes; } in[] = {{a->score, 4}, {a->logZ, 4}, {a->weight, 4}, {a->finished, 1}},
@@ -140,6 +143,9 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
       const bool itself = a->n == a->W && x.at == y.at && ((x.at == a->score && y.at == a->score_out) || (x.at == a->finished && y.at == a->finished_out));
       if (!itself && share({x.at, beams * x.bytes}, {y.at, kept * y.bytes})) return HOLA_ERR_INVALID_ARG;
     }
+  const Bytes rows(a->logits, static_cast<long long>(a->V) * entry, {{a->B, a->seq_stride * entry}, {a->W, a->beam_stride * entry}});
+  for (int i = 0; i < 4; ++i)
+    if (share({out[i].at, kept * out[i].bytes}, rows)) return HOLA_ERR_INVALID_ARG;
   for (int i = 0; i < 4; ++i)
     for (int j = 0; j < i; ++j)
       if (share({out[i].at, kept * out[i].bytes}, {out[j].at, kept * out[j].bytes})) return HOLA_ERR_INVALID_ARG;

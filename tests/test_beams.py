@@ -750,3 +750,22 @@ def test_states_side_by_side_in_one_buffer():
         want = reordered(xs, xs, [0, 0], [None, None], parent)
         binding.hola_beam_reorder(binding.BeamStates(xs), parent)
         assert equal(xs, want)
+
+
+def test_selections_into_their_logits_are_refused():
+    """Results on an entry of any row; behind the rows and between them there is room."""
+    lib = binding.load_library()
+    base = 1 << 24
+    for l_dtype, e in ((binding.HOLA_L_F32, 4), (binding.HOLA_L_BF16, 2), (binding.HOLA_L_F16, 2)):
+        a = _args(logits=base, l_dtype=l_dtype, seq_stride=800, beam_stride=200, end_token=5, finished_out=1 << 22)      # rows of 100 entries, 200 apart
+        row = 100 * e
+        for name, length in (("score_out", 32), ("parent", 32), ("token", 32), ("finished_out", 8)):
+            kept = getattr(a, name)
+            for at in (base, base + row - length, base + 2 * row, base + 7 * 2 * row + row - 4, base - length + 4, base + 4 * 2 * row - length + 4):
+                setattr(a, name, at)
+                assert lib.hola_beam_select(ctypes.byref(a), None) == 1, (l_dtype, name, at - base)
+            for at in (base + row, base + 2 * row - length, base + 7 * 2 * row + row, base - length):
+                setattr(a, name, at)
+                if not torch.cuda.is_available():             # (no device here: nothing runs)
+                    assert lib.hola_beam_select(ctypes.byref(a), None) not in (0, 1), (l_dtype, name, at - base)
+            setattr(a, name, kept)

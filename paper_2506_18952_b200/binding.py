@@ -567,7 +567,7 @@ class BeamSelection:
     score: torch.Tensor                 # fp32 [B, n]
     parent: torch.Tensor                # int32 [B, n]
     token: torch.Tensor                 # int32 [B, n]
-    finished: torch.Tensor | None       # bool [B, n], where beams can end
+    finished: torch.Tensor | None       # bool [B, n], where beams can end (given all the same: filled with False)
 
 
 def _same(what, t, dtype, size, dev, name):
@@ -626,7 +626,7 @@ def hola_beam_select(logits: torch.Tensor, logZ: torch.Tensor, score: torch.Tens
             torch.empty((B, n), dtype=torch.int32, device=dev), torch.empty((B, n), dtype=torch.bool, device=dev) if ends else None))
     a.score_out = _same(what, out.score, torch.float32, (B, n), dev, "out.score")
     a.parent, a.token = (_same(what, t, torch.int32, (B, n), dev, "out") for t in (out.parent, out.token))
-    if ends:
+    if ends or out.finished is not None:                         # (where no beam can end, none has)
         a.finished_out = _same(what, out.finished, torch.bool, (B, n), dev, "out.finished")
     with torch.cuda.device(dev):
         _check(lib, None, lib.hola_beam_select(ctypes.byref(a), _stream_ptr(stream)), what)

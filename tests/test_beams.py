@@ -769,3 +769,17 @@ def test_selections_into_their_logits_are_refused():
                 if not torch.cuda.is_available():             # (no device here: nothing runs)
                     assert lib.hola_beam_select(ctypes.byref(a), None) not in (0, 1), (l_dtype, name, at - base)
             setattr(a, name, kept)
+
+
+@gpu
+def test_results_of_a_call_with_ends_filled_again_without():
+    """What an earlier call has left in out.finished does not stay there."""
+    l, z, s = make(3, 4, 200, torch.float32, 11)
+    f = torch.ones((3, 4), dtype=torch.bool, device="cuda")
+    out = binding.hola_beam_select(l, z, s, finished=f, end_token=7)
+    assert out.finished.all()
+    for keep in (False, True):
+        out.finished.fill_(True)
+        binding.hola_beam_select(l, z, s, keep_slots=keep, out=out)
+        same(out, reference(l, z, s, 4, keep_slots=keep))
+        assert not out.finished.any()

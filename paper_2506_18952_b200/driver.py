@@ -49,13 +49,21 @@ class SyntheticPair:
     def _norm(self, h, prev1):
         return h / h.norm(dim=-1, keepdim=True) * self.gain[prev1].unsqueeze(-1)
 
+    @staticmethod
+    def _rows(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, add: torch.Tensor | None = None) -> torch.Tensor:
+        """add + scale * table[tokens].  (Tokens on the host, of models to be compared with: by plain indexing.)"""
+        if tokens.is_cuda:
+            return binding.hola_embed(tokens.contiguous(), table, scale=scale, add=add)
+        rows = table[tokens] * scale
+        return rows if add is None else add + rows
+
     def target_hidden(self, prev1: torch.Tensor, prev2: torch.Tensor) -> torch.Tensor:
         """Verifier trunk stand-in: hidden state for the position that follows (..., prev2, prev1).  bf16 [..., H]."""
-        return self.target_hidden_from(prev1, binding.hola_embed(prev2.contiguous(), self.E2, scale=0.35))
+        return self.target_hidden_from(prev1, self._rows(prev2, self.E2, 0.35))
 
     def target_hidden_from(self, prev1: torch.Tensor, state: torch.Tensor) -> torch.Tensor:
         """The same from what the trunk keeps of the token before, 0.35 E2[prev2], fp32 [..., H]."""
-        return self._norm(binding.hola_embed(prev1.contiguous(), self.E1, add=state), prev1).to(torch.bfloat16)
+        return self._norm(self._rows(prev1, self.E1, add=state), prev1).to(torch.bfloat16)
 
     def draft_table(self) -> torch.Tensor:
         """The draft's own copy of its embedding table, for hsd_decode's distill."""
@@ -63,7 +71,7 @@ class SyntheticPair:
 
     def draft_probs(self, prev1: torch.Tensor, table: torch.Tensor | None = None) -> torch.Tensor:
         """Draft model stand-in: q(. | prev1), fp32 [..., V].  table: the draft's own embedding table."""
-        e = binding.hola_embed(prev1.contiguous(), self.E1 if table is None else table)
+        e = self._rows(prev1, self.E1 if table is None else table)
         h = self._norm(e, prev1).to(torch.bfloat16).float()
         return torch.softmax(h @ self.W_lm.float().T, dim=-1)
 

@@ -786,3 +786,15 @@ def test_a_workspace_for_many_tokens_serves_fewer(V, H):
         a.N, a.workspace_bytes = n, more
         if not torch.cuda.is_available():                     # (no device here: nothing runs)
             assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1), n
+
+
+def test_the_drivers_models_on_the_host():
+    """Hidden rows and draft probabilities of models that lie on the CPU, from the tables as they are."""
+    from paper_2506_18952_b200 import driver
+    models = driver.SyntheticPair(300, 32, 3, torch.device("cpu"))
+    g = torch.Generator().manual_seed(1)
+    a, b = torch.randint(0, 300, (2, 5, 6), generator=g).unbind(0)
+    want = models._norm(models.E1[a] + 0.35 * models.E2[b], a).to(torch.bfloat16)
+    assert torch.equal(models.target_hidden(a, b), want) and torch.equal(models.target_hidden(a.t(), b.t()), want.transpose(0, 1))
+    h = models._norm(models.E1[a], a).to(torch.bfloat16).float()
+    assert torch.equal(models.draft_probs(a), torch.softmax(h @ models.W_lm.float().T, dim=-1))

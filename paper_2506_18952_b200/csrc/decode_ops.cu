@@ -287,10 +287,17 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
     return HOLA_ERR_INVALID_ARG;
   const Bytes out(a->out, static_cast<long long>(a->H) * oe, {{a->N, a->out_stride * oe}});
   const bool itself = a->add == a->out && (a->N == 1 || a->add_stride == a->out_stride);
-  if ((!itself && share({a->add, static_cast<long long>(a->H) * oe, {{a->N, a->add_stride * oe}}}, out)) ||
-      (!mixed && share({a->table, static_cast<long long>(a->H) * te, {{a->V, a->row_stride * te}}}, out)) ||
-      share({a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, out))
+  const long long H = a->H;
+  if ((!itself && share({a->add, H * oe, {{a->N, a->add_stride * oe}}}, out)) || share({a->tokens, a->N * (a->wide_tokens ? 8 : 4)}, out) ||
+      share({a->w_scale, a->V * 4ll}, out) || (!mixed && share({a->table, H * te, {{a->V, a->row_stride * te}}}, out)))
     return HOLA_ERR_INVALID_ARG;
+  if (mixed) {
+    const hola_wmix& m = *a->wmix;
+    const long long groups = (static_cast<long long>(a->V) + 255) / 256;
+    for (const Bytes& x : {Bytes(m.W16, m.rows16 * H * 2), Bytes(m.W8, m.rows8 * H), Bytes(m.W4, m.rows4 * (H / 2)), Bytes(m.shift4, m.rows4 * (H / 128)),
+                           Bytes(m.group_width, groups), Bytes(m.group_row, groups * 4)})
+      if (share(x, out)) return HOLA_ERR_INVALID_ARG;
+  }
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   EmParams p = {};

@@ -798,3 +798,29 @@ def test_the_drivers_models_on_the_host():
     assert torch.equal(models.target_hidden(a, b), want) and torch.equal(models.target_hidden(a.t(), b.t()), want.transpose(0, 1))
     h = models._norm(models.E1[a], a).to(torch.bfloat16).float()
     assert torch.equal(models.draft_probs(a), torch.softmax(h @ models.W_lm.float().T, dim=-1))
+
+
+def test_results_on_scales_codes_and_their_tables_are_refused():
+    """What a lookup in the quantised forms reads beside the table: one byte of it in one row of the result."""
+    lib = binding.load_library()
+    out, N, V, H = 1 << 30, 3, 600, 128
+    last = out + 2 * 160 * 4 + 4 * H                          # (rows of fp32, 160 entries apart)
+    a = _embed_args(N=N, V=V, H=H, t_dtype=3, row_stride=H, out=out, out_stride=160, w_scale=1 << 24, table=1 << 20)
+    for at, status in ((out, 1), (last - 4, 1), (out - 4 * V + 4, 1), (last, 0), (out - 4 * V, 0)):
+        a.w_scale = at
+        if status or not torch.cuda.is_available():           # (no device here: nothing runs)
+            assert (lib.hola_embed(ctypes.byref(a), None) == 1) == bool(status), at
+    mix = binding.hola_wmix()
+    sizes = dict(W16=88 * H * 2, W8=256 * H, W4=256 * H // 2, shift4=256, group_width=3, group_row=12)
+    for i, name in enumerate(sizes):
+        setattr(mix, name, (2 + i) << 32)
+    mix.rows16, mix.rows8, mix.rows4 = 88, 256, 256
+    a.t_dtype, a.w_scale, a.wmix, a.table = 4, 1 << 24, ctypes.addressof(mix), None
+    for name, size in sizes.items():
+        kept = getattr(mix, name)
+        step = {"W16": 2, "group_row": 4}.get(name, 1)
+        for at, status in ((out, 1), (last - step, 1), (out - size + step, 1), (last, 0), (out - size, 0)):
+            setattr(mix, name, at)
+            if status or not torch.cuda.is_available():
+                assert (lib.hola_embed(ctypes.byref(a), None) == 1) == bool(status), (name, at)
+        setattr(mix, name, kept)

@@ -357,7 +357,7 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
     for (int j = 0; j < i; ++j)
       if (share(out[j], out[i])) return HOLA_ERR_INVALID_ARG;
   }
-  const long long blank = (static_cast<long long>(a->V) + p.blank - 1) / p.blank;
+  const long long blank = by_rows || a->accumulate ? 0 : (static_cast<long long>(a->V) + p.blank - 1) / p.blank;       // (CTAs that write zeros)
   const long long ctas = p.few ? blank + kEfPerSm * kEgPlanSms : ((a->N + p.window - 1) / p.window + 1 + blank) * p.slices;
   if (ctas > INT32_MAX) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (!device_facts()) return HOLA_ERR_NO_DEVICE;

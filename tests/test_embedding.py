@@ -824,3 +824,17 @@ def test_results_on_scales_codes_and_their_tables_are_refused():
             if status or not torch.cuda.is_available():
                 assert (lib.hola_embed(ctypes.byref(a), None) == 1) == bool(status), (name, at)
         setattr(mix, name, kept)
+
+
+def test_large_vocabularies_by_rows_and_added_to_are_not_refused_for_zeros_that_nobody_writes():
+    lib = binding.load_library()
+    a = binding.hola_embed_grad_args()
+    N, V, H = 600, 2 ** 30, 2 ** 18
+    a.N, a.V, a.H, a.grad_stride, a.out_stride, a.workspace_bytes = N, V, H, 0, H, lib.hola_embed_grad_workspace_bytes(N, V, H)
+    a.tokens, a.grad, a.out, a.workspace = 1 << 16, 1 << 20, 1 << 56, 1 << 40
+    assert lib.hola_embed_grad(ctypes.byref(a), None) == 2    # (the whole table: 2^24 x 256 CTAs of zeros and more)
+    if not torch.cuda.is_available():                         # (no device here: nothing runs)
+        a.accumulate = 1
+        assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1, 2)
+        a.accumulate, a.ids_out, a.count_out = 0, 1 << 17, 1 << 18
+        assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1, 2)

@@ -876,6 +876,8 @@ def _embed_grad(what, tokens, grad, V, scale, v_offset, V_global, status, stream
     if status is not None:
         a.status_word = _same(what, status, torch.int32, (1,), dev, "status")
     a.workspace_bytes = lib.hola_embed_grad_workspace_bytes(N, V, H)
+    if a.workspace_bytes == 0:
+        raise HolaError(f"{what}: at most 2^25 tokens and 2^30 rows")
     out = _make_on(stream, dev, lambda: fill(a, dev, N, H))
     workspace, = _make_on(stream, dev, lambda: (torch.empty(a.workspace_bytes, dtype=torch.uint8, device=dev),))
     a.workspace = workspace.data_ptr()

@@ -597,6 +597,9 @@ PyObject* embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (a.grad_stride < 0 || a.out_dtype < 0 || a.out_dtype > HOLA_T_F16 || a.v_offset < 0 || a.V_global < 0 ||
       (a.V_global ? static_cast<int64_t>(a.v_offset) + a.V > a.V_global : a.v_offset != 0) || !in.perhaps(v[13], at::kInt, {1}, &a.status_word))
     Py_RETURN_NONE;
+  // (sizes that are not served are refused before anything is made for them)
+  a.workspace_bytes = reinterpret_cast<WorkspaceFn>(size_fn)(a.N, a.V, a.H);
+  if (a.workspace_bytes == 0) Py_RETURN_NONE;
   at::Tensor out, ids, count, workspace;
   const bool given = v[11] != Py_None;
   if (given) {
@@ -619,7 +622,6 @@ PyObject* embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
         count = at::empty({1}, on.dtype(at::kInt)); a.count_out = static_cast<int32_t*>(count.data_ptr());
       }
     }
-    a.workspace_bytes = reinterpret_cast<WorkspaceFn>(size_fn)(a.N, a.V, a.H);
     workspace = at::empty({static_cast<int64_t>(a.workspace_bytes)}, on.dtype(at::kByte));
     a.workspace = workspace.data_ptr();
     s = reinterpret_cast<GradFn>(fn)(&a, stream);

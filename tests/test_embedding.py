@@ -838,3 +838,19 @@ def test_large_vocabularies_by_rows_and_added_to_are_not_refused_for_zeros_that_
         assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1, 2)
         a.accumulate, a.ids_out, a.count_out = 0, 1 << 17, 1 << 18
         assert lib.hola_embed_grad(ctypes.byref(a), None) not in (0, 1, 2)
+
+
+@gpu
+def test_sizes_that_are_not_served_are_refused_before_anything_is_made(monkeypatch):
+    """2^30 + 1 rows of the whole table would be more memory than there is."""
+    t, grad = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros((4, 4096), device="cuda")
+    many = torch.zeros(2 ** 25 + 1, dtype=torch.int32, device="cuda")
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    for _ in range(2):                                        # through the native helper and without it
+        for call in (lambda: binding.hola_embed_grad(t, grad, 2 ** 30 + 1), lambda: binding.hola_embed_grad_rows(t, grad, 2 ** 30 + 1),
+                     lambda: binding.hola_embed_grad_rows(many, grad[:1, :8].expand(2 ** 25 + 1, 8), 100)):
+            with pytest.raises(binding.HolaError, match="at most"):
+                call()
+        monkeypatch.setattr(binding, "_host", None)
+    assert torch.cuda.max_memory_allocated() == before

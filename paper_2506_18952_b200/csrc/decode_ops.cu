@@ -16,6 +16,7 @@
 #include <cooperative_groups.h>
 
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 #include <type_traits>
 
@@ -29,6 +30,13 @@ namespace {
 #include "logit_rows.cuh"
 #include "beams.cuh"
 #include "embedding.cuh"
+
+// Whether any of these lies on no address of 32-bit words.
+bool off_words(std::initializer_list<const void*> of) {
+  uintptr_t all = 0;
+  for (const void* x : of) all |= reinterpret_cast<uintptr_t>(x);
+  return all % 4 != 0;
+}
 
 // ------------------------------------------------------------------------------------------------ bytes that operands share
 // Bytes of an operand: runs that start at every index of some axes, by falling stride.
@@ -133,7 +141,8 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   if (a->B == 0) return HOLA_OK;
   if (!a->logits || !a->logZ || !a->score || !a->score_out || !a->parent || !a->token) return HOLA_ERR_INVALID_ARG;
   const int entry = a->l_dtype == HOLA_L_F32 ? 4 : 2;
-  if (reinterpret_cast<uintptr_t>(a->logits) % entry) return HOLA_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(a->logits) % entry || off_words({a->logZ, a->score, a->weight, a->score_out, a->parent, a->token, a->status_word}))
+    return HOLA_ERR_INVALID_ARG;
   // A sequence is written when all of it has been read; another one's beams may lie where its candidates go, but for the same layout.
   const long long beams = static_cast<long long>(a->B) * a->W, kept = static_cast<long long>(a->B) * a->n;
   const struct { const void* at; int bytes; } in[] = {{a->score, 4}, {a->logZ, 4}, {a->weight, 4}, {a->finished, 1}},
@@ -177,7 +186,7 @@ static hola_status look_at_states(const hola_reorder_args* a, bool call, int* in
   if (!a || a->B < 0 || a->W <= 0 || a->n <= 0 || a->count < 0 || (call && a->parent_stride < 0)) return HOLA_ERR_INVALID_ARG;
   if (a->W > kBsMaxBeams || a->n > kBsMaxBeams) return HOLA_ERR_UNSUPPORTED_SHAPE;
   if (a->B == 0 || a->count == 0) return HOLA_OK;
-  if (!a->states || (call && !a->parent)) return HOLA_ERR_INVALID_ARG;
+  if (!a->states || (call && (!a->parent || off_words({a->parent, a->used, a->status_word})))) return HOLA_ERR_INVALID_ARG;
   const Bytes parent(call ? a->parent : nullptr, a->n * 4ll, {{a->B, a->parent_stride * 4}}), used(call ? a->used : nullptr, a->B * 4ll);
   for (int i = 0; i < a->count; ++i) {
     const hola_beam_state& s = a->states[i];
@@ -283,7 +292,8 @@ hola_status hola_embed(const hola_embed_args* a, void* cuda_stream) {
   if ((mixed || a->t_dtype == HOLA_T_INT8) != (a->w_scale != nullptr)) return HOLA_ERR_INVALID_ARG;
   const int te = mixed ? 1 : tab_bytes(a->t_dtype), oe = tab_bytes(a->out_dtype);
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->out) % oe ||
-      reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te))
+      reinterpret_cast<uintptr_t>(a->add) % oe || (!mixed && reinterpret_cast<uintptr_t>(a->table) % te) || off_words({a->w_scale, a->status_word}) ||
+      (mixed && (reinterpret_cast<uintptr_t>(a->wmix->W16) % 2 || off_words({a->wmix->group_row}))))
     return HOLA_ERR_INVALID_ARG;
   const Bytes out(a->out, static_cast<long long>(a->H) * oe, {{a->N, a->out_stride * oe}});
   const bool itself = a->add == a->out && (a->N == 1 || a->add_stride == a->out_stride);
@@ -344,7 +354,7 @@ hola_status hola_embed_grad(const hola_embed_grad_args* a, void* cuda_stream) {
   if ((by_rows ? a->N : static_cast<long long>(a->V)) > 1 && a->out_stride < a->H) return HOLA_ERR_INVALID_ARG;
   const int ge = tab_bytes(a->g_dtype), oe = tab_bytes(a->out_dtype);
   if (reinterpret_cast<uintptr_t>(a->tokens) % (a->wide_tokens ? 8 : 4) || reinterpret_cast<uintptr_t>(a->grad) % ge ||
-      reinterpret_cast<uintptr_t>(a->out) % oe)
+      reinterpret_cast<uintptr_t>(a->out) % oe || off_words({a->ids_out, a->count_out, a->status_word}))
     return HOLA_ERR_INVALID_ARG;
   // (CTAs read tokens and rows while others write results, and the sort's lists lie in the workspace)
   const long long rows = by_rows ? a->N : a->V, width = a->H;

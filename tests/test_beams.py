@@ -783,3 +783,23 @@ def test_results_of_a_call_with_ends_filled_again_without():
         binding.hola_beam_select(l, z, s, keep_slots=keep, out=out)
         same(out, reference(l, z, s, 4, keep_slots=keep))
         assert not out.finished.any()
+
+
+def test_operands_on_no_address_of_their_type_are_refused():
+    lib = binding.load_library()
+    ok = dict(finished=1 << 20, finished_out=1 << 21, weight=1 << 22, status_word=1 << 23, end_token=3)
+    for name in ("logZ", "score", "weight", "score_out", "parent", "token", "status_word"):
+        for off in (1, 2, 3):
+            a = _args(**ok)
+            setattr(a, name, getattr(a, name) + off)
+            assert lib.hola_beam_select(ctypes.byref(a), None) == 1, (name, off)
+    s = (binding.hola_beam_state * 1)(_state())
+    for name in ("parent", "used", "status_word"):
+        for off in (0, 1, 2, 3):
+            a = binding.hola_reorder_args()
+            a.B, a.W, a.n, a.count, a.states, a.parent, a.parent_stride, a.used, a.status_word = 2, 4, 4, 1, ctypes.addressof(s), 1 << 20, 4, 1 << 21, 1 << 22
+            setattr(a, name, getattr(a, name) + off)
+            if off or not torch.cuda.is_available():          # (no device here: nothing runs)
+                assert (lib.hola_beam_reorder(ctypes.byref(a), None) == 1) == (off > 0), (name, off)
+    if not torch.cuda.is_available():                         # flags of one byte and logits lie anywhere
+        assert lib.hola_beam_select(ctypes.byref(_args(**{**ok, "finished": (1 << 20) + 1, "finished_out": (1 << 21) + 3})), None) not in (0, 1)

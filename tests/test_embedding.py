@@ -854,3 +854,23 @@ def test_sizes_that_are_not_served_are_refused_before_anything_is_made(monkeypat
                 call()
         monkeypatch.setattr(binding, "_host", None)
     assert torch.cuda.max_memory_allocated() == before
+
+
+def test_operands_on_no_address_of_their_type_are_refused():
+    lib = binding.load_library()
+    a = _embed_args(t_dtype=3, w_scale=1 << 24, out=1 << 28, status_word=1 << 29)
+    mix = binding.hola_wmix()
+    mix.W16, mix.group_width, mix.group_row, mix.rows16 = 1 << 32, 1 << 33, 1 << 34, 10
+    b = _embed_args(t_dtype=4, H=128, out_stride=128, out=1 << 28, w_scale=1 << 24, wmix=ctypes.addressof(mix))
+    g = binding.hola_embed_grad_args()
+    g.N, g.V, g.H, g.grad_stride, g.out_stride, g.workspace_bytes = 4, 10, 16, 16, 16, 256
+    g.tokens, g.grad, g.out, g.workspace, g.ids_out, g.count_out, g.status_word = (1 << (16 + i) for i in range(7))
+    for call, args, of, name in ((lib.hola_embed, a, a, "w_scale"), (lib.hola_embed, a, a, "status_word"), (lib.hola_embed, b, b, "w_scale"),
+                                 (lib.hola_embed, b, mix, "W16"), (lib.hola_embed, b, mix, "group_row"), (lib.hola_embed_grad, g, g, "ids_out"),
+                                 (lib.hola_embed_grad, g, g, "count_out"), (lib.hola_embed_grad, g, g, "status_word")):
+        kept = getattr(of, name)
+        for off in (0, 1, 3) if name == "W16" else (0, 1, 2, 3):
+            setattr(of, name, kept + off)
+            if off or not torch.cuda.is_available():          # (no device here: nothing runs)
+                assert (call(ctypes.byref(args), None) == 1) == (off > 0), (name, off)
+        setattr(of, name, kept)

@@ -874,3 +874,218 @@ def test_operands_on_no_address_of_their_type_are_refused():
             if off or not torch.cuda.is_available():          # (no device here: nothing runs)
                 assert (call(ctypes.byref(args), None) == 1) == (off > 0), (name, off)
         setattr(of, name, kept)
+
+
+# ------------------------------------------------------------------------------------------------ one launch and two
+# Up to 512 tokens are served by one kernel, more by a sort (of 16 warps, of more from 1025 tokens on, with wide counters from 65536) and the
+# sums behind it: what every call is promised, on all sides of these borders.
+BOTH = [300, 513, 1025, 66000]
+
+
+def spread_over(t, N, seed):
+    """The tokens of `t`, each at some places of N, in some order; -1 elsewhere."""
+    g = torch.Generator().manual_seed(seed)
+    out = torch.full((N,), -1, dtype=torch.int64)
+    at = torch.randperm(N, generator=g)
+    times = max(1, N // (2 * t.numel()))
+    out[at[:t.numel() * times]] = t.cpu().long().repeat(times)
+    return out.cuda()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+@pytest.mark.parametrize("N", BOTH)
+def test_gradients_of_parts_of_a_vocabulary(N, dtype):
+    V, H, cuts = 1000, 72, [0, 130, 131, 600, 1000]
+    tokens, grad = some_tokens(N, V, 4, dtype), rnd((N, H), torch.float32, 5)
+    dense = binding.hola_embed_grad(tokens, grad, V, 3.0)
+    check_grad(tokens, grad, V, 3.0, dense)
+    status, ids = torch.zeros(1, dtype=torch.int32, device="cuda"), []
+    for a, b in zip(cuts, cuts[1:]):
+        for whole in (V, 2 ** 31 - 1):                        # (the same part of a larger vocabulary)
+            assert torch.equal(binding.hola_embed_grad(tokens, grad, b - a, 3.0, v_offset=a, V_global=whole, status=status), dense[a:b])
+            rows = binding.hola_embed_grad_rows(tokens, grad, b - a, 3.0, v_offset=a, V_global=whole, status=status)
+            n = rows.count.item()
+            assert torch.equal(rows.rows[:n], dense[rows.ids[:n].long()])
+        ids += rows.ids[:n].tolist()
+    assert status.item() == 0 and ids == sorted(set(tokens.tolist()) - {-1})
+    # the last part of the largest vocabulary: ids up to 2^31 - 2
+    shift = 2 ** 31 - 1 - V
+    far = torch.where(tokens >= 0, tokens + shift, -1)
+    assert torch.equal(binding.hola_embed_grad(far, grad, V, 3.0, v_offset=shift, V_global=2 ** 31 - 1, status=status), dense)
+    rows = binding.hola_embed_grad_rows(far, grad, V, 3.0, v_offset=shift, V_global=2 ** 31 - 1, status=status)
+    n = rows.count.item()
+    assert rows.ids[:n].tolist() == [v + shift for v in ids] and torch.equal(rows.rows[:n], dense[(rows.ids[:n] - shift).long()])
+    assert status.item() == 0
+    binding.hola_embed_grad(tokens, grad, 130, v_offset=0, V_global=999, status=status)
+    assert status.item() == (binding.FLAG_BAD_TOKEN if bool((tokens == 999).any()) else 0)
+
+
+@gpu
+@pytest.mark.parametrize("N", BOTH)
+def test_gradients_of_tokens_that_there_are_not(N):
+    V, H = 50, 40
+    some = torch.tensor([0, 49, 50, -2, 2 ** 31 - 1, -2 ** 31, 7])
+    big = torch.tensor([2 ** 32, 2 ** 32 + 3, 2 ** 40 - 1, -2 ** 32 + 5, 2 ** 63 - 1, -2 ** 63, 2 ** 32 - 1])          # not 0, 3, -1, 5, -1, 0, -1 cut off
+    for t in (some.int(), some, big):
+        tokens = spread_over(t, N, 1).to(t.dtype)
+        grad = rnd((N, H), torch.float32, 2)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        got = binding.hola_embed_grad(tokens, grad, V, status=status)
+        assert status.item() == binding.FLAG_BAD_TOKEN
+        check_grad(tokens, grad, V, 1.0, got)
+        assert set(got.count_nonzero(dim=1).nonzero()[:, 0].tolist()) == ({0, 7, 49} if t is not big else set())
+        rows = binding.hola_embed_grad_rows(tokens, grad, V)
+        assert rows.ids[:rows.count.item()].tolist() == ([0, 7, 49] if t is not big else [])
+        status.zero_()
+        fine = torch.where((tokens >= 0) & (tokens < V), tokens, -1)
+        assert torch.equal(binding.hola_embed_grad(fine, grad, V, status=status), got) and status.item() == 0
+
+
+@gpu
+@pytest.mark.parametrize("N", BOTH)
+def test_gradients_of_vocabularies_of_any_size(N):
+    """Whole numbers: exact sums.  (Where the marks of the sort's ranges coincide.)"""
+    for V in (1, 2, 3, 73, 74, 75, 147, 148, 149, 1536 * 148, 1536 * 148 + 1, 3000001):
+        few = torch.tensor(sorted({0, V - 1, V // 2, max(0, V - 2), min(1, V - 1), V // 3}))
+        t = spread_over(few, N, V)
+        grad = torch.randint(-8, 9, (N, 8), device="cuda", generator=torch.Generator(device="cuda").manual_seed(4)).float()
+        rows = binding.hola_embed_grad_rows(t, grad, V)
+        n = rows.count.item()
+        assert rows.ids[:n].tolist() == few.tolist()
+        for i, v in enumerate(few.tolist()):
+            assert torch.equal(rows.rows[i], grad[t == v].double().sum(dim=0).float())
+        if V < 10 ** 6:
+            assert torch.equal(binding.hola_embed_grad(t, grad, V)[few.cuda()], rows.rows[:n])
+
+
+@gpu
+@pytest.mark.parametrize("N", BOTH)
+def test_strides_of_gradients_of_few_and_of_many_tokens(N):
+    """Rows further apart, on any address, one row for all; results in a part of a wider buffer."""
+    V = 30
+    t = some_tokens(N, V, 1)
+    for H in (8, 9, 256, 264) if N > 2000 else (8, 9, 264, 1024):
+        wide = rnd((N, H + 8), torch.bfloat16, 2)
+        for grad in (wide[:, :H], wide[:, 1:H + 1], wide[:1, :H].expand(N, H), wide[:1, 3:H + 3].expand(N, H)):
+            got = binding.hola_embed_grad(t, grad, V)
+            check_grad(t, grad, V, 1.0, got)
+            for lead in (0, 1):
+                out = torch.full((V, H + 3), 7.0, device="cuda")
+                binding.hola_embed_grad(t, grad, V, out=out[:, lead:lead + H])
+                assert torch.equal(out[:, lead:lead + H], got)
+                out[:, lead:lead + H] = 7.0
+                assert (out == 7.0).all()
+            rows = binding.hola_embed_grad_rows(t, grad, V)
+            n = rows.count.item()
+            assert torch.equal(rows.rows[:n], got[rows.ids[:n].long()])
+
+
+@gpu
+@pytest.mark.parametrize("N", [300, 600])
+def test_gradients_beyond_32_bits(N):
+    """Rows that begin more than 2^32 bytes into a gradient, and into its result."""
+    V, H = 300001, 8192
+    buf = torch.empty((V, H), dtype=torch.bfloat16, device="cuda")
+    grad = torch.as_strided(buf, (N, H), (300000 // N * H, 1))
+    grad.copy_(rnd((N, H), torch.bfloat16, 2))
+    t = torch.full((N,), -1, dtype=torch.int64, device="cuda")
+    at = torch.tensor([0, N - 1, N // 2, N - 2, 5], device="cuda")
+    t[at] = torch.tensor([V - 1, 0, 262144, 131072, V // 2], device="cuda")
+    rows = binding.hola_embed_grad_rows(t, grad, V)
+    order = torch.argsort(t[at])
+    assert rows.count.item() == 5 and torch.equal(rows.ids[:5].long(), t[at][order]) and torch.equal(rows.rows[:5], grad[at][order].float())
+    out = binding.hola_embed_grad(t, grad, V, dtype=torch.bfloat16)
+    assert torch.equal(out[t[at]], grad[at]) and int(out.count_nonzero()) == int(grad[at].count_nonzero())
+
+
+@gpu
+@pytest.mark.parametrize("N", BOTH)
+def test_gradients_of_absent_tokens_and_of_rows_that_are_not_finite(N):
+    V, H = 90, 64
+    t = some_tokens(N, V, 1, absent=0.3)
+    grad = rnd((N, H), torch.float32, 2)
+    want = binding.hola_embed_grad(t, grad, V)
+    dirty = grad.clone()
+    dirty[t < 0] = math.nan
+    assert torch.equal(binding.hola_embed_grad(t, dirty, V), want)
+    one = int(t[t >= 0][7])
+    dirty[t == one] = math.inf
+    got = binding.hola_embed_grad(t, dirty, V)
+    assert (got[one] == math.inf).all()
+    got[one] = want[one]
+    assert torch.equal(got, want)
+
+
+@gpu
+@pytest.mark.parametrize("N", BOTH)
+def test_gradients_through_the_native_helper_and_without_it(N, monkeypatch):
+    V, H = 300, 128
+    t, g = some_tokens(N, V, 1), rnd((N, H), torch.float16, 4)
+
+    def run():
+        got = [binding.hola_embed_grad(t, g, V, 2.0), binding.hola_embed_grad(t.long(), g, V, dtype=torch.bfloat16),
+               binding.hola_embed_grad(t, g, 100, v_offset=200, V_global=V)]
+        for rows in (binding.hola_embed_grad_rows(t, g, V), binding.hola_embed_grad_rows(t, g, 50, v_offset=10, V_global=V, dtype=torch.float16)):
+            n = rows.count.item()
+            got += [rows.ids[:n], rows.rows[:n]]
+        return got
+
+    assert binding._host is not None
+    with_it = run()
+    monkeypatch.setattr(binding, "_host", None)
+    assert all(x.dtype == y.dtype and torch.equal(x, y) for x, y in zip(with_it, run(), strict=True))
+
+
+@gpu
+@pytest.mark.parametrize("N", BOTH)
+def test_captured_gradients_two_at_once(N):
+    """Two graphs of a lookup and both forms of its gradient, replayed by turns, together and with other inputs."""
+    V, H = 700, 256
+    tokens, grads = [some_tokens(N, V, i) for i in (1, 2)], [rnd((N, H), torch.bfloat16, i) for i in (3, 4)]
+    table = rnd((V, H), torch.bfloat16, 5)
+    want = [(binding.hola_embed(t, table), binding.hola_embed_grad(t, g, V), binding.hola_embed_grad_rows(t, g, V)) for t, g in zip(tokens, grads)]
+    graphs = []
+    for i in (0, 1):
+        t, g = tokens[i].clone(), grads[i].clone()
+        out = [torch.zeros((N, H), dtype=torch.bfloat16, device="cuda"), torch.zeros((V, H), device="cuda"),
+               binding.TokenRows(torch.zeros_like(want[i][2].ids), torch.zeros((N, H), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"))]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            binding.hola_embed(t, table, out=out[0])
+            binding.hola_embed_grad(t, g, V, out=out[1])
+            binding.hola_embed_grad_rows(t, g, V, out=out[2])
+        graphs.append((graph, t, g, out))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for swap in (0, 1, 0):
+        for i, (_, t, g, _) in enumerate(graphs):
+            t.copy_(tokens[i ^ swap])
+            g.copy_(grads[i ^ swap])
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for (graph, *_), s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for i, (*_, out) in enumerate(graphs):
+            e, d, r = want[i ^ swap]
+            n = r.count.item()
+            assert torch.equal(out[0], e) and torch.equal(out[1], d) and out[2].count.item() == n
+            assert torch.equal(out[2].ids[:n], r.ids[:n]) and torch.equal(out[2].rows[:n], r.rows[:n])
+
+
+@gpu
+@pytest.mark.parametrize("N", [700, 1500])
+def test_gradient_of_many_tokens_against_differences(N):
+    """As test_gradient_against_differences, where a sort comes first; the same bounds."""
+    H, V, scale, h = 25, 60, 1.5, 2.0 ** -8
+    t, W, D = some_tokens(N, V, 1), rnd((V, H), torch.float32, 2), rnd((V, H), torch.float32, 3)
+    r = rnd((N, H), torch.float64, 4)
+    f = lambda w: float((r * torch.sin(binding.hola_embed(t, w.float(), scale).double())).sum())          # noqa: E731
+    g = (r * torch.cos(binding.hola_embed(t, W, scale).double())).float()
+    got = float((binding.hola_embed_grad(t, g, V, scale).double() * D.double()).sum())
+    want = (f(W.double() + h * D.double()) - f(W.double() - h * D.double())) / (2 * h)
+    d = scale * D[t.long().clamp_min(0)].double().abs() * (t >= 0)[:, None]
+    w = scale * W[t.long().clamp_min(0)].double().abs()
+    tol = h * h / 6 * (r.abs() * d ** 3).sum() + 2 * 2.0 ** -24 / h * (r.abs() * (w + h * d)).sum() + 2.0 ** -24 * (N + 3) * (r.abs() * d).sum()
+    assert abs(got - want) <= float(tol)

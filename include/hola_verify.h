@@ -352,13 +352,14 @@ hola_status hola_token_logprobs(const hola_logprobs_args* args, void* cuda_strea
  * its k + 1 positions leaves the logits and logZ that are read here).  For beam w of a sequence and token v
  *   c(w, v) = (score[w] - logZ[w]) + l[w][v],   key = c * weight[w],   both evaluated in 64 bits,
  * and the first n candidates in the order (key descending, beam ascending, logit descending, id ascending) are written: c rounded to
- * fp32, w, v.  An ended beam (finished[w] != 0) has one candidate, end_token with c = score[w]; its logits are not read.  A score of
- * -inf is no beam, an entry of -inf no candidate.  Where fewer than n candidates are left: score -inf, parent and token -1.  A row
- * that holds NaN or +inf, a score or logZ that is NaN or +inf, or a weight that is not positive and finite: that beam has no
- * candidates, and HOLA_FLAG_BAD_LOGIT is set. keep_slots (n = W): instead of by rank, the best child of a beam is written at that
- * beam's own place, so that its state need not move; the other candidates take the free places in their order. finished_out: 1 where
- * the parent had ended or the token is end_token. Outputs may not overlap inputs nor one another, but with n = W score_out may be score
- * itself, and finished_out finished. Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing,
+ * fp32, w, v.  An ended beam (finished[w] != 0) has one candidate, end_token with c = score[w]; its logits and logZ are not read.  A score
+ * of -inf is no beam, whatever else it has; an entry of -inf is no candidate, and a logZ of -inf a row without any.  Where fewer than n
+ * candidates are left: score -inf, parent and token -1.  A row that holds NaN or +inf, a score or logZ that is NaN or +inf, or a weight
+ * that is not positive and finite: that beam has no candidates, and HOLA_FLAG_BAD_LOGIT is set.  keep_slots (n = W): instead of by rank,
+ * the best child of a beam is written at that beam's own place, so that its state need not move; the other candidates take the free
+ * places in their order.  finished_out: 1 where the parent had ended or the token is end_token.  Outputs may not overlap inputs nor one
+ * another, but with n = W score_out may be score
+ * itself, and finished_out finished.  Every pointer is a DEVICE pointer of the current device.  Asynchronous on cuda_stream, allocates nothing,
  * needs no context, and launched like hola_verify (programmatic stream serialization, waits before it reads). */
 #define HOLA_MAX_BEAMS 32
 typedef struct hola_beam_args {

@@ -165,7 +165,8 @@ __global__ void __launch_bounds__(kBsThreads, 2) beam_select_kernel(const BsPara
     if (p.weight) weight = p.weight[at];
     if (!ended) logZ = p.logZ[at];
   }
-  const bool bad_beam = !(score < CUDART_INF_F) || !(logZ < CUDART_INF_F) || !(weight > 0.f && weight < CUDART_INF_F);
+  // (of what is no beam nothing but the score counts)
+  const bool bad_beam = score != -CUDART_INF_F && (!(score < CUDART_INF_F) || !(logZ < CUDART_INF_F) || !(weight > 0.f && weight < CUDART_INF_F));
   const bool there = !bad_beam && score != -CUDART_INF_F, reads = there && !ended && logZ != -CUDART_INF_F;
   if (__any_sync(0xffffffffu, bad_beam)) flags |= HOLA_FLAG_BAD_LOGIT;
   const unsigned ended_mask = __ballot_sync(0xffffffffu, there && ended);

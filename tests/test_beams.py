@@ -803,3 +803,23 @@ def test_operands_on_no_address_of_their_type_are_refused():
                 assert (lib.hola_beam_reorder(ctypes.byref(a), None) == 1) == (off > 0), (name, off)
     if not torch.cuda.is_available():                         # flags of one byte and logits lie anywhere
         assert lib.hola_beam_select(ctypes.byref(_args(**{**ok, "finished": (1 << 20) + 1, "finished_out": (1 << 21) + 3})), None) not in (0, 1)
+
+
+@gpu
+@pytest.mark.parametrize("V", [30, 9000])
+def test_what_is_no_beam_is_not_reported(V):
+    """A score of -inf beside a logZ, a weight and logits that are nothing; rows without entries beside others."""
+    W, n = 4, 6
+    l, z, s = make(6, W, V, torch.float32, 12)
+    w = torch.rand((6, W), device="cuda") + 0.5
+    s[:, 2] = -math.inf
+    l[:, 2] = math.nan
+    for b, x in enumerate((math.nan, math.inf, -math.inf, 0.0)):
+        z[b, 2] = x
+        w[b, 2] = (math.nan, -1.0, 0.0, math.inf)[b]
+    l[4, 1], z[4, 1] = -math.inf, -math.inf
+    s[5], z[5], w[5] = -math.inf, math.nan, math.nan
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for weight in (None, w):
+        same(binding.hola_beam_select(l, z, s, n, weight=weight, status=status), reference(l, z, s, n, weight=weight))
+        assert status.item() == 0

@@ -92,6 +92,12 @@ bool share(const Bytes& a, const Bytes& b) {
   return meet(a, 0, b, 0, d, &looks);
 }
 
+// The same of operands without axes.
+inline bool share(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
+}
+
 // Whether two indices of a's axes from i on have a byte in common.
 bool shares_with_itself(const Bytes& a) {
   int looks = 0;
@@ -150,14 +156,14 @@ hola_status hola_beam_select(const hola_beam_args* a, void* cuda_stream) {
   for (const auto& x : in)
     for (const auto& y : out) {
       const bool itself = a->n == a->W && x.at == y.at && ((x.at == a->score && y.at == a->score_out) || (x.at == a->finished && y.at == a->finished_out));
-      if (!itself && share({x.at, beams * x.bytes}, {y.at, kept * y.bytes})) return HOLA_ERR_INVALID_ARG;
+      if (!itself && share(x.at, beams * x.bytes, y.at, kept * y.bytes)) return HOLA_ERR_INVALID_ARG;
     }
   const Bytes rows(a->logits, static_cast<long long>(a->V) * entry, {{a->B, a->seq_stride * entry}, {a->W, a->beam_stride * entry}});
   for (int i = 0; i < 4; ++i)
     if (share({out[i].at, kept * out[i].bytes}, rows)) return HOLA_ERR_INVALID_ARG;
   for (int i = 0; i < 4; ++i)
     for (int j = 0; j < i; ++j)
-      if (share({out[i].at, kept * out[i].bytes}, {out[j].at, kept * out[j].bytes})) return HOLA_ERR_INVALID_ARG;
+      if (share(out[i].at, kept * out[i].bytes, out[j].at, kept * out[j].bytes)) return HOLA_ERR_INVALID_ARG;
   const DeviceFacts* dev = device_facts();
   if (!dev) return HOLA_ERR_NO_DEVICE;
   BsParams p = {};

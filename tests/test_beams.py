@@ -823,3 +823,22 @@ def test_what_is_no_beam_is_not_reported(V):
     for weight in (None, w):
         same(binding.hola_beam_select(l, z, s, n, weight=weight, status=status), reference(l, z, s, n, weight=weight))
         assert status.item() == 0
+
+
+@gpu
+@pytest.mark.parametrize("lead", [0, 1])
+def test_the_longest_rows(lead):
+    """2^27 entries a row: the best at its ends, some equal ones among them."""
+    W, V, n = 3, 2 ** 27, 12
+    buf = torch.full((W * V + lead,), -9.0, dtype=torch.bfloat16, device="cuda")
+    l = buf[lead:].view(1, W, V)
+    s, z = torch.tensor([[-1.0, -1.25, -1.0]], device="cuda"), torch.full((1, W), 2.0, device="cuda")
+    want = []
+    for w, marks in enumerate(({0: 3.0, V - 1: 3.0, V // 2: 1.0}, {V - 1: 4.0, V - 2: 3.25, 7: 0.5}, {V - 1: 3.0, 1: 2.0, V - 17: 2.0})):
+        for v, x in marks.items():
+            l[0, w, v] = x
+            want.append((float(s[0, w]) - 2.0 + x, w, v))
+    want.sort(key=lambda c: (-c[0], c[1], c[2]))
+    want += [(-1.0 - 2.0 - 9.0, 0, v) for v in (1, 2, 3)]
+    out = binding.hola_beam_select(l, z, s, n)
+    assert list(zip(out.score[0].tolist(), out.parent[0].tolist(), out.token[0].tolist())) == want

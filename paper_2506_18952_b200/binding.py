@@ -635,6 +635,7 @@ def hola_beam_select(logits: torch.Tensor, logZ: torch.Tensor, score: torch.Tens
 
 class BeamStates:
     """States of the beams for hola_beam_reorder, laid out once: tensors [..., B, W, ...] (token histories, keys and values, page tables).
+    (Some 20 us of host time a tensor: for tensors that stay where they are, not for each step.)
 
     axes: the axis of the sequences in each tensor (one number: in all), the beams' is the next one.  positions: for each tensor the axis that counts
     positions, of which only the first used[b] are moved, or None.  into: tensors that take the reordered states (double buffers; perhaps with
@@ -783,7 +784,8 @@ def hola_embed(tokens: torch.Tensor, table, scale: float = 1.0, add: torch.Tenso
 
     table: fp32, bf16, fp16 [V, H], int8 [V, H] with w_scale (hola_quantize_w8) or a MixedHead.  Evaluated in fp32; dtype: of the result
     (None: of out, of add, of the table, bf16 for the quantised ones).  add: the same type, [..., H]; it may be out.  v_offset, V_global: the table
-    is rows v_offset .. of a vocabulary of V_global; tokens of other parts count as none.
+    is rows v_offset .. of a vocabulary of V_global; tokens of other parts count as none.  Not recorded for autograd: the gradient of the
+    table is hola_embed_grad's or hola_embed_grad_rows', by a call of one's own.
     status: int32 [1] on the device, HOLA_FLAG_* bits are OR-ed in.  stream: see HolaVerify."""
     lib = load_library()
     what = "hola_embed"
@@ -919,7 +921,8 @@ def hola_embed_grad_rows(tokens: torch.Tensor, grad: torch.Tensor, V: int, scale
                          dtype: torch.dtype = torch.float32, v_offset: int = 0, V_global: int = 0, status: torch.Tensor | None = None,
                          stream=None) -> TokenRows:
     """The same by rows: the distinct tokens in rising order, and the gradient's row of each.  out: an earlier call's result, or buffers
-    with room for as many rows as there are tokens; what lies behind the distinct ones is left as it was."""
+    with room for as many rows as there are tokens, apart from tokens and grad and from one another; what lies behind the distinct ones
+    is left as it was."""
     what = "hola_embed_grad_rows"
     load_library()
     if stream is None and (out is None or type(out) is TokenRows):
